@@ -101,7 +101,8 @@ typedef struct {
   unsigned* n_last;      /* [H][W]: list positions walked up to the last contributor */
 } abcd_fwd_state;
 
-enum { ABCD_F16 = 0, ABCD_F32 = 1 };   /* element type of F, B and cached layers */
+/* Element types: of F, B and cached layers (the first two), of matrices over tokens (all three). */
+enum { ABCD_F16 = 0, ABCD_F32 = 1, ABCD_BF16 = 2 };
 
 /* ---- context, stream, workspace ------------------------------------------------------ */
 abcd_status abcd_create(abcd_ctx** ctx, int device, void* cuda_stream);
@@ -441,6 +442,93 @@ abcd_status abcd_assign_cells(const float* means_host, int n, const double origi
 abcd_status abcd_partition_split(const int dims[3], const double origin[3], double side,
                                  const double campos[3], int active, int* front, int* n_front,
                                  int* back, int* n_back);
+
+/* ---- a network over the block's Gaussians ---------------------------------------------- *
+ * Photographs of one scene differ in exposure and white balance, so the colours of a block's
+ * Gaussians may depend on the camera through a learned function: one token per Gaussian (its SH
+ * coefficients next to the camera's embedding) goes through residual layers
+ * x + dropout(gated_ff(layer_norm(x))), the result is rendered (abcd_project), and the gradient of
+ * the colours (abcd_backward's grads->sh) goes back through the layers.  These calls are the
+ * layers' operators, forward and backward.
+ *
+ * A matrix is row-major with consecutive columns and `stride` elements from row to row, aligned to
+ * its element type; rows may be 0 and the data of a matrix without rows NULL.  All sums (products,
+ * statistics, reductions over the rows) are held in 32 bits, results are rounded once to the type of
+ * their matrix, and every result is the same in every run (no atomic sums).  An output may not
+ * overlap an input unless a call says so.  Like every call these are asynchronous on the context's
+ * stream, and what they read must be ready there. */
+typedef struct {
+  void* data;
+  long long rows;
+  long long cols;
+  long long stride;  /* elements between rows, >= cols */
+  int dtype;         /* ABCD_F16, ABCD_F32 or ABCD_BF16 */
+} abcd_matrix;
+
+/* The gate's activation: z sigmoid(z), z Phi(z) with the normal distribution's Phi, max(z, 0). */
+enum { ABCD_SILU = 0, ABCD_GELU = 1, ABCD_RELU = 2 };
+
+/* Bytes of device scratch with which abcd_layer_norm_backward takes matrices of up to `cols`
+ * columns and, with ff > 0, the gated feed-forward calls take up to `rows` tokens of up to `cols`
+ * columns with up to `ff` hidden ones, all in type dtype.  It is separate from the renderer's
+ * workspace; dropout and the layer norm's forward pass take none. */
+abcd_status abcd_network_workspace_size(long long rows, long long cols, long long ff, int dtype,
+                                        size_t* bytes);
+/* Hands the context a caller-owned device buffer for these calls (256-byte aligned).  A call that
+ * needs more than `bytes` returns ABCD_ERR_WORKSPACE.  Nothing is kept in it from call to call
+ * that a result depends on. */
+abcd_status abcd_set_network_workspace(abcd_ctx* ctx, void* device_ptr, size_t bytes);
+
+/* Layer norm: y = (x - mean) rstd weight + bias for each row, with the row's mean and
+ * rstd = 1 / sqrt(variance + eps) (variance: the mean squared deviation).  weight, bias: [cols]
+ * of type weight_dtype (the matrices' or ABCD_F32), either may be NULL (1 and 0).  mean, rstd:
+ * [rows] fp32, both NULL or both given; the backward pass needs them.  y may be x. */
+abcd_status abcd_layer_norm(abcd_ctx* ctx, const abcd_matrix* x, const void* weight,
+                            const void* bias, int weight_dtype, float eps, const abcd_matrix* y,
+                            float* mean, float* rstd);
+/* Its backward pass: with xh = (x - mean) rstd and g = dy weight,
+ * dx = rstd (g - mean(g) - xh mean(g xh)), dweight = sum over the rows of dy xh, dbias = sum over
+ * the rows of dy.  dweight, dbias: [cols] of weight_dtype, written (zero without rows), either may
+ * be NULL; dx may be NULL, and may be dy.  d_residual (NULL for none) is added to dx: in the layer
+ * x + f(layer_norm(x)) the gradient that reaches x past f; dx may be d_residual too. */
+abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix* dy, const abcd_matrix* x,
+                                     const void* weight, int weight_dtype, const float* mean,
+                                     const float* rstd, const abcd_matrix* d_residual,
+                                     const abcd_matrix* dx, void* dweight, void* dbias);
+
+/* Gated feed-forward layer: y = (act(x w_gate^T) * (x w_up^T)) w_down^T.  x, y [rows][d];
+ * w_gate, w_up [ff][d]; w_down [d][ff]; all of one type.  gate, up [rows][ff], both NULL or both
+ * given: x w_gate^T and x w_up^T, which the backward pass reads.  The hidden matrix
+ * act(gate) * up is rounded to the matrices' type between the two products. */
+abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const abcd_matrix* w_gate,
+                          const abcd_matrix* w_up, const abcd_matrix* w_down, int activation,
+                          const abcd_matrix* y, const abcd_matrix* gate, const abcd_matrix* up);
+/* Its backward pass.  With dh = dy w_down, du = dh act(gate), dg = dh up act'(gate):
+ * dx = dg w_gate + du w_up, dw_gate = dg^T x, dw_up = du^T x, dw_down = dy^T (act(gate) * up); each
+ * may be NULL, and the weights' gradients are zero without rows.  act'(0) of ABCD_RELU is 0.  dg,
+ * du and the hidden matrix are rounded to the matrices' type between the products. */
+abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* dy, const abcd_matrix* x,
+                                   const abcd_matrix* w_gate, const abcd_matrix* w_up,
+                                   const abcd_matrix* w_down, int activation,
+                                   const abcd_matrix* gate, const abcd_matrix* up,
+                                   const abcd_matrix* dx, const abcd_matrix* dw_gate,
+                                   const abcd_matrix* dw_up, const abcd_matrix* dw_down);
+
+/* Dropout: y = residual + (kept ? x s : 0), residual NULL for none.  Which elements are kept comes
+ * from a counter-based generator (Philox4x32-10; Salmon et al., Parallel random numbers: as easy as
+ * 1, 2, 3, 2011), so no mask is stored and the backward pass takes the same one again: element
+ * e = row * cols + column reads the 16-bit number e % 8 (low halves first) of the four words of
+ * counter offset + e / 8 (64 bits, the upper 64 zero) under the key `seed`, and is kept where that
+ * number is at least t = floor(65536 p + 0.5); s = 65536 / (65536 - t), so the mean is exact.  p in
+ * [0, 1]; at t = 65536 nothing is kept.  A call takes the counters offset ... offset +
+ * ceil(rows * cols / 8) - 1.  y may be x or residual. */
+abcd_status abcd_dropout(abcd_ctx* ctx, const abcd_matrix* x, double p, unsigned long long seed,
+                         unsigned long long offset, const abcd_matrix* residual,
+                         const abcd_matrix* y);
+/* Its backward pass: dx = kept ? dy s : 0 (the residual's gradient is dy).  dx may be dy. */
+abcd_status abcd_dropout_backward(abcd_ctx* ctx, const abcd_matrix* dy, double p,
+                                  unsigned long long seed, unsigned long long offset,
+                                  const abcd_matrix* dx);
 
 #ifdef __cplusplus
 }

@@ -20,7 +20,8 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "abcd.h")
 
 ABCD_OK, ABCD_ERR_INVALID_ARG, ABCD_ERR_CUDA, ABCD_ERR_CAPACITY, ABCD_ERR_TIMEOUT, \
     ABCD_ERR_WORKSPACE = range(6)
-ABCD_F16, ABCD_F32 = 0, 1
+ABCD_F16, ABCD_F32, ABCD_BF16 = 0, 1, 2
+ABCD_SILU, ABCD_GELU, ABCD_RELU = 0, 1, 2
 ABCD_MAX_CACHE_SLOTS = 4096
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "CUDA", 3: "CAPACITY", 4: "TIMEOUT", 5: "WORKSPACE"}
 TILE = 16
@@ -63,6 +64,11 @@ class abcd_tiles(C.Structure):
 
 class abcd_fwd_state(C.Structure):
     _fields_ = [("A_T", C.c_void_p), ("n_last", C.c_void_p)]
+
+
+class abcd_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_longlong), ("cols", C.c_longlong),
+                ("stride", C.c_longlong), ("dtype", C.c_int)]
 
 
 class abcd_alu_peaks(C.Structure):
@@ -120,6 +126,20 @@ _SIGS = {
     "abcd_cache_sync": [C.c_void_p],
     "abcd_composite_fold_packed": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int,
                                    C.c_void_p, C.c_void_p, C.c_void_p],
+    "abcd_network_workspace_size": [C.c_longlong, C.c_longlong, C.c_longlong, C.c_int,
+                                    C.POINTER(C.c_size_t)],
+    "abcd_set_network_workspace": [C.c_void_p, C.c_void_p, C.c_size_t],
+    "abcd_layer_norm": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_float,
+                        C.c_void_p, C.c_void_p, C.c_void_p],
+    "abcd_layer_norm_backward": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                 C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                 C.c_void_p],
+    "abcd_gated_ff": [C.c_void_p] * 5 + [C.c_int] + [C.c_void_p] * 3,
+    "abcd_gated_ff_backward": [C.c_void_p] * 6 + [C.c_int] + [C.c_void_p] * 6,
+    "abcd_dropout": [C.c_void_p, C.c_void_p, C.c_double, C.c_ulonglong, C.c_ulonglong, C.c_void_p,
+                     C.c_void_p],
+    "abcd_dropout_backward": [C.c_void_p, C.c_void_p, C.c_double, C.c_ulonglong, C.c_ulonglong,
+                              C.c_void_p],
     "abcd_measure_alu_peaks": [C.c_int, C.c_void_p],
     "abcd_block_bounds": [C.c_void_p, C.c_void_p, C.c_void_p],
     "abcd_pair_visible": [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(C.c_int)],
@@ -305,6 +325,7 @@ class Context:
         self.h = h
         self.workspace = None
         self.limits = (0, 0, 0)
+        self.network_workspace, self.network_bytes = None, 0
 
     def __del__(self):
         try:
@@ -333,6 +354,29 @@ class Context:
                                             mg, mp, mx))
         self.limits = (mg, mp, mx)
 
+    def reserve_network(self, rows, cols, ff=0, dtype=None):
+        """(Re)allocates the network calls' workspace if matrices of `rows` tokens of `cols`
+        columns, with `ff` hidden ones, of torch type dtype (float32 if None) need more than it
+        has.  Call it before a CUDA graph is captured, not inside: a larger workspace replaces
+        the one that captured calls use."""
+        torch = _torch()
+        nbytes = C.c_size_t()
+        st = lib().abcd_network_workspace_size(int(rows), int(cols), int(ff),
+                                               _dtypes().get(dtype, -1) if dtype is not None else ABCD_F32,
+                                               C.byref(nbytes))
+        if st != ABCD_OK:
+            raise AbcdError(st, "abcd_network_workspace_size")
+        if nbytes.value <= self.network_bytes:
+            return
+        ws = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=self.device)
+        ws.record_stream(self.stream)
+        if self.network_workspace is not None:       # calls in flight may still use it
+            self.network_workspace.record_stream(self.stream)
+        off = (-ws.data_ptr()) % 256
+        self.check(lib().abcd_set_network_workspace(self.h, C.c_void_p(ws.data_ptr() + off),
+                                                    nbytes.value))
+        self.network_workspace, self.network_bytes = ws, nbytes.value
+
     def sync(self):
         self.check(lib().abcd_sync(self.h))
 
@@ -341,6 +385,18 @@ class Context:
 
     def launches(self):
         return int(lib().abcd_launch_count(self.h))
+
+
+_dtype_ids = {}
+
+
+def _dtypes():
+    """torch type -> ABCD_* element type."""
+    if not _dtype_ids:
+        torch = _torch()
+        _dtype_ids.update({torch.float16: ABCD_F16, torch.float32: ABCD_F32,
+                           torch.bfloat16: ABCD_BF16})
+    return _dtype_ids
 
 
 # ---------------------------------------------------------------------------------------
@@ -660,3 +716,8 @@ def visible_pairs(ctx: Context, blocks, cameras, dims, origin, side, opts=None):
         for ci, cam in enumerate(cams):
             out[ci, b] = abcd_pair_visible(cam, box, opts)
     return out
+
+
+from .network import (FeedForwardBlock, abcd_dropout, abcd_dropout_backward,  # noqa: E402,F401
+                      abcd_gated_ff, abcd_gated_ff_backward, abcd_layer_norm,
+                      abcd_layer_norm_backward)

@@ -25,7 +25,7 @@ constexpr int kVisSumCopies = 8;          // copies of the layer visibility sums
 // words of Workspace::os_ctr: [2 sorts][2] tile and finished-CTA counters of a radix pass, the run
 // placement's two, [2 calls in turn][2] the visible depth keys' range, the count kernel's finished CTAs
 constexpr int kCtrSorts = 0, kCtrPlace = 4, kCtrKeyRange = 8, kCtrTicket = 12;
-constexpr int kSmemKernels = 16;          // kernels with dynamic shared memory, at most
+constexpr int kSmemKernels = 64;          // kernels with dynamic shared memory, at most
 
 // Device status bits (OR-ed into the status word; abcd_sync reports the lowest set code).
 constexpr unsigned kStatusCapacity = 1u << ABCD_ERR_CAPACITY;
@@ -151,6 +151,8 @@ struct abcd_ctx {
   long long max_pairs = 0;
   long long max_pixels = 0;
   abcd::Workspace ws{};
+  char* net_base = nullptr;             // the network calls' own workspace
+  size_t net_bytes = 0;
   const void* order_ranges = nullptr;   // tile ranges the order in ws.tile_order belongs to
   const void* ck_state = nullptr;       // forward state the render checkpoints belong to
   const void* ck_ranges = nullptr;      // and the tile ranges and block count they were made for

@@ -1,0 +1,56 @@
+// What the network calls (layernorm.cu, gatedff.cu, dropout.cu) share: element types, checks of
+// their matrices, aligned accesses of several elements.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "abcd_internal.cuh"
+
+namespace abcd {
+
+constexpr long long kMaxNetCols = 1LL << 24;   // columns of a matrix, hidden columns
+constexpr long long kMaxNetRows = 1LL << 30;   // its rows
+
+inline size_t elem_size(int dtype) { return dtype == ABCD_F32 ? 4 : 2; }
+inline bool dtype_ok(int dtype) {
+  return dtype == ABCD_F16 || dtype == ABCD_F32 || dtype == ABCD_BF16;
+}
+inline size_t net_align(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// A matrix that a call may read or write: its type and shape within the limits, its rows apart, its
+// data there (unless it has no rows) and aligned to its type.
+inline bool matrix_ok(const abcd_matrix* m) {
+  return m && dtype_ok(m->dtype) && m->rows >= 0 && m->rows <= kMaxNetRows && m->cols >= 1 &&
+         m->cols <= kMaxNetCols && m->stride >= m->cols && m->stride <= (1LL << 31) &&
+         (m->rows == 0 || m->data) && ((uintptr_t)m->data & (elem_size(m->dtype) - 1)) == 0;
+}
+inline bool same_form(const abcd_matrix* a, const abcd_matrix* b) {
+  return a->dtype == b->dtype && a->rows == b->rows && a->cols == b->cols;
+}
+// Whether rows of the matrix start on multiples of `bytes` (a power of two).
+inline bool rows_aligned(const abcd_matrix* m, size_t bytes) {
+  return (((uintptr_t)m->data | (m->rows > 1 ? (size_t)m->stride * elem_size(m->dtype) : 0)) &
+          (bytes - 1)) == 0;
+}
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) {
+  return __float2bfloat16_rn(v);
+}
+
+// V elements of T as one aligned access.
+template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
+
+// Calls f with a value of the element type that dtype names.
+template <typename F> auto with_type(int dtype, F&& f) {
+  if (dtype == ABCD_F32) return f(float());
+  if (dtype == ABCD_F16) return f(__half());
+  return f(__nv_bfloat16());
+}
+
+}  // namespace abcd

@@ -1,0 +1,91 @@
+"""The 64-bit formulas of the network operators: gradients against central differences, the
+generator against a published vector, and the calls' refusals that need no GPU."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import paper_2608_27735_gb300 as ab
+
+from . import _network as N
+
+
+def directional(f, args, k, v, h=1e-5):
+    up, down = [a.copy() for a in args], [a.copy() for a in args]
+    up[k] += h * v
+    down[k] -= h * v
+    return (f(*up) - f(*down)) / (2 * h)
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_norm_gradient_is_the_difference_quotient(seed):
+    r = np.random.default_rng(seed)
+    x, dy = r.normal(1, 2, (5, 9)), r.normal(size=(5, 9))
+    w, b = r.normal(1, 0.3, 9), r.normal(size=9)
+    f = lambda x, w, b: float((N.norm(x, w, b, 1e-5)[0] * dy).sum())
+    _, mean, rstd = N.norm(x, w, b, 1e-5)
+    grads = N.norm_grad(dy, x, w, mean, rstd)
+    for k, (a, g) in enumerate(zip((x, w, b), grads)):
+        v = r.normal(size=a.shape)
+        # third derivatives of order one: h^2 for the quotient, 2^-53 / h for the subtraction
+        assert directional(f, (x, w, b), k, v) == pytest.approx(float((g * v).sum()), rel=1e-6, abs=1e-7)
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu", "relu"])
+def test_ff_gradient_is_the_difference_quotient(name):
+    r = np.random.default_rng(4)
+    x, dy = r.normal(size=(6, 5)), r.normal(size=(6, 5))
+    wg, wu, wd = r.normal(size=(7, 5)), r.normal(size=(7, 5)), r.normal(size=(5, 7))
+    _, z, u = N.ff(x, wg, wu, wd, name)
+    assert np.abs(z).min() > 1e-3                      # no difference crosses relu's corner
+    f = lambda *a: float((N.ff(*a, name)[0] * dy).sum())
+    for k, g in enumerate(N.ff_grad(dy, x, wg, wu, wd, name, z, u)):
+        v = r.normal(size=g.shape)
+        assert directional(f, (x, wg, wu, wd), k, v) == pytest.approx(float((g * v).sum()), rel=1e-6, abs=1e-6)
+
+
+def test_generator_against_the_published_vector():
+    """Philox4x32-10 of counter and key zero is 6627e8d5 e169c58d bc57ac4c 9b00dbd8 (known answers
+    published with the generator): the thresholds just at and above a number decide it."""
+    words = (0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8)
+    numbers = [h for w in words for h in (w & 0xFFFF, w >> 16)]
+    for j, u in enumerate(numbers):
+        assert N.kept(1, 8, u / 65536, 0, 0)[0][0, j]
+        assert not N.kept(1, 8, (u + 1) / 65536, 0, 0)[0][0, j]
+
+
+def test_calls_reject_a_null_context():
+    ab.build()
+    lib = ab.lib()
+    n = C.c_size_t()
+    assert lib.abcd_layer_norm(None, None, None, None, 1, 0.0, None, None, None) == ab.ABCD_ERR_INVALID_ARG
+    assert lib.abcd_gated_ff(None, None, None, None, None, 0, None, None, None) == ab.ABCD_ERR_INVALID_ARG
+    assert lib.abcd_dropout(None, None, 0.1, 0, 0, None, None) == ab.ABCD_ERR_INVALID_ARG
+    assert lib.abcd_set_network_workspace(None, None, 0) == ab.ABCD_ERR_INVALID_ARG
+    for bad in ((-1, 8, 8, 1), (1, 0, 8, 1), (1, 8, -1, 1), (1, 8, 8, 3), (1, 1 << 40, 8, 1)):
+        assert lib.abcd_network_workspace_size(*bad, C.byref(n)) == ab.ABCD_ERR_INVALID_ARG
+    assert lib.abcd_network_workspace_size(4, 8, 8, 1, None) == ab.ABCD_ERR_INVALID_ARG
+
+
+def test_workspace_grows_with_every_size():
+    ab.build()
+    n = C.c_size_t()
+    size = lambda *a: (ab.lib().abcd_network_workspace_size(*a, C.byref(n)), n.value)[1]
+    base = size(1000, 64, 256, ab.ABCD_F32)
+    assert size(4000, 64, 256, ab.ABCD_F32) > base < size(1000, 64, 1024, ab.ABCD_F32)
+    assert size(0, 1, 0, ab.ABCD_F16) > 0
+
+
+def test_struct_layout_matches_header(tmp_path):
+    import os
+    import subprocess
+    src, exe = tmp_path / "m.c", tmp_path / "m"
+    fields = [f for f, _ in ab.abcd_matrix._fields_]
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "abcd.h"\nint main(void){printf("%zu"'
+                   + ', sizeof(abcd_matrix));'
+                   + "".join(f'printf(" %zu", offsetof(abcd_matrix, {f}));' for f in fields)
+                   + f'printf(" %d %d %d %d", ABCD_BF16, ABCD_SILU, ABCD_GELU, ABCD_RELU);return 0;}}\n')
+    subprocess.run(["gcc", "-I", os.path.dirname(ab.HEADER), str(src), "-o", str(exe)], check=True)
+    got = [int(v) for v in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == [C.sizeof(ab.abcd_matrix)] + [getattr(ab.abcd_matrix, f).offset for f in fields] + \
+        [ab.ABCD_BF16, ab.ABCD_SILU, ab.ABCD_GELU, ab.ABCD_RELU]
