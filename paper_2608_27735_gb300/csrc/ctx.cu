@@ -6,7 +6,7 @@
 #include <cstring>
 #include <vector>
 
-#include "abcd_internal.cuh"
+#include "network.cuh"
 
 namespace abcd {
 
@@ -259,8 +259,10 @@ abcd_status abcd_set_workspace(abcd_ctx* ctx, void* ptr, size_t bytes, int max_g
 }
 
 abcd_status abcd_clear_status(abcd_ctx* ctx) {
-  if (!has_workspace(ctx)) return ABCD_ERR_WORKSPACE;
-  cudaError_t e = cudaMemsetAsync(ctx->ws.status, 0, 8, ctx->stream);
+  if (!has_workspace(ctx) && !ctx->net_base) return ABCD_ERR_WORKSPACE;
+  cudaError_t e = has_workspace(ctx) ? cudaMemsetAsync(ctx->ws.status, 0, 8, ctx->stream) : cudaSuccess;
+  // the products' status, and the counters that a product which gave up left in between
+  if (e == cudaSuccess && ctx->net_base) e = cudaMemsetAsync(ctx->net_base, 0, kNetHeader, ctx->stream);
   return e == cudaSuccess ? ABCD_OK : fail(ctx, ABCD_ERR_CUDA, "clear status: %s", cudaGetErrorString(e));
 }
 
@@ -268,9 +270,10 @@ abcd_status abcd_sync(abcd_ctx* ctx) {
   if (!ctx) return ABCD_ERR_INVALID_ARG;
   cudaError_t e = cudaStreamSynchronize(ctx->stream);
   if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "stream: %s", cudaGetErrorString(e));
-  if (!has_workspace(ctx)) return ABCD_OK;
-  unsigned word = 0;
-  e = cudaMemcpy(&word, ctx->ws.status, sizeof word, cudaMemcpyDeviceToHost);
+  unsigned word = 0, net = 0;
+  if (has_workspace(ctx)) e = cudaMemcpy(&word, ctx->ws.status, sizeof word, cudaMemcpyDeviceToHost);
+  if (e == cudaSuccess && ctx->net_base) e = cudaMemcpy(&net, ctx->net_base, sizeof net, cudaMemcpyDeviceToHost);
+  word |= net;
   if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "status read: %s", cudaGetErrorString(e));
   for (int code = 1; code < 32; ++code)
     if (word & (1u << code)) return fail(ctx, (abcd_status)code, "device reported status %d", code);

@@ -1,0 +1,532 @@
+// The matrix products of the gated feed-forward layer (gatedff.cu), one kernel template.
+//
+// C = sum over segments of A_s B_s^T with 16-bit operands and 32-bit sums, A_s [m][k], B_s [n][k].
+// Either operand may lie with k or with its other dimension contiguous.  Segments are how sums of
+// several products stay one pass: dx = dG Wg + dU Wu has two, and an operand in 32 bits is three
+// 16-bit terms v = t0 + t1 + t2 (each the rounding of what the ones before leave, 24 bits
+// together), whose product keeps the six pairs t_i u_j with i + j <= 2: what is left out is below
+// 2^-24 of the product.
+//
+// What bounds it: the tensor cores for wide layers, HBM (the hidden matrices) for narrow ones, the
+// weights' bytes for few tokens.  Layout: a persistent grid, one CTA (or pair of CTAs, which share a
+// 256 x 256 tile: each stages half of B) per SM; one warp issues the TMA loads of 128-byte swizzled
+// tiles into a ring of stages, one the tcgen05 matrix instructions, eight warps turn the sums that
+// lie in tensor memory into results while the next tile's are made in its other half.  Where the
+// tiles do not fill the SMs, k is split: each part leaves its 32-bit sums in the workspace, and the
+// warp that comes last adds the parts in their order, so that the result does not depend on who
+// that was.
+#pragma once
+
+#include "network.cuh"
+#include "tensor_core.cuh"
+
+namespace abcd {
+
+enum { kPlain, kUp, kDown };          // what becomes of the sums, see store()
+
+constexpr int kMaxSegments = 12;
+constexpr int kBlockK = 64;           // elements of k per stage: 128 bytes, the swizzle's row
+constexpr int kFfThreads = 320;       // TMA warp, MMA warp, eight epilogue warps
+constexpr int kEpilogueWarps = 8;
+constexpr size_t kStageBuffer = 4096; // bytes in which an epilogue warp turns its rows round
+
+// A result: a matrix of the call (one 32-bit or 16-bit value per element), or an operand of a later
+// product (terms planes of 16-bit values).
+struct Out {
+  void* p;
+  long long stride;                   // elements between rows
+  long long plane;                    // elements between the terms' planes (operands in 32 bits)
+  int vec;                            // rows start on 16-byte boundaries
+};
+
+struct alignas(64) ProductArgs {
+  CUtensorMap a, b[2];
+  int m, n;                           // rows of A and B (kUp: of each B)
+  int kblocks;                        // stages per segment
+  int segments;
+  unsigned char az[kMaxSegments], bsel[kMaxSegments], bz[kMaxSegments];
+  int batch_az;                       // added to az for the second batch
+  int tiles_m, tiles_n, batches, splits;
+  int dtype;
+  int act;
+  Out c[2];                           // kPlain: per batch; kUp, kDown: c[0] the hidden matrix
+  Out g[2];                           // kUp: gate and up (p NULL: not wanted); kDown: dG and dU
+  Out in[2];                          // kDown: the saved gate and up
+  float* part;                        // sums of the splits
+  unsigned* count;                    // finished splits per warp of a tile; zero between calls
+  unsigned* status;
+  unsigned limit;                     // polls of a wait
+};
+
+// SiLU in terms of the sigmoid, GELU of the error function; the slopes are their derivatives.
+__device__ __forceinline__ float sigmoid_of(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ float act_value(float z, int act) {
+  if (act == ABCD_SILU) return z * sigmoid_of(z);
+  if (act == ABCD_GELU) return z * (0.5f + 0.5f * erff(z * 0.70710678f));
+  return z > 0.f ? z : (z == z ? 0.f : z);
+}
+__device__ __forceinline__ void act_both(float z, int act, float& value, float& slope) {
+  if (act == ABCD_SILU) {
+    const float s = sigmoid_of(z);
+    value = z * s;
+    slope = s + value * (1.f - s);
+  } else if (act == ABCD_GELU) {
+    const float c = 0.5f + 0.5f * erff(z * 0.70710678f);
+    value = z * c;
+    slope = c + z * 0.39894228f * __expf(-0.5f * z * z);
+  } else {
+    value = z > 0.f ? z : (z == z ? 0.f : z);
+    slope = z > 0.f ? 1.f : 0.f;
+  }
+}
+
+__device__ __forceinline__ unsigned pack2(float a, float b, bool bf16) {
+  if (bf16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const unsigned*>(&v);
+  }
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const unsigned*>(&v);
+}
+__device__ __forceinline__ float unpack(unsigned short v, bool bf16) {
+  return bf16 ? __uint_as_float((unsigned)v << 16) : __half2float(__ushort_as_half(v));
+}
+// The next 16-bit term of v, which is left with the rest (nothing of an infinity or NaN).
+__device__ __forceinline__ float take_term(float& v) {
+  const float t = __bfloat162float(__float2bfloat16_rn(v));
+  v = fabsf(v) <= 3.4028234e38f && fabsf(t) <= 3.4028234e38f ? v - t : 0.f;
+  return t;
+}
+
+// A warp's 32 rows x CW columns, lane l holding row l as words of 16-bit pairs (or 32-bit values):
+// turned round in the warp's buffer, so that consecutive lanes write consecutive 16 bytes of a row.
+// The buffer's 16-byte pieces are swapped by row so that neither side meets bank conflicts.
+template <int WORDS>
+__device__ __forceinline__ void store_words(const unsigned (&w)[WORDS], char* buf, void* base,
+                                            long long stride_bytes, int rows, int bytes, bool vec, int elem) {
+  constexpr int PIECES = WORDS / 4;                 // 16-byte pieces of a row
+  constexpr int ROWS = 32 / PIECES;                 // rows that the lanes take at a time
+  const int lane = threadIdx.x & 31;
+  constexpr int SPREAD = 8 / PIECES > 0 ? 8 / PIECES : 1;   // rows within 128 bytes of the buffer
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < PIECES; ++j)
+    *reinterpret_cast<uint4*>(buf + lane * PIECES * 16 + ((j ^ ((lane / SPREAD) % PIECES)) * 16)) =
+        make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    const int row = i * ROWS + lane / PIECES, j = lane % PIECES;
+    const uint4 v = *reinterpret_cast<const uint4*>(buf + row * PIECES * 16 + ((j ^ ((row / SPREAD) % PIECES)) * 16));
+    if (row >= rows || 16 * j >= bytes) continue;
+    char* at = (char*)base + row * stride_bytes + 16 * j;
+    if (vec && 16 * j + 16 <= bytes) {
+      *reinterpret_cast<uint4*>(at) = v;
+    } else {
+      const unsigned e[4] = {v.x, v.y, v.z, v.w};
+      if (elem == 4) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (16 * j + 4 * q < bytes) *reinterpret_cast<unsigned*>(at + 4 * q) = e[q];
+      } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (16 * j + 2 * q < bytes)
+            *reinterpret_cast<unsigned short*>(at + 2 * q) = (unsigned short)(e[q / 2] >> (16 * (q & 1)));
+      }
+    }
+  }
+}
+
+// v as values of the call's type, to rows m... of matrix o from column n on.
+template <int CW>
+__device__ __forceinline__ void store_matrix(const float (&v)[CW], const Out& o, long long m, int n,
+                                             int rows, int cols, int dtype, char* buf) {
+  if (dtype == ABCD_F32) {
+    unsigned w[CW];
+#pragma unroll
+    for (int i = 0; i < CW; ++i) w[i] = __float_as_uint(v[i]);
+    store_words<CW>(w, buf, (float*)o.p + m * o.stride + n, o.stride * 4, rows, cols * 4, o.vec, 4);
+  } else {
+    unsigned w[CW / 2];
+#pragma unroll
+    for (int i = 0; i < CW / 2; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], dtype == ABCD_BF16);
+    store_words<CW / 2>(w, buf, (unsigned short*)o.p + m * o.stride + n, o.stride * 2, rows, cols * 2, o.vec, 2);
+  }
+}
+
+// v as an operand of a later product: of the 16-bit types the values, of 32 bits three terms.
+template <int CW>
+__device__ __forceinline__ void store_operand(const float (&v)[CW], const Out& o, long long m, int n,
+                                              int rows, int cols, int dtype, char* buf) {
+  if (dtype != ABCD_F32) return store_matrix<CW>(v, o, m, n, rows, cols, dtype, buf);
+  float rest[CW];
+#pragma unroll
+  for (int i = 0; i < CW; ++i) rest[i] = v[i];
+#pragma unroll 1
+  for (int t = 0; t < 3; ++t) {
+    unsigned w[CW / 2];
+#pragma unroll
+    for (int i = 0; i < CW / 2; ++i) {
+      const float a = take_term(rest[2 * i]), b = take_term(rest[2 * i + 1]);
+      w[i] = pack2(a, b, true);
+    }
+    store_words<CW / 2>(w, buf, (unsigned short*)o.p + t * o.plane + m * o.stride + n, o.stride * 2, rows,
+                        cols * 2, o.vec, 2);
+  }
+}
+
+// Row m's CW values from column n on (lanes past the matrix get zeros).
+template <int CW>
+__device__ __forceinline__ void load_row(float (&v)[CW], const Out& o, long long m, int n, bool in,
+                                         int cols, int dtype) {
+  const bool bf16 = dtype == ABCD_BF16;
+  if (dtype == ABCD_F32) {
+    const float* p = (const float*)o.p + m * o.stride + n;
+#pragma unroll
+    for (int i = 0; i < CW; i += 4) {
+      if (in && o.vec && i + 4 <= cols) {
+        const float4 q = *reinterpret_cast<const float4*>(p + i);
+        v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i + e] = in && i + e < cols ? p[i + e] : 0.f;
+      }
+    }
+  } else {
+    const unsigned short* p = (const unsigned short*)o.p + m * o.stride + n;
+#pragma unroll
+    for (int i = 0; i < CW; i += 8) {
+      unsigned w[4] = {0u, 0u, 0u, 0u};
+      if (in && o.vec && i + 8 <= cols) {
+        const uint4 q = *reinterpret_cast<const uint4*>(p + i);
+        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (in && i + e < cols) w[e / 2] |= (unsigned)p[i + e] << (16 * (e & 1));
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i + e] = unpack((unsigned short)(w[e / 2] >> (16 * (e & 1))), bf16);
+    }
+  }
+}
+
+// A work item of the persistent loop.
+struct Item {
+  int batch, split, tm, tn;
+  int tile;                           // number of (batch, tm, tn)
+  int k0, k1;                         // stages [k0, k1) of the sum
+};
+
+// Items in order: the splits of a tile next to each other (they finish together), tiles in bands of
+// eight along m, so that the CTAs that run at once share operands in L2.
+__device__ __forceinline__ Item item_of(const ProductArgs& a, int i) {
+  constexpr int BAND = 8;
+  Item it;
+  it.split = i % a.splits;
+  int t = i / a.splits;
+  it.tile = t;
+  const int per_batch = a.tiles_m * a.tiles_n;
+  it.batch = t / per_batch;
+  t -= it.batch * per_batch;
+  const int band = t / (BAND * a.tiles_n);
+  t -= band * BAND * a.tiles_n;
+  const int height = min(BAND, a.tiles_m - band * BAND);
+  it.tn = t / height;
+  it.tm = band * BAND + t % height;
+  const long long total = (long long)a.segments * a.kblocks;
+  it.k0 = (int)(total * it.split / a.splits);
+  it.k1 = (int)(total * (it.split + 1) / a.splits);
+  return it;
+}
+
+// CG: CTAs that share a tile (1 or 2) of 128 CG rows and BN sums per row; AMN, BMN: whether the
+// operand lies with its own dimension contiguous instead of k; EPI: what becomes of the sums.
+template <int CG, int BN, bool AMN, bool BMN, int EPI>
+struct Product {
+  static constexpr int kRows = 128;                      // rows of A per CTA
+  static constexpr int kBRows = BN / CG;                 // rows of B per CTA
+  static constexpr int kABytes = kRows * 128, kBBytes = kBRows * 128;
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kStages = 196608 / kStageBytes > 8 ? 8 : 196608 / kStageBytes;
+  static constexpr int kTmemCols = 2 * BN;
+  static constexpr int kOutCols = EPI == kUp ? BN / 2 : BN;   // results per row of a tile
+  static constexpr int kWarpCols = kOutCols / 2;         // results per row of an epilogue warp
+  static constexpr int CW = kWarpCols < 32 ? 16 : 32;    // taken at a time
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kStageBuffer;
+};
+
+template <int CG, int BN, bool AMN, bool BMN, int EPI>
+__global__ void __launch_bounds__(kFfThreads, 1) product_kernel(const __grid_constant__ ProductArgs a) {
+  using P = Product<CG, BN, AMN, BMN, EPI>;
+  extern __shared__ char smem_raw[];
+  __shared__ uint64_t bars[2 * P::kStages + 4];
+  __shared__ uint32_t tmem_base;
+  __shared__ volatile int dead;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+  const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
+  char* buffers = smem_raw + (ring - smem_addr(smem_raw)) + P::kStages * P::kStageBytes;
+  const uint32_t full = smem_addr(bars), empty = full + 8 * P::kStages;
+  const uint32_t sums_full = empty + 8 * P::kStages, sums_empty = sums_full + 16;
+  if (threadIdx.x == 0) {
+    dead = 0;
+    for (int s = 0; s < P::kStages; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(empty + 8 * s, 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(sums_full + 8 * s, 1);
+      mbar_init(sums_empty + 8 * s, kEpilogueWarps * CG);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&a.a);
+    prefetch_map(&a.b[0]);
+    prefetch_map(&a.b[1]);
+  }
+  if (warp == 1) tmem_alloc<CG>(smem_addr(&tmem_base), P::kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  if (CG == 2) cluster_sync();
+  tc_fence_after();
+  pdl_wait();
+  const uint32_t tmem = tmem_base;
+  const int first = blockIdx.x / CG, step = gridDim.x / CG;
+  const int items = a.batches * a.tiles_m * a.tiles_n * a.splits;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint32_t full0 = CG == 2 ? at_rank(full, 0) : full;   // the barriers of the pair's first CTA
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int i = first; ok && i < items; i += step) {
+        const Item it = item_of(a, i);
+        const int row_a = (it.tm * CG + (int)rank) * P::kRows;
+        for (int kb = it.k0; kb < it.k1; ++kb) {
+          if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, a.limit, &dead))) break;
+          const uint32_t bar = full0 + 8 * stage;
+          if (rank == 0) mbar_expect(full + 8 * stage, P::kStageBytes * CG);
+          const int seg = kb / a.kblocks, k = (kb - seg * a.kblocks) * kBlockK;
+          const uint32_t sa = ring + stage * P::kStageBytes, sb = sa + P::kABytes;
+          const int az = a.az[seg] + it.batch * a.batch_az, bz = a.bz[seg];
+          if (AMN) {
+#pragma unroll
+            for (int c = 0; c < P::kRows / 64; ++c) tma_load<CG>(sa + c * 8192, &a.a, row_a + c * 64, k, az, bar);
+          } else {
+            tma_load<CG>(sa, &a.a, k, row_a, az, bar);
+          }
+          if (EPI == kUp) {
+            // gate and up rows of the same hidden columns: sums [0, BN/2) and [BN/2, BN)
+            if (CG == 2) {
+              tma_load<CG>(sb, &a.b[rank], k, it.tn * P::kOutCols, bz, bar);
+            } else {
+              tma_load<CG>(sb, &a.b[0], k, it.tn * P::kOutCols, bz, bar);
+              tma_load<CG>(sb + P::kBBytes / 2, &a.b[1], k, it.tn * P::kOutCols, bz, bar);
+            }
+          } else {
+            const CUtensorMap* b = &a.b[a.bsel[seg]];
+            const int row_b = it.tn * BN + (int)rank * P::kBRows;
+            if (BMN) {
+#pragma unroll
+              for (int c = 0; c < P::kBRows / 64; ++c) tma_load<CG>(sb + c * 8192, b, row_b + c * 64, k, bz, bar);
+            } else {
+              tma_load<CG>(sb, b, k, row_b, bz, bar);
+            }
+          }
+          if (++stage == P::kStages) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      const uint32_t idesc = (1u << 4) | ((a.dtype == ABCD_F16 ? 0u : 1u) << 7) | ((a.dtype == ABCD_F16 ? 0u : 1u) << 10) |
+                             ((AMN ? 1u : 0u) << 15) | ((BMN ? 1u : 0u) << 16) | ((uint32_t)(BN / 8) << 17) |
+                             ((uint32_t)(128 * CG / 16) << 24);
+      int stage = 0;
+      uint32_t phase = 0;
+      int buf = 0;
+      uint32_t sums_phase = 0;
+      bool ok = true;
+      for (int i = first; ok && i < items; i += step) {
+        const Item it = item_of(a, i);
+        if (!(ok = mbar_wait(sums_empty + 8 * buf, sums_phase ^ 1, a.limit, &dead))) break;
+        tc_fence_after();
+        for (int kb = it.k0; kb < it.k1; ++kb) {
+          if (!(ok = mbar_wait(full + 8 * stage, phase, a.limit, &dead))) break;
+          tc_fence_after();
+          const uint32_t sa = ring + stage * P::kStageBytes, sb = sa + P::kABytes;
+#pragma unroll
+          for (int q = 0; q < kBlockK / 16; ++q)
+            mma16<CG>(tmem + buf * BN, tile_descriptor(sa + q * (AMN ? 2048 : 32), 8192),
+                      tile_descriptor(sb + q * (BMN ? 2048 : 32), 8192), idesc, kb > it.k0 || q > 0);
+          mma_commit<CG>(empty + 8 * stage);
+          if (++stage == P::kStages) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
+        if (ok) mma_commit<CG>(sums_full + 8 * buf);
+        buf ^= 1;
+        if (buf == 0) sums_phase ^= 1;
+      }
+    }
+  } else {
+    // a warp reads the quarter of tensor memory's lanes that its number in the CTA gives it
+    const int quarter = warp & 3, half = (warp - 2) / 4, ewarp = warp - 2;
+    char* buffer = buffers + ewarp * kStageBuffer;
+    const uint32_t empty0 = CG == 2 ? at_rank(sums_empty, 0) : sums_empty;
+    int buf = 0;
+    uint32_t phase = 0;
+    for (int i = first; i < items; i += step) {
+      const Item it = item_of(a, i);
+      const int m = (it.tm * CG + (int)rank) * P::kRows + quarter * 32;   // the warp's first row
+      const int n = it.tn * P::kOutCols + half * P::kWarpCols;
+      const int rows = min(32, a.m - m), cols = min(P::kWarpCols, a.n - n);
+      if (!mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead)) break;
+      tc_fence_after();
+      const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16) + half * P::kWarpCols;
+      bool mine = rows > 0 && cols > 0;
+      float* part = nullptr;
+      if (a.splits > 1) {
+        // this part's sums to the workspace [column][row]; the last warp to have done so goes on
+        constexpr int PARTS = EPI == kUp ? 2 : 1;
+        const long long piece = (long long)CG * kEpilogueWarps * PARTS * P::kWarpCols * 32;
+        part = a.part + (long long)it.tile * a.splits * piece +
+               ((long long)rank * kEpilogueWarps + ewarp) * PARTS * P::kWarpCols * 32 + lane;
+        if (mine) {
+          float* mypart = part + it.split * piece;
+#pragma unroll 1
+          for (int c = 0; c < PARTS * P::kWarpCols; c += P::CW) {
+            float v[P::CW];
+            tmem_load(sums + (c < P::kWarpCols ? c : BN / 2 + c - P::kWarpCols), v);
+            tmem_load_wait(v);
+#pragma unroll
+            for (int q = 0; q < P::CW; ++q) mypart[(c + q) * 32] = v[q];
+          }
+          __threadfence();
+          __syncwarp();
+          unsigned done = 0;
+          unsigned* count = a.count + ((long long)it.tile * CG + rank) * kEpilogueWarps + ewarp;
+          if (lane == 0) {
+            done = atomicAdd(count, 1u);
+            if (done == (unsigned)a.splits - 1) *count = 0;
+          }
+          done = __shfl_sync(~0u, done, 0);
+          __threadfence();
+          mine = done == (unsigned)a.splits - 1;
+        }
+      }
+      auto sum_columns = [&](int c, int which, float (&v)[P::CW]) {
+        if (a.splits == 1) {
+          tmem_load(sums + which * (BN / 2) + c, v);
+        } else {
+          constexpr int PARTS = EPI == kUp ? 2 : 1;
+          const long long piece = (long long)CG * kEpilogueWarps * PARTS * P::kWarpCols * 32;
+#pragma unroll
+          for (int q = 0; q < P::CW; ++q) v[q] = 0.f;
+#pragma unroll 2
+          for (int s = 0; s < a.splits; ++s) {
+            const float* p = part + s * piece + (which * P::kWarpCols + c) * 32;
+#pragma unroll
+            for (int q = 0; q < P::CW; ++q) v[q] += __ldcg(p + q * 32);
+          }
+        }
+      };
+      if (mine) {
+#pragma unroll 1
+        for (int c = 0; c < P::kWarpCols; c += P::CW) {
+          const int left = cols - c;
+          if (left <= 0) break;
+          const int w = min(left, P::CW);
+          float v[P::CW];
+          if (EPI == kUp) {
+            float u[P::CW];
+            sum_columns(c, 0, v);
+            sum_columns(c, 1, u);
+            if (a.splits == 1) {
+              tmem_load_wait(v);
+              tmem_load_wait(u);
+            }
+            if (a.g[0].p) {
+              store_matrix<P::CW>(v, a.g[0], m, n + c, rows, w, a.dtype, buffer);
+              store_matrix<P::CW>(u, a.g[1], m, n + c, rows, w, a.dtype, buffer);
+            }
+#pragma unroll
+            for (int q = 0; q < P::CW; ++q) v[q] = act_value(v[q], a.act) * u[q];
+            store_operand<P::CW>(v, a.c[0], m, n + c, rows, w, a.dtype, buffer);
+          } else if (EPI == kDown) {
+            float z[P::CW], u[P::CW];
+            load_row<P::CW>(z, a.in[0], m + lane, n + c, lane < rows, w, a.dtype);
+            load_row<P::CW>(u, a.in[1], m + lane, n + c, lane < rows, w, a.dtype);
+            sum_columns(c, 0, v);
+            if (a.splits == 1) tmem_load_wait(v);
+            float h[P::CW];
+#pragma unroll
+            for (int q = 0; q < P::CW; ++q) {
+              float value, slope;
+              act_both(z[q], a.act, value, slope);
+              h[q] = value * u[q];
+              z[q] = v[q] * u[q] * slope;
+              u[q] = v[q] * value;
+            }
+            store_operand<P::CW>(h, a.c[0], m, n + c, rows, w, a.dtype, buffer);
+            store_operand<P::CW>(z, a.g[0], m, n + c, rows, w, a.dtype, buffer);
+            store_operand<P::CW>(u, a.g[1], m, n + c, rows, w, a.dtype, buffer);
+          } else {
+            sum_columns(c, 0, v);
+            if (a.splits == 1) tmem_load_wait(v);
+            store_matrix<P::CW>(v, a.c[it.batch], m, n + c, rows, w, a.dtype, buffer);
+          }
+        }
+      }
+      // the sums have been read: the next tile but one may overwrite them
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(empty0 + 8 * buf);
+      buf ^= 1;
+      if (buf == 0) phase ^= 1;
+    }
+  }
+  __syncthreads();
+  // a wait gave up: the copies and matrix instructions that are still in flight get time to end
+  // before their memory is given back (about 2 ms, far above what any of them takes)
+  if (dead)
+    for (int q = 0; q < 2000; ++q) __nanosleep(1000);
+  tc_fence_before();
+  __syncthreads();
+  if (CG == 2) cluster_sync();
+  tc_fence_after();
+  if (warp == 1) tmem_free<CG>(tmem, P::kTmemCols);
+  if (threadIdx.x == 0 && dead) atomicOr(a.status, kStatusTimeout);
+}
+
+template <int CG, int BN, bool AMN, bool BMN, int EPI>
+abcd_status launch_product(abcd_ctx* ctx, const ProductArgs& a) {
+  using P = Product<CG, BN, AMN, BMN, EPI>;
+  auto* kernel = product_kernel<CG, BN, AMN, BMN, EPI>;
+  const cudaError_t e = allow_smem(ctx, (const void*)kernel);
+  if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "product_kernel: %s", cudaGetErrorString(e));
+  const long long items = (long long)a.batches * a.tiles_m * a.tiles_n * a.splits;
+  const int units = ctx->num_sms / CG;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(CG * (items < units ? items : units)));
+  cfg.blockDim = dim3(kFfThreads);
+  cfg.dynamicSmemBytes = P::kSmem;
+  cfg.stream = ctx->stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CG;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return check_launch(ctx, "product_kernel", cudaLaunchKernelEx(&cfg, kernel, a));
+}
+
+}  // namespace abcd

@@ -2,126 +2,243 @@
 //   G = x Wg^T, U = x Wu^T, H = act(G) U, y = H Wd^T
 //   dH = dy Wd, dU = dH act(G), dG = dH U act'(G), dx = dG Wg + dU Wu,
 //   dWg = dG^T x, dWu = dU^T x, dWd = dy^T H.
-// Both projections, the activation and their product are one kernel, and so are dH and what becomes
-// of it.
+// Five products: both projections with the activation and H; y; dH with dG, dU and H again (from the
+// saved G and U, so that H need not be kept from the forward pass); dx as one sum over both weights;
+// dWg and dWu in one grid, and dWd.  The kernel is in ffproduct.cuh; this file is the host's side:
+// operands, tensor maps, the choice of tiles and splits, the workspace.
 #include <algorithm>
+#include <cstring>
 
-#include "network.cuh"
+#include "ffproduct.cuh"
 
 namespace abcd {
 namespace {
 
-// element (i, k) at p[i * si + k * sk]
+constexpr size_t kPartBytes = (size_t)kNetSms * 128 * 256 * 4;   // one tile of sums per SM
+
+// A 16-bit operand of a product in device memory: planes of rows of cols values.
 struct Operand {
   const void* p;
-  long long si, sk;
+  long long rows, cols, pitch, plane;
+  int planes;
 };
 
-struct ProductArgs {
-  Operand a[2], b[2];
-  int pairs;                 // products that are added up (of kUp: the two that are gated)
-  long long m, n, k;
-  void* c;
-  long long sc;
-  const void* gate;          // kDown: the saved projections
-  const void* up;
-  void* gate_out;            // kUp: G and U, or NULL; kDown: dG and dU (row stride sc)
-  void* up_out;
-  long long sg, su, sgo, suo;
-  int act;
+int terms_of(int dtype) { return dtype == ABCD_F32 ? 3 : 1; }
+long long pitch_of(long long cols) { return (cols + 63) / 64 * 64; }   // whole 128-byte lines
+
+struct PackArgs {
+  const void* src;
+  long long rows, cols, stride, pitch, plane;
+  unsigned short* dst;
 };
 
-enum { kPlain, kUp, kDown };
-constexpr int kTile64 = 64, kStep = 16;
-
-__device__ __forceinline__ float act_value(float z, int act) {
-  if (act == ABCD_SILU) return z / (1.f + __expf(-z));
-  if (act == ABCD_GELU) return z * (0.5f * (1.f + erff(z * 0.70710678f)));
-  return fmaxf(z, 0.f);
-}
-
-__device__ __forceinline__ float act_slope(float z, int act) {
-  if (act == ABCD_SILU) {
-    const float s = 1.f / (1.f + __expf(-z));
-    return s * (1.f + z * (1.f - s));
-  }
-  if (act == ABCD_GELU) return 0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
-  return z > 0.f ? 1.f : 0.f;
-}
-
-// 64 x 64 outputs per CTA, 4 x 4 per thread.
-template <typename T, int MODE>
-__global__ void __launch_bounds__(256) product_kernel(const __grid_constant__ ProductArgs a) {
+// An operand from a matrix that TMA cannot read as it is: 32-bit values as three 16-bit terms, or
+// 16-bit rows moved to 16-byte boundaries.  One thread per eight columns of a row.
+template <typename T>
+__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackArgs a) {
   pdl_wait();
-  __shared__ float sa[kStep][kTile64 + 1], sb[2][kStep][kTile64 + 1];
-  const long long m0 = (long long)blockIdx.y * kTile64, n0 = (long long)blockIdx.x * kTile64;
-  const int tm = threadIdx.x / 16, tn = threadIdx.x % 16;
-  float acc[2][4][4] = {};
-  for (int pair = 0; pair < (MODE == kUp ? 1 : a.pairs); ++pair)
-    for (long long k0 = 0; k0 < a.k; k0 += kStep) {
-      for (int q = threadIdx.x; q < kTile64 * kStep; q += 256) {
-        const int i = q / kStep, k = q % kStep;
-        const bool in = k0 + k < a.k;
-        sa[k][i] = in && m0 + i < a.m ? to_f32(((const T*)a.a[pair].p)[(m0 + i) * a.a[pair].si + (k0 + k) * a.a[pair].sk]) : 0.f;
-        for (int s = 0; s < (MODE == kUp ? 2 : 1); ++s) {
-          const Operand& b = a.b[MODE == kUp ? s : pair];
-          sb[s][k][i] = in && n0 + i < a.n ? to_f32(((const T*)b.p)[(n0 + i) * b.si + (k0 + k) * b.sk]) : 0.f;
+  const long long groups = (a.cols + 7) / 8, total = groups * a.rows;
+  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < total; i += gridDim.x * 256LL) {
+    const long long row = i / groups, col = 8 * (i - row * groups);
+    const T* src = (const T*)a.src + row * a.stride + col;
+    unsigned short* dst = a.dst + row * a.pitch + col;
+    if constexpr (sizeof(T) == 4) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = col + j < a.cols ? src[j] : 0.f;
+#pragma unroll
+      for (int t = 0; t < 3; ++t) {
+        unsigned w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float lo = take_term(v[2 * j]), hi = take_term(v[2 * j + 1]);
+          w[j] = pack2(lo, hi, true);
         }
+        *reinterpret_cast<uint4*>(dst + t * a.plane) = make_uint4(w[0], w[1], w[2], w[3]);
       }
-      __syncthreads();
+    } else {
+      unsigned w[4];
 #pragma unroll
-      for (int k = 0; k < kStep; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int s = 0; s < (MODE == kUp ? 2 : 1); ++s)
-              acc[s][i][j] += sa[k][tm * 4 + i] * sb[s][k][tn * 4 + j];
-      __syncthreads();
+      for (int j = 0; j < 4; ++j) {
+        const unsigned lo = col + 2 * j < a.cols ? reinterpret_cast<const unsigned short*>(src)[2 * j] : 0u;
+        const unsigned hi = col + 2 * j + 1 < a.cols ? reinterpret_cast<const unsigned short*>(src)[2 * j + 1] : 0u;
+        w[j] = lo | hi << 16;
+      }
+      *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
     }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const long long m = m0 + tm * 4 + i, n = n0 + tn * 4 + j;
-      if (m >= a.m || n >= a.n) continue;
-      T* c = (T*)a.c + m * a.sc + n;
-      if (MODE == kPlain) *c = from_f32<T>(acc[0][i][j]);
-      if (MODE == kUp) {
-        *c = from_f32<T>(act_value(acc[0][i][j], a.act) * acc[1][i][j]);
-        if (a.gate_out) {
-          ((T*)a.gate_out)[m * a.sgo + n] = from_f32<T>(acc[0][i][j]);
-          ((T*)a.up_out)[m * a.suo + n] = from_f32<T>(acc[1][i][j]);
-        }
-      }
-      if (MODE == kDown) {
-        const float z = to_f32(((const T*)a.gate)[m * a.sg + n]), u = to_f32(((const T*)a.up)[m * a.su + n]);
-        const float h = act_value(z, a.act);
-        *c = from_f32<T>(h * u);
-        ((T*)a.gate_out)[m * a.sgo + n] = from_f32<T>(acc[0][i][j] * u * act_slope(z, a.act));
-        ((T*)a.up_out)[m * a.suo + n] = from_f32<T>(acc[0][i][j] * h);
-      }
-    }
+  }
 }
 
-template <int MODE>
-abcd_status product(abcd_ctx* ctx, int dtype, const ProductArgs& a) {
-  const dim3 grid((unsigned)((a.n + kTile64 - 1) / kTile64), (unsigned)((a.m + kTile64 - 1) / kTile64));
-  return with_type(dtype, [&](auto t) {
-    return check_launch(ctx, "product_kernel",
-                        launch_pdl(product_kernel<decltype(t), MODE>, grid, dim3(256), 0, ctx->stream, a));
+// Hands out the network workspace after its header; without a base it only counts.
+struct Scratch {
+  char* base;
+  size_t at = kNetHeader;
+  void* take(size_t bytes) {
+    char* p = base ? base + at : nullptr;
+    at += net_align(bytes);
+    return p;
+  }
+  Operand operand(long long rows, long long cols, int dtype, int matrices = 1) {
+    Operand o{nullptr, rows, cols, pitch_of(cols), 0, matrices * terms_of(dtype)};
+    o.plane = rows * o.pitch;
+    o.p = take((size_t)o.planes * (size_t)o.plane * 2);
+    return o;
+  }
+};
+
+bool needs_pack(const abcd_matrix* m) { return m->dtype == ABCD_F32 || !rows_aligned(m, 16); }
+
+// m as an operand: in place where TMA can read it, else a copy in the workspace.
+abcd_status operand_of(abcd_ctx* ctx, Scratch& s, const abcd_matrix* m, Operand* o) {
+  if (!needs_pack(m)) {
+    *o = Operand{m->data, m->rows, m->cols, (m->stride + 7) / 8 * 8, 0, 1};
+    return ABCD_OK;
+  }
+  *o = s.operand(m->rows, m->cols, m->dtype);
+  const PackArgs a{m->data, m->rows, m->cols, m->stride, o->pitch, o->plane, (unsigned short*)o->p};
+  const long long blocks = std::min<long long>(((m->cols + 7) / 8 * m->rows + 255) / 256, 16LL * ctx->num_sms);
+  return with_type(m->dtype, [&](auto t) {
+    return check_launch(ctx, "pack_kernel", launch_pdl(pack_kernel<decltype(t)>, dim3((unsigned)blocks),
+                                                       dim3(256), 0, ctx->stream, a));
   });
 }
 
-Operand rows_of(const abcd_matrix* m) { return Operand{m->data, m->stride, 1}; }
-Operand cols_of(const abcd_matrix* m) { return Operand{m->data, 1, m->stride}; }
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                              const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                              CUtensorMapFloatOOBfill);
 
-// The scratch of one call: the hidden matrix, dG and dU.
-size_t ff_scratch(long long rows, long long ff, int dtype) {
-  return 3 * net_align((size_t)rows * (size_t)ff * elem_size(dtype));
+EncodeFn encode_fn() {
+  static const EncodeFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+        r != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return (EncodeFn)p;
+  }();
+  return fn;
+}
+
+// The tensor map of an operand with boxes of 64 consecutive columns and `box_rows` rows; what lies
+// outside the matrix reads as zero.
+bool make_map(CUtensorMap* map, const Operand& o, int dtype, int box_rows) {
+  const EncodeFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.planes};
+  const cuuint64_t strides[2] = {(cuuint64_t)o.pitch * 2, (cuuint64_t)std::max<long long>(o.plane, o.pitch) * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, unit[3] = {1, 1, 1};
+  return fn(map, dtype == ABCD_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+            const_cast<void*>(o.p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+Out out_of(const abcd_matrix* m) {
+  return Out{m->data, m->stride, 0, rows_aligned(m, 16) ? 1 : 0};
+}
+Out out_of(const Operand& o, int matrix, int dtype) {
+  return Out{(unsigned short*)const_cast<void*>(o.p) + matrix * terms_of(dtype) * o.plane, o.pitch, o.plane, 1};
+}
+
+// One product: A and up to two B operands, whether each lies with its own dimension contiguous.
+struct Job {
+  Operand a, b[2];
+  int nb;                    // B operands (kPlain with two: the sum of both products)
+  long long m, n, k;
+  int batches;
+  ProductArgs args;
+};
+
+// The tiles: 256 x 256 on a pair of CTAs, 128 x 128 or 128 x 64 sums on one.
+struct Shape {
+  int cg, bn;
+  int cycles;                // of a stage (64 of k), about
+};
+constexpr Shape kShapes[3] = {{2, 256, 560}, {1, 128, 300}, {1, 64, 200}};
+
+// Picks the shape and the number of splits with the least estimated time: the waves of tiles times
+// their stages, plus what a tile costs apart from them, plus the splits' joining.
+void plan(int sms, long long m, long long n, int epi, long long stages, long long batches, int* shape, int* splits) {
+  double best = 1e300;
+  for (int s = 0; s < 3; ++s) {
+    const long long cols = epi == kUp ? kShapes[s].bn / 2 : kShapes[s].bn;
+    const long long units = sms / kShapes[s].cg;
+    const long long tiles = batches * ((m + 128 * kShapes[s].cg - 1) / (128 * kShapes[s].cg)) * ((n + cols - 1) / cols);
+    const long long most = std::max<long long>(1, std::min<long long>({units / std::max<long long>(1, tiles), stages / 4, 64}));
+    for (long long p = 1; p <= most; ++p) {
+      const double waves = (double)((tiles * p + units - 1) / units);
+      const double t = waves * ((double)((stages + p - 1) / p) * kShapes[s].cycles + 2000.0) + (p > 1 ? 3000.0 + 150.0 * p : 0.0);
+      if (t < best) {
+        best = t;
+        *shape = s;
+        *splits = (int)p;
+      }
+    }
+  }
+}
+
+template <bool AMN, bool BMN, int EPI>
+abcd_status run(abcd_ctx* ctx, int dtype, Job& j) {
+  ProductArgs& a = j.args;
+  const int terms = terms_of(dtype);
+  a.m = (int)j.m;
+  a.n = (int)j.n;
+  a.kblocks = (int)((j.k + kBlockK - 1) / kBlockK);
+  a.segments = 0;
+  // pairs of terms, the smallest products first
+  const int pairs = EPI == kUp ? 1 : j.nb;
+  for (int order = terms - 1; order >= 0; --order)
+    for (int b = 0; b < pairs; ++b)
+      for (int t = order; t >= 0; --t) {
+        a.az[a.segments] = (unsigned char)(b * terms + t);
+        a.bsel[a.segments] = (unsigned char)b;
+        a.bz[a.segments++] = (unsigned char)(order - t);
+      }
+  a.batches = j.batches;
+  a.batch_az = terms;
+  a.dtype = dtype;
+  int shape = 0, splits = 1;
+  plan(std::min(ctx->num_sms, kNetSms), j.m, j.n, EPI, (long long)a.segments * a.kblocks, j.batches, &shape, &splits);
+  const int cg = kShapes[shape].cg, bn = kShapes[shape].bn;
+  a.tiles_m = (int)((j.m + 128 * cg - 1) / (128 * cg));
+  const int cols = EPI == kUp ? bn / 2 : bn;
+  a.tiles_n = (int)((j.n + cols - 1) / cols);
+  a.splits = splits;
+  a.count = (unsigned*)(ctx->net_base + kNetCounters);
+  a.part = (float*)(ctx->net_base + kNetHeader);
+  a.status = (unsigned*)ctx->net_base;
+  a.limit = ctx->wait_limit;
+  bool ok = make_map(&a.a, j.a, dtype, AMN ? 64 : 128);
+  for (int b = 0; ok && b < j.nb; ++b) ok = make_map(&a.b[b], j.b[b], dtype, BMN ? 64 : EPI == kUp ? bn / 2 : bn / cg);
+  if (!ok) return fail(ctx, ABCD_ERR_CUDA, "tensor map of a product");
+  if (j.nb < 2) a.b[1] = a.b[0];
+  if (shape == 0) return launch_product<2, 256, AMN, BMN, EPI>(ctx, a);
+  if (shape == 1) return launch_product<1, 128, AMN, BMN, EPI>(ctx, a);
+  return launch_product<1, 64, AMN, BMN, EPI>(ctx, a);
 }
 
 bool shape_is(const abcd_matrix* m, int dtype, long long rows, long long cols) {
   return matrix_ok(m) && m->dtype == dtype && m->rows == rows && m->cols == cols;
+}
+
+// The scratch of the calls when every matrix has to be copied: the most that they take.
+size_t ff_scratch(long long rows, long long cols, long long ff, int dtype) {
+  Scratch s{nullptr};
+  s.take(kPartBytes);
+  s.operand(rows, cols, dtype);           // x
+  s.operand(rows, cols, dtype);           // dy
+  s.operand(ff, cols, dtype);             // w_gate
+  s.operand(ff, cols, dtype);             // w_up
+  s.operand(cols, ff, dtype);             // w_down
+  s.operand(rows, ff, dtype);             // hidden
+  s.operand(rows, ff, dtype, 2);          // dG, dU
+  return s.at;
+}
+
+abcd_status room(abcd_ctx* ctx, const char* what, size_t need) {
+  if (need <= ctx->net_bytes) return ABCD_OK;
+  return fail(ctx, ABCD_ERR_WORKSPACE, "%s: the network workspace has %zu bytes, needs %zu", what, ctx->net_bytes, need);
 }
 
 }  // namespace
@@ -137,17 +254,17 @@ extern "C" abcd_status abcd_network_workspace_size(long long rows, long long col
   if (!bytes || rows < 0 || rows > kMaxNetRows || cols < 1 || cols > kMaxNetCols || ff < 0 ||
       ff > kMaxNetCols || !dtype_ok(dtype))
     return ABCD_ERR_INVALID_ARG;
-  int sms = 0;
-  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, 0) != cudaSuccess) sms = 160;
-  *bytes = std::max((size_t)norm_bwd_ctas(sms) * 2 * (size_t)cols * sizeof(float),
-                    ff_scratch(rows, ff, dtype));
+  const size_t norm = kNetHeader + (size_t)norm_bwd_ctas(kNetSms) * 2 * (size_t)cols * sizeof(float);
+  *bytes = ff > 0 ? std::max(norm, ff_scratch(rows, cols, ff, dtype)) : norm;
   return ABCD_OK;
 }
 
 extern "C" abcd_status abcd_set_network_workspace(abcd_ctx* ctx, void* ptr, size_t bytes) {
   if (!ctx) return ABCD_ERR_INVALID_ARG;
-  if (!ptr || ((uintptr_t)ptr & 255))
-    return fail(ctx, ABCD_ERR_INVALID_ARG, "the network workspace must be a 256-byte aligned device pointer");
+  if (!ptr || ((uintptr_t)ptr & 255) || bytes < kNetHeader)
+    return fail(ctx, ABCD_ERR_INVALID_ARG, "the network workspace must be a 256-byte aligned device pointer to %zu bytes at least", kNetHeader);
+  const cudaError_t e = cudaMemsetAsync(ptr, 0, kNetHeader, ctx->stream);
+  if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "clearing the network workspace: %s", cudaGetErrorString(e));
   ctx->net_base = (char*)ptr;
   ctx->net_bytes = bytes;
   return ABCD_OK;
@@ -157,42 +274,46 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
                                      const abcd_matrix* w_up, const abcd_matrix* w_down,
                                      int activation, const abcd_matrix* y, const abcd_matrix* gate,
                                      const abcd_matrix* up) {
+  const char* what = "abcd_gated_ff";
   if (!ctx) return ABCD_ERR_INVALID_ARG;
-  if (!matrix_ok(x) || !matrix_ok(w_gate)) return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_gated_ff: bad x or w_gate");
+  if (!matrix_ok(x) || !matrix_ok(w_gate)) return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: bad x or w_gate", what);
   const long long m = x->rows, d = x->cols, f = w_gate->rows;
-  if (f < 1 || f > kMaxNetCols || !shape_is(w_gate, x->dtype, f, d) || !shape_is(w_up, x->dtype, f, d) ||
-      !shape_is(w_down, x->dtype, d, f))
-    return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_gated_ff: the weights do not fit x");
-  if (!shape_is(y, x->dtype, m, d) || (gate == nullptr) != (up == nullptr) ||
-      (gate && (!shape_is(gate, x->dtype, m, f) || !shape_is(up, x->dtype, m, f))))
-    return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_gated_ff: the outputs do not fit x and the weights");
+  const int t = x->dtype;
+  if (f < 1 || f > kMaxNetCols || !shape_is(w_gate, t, f, d) || !shape_is(w_up, t, f, d) || !shape_is(w_down, t, d, f))
+    return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: the weights do not fit x", what);
+  if (!shape_is(y, t, m, d) || (gate == nullptr) != (up == nullptr) ||
+      (gate && (!shape_is(gate, t, m, f) || !shape_is(up, t, m, f))))
+    return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: the outputs do not fit x and the weights", what);
   if (activation < ABCD_SILU || activation > ABCD_RELU)
-    return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_gated_ff: unknown activation");
+    return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: unknown activation", what);
   if (m == 0) return ABCD_OK;
-  const size_t need = ff_scratch(m, f, x->dtype);
-  if (need > ctx->net_bytes)
-    return fail(ctx, ABCD_ERR_WORKSPACE, "abcd_gated_ff: the network workspace has %zu bytes, needs %zu", ctx->net_bytes, need);
-  const abcd_matrix h{ctx->net_base, m, f, f, x->dtype};
-  ProductArgs a{};
-  a.a[0] = rows_of(x);
-  a.b[0] = rows_of(w_gate);
-  a.b[1] = rows_of(w_up);
-  a.m = m; a.n = f; a.k = d;
-  a.c = h.data; a.sc = f;
-  a.act = activation;
-  if (gate) {
-    a.gate_out = gate->data; a.sgo = gate->stride;
-    a.up_out = up->data; a.suo = up->stride;
-  }
-  abcd_status st = product<kUp>(ctx, x->dtype, a);
+  Scratch need{nullptr};
+  need.take(kPartBytes);
+  if (needs_pack(x)) need.operand(m, d, t);
+  if (needs_pack(w_gate)) need.operand(f, d, t);
+  if (needs_pack(w_up)) need.operand(f, d, t);
+  if (needs_pack(w_down)) need.operand(d, f, t);
+  need.operand(m, f, t);
+  abcd_status st = room(ctx, what, need.at);
   if (st != ABCD_OK) return st;
-  ProductArgs b{};
-  b.a[0] = rows_of(&h);
-  b.b[0] = rows_of(w_down);
-  b.pairs = 1;
-  b.m = m; b.n = d; b.k = f;
-  b.c = y->data; b.sc = y->stride;
-  return product<kPlain>(ctx, x->dtype, b);
+  Scratch s{ctx->net_base};
+  s.take(kPartBytes);
+  Operand ox, og, ou, od;
+  if ((st = operand_of(ctx, s, x, &ox)) != ABCD_OK || (st = operand_of(ctx, s, w_gate, &og)) != ABCD_OK ||
+      (st = operand_of(ctx, s, w_up, &ou)) != ABCD_OK || (st = operand_of(ctx, s, w_down, &od)) != ABCD_OK)
+    return st;
+  const Operand h = s.operand(m, f, t);
+  Job up_job{ox, {og, ou}, 2, m, f, d, 1, {}};
+  up_job.args.act = activation;
+  up_job.args.c[0] = out_of(h, 0, t);
+  if (gate) {
+    up_job.args.g[0] = out_of(gate);
+    up_job.args.g[1] = out_of(up);
+  }
+  if ((st = run<false, false, kUp>(ctx, t, up_job)) != ABCD_OK) return st;
+  Job y_job{h, {od, od}, 1, m, d, f, 1, {}};
+  y_job.args.c[0] = out_of(y);
+  return run<false, false, kPlain>(ctx, t, y_job);
 }
 
 extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* dy,
@@ -216,49 +337,60 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: the gradients do not fit x and the weights", what);
   if (activation < ABCD_SILU || activation > ABCD_RELU)
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: unknown activation", what);
-  const size_t need = ff_scratch(m, f, t);
-  if (need > ctx->net_bytes)
-    return fail(ctx, ABCD_ERR_WORKSPACE, "%s: the network workspace has %zu bytes, needs %zu", what, ctx->net_bytes, need);
-  const size_t one = need / 3;
-  const abcd_matrix h{ctx->net_base, m, f, f, t}, dg{ctx->net_base + one, m, f, f, t},
-      du{ctx->net_base + 2 * one, m, f, f, t};
-  abcd_status st = ABCD_OK;
-  if (m > 0) {
-    ProductArgs a{};
-    a.a[0] = rows_of(dy);
-    a.b[0] = cols_of(w_down);
-    a.pairs = 1;
-    a.m = m; a.n = f; a.k = d;
-    a.c = h.data; a.sc = f;
-    a.gate = gate->data; a.sg = gate->stride;
-    a.up = up->data; a.su = up->stride;
-    a.gate_out = dg.data; a.sgo = f;
-    a.up_out = du.data; a.suo = f;
-    a.act = activation;
-    st = product<kDown>(ctx, t, a);
-    if (st != ABCD_OK) return st;
-    if (dx) {
-      ProductArgs b{};
-      b.a[0] = rows_of(&dg); b.a[1] = rows_of(&du);
-      b.b[0] = cols_of(w_gate); b.b[1] = cols_of(w_up);
-      b.pairs = 2;
-      b.m = m; b.n = d; b.k = f;
-      b.c = dx->data; b.sc = dx->stride;
-      if ((st = product<kPlain>(ctx, t, b)) != ABCD_OK) return st;
+  if (m == 0) {                                   // sums over no rows
+    for (const abcd_matrix* w : {dw_gate, dw_up, dw_down}) {
+      if (!w) continue;
+      const size_t e = elem_size(t);
+      const cudaError_t c = cudaMemset2DAsync(w->data, (size_t)w->stride * e, 0, (size_t)w->cols * e, (size_t)w->rows, ctx->stream);
+      if (c != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(c));
     }
+    return ABCD_OK;
   }
-  const abcd_matrix* left[3] = {&dg, &du, dy};
-  const abcd_matrix* right[3] = {x, x, &h};
-  const abcd_matrix* out[3] = {dw_gate, dw_up, dw_down};
-  for (int k = 0; k < 3; ++k) {
-    if (!out[k]) continue;
-    ProductArgs b{};
-    b.a[0] = cols_of(left[k]);
-    b.b[0] = cols_of(right[k]);
-    b.pairs = 1;
-    b.m = out[k]->rows; b.n = out[k]->cols; b.k = m;
-    b.c = out[k]->data; b.sc = out[k]->stride;
-    if ((st = product<kPlain>(ctx, t, b)) != ABCD_OK) return st;
+  Scratch need{nullptr};
+  need.take(kPartBytes);
+  if (needs_pack(dy)) need.operand(m, d, t);
+  if (needs_pack(x)) need.operand(m, d, t);
+  if (needs_pack(w_gate)) need.operand(f, d, t);
+  if (needs_pack(w_up)) need.operand(f, d, t);
+  if (needs_pack(w_down)) need.operand(d, f, t);
+  need.operand(m, f, t);
+  need.operand(m, f, t, 2);
+  abcd_status st = room(ctx, what, need.at);
+  if (st != ABCD_OK) return st;
+  Scratch s{ctx->net_base};
+  s.take(kPartBytes);
+  Operand ody, ox, og, ou, od;
+  if ((st = operand_of(ctx, s, dy, &ody)) != ABCD_OK || (st = operand_of(ctx, s, w_down, &od)) != ABCD_OK) return st;
+  if ((dw_gate || dw_up) && (st = operand_of(ctx, s, x, &ox)) != ABCD_OK) return st;
+  if (dx && ((st = operand_of(ctx, s, w_gate, &og)) != ABCD_OK || (st = operand_of(ctx, s, w_up, &ou)) != ABCD_OK)) return st;
+  const Operand h = s.operand(m, f, t), dgu = s.operand(m, f, t, 2);
+  Job down{ody, {od, od}, 1, m, f, d, 1, {}};
+  down.args.act = activation;
+  down.args.in[0] = out_of(gate);
+  down.args.in[1] = out_of(up);
+  down.args.c[0] = out_of(h, 0, t);
+  down.args.g[0] = out_of(dgu, 0, t);
+  down.args.g[1] = out_of(dgu, 1, t);
+  if ((st = run<false, true, kDown>(ctx, t, down)) != ABCD_OK) return st;
+  if (dx) {
+    Job j{dgu, {og, ou}, 2, m, d, f, 1, {}};
+    j.args.c[0] = out_of(dx);
+    if ((st = run<false, true, kPlain>(ctx, t, j)) != ABCD_OK) return st;
+  }
+  if (dw_gate || dw_up) {
+    // dG^T x and dU^T x: the second starts at dU's planes
+    Operand left = dgu;
+    if (!dw_gate) left.p = (const unsigned short*)dgu.p + (long long)terms_of(t) * dgu.plane;
+    left.planes = dw_gate && dw_up ? dgu.planes : terms_of(t);
+    Job j{left, {ox, ox}, 1, f, d, m, dw_gate && dw_up ? 2 : 1, {}};
+    j.args.c[0] = out_of(dw_gate ? dw_gate : dw_up);
+    if (dw_gate && dw_up) j.args.c[1] = out_of(dw_up);
+    if ((st = run<true, true, kPlain>(ctx, t, j)) != ABCD_OK) return st;
+  }
+  if (dw_down) {
+    Job j{ody, {h, h}, 1, d, f, m, 1, {}};
+    j.args.c[0] = out_of(dw_down);
+    if ((st = run<true, true, kPlain>(ctx, t, j)) != ABCD_OK) return st;
   }
   return ABCD_OK;
 }

@@ -174,13 +174,14 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
     return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_layer_norm_backward: bad weight or gradients");
   if (x->rows > 0 && (!mean || !rstd))
     return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_layer_norm_backward: no statistics");
-  const int ctas = (int)std::min<long long>(x->rows, norm_bwd_ctas(ctx->num_sms));
-  const size_t need = (size_t)ctas * 2 * (size_t)x->cols * sizeof(float);
+  const int ctas = (int)std::min<long long>(x->rows, norm_bwd_ctas(std::min(ctx->num_sms, kNetSms)));
+  float* part = (float*)(ctx->net_base + kNetHeader);
+  const size_t need = kNetHeader + (size_t)ctas * 2 * (size_t)x->cols * sizeof(float);
   if (need > ctx->net_bytes)
     return fail(ctx, ABCD_ERR_WORKSPACE, "abcd_layer_norm_backward: the network workspace has %zu bytes, needs %zu", ctx->net_bytes, need);
   const NormArgs a{x->data, dy->data, weight, nullptr, dx ? dx->data : nullptr,
                    d_residual ? d_residual->data : nullptr, (float*)mean, (float*)rstd,
-                   (float*)ctx->net_base, x->rows, (int)x->cols, x->stride, dy->stride,
+                   part, x->rows, (int)x->cols, x->stride, dy->stride,
                    dx ? dx->stride : 0, d_residual ? d_residual->stride : 0, 0.f};
   return with_types(x->dtype, weight_dtype, [&](auto t, auto w) {
     abcd_status st = ABCD_OK;
@@ -191,7 +192,7 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
     if (st != ABCD_OK || (!dweight && !dbias)) return st;
     return check_launch(ctx, "norm_sum_kernel",
                         launch_pdl(norm_sum_kernel<decltype(w)>, dim3((unsigned)((x->cols + 127) / 128)),
-                                   dim3(128), 0, ctx->stream, (const float*)ctx->net_base, ctas,
+                                   dim3(128), 0, ctx->stream, (const float*)part, ctas,
                                    (int)x->cols, (decltype(w)*)dweight, (decltype(w)*)dbias));
   });
 }

@@ -10,6 +10,10 @@ namespace abcd {
 
 constexpr long long kMaxNetCols = 1LL << 24;   // columns of a matrix, hidden columns
 constexpr long long kMaxNetRows = 1LL << 30;   // its rows
+constexpr int kNetSms = 160;                   // SMs for which the network workspace has room
+// The workspace's header: the status word of the products' waits and, from kNetCounters on, the
+// counters of their splits, zero between calls.
+constexpr size_t kNetHeader = 65536, kNetCounters = 256;
 
 inline size_t elem_size(int dtype) { return dtype == ABCD_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) {
