@@ -39,7 +39,7 @@ struct Out {
   int vec;                            // rows start on 16-byte boundaries
 };
 
-struct alignas(64) ProductArgs {
+struct ProductArgs {
   CUtensorMap a, b[2];
   int m, n;                           // rows of A and B (kUp: of each B)
   int kblocks;                        // stages per segment
@@ -216,7 +216,7 @@ __device__ __forceinline__ void load_row(float (&v)[CW], const Out& o, long long
 struct Item {
   int batch, split, tm, tn;
   int tile;                           // number of (batch, tm, tn)
-  int k0, k1;                         // stages [k0, k1) of the sum
+  int k0, k1;                         // stages [k0, k1) of every segment
 };
 
 // Items in order: the splits of a tile next to each other (they finish together), tiles in bands of
@@ -235,9 +235,8 @@ __device__ __forceinline__ Item item_of(const ProductArgs& a, int i) {
   const int height = min(BAND, a.tiles_m - band * BAND);
   it.tn = t / height;
   it.tm = band * BAND + t % height;
-  const long long total = (long long)a.segments * a.kblocks;
-  it.k0 = (int)(total * it.split / a.splits);
-  it.k1 = (int)(total * (it.split + 1) / a.splits);
+  it.k0 = (int)((long long)a.kblocks * it.split / a.splits);
+  it.k1 = (int)((long long)a.kblocks * (it.split + 1) / a.splits);
   return it;
 }
 
@@ -304,11 +303,11 @@ __global__ void __launch_bounds__(kFfThreads, 1) product_kernel(const __grid_con
       for (int i = first; ok && i < items; i += step) {
         const Item it = item_of(a, i);
         const int row_a = (it.tm * CG + (int)rank) * P::kRows;
-        for (int kb = it.k0; kb < it.k1; ++kb) {
+        for (int seg = 0, kb = it.k0; seg < a.segments; kb + 1 < it.k1 ? ++kb : (++seg, kb = it.k0)) {
           if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, a.limit, &dead))) break;
           const uint32_t bar = full0 + 8 * stage;
           if (rank == 0) mbar_expect(full + 8 * stage, P::kStageBytes * CG);
-          const int seg = kb / a.kblocks, k = (kb - seg * a.kblocks) * kBlockK;
+          const int k = kb * kBlockK;
           const uint32_t sa = ring + stage * P::kStageBytes, sb = sa + P::kABytes;
           const int az = a.az[seg] + it.batch * a.batch_az, bz = a.bz[seg];
           if (AMN) {
@@ -356,14 +355,15 @@ __global__ void __launch_bounds__(kFfThreads, 1) product_kernel(const __grid_con
         const Item it = item_of(a, i);
         if (!(ok = mbar_wait(sums_empty + 8 * buf, sums_phase ^ 1, a.limit, &dead))) break;
         tc_fence_after();
-        for (int kb = it.k0; kb < it.k1; ++kb) {
+        const int stages = a.segments * (it.k1 - it.k0);
+        for (int kb = 0; kb < stages; ++kb) {
           if (!(ok = mbar_wait(full + 8 * stage, phase, a.limit, &dead))) break;
           tc_fence_after();
           const uint32_t sa = ring + stage * P::kStageBytes, sb = sa + P::kABytes;
 #pragma unroll
           for (int q = 0; q < kBlockK / 16; ++q)
             mma16<CG>(tmem + buf * BN, tile_descriptor(sa + q * (AMN ? 2048 : 32), 8192),
-                      tile_descriptor(sb + q * (BMN ? 2048 : 32), 8192), idesc, kb > it.k0 || q > 0);
+                      tile_descriptor(sb + q * (BMN ? 2048 : 32), 8192), idesc, kb > 0 || q > 0);
           mma_commit<CG>(empty + 8 * stage);
           if (++stage == P::kStages) {
             stage = 0;

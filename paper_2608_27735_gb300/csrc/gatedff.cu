@@ -159,16 +159,16 @@ constexpr Shape kShapes[3] = {{2, 256, 560}, {1, 128, 300}, {1, 64, 200}};
 
 // Picks the shape and the number of splits with the least estimated time: the waves of tiles times
 // their stages, plus what a tile costs apart from them, plus the splits' joining.
-void plan(int sms, long long m, long long n, int epi, long long stages, long long batches, int* shape, int* splits) {
+void plan(int sms, long long m, long long n, int epi, long long kblocks, int segments, long long batches, int* shape, int* splits) {
   double best = 1e300;
   for (int s = 0; s < 3; ++s) {
     const long long cols = epi == kUp ? kShapes[s].bn / 2 : kShapes[s].bn;
     const long long units = sms / kShapes[s].cg;
     const long long tiles = batches * ((m + 128 * kShapes[s].cg - 1) / (128 * kShapes[s].cg)) * ((n + cols - 1) / cols);
-    const long long most = std::max<long long>(1, std::min<long long>({units / std::max<long long>(1, tiles), stages / 4, 64}));
+    const long long most = std::max<long long>(1, std::min<long long>({units / std::max<long long>(1, tiles), kblocks * segments / 4, kblocks, 64}));
     for (long long p = 1; p <= most; ++p) {
       const double waves = (double)((tiles * p + units - 1) / units);
-      const double t = waves * ((double)((stages + p - 1) / p) * kShapes[s].cycles + 2000.0) + (p > 1 ? 3000.0 + 150.0 * p : 0.0);
+      const double t = waves * ((double)(segments * ((kblocks + p - 1) / p)) * kShapes[s].cycles + 2000.0) + (p > 1 ? 3000.0 + 150.0 * p : 0.0);
       if (t < best) {
         best = t;
         *shape = s;
@@ -199,7 +199,7 @@ abcd_status run(abcd_ctx* ctx, int dtype, Job& j) {
   a.batch_az = terms;
   a.dtype = dtype;
   int shape = 0, splits = 1;
-  plan(std::min(ctx->num_sms, kNetSms), j.m, j.n, EPI, (long long)a.segments * a.kblocks, j.batches, &shape, &splits);
+  plan(std::min(ctx->num_sms, kNetSms), j.m, j.n, EPI, a.kblocks, a.segments, j.batches, &shape, &splits);
   const int cg = kShapes[shape].cg, bn = kShapes[shape].bn;
   a.tiles_m = (int)((j.m + 128 * cg - 1) / (128 * cg));
   const int cols = EPI == kUp ? bn / 2 : bn;

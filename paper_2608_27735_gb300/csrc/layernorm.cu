@@ -2,10 +2,19 @@
 //   y = (x - mean) rstd w + b,   rstd = 1 / sqrt(mean((x - mean)^2) + eps)
 //   g = dy w, xh = (x - mean) rstd:  dx = rstd (g - mean(g) - xh mean(g xh)),
 //   dw = sum_rows dy xh,  db = sum_rows dy.
-// The variance is taken from the deviations (a second pass over the row), not from the difference
-// of two moments.  The sums over the rows are taken in a fixed order: each CTA adds its rows' terms,
-// a second kernel adds the CTAs'.
+// The variance is taken from the deviations, not from the difference of two moments, so a mean far
+// from zero costs it no digits.
+//
+// Bound by HBM (forward x -> y, backward x, dy -> dx).  A row is read once: TPR lanes (part of a
+// warp, a warp, or a CTA) hold it in registers, NV accesses of V consecutive elements each, V = 16
+// bytes where the rows lie on 16-byte boundaries and one element where they do not; rows too long
+// for that are read again from L2.  Backward, a CTA takes many rows and its lanes keep dw and db of
+// their own columns in registers; the next rows are copied to shared memory meanwhile
+// (cp.async, each thread its own bytes, so no barrier is needed), which keeps the loads in flight
+// that eight warps of about 180 registers could not.  The CTAs' sums go to the workspace and a
+// second kernel adds them in their order.
 #include <algorithm>
+#include <type_traits>
 
 #include "network.cuh"
 
@@ -26,43 +35,291 @@ struct NormArgs {
   int cols;
   long long sx, sdy, sy, sres;
   float eps;
+  int wide_w;                         // weight and bias are fp32 whatever the matrices' type
 };
 
-constexpr int kNormThreads = 256;
+// How a row lies over threads.
+template <int TPR_, int V_, int NV_> struct RowShape {
+  static constexpr int TPR = TPR_, V = V_, NV = NV_;
+  static constexpr int kThreads = TPR > 256 ? TPR : 256;
+  static constexpr int kGroups = kThreads / TPR;          // rows of a CTA at a time
+  static constexpr int kWarps = kThreads / 32;
+  static constexpr int kCapacity = TPR * V * NV;
+  // Shared memory of the backward kernel: four rows' x and dy per group while it runs (three where
+  // four are too many; none are copied ahead element by element), the sums of the CTA's columns at
+  // its end.
+  static constexpr size_t kAhead = (size_t)2 * NV * kThreads * 16;
+  static constexpr int kDepth = 4 * kAhead > 200 * 1024 ? 3 : 4;
+  static constexpr size_t kRing = V > 1 ? kDepth * kAhead : 0, kSums = (size_t)2 * kCapacity * 4;
+  static constexpr size_t kBwdSmem = kRing > kSums ? kRing : kSums;
+};
 
-// Sum over the CTA's threads, in every thread.
-__device__ __forceinline__ float cta_sum(float v, float* red) {
+template <typename T, int V>
+__device__ __forceinline__ void load_vec(float (&v)[V], const T* p, int left) {
+  if (V > 1 && left >= V) {
+    const Pack<T, V> q = *reinterpret_cast<const Pack<T, V>*>(p);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x / 32] = v;
-  __syncthreads();
-  v = 0.f;
+    for (int i = 0; i < V; ++i) v[i] = to_f32(q.v[i]);
+  } else {
 #pragma unroll
-  for (int k = 0; k < kNormThreads / 32; ++k) v += red[k];
-  return v;
+    for (int i = 0; i < V; ++i) v[i] = i < left ? to_f32(p[i]) : 0.f;
+  }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T* p, const float (&v)[V], int left) {
+  if (V > 1 && left >= V) {
+    Pack<T, V> q;
+#pragma unroll
+    for (int i = 0; i < V; ++i) q.v[i] = from_f32<T>(v[i]);
+    *reinterpret_cast<Pack<T, V>*>(p) = q;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < left) p[i] = from_f32<T>(v[i]);
+  }
+}
+// V elements of a weight vector of T or fp32, `none` where there is no vector.
+template <typename T, int V>
+__device__ __forceinline__ void load_weight(float (&v)[V], const void* w, int wide, int c, int left, float none) {
+  if (!w) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = none;
+  } else if (wide && V % 4 == 0 && left >= V && ((uintptr_t)w & 15) == 0) {
+#pragma unroll
+    for (int i = 0; i < V / 4 * 4; i += 4) {
+      const float4 q = __ldg(reinterpret_cast<const float4*>((const float*)w + c + i));
+      v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+    }
+  } else if (wide) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = i < left ? __ldg((const float*)w + c + i) : 0.f;
+  } else if (V > 1 && left >= V && ((uintptr_t)w & (sizeof(T) * V - 1)) == 0) {
+    load_vec<T, V>(v, (const T*)w + c, V);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = i < left ? to_f32(((const T*)w)[c + i]) : 0.f;
+  }
 }
 
-// One CTA per row.
-template <typename T, typename W>
-__global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const __grid_constant__ NormArgs a) {
+// Sums of a and b over the TPR threads of a row, in each of them.  Rows of several warps meet in
+// red (turn: which half of it this row uses; a row's use ends before the next but one begins).
+template <int TPR>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float2 (*red)[32], int turn) {
+#pragma unroll
+  for (int o = (TPR < 32 ? TPR : 32) / 2; o; o >>= 1) {
+    a += __shfl_xor_sync(~0u, a, o);
+    b += __shfl_xor_sync(~0u, b, o);
+  }
+  if constexpr (TPR > 32) {
+    constexpr int WARPS = TPR / 32;
+    const int w = threadIdx.x / 32, first = w / WARPS * WARPS;
+    if ((threadIdx.x & 31) == 0) red[turn][w] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int k = 0; k < WARPS; ++k) {
+      a += red[turn][first + k].x;
+      b += red[turn][first + k].y;
+    }
+  }
+}
+
+template <typename T, typename R>
+__global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_constant__ NormArgs a) {
+  constexpr int V = R::V, NV = R::NV, TPR = R::TPR;
+  __shared__ float2 red[2][32];
   pdl_wait();
-  __shared__ float red[kNormThreads / 32];
+  const int lane = threadIdx.x % TPR;
+  const long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR;
+  const bool in = r < a.rows;
+  const T* x = (const T*)a.x + r * a.sx;
+  float v[NV][V];
+  float s = 0.f, unused = 0.f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * TPR + lane) * V;
+    load_vec<T, V>(v[j], x + c, in ? a.cols - c : 0);
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < V; ++i) s += v[j][i];
+  row_sum2<TPR>(s, unused, red, 0);
+  const float mean = s / (float)a.cols;
+  float q = 0.f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      v[j][i] -= mean;
+      if ((j * TPR + lane) * V + i < a.cols) q += v[j][i] * v[j][i];
+    }
+  row_sum2<TPR>(q, unused, red, 1);
+  const float rstd = rsqrtf(q / (float)a.cols + a.eps);
+  if (!in) return;
+  T* y = (T*)a.y + r * a.sy;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * TPR + lane) * V, left = a.cols - c;
+    if (left <= 0) break;
+    float w[V], b[V];
+    load_weight<T, V>(w, a.w, a.wide_w, c, left, 1.f);
+    load_weight<T, V>(b, a.b, a.wide_w, c, left, 0.f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[j][i] = v[j][i] * rstd * w[i] + b[i];
+    store_vec<T, V>(y + c, v[j], left);
+  }
+  if (a.mean && lane == 0) {
+    a.mean[r] = mean;
+    a.rstd[r] = rstd;
+  }
+}
+
+// Asynchronous copy of min(16, bytes) bytes to 16 bytes of shared memory, zeros after them.
+__device__ __forceinline__ void copy16(void* dst, const void* src, int bytes) {
+  const unsigned d = (unsigned)__cvta_generic_to_shared(dst);
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(bytes < 16 ? bytes : 16) : "memory");
+}
+
+template <typename T, typename R>
+__global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_constant__ NormArgs a) {
+  constexpr int V = R::V, NV = R::NV, TPR = R::TPR, kDepth = R::kDepth;
+  extern __shared__ char smem[];
+  __shared__ float2 red[2][32];
+  pdl_wait();
+  const int lane = threadIdx.x % TPR;
+  const long long first = (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR;
+  const long long step = (long long)gridDim.x * R::kGroups;
+  const long long turns = (a.rows - (long long)blockIdx.x * R::kGroups + step - 1) / step;   // alike in the CTA
+  // the thread's own 16-byte slots: [depth][x, dy][NV][thread]
+  auto slot = [&](int d, int which, int j) { return smem + ((((size_t)d * 2 + which) * NV + j) * R::kThreads + threadIdx.x) * 16; };
+  auto fetch = [&](long long t) {
+    if (V > 1 && t < turns) {
+      const long long r = first + t * step;
+      const int d = (int)(t % kDepth);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int c = (j * TPR + lane) * V, bytes = r < a.rows ? (a.cols - c) * (int)sizeof(T) : 0;
+        if (bytes > 0) {
+          copy16(slot(d, 0, j), (const T*)a.x + r * a.sx + c, bytes);
+          copy16(slot(d, 1, j), (const T*)a.dy + r * a.sdy + c, bytes);
+        }
+      }
+    }
+    if (V > 1) asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  float dw[NV][V] = {}, db[NV][V] = {};
+#pragma unroll
+  for (int d = 0; d < kDepth - 1; ++d) fetch(d);
+  const float inv = 1.f / (float)a.cols;
+  for (long long t = 0; t < turns; ++t) {
+    fetch(t + kDepth - 1);
+    const long long r = first + t * step;
+    const bool in = r < a.rows;
+    const float mean = in ? a.mean[r] : 0.f, rstd = in ? a.rstd[r] : 0.f;
+    if (V > 1) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+    float xh[NV][V], g[NV][V];
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (j * TPR + lane) * V, left = in ? a.cols - c : 0;
+      float w[V];
+      load_weight<T, V>(w, left > 0 ? a.w : nullptr, a.wide_w, c, left, 1.f);
+      if (V > 1) {
+        const int d = (int)(t % kDepth);
+        load_vec<T, V>(xh[j], (const T*)slot(d, 0, j), left > 0 ? V : 0);
+        load_vec<T, V>(g[j], (const T*)slot(d, 1, j), left > 0 ? V : 0);
+      } else {
+        load_vec<T, V>(xh[j], (const T*)a.x + r * a.sx + c, left);
+        load_vec<T, V>(g[j], (const T*)a.dy + r * a.sdy + c, left);
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        xh[j][i] = i < left ? (xh[j][i] - mean) * rstd : 0.f;
+        dw[j][i] += g[j][i] * xh[j][i];
+        db[j][i] += g[j][i];
+        g[j][i] *= w[i];
+        s1 += g[j][i];
+        s2 += g[j][i] * xh[j][i];
+      }
+    }
+    row_sum2<TPR>(s1, s2, red, (int)(t & 1));
+    s1 *= inv;
+    s2 *= inv;
+    if (a.y && in) {
+      T* dx = (T*)a.y + r * a.sy;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int c = (j * TPR + lane) * V, left = a.cols - c;
+        if (left <= 0) break;
+        float v[V] = {};
+        if (a.res) load_vec<T, V>(v, (const T*)a.res + r * a.sres + c, left);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] += rstd * (g[j][i] - s1 - xh[j][i] * s2);
+        store_vec<T, V>(dx + c, v, left);
+      }
+    }
+  }
+  // the CTA's sums: rows that share a warp by shuffles, then the warps of a column one after another
+  if (V > 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  float* sums = (float*)smem;
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int o = 16; o >= TPR; o >>= 1) {
+        dw[j][i] += __shfl_xor_sync(~0u, dw[j][i], o);
+        db[j][i] += __shfl_xor_sync(~0u, db[j][i], o);
+      }
+  constexpr int ROUNDS = TPR > 32 ? R::kGroups : R::kWarps;
+  const int mine = TPR > 32 ? threadIdx.x / TPR : threadIdx.x / 32;
+  const bool one = TPR >= 32 || (threadIdx.x & 31) < TPR;
+  for (int k = 0; k < ROUNDS; ++k) {
+    __syncthreads();
+    if (mine != k || !one) continue;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = (j * TPR + lane) * V + i;
+        sums[c] = (k ? sums[c] : 0.f) + dw[j][i];
+        sums[R::kCapacity + c] = (k ? sums[R::kCapacity + c] : 0.f) + db[j][i];
+      }
+  }
+  __syncthreads();
+  float* part = a.part + (long long)blockIdx.x * 2 * a.cols;
+  for (int c = threadIdx.x; c < a.cols; c += R::kThreads) {
+    part[c] = sums[c];
+    part[a.cols + c] = sums[R::kCapacity + c];
+  }
+}
+
+// Rows too long for registers: one CTA per row, read again for each use (from L2).
+constexpr int kLongThreads = 1024;
+
+template <typename T>
+__global__ void __launch_bounds__(kLongThreads) norm_fwd_long_kernel(const __grid_constant__ NormArgs a) {
+  pdl_wait();
+  __shared__ float2 red[2][32];
   for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* x = (const T*)a.x + r * a.sx;
     T* y = (T*)a.y + r * a.sy;
-    float s = 0.f;
-    for (int c = threadIdx.x; c < a.cols; c += kNormThreads) s += to_f32(x[c]);
-    const float mean = cta_sum(s, red) / (float)a.cols;
-    float q = 0.f;
-    for (int c = threadIdx.x; c < a.cols; c += kNormThreads) {
+    float s = 0.f, q = 0.f, unused = 0.f;
+    for (int c = threadIdx.x; c < a.cols; c += kLongThreads) s += to_f32(x[c]);
+    row_sum2<kLongThreads>(s, unused, red, 0);
+    const float mean = s / (float)a.cols;
+    for (int c = threadIdx.x; c < a.cols; c += kLongThreads) {
       const float d = to_f32(x[c]) - mean;
       q += d * d;
     }
-    const float rstd = rsqrtf(cta_sum(q, red) / (float)a.cols + a.eps);
-    for (int c = threadIdx.x; c < a.cols; c += kNormThreads) {
-      const float w = a.w ? to_f32(((const W*)a.w)[c]) : 1.f, b = a.b ? to_f32(((const W*)a.b)[c]) : 0.f;
-      y[c] = from_f32<T>((to_f32(x[c]) - mean) * rstd * w + b);
+    row_sum2<kLongThreads>(q, unused, red, 1);
+    const float rstd = rsqrtf(q / (float)a.cols + a.eps);
+    for (int c = threadIdx.x; c < a.cols; c += kLongThreads) {
+      float w[1], b[1];
+      load_weight<T, 1>(w, a.w, a.wide_w, c, 1, 1.f);
+      load_weight<T, 1>(b, a.b, a.wide_w, c, 1, 0.f);
+      y[c] = from_f32<T>((to_f32(x[c]) - mean) * rstd * w[0] + b[0]);
     }
     if (a.mean && threadIdx.x == 0) {
       a.mean[r] = mean;
@@ -71,59 +328,89 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_kernel(const __grid_con
   }
 }
 
-template <typename T, typename W>
-__global__ void __launch_bounds__(kNormThreads) norm_bwd_kernel(const __grid_constant__ NormArgs a) {
+template <typename T>
+__global__ void __launch_bounds__(kLongThreads) norm_bwd_long_kernel(const __grid_constant__ NormArgs a) {
   pdl_wait();
-  __shared__ float red[kNormThreads / 32];
+  __shared__ float2 red[2][32];
   float* pw = a.part + (long long)blockIdx.x * 2 * a.cols;
   float* pb = pw + a.cols;
-  for (int c = threadIdx.x; c < a.cols; c += kNormThreads) pw[c] = pb[c] = 0.f;
-  for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
+  for (int c = threadIdx.x; c < a.cols; c += kLongThreads) pw[c] = pb[c] = 0.f;
+  const float inv = 1.f / (float)a.cols;
+  int turn = 0;
+  for (long long r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
     const T* x = (const T*)a.x + r * a.sx;
     const T* dy = (const T*)a.dy + r * a.sdy;
     T* dx = (T*)a.y + r * a.sy;
     const float mean = a.mean[r], rstd = a.rstd[r];
     float s1 = 0.f, s2 = 0.f;
-    for (int c = threadIdx.x; c < a.cols; c += kNormThreads) {
+    for (int c = threadIdx.x; c < a.cols; c += kLongThreads) {
       const float d = to_f32(dy[c]), xh = (to_f32(x[c]) - mean) * rstd;
-      const float g = a.w ? d * to_f32(((const W*)a.w)[c]) : d;
-      s1 += g;
-      s2 += g * xh;
+      float w[1];
+      load_weight<T, 1>(w, a.w, a.wide_w, c, 1, 1.f);
+      s1 += d * w[0];
+      s2 += d * w[0] * xh;
       pw[c] += d * xh;
       pb[c] += d;
     }
-    s1 = cta_sum(s1, red) / (float)a.cols;
-    s2 = cta_sum(s2, red) / (float)a.cols;
+    row_sum2<kLongThreads>(s1, s2, red, turn);
+    s1 *= inv;
+    s2 *= inv;
     if (a.y)
-      for (int c = threadIdx.x; c < a.cols; c += kNormThreads) {
+      for (int c = threadIdx.x; c < a.cols; c += kLongThreads) {
         const float d = to_f32(dy[c]), xh = (to_f32(x[c]) - mean) * rstd;
-        const float g = a.w ? d * to_f32(((const W*)a.w)[c]) : d;
+        float w[1];
+        load_weight<T, 1>(w, a.w, a.wide_w, c, 1, 1.f);
         const float res = a.res ? to_f32(((const T*)a.res)[r * a.sres + c]) : 0.f;
-        dx[c] = from_f32<T>(rstd * (g - s1 - xh * s2) + res);
+        dx[c] = from_f32<T>(rstd * (d * w[0] - s1 - xh * s2) + res);
       }
   }
 }
 
-// dw and db from the CTAs' sums, in the order of the CTAs: one thread per column.
+// dw and db from the CTAs' sums: 32 columns per CTA, 32 runs of consecutive CTAs added side by side
+// and then in their order.
 template <typename W>
-__global__ void __launch_bounds__(128) norm_sum_kernel(const float* part, int ctas, int cols, W* dw, W* db) {
+__global__ void __launch_bounds__(1024) norm_sum_kernel(const float* part, int ctas, int cols, W* dw, W* db) {
   pdl_wait();
-  const int c = blockIdx.x * 128 + threadIdx.x;
-  if (c >= cols) return;
-  float w = 0.f, b = 0.f;
-  for (int k = 0; k < ctas; ++k) {
-    w += part[(long long)k * 2 * cols + c];
-    b += part[(long long)k * 2 * cols + cols + c];
+  __shared__ float run[32][33];
+  const int lane = threadIdx.x & 31, k = threadIdx.x / 32;
+  const int c = blockIdx.x * 32 + lane;            // of [dw | db]
+  float s = 0.f;
+  if (c < 2 * cols) {
+    const int k0 = ctas * k / 32, k1 = ctas * (k + 1) / 32;
+#pragma unroll 4
+    for (int q = k0; q < k1; ++q) s += part[(long long)q * 2 * cols + c];
   }
-  if (dw) dw[c] = from_f32<W>(w);
-  if (db) db[c] = from_f32<W>(b);
+  run[k][lane] = s;
+  __syncthreads();
+  if (k || c >= 2 * cols) return;
+  s = 0.f;
+#pragma unroll
+  for (int q = 0; q < 32; ++q) s += run[q][lane];
+  W* out = c < cols ? dw : db;
+  if (out) out[c < cols ? c : c - cols] = from_f32<W>(s);
 }
 
-// Calls f(T(), W()) with the matrices' type and the weights'.
-template <typename F> abcd_status with_types(int dtype, int wtype, F&& f) {
-  return with_type(dtype, [&](auto t) {
-    return wtype == ABCD_F32 ? f(t, float()) : f(t, decltype(t)());
-  });
+constexpr int kNormCtasPerSm = 4;
+
+// Calls f with the row shape for `cols` columns of T: the fewest threads whose registers hold a row;
+// f of an int where none does.
+template <typename T, typename F> abcd_status with_shape(long long cols, bool aligned, F&& f) {
+  if (aligned) {
+    constexpr int V = 16 / sizeof(T), W = sizeof(T) / 2;    // f32: twice the accesses of 16 bytes
+    if (cols <= 8 * V) return f(RowShape<8, V, 1>());
+    if (cols <= 16 * V) return f(RowShape<16, V, 1>());
+    if (cols <= 32 * V) return f(RowShape<32, V, 1>());
+    if (cols <= 64 * V) return f(RowShape<32, V, 2>());
+    if (cols <= 32 * V * 4 * W) return f(RowShape<32, V, 4 * W>());
+    if (cols <= 128 * V * 4 * W) return f(RowShape<128, V, 4 * W>());
+    if (cols <= 512 * V * 2 * W) return f(RowShape<512, V, 2 * W>());
+  } else {
+    if (cols <= 64) return f(RowShape<32, 1, 2>());
+    if (cols <= 256) return f(RowShape<32, 1, 8>());
+    if (cols <= 2048) return f(RowShape<256, 1, 8>());
+    if (cols <= 8192) return f(RowShape<1024, 1, 8>());
+  }
+  return f(0);
 }
 
 bool weights_ok(const abcd_matrix* x, int wtype, const void* a, const void* b) {
@@ -133,7 +420,7 @@ bool weights_ok(const abcd_matrix* x, int wtype, const void* a, const void* b) {
 
 }  // namespace
 
-int norm_bwd_ctas(int num_sms) { return 2 * num_sms; }
+int norm_bwd_ctas(int num_sms) { return kNormCtasPerSm * num_sms; }
 
 }  // namespace abcd
 
@@ -151,12 +438,19 @@ extern "C" abcd_status abcd_layer_norm(abcd_ctx* ctx, const abcd_matrix* x, cons
     return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_layer_norm: bad eps or statistics");
   if (x->rows == 0) return ABCD_OK;
   const NormArgs a{x->data, nullptr, weight, bias, y->data, nullptr, mean, rstd, nullptr, x->rows,
-                   (int)x->cols, x->stride, 0, y->stride, 0, eps};
-  const unsigned grid = (unsigned)std::min<long long>(x->rows, 16LL * ctx->num_sms);
-  return with_types(x->dtype, weight_dtype, [&](auto t, auto w) {
-    return check_launch(ctx, "norm_fwd_kernel",
-                        launch_pdl(norm_fwd_kernel<decltype(t), decltype(w)>, dim3(grid),
-                                   dim3(kNormThreads), 0, ctx->stream, a));
+                   (int)x->cols, x->stride, 0, y->stride, 0, eps, weight_dtype == ABCD_F32};
+  return with_type(x->dtype, [&](auto t) {
+    using T = decltype(t);
+    return with_shape<T>(x->cols, rows_aligned(x, 16) && rows_aligned(y, 16), [&](auto shape) {
+      using R = decltype(shape);
+      if constexpr (std::is_same_v<R, int>) {
+        const unsigned grid = (unsigned)std::min<long long>(x->rows, 2LL * ctx->num_sms);
+        return check_launch(ctx, "norm_fwd_long_kernel", launch_pdl(norm_fwd_long_kernel<T>, dim3(grid), dim3(kLongThreads), 0, ctx->stream, a));
+      } else {
+        const unsigned grid = (unsigned)((x->rows + R::kGroups - 1) / R::kGroups);
+        return check_launch(ctx, "norm_fwd_kernel", launch_pdl(norm_fwd_kernel<T, R>, dim3(grid), dim3(R::kThreads), 0, ctx->stream, a));
+      }
+    });
   });
 }
 
@@ -174,25 +468,49 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
     return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_layer_norm_backward: bad weight or gradients");
   if (x->rows > 0 && (!mean || !rstd))
     return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_layer_norm_backward: no statistics");
-  const int ctas = (int)std::min<long long>(x->rows, norm_bwd_ctas(std::min(ctx->num_sms, kNetSms)));
+  const int sms = std::min(ctx->num_sms, kNetSms);
   float* part = (float*)(ctx->net_base + kNetHeader);
-  const size_t need = kNetHeader + (size_t)ctas * 2 * (size_t)x->cols * sizeof(float);
-  if (need > ctx->net_bytes)
-    return fail(ctx, ABCD_ERR_WORKSPACE, "abcd_layer_norm_backward: the network workspace has %zu bytes, needs %zu", ctx->net_bytes, need);
-  const NormArgs a{x->data, dy->data, weight, nullptr, dx ? dx->data : nullptr,
-                   d_residual ? d_residual->data : nullptr, (float*)mean, (float*)rstd,
-                   part, x->rows, (int)x->cols, x->stride, dy->stride,
-                   dx ? dx->stride : 0, d_residual ? d_residual->stride : 0, 0.f};
-  return with_types(x->dtype, weight_dtype, [&](auto t, auto w) {
-    abcd_status st = ABCD_OK;
-    if (ctas > 0)
-      st = check_launch(ctx, "norm_bwd_kernel",
-                        launch_pdl(norm_bwd_kernel<decltype(t), decltype(w)>, dim3(ctas),
-                                   dim3(kNormThreads), 0, ctx->stream, a));
-    if (st != ABCD_OK || (!dweight && !dbias)) return st;
-    return check_launch(ctx, "norm_sum_kernel",
-                        launch_pdl(norm_sum_kernel<decltype(w)>, dim3((unsigned)((x->cols + 127) / 128)),
-                                   dim3(128), 0, ctx->stream, (const float*)part, ctas,
-                                   (int)x->cols, (decltype(w)*)dweight, (decltype(w)*)dbias));
+  const bool aligned = rows_aligned(x, 16) && rows_aligned(dy, 16) && (!dx || rows_aligned(dx, 16)) &&
+                       (!d_residual || rows_aligned(d_residual, 16));
+  NormArgs a{x->data, dy->data, weight, nullptr, dx ? dx->data : nullptr, d_residual ? d_residual->data : nullptr,
+             (float*)mean, (float*)rstd, part, x->rows, (int)x->cols, x->stride, dy->stride, dx ? dx->stride : 0,
+             d_residual ? d_residual->stride : 0, 0.f, weight_dtype == ABCD_F32};
+  int ctas = 0;
+  const abcd_status st = with_type(x->dtype, [&](auto t) {
+    using T = decltype(t);
+    return with_shape<T>(x->cols, aligned, [&](auto shape) {
+      using R = decltype(shape);
+      // CTAs: as many rows at a time as stay resident, each with its sums in the workspace
+      constexpr bool kLong = std::is_same_v<R, int>;
+      if constexpr (kLong) {
+        ctas = (int)std::min<long long>(x->rows, 2LL * sms);
+      } else {
+        constexpr int kElems = R::V * R::NV;
+        const long long per_sm = R::kThreads > 256 ? 1 : kElems <= 8 ? kNormCtasPerSm : kElems <= 16 ? 2 : 1;
+        ctas = (int)std::min<long long>((x->rows + R::kGroups - 1) / R::kGroups, per_sm * sms);
+      }
+      const size_t need = kNetHeader + (size_t)ctas * 2 * (size_t)x->cols * sizeof(float);
+      if (need > ctx->net_bytes)
+        return fail(ctx, ABCD_ERR_WORKSPACE, "abcd_layer_norm_backward: the network workspace has %zu bytes, needs %zu", ctx->net_bytes, need);
+      if (ctas == 0) return ABCD_OK;
+      if constexpr (kLong) {
+        return check_launch(ctx, "norm_bwd_long_kernel", launch_pdl(norm_bwd_long_kernel<T>, dim3(ctas), dim3(kLongThreads), 0, ctx->stream, a));
+      } else {
+        auto* kernel = norm_bwd_kernel<T, R>;
+        constexpr size_t kSmem = R::kBwdSmem;
+        if (kSmem > 48 * 1024 - 1024) {
+          const cudaError_t e = allow_smem(ctx, (const void*)kernel);
+          if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "norm_bwd_kernel: %s", cudaGetErrorString(e));
+        }
+        return check_launch(ctx, "norm_bwd_kernel", launch_pdl(kernel, dim3(ctas), dim3(R::kThreads), kSmem, ctx->stream, a));
+      }
+    });
+  });
+  if (st != ABCD_OK || (!dweight && !dbias)) return st;
+  const dim3 grid((unsigned)((2 * x->cols + 31) / 32));
+  return with_type(weight_dtype, [&](auto w) {
+    using W = decltype(w);
+    return check_launch(ctx, "norm_sum_kernel", launch_pdl(norm_sum_kernel<W>, grid, dim3(1024), 0, ctx->stream,
+                                                           (const float*)part, ctas, (int)x->cols, (W*)dweight, (W*)dbias));
   });
 }
