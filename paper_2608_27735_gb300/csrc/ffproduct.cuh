@@ -10,7 +10,7 @@
 // What bounds it: the tensor cores for wide layers, HBM (the hidden matrices) for narrow ones, the
 // weights' bytes for few tokens.  Layout: a persistent grid, one CTA (or pair of CTAs, which share a
 // 256 x 256 tile: each stages half of B) per SM; one warp issues the TMA loads of 128-byte swizzled
-// tiles into a ring of stages, one the tcgen05 matrix instructions, eight warps turn the sums that
+// tiles into a ring of stages, one the tcgen05 matrix instructions, the others turn the sums that
 // lie in tensor memory into results while the next tile's are made in its other half.  Where the
 // tiles do not fill the SMs, k is split: each part leaves its 32-bit sums in the workspace, and the
 // warp that comes last adds the parts in their order, so that the result does not depend on who
@@ -26,9 +26,6 @@ enum { kPlain, kUp, kDown };          // what becomes of the sums, see store()
 
 constexpr int kMaxSegments = 12;
 constexpr int kBlockK = 64;           // elements of k per stage: 128 bytes, the swizzle's row
-constexpr int kFfThreads = 320;       // TMA warp, MMA warp, eight epilogue warps
-constexpr int kEpilogueWarps = 8;
-constexpr size_t kStageBuffer = 4096; // bytes in which an epilogue warp turns its rows round
 
 // A result: a matrix of the call (one 32-bit or 16-bit value per element), or an operand of a later
 // product (terms planes of 16-bit values).
@@ -58,25 +55,68 @@ struct ProductArgs {
   unsigned limit;                     // polls of a wait
 };
 
-// SiLU in terms of the sigmoid, GELU of the error function; the slopes are their derivatives.
-__device__ __forceinline__ float sigmoid_of(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
-__device__ __forceinline__ float act_value(float z, int act) {
-  if (act == ABCD_SILU) return z * sigmoid_of(z);
-  if (act == ABCD_GELU) return z * (0.5f + 0.5f * erff(z * 0.70710678f));
-  return z > 0.f ? z : (z == z ? 0.f : z);
+// The activations and their slopes.  The device's approximations of 2^x and 1/x, each within a few
+// units of 2^-23, are enough for sums whose terms were rounded to as much.
+__device__ __forceinline__ float exp2_of(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
-__device__ __forceinline__ void act_both(float z, int act, float& value, float& slope) {
+__device__ __forceinline__ float inverse_of(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float sigmoid_of(float z) { return inverse_of(1.f + exp2_of(-1.44269504f * z)); }
+// The normal distribution's Phi(z) and e = exp(-z^2 / 2): Abramowitz and Stegun, Handbook of
+// Mathematical Functions, 7.1.26 (erf within 1.5e-7), with x = |z| / sqrt(2).
+__device__ __forceinline__ float phi_of(float z, float& e) {
+  const float x = fabsf(z) * 0.70710678f;
+  const float t = inverse_of(1.f + 0.3275911f * x);
+  e = exp2_of(-0.72134752f * z * z);
+  const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+  return z < 0.f ? tail : 1.f - tail;
+}
+__device__ __forceinline__ float relu_of(float z) { return z > 0.f ? z : (z == z ? 0.f : z); }
+
+template <int N> __device__ __forceinline__ void act_values(float (&z)[N], int act) {
   if (act == ABCD_SILU) {
-    const float s = sigmoid_of(z);
-    value = z * s;
-    slope = s + value * (1.f - s);
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] *= sigmoid_of(z[i]);
   } else if (act == ABCD_GELU) {
-    const float c = 0.5f + 0.5f * erff(z * 0.70710678f);
-    value = z * c;
-    slope = c + z * 0.39894228f * __expf(-0.5f * z * z);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float e;
+      z[i] *= phi_of(z[i], e);
+    }
   } else {
-    value = z > 0.f ? z : (z == z ? 0.f : z);
-    slope = z > 0.f ? 1.f : 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = relu_of(z[i]);
+  }
+}
+// z becomes act(z), s its slope.
+template <int N> __device__ __forceinline__ void act_slopes(float (&z)[N], float (&s)[N], int act) {
+  if (act == ABCD_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float g = sigmoid_of(z[i]), v = z[i] * g;
+      s[i] = g + v * (1.f - g);
+      z[i] = v;
+    }
+  } else if (act == ABCD_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float e;
+      const float c = phi_of(z[i], e);
+      s[i] = c + z[i] * 0.39894228f * e;
+      z[i] *= c;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      s[i] = z[i] > 0.f ? 1.f : 0.f;
+      z[i] = relu_of(z[i]);
+    }
   }
 }
 
@@ -139,10 +179,10 @@ __device__ __forceinline__ void store_words(const unsigned (&w)[WORDS], char* bu
 }
 
 // v as values of the call's type, to rows m... of matrix o from column n on.
-template <int CW>
+template <bool F32, int CW>
 __device__ __forceinline__ void store_matrix(const float (&v)[CW], const Out& o, long long m, int n,
-                                             int rows, int cols, int dtype, char* buf) {
-  if (dtype == ABCD_F32) {
+                                             int rows, int cols, bool bf16, char* buf) {
+  if constexpr (F32) {
     unsigned w[CW];
 #pragma unroll
     for (int i = 0; i < CW; ++i) w[i] = __float_as_uint(v[i]);
@@ -150,38 +190,40 @@ __device__ __forceinline__ void store_matrix(const float (&v)[CW], const Out& o,
   } else {
     unsigned w[CW / 2];
 #pragma unroll
-    for (int i = 0; i < CW / 2; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], dtype == ABCD_BF16);
+    for (int i = 0; i < CW / 2; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], bf16);
     store_words<CW / 2>(w, buf, (unsigned short*)o.p + m * o.stride + n, o.stride * 2, rows, cols * 2, o.vec, 2);
   }
 }
 
 // v as an operand of a later product: of the 16-bit types the values, of 32 bits three terms.
-template <int CW>
+template <bool F32, int CW>
 __device__ __forceinline__ void store_operand(const float (&v)[CW], const Out& o, long long m, int n,
-                                              int rows, int cols, int dtype, char* buf) {
-  if (dtype != ABCD_F32) return store_matrix<CW>(v, o, m, n, rows, cols, dtype, buf);
-  float rest[CW];
+                                              int rows, int cols, bool bf16, char* buf) {
+  if constexpr (!F32) {
+    store_matrix<false, CW>(v, o, m, n, rows, cols, bf16, buf);
+  } else {
+    float rest[CW];
 #pragma unroll
-  for (int i = 0; i < CW; ++i) rest[i] = v[i];
+    for (int i = 0; i < CW; ++i) rest[i] = v[i];
 #pragma unroll 1
-  for (int t = 0; t < 3; ++t) {
-    unsigned w[CW / 2];
+    for (int t = 0; t < 3; ++t) {
+      unsigned w[CW / 2];
 #pragma unroll
-    for (int i = 0; i < CW / 2; ++i) {
-      const float a = take_term(rest[2 * i]), b = take_term(rest[2 * i + 1]);
-      w[i] = pack2(a, b, true);
+      for (int i = 0; i < CW / 2; ++i) {
+        const float a = take_term(rest[2 * i]), b = take_term(rest[2 * i + 1]);
+        w[i] = pack2(a, b, true);
+      }
+      store_words<CW / 2>(w, buf, (unsigned short*)o.p + t * o.plane + m * o.stride + n, o.stride * 2, rows,
+                          cols * 2, o.vec, 2);
     }
-    store_words<CW / 2>(w, buf, (unsigned short*)o.p + t * o.plane + m * o.stride + n, o.stride * 2, rows,
-                        cols * 2, o.vec, 2);
   }
 }
 
 // Row m's CW values from column n on (lanes past the matrix get zeros).
-template <int CW>
+template <bool F32, int CW>
 __device__ __forceinline__ void load_row(float (&v)[CW], const Out& o, long long m, int n, bool in,
-                                         int cols, int dtype) {
-  const bool bf16 = dtype == ABCD_BF16;
-  if (dtype == ABCD_F32) {
+                                         int cols, bool bf16) {
+  if constexpr (F32) {
     const float* p = (const float*)o.p + m * o.stride + n;
 #pragma unroll
     for (int i = 0; i < CW; i += 4) {
@@ -241,8 +283,9 @@ __device__ __forceinline__ Item item_of(const ProductArgs& a, int i) {
 }
 
 // CG: CTAs that share a tile (1 or 2) of 128 CG rows and BN sums per row; AMN, BMN: whether the
-// operand lies with its own dimension contiguous instead of k; EPI: what becomes of the sums.
-template <int CG, int BN, bool AMN, bool BMN, int EPI>
+// operand lies with its own dimension contiguous instead of k; EPI: what becomes of the sums; F32:
+// whether the call's matrices are in 32 bits.
+template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
 struct Product {
   static constexpr int kRows = 128;                      // rows of A per CTA
   static constexpr int kBRows = BN / CG;                 // rows of B per CTA
@@ -251,14 +294,20 @@ struct Product {
   static constexpr int kStages = 196608 / kStageBytes > 8 ? 8 : 196608 / kStageBytes;
   static constexpr int kTmemCols = 2 * BN;
   static constexpr int kOutCols = EPI == kUp ? BN / 2 : BN;   // results per row of a tile
-  static constexpr int kWarpCols = kOutCols / 2;         // results per row of an epilogue warp
-  static constexpr int CW = kWarpCols < 32 ? 16 : 32;    // taken at a time
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kStageBuffer;
+  // Epilogue warps: each takes 32 rows (a quarter of tensor memory's lanes) and a share of the
+  // columns.  Sixteen for the large tile of 16-bit matrices, whose products of few stages wait for
+  // them.
+  static constexpr int kWarps = BN == 256 && !F32 ? 16 : 8;
+  static constexpr int kThreads = 64 + 32 * kWarps;      // TMA warp, MMA warp, epilogue
+  static constexpr int kWarpCols = kOutCols / (kWarps / 4);
+  static constexpr int CW = EPI != kPlain || kWarpCols < 32 ? 16 : 32;    // taken at a time
+  static constexpr int kBuffer = 32 * CW * (F32 ? 4 : 2);   // in which a warp turns its rows round
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (size_t)kWarps * kBuffer;
 };
 
-template <int CG, int BN, bool AMN, bool BMN, int EPI>
-__global__ void __launch_bounds__(kFfThreads, 1) product_kernel(const __grid_constant__ ProductArgs a) {
-  using P = Product<CG, BN, AMN, BMN, EPI>;
+template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
+__global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads, 1) product_kernel(const __grid_constant__ ProductArgs a) {
+  using P = Product<CG, BN, AMN, BMN, EPI, F32>;
   extern __shared__ char smem_raw[];
   __shared__ uint64_t bars[2 * P::kStages + 4];
   __shared__ uint32_t tmem_base;
@@ -277,7 +326,7 @@ __global__ void __launch_bounds__(kFfThreads, 1) product_kernel(const __grid_con
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(sums_full + 8 * s, 1);
-      mbar_init(sums_empty + 8 * s, kEpilogueWarps * CG);
+      mbar_init(sums_empty + 8 * s, P::kWarps * CG);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_map(&a.a);
@@ -377,27 +426,28 @@ __global__ void __launch_bounds__(kFfThreads, 1) product_kernel(const __grid_con
     }
   } else {
     // a warp reads the quarter of tensor memory's lanes that its number in the CTA gives it
-    const int quarter = warp & 3, half = (warp - 2) / 4, ewarp = warp - 2;
-    char* buffer = buffers + ewarp * kStageBuffer;
+    const int quarter = warp & 3, share = (warp - 2) / 4, ewarp = warp - 2;
+    const bool bf16 = a.dtype == ABCD_BF16;
+    char* buffer = buffers + ewarp * P::kBuffer;
     const uint32_t empty0 = CG == 2 ? at_rank(sums_empty, 0) : sums_empty;
     int buf = 0;
     uint32_t phase = 0;
     for (int i = first; i < items; i += step) {
       const Item it = item_of(a, i);
       const int m = (it.tm * CG + (int)rank) * P::kRows + quarter * 32;   // the warp's first row
-      const int n = it.tn * P::kOutCols + half * P::kWarpCols;
+      const int n = it.tn * P::kOutCols + share * P::kWarpCols;
       const int rows = min(32, a.m - m), cols = min(P::kWarpCols, a.n - n);
       if (!mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead)) break;
       tc_fence_after();
-      const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16) + half * P::kWarpCols;
+      const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16) + share * P::kWarpCols;
       bool mine = rows > 0 && cols > 0;
       float* part = nullptr;
       if (a.splits > 1) {
         // this part's sums to the workspace [column][row]; the last warp to have done so goes on
         constexpr int PARTS = EPI == kUp ? 2 : 1;
-        const long long piece = (long long)CG * kEpilogueWarps * PARTS * P::kWarpCols * 32;
+        const long long piece = (long long)CG * P::kWarps * PARTS * P::kWarpCols * 32;
         part = a.part + (long long)it.tile * a.splits * piece +
-               ((long long)rank * kEpilogueWarps + ewarp) * PARTS * P::kWarpCols * 32 + lane;
+               ((long long)rank * P::kWarps + ewarp) * PARTS * P::kWarpCols * 32 + lane;
         if (mine) {
           float* mypart = part + it.split * piece;
 #pragma unroll 1
@@ -411,7 +461,7 @@ __global__ void __launch_bounds__(kFfThreads, 1) product_kernel(const __grid_con
           __threadfence();
           __syncwarp();
           unsigned done = 0;
-          unsigned* count = a.count + ((long long)it.tile * CG + rank) * kEpilogueWarps + ewarp;
+          unsigned* count = a.count + ((long long)it.tile * CG + rank) * P::kWarps + ewarp;
           if (lane == 0) {
             done = atomicAdd(count, 1u);
             if (done == (unsigned)a.splits - 1) *count = 0;
@@ -426,7 +476,7 @@ __global__ void __launch_bounds__(kFfThreads, 1) product_kernel(const __grid_con
           tmem_load(sums + which * (BN / 2) + c, v);
         } else {
           constexpr int PARTS = EPI == kUp ? 2 : 1;
-          const long long piece = (long long)CG * kEpilogueWarps * PARTS * P::kWarpCols * 32;
+          const long long piece = (long long)CG * P::kWarps * PARTS * P::kWarpCols * 32;
 #pragma unroll
           for (int q = 0; q < P::CW; ++q) v[q] = 0.f;
 #pragma unroll 2
@@ -453,34 +503,33 @@ __global__ void __launch_bounds__(kFfThreads, 1) product_kernel(const __grid_con
               tmem_load_wait(u);
             }
             if (a.g[0].p) {
-              store_matrix<P::CW>(v, a.g[0], m, n + c, rows, w, a.dtype, buffer);
-              store_matrix<P::CW>(u, a.g[1], m, n + c, rows, w, a.dtype, buffer);
+              store_matrix<F32, P::CW>(v, a.g[0], m, n + c, rows, w, bf16, buffer);
+              store_matrix<F32, P::CW>(u, a.g[1], m, n + c, rows, w, bf16, buffer);
             }
+            act_values(v, a.act);
 #pragma unroll
-            for (int q = 0; q < P::CW; ++q) v[q] = act_value(v[q], a.act) * u[q];
-            store_operand<P::CW>(v, a.c[0], m, n + c, rows, w, a.dtype, buffer);
+            for (int q = 0; q < P::CW; ++q) v[q] *= u[q];
+            store_operand<F32, P::CW>(v, a.c[0], m, n + c, rows, w, bf16, buffer);
           } else if (EPI == kDown) {
-            float z[P::CW], u[P::CW];
-            load_row<P::CW>(z, a.in[0], m + lane, n + c, lane < rows, w, a.dtype);
-            load_row<P::CW>(u, a.in[1], m + lane, n + c, lane < rows, w, a.dtype);
+            float z[P::CW], u[P::CW], s[P::CW];
+            load_row<F32, P::CW>(z, a.in[0], m + lane, n + c, lane < rows, w, bf16);
+            load_row<F32, P::CW>(u, a.in[1], m + lane, n + c, lane < rows, w, bf16);
             sum_columns(c, 0, v);
+            act_slopes(z, s, a.act);
             if (a.splits == 1) tmem_load_wait(v);
-            float h[P::CW];
 #pragma unroll
             for (int q = 0; q < P::CW; ++q) {
-              float value, slope;
-              act_both(z[q], a.act, value, slope);
-              h[q] = value * u[q];
-              z[q] = v[q] * u[q] * slope;
-              u[q] = v[q] * value;
+              s[q] *= v[q] * u[q];
+              u[q] *= z[q];                              // the hidden matrix
+              z[q] *= v[q];
             }
-            store_operand<P::CW>(h, a.c[0], m, n + c, rows, w, a.dtype, buffer);
-            store_operand<P::CW>(z, a.g[0], m, n + c, rows, w, a.dtype, buffer);
-            store_operand<P::CW>(u, a.g[1], m, n + c, rows, w, a.dtype, buffer);
+            store_operand<F32, P::CW>(s, a.g[0], m, n + c, rows, w, bf16, buffer);
+            store_operand<F32, P::CW>(z, a.g[1], m, n + c, rows, w, bf16, buffer);
+            store_operand<F32, P::CW>(u, a.c[0], m, n + c, rows, w, bf16, buffer);
           } else {
             sum_columns(c, 0, v);
             if (a.splits == 1) tmem_load_wait(v);
-            store_matrix<P::CW>(v, a.c[it.batch], m, n + c, rows, w, a.dtype, buffer);
+            store_matrix<F32, P::CW>(v, a.c[it.batch], m, n + c, rows, w, bf16, buffer);
           }
         }
       }
@@ -505,17 +554,17 @@ __global__ void __launch_bounds__(kFfThreads, 1) product_kernel(const __grid_con
   if (threadIdx.x == 0 && dead) atomicOr(a.status, kStatusTimeout);
 }
 
-template <int CG, int BN, bool AMN, bool BMN, int EPI>
+template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
 abcd_status launch_product(abcd_ctx* ctx, const ProductArgs& a) {
-  using P = Product<CG, BN, AMN, BMN, EPI>;
-  auto* kernel = product_kernel<CG, BN, AMN, BMN, EPI>;
+  using P = Product<CG, BN, AMN, BMN, EPI, F32>;
+  auto* kernel = product_kernel<CG, BN, AMN, BMN, EPI, F32>;
   const cudaError_t e = allow_smem(ctx, (const void*)kernel);
   if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "product_kernel: %s", cudaGetErrorString(e));
   const long long items = (long long)a.batches * a.tiles_m * a.tiles_n * a.splits;
   const int units = ctx->num_sms / CG;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(CG * (items < units ? items : units)));
-  cfg.blockDim = dim3(kFfThreads);
+  cfg.blockDim = dim3(P::kThreads);
   cfg.dynamicSmemBytes = P::kSmem;
   cfg.stream = ctx->stream;
   cudaLaunchAttribute attr[2];
@@ -528,5 +577,32 @@ abcd_status launch_product(abcd_ctx* ctx, const ProductArgs& a) {
   cfg.numAttrs = 2;
   return check_launch(ctx, "product_kernel", cudaLaunchKernelEx(&cfg, kernel, a));
 }
+
+// The tiles that the products come in: 256 x 256 on a pair of CTAs, 128 x 128 or 128 x 64 on one.
+struct Shape {
+  int cg, bn;
+  int cycles;                // of a stage (64 of k), about
+};
+constexpr Shape kShapes[3] = {{2, 256, 600}, {1, 128, 550}, {1, 64, 420}};
+
+template <bool AMN, bool BMN, int EPI, bool F32>
+abcd_status launch_shape(abcd_ctx* ctx, int shape, const ProductArgs& a) {
+  if (shape == 0) return launch_product<2, 256, AMN, BMN, EPI, F32>(ctx, a);
+  if (shape == 1) return launch_product<1, 128, AMN, BMN, EPI, F32>(ctx, a);
+  return launch_product<1, 64, AMN, BMN, EPI, F32>(ctx, a);
+}
+
+// The five products of the layer, by what they are of.
+enum { kProductUp, kProductOut, kProductDown, kProductDx, kProductDw };
+template <bool F32> abcd_status launch_any(abcd_ctx* ctx, int which, int shape, const ProductArgs& a) {
+  if (which == kProductUp) return launch_shape<false, false, kUp, F32>(ctx, shape, a);
+  if (which == kProductOut) return launch_shape<false, false, kPlain, F32>(ctx, shape, a);
+  if (which == kProductDown) return launch_shape<false, true, kDown, F32>(ctx, shape, a);
+  if (which == kProductDx) return launch_shape<false, true, kPlain, F32>(ctx, shape, a);
+  return launch_shape<true, true, kPlain, F32>(ctx, shape, a);
+}
+// One translation unit each.
+abcd_status launch_16(abcd_ctx* ctx, int which, int shape, const ProductArgs& a);
+abcd_status launch_32(abcd_ctx* ctx, int which, int shape, const ProductArgs& a);
 
 }  // namespace abcd

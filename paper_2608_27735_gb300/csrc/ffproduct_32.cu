@@ -1,0 +1,10 @@
+// The gated feed-forward layer's products of 32-bit matrices.
+#include "ffproduct.cuh"
+
+namespace abcd {
+
+abcd_status launch_32(abcd_ctx* ctx, int which, int shape, const ProductArgs& a) {
+  return launch_any<true>(ctx, which, shape, a);
+}
+
+}  // namespace abcd

@@ -150,13 +150,6 @@ struct Job {
   ProductArgs args;
 };
 
-// The tiles: 256 x 256 on a pair of CTAs, 128 x 128 or 128 x 64 sums on one.
-struct Shape {
-  int cg, bn;
-  int cycles;                // of a stage (64 of k), about
-};
-constexpr Shape kShapes[3] = {{2, 256, 560}, {1, 128, 300}, {1, 64, 200}};
-
 // Picks the shape and the number of splits with the least estimated time: the waves of tiles times
 // their stages, plus what a tile costs apart from them, plus the splits' joining.
 void plan(int sms, long long m, long long n, int epi, long long kblocks, int segments, long long batches, int* shape, int* splits) {
@@ -178,8 +171,9 @@ void plan(int sms, long long m, long long n, int epi, long long kblocks, int seg
   }
 }
 
-template <bool AMN, bool BMN, int EPI>
-abcd_status run(abcd_ctx* ctx, int dtype, Job& j) {
+abcd_status run(abcd_ctx* ctx, int dtype, int which, Job& j) {
+  const int epi = which == kProductUp ? kUp : which == kProductDown ? kDown : kPlain;
+  const bool amn = which == kProductDw, bmn = amn || which == kProductDown || which == kProductDx;
   ProductArgs& a = j.args;
   const int terms = terms_of(dtype);
   a.m = (int)j.m;
@@ -187,7 +181,7 @@ abcd_status run(abcd_ctx* ctx, int dtype, Job& j) {
   a.kblocks = (int)((j.k + kBlockK - 1) / kBlockK);
   a.segments = 0;
   // pairs of terms, the smallest products first
-  const int pairs = EPI == kUp ? 1 : j.nb;
+  const int pairs = epi == kUp ? 1 : j.nb;
   for (int order = terms - 1; order >= 0; --order)
     for (int b = 0; b < pairs; ++b)
       for (int t = order; t >= 0; --t) {
@@ -199,23 +193,21 @@ abcd_status run(abcd_ctx* ctx, int dtype, Job& j) {
   a.batch_az = terms;
   a.dtype = dtype;
   int shape = 0, splits = 1;
-  plan(std::min(ctx->num_sms, kNetSms), j.m, j.n, EPI, a.kblocks, a.segments, j.batches, &shape, &splits);
+  plan(std::min(ctx->num_sms, kNetSms), j.m, j.n, epi, a.kblocks, a.segments, j.batches, &shape, &splits);
   const int cg = kShapes[shape].cg, bn = kShapes[shape].bn;
   a.tiles_m = (int)((j.m + 128 * cg - 1) / (128 * cg));
-  const int cols = EPI == kUp ? bn / 2 : bn;
+  const int cols = epi == kUp ? bn / 2 : bn;
   a.tiles_n = (int)((j.n + cols - 1) / cols);
   a.splits = splits;
   a.count = (unsigned*)(ctx->net_base + kNetCounters);
   a.part = (float*)(ctx->net_base + kNetHeader);
   a.status = (unsigned*)ctx->net_base;
   a.limit = ctx->wait_limit;
-  bool ok = make_map(&a.a, j.a, dtype, AMN ? 64 : 128);
-  for (int b = 0; ok && b < j.nb; ++b) ok = make_map(&a.b[b], j.b[b], dtype, BMN ? 64 : EPI == kUp ? bn / 2 : bn / cg);
+  bool ok = make_map(&a.a, j.a, dtype, amn ? 64 : 128);
+  for (int b = 0; ok && b < j.nb; ++b) ok = make_map(&a.b[b], j.b[b], dtype, bmn ? 64 : epi == kUp ? bn / 2 : bn / cg);
   if (!ok) return fail(ctx, ABCD_ERR_CUDA, "tensor map of a product");
   if (j.nb < 2) a.b[1] = a.b[0];
-  if (shape == 0) return launch_product<2, 256, AMN, BMN, EPI>(ctx, a);
-  if (shape == 1) return launch_product<1, 128, AMN, BMN, EPI>(ctx, a);
-  return launch_product<1, 64, AMN, BMN, EPI>(ctx, a);
+  return dtype == ABCD_F32 ? launch_32(ctx, which, shape, a) : launch_16(ctx, which, shape, a);
 }
 
 bool shape_is(const abcd_matrix* m, int dtype, long long rows, long long cols) {
@@ -310,10 +302,10 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
     up_job.args.g[0] = out_of(gate);
     up_job.args.g[1] = out_of(up);
   }
-  if ((st = run<false, false, kUp>(ctx, t, up_job)) != ABCD_OK) return st;
+  if ((st = run(ctx, t, kProductUp, up_job)) != ABCD_OK) return st;
   Job y_job{h, {od, od}, 1, m, d, f, 1, {}};
   y_job.args.c[0] = out_of(y);
-  return run<false, false, kPlain>(ctx, t, y_job);
+  return run(ctx, t, kProductOut, y_job);
 }
 
 extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* dy,
@@ -371,11 +363,11 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
   down.args.c[0] = out_of(h, 0, t);
   down.args.g[0] = out_of(dgu, 0, t);
   down.args.g[1] = out_of(dgu, 1, t);
-  if ((st = run<false, true, kDown>(ctx, t, down)) != ABCD_OK) return st;
+  if ((st = run(ctx, t, kProductDown, down)) != ABCD_OK) return st;
   if (dx) {
     Job j{dgu, {og, ou}, 2, m, d, f, 1, {}};
     j.args.c[0] = out_of(dx);
-    if ((st = run<false, true, kPlain>(ctx, t, j)) != ABCD_OK) return st;
+    if ((st = run(ctx, t, kProductDx, j)) != ABCD_OK) return st;
   }
   if (dw_gate || dw_up) {
     // dG^T x and dU^T x: the second starts at dU's planes
@@ -385,12 +377,12 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
     Job j{left, {ox, ox}, 1, f, d, m, dw_gate && dw_up ? 2 : 1, {}};
     j.args.c[0] = out_of(dw_gate ? dw_gate : dw_up);
     if (dw_gate && dw_up) j.args.c[1] = out_of(dw_up);
-    if ((st = run<true, true, kPlain>(ctx, t, j)) != ABCD_OK) return st;
+    if ((st = run(ctx, t, kProductDw, j)) != ABCD_OK) return st;
   }
   if (dw_down) {
     Job j{ody, {h, h}, 1, d, f, m, 1, {}};
     j.args.c[0] = out_of(dw_down);
-    if ((st = run<true, true, kPlain>(ctx, t, j)) != ABCD_OK) return st;
+    if ((st = run(ctx, t, kProductDw, j)) != ABCD_OK) return st;
   }
   return ABCD_OK;
 }

@@ -8,10 +8,10 @@
 // Bound by HBM (forward x -> y, backward x, dy -> dx).  A row is read once: TPR lanes (part of a
 // warp, a warp, or a CTA) hold it in registers, NV accesses of V consecutive elements each, V = 16
 // bytes where the rows lie on 16-byte boundaries and one element where they do not; rows too long
-// for that are read again from L2.  Backward, a CTA takes many rows and its lanes keep dw and db of
-// their own columns in registers; the next rows are copied to shared memory meanwhile
-// (cp.async, each thread its own bytes, so no barrier is needed), which keeps the loads in flight
-// that eight warps of about 180 registers could not.  The CTAs' sums go to the workspace and a
+// for that are read again from L2.  A group of lanes takes many rows: the weights (and backward dw
+// and db of its own columns) stay in registers, and the next rows are copied to shared memory
+// meanwhile (cp.async, each thread its own bytes, so no barrier is needed), which keeps the loads in
+// flight that the few warps of so many registers could not.  The CTAs' sums go to the workspace and a
 // second kernel adds them in their order.
 #include <algorithm>
 #include <type_traits>
@@ -45,13 +45,16 @@ template <int TPR_, int V_, int NV_> struct RowShape {
   static constexpr int kGroups = kThreads / TPR;          // rows of a CTA at a time
   static constexpr int kWarps = kThreads / 32;
   static constexpr int kCapacity = TPR * V * NV;
-  // Shared memory of the backward kernel: four rows' x and dy per group while it runs (three where
-  // four are too many; none are copied ahead element by element), the sums of the CTA's columns at
-  // its end.
-  static constexpr size_t kAhead = (size_t)2 * NV * kThreads * 16;
-  static constexpr int kDepth = 4 * kAhead > 200 * 1024 ? 3 : 4;
-  static constexpr size_t kRing = V > 1 ? kDepth * kAhead : 0, kSums = (size_t)2 * kCapacity * 4;
-  static constexpr size_t kBwdSmem = kRing > kSums ? kRing : kSums;
+  // Shared memory: four rows of each of MATS matrices per group (three where four are too many; none
+  // are copied ahead element by element), and, backward, the sums of the CTA's columns at its end.
+  template <int MATS> static constexpr size_t kAhead = (size_t)MATS * NV * kThreads * 16;
+  template <int MATS> static constexpr int kDepth = 4 * kAhead<MATS> > 200 * 1024 ? 3 : 4;
+  template <int MATS> static constexpr size_t kRing = V > 1 ? kDepth<MATS> * kAhead<MATS> : 0;
+  static constexpr size_t kSums = (size_t)2 * kCapacity * 4;
+  static constexpr size_t kFwdSmem = kRing<1>, kBwdSmem = kRing<2> > kSums ? kRing<2> : kSums;
+  // CTAs per SM that the grid offers: as many as hold their rows in registers
+  static constexpr int kFwdCtas = kThreads > 512 ? 1 : kThreads > 256 || V * NV > 16 ? 2 : 4;
+  static constexpr int kBwdCtas = kThreads > 256 ? 1 : V * NV <= 8 ? 4 : V * NV <= 16 ? 2 : 1;
 };
 
 template <typename T, int V>
@@ -124,138 +127,185 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float2 (*red)[32], 
   }
 }
 
-template <typename T, typename R>
-__global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_constant__ NormArgs a) {
-  constexpr int V = R::V, NV = R::NV, TPR = R::TPR;
-  __shared__ float2 red[2][32];
-  pdl_wait();
-  const int lane = threadIdx.x % TPR;
-  const long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR;
-  const bool in = r < a.rows;
-  const T* x = (const T*)a.x + r * a.sx;
-  float v[NV][V];
-  float s = 0.f, unused = 0.f;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = (j * TPR + lane) * V;
-    load_vec<T, V>(v[j], x + c, in ? a.cols - c : 0);
-  }
-#pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int i = 0; i < V; ++i) s += v[j][i];
-  row_sum2<TPR>(s, unused, red, 0);
-  const float mean = s / (float)a.cols;
-  float q = 0.f;
-#pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      v[j][i] -= mean;
-      if ((j * TPR + lane) * V + i < a.cols) q += v[j][i] * v[j][i];
-    }
-  row_sum2<TPR>(q, unused, red, 1);
-  const float rstd = rsqrtf(q / (float)a.cols + a.eps);
-  if (!in) return;
-  T* y = (T*)a.y + r * a.sy;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = (j * TPR + lane) * V, left = a.cols - c;
-    if (left <= 0) break;
-    float w[V], b[V];
-    load_weight<T, V>(w, a.w, a.wide_w, c, left, 1.f);
-    load_weight<T, V>(b, a.b, a.wide_w, c, left, 0.f);
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[j][i] = v[j][i] * rstd * w[i] + b[i];
-    store_vec<T, V>(y + c, v[j], left);
-  }
-  if (a.mean && lane == 0) {
-    a.mean[r] = mean;
-    a.rstd[r] = rstd;
-  }
-}
-
 // Asynchronous copy of min(16, bytes) bytes to 16 bytes of shared memory, zeros after them.
 __device__ __forceinline__ void copy16(void* dst, const void* src, int bytes) {
   const unsigned d = (unsigned)__cvta_generic_to_shared(dst);
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(bytes < 16 ? bytes : 16) : "memory");
 }
 
+// The rows that a group of TPR threads takes one after another, their next ones on the way: each
+// thread copies its own bytes of MATS matrices to its own 16-byte slots [depth][matrix][NV][thread].
+template <typename T, typename R, int MATS> struct RowRing {
+  char* slots;
+  const T* src[2];
+  long long stride[2];
+  long long rows, first, step, turns;
+  int cols, lane;
+
+  static constexpr int kDepth = R::template kDepth<MATS>;
+  __device__ __forceinline__ char* slot(int d, int mat, int j) const {
+    return slots + ((((size_t)d * MATS + mat) * R::NV + j) * R::kThreads + threadIdx.x) * 16;
+  }
+  __device__ __forceinline__ void fetch(long long t) const {
+    if constexpr (R::V > 1) {
+      if (t < turns) {
+        const long long r = first + t * step;
+        const int d = (int)(t % kDepth);
+#pragma unroll
+        for (int j = 0; j < R::NV; ++j) {
+          const int c = (j * R::TPR + lane) * R::V, bytes = r < rows ? (cols - c) * (int)sizeof(T) : 0;
+          if (bytes > 0) {
+#pragma unroll
+            for (int q = 0; q < MATS; ++q) copy16(slot(d, q, j), src[q] + r * stride[q] + c, bytes);
+          }
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+  }
+  __device__ __forceinline__ void start() const {
+#pragma unroll
+    for (int d = 0; d < kDepth - 1; ++d) fetch(d);
+  }
+  // Asks for the row kDepth - 1 turns on and waits for the one of turn t.
+  __device__ __forceinline__ void turn(long long t) const {
+    fetch(t + kDepth - 1);
+    if constexpr (R::V > 1) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+  }
+  // Vector j of the turn's row of a matrix; zeros past its end.
+  __device__ __forceinline__ void get(float (&v)[R::V], long long t, int mat, int j, int left) const {
+    if constexpr (R::V > 1) {
+      load_vec<T, R::V>(v, (const T*)slot((int)(t % kDepth), mat, j), left > 0 ? R::V : 0);
+    } else {
+      load_vec<T, R::V>(v, src[mat] + (first + t * step) * stride[mat] + j * R::TPR + lane, left);
+    }
+  }
+};
+
 template <typename T, typename R>
-__global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_constant__ NormArgs a) {
-  constexpr int V = R::V, NV = R::NV, TPR = R::TPR, kDepth = R::kDepth;
+__global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_constant__ NormArgs a) {
+  constexpr int V = R::V, NV = R::NV, TPR = R::TPR;
   extern __shared__ char smem[];
   __shared__ float2 red[2][32];
   pdl_wait();
   const int lane = threadIdx.x % TPR;
-  const long long first = (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR;
-  const long long step = (long long)gridDim.x * R::kGroups;
-  const long long turns = (a.rows - (long long)blockIdx.x * R::kGroups + step - 1) / step;   // alike in the CTA
-  // the thread's own 16-byte slots: [depth][x, dy][NV][thread]
-  auto slot = [&](int d, int which, int j) { return smem + ((((size_t)d * 2 + which) * NV + j) * R::kThreads + threadIdx.x) * 16; };
-  auto fetch = [&](long long t) {
-    if (V > 1 && t < turns) {
-      const long long r = first + t * step;
-      const int d = (int)(t % kDepth);
+  RowRing<T, R, 1> ring{smem, {(const T*)a.x, nullptr}, {a.sx, 0}, a.rows,
+                        (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR, (long long)gridDim.x * R::kGroups,
+                        0, a.cols, lane};
+  ring.turns = (a.rows - (long long)blockIdx.x * R::kGroups + ring.step - 1) / ring.step;   // alike in the CTA
+  ring.start();
+  float w[NV][V], b[NV][V];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int c = (j * TPR + lane) * V, bytes = r < a.rows ? (a.cols - c) * (int)sizeof(T) : 0;
-        if (bytes > 0) {
-          copy16(slot(d, 0, j), (const T*)a.x + r * a.sx + c, bytes);
-          copy16(slot(d, 1, j), (const T*)a.dy + r * a.sdy + c, bytes);
-        }
-      }
-    }
-    if (V > 1) asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  float dw[NV][V] = {}, db[NV][V] = {};
-#pragma unroll
-  for (int d = 0; d < kDepth - 1; ++d) fetch(d);
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * TPR + lane) * V;
+    load_weight<T, V>(w[j], a.w, a.wide_w, c, a.cols - c, 1.f);
+    load_weight<T, V>(b[j], a.b, a.wide_w, c, a.cols - c, 0.f);
+  }
   const float inv = 1.f / (float)a.cols;
-  for (long long t = 0; t < turns; ++t) {
-    fetch(t + kDepth - 1);
-    const long long r = first + t * step;
+  for (long long t = 0; t < ring.turns; ++t) {
+    ring.turn(t);
+    const long long r = ring.first + t * ring.step;
     const bool in = r < a.rows;
-    const float mean = in ? a.mean[r] : 0.f, rstd = in ? a.rstd[r] : 0.f;
-    if (V > 1) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
-    float xh[NV][V], g[NV][V];
-    float s1 = 0.f, s2 = 0.f;
+    float v[NV][V], s = 0.f, q = 0.f, unused = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + lane) * V, left = in ? a.cols - c : 0;
-      float w[V];
-      load_weight<T, V>(w, left > 0 ? a.w : nullptr, a.wide_w, c, left, 1.f);
-      if (V > 1) {
-        const int d = (int)(t % kDepth);
-        load_vec<T, V>(xh[j], (const T*)slot(d, 0, j), left > 0 ? V : 0);
-        load_vec<T, V>(g[j], (const T*)slot(d, 1, j), left > 0 ? V : 0);
-      } else {
-        load_vec<T, V>(xh[j], (const T*)a.x + r * a.sx + c, left);
-        load_vec<T, V>(g[j], (const T*)a.dy + r * a.sdy + c, left);
+      ring.get(v[j], t, 0, j, in ? a.cols - (j * TPR + lane) * V : 0);
+#pragma unroll
+      for (int i = 0; i < V; ++i) s += v[j][i];
+    }
+    row_sum2<TPR>(s, unused, red, 0);
+    const float mean = s * inv;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int left = a.cols - (j * TPR + lane) * V;
+      if (left < V) {                                  // past the row's end nothing deviates
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[j][i] = i < left ? v[j][i] : mean;
       }
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        xh[j][i] = i < left ? (xh[j][i] - mean) * rstd : 0.f;
+        v[j][i] -= mean;
+        q += v[j][i] * v[j][i];
+      }
+    }
+    row_sum2<TPR>(q, unused, red, 1);
+    const float rstd = rsqrtf(q * inv + a.eps);
+    if (!in) continue;
+    T* y = (T*)a.y + r * a.sy;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (j * TPR + lane) * V, left = a.cols - c;
+      if (left <= 0) break;
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[j][i] = v[j][i] * rstd * w[j][i] + b[j][i];
+      store_vec<T, V>(y + c, v[j], left);
+    }
+    if (a.mean && lane == 0) {
+      a.mean[r] = mean;
+      a.rstd[r] = rstd;
+    }
+  }
+}
+
+template <typename T, typename R>
+__global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_constant__ NormArgs a) {
+  constexpr int V = R::V, NV = R::NV, TPR = R::TPR;
+  extern __shared__ char smem[];
+  __shared__ float2 red[2][32];
+  pdl_wait();
+  const int lane = threadIdx.x % TPR;
+  RowRing<T, R, 2> ring{smem, {(const T*)a.x, (const T*)a.dy}, {a.sx, a.sdy}, a.rows,
+                        (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR, (long long)gridDim.x * R::kGroups,
+                        0, a.cols, lane};
+  ring.turns = (a.rows - (long long)blockIdx.x * R::kGroups + ring.step - 1) / ring.step;
+  ring.start();
+  float w[NV][V], dw[NV][V] = {}, db[NV][V] = {};
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * TPR + lane) * V;
+    load_weight<T, V>(w[j], a.w, a.wide_w, c, a.cols - c, 1.f);
+  }
+  const float inv = 1.f / (float)a.cols;
+  for (long long t = 0; t < ring.turns; ++t) {
+    ring.turn(t);
+    const long long r = ring.first + t * ring.step;
+    const bool in = r < a.rows;
+    const float mean = in ? a.mean[r] : 0.f, rstd = in ? a.rstd[r] : 0.f;
+    // past the row's end dy is zero, and so is what xh meets there
+    float xh[NV][V], g[NV][V], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int left = in ? a.cols - (j * TPR + lane) * V : 0;
+      ring.get(xh[j], t, 0, j, left);
+      ring.get(g[j], t, 1, j, left);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        xh[j][i] = (xh[j][i] - mean) * rstd;
         dw[j][i] += g[j][i] * xh[j][i];
         db[j][i] += g[j][i];
-        g[j][i] *= w[i];
+        g[j][i] *= w[j][i];
         s1 += g[j][i];
         s2 += g[j][i] * xh[j][i];
       }
     }
     row_sum2<TPR>(s1, s2, red, (int)(t & 1));
-    s1 *= inv;
-    s2 *= inv;
+    s1 *= inv * rstd;
+    s2 *= inv * rstd;
     if (a.y && in) {
       T* dx = (T*)a.y + r * a.sy;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const int c = (j * TPR + lane) * V, left = a.cols - c;
         if (left <= 0) break;
-        float v[V] = {};
-        if (a.res) load_vec<T, V>(v, (const T*)a.res + r * a.sres + c, left);
+        float v[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += rstd * (g[j][i] - s1 - xh[j][i] * s2);
+        for (int i = 0; i < V; ++i) v[i] = rstd * g[j][i] - s1 - xh[j][i] * s2;
+        if (a.res) {
+          float res[V];
+          load_vec<T, V>(res, (const T*)a.res + r * a.sres + c, left);
+#pragma unroll
+          for (int i = 0; i < V; ++i) v[i] += res[i];
+        }
         store_vec<T, V>(dx + c, v, left);
       }
     }
@@ -413,6 +463,12 @@ template <typename T, typename F> abcd_status with_shape(long long cols, bool al
   return f(0);
 }
 
+abcd_status room_for(abcd_ctx* ctx, const void* kernel, size_t smem) {
+  if (smem <= 47 * 1024) return ABCD_OK;
+  const cudaError_t e = allow_smem(ctx, kernel);
+  return e == cudaSuccess ? ABCD_OK : fail(ctx, ABCD_ERR_CUDA, "layer norm: %s", cudaGetErrorString(e));
+}
+
 bool weights_ok(const abcd_matrix* x, int wtype, const void* a, const void* b) {
   return (wtype == ABCD_F32 || wtype == x->dtype) &&
          (((uintptr_t)a | (uintptr_t)b) & (elem_size(wtype) - 1)) == 0;
@@ -447,8 +503,11 @@ extern "C" abcd_status abcd_layer_norm(abcd_ctx* ctx, const abcd_matrix* x, cons
         const unsigned grid = (unsigned)std::min<long long>(x->rows, 2LL * ctx->num_sms);
         return check_launch(ctx, "norm_fwd_long_kernel", launch_pdl(norm_fwd_long_kernel<T>, dim3(grid), dim3(kLongThreads), 0, ctx->stream, a));
       } else {
-        const unsigned grid = (unsigned)((x->rows + R::kGroups - 1) / R::kGroups);
-        return check_launch(ctx, "norm_fwd_kernel", launch_pdl(norm_fwd_kernel<T, R>, dim3(grid), dim3(R::kThreads), 0, ctx->stream, a));
+        auto* kernel = norm_fwd_kernel<T, R>;
+        const abcd_status st = room_for(ctx, (const void*)kernel, R::kFwdSmem);
+        if (st != ABCD_OK) return st;
+        const unsigned grid = (unsigned)std::min<long long>((x->rows + R::kGroups - 1) / R::kGroups, R::kFwdCtas * ctx->num_sms);
+        return check_launch(ctx, "norm_fwd_kernel", launch_pdl(kernel, dim3(grid), dim3(R::kThreads), R::kFwdSmem, ctx->stream, a));
       }
     });
   });
@@ -485,9 +544,8 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
       if constexpr (kLong) {
         ctas = (int)std::min<long long>(x->rows, 2LL * sms);
       } else {
-        constexpr int kElems = R::V * R::NV;
-        const long long per_sm = R::kThreads > 256 ? 1 : kElems <= 8 ? kNormCtasPerSm : kElems <= 16 ? 2 : 1;
-        ctas = (int)std::min<long long>((x->rows + R::kGroups - 1) / R::kGroups, per_sm * sms);
+        static_assert(R::kBwdCtas <= kNormCtasPerSm);
+        ctas = (int)std::min<long long>((x->rows + R::kGroups - 1) / R::kGroups, R::kBwdCtas * sms);
       }
       const size_t need = kNetHeader + (size_t)ctas * 2 * (size_t)x->cols * sizeof(float);
       if (need > ctx->net_bytes)
@@ -497,12 +555,9 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
         return check_launch(ctx, "norm_bwd_long_kernel", launch_pdl(norm_bwd_long_kernel<T>, dim3(ctas), dim3(kLongThreads), 0, ctx->stream, a));
       } else {
         auto* kernel = norm_bwd_kernel<T, R>;
-        constexpr size_t kSmem = R::kBwdSmem;
-        if (kSmem > 48 * 1024 - 1024) {
-          const cudaError_t e = allow_smem(ctx, (const void*)kernel);
-          if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "norm_bwd_kernel: %s", cudaGetErrorString(e));
-        }
-        return check_launch(ctx, "norm_bwd_kernel", launch_pdl(kernel, dim3(ctas), dim3(R::kThreads), kSmem, ctx->stream, a));
+        const abcd_status st = room_for(ctx, (const void*)kernel, R::kBwdSmem);
+        if (st != ABCD_OK) return st;
+        return check_launch(ctx, "norm_bwd_kernel", launch_pdl(kernel, dim3(ctas), dim3(R::kThreads), R::kBwdSmem, ctx->stream, a));
       }
     });
   });
