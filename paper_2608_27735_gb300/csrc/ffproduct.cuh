@@ -12,9 +12,10 @@
 // 256 x 256 tile: each stages half of B) per SM; one warp issues the TMA loads of 128-byte swizzled
 // tiles into a ring of stages, one the tcgen05 matrix instructions, the others turn the sums that
 // lie in tensor memory into results while the next tile's are made in its other half.  Where the
-// tiles do not fill the SMs, k is split: each part leaves its 32-bit sums in the workspace, and the
-// warp that comes last adds the parts in their order, so that the result does not depend on who
-// that was.
+// tiles do not fill the SMs, k is split: each part leaves its 32-bit sums in the workspace, and they
+// are added in their order, by a kernel of its own (whose CTAs share the work: dWd of 20,000 x 64 x
+// 256 in 32 bits took 64 us with a tile's parts added by its last warps) or, where the sums are
+// not yet the result, by the warp that comes last.
 #pragma once
 
 #include "network.cuh"
@@ -49,7 +50,10 @@ struct ProductArgs {
   Out c[2];                           // kPlain: per batch; kUp, kDown: c[0] the hidden matrix
   Out g[2];                           // kUp: gate and up (p NULL: not wanted); kDown: dG and dU
   Out in[2];                          // kDown: the saved gate and up
-  float* part;                        // sums of the splits
+  // sums of the splits: kPlain [split][batch][m][part_ld], which a kernel of its own adds up;
+  // otherwise per warp of a tile, which the last warp to come adds up
+  float* part;
+  long long part_ld;
   unsigned* count;                    // finished splits per warp of a tile; zero between calls
   unsigned* status;
   unsigned limit;                     // polls of a wait
@@ -302,7 +306,9 @@ struct Product {
   static constexpr int kWarpCols = kOutCols / (kWarps / 4);
   static constexpr int CW = EPI != kPlain || kWarpCols < 32 ? 16 : 32;    // taken at a time
   static constexpr int kBuffer = 32 * CW * (F32 ? 4 : 2);   // in which a warp turns its rows round
+  static_assert(kBuffer >= (EPI == kPlain ? 32 * 16 * 4 : 0));
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (size_t)kWarps * kBuffer;
+  static_assert(kSmem + 512 <= 227 * 1024);
 };
 
 template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
@@ -442,7 +448,7 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16) + share * P::kWarpCols;
       bool mine = rows > 0 && cols > 0;
       float* part = nullptr;
-      if (a.splits > 1) {
+      if (EPI != kPlain && a.splits > 1) {
         // this part's sums to the workspace [column][row]; the last warp to have done so goes on
         constexpr int PARTS = EPI == kUp ? 2 : 1;
         const long long piece = (long long)CG * P::kWarps * PARTS * P::kWarpCols * 32;
@@ -527,9 +533,20 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
             store_operand<F32, P::CW>(z, a.g[1], m, n + c, rows, w, bf16, buffer);
             store_operand<F32, P::CW>(u, a.c[0], m, n + c, rows, w, bf16, buffer);
           } else {
-            sum_columns(c, 0, v);
-            if (a.splits == 1) tmem_load_wait(v);
-            store_matrix<F32, P::CW>(v, a.c[it.batch], m, n + c, rows, w, bf16, buffer);
+            tmem_load(sums + c, v);
+            tmem_load_wait(v);
+            if (a.splits == 1) {
+              store_matrix<F32, P::CW>(v, a.c[it.batch], m, n + c, rows, w, bf16, buffer);
+            } else {
+              const Out o{a.part + ((long long)it.split * a.batches + it.batch) * a.m * a.part_ld, a.part_ld, 0, 1};
+#pragma unroll
+              for (int e = 0; e < P::CW; e += 16) {      // sixteen of 32 bits take the buffer of 32 of 16
+                float x[16];
+#pragma unroll
+                for (int q = 0; q < 16; ++q) x[q] = v[e + q];
+                if (w > e) store_matrix<true, 16>(x, o, m, n + c + e, rows, min(16, w - e), false, buffer);
+              }
+            }
           }
         }
       }

@@ -26,10 +26,16 @@ struct Operand {
 int terms_of(int dtype) { return dtype == ABCD_F32 ? 3 : 1; }
 long long pitch_of(long long cols) { return (cols + 63) / 64 * 64; }   // whole 128-byte lines
 
+// Up to five matrices that are laid out as operands by one launch.
 struct PackArgs {
-  const void* src;
-  long long rows, cols, stride, pitch, plane;
-  unsigned short* dst;
+  struct One {
+    const void* src;
+    unsigned short* dst;
+    long long rows, cols, stride, pitch, plane;
+    long long first;                  // blocks of eight columns before this matrix's
+  } m[5];
+  int n;
+  long long blocks;
 };
 
 // An operand from a matrix that TMA cannot read as it is: 32-bit values as three 16-bit terms, or
@@ -37,15 +43,26 @@ struct PackArgs {
 template <typename T>
 __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackArgs a) {
   pdl_wait();
-  const long long groups = (a.cols + 7) / 8, total = groups * a.rows;
-  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < total; i += gridDim.x * 256LL) {
-    const long long row = i / groups, col = 8 * (i - row * groups);
-    const T* src = (const T*)a.src + row * a.stride + col;
-    unsigned short* dst = a.dst + row * a.pitch + col;
+  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < a.blocks; i += gridDim.x * 256LL) {
+    int k = 0;
+#pragma unroll
+    for (int q = 1; q < 5; ++q) k += q < a.n && i >= a.m[q].first;
+    const PackArgs::One& o = a.m[k];
+    const long long groups = (o.cols + 7) / 8, at = i - o.first;
+    const long long row = at < (1LL << 32) ? (unsigned)at / (unsigned)groups : at / groups;
+    const int col = (int)(8 * (at - row * groups)), left = (int)(o.cols - col);
+    const T* src = (const T*)o.src + row * o.stride + col;
+    unsigned short* dst = o.dst + row * o.pitch + col;
     if constexpr (sizeof(T) == 4) {
       float v[8];
+      if (left >= 8 && ((uintptr_t)src & 15) == 0) {
+        const float4 lo = reinterpret_cast<const float4*>(src)[0], hi = reinterpret_cast<const float4*>(src)[1];
+        v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w;
+        v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+      } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = col + j < a.cols ? src[j] : 0.f;
+        for (int j = 0; j < 8; ++j) v[j] = j < left ? src[j] : 0.f;
+      }
 #pragma unroll
       for (int t = 0; t < 3; ++t) {
         unsigned w[4];
@@ -54,18 +71,53 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackA
           const float lo = take_term(v[2 * j]), hi = take_term(v[2 * j + 1]);
           w[j] = pack2(lo, hi, true);
         }
-        *reinterpret_cast<uint4*>(dst + t * a.plane) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(dst + t * o.plane) = make_uint4(w[0], w[1], w[2], w[3]);
       }
     } else {
       unsigned w[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const unsigned lo = col + 2 * j < a.cols ? reinterpret_cast<const unsigned short*>(src)[2 * j] : 0u;
-        const unsigned hi = col + 2 * j + 1 < a.cols ? reinterpret_cast<const unsigned short*>(src)[2 * j + 1] : 0u;
+        const unsigned lo = 2 * j < left ? reinterpret_cast<const unsigned short*>(src)[2 * j] : 0u;
+        const unsigned hi = 2 * j + 1 < left ? reinterpret_cast<const unsigned short*>(src)[2 * j + 1] : 0u;
         w[j] = lo | hi << 16;
       }
       *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
     }
+  }
+}
+
+// The result of a product whose k was split: its parts added in their order, rounded to the type of
+// the matrices.  One thread per four columns of a row.
+struct JoinArgs {
+  const float* part;
+  long long ld, plane;                // elements between rows, between splits
+  int rows, cols, splits;
+  Out c[2];                           // per batch
+};
+template <typename T>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinArgs a) {
+  pdl_wait();
+  const unsigned groups = (a.cols + 3) / 4;
+  const unsigned i = blockIdx.x * 256u + threadIdx.x, row = i / groups, col = 4 * (i - row * groups);
+  if (row >= (unsigned)a.rows) return;
+  const float* p = a.part + (long long)blockIdx.y * a.rows * a.ld + row * a.ld + col;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int k = 0; k < a.splits; ++k) {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(p + k * a.plane));
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  const Out& o = a.c[blockIdx.y];
+  T* c = (T*)o.p + row * o.stride + col;
+  if (o.vec && (int)col + 4 <= a.cols) {
+    Pack<T, 4> q;
+    q.v[0] = from_f32<T>(s.x); q.v[1] = from_f32<T>(s.y); q.v[2] = from_f32<T>(s.z); q.v[3] = from_f32<T>(s.w);
+    *reinterpret_cast<Pack<T, 4>*>(c) = q;
+  } else {
+    const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if ((int)col + e < a.cols) c[e] = from_f32<T>(v[e]);
   }
 }
 
@@ -88,20 +140,25 @@ struct Scratch {
 
 bool needs_pack(const abcd_matrix* m) { return m->dtype == ABCD_F32 || !rows_aligned(m, 16); }
 
-// m as an operand: in place where TMA can read it, else a copy in the workspace.
-abcd_status operand_of(abcd_ctx* ctx, Scratch& s, const abcd_matrix* m, Operand* o) {
-  if (!needs_pack(m)) {
-    *o = Operand{m->data, m->rows, m->cols, (m->stride + 7) / 8 * 8, 0, 1};
-    return ABCD_OK;
+// The matrices of a call as operands: in place where TMA can read them, else as copies in the
+// workspace, which one launch makes.
+struct Operands {
+  Scratch& s;
+  PackArgs args{};
+  Operand add(const abcd_matrix* m) {
+    if (!needs_pack(m)) return Operand{m->data, m->rows, m->cols, (m->stride + 7) / 8 * 8, 0, 1};
+    const Operand o = s.operand(m->rows, m->cols, m->dtype);
+    args.m[args.n++] = PackArgs::One{m->data, (unsigned short*)o.p, m->rows, m->cols, m->stride, o.pitch, o.plane, args.blocks};
+    args.blocks += (m->cols + 7) / 8 * m->rows;
+    return o;
   }
-  *o = s.operand(m->rows, m->cols, m->dtype);
-  const PackArgs a{m->data, m->rows, m->cols, m->stride, o->pitch, o->plane, (unsigned short*)o->p};
-  const long long blocks = std::min<long long>(((m->cols + 7) / 8 * m->rows + 255) / 256, 16LL * ctx->num_sms);
-  return with_type(m->dtype, [&](auto t) {
-    return check_launch(ctx, "pack_kernel", launch_pdl(pack_kernel<decltype(t)>, dim3((unsigned)blocks),
-                                                       dim3(256), 0, ctx->stream, a));
-  });
-}
+  abcd_status pack(abcd_ctx* ctx, int dtype) const {
+    if (args.n == 0) return ABCD_OK;
+    const long long grid = std::min<long long>((args.blocks + 255) / 256, 16LL * ctx->num_sms);
+    return check_launch(ctx, "pack_kernel", launch_pdl(dtype == ABCD_F32 ? pack_kernel<float> : pack_kernel<unsigned short>,
+                                                       dim3((unsigned)grid), dim3(256), 0, ctx->stream, args));
+  }
+};
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                               const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -207,7 +264,14 @@ abcd_status run(abcd_ctx* ctx, int dtype, int which, Job& j) {
   for (int b = 0; ok && b < j.nb; ++b) ok = make_map(&a.b[b], j.b[b], dtype, bmn ? 64 : epi == kUp ? bn / 2 : bn / cg);
   if (!ok) return fail(ctx, ABCD_ERR_CUDA, "tensor map of a product");
   if (j.nb < 2) a.b[1] = a.b[0];
-  return dtype == ABCD_F32 ? launch_32(ctx, which, shape, a) : launch_16(ctx, which, shape, a);
+  a.part_ld = (j.n + 3) / 4 * 4;
+  const abcd_status st = dtype == ABCD_F32 ? launch_32(ctx, which, shape, a) : launch_16(ctx, which, shape, a);
+  if (st != ABCD_OK || epi != kPlain || splits == 1) return st;
+  const JoinArgs q{a.part, a.part_ld, j.batches * j.m * a.part_ld, a.m, a.n, splits, {a.c[0], a.c[1]}};
+  const dim3 grid((unsigned)((j.m * ((j.n + 3) / 4) + 255) / 256), (unsigned)j.batches);
+  return with_type(dtype, [&](auto t) {
+    return check_launch(ctx, "join_kernel", launch_pdl(join_kernel<decltype(t)>, grid, dim3(256), 0, ctx->stream, q));
+  });
 }
 
 bool shape_is(const abcd_matrix* m, int dtype, long long rows, long long cols) {
@@ -290,10 +354,9 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
   if (st != ABCD_OK) return st;
   Scratch s{ctx->net_base};
   s.take(kPartBytes);
-  Operand ox, og, ou, od;
-  if ((st = operand_of(ctx, s, x, &ox)) != ABCD_OK || (st = operand_of(ctx, s, w_gate, &og)) != ABCD_OK ||
-      (st = operand_of(ctx, s, w_up, &ou)) != ABCD_OK || (st = operand_of(ctx, s, w_down, &od)) != ABCD_OK)
-    return st;
+  Operands in{s};
+  const Operand ox = in.add(x), og = in.add(w_gate), ou = in.add(w_up), od = in.add(w_down);
+  if ((st = in.pack(ctx, t)) != ABCD_OK) return st;
   const Operand h = s.operand(m, f, t);
   Job up_job{ox, {og, ou}, 2, m, f, d, 1, {}};
   up_job.args.act = activation;
@@ -351,10 +414,15 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
   if (st != ABCD_OK) return st;
   Scratch s{ctx->net_base};
   s.take(kPartBytes);
-  Operand ody, ox, og, ou, od;
-  if ((st = operand_of(ctx, s, dy, &ody)) != ABCD_OK || (st = operand_of(ctx, s, w_down, &od)) != ABCD_OK) return st;
-  if ((dw_gate || dw_up) && (st = operand_of(ctx, s, x, &ox)) != ABCD_OK) return st;
-  if (dx && ((st = operand_of(ctx, s, w_gate, &og)) != ABCD_OK || (st = operand_of(ctx, s, w_up, &ou)) != ABCD_OK)) return st;
+  Operands in{s};
+  const Operand ody = in.add(dy), od = in.add(w_down);
+  Operand ox{}, og{}, ou{};
+  if (dw_gate || dw_up) ox = in.add(x);
+  if (dx) {
+    og = in.add(w_gate);
+    ou = in.add(w_up);
+  }
+  if ((st = in.pack(ctx, t)) != ABCD_OK) return st;
   const Operand h = s.operand(m, f, t), dgu = s.operand(m, f, t, 2);
   Job down{ody, {od, od}, 1, m, f, d, 1, {}};
   down.args.act = activation;

@@ -38,23 +38,22 @@ struct NormArgs {
   int wide_w;                         // weight and bias are fp32 whatever the matrices' type
 };
 
-// How a row lies over threads.
-template <int TPR_, int V_, int NV_> struct RowShape {
+// How a row lies over threads, forward (one matrix is read) and backward (two).
+template <int TPR_, int V_, int NV_, bool BWD> struct RowShape {
   static constexpr int TPR = TPR_, V = V_, NV = NV_;
   static constexpr int kThreads = TPR > 256 ? TPR : 256;
   static constexpr int kGroups = kThreads / TPR;          // rows of a CTA at a time
-  static constexpr int kWarps = kThreads / 32;
   static constexpr int kCapacity = TPR * V * NV;
-  // Shared memory: four rows of each of MATS matrices per group (three where four are too many; none
-  // are copied ahead element by element), and, backward, the sums of the CTA's columns at its end.
-  template <int MATS> static constexpr size_t kAhead = (size_t)MATS * NV * kThreads * 16;
-  template <int MATS> static constexpr int kDepth = 4 * kAhead<MATS> > 200 * 1024 ? 3 : 4;
-  template <int MATS> static constexpr size_t kRing = V > 1 ? kDepth<MATS> * kAhead<MATS> : 0;
-  static constexpr size_t kSums = (size_t)2 * kCapacity * 4;
-  static constexpr size_t kFwdSmem = kRing<1>, kBwdSmem = kRing<2> > kSums ? kRing<2> : kSums;
-  // CTAs per SM that the grid offers: as many as hold their rows in registers
-  static constexpr int kFwdCtas = kThreads > 512 ? 1 : kThreads > 256 || V * NV > 16 ? 2 : 4;
-  static constexpr int kBwdCtas = kThreads > 256 ? 1 : V * NV <= 8 ? 4 : V * NV <= 16 ? 2 : 1;
+  // Shared memory: four rows of each matrix per group (three where four leave no room for a second
+  // CTA; none are copied ahead element by element), and, backward, the sums of the CTA's columns at
+  // its end.
+  static constexpr int kMats = BWD ? 2 : 1;
+  static constexpr size_t kAhead = (size_t)kMats * NV * kThreads * 16;
+  static constexpr int kDepth = 4 * kAhead > 100 * 1024 ? 3 : 4;
+  static constexpr size_t kRing = V > 1 ? kDepth * kAhead : 0, kSums = BWD ? (size_t)2 * kCapacity * 4 : 0;
+  static constexpr size_t kSmem = kRing > kSums ? kRing : kSums;
+  // CTAs per SM that the grid offers: as many as their registers (and rows) leave room for
+  static constexpr int kCtas = kThreads > 256 || kSmem > 100 * 1024 ? 1 : V * NV > 8 ? 2 : 4;
 };
 
 template <typename T, int V>
@@ -117,7 +116,8 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float2 (*red)[32], 
     constexpr int WARPS = TPR / 32;
     const int w = threadIdx.x / 32, first = w / WARPS * WARPS;
     if ((threadIdx.x & 31) == 0) red[turn][w] = make_float2(a, b);
-    __syncthreads();
+    // the row's warps alone: barriers 1 ... of the CTA's rows
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / TPR), "n"(TPR) : "memory");
     a = b = 0.f;
 #pragma unroll
     for (int k = 0; k < WARPS; ++k) {
@@ -134,17 +134,17 @@ __device__ __forceinline__ void copy16(void* dst, const void* src, int bytes) {
 }
 
 // The rows that a group of TPR threads takes one after another, their next ones on the way: each
-// thread copies its own bytes of MATS matrices to its own 16-byte slots [depth][matrix][NV][thread].
-template <typename T, typename R, int MATS> struct RowRing {
+// thread copies its own bytes of the matrices to its own 16-byte slots [depth][matrix][NV][thread].
+template <typename T, typename R> struct RowRing {
   char* slots;
   const T* src[2];
   long long stride[2];
   long long rows, first, step, turns;
   int cols, lane;
 
-  static constexpr int kDepth = R::template kDepth<MATS>;
+  static constexpr int kDepth = R::kDepth;
   __device__ __forceinline__ char* slot(int d, int mat, int j) const {
-    return slots + ((((size_t)d * MATS + mat) * R::NV + j) * R::kThreads + threadIdx.x) * 16;
+    return slots + ((((size_t)d * R::kMats + mat) * R::NV + j) * R::kThreads + threadIdx.x) * 16;
   }
   __device__ __forceinline__ void fetch(long long t) const {
     if constexpr (R::V > 1) {
@@ -156,7 +156,7 @@ template <typename T, typename R, int MATS> struct RowRing {
           const int c = (j * R::TPR + lane) * R::V, bytes = r < rows ? (cols - c) * (int)sizeof(T) : 0;
           if (bytes > 0) {
 #pragma unroll
-            for (int q = 0; q < MATS; ++q) copy16(slot(d, q, j), src[q] + r * stride[q] + c, bytes);
+            for (int q = 0; q < R::kMats; ++q) copy16(slot(d, q, j), src[q] + r * stride[q] + c, bytes);
           }
         }
       }
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_cons
   __shared__ float2 red[2][32];
   pdl_wait();
   const int lane = threadIdx.x % TPR;
-  RowRing<T, R, 1> ring{smem, {(const T*)a.x, nullptr}, {a.sx, 0}, a.rows,
+  RowRing<T, R> ring{smem, {(const T*)a.x, nullptr}, {a.sx, 0}, a.rows,
                         (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR, (long long)gridDim.x * R::kGroups,
                         0, a.cols, lane};
   ring.turns = (a.rows - (long long)blockIdx.x * R::kGroups + ring.step - 1) / ring.step;   // alike in the CTA
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
   __shared__ float2 red[2][32];
   pdl_wait();
   const int lane = threadIdx.x % TPR;
-  RowRing<T, R, 2> ring{smem, {(const T*)a.x, (const T*)a.dy}, {a.sx, a.sdy}, a.rows,
+  RowRing<T, R> ring{smem, {(const T*)a.x, (const T*)a.dy}, {a.sx, a.sdy}, a.rows,
                         (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR, (long long)gridDim.x * R::kGroups,
                         0, a.cols, lane};
   ring.turns = (a.rows - (long long)blockIdx.x * R::kGroups + ring.step - 1) / ring.step;
@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
         dw[j][i] += __shfl_xor_sync(~0u, dw[j][i], o);
         db[j][i] += __shfl_xor_sync(~0u, db[j][i], o);
       }
-  constexpr int ROUNDS = TPR > 32 ? R::kGroups : R::kWarps;
+  constexpr int ROUNDS = TPR > 32 ? R::kGroups : R::kThreads / 32;
   const int mine = TPR > 32 ? threadIdx.x / TPR : threadIdx.x / 32;
   const bool one = TPR >= 32 || (threadIdx.x & 31) < TPR;
   for (int k = 0; k < ROUNDS; ++k) {
@@ -442,23 +442,26 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* part, int c
 
 constexpr int kNormCtasPerSm = 4;
 
-// Calls f with the row shape for `cols` columns of T: the fewest threads whose registers hold a row;
-// f of an int where none does.
-template <typename T, typename F> abcd_status with_shape(long long cols, bool aligned, F&& f) {
+// Calls f with the row shape for `cols` columns of T: the fewest threads whose registers hold a row,
+// 32 elements a thread forward (with as many weights and biases) and 16 backward (with as many
+// weights and sums); f of an int where none does.  Backward, 100,000 x 1,024 bf16 with 32 elements a
+// thread (eight warps per SM) took 164 us.
+template <typename T, bool BWD, typename F> abcd_status with_shape(long long cols, bool aligned, F&& f) {
   if (aligned) {
-    constexpr int V = 16 / sizeof(T), W = sizeof(T) / 2;    // f32: twice the accesses of 16 bytes
-    if (cols <= 8 * V) return f(RowShape<8, V, 1>());
-    if (cols <= 16 * V) return f(RowShape<16, V, 1>());
-    if (cols <= 32 * V) return f(RowShape<32, V, 1>());
-    if (cols <= 64 * V) return f(RowShape<32, V, 2>());
-    if (cols <= 32 * V * 4 * W) return f(RowShape<32, V, 4 * W>());
-    if (cols <= 128 * V * 4 * W) return f(RowShape<128, V, 4 * W>());
-    if (cols <= 512 * V * 2 * W) return f(RowShape<512, V, 2 * W>());
+    constexpr int V = 16 / sizeof(T), N = (BWD ? 16 : 32) / V;   // accesses of 16 bytes per thread
+    if (cols <= 8 * V) return f(RowShape<8, V, 1, BWD>());
+    if (cols <= 16 * V) return f(RowShape<16, V, 1, BWD>());
+    if (cols <= 32 * V) return f(RowShape<32, V, 1, BWD>());
+    if (cols <= 64 * V) return f(RowShape<32, V, 2, BWD>());
+    if (cols <= 32 * V * N) return f(RowShape<32, V, N, BWD>());
+    if (cols <= 64 * V * N) return f(RowShape<64, V, N, BWD>());
+    if (cols <= 256 * V * N) return f(RowShape<256, V, N, BWD>());
+    if (cols <= 512 * V * N) return f(RowShape<512, V, N, BWD>());
   } else {
-    if (cols <= 64) return f(RowShape<32, 1, 2>());
-    if (cols <= 256) return f(RowShape<32, 1, 8>());
-    if (cols <= 2048) return f(RowShape<256, 1, 8>());
-    if (cols <= 8192) return f(RowShape<1024, 1, 8>());
+    if (cols <= 64) return f(RowShape<32, 1, 2, BWD>());
+    if (cols <= 256) return f(RowShape<32, 1, 8, BWD>());
+    if (cols <= 2048) return f(RowShape<256, 1, 8, BWD>());
+    if (cols <= 8192) return f(RowShape<1024, 1, 8, BWD>());
   }
   return f(0);
 }
@@ -497,17 +500,17 @@ extern "C" abcd_status abcd_layer_norm(abcd_ctx* ctx, const abcd_matrix* x, cons
                    (int)x->cols, x->stride, 0, y->stride, 0, eps, weight_dtype == ABCD_F32};
   return with_type(x->dtype, [&](auto t) {
     using T = decltype(t);
-    return with_shape<T>(x->cols, rows_aligned(x, 16) && rows_aligned(y, 16), [&](auto shape) {
+    return with_shape<T, false>(x->cols, rows_aligned(x, 16) && rows_aligned(y, 16), [&](auto shape) {
       using R = decltype(shape);
       if constexpr (std::is_same_v<R, int>) {
         const unsigned grid = (unsigned)std::min<long long>(x->rows, 2LL * ctx->num_sms);
         return check_launch(ctx, "norm_fwd_long_kernel", launch_pdl(norm_fwd_long_kernel<T>, dim3(grid), dim3(kLongThreads), 0, ctx->stream, a));
       } else {
         auto* kernel = norm_fwd_kernel<T, R>;
-        const abcd_status st = room_for(ctx, (const void*)kernel, R::kFwdSmem);
+        const abcd_status st = room_for(ctx, (const void*)kernel, R::kSmem);
         if (st != ABCD_OK) return st;
-        const unsigned grid = (unsigned)std::min<long long>((x->rows + R::kGroups - 1) / R::kGroups, R::kFwdCtas * ctx->num_sms);
-        return check_launch(ctx, "norm_fwd_kernel", launch_pdl(kernel, dim3(grid), dim3(R::kThreads), R::kFwdSmem, ctx->stream, a));
+        const unsigned grid = (unsigned)std::min<long long>((x->rows + R::kGroups - 1) / R::kGroups, R::kCtas * ctx->num_sms);
+        return check_launch(ctx, "norm_fwd_kernel", launch_pdl(kernel, dim3(grid), dim3(R::kThreads), R::kSmem, ctx->stream, a));
       }
     });
   });
@@ -537,15 +540,15 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
   int ctas = 0;
   const abcd_status st = with_type(x->dtype, [&](auto t) {
     using T = decltype(t);
-    return with_shape<T>(x->cols, aligned, [&](auto shape) {
+    return with_shape<T, true>(x->cols, aligned, [&](auto shape) {
       using R = decltype(shape);
       // CTAs: as many rows at a time as stay resident, each with its sums in the workspace
       constexpr bool kLong = std::is_same_v<R, int>;
       if constexpr (kLong) {
         ctas = (int)std::min<long long>(x->rows, 2LL * sms);
       } else {
-        static_assert(R::kBwdCtas <= kNormCtasPerSm);
-        ctas = (int)std::min<long long>((x->rows + R::kGroups - 1) / R::kGroups, R::kBwdCtas * sms);
+        static_assert(R::kCtas <= kNormCtasPerSm);
+        ctas = (int)std::min<long long>((x->rows + R::kGroups - 1) / R::kGroups, R::kCtas * sms);
       }
       const size_t need = kNetHeader + (size_t)ctas * 2 * (size_t)x->cols * sizeof(float);
       if (need > ctx->net_bytes)
@@ -555,9 +558,9 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
         return check_launch(ctx, "norm_bwd_long_kernel", launch_pdl(norm_bwd_long_kernel<T>, dim3(ctas), dim3(kLongThreads), 0, ctx->stream, a));
       } else {
         auto* kernel = norm_bwd_kernel<T, R>;
-        const abcd_status st = room_for(ctx, (const void*)kernel, R::kBwdSmem);
+        const abcd_status st = room_for(ctx, (const void*)kernel, R::kSmem);
         if (st != ABCD_OK) return st;
-        return check_launch(ctx, "norm_bwd_kernel", launch_pdl(kernel, dim3(ctas), dim3(R::kThreads), R::kBwdSmem, ctx->stream, a));
+        return check_launch(ctx, "norm_bwd_kernel", launch_pdl(kernel, dim3(ctas), dim3(R::kThreads), R::kSmem, ctx->stream, a));
       }
     });
   });
