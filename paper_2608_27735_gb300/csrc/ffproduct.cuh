@@ -142,6 +142,34 @@ __device__ __forceinline__ float take_term(float& v) {
   return t;
 }
 
+// Pairs of v as 16-bit values.
+template <int CW>
+__device__ __forceinline__ void pack_all(const float (&v)[CW], unsigned (&w)[CW / 2], bool bf16) {
+  if (bf16) {
+#pragma unroll
+    for (int i = 0; i < CW / 2; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], true);
+  } else {
+#pragma unroll
+    for (int i = 0; i < CW / 2; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], false);
+  }
+}
+
+// 16 bytes of a row of which `bytes` are inside the matrix.
+static __device__ __noinline__ void store_edge(char* at, uint4 v, int bytes, int vec, int elem) {
+  if (bytes <= 0) return;
+  if (vec && bytes >= 16) {
+    *reinterpret_cast<uint4*>(at) = v;
+    return;
+  }
+  const unsigned e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    if (2 * q >= bytes) break;
+    if (elem == 2) *reinterpret_cast<unsigned short*>(at + 2 * q) = (unsigned short)(e[q / 2] >> (16 * (q & 1)));
+    else if (!(q & 1)) *reinterpret_cast<unsigned*>(at + 2 * q) = e[q / 2];
+  }
+}
+
 // A warp's 32 rows x CW columns, lane l holding row l as words of 16-bit pairs (or 32-bit values):
 // turned round in the warp's buffer, so that consecutive lanes write consecutive 16 bytes of a row.
 // The buffer's 16-byte pieces are swapped by row so that neither side meets bank conflicts.
@@ -150,35 +178,24 @@ __device__ __forceinline__ void store_words(const unsigned (&w)[WORDS], char* bu
                                             long long stride_bytes, int rows, int bytes, bool vec, int elem) {
   constexpr int PIECES = WORDS / 4;                 // 16-byte pieces of a row
   constexpr int ROWS = 32 / PIECES;                 // rows that the lanes take at a time
-  const int lane = threadIdx.x & 31;
   constexpr int SPREAD = 8 / PIECES > 0 ? 8 / PIECES : 1;   // rows within 128 bytes of the buffer
+  const int lane = threadIdx.x & 31;
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < PIECES; ++j)
     *reinterpret_cast<uint4*>(buf + lane * PIECES * 16 + ((j ^ ((lane / SPREAD) % PIECES)) * 16)) =
         make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
   __syncwarp();
+  const int row0 = lane / PIECES, j = lane % PIECES;
+  char* at = (char*)base + row0 * stride_bytes + 16 * j;
+  const bool whole = vec && rows >= 32 && bytes >= PIECES * 16;
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
-    const int row = i * ROWS + lane / PIECES, j = lane % PIECES;
+    const int row = i * ROWS + row0;
     const uint4 v = *reinterpret_cast<const uint4*>(buf + row * PIECES * 16 + ((j ^ ((row / SPREAD) % PIECES)) * 16));
-    if (row >= rows || 16 * j >= bytes) continue;
-    char* at = (char*)base + row * stride_bytes + 16 * j;
-    if (vec && 16 * j + 16 <= bytes) {
-      *reinterpret_cast<uint4*>(at) = v;
-    } else {
-      const unsigned e[4] = {v.x, v.y, v.z, v.w};
-      if (elem == 4) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (16 * j + 4 * q < bytes) *reinterpret_cast<unsigned*>(at + 4 * q) = e[q];
-      } else {
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-          if (16 * j + 2 * q < bytes)
-            *reinterpret_cast<unsigned short*>(at + 2 * q) = (unsigned short)(e[q / 2] >> (16 * (q & 1)));
-      }
-    }
+    if (whole) *reinterpret_cast<uint4*>(at) = v;
+    else if (row < rows) store_edge(at, v, bytes - 16 * j, vec, elem);
+    at += ROWS * stride_bytes;
   }
 }
 
@@ -193,8 +210,7 @@ __device__ __forceinline__ void store_matrix(const float (&v)[CW], const Out& o,
     store_words<CW>(w, buf, (float*)o.p + m * o.stride + n, o.stride * 4, rows, cols * 4, o.vec, 4);
   } else {
     unsigned w[CW / 2];
-#pragma unroll
-    for (int i = 0; i < CW / 2; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], bf16);
+    pack_all(v, w, bf16);
     store_words<CW / 2>(w, buf, (unsigned short*)o.p + m * o.stride + n, o.stride * 2, rows, cols * 2, o.vec, 2);
   }
 }
@@ -258,6 +274,39 @@ __device__ __forceinline__ void load_row(float (&v)[CW], const Out& o, long long
   }
 }
 
+// Asynchronous copy of `bytes` (16 at most) to 16 bytes of shared memory, zeros after them.
+__device__ __forceinline__ void copy_piece(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes < 0 ? 0 : bytes < 16 ? bytes : 16) : "memory");
+}
+// Rows m ... m + rows of 32 columns of 16 bits from column n on, on their way to a warp's buffer of 32
+// rows of 64 bytes (pieces swapped by row as above).
+__device__ __forceinline__ void rows_ahead(char* buf, const Out& o, long long m, int n, int rows, int cols) {
+  const int lane = threadIdx.x & 31, j = lane % 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 8 * i + lane / 4, bytes = row < rows ? 2 * cols - 16 * j : 0;
+    const unsigned short* src = (const unsigned short*)o.p + (m + row) * o.stride + n + 8 * j;
+    copy_piece(smem_addr(buf + row * 64 + ((j ^ ((row / 2) % 4)) * 16)), bytes > 0 ? src : o.p, bytes);
+  }
+}
+// The lane's row of such a buffer: 16 values from its `half` on.
+__device__ __forceinline__ void row_of(float (&v)[16], const char* buf, int half, bool bf16) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int j = 2 * half + q;
+    const uint4 x = *reinterpret_cast<const uint4*>(buf + lane * 64 + ((j ^ ((lane / 2) % 4)) * 16));
+    const unsigned w[4] = {x.x, x.y, x.z, x.w};
+    if (bf16) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[8 * q + e] = unpack((unsigned short)(w[e / 2] >> (16 * (e & 1))), true);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[8 * q + e] = unpack((unsigned short)(w[e / 2] >> (16 * (e & 1))), false);
+    }
+  }
+}
+
 // A work item of the persistent loop.
 struct Item {
   int batch, split, tm, tn;
@@ -295,7 +344,6 @@ struct Product {
   static constexpr int kBRows = BN / CG;                 // rows of B per CTA
   static constexpr int kABytes = kRows * 128, kBBytes = kBRows * 128;
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = 196608 / kStageBytes > 8 ? 8 : 196608 / kStageBytes;
   static constexpr int kTmemCols = 2 * BN;
   static constexpr int kOutCols = EPI == kUp ? BN / 2 : BN;   // results per row of a tile
   // Epilogue warps: each takes 32 rows (a quarter of tensor memory's lanes) and a share of the
@@ -305,10 +353,15 @@ struct Product {
   static constexpr int kThreads = 64 + 32 * kWarps;      // TMA warp, MMA warp, epilogue
   static constexpr int kWarpCols = kOutCols / (kWarps / 4);
   static constexpr int CW = EPI != kPlain || kWarpCols < 32 ? 16 : 32;    // taken at a time
-  static constexpr int kBuffer = 32 * CW * (F32 ? 4 : 2);   // in which a warp turns its rows round
-  static_assert(kBuffer >= (EPI == kPlain ? 32 * 16 * 4 : 0));
+  // The saved projections that the epilogue reads come ahead, 32 columns at a time, where there is
+  // room for that: without it the large tile's epilogue waited most of its time for them.
+  static constexpr bool kAhead = EPI == kDown && !F32 && BN == 256;
+  static constexpr int kTurn = 32 * CW * (F32 ? 4 : 2);  // bytes in which a warp turns its rows round
+  static constexpr int kBuffer = kTurn + (kAhead ? 4096 : 0);
+  static constexpr int kRoom = (227 * 1024 - 512 - 1024 - kWarps * kBuffer) / kStageBytes;
+  static constexpr int kStages = kRoom > 8 ? 8 : kRoom;
+  static_assert(kTurn >= (EPI == kPlain ? 32 * 16 * 4 : 0) && kStages >= 4);
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (size_t)kWarps * kBuffer;
-  static_assert(kSmem + 512 <= 227 * 1024);
 };
 
 template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
@@ -438,24 +491,50 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
     const uint32_t empty0 = CG == 2 ? at_rank(sums_empty, 0) : sums_empty;
     int buf = 0;
     uint32_t phase = 0;
+    // the warp's rows and columns of an item
+    struct Part { int m, n, rows, cols; };
+    auto part_of = [&](const Item& it) {
+      Part p;
+      p.m = (it.tm * CG + (int)rank) * P::kRows + quarter * 32;
+      p.n = it.tn * P::kOutCols + share * P::kWarpCols;
+      p.rows = min(32, a.m - p.m);
+      p.cols = min(P::kWarpCols, a.n - p.n);
+      return p;
+    };
+    const bool ahead = P::kAhead && a.in[0].vec && a.in[1].vec;
+    char* zbuf = buffer + P::kTurn;
+    char* ubuf = zbuf + 2048;
+    auto ask = [&](const Part& p, int c) {             // 32 columns from c on of the saved projections
+      if (p.rows > 0 && p.cols > c) {
+        rows_ahead(zbuf, a.in[0], p.m, p.n + c, p.rows, p.cols - c);
+        rows_ahead(ubuf, a.in[1], p.m, p.n + c, p.rows, p.cols - c);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (ahead && first < items) ask(part_of(item_of(a, first)), 0);
     for (int i = first; i < items; i += step) {
       const Item it = item_of(a, i);
-      const int m = (it.tm * CG + (int)rank) * P::kRows + quarter * 32;   // the warp's first row
-      const int n = it.tn * P::kOutCols + share * P::kWarpCols;
-      const int rows = min(32, a.m - m), cols = min(P::kWarpCols, a.n - n);
+      const Part p = part_of(it);
+      const int m = p.m, n = p.n, rows = p.rows, cols = p.cols;
       if (!mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead)) break;
       tc_fence_after();
       const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16) + share * P::kWarpCols;
-      bool mine = rows > 0 && cols > 0;
+      // the sums have been read: the next tile but one may overwrite them
+      auto release = [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(empty0 + 8 * buf);
+      };
+      bool mine = rows > 0 && cols > 0, held = true;
       float* part = nullptr;
+      constexpr int PARTS = EPI == kUp ? 2 : 1;
+      constexpr long long PIECE = (long long)CG * P::kWarps * PARTS * P::kWarpCols * 32;
       if (EPI != kPlain && a.splits > 1) {
         // this part's sums to the workspace [column][row]; the last warp to have done so goes on
-        constexpr int PARTS = EPI == kUp ? 2 : 1;
-        const long long piece = (long long)CG * P::kWarps * PARTS * P::kWarpCols * 32;
-        part = a.part + (long long)it.tile * a.splits * piece +
+        part = a.part + (long long)it.tile * a.splits * PIECE +
                ((long long)rank * P::kWarps + ewarp) * PARTS * P::kWarpCols * 32 + lane;
         if (mine) {
-          float* mypart = part + it.split * piece;
+          float* mypart = part + it.split * PIECE;
 #pragma unroll 1
           for (int c = 0; c < PARTS * P::kWarpCols; c += P::CW) {
             float v[P::CW];
@@ -464,6 +543,8 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
 #pragma unroll
             for (int q = 0; q < P::CW; ++q) mypart[(c + q) * 32] = v[q];
           }
+          release();
+          held = false;
           __threadfence();
           __syncwarp();
           unsigned done = 0;
@@ -478,85 +559,103 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
         }
       }
       auto sum_columns = [&](int c, int which, float (&v)[P::CW]) {
-        if (a.splits == 1) {
+        if (EPI == kPlain || a.splits == 1) {
           tmem_load(sums + which * (BN / 2) + c, v);
         } else {
-          constexpr int PARTS = EPI == kUp ? 2 : 1;
-          const long long piece = (long long)CG * P::kWarps * PARTS * P::kWarpCols * 32;
 #pragma unroll
           for (int q = 0; q < P::CW; ++q) v[q] = 0.f;
 #pragma unroll 2
           for (int s = 0; s < a.splits; ++s) {
-            const float* p = part + s * piece + (which * P::kWarpCols + c) * 32;
+            const float* from = part + s * PIECE + (which * P::kWarpCols + c) * 32;
 #pragma unroll
-            for (int q = 0; q < P::CW; ++q) v[q] += __ldcg(p + q * 32);
+            for (int q = 0; q < P::CW; ++q) v[q] += __ldcg(from + q * 32);
           }
         }
       };
-      if (mine) {
+      const int end = mine ? min(cols, P::kWarpCols) : 0;
 #pragma unroll 1
-        for (int c = 0; c < P::kWarpCols; c += P::CW) {
-          const int left = cols - c;
-          if (left <= 0) break;
-          const int w = min(left, P::CW);
-          float v[P::CW];
-          if (EPI == kUp) {
-            float u[P::CW];
-            sum_columns(c, 0, v);
-            sum_columns(c, 1, u);
-            if (a.splits == 1) {
-              tmem_load_wait(v);
-              tmem_load_wait(u);
-            }
-            if (a.g[0].p) {
-              store_matrix<F32, P::CW>(v, a.g[0], m, n + c, rows, w, bf16, buffer);
-              store_matrix<F32, P::CW>(u, a.g[1], m, n + c, rows, w, bf16, buffer);
-            }
-            act_values(v, a.act);
+      for (int c = 0; c < end; c += P::CW) {
+        const int w = min(end - c, P::CW);
+        const bool last = held && c + P::CW >= end;
+        float v[P::CW];
+        if (EPI == kUp) {
+          float u[P::CW];
+          sum_columns(c, 0, v);
+          sum_columns(c, 1, u);
+          tmem_load_wait(v);
+          tmem_load_wait(u);
+          if (last) release();
+          if (a.g[0].p) {
+            store_matrix<F32, P::CW>(v, a.g[0], m, n + c, rows, w, bf16, buffer);
+            store_matrix<F32, P::CW>(u, a.g[1], m, n + c, rows, w, bf16, buffer);
+          }
+          act_values(v, a.act);
 #pragma unroll
-            for (int q = 0; q < P::CW; ++q) v[q] *= u[q];
-            store_operand<F32, P::CW>(v, a.c[0], m, n + c, rows, w, bf16, buffer);
-          } else if (EPI == kDown) {
-            float z[P::CW], u[P::CW], s[P::CW];
+          for (int q = 0; q < P::CW; ++q) v[q] *= u[q];
+          store_operand<F32, P::CW>(v, a.c[0], m, n + c, rows, w, bf16, buffer);
+        } else if (EPI == kDown) {
+          float z[P::CW], u[P::CW], s[P::CW];
+          if (ahead) {
+            if constexpr (P::kAhead) {
+              const int half = (c / 16) & 1;
+              if (half == 0) {
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                __syncwarp();
+              }
+              row_of(z, zbuf, half, bf16);
+              row_of(u, ubuf, half, bf16);
+              if (half == 1 || c + P::CW >= end) {     // both halves are read: ask for the next 32 columns
+                __syncwarp();
+                if (c + P::CW < end) ask(p, c + P::CW);
+                else if (i + step < items) ask(part_of(item_of(a, i + step)), 0);
+              }
+            }
+          } else {
             load_row<F32, P::CW>(z, a.in[0], m + lane, n + c, lane < rows, w, bf16);
             load_row<F32, P::CW>(u, a.in[1], m + lane, n + c, lane < rows, w, bf16);
-            sum_columns(c, 0, v);
-            act_slopes(z, s, a.act);
-            if (a.splits == 1) tmem_load_wait(v);
+          }
+          sum_columns(c, 0, v);
+          act_slopes(z, s, a.act);
+          tmem_load_wait(v);
+          if (last) release();
 #pragma unroll
-            for (int q = 0; q < P::CW; ++q) {
-              s[q] *= v[q] * u[q];
-              u[q] *= z[q];                              // the hidden matrix
-              z[q] *= v[q];
-            }
-            store_operand<F32, P::CW>(s, a.g[0], m, n + c, rows, w, bf16, buffer);
-            store_operand<F32, P::CW>(z, a.g[1], m, n + c, rows, w, bf16, buffer);
-            store_operand<F32, P::CW>(u, a.c[0], m, n + c, rows, w, bf16, buffer);
+          for (int q = 0; q < P::CW; ++q) {
+            s[q] *= v[q] * u[q];
+            u[q] *= z[q];                              // the hidden matrix
+            z[q] *= v[q];
+          }
+          store_operand<F32, P::CW>(s, a.g[0], m, n + c, rows, w, bf16, buffer);
+          store_operand<F32, P::CW>(z, a.g[1], m, n + c, rows, w, bf16, buffer);
+          store_operand<F32, P::CW>(u, a.c[0], m, n + c, rows, w, bf16, buffer);
+        } else {
+          sum_columns(c, 0, v);
+          tmem_load_wait(v);
+          if (last) release();
+          if (a.splits == 1) {
+            store_matrix<F32, P::CW>(v, a.c[it.batch], m, n + c, rows, w, bf16, buffer);
           } else {
-            tmem_load(sums + c, v);
-            tmem_load_wait(v);
-            if (a.splits == 1) {
-              store_matrix<F32, P::CW>(v, a.c[it.batch], m, n + c, rows, w, bf16, buffer);
-            } else {
-              const Out o{a.part + ((long long)it.split * a.batches + it.batch) * a.m * a.part_ld, a.part_ld, 0, 1};
+            const Out o{a.part + ((long long)it.split * a.batches + it.batch) * a.m * a.part_ld, a.part_ld, 0, 1};
 #pragma unroll
-              for (int e = 0; e < P::CW; e += 16) {      // sixteen of 32 bits take the buffer of 32 of 16
-                float x[16];
+            for (int e = 0; e < P::CW; e += 16) {      // sixteen of 32 bits take the buffer of 32 of 16
+              float x[16];
 #pragma unroll
-                for (int q = 0; q < 16; ++q) x[q] = v[e + q];
-                if (w > e) store_matrix<true, 16>(x, o, m, n + c + e, rows, min(16, w - e), false, buffer);
-              }
+              for (int q = 0; q < 16; ++q) x[q] = v[e + q];
+              if (w > e) store_matrix<true, 16>(x, o, m, n + c + e, rows, min(16, w - e), false, buffer);
             }
           }
         }
       }
-      // the sums have been read: the next tile but one may overwrite them
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(empty0 + 8 * buf);
+      if (end <= 0) {                                  // nothing to write: on to the next item's
+        if (held) release();
+        if (ahead && i + step < items) {
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+          ask(part_of(item_of(a, i + step)), 0);
+        }
+      }
       buf ^= 1;
       if (buf == 0) phase ^= 1;
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
   }
   __syncthreads();
   // a wait gave up: the copies and matrix instructions that are still in flight get time to end
