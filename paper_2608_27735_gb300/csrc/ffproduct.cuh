@@ -39,6 +39,9 @@ struct Out {
 
 struct ProductArgs {
   CUtensorMap a, b[2];
+  // the large tile of 16-bit matrices: kUp stores c, gate, up (g); kDown loads gate, up (in) and stores
+  // c, dG and dU (planes 0 and 1 of g[0])
+  CUtensorMap c_map, g_map[2], in_map[2];
   int m, n;                           // rows of A and B (kUp: of each B)
   int kblocks;                        // stages per segment
   int segments;
@@ -278,33 +281,61 @@ __device__ __forceinline__ void load_row(float (&v)[CW], const Out& o, long long
 __device__ __forceinline__ void copy_piece(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes < 0 ? 0 : bytes < 16 ? bytes : 16) : "memory");
 }
-// Rows m ... m + rows of 32 columns of 16 bits from column n on, on their way to a warp's buffer of 32
-// rows of 64 bytes (pieces swapped by row as above).
+// A warp's buffer of 32 rows of sixteen values: 16-byte pieces, swapped by row so that lanes which
+// read the same piece of their rows meet no bank conflicts.
+template <bool F32> struct RowBuffer {
+  static constexpr int kPieces = F32 ? 4 : 2;
+  static constexpr int kBytes = 32 * kPieces * 16;
+  __device__ static __forceinline__ int at(int row, int j) {
+    return (row * kPieces + (j ^ (row * kPieces / 8 % kPieces))) * 16;
+  }
+};
+// Rows m ... m + rows of sixteen columns from column n on, on their way to such a buffer.
+template <bool F32>
 __device__ __forceinline__ void rows_ahead(char* buf, const Out& o, long long m, int n, int rows, int cols) {
-  const int lane = threadIdx.x & 31, j = lane % 4;
+  using B = RowBuffer<F32>;
+  constexpr int SIZE = F32 ? 4 : 2;
+  const int lane = threadIdx.x & 31, j = lane % B::kPieces;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = 8 * i + lane / 4, bytes = row < rows ? 2 * cols - 16 * j : 0;
-    const unsigned short* src = (const unsigned short*)o.p + (m + row) * o.stride + n + 8 * j;
-    copy_piece(smem_addr(buf + row * 64 + ((j ^ ((row / 2) % 4)) * 16)), bytes > 0 ? src : o.p, bytes);
+  for (int i = 0; i < B::kPieces; ++i) {
+    const int row = i * (32 / B::kPieces) + lane / B::kPieces, bytes = row < rows ? SIZE * cols - 16 * j : 0;
+    const char* src = (const char*)o.p + ((m + row) * o.stride + n) * SIZE + 16 * j;
+    copy_piece(smem_addr(buf + B::at(row, j)), bytes > 0 ? src : (const char*)o.p, bytes);
   }
 }
-// The lane's row of such a buffer: 16 values from its `half` on.
-__device__ __forceinline__ void row_of(float (&v)[16], const char* buf, int half, bool bf16) {
+// Eight 16-bit values of 16 bytes.
+__device__ __forceinline__ void unpack8(float* v, const uint4& x, bool bf16) {
+  const unsigned w[4] = {x.x, x.y, x.z, x.w};
+  if (bf16) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = unpack((unsigned short)(w[e / 2] >> (16 * (e & 1))), true);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = unpack((unsigned short)(w[e / 2] >> (16 * (e & 1))), false);
+  }
+}
+// The lane's row of such a buffer.
+template <bool F32>
+__device__ __forceinline__ void row_of(float (&v)[16], const char* buf, bool bf16) {
+  using B = RowBuffer<F32>;
   const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int j = 2 * half + q;
-    const uint4 x = *reinterpret_cast<const uint4*>(buf + lane * 64 + ((j ^ ((lane / 2) % 4)) * 16));
-    const unsigned w[4] = {x.x, x.y, x.z, x.w};
-    if (bf16) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[8 * q + e] = unpack((unsigned short)(w[e / 2] >> (16 * (e & 1))), true);
+  for (int q = 0; q < B::kPieces; ++q) {
+    const uint4 x = *reinterpret_cast<const uint4*>(buf + B::at(lane, q));
+    if constexpr (F32) {
+      v[4 * q] = __uint_as_float(x.x); v[4 * q + 1] = __uint_as_float(x.y);
+      v[4 * q + 2] = __uint_as_float(x.z); v[4 * q + 3] = __uint_as_float(x.w);
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[8 * q + e] = unpack((unsigned short)(w[e / 2] >> (16 * (e & 1))), false);
+      unpack8(v + 8 * q, x, bf16);
     }
   }
+}
+
+// Where 16-byte piece j of a row lies in a block of 128 rows of 64 bytes under TMA's 64-byte swizzle.
+__device__ __forceinline__ int block_at(int row, int j) { return row * 64 + ((j ^ ((row / 2) % 4)) * 16); }
+__device__ __forceinline__ void put_block(char* block, int row, int j, const unsigned (&w)[8]) {
+  *reinterpret_cast<uint4*>(block + block_at(row, j)) = make_uint4(w[0], w[1], w[2], w[3]);
+  *reinterpret_cast<uint4*>(block + block_at(row, j + 1)) = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
 // A work item of the persistent loop.
@@ -350,25 +381,34 @@ struct Product {
   // columns.  Sixteen for the large tile of 16-bit matrices, whose products of few stages wait for
   // them.
   static constexpr int kWarps = BN == 256 && !F32 ? 16 : 8;
-  static constexpr int kThreads = 64 + 32 * kWarps;      // TMA warp, MMA warp, epilogue
+  // There the results (and the saved projections) also go through shared memory by TMA, in blocks of
+  // 128 rows x 32 columns that two groups of eight warps take in turn; kDown has a warp more, which
+  // asks for the blocks of the saved projections up to four ahead.  With accesses of the warps' own
+  // instead (32 bytes of a row at a time), 100,000 x 256 x 1,024 took 167 and 196 us for kUp and kDown.
+  static constexpr bool kBlocks = BN == 256 && !F32 && EPI != kPlain;
+  static constexpr int kBlockBytes = 128 * 64;
+  static constexpr int kSlots = 4;                       // kDown: blocks of gate and up
+  static constexpr int kBlockRoom = EPI == kUp ? 2 * 3 * kBlockBytes : (2 * kSlots + 2) * kBlockBytes;
+  static constexpr int kThreads = 64 + 32 * kWarps + (kBlocks && EPI == kDown ? 32 : 0);
   static constexpr int kWarpCols = kOutCols / (kWarps / 4);
   static constexpr int CW = EPI != kPlain || kWarpCols < 32 ? 16 : 32;    // taken at a time
-  // The saved projections that the epilogue reads come ahead, 32 columns at a time, where there is
-  // room for that: without it the large tile's epilogue waited most of its time for them.
-  static constexpr bool kAhead = EPI == kDown && !F32 && BN == 256;
-  static constexpr int kTurn = 32 * CW * (F32 ? 4 : 2);  // bytes in which a warp turns its rows round
-  static constexpr int kBuffer = kTurn + (kAhead ? 4096 : 0);
-  static constexpr int kRoom = (227 * 1024 - 512 - 1024 - kWarps * kBuffer) / kStageBytes;
+  // Elsewhere a warp turns its rows round in a buffer of its own, and kDown has the saved projections
+  // come two turns ahead.
+  static constexpr int kTurn = 32 * CW * (F32 ? 4 : 2);
+  static constexpr int kBuffer = kTurn + (EPI == kDown ? 4 * RowBuffer<F32>::kBytes : 0);
+  static constexpr int kEpilogueBytes = kBlocks ? kBlockRoom : kWarps * kBuffer;
+  static constexpr int kRoom = (227 * 1024 - 512 - 1024 - kEpilogueBytes) / kStageBytes;
   static constexpr int kStages = kRoom > 8 ? 8 : kRoom;
   static_assert(kTurn >= (EPI == kPlain ? 32 * 16 * 4 : 0) && kStages >= 4);
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (size_t)kWarps * kBuffer;
+  static_assert(EPI == kPlain || (CW == 16 && kWarpCols % 16 == 0));
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueBytes;
 };
 
 template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
 __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads, 1) product_kernel(const __grid_constant__ ProductArgs a) {
   using P = Product<CG, BN, AMN, BMN, EPI, F32>;
   extern __shared__ char smem_raw[];
-  __shared__ uint64_t bars[2 * P::kStages + 4];
+  __shared__ uint64_t bars[2 * P::kStages + 4 + 2 * P::kSlots];
   __shared__ uint32_t tmem_base;
   __shared__ volatile int dead;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
@@ -377,6 +417,7 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
   char* buffers = smem_raw + (ring - smem_addr(smem_raw)) + P::kStages * P::kStageBytes;
   const uint32_t full = smem_addr(bars), empty = full + 8 * P::kStages;
   const uint32_t sums_full = empty + 8 * P::kStages, sums_empty = sums_full + 16;
+  const uint32_t slot_full = sums_empty + 16, slot_empty = slot_full + 8 * P::kSlots;
   if (threadIdx.x == 0) {
     dead = 0;
     for (int s = 0; s < P::kStages; ++s) {
@@ -386,6 +427,10 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
     for (int s = 0; s < 2; ++s) {
       mbar_init(sums_full + 8 * s, 1);
       mbar_init(sums_empty + 8 * s, P::kWarps * CG);
+    }
+    for (int s = 0; s < P::kSlots; ++s) {
+      mbar_init(slot_full + 8 * s, 1);
+      mbar_init(slot_empty + 8 * s, 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_map(&a.a);
@@ -483,6 +528,135 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
         if (buf == 0) sums_phase ^= 1;
       }
     }
+  } else if constexpr (P::kBlocks) {
+    // Blocks of 32 result columns: the two groups take them in turn.  A wait that gave up skips the
+    // later waits and stores, not the groups' barriers.
+    constexpr int BLOCKS = P::kOutCols / 32;
+    const int row0 = (int)rank * P::kRows;
+    bool ok = true;
+    if (warp == 2 + P::kWarps) {
+      if (lane == 0) {
+        unsigned q = 0;
+        for (int i = first; ok && i < items; i += step) {
+          const Item it = item_of(a, i);
+          const int m = it.tm * CG * P::kRows + row0;
+          if (m >= a.m) continue;
+          for (int s = 0; s < BLOCKS; ++s) {
+            const int n = it.tn * P::kOutCols + 32 * s;
+            if (n >= a.n) break;
+            const int slot = q % P::kSlots;
+            if (!(ok = mbar_wait(slot_empty + 8 * slot, (q / P::kSlots & 1) ^ 1, a.limit, &dead))) break;
+            const uint32_t bar = slot_full + 8 * slot, at = smem_addr(buffers) + 2 * slot * P::kBlockBytes;
+            mbar_expect(bar, 2 * P::kBlockBytes);
+            tma_load<1>(at, &a.in_map[0], n, m, 0, bar);
+            tma_load<1>(at + P::kBlockBytes, &a.in_map[1], n, m, 0, bar);
+            ++q;
+          }
+        }
+      }
+    } else {
+      const int quarter = warp & 3, share = (warp - 2) / 4, group = share / 2, half = share & 1;
+      const int row = quarter * 32 + lane;
+      const bool bf16 = a.dtype == ABCD_BF16;
+      const bool saved = EPI == kUp && a.g[0].p;
+      const bool elected = (warp - 2) % 8 == 0 && lane == 0;   // of the group
+      const uint32_t empty0 = at_rank(sums_empty, 0);
+      // kUp: a group's three blocks; kDown: the slots, then a group's block of the hidden matrix
+      char* own = buffers + (EPI == kUp ? group * 3 * P::kBlockBytes : (2 * P::kSlots + group) * P::kBlockBytes);
+      int buf = 0, last_slot = -1;
+      uint32_t phase = 0;
+      unsigned q = 0;                                          // blocks of the CTA so far
+      for (int i = first; i < items; i += step) {
+        const Item it = item_of(a, i);
+        const int m = it.tm * CG * P::kRows + row0, n0 = it.tn * P::kOutCols;
+        ok = ok && mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead);
+        tc_fence_after();
+        const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16);
+        const int blocks = m < a.m ? min(BLOCKS, (a.n - n0 + 31) / 32) : 0;
+#pragma unroll 1
+        for (int s = (q + group) & 1; s < blocks; s += 2) {
+          const int c = 32 * s + 16 * half;
+          float v[16], u[16];
+          unsigned x[8];
+          tmem_load(sums + c, v);
+          if constexpr (EPI == kUp) {
+            tmem_load(sums + BN / 2 + c, u);
+            tmem_load_wait(v);
+            tmem_load_wait(u);
+            if (elected) tma_store_read();
+            named_barrier(1 + group, 256);                     // the group's blocks may be written
+            if (saved) {
+              pack_all(v, x, bf16);
+              put_block(own + P::kBlockBytes, row, 2 * half, x);
+              pack_all(u, x, bf16);
+              put_block(own + 2 * P::kBlockBytes, row, 2 * half, x);
+            }
+            act_values(v, a.act);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] *= u[e];
+            pack_all(v, x, bf16);
+            put_block(own, row, 2 * half, x);
+          } else {
+            const unsigned at = q + s;
+            const int slot = at % P::kSlots;
+            char* zblock = buffers + 2 * slot * P::kBlockBytes;
+            char* ublock = zblock + P::kBlockBytes;
+            ok = ok && mbar_wait(slot_full + 8 * slot, at / P::kSlots & 1, a.limit, &dead);
+            float z[16], d[16];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              unpack8(z + 8 * e, *reinterpret_cast<const uint4*>(zblock + block_at(row, 2 * half + e)), bf16);
+              unpack8(u + 8 * e, *reinterpret_cast<const uint4*>(ublock + block_at(row, 2 * half + e)), bf16);
+            }
+            act_slopes(z, d, a.act);
+            tmem_load_wait(v);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              d[e] *= v[e] * u[e];
+              u[e] *= z[e];                                    // the hidden matrix
+              z[e] *= v[e];
+            }
+            if (elected) {
+              tma_store_read();                                // the group's last block has been read
+              if (last_slot >= 0) mbar_arrive(slot_empty + 8 * last_slot);
+              last_slot = slot;
+            }
+            named_barrier(1 + group, 256);
+            pack_all(d, x, bf16);                              // in the places of what the lane has read
+            put_block(zblock, row, 2 * half, x);
+            pack_all(z, x, bf16);
+            put_block(ublock, row, 2 * half, x);
+            pack_all(u, x, bf16);
+            put_block(own, row, 2 * half, x);
+          }
+          smem_to_tma();
+          named_barrier(1 + group, 256);
+          if (elected && ok) {
+            const int n = n0 + 32 * s;
+            if constexpr (EPI == kUp) {
+              if (saved) {
+                tma_store(&a.g_map[0], n, m, 0, smem_addr(own + P::kBlockBytes));
+                tma_store(&a.g_map[1], n, m, 0, smem_addr(own + 2 * P::kBlockBytes));
+              }
+            } else {
+              const int slot = (q + s) % P::kSlots;
+              tma_store(&a.g_map[0], n, m, 0, smem_addr(buffers + 2 * slot * P::kBlockBytes));
+              tma_store(&a.g_map[0], n, m, 1, smem_addr(buffers + (2 * slot + 1) * P::kBlockBytes));
+            }
+            tma_store(&a.c_map, n, m, 0, smem_addr(own));
+            tma_store_commit();
+          }
+        }
+        // the sums have been read: the next tile but one may overwrite them
+        q += blocks;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(empty0 + 8 * buf);
+        buf ^= 1;
+        if (buf == 0) phase ^= 1;
+      }
+      if (elected) tma_store_done();
+    }
   } else {
     // a warp reads the quarter of tensor memory's lanes that its number in the CTA gives it
     const int quarter = warp & 3, share = (warp - 2) / 4, ewarp = warp - 2;
@@ -501,20 +675,31 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       p.cols = min(P::kWarpCols, a.n - p.n);
       return p;
     };
-    const bool ahead = P::kAhead && a.in[0].vec && a.in[1].vec;
-    char* zbuf = buffer + P::kTurn;
-    char* ubuf = zbuf + 2048;
-    auto ask = [&](const Part& p, int c) {             // 32 columns from c on of the saved projections
-      if (p.rows > 0 && p.cols > c) {
-        rows_ahead(zbuf, a.in[0], p.m, p.n + c, p.rows, p.cols - c);
-        rows_ahead(ubuf, a.in[1], p.m, p.n + c, p.rows, p.cols - c);
+    const bool ahead = EPI == kDown && a.in[0].vec && a.in[1].vec;
+    // kDown: the saved projections of turn t of an item (16 columns), to one of two pairs of buffers
+    char* saved = buffer + P::kTurn;
+    constexpr int TURNS = P::kWarpCols / P::CW, SAVED = RowBuffer<F32>::kBytes;
+    auto ask = [&](const Part& p, int t) {
+      if (p.rows > 0 && p.cols > t * 16) {
+        rows_ahead<F32>(saved + (t & 1) * 2 * SAVED, a.in[0], p.m, p.n + t * 16, p.rows, p.cols - t * 16);
+        rows_ahead<F32>(saved + (t & 1) * 2 * SAVED + SAVED, a.in[1], p.m, p.n + t * 16, p.rows, p.cols - t * 16);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    if (ahead && first < items) ask(part_of(item_of(a, first)), 0);
+    Item it{};
+    Part p{0, 0, 0, 0};
+    if (first < items) {
+      it = item_of(a, first);
+      p = part_of(it);
+    }
+    if (ahead) {
+      ask(p, 0);
+      ask(p, 1);
+    }
     for (int i = first; i < items; i += step) {
-      const Item it = item_of(a, i);
-      const Part p = part_of(it);
+      const Item next = item_of(a, min(i + step, items - 1));
+      Part then = part_of(next);
+      if (i + step >= items) then.rows = 0;
       const int m = p.m, n = p.n, rows = p.rows, cols = p.cols;
       if (!mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead)) break;
       tc_fence_after();
@@ -574,11 +759,18 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       };
       const int end = mine ? min(cols, P::kWarpCols) : 0;
 #pragma unroll 1
-      for (int c = 0; c < end; c += P::CW) {
+      for (int c = 0; c < P::kWarpCols; c += P::CW) {
+        if (c >= end) {
+          if (!ahead) break;
+          asm volatile("cp.async.wait_group 1;" ::: "memory");
+          if (c / 16 + 2 < TURNS) ask(p, c / 16 + 2);
+          else ask(then, c / 16 + 2 - TURNS);
+          continue;
+        }
         const int w = min(end - c, P::CW);
         const bool last = held && c + P::CW >= end;
         float v[P::CW];
-        if (EPI == kUp) {
+        if constexpr (EPI == kUp) {
           float u[P::CW];
           sum_columns(c, 0, v);
           sum_columns(c, 1, u);
@@ -593,23 +785,17 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
 #pragma unroll
           for (int q = 0; q < P::CW; ++q) v[q] *= u[q];
           store_operand<F32, P::CW>(v, a.c[0], m, n + c, rows, w, bf16, buffer);
-        } else if (EPI == kDown) {
+        } else if constexpr (EPI == kDown) {
           float z[P::CW], u[P::CW], s[P::CW];
+          const char* zbuf = saved + (c / 16 & 1) * 2 * SAVED;
           if (ahead) {
-            if constexpr (P::kAhead) {
-              const int half = (c / 16) & 1;
-              if (half == 0) {
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-                __syncwarp();
-              }
-              row_of(z, zbuf, half, bf16);
-              row_of(u, ubuf, half, bf16);
-              if (half == 1 || c + P::CW >= end) {     // both halves are read: ask for the next 32 columns
-                __syncwarp();
-                if (c + P::CW < end) ask(p, c + P::CW);
-                else if (i + step < items) ask(part_of(item_of(a, i + step)), 0);
-              }
-            }
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            __syncwarp();
+            row_of<F32>(z, zbuf, bf16);
+            row_of<F32>(u, zbuf + SAVED, bf16);
+            __syncwarp();
+            if (c / 16 + 2 < TURNS) ask(p, c / 16 + 2);
+            else ask(then, c / 16 + 2 - TURNS);
           } else {
             load_row<F32, P::CW>(z, a.in[0], m + lane, n + c, lane < rows, w, bf16);
             load_row<F32, P::CW>(u, a.in[1], m + lane, n + c, lane < rows, w, bf16);
@@ -645,13 +831,9 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
           }
         }
       }
-      if (end <= 0) {                                  // nothing to write: on to the next item's
-        if (held) release();
-        if (ahead && i + step < items) {
-          asm volatile("cp.async.wait_group 0;" ::: "memory");
-          ask(part_of(item_of(a, i + step)), 0);
-        }
-      }
+      if (held && end <= 0) release();
+      it = next;
+      p = then;
       buf ^= 1;
       if (buf == 0) phase ^= 1;
     }

@@ -26,14 +26,14 @@ struct Operand {
 int terms_of(int dtype) { return dtype == ABCD_F32 ? 3 : 1; }
 long long pitch_of(long long cols) { return (cols + 63) / 64 * 64; }   // whole 128-byte lines
 
-// Up to five matrices that are laid out as operands by one launch.
+// Up to seven matrices that are laid out as operands by one launch.
 struct PackArgs {
   struct One {
     const void* src;
     unsigned short* dst;
     long long rows, cols, stride, pitch, plane;
     long long first;                  // blocks of eight columns before this matrix's
-  } m[5];
+  } m[7];
   int n;
   long long blocks;
 };
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackA
   for (long long i = blockIdx.x * 256LL + threadIdx.x; i < a.blocks; i += gridDim.x * 256LL) {
     int k = 0;
 #pragma unroll
-    for (int q = 1; q < 5; ++q) k += q < a.n && i >= a.m[q].first;
+    for (int q = 1; q < 7; ++q) k += q < a.n && i >= a.m[q].first;
     const PackArgs::One& o = a.m[k];
     const long long groups = (o.cols + 7) / 8, at = i - o.first;
     const long long row = at < (1LL << 32) ? (unsigned)at / (unsigned)groups : at / groups;
@@ -83,6 +83,28 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackA
       }
       *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
     }
+  }
+}
+
+// Two 16-bit operands of rows of 16-byte boundaries to matrices whose rows start anywhere.
+struct UnpackArgs {
+  const unsigned short* src[2];
+  unsigned short* dst[2];
+  long long rows, cols, pitch, stride[2];
+};
+__global__ void __launch_bounds__(256) unpack_kernel(const __grid_constant__ UnpackArgs a) {
+  pdl_wait();
+  const long long groups = (a.cols + 7) / 8, total = groups * a.rows;
+  const int k = blockIdx.y;
+  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < total; i += gridDim.x * 256LL) {
+    const long long row = i < (1LL << 32) ? (unsigned)i / (unsigned)groups : i / groups;
+    const int col = (int)(8 * (i - row * groups)), left = (int)(a.cols - col);
+    const uint4 v = *reinterpret_cast<const uint4*>(a.src[k] + row * a.pitch + col);
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+    unsigned short* to = a.dst[k] + row * a.stride[k] + col;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) to[j] = (unsigned short)(w[j / 2] >> (16 * (j & 1)));
   }
 }
 
@@ -140,13 +162,17 @@ struct Scratch {
 
 bool needs_pack(const abcd_matrix* m) { return m->dtype == ABCD_F32 || !rows_aligned(m, 16); }
 
+Operand in_place(const abcd_matrix* m) {
+  return Operand{m->data, m->rows, m->cols, (m->stride + 7) / 8 * 8, 0, 1};
+}
+
 // The matrices of a call as operands: in place where TMA can read them, else as copies in the
 // workspace, which one launch makes.
 struct Operands {
   Scratch& s;
   PackArgs args{};
   Operand add(const abcd_matrix* m) {
-    if (!needs_pack(m)) return Operand{m->data, m->rows, m->cols, (m->stride + 7) / 8 * 8, 0, 1};
+    if (!needs_pack(m)) return in_place(m);
     const Operand o = s.operand(m->rows, m->cols, m->dtype);
     args.m[args.n++] = PackArgs::One{m->data, (unsigned short*)o.p, m->rows, m->cols, m->stride, o.pitch, o.plane, args.blocks};
     args.blocks += (m->cols + 7) / 8 * m->rows;
@@ -177,17 +203,17 @@ EncodeFn encode_fn() {
   return fn;
 }
 
-// The tensor map of an operand with boxes of 64 consecutive columns and `box_rows` rows; what lies
-// outside the matrix reads as zero.
-bool make_map(CUtensorMap* map, const Operand& o, int dtype, int box_rows) {
+// The tensor map of an operand with boxes of 64 (or 32) consecutive columns and `box_rows` rows, their
+// rows' 128 (64) bytes swizzled; what lies outside the matrix reads as zero.
+bool make_map(CUtensorMap* map, const Operand& o, int dtype, int box_rows, int box_cols = 64) {
   const EncodeFn fn = encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.planes};
   const cuuint64_t strides[2] = {(cuuint64_t)o.pitch * 2, (cuuint64_t)std::max<long long>(o.plane, o.pitch) * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, unit[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, unit[3] = {1, 1, 1};
   return fn(map, dtype == ABCD_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
             const_cast<void*>(o.p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -201,24 +227,36 @@ Out out_of(const Operand& o, int matrix, int dtype) {
 // One product: A and up to two B operands, whether each lies with its own dimension contiguous.
 struct Job {
   Operand a, b[2];
+  Operand c, g[2], in[2];    // kUp, kDown: the matrices of the epilogue (g[0].p NULL: no gate and up)
   int nb;                    // B operands (kPlain with two: the sum of both products)
   long long m, n, k;
   int batches;
   ProductArgs args;
 };
 
-// Picks the shape and the number of splits with the least estimated time: the waves of tiles times
-// their stages, plus what a tile costs apart from them, plus the splits' joining.
-void plan(int sms, long long m, long long n, int epi, long long kblocks, int segments, long long batches, int* shape, int* splits) {
+// Cycles that a tile's epilogue takes per column of sums: about what the products of few stages
+// measured (the large tile's sixteen warps of 16-bit matrices; half as many otherwise).
+double epilogue_cycles(int epi, bool f32, int bn) {
+  const double per_column[3] = {20, 33, 80};           // kPlain, kUp, kDown
+  return per_column[epi] * bn * (f32 ? 3.0 : bn == 256 ? 1.0 : 1.5);
+}
+
+// Picks the shape and the number of splits with the least estimated time: the waves of tiles, each
+// its stages or (beside the next tile's stages) its epilogue, plus the last epilogue, plus the
+// splits' joining.
+void plan(int sms, long long m, long long n, int epi, bool f32, long long kblocks, int segments, long long batches, int* shape, int* splits) {
   double best = 1e300;
   for (int s = 0; s < 3; ++s) {
     const long long cols = epi == kUp ? kShapes[s].bn / 2 : kShapes[s].bn;
     const long long units = sms / kShapes[s].cg;
     const long long tiles = batches * ((m + 128 * kShapes[s].cg - 1) / (128 * kShapes[s].cg)) * ((n + cols - 1) / cols);
     const long long most = std::max<long long>(1, std::min<long long>({units / std::max<long long>(1, tiles), kblocks * segments / 4, kblocks, 64}));
-    for (long long p = 1; p <= most; ++p) {
+    const double epilogue = epilogue_cycles(epi, f32, kShapes[s].bn);
+    // the large tile's blocks of results are whole sums
+    for (long long p = 1; p <= (s == 0 && epi != kPlain && !f32 ? 1 : most); ++p) {
       const double waves = (double)((tiles * p + units - 1) / units);
-      const double t = waves * ((double)(segments * ((kblocks + p - 1) / p)) * kShapes[s].cycles + 2000.0) + (p > 1 ? 3000.0 + 150.0 * p : 0.0);
+      const double stages = (double)(segments * ((kblocks + p - 1) / p)) * kShapes[s].cycles;
+      const double t = waves * std::max(stages, epilogue) + std::min(stages, epilogue) + 2000.0 + (p > 1 ? 3000.0 + 150.0 * p : 0.0);
       if (t < best) {
         best = t;
         *shape = s;
@@ -228,8 +266,26 @@ void plan(int sms, long long m, long long n, int epi, long long kblocks, int seg
   }
 }
 
+// Segments of a product: pairs of its operands' terms.
+int segments_of(int which, int dtype, int nb) {
+  return (which == kProductUp ? 1 : nb) * (dtype == ABCD_F32 ? 6 : 1);
+}
+int epilogue_of(int which) { return which == kProductUp ? kUp : which == kProductDown ? kDown : kPlain; }
+
+void plan_of(const abcd_ctx* ctx, int dtype, int which, int nb, long long m, long long n, long long k, long long batches, int* shape, int* splits) {
+  plan(std::min(ctx->num_sms, kNetSms), m, n, epilogue_of(which), dtype == ABCD_F32, (k + kBlockK - 1) / kBlockK,
+       segments_of(which, dtype, nb), batches, shape, splits);
+}
+// Whether the epilogue of kProductUp or kProductDown moves the saved projections by TMA.
+bool by_blocks(const abcd_ctx* ctx, int dtype, int which, long long m, long long n, long long k) {
+  int shape = 0, splits = 1;
+  if (dtype == ABCD_F32) return false;
+  plan_of(ctx, dtype, which, 1, m, n, k, 1, &shape, &splits);
+  return shape == 0;
+}
+
 abcd_status run(abcd_ctx* ctx, int dtype, int which, Job& j) {
-  const int epi = which == kProductUp ? kUp : which == kProductDown ? kDown : kPlain;
+  const int epi = epilogue_of(which);
   const bool amn = which == kProductDw, bmn = amn || which == kProductDown || which == kProductDx;
   ProductArgs& a = j.args;
   const int terms = terms_of(dtype);
@@ -250,7 +306,7 @@ abcd_status run(abcd_ctx* ctx, int dtype, int which, Job& j) {
   a.batch_az = terms;
   a.dtype = dtype;
   int shape = 0, splits = 1;
-  plan(std::min(ctx->num_sms, kNetSms), j.m, j.n, epi, a.kblocks, a.segments, j.batches, &shape, &splits);
+  plan_of(ctx, dtype, which, j.nb, j.m, j.n, j.k, j.batches, &shape, &splits);
   const int cg = kShapes[shape].cg, bn = kShapes[shape].bn;
   a.tiles_m = (int)((j.m + 128 * cg - 1) / (128 * cg));
   const int cols = epi == kUp ? bn / 2 : bn;
@@ -264,6 +320,13 @@ abcd_status run(abcd_ctx* ctx, int dtype, int which, Job& j) {
   for (int b = 0; ok && b < j.nb; ++b) ok = make_map(&a.b[b], j.b[b], dtype, bmn ? 64 : epi == kUp ? bn / 2 : bn / cg);
   if (!ok) return fail(ctx, ABCD_ERR_CUDA, "tensor map of a product");
   if (j.nb < 2) a.b[1] = a.b[0];
+  if (epi != kPlain && shape == 0 && dtype != ABCD_F32) {
+    ok = make_map(&a.c_map, j.c, dtype, 128, 32);
+    if (ok && j.g[0].p) ok = make_map(&a.g_map[0], j.g[0], dtype, 128, 32);
+    if (ok && j.g[1].p) ok = make_map(&a.g_map[1], j.g[1], dtype, 128, 32);
+    for (int b = 0; ok && epi == kDown && b < 2; ++b) ok = make_map(&a.in_map[b], j.in[b], dtype, 128, 32);
+    if (!ok) return fail(ctx, ABCD_ERR_CUDA, "tensor map of a product's results");
+  }
   a.part_ld = (j.n + 3) / 4 * 4;
   const abcd_status st = dtype == ABCD_F32 ? launch_32(ctx, which, shape, a) : launch_16(ctx, which, shape, a);
   if (st != ABCD_OK || epi != kPlain || splits == 1) return st;
@@ -289,6 +352,7 @@ size_t ff_scratch(long long rows, long long cols, long long ff, int dtype) {
   s.operand(cols, ff, dtype);             // w_down
   s.operand(rows, ff, dtype);             // hidden
   s.operand(rows, ff, dtype, 2);          // dG, dU
+  if (dtype != ABCD_F32) s.operand(rows, ff, dtype, 2);   // gate, up
   return s.at;
 }
 
@@ -350,6 +414,9 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
   if (needs_pack(w_up)) need.operand(f, d, t);
   if (needs_pack(w_down)) need.operand(d, f, t);
   need.operand(m, f, t);
+  // the saved projections by way of the workspace where TMA has to store them and cannot
+  const bool apart = gate && (needs_pack(gate) || needs_pack(up)) && by_blocks(ctx, t, kProductUp, m, f, d);
+  if (apart) need.operand(m, f, t, 2);
   abcd_status st = room(ctx, what, need.at);
   if (st != ABCD_OK) return st;
   Scratch s{ctx->net_base};
@@ -358,15 +425,29 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
   const Operand ox = in.add(x), og = in.add(w_gate), ou = in.add(w_up), od = in.add(w_down);
   if ((st = in.pack(ctx, t)) != ABCD_OK) return st;
   const Operand h = s.operand(m, f, t);
-  Job up_job{ox, {og, ou}, 2, m, f, d, 1, {}};
+  Job up_job{ox, {og, ou}, h, {}, {}, 2, m, f, d, 1, {}};
   up_job.args.act = activation;
   up_job.args.c[0] = out_of(h, 0, t);
-  if (gate) {
+  if (apart) {
+    const Operand saved = s.operand(m, f, t, 2);
+    up_job.g[0] = Operand{saved.p, m, f, saved.pitch, 0, 1};
+    up_job.g[1] = Operand{(unsigned short*)saved.p + saved.plane, m, f, saved.pitch, 0, 1};
+    for (int k = 0; k < 2; ++k) up_job.args.g[k] = out_of(up_job.g[k], 0, t);
+  } else if (gate) {
     up_job.args.g[0] = out_of(gate);
     up_job.args.g[1] = out_of(up);
+    up_job.g[0] = in_place(gate);
+    up_job.g[1] = in_place(up);
   }
   if ((st = run(ctx, t, kProductUp, up_job)) != ABCD_OK) return st;
-  Job y_job{h, {od, od}, 1, m, d, f, 1, {}};
+  if (apart) {
+    const UnpackArgs u{{(const unsigned short*)up_job.g[0].p, (const unsigned short*)up_job.g[1].p},
+                       {(unsigned short*)gate->data, (unsigned short*)up->data},
+                       m, f, up_job.g[0].pitch, {gate->stride, up->stride}};
+    const dim3 grid((unsigned)std::min<long long>((m * ((f + 7) / 8) + 255) / 256, 8LL * ctx->num_sms), 2);
+    if ((st = check_launch(ctx, "unpack_kernel", launch_pdl(unpack_kernel, grid, dim3(256), 0, ctx->stream, u))) != ABCD_OK) return st;
+  }
+  Job y_job{h, {od, od}, {}, {}, {}, 1, m, d, f, 1, {}};
   y_job.args.c[0] = out_of(y);
   return run(ctx, t, kProductOut, y_job);
 }
@@ -408,6 +489,9 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
   if (needs_pack(w_gate)) need.operand(f, d, t);
   if (needs_pack(w_up)) need.operand(f, d, t);
   if (needs_pack(w_down)) need.operand(d, f, t);
+  const bool apart = t != ABCD_F32;                // gate and up are read as they are in 32 bits
+  if (apart && needs_pack(gate)) need.operand(m, f, t);
+  if (apart && needs_pack(up)) need.operand(m, f, t);
   need.operand(m, f, t);
   need.operand(m, f, t, 2);
   abcd_status st = room(ctx, what, need.at);
@@ -416,7 +500,11 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
   s.take(kPartBytes);
   Operands in{s};
   const Operand ody = in.add(dy), od = in.add(w_down);
-  Operand ox{}, og{}, ou{};
+  Operand ox{}, og{}, ou{}, ogate{}, oup{};
+  if (apart) {
+    ogate = in.add(gate);
+    oup = in.add(up);
+  }
   if (dw_gate || dw_up) ox = in.add(x);
   if (dx) {
     og = in.add(w_gate);
@@ -424,16 +512,16 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
   }
   if ((st = in.pack(ctx, t)) != ABCD_OK) return st;
   const Operand h = s.operand(m, f, t), dgu = s.operand(m, f, t, 2);
-  Job down{ody, {od, od}, 1, m, f, d, 1, {}};
+  Job down{ody, {od, od}, h, {dgu, {}}, {ogate, oup}, 1, m, f, d, 1, {}};
   down.args.act = activation;
-  down.args.in[0] = out_of(gate);
-  down.args.in[1] = out_of(up);
+  down.args.in[0] = apart ? out_of(ogate, 0, t) : out_of(gate);
+  down.args.in[1] = apart ? out_of(oup, 0, t) : out_of(up);
   down.args.c[0] = out_of(h, 0, t);
   down.args.g[0] = out_of(dgu, 0, t);
   down.args.g[1] = out_of(dgu, 1, t);
   if ((st = run(ctx, t, kProductDown, down)) != ABCD_OK) return st;
   if (dx) {
-    Job j{dgu, {og, ou}, 2, m, d, f, 1, {}};
+    Job j{dgu, {og, ou}, {}, {}, {}, 2, m, d, f, 1, {}};
     j.args.c[0] = out_of(dx);
     if ((st = run(ctx, t, kProductDx, j)) != ABCD_OK) return st;
   }
@@ -442,13 +530,13 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
     Operand left = dgu;
     if (!dw_gate) left.p = (const unsigned short*)dgu.p + (long long)terms_of(t) * dgu.plane;
     left.planes = dw_gate && dw_up ? dgu.planes : terms_of(t);
-    Job j{left, {ox, ox}, 1, f, d, m, dw_gate && dw_up ? 2 : 1, {}};
+    Job j{left, {ox, ox}, {}, {}, {}, 1, f, d, m, dw_gate && dw_up ? 2 : 1, {}};
     j.args.c[0] = out_of(dw_gate ? dw_gate : dw_up);
     if (dw_gate && dw_up) j.args.c[1] = out_of(dw_up);
     if ((st = run(ctx, t, kProductDw, j)) != ABCD_OK) return st;
   }
   if (dw_down) {
-    Job j{ody, {h, h}, 1, d, f, m, 1, {}};
+    Job j{ody, {h, h}, {}, {}, {}, 1, d, f, m, 1, {}};
     j.args.c[0] = out_of(dw_down);
     if ((st = run(ctx, t, kProductDw, j)) != ABCD_OK) return st;
   }

@@ -145,7 +145,8 @@ def test_norm_keeps_a_bad_row_to_itself(ctx):
 # ---- gated feed-forward
 
 FF_SHAPES = [(1, 1, 1), (1, 64, 128), (2, 59, 77), (7, 64, 256), (129, 64, 128), (130, 250, 999),
-             (300, 33, 513), (257, 256, 64), (64, 520, 136), (16, 1024, 512), (1500, 8, 16)]
+             (300, 33, 513), (257, 256, 64), (64, 520, 136), (16, 1024, 512), (1500, 8, 16),
+            (3001, 72, 1032), (2900, 136, 1100)]
 
 
 def ff_weights(r, d, f, kind, pad, lead):
