@@ -383,12 +383,16 @@ struct Product {
   static constexpr int kWarps = BN == 256 && !F32 ? 16 : 8;
   // There the results (and the saved projections) also go through shared memory by TMA, in blocks of
   // 128 rows x 32 columns that two groups of eight warps take in turn; kDown has a warp more, which
-  // asks for the blocks of the saved projections up to four ahead.  With accesses of the warps' own
+  // asks for the blocks of the saved projections up to three ahead.  With accesses of the warps' own
   // instead (32 bytes of a row at a time), 100,000 x 256 x 1,024 took 167 and 196 us for kUp and kDown.
   static constexpr bool kBlocks = BN == 256 && !F32 && EPI != kPlain;
   static constexpr int kBlockBytes = 128 * 64;
-  static constexpr int kSlots = 4;                       // kDown: blocks of gate and up
-  static constexpr int kBlockRoom = EPI == kUp ? 2 * 3 * kBlockBytes : (2 * kSlots + 2) * kBlockBytes;
+  // Three blocks of results per group (twice for kUp, whose next ones need not wait for TMA to have
+  // read the last), and for kDown slots of a block of gate and one of up.
+  // (A slot's blocks go to the groups in turn.  So it has two barriers that say it is full, one for each
+  // group: a wait for a phase is right only for who has seen the phase before it end.)
+  static constexpr int kSlots = 3, kTurns = EPI == kUp ? 2 : 1;
+  static constexpr int kBlockRoom = (2 * 3 * kTurns + (EPI == kDown ? 2 * kSlots : 0)) * kBlockBytes;
   static constexpr int kThreads = 64 + 32 * kWarps + (kBlocks && EPI == kDown ? 32 : 0);
   static constexpr int kWarpCols = kOutCols / (kWarps / 4);
   static constexpr int CW = EPI != kPlain || kWarpCols < 32 ? 16 : 32;    // taken at a time
@@ -408,7 +412,7 @@ template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
 __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads, 1) product_kernel(const __grid_constant__ ProductArgs a) {
   using P = Product<CG, BN, AMN, BMN, EPI, F32>;
   extern __shared__ char smem_raw[];
-  __shared__ uint64_t bars[2 * P::kStages + 4 + 2 * P::kSlots];
+  __shared__ uint64_t bars[2 * P::kStages + 4 + 3 * P::kSlots];
   __shared__ uint32_t tmem_base;
   __shared__ volatile int dead;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
@@ -417,7 +421,7 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
   char* buffers = smem_raw + (ring - smem_addr(smem_raw)) + P::kStages * P::kStageBytes;
   const uint32_t full = smem_addr(bars), empty = full + 8 * P::kStages;
   const uint32_t sums_full = empty + 8 * P::kStages, sums_empty = sums_full + 16;
-  const uint32_t slot_full = sums_empty + 16, slot_empty = slot_full + 8 * P::kSlots;
+  const uint32_t slot_full = sums_empty + 16, slot_empty = slot_full + 16 * P::kSlots;
   if (threadIdx.x == 0) {
     dead = 0;
     for (int s = 0; s < P::kStages; ++s) {
@@ -429,8 +433,9 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       mbar_init(sums_empty + 8 * s, P::kWarps * CG);
     }
     for (int s = 0; s < P::kSlots; ++s) {
-      mbar_init(slot_full + 8 * s, 1);
-      mbar_init(slot_empty + 8 * s, 1);
+      mbar_init(slot_full + 16 * s, 1);
+      mbar_init(slot_full + 16 * s + 8, 1);
+      mbar_init(slot_empty + 8 * s, 8);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_map(&a.a);
@@ -546,7 +551,7 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
             if (n >= a.n) break;
             const int slot = q % P::kSlots;
             if (!(ok = mbar_wait(slot_empty + 8 * slot, (q / P::kSlots & 1) ^ 1, a.limit, &dead))) break;
-            const uint32_t bar = slot_full + 8 * slot, at = smem_addr(buffers) + 2 * slot * P::kBlockBytes;
+            const uint32_t bar = slot_full + 8 * (q % (2 * P::kSlots)), at = smem_addr(buffers) + (6 + 2 * slot) * P::kBlockBytes;
             mbar_expect(bar, 2 * P::kBlockBytes);
             tma_load<1>(at, &a.in_map[0], n, m, 0, bar);
             tma_load<1>(at + P::kBlockBytes, &a.in_map[1], n, m, 0, bar);
@@ -561,15 +566,16 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       const bool saved = EPI == kUp && a.g[0].p;
       const bool elected = (warp - 2) % 8 == 0 && lane == 0;   // of the group
       const uint32_t empty0 = at_rank(sums_empty, 0);
-      // kUp: a group's three blocks; kDown: the slots, then a group's block of the hidden matrix
-      char* own = buffers + (EPI == kUp ? group * 3 * P::kBlockBytes : (2 * P::kSlots + group) * P::kBlockBytes);
-      int buf = 0, last_slot = -1;
+      char* own = buffers + group * 3 * P::kTurns * P::kBlockBytes;
+      int buf = 0;
       uint32_t phase = 0;
       unsigned q = 0;                                          // blocks of the CTA so far
+      int turn = 0;
       for (int i = first; i < items; i += step) {
         const Item it = item_of(a, i);
         const int m = it.tm * CG * P::kRows + row0, n0 = it.tn * P::kOutCols;
         ok = ok && mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead);
+        __syncwarp();
         tc_fence_after();
         const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16);
         const int blocks = m < a.m ? min(BLOCKS, (a.n - n0 + 31) / 32) : 0;
@@ -577,37 +583,35 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
         for (int s = (q + group) & 1; s < blocks; s += 2) {
           const int c = 32 * s + 16 * half;
           float v[16], u[16];
-          unsigned x[8];
+          unsigned x[3][8];                                    // of the matrices c, g[0], g[1]
           tmem_load(sums + c, v);
           if constexpr (EPI == kUp) {
             tmem_load(sums + BN / 2 + c, u);
             tmem_load_wait(v);
             tmem_load_wait(u);
-            if (elected) tma_store_read();
-            named_barrier(1 + group, 256);                     // the group's blocks may be written
             if (saved) {
-              pack_all(v, x, bf16);
-              put_block(own + P::kBlockBytes, row, 2 * half, x);
-              pack_all(u, x, bf16);
-              put_block(own + 2 * P::kBlockBytes, row, 2 * half, x);
+              pack_all(v, x[1], bf16);
+              pack_all(u, x[2], bf16);
             }
             act_values(v, a.act);
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] *= u[e];
-            pack_all(v, x, bf16);
-            put_block(own, row, 2 * half, x);
+            pack_all(v, x[0], bf16);
           } else {
             const unsigned at = q + s;
             const int slot = at % P::kSlots;
-            char* zblock = buffers + 2 * slot * P::kBlockBytes;
-            char* ublock = zblock + P::kBlockBytes;
-            ok = ok && mbar_wait(slot_full + 8 * slot, at / P::kSlots & 1, a.limit, &dead);
+            const char* block = buffers + (6 + 2 * slot) * P::kBlockBytes;
+            ok = ok && mbar_wait(slot_full + 8 * (at % (2 * P::kSlots)), at / (2 * P::kSlots) & 1, a.limit, &dead);
+            __syncwarp();
             float z[16], d[16];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              unpack8(z + 8 * e, *reinterpret_cast<const uint4*>(zblock + block_at(row, 2 * half + e)), bf16);
-              unpack8(u + 8 * e, *reinterpret_cast<const uint4*>(ublock + block_at(row, 2 * half + e)), bf16);
+              unpack8(z + 8 * e, *reinterpret_cast<const uint4*>(block + block_at(row, 2 * half + e)), bf16);
+              unpack8(u + 8 * e, *reinterpret_cast<const uint4*>(block + P::kBlockBytes + block_at(row, 2 * half + e)), bf16);
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(slot_empty + 8 * slot);
+            __syncwarp();
             act_slopes(z, d, a.act);
             tmem_load_wait(v);
 #pragma unroll
@@ -616,36 +620,39 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
               u[e] *= z[e];                                    // the hidden matrix
               z[e] *= v[e];
             }
-            if (elected) {
-              tma_store_read();                                // the group's last block has been read
-              if (last_slot >= 0) mbar_arrive(slot_empty + 8 * last_slot);
-              last_slot = slot;
-            }
+            pack_all(u, x[0], bf16);
+            pack_all(d, x[1], bf16);
+            pack_all(z, x[2], bf16);
+          }
+          // kUp writes the blocks of the turn before the last, which TMA had read before that turn's
+          // barrier; kDown waits here until it has read the last turn's
+          if (P::kTurns == 1) {
+            if (elected) tma_store_read();
             named_barrier(1 + group, 256);
-            pack_all(d, x, bf16);                              // in the places of what the lane has read
-            put_block(zblock, row, 2 * half, x);
-            pack_all(z, x, bf16);
-            put_block(ublock, row, 2 * half, x);
-            pack_all(u, x, bf16);
-            put_block(own, row, 2 * half, x);
+          }
+          char* blocks_out = own + (P::kTurns == 2 ? turn * 3 * P::kBlockBytes : 0);
+          put_block(blocks_out, row, 2 * half, x[0]);
+          if (EPI == kDown || saved) {
+            put_block(blocks_out + P::kBlockBytes, row, 2 * half, x[1]);
+            put_block(blocks_out + 2 * P::kBlockBytes, row, 2 * half, x[2]);
           }
           smem_to_tma();
+          if (P::kTurns == 2 && elected) tma_store_read();
           named_barrier(1 + group, 256);
           if (elected && ok) {
             const int n = n0 + 32 * s;
-            if constexpr (EPI == kUp) {
-              if (saved) {
-                tma_store(&a.g_map[0], n, m, 0, smem_addr(own + P::kBlockBytes));
-                tma_store(&a.g_map[1], n, m, 0, smem_addr(own + 2 * P::kBlockBytes));
-              }
-            } else {
-              const int slot = (q + s) % P::kSlots;
-              tma_store(&a.g_map[0], n, m, 0, smem_addr(buffers + 2 * slot * P::kBlockBytes));
-              tma_store(&a.g_map[0], n, m, 1, smem_addr(buffers + (2 * slot + 1) * P::kBlockBytes));
+            const uint32_t from = smem_addr(blocks_out);
+            tma_store(&a.c_map, n, m, 0, from);
+            if (EPI == kDown) {
+              tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
+              tma_store(&a.g_map[0], n, m, 1, from + 2 * P::kBlockBytes);
+            } else if (saved) {
+              tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
+              tma_store(&a.g_map[1], n, m, 0, from + 2 * P::kBlockBytes);
             }
-            tma_store(&a.c_map, n, m, 0, smem_addr(own));
             tma_store_commit();
           }
+          turn ^= 1;
         }
         // the sums have been read: the next tile but one may overwrite them
         q += blocks;
@@ -701,7 +708,7 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       Part then = part_of(next);
       if (i + step >= items) then.rows = 0;
       const int m = p.m, n = p.n, rows = p.rows, cols = p.cols;
-      if (!mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead)) break;
+      if (!__all_sync(~0u, mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead))) break;
       tc_fence_after();
       const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16) + share * P::kWarpCols;
       // the sums have been read: the next tile but one may overwrite them

@@ -83,8 +83,9 @@ __device__ __forceinline__ void smem_to_tma() { asm volatile("fence.proxy.async.
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// A barrier of `threads` threads of the CTA.
+// A barrier of `threads` threads of the CTA (whole warps).
 __device__ __forceinline__ void named_barrier(int id, int threads) {
+  __syncwarp();
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
