@@ -364,6 +364,11 @@ abcd_status room(abcd_ctx* ctx, const char* what, size_t need) {
 }  // namespace
 
 int norm_bwd_ctas(int num_sms);   // layernorm.cu
+abcd_status few_tokens(abcd_ctx* ctx, const abcd_matrix* x, const abcd_matrix* w_gate, const abcd_matrix* w_up,
+                       const abcd_matrix* w_down, int activation, const abcd_matrix* y, const abcd_matrix* gate,
+                       const abcd_matrix* up, void* hidden);   // fffew.cu
+// Tokens up to which the forward pass goes without tensor cores.
+constexpr long long kFewRows = 8;
 
 }  // namespace abcd
 
@@ -408,6 +413,11 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: unknown activation", what);
   if (m == 0) return ABCD_OK;
   Scratch need{nullptr};
+  if (m <= kFewRows) {
+    need.operand(m, f, ABCD_F32);                  // room for the hidden matrix in any type
+    const abcd_status st = room(ctx, what, need.at);
+    return st != ABCD_OK ? st : few_tokens(ctx, x, w_gate, w_up, w_down, activation, y, gate, up, ctx->net_base + kNetHeader);
+  }
   need.take(kPartBytes);
   if (needs_pack(x)) need.operand(m, d, t);
   if (needs_pack(w_gate)) need.operand(f, d, t);

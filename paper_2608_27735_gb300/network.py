@@ -13,112 +13,141 @@ from . import (ABCD_GELU, ABCD_RELU, ABCD_SILU, Context, _dtypes, _torch, abcd_m
 ACTIVATIONS = {"silu": ABCD_SILU, "gelu": ABCD_GELU, "relu": ABCD_RELU}
 
 
+_F32 = None
+_KINDS = {}
+_CALLS = {}
+
+
+def _call(name):
+    """The library's function; looked up once (these calls are short, and so is their host time)."""
+    global _F32
+    f = _CALLS.get(name)
+    if f is None:
+        _F32 = _torch().float32
+        _KINDS.update(_dtypes())
+        f = _CALLS[name] = getattr(lib(), name)
+    return f
+
+
 def _matrix(t, what):
-    """abcd_matrix of a 2-D CUDA tensor (None for None)."""
-    if t is None:
-        return None
+    """abcd_matrix of a 2-D CUDA tensor."""
     if not t.is_cuda or t.dim() != 2:
         raise ValueError(f"{what} must be a 2-D CUDA tensor")
     rows, cols = t.shape
     stride, unit = t.stride()
-    if cols > 1 and unit != 1:
+    if unit != 1 and cols > 1:
         raise ValueError(f"{what} must have consecutive columns")
-    dtype = _dtypes().get(t.dtype)
-    if dtype is None:
+    kind = _KINDS.get(t.dtype)
+    if kind is None:
         raise ValueError(f"{what} has type {t.dtype}; float32, float16 and bfloat16 are taken")
-    return abcd_matrix(t.data_ptr(), rows, cols, stride if rows > 1 else max(stride, cols), dtype)
+    if rows <= 1 and stride < cols:
+        stride = cols
+    return abcd_matrix(t.data_ptr(), rows, cols, stride, kind)
 
 
-def _ref(m):
-    return None if m is None else C.byref(m)
+def _optional(t, what):
+    return None if t is None else C.byref(_matrix(t, what))
 
 
-def _vector(t, n, what, dtypes):
+def _vector(t, n, what, dtype):
     """Address of a consecutive CUDA vector of n elements (None for None)."""
     if t is None:
         return None
-    if not t.is_cuda or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if not t.is_cuda or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must be a consecutive CUDA vector of {n} elements")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{what} has type {t.dtype}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{what} has type {t.dtype}, not {dtype}")
     return t.data_ptr()
 
 
 def _weight_type(x, *vectors):
     """The torch type of the given weight vectors (x's or float32, one for all)."""
-    torch = _torch()
-    kinds = {v.dtype for v in vectors if v is not None} or {x.dtype}
-    if len(kinds) > 1 or not kinds <= {x.dtype, torch.float32}:
-        raise ValueError("weights are all of the matrices' type or all float32")
-    return kinds.pop()
+    for v in vectors:
+        if v is not None:
+            if v.dtype is not x.dtype and v.dtype is not _F32:
+                raise ValueError("weights are of the matrices' type or float32")
+            return v.dtype
+    return x.dtype
 
 
 def _activation(name):
-    if name not in ACTIVATIONS:
+    act = ACTIVATIONS.get(name)
+    if act is None:
         raise ValueError(f"unknown activation {name!r}; one of {sorted(ACTIVATIONS)}")
-    return ACTIVATIONS[name]
+    return act
 
 
 def abcd_layer_norm(ctx: Context, x, weight, bias, eps, y, mean=None, rstd=None):
     """y = layer norm of x's rows; weight, bias: [cols] or None; mean, rstd: float32 [rows] that the
     backward pass needs, or None."""
+    call = _call("abcd_layer_norm")
     mx, my = _matrix(x, "x"), _matrix(y, "y")
     wt = _weight_type(x, weight, bias)
-    f32 = (_torch().float32,)
-    ctx.check(lib().abcd_layer_norm(
-        ctx.h, C.byref(mx), _vector(weight, mx.cols, "weight", (wt,)),
-        _vector(bias, mx.cols, "bias", (wt,)), _dtypes()[wt], float(eps), C.byref(my),
-        _vector(mean, mx.rows, "mean", f32), _vector(rstd, mx.rows, "rstd", f32)))
+    st = call(ctx.h, C.byref(mx), _vector(weight, mx.cols, "weight", wt),
+              _vector(bias, mx.cols, "bias", wt), _KINDS[wt], eps, C.byref(my),
+              _vector(mean, mx.rows, "mean", _F32), _vector(rstd, mx.rows, "rstd", _F32))
+    if st:
+        ctx.check(st)
 
 
 def abcd_layer_norm_backward(ctx: Context, dy, x, weight, mean, rstd, dx=None, dweight=None,
                              dbias=None, d_residual=None):
     """dx, dweight and dbias (each may be None) of abcd_layer_norm; d_residual is added to dx (which
     may be dy or d_residual).  Takes the network workspace (Context.reserve_network)."""
-    md, mx, mg = _matrix(dy, "dy"), _matrix(x, "x"), _matrix(dx, "dx")
-    mr = _matrix(d_residual, "d_residual")
+    call = _call("abcd_layer_norm_backward")
+    md, mx = _matrix(dy, "dy"), _matrix(x, "x")
     wt = _weight_type(x, weight, dweight, dbias)
-    f32 = (_torch().float32,)
-    ctx.check(lib().abcd_layer_norm_backward(
-        ctx.h, C.byref(md), C.byref(mx), _vector(weight, mx.cols, "weight", (wt,)), _dtypes()[wt],
-        _vector(mean, mx.rows, "mean", f32), _vector(rstd, mx.rows, "rstd", f32), _ref(mr), _ref(mg),
-        _vector(dweight, mx.cols, "dweight", (wt,)), _vector(dbias, mx.cols, "dbias", (wt,))))
+    st = call(ctx.h, C.byref(md), C.byref(mx), _vector(weight, mx.cols, "weight", wt), _KINDS[wt],
+              _vector(mean, mx.rows, "mean", _F32), _vector(rstd, mx.rows, "rstd", _F32),
+              _optional(d_residual, "d_residual"), _optional(dx, "dx"),
+              _vector(dweight, mx.cols, "dweight", wt), _vector(dbias, mx.cols, "dbias", wt))
+    if st:
+        ctx.check(st)
 
 
 def abcd_gated_ff(ctx: Context, x, w_gate, w_up, w_down, activation, y, gate=None, up=None):
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T; gate, up: [rows][ff] that the backward pass
     needs, or None; activation: "silu", "gelu" or "relu".  Takes the network workspace."""
-    ms = [_matrix(t, n) for t, n in ((x, "x"), (w_gate, "w_gate"), (w_up, "w_up"),
-                                     (w_down, "w_down"), (y, "y"), (gate, "gate"), (up, "up"))]
-    r = [_ref(m) for m in ms]
-    ctx.check(lib().abcd_gated_ff(ctx.h, *r[:4], _activation(activation), *r[4:]))
+    call = _call("abcd_gated_ff")
+    st = call(ctx.h, C.byref(_matrix(x, "x")), C.byref(_matrix(w_gate, "w_gate")),
+              C.byref(_matrix(w_up, "w_up")), C.byref(_matrix(w_down, "w_down")),
+              _activation(activation), C.byref(_matrix(y, "y")), _optional(gate, "gate"),
+              _optional(up, "up"))
+    if st:
+        ctx.check(st)
 
 
 def abcd_gated_ff_backward(ctx: Context, dy, x, w_gate, w_up, w_down, activation, gate, up,
                            dx=None, dw_gate=None, dw_up=None, dw_down=None):
     """dx and the weights' gradients (each may be None) of abcd_gated_ff, from what its forward call
     left in gate and up.  Takes the network workspace."""
-    ms = [_matrix(t, n) for t, n in ((dy, "dy"), (x, "x"), (w_gate, "w_gate"), (w_up, "w_up"),
-                                     (w_down, "w_down"), (gate, "gate"), (up, "up"), (dx, "dx"),
-                                     (dw_gate, "dw_gate"), (dw_up, "dw_up"),
-                                     (dw_down, "dw_down"))]
-    r = [_ref(m) for m in ms]
-    ctx.check(lib().abcd_gated_ff_backward(ctx.h, *r[:5], _activation(activation), *r[5:]))
+    call = _call("abcd_gated_ff_backward")
+    st = call(ctx.h, C.byref(_matrix(dy, "dy")), C.byref(_matrix(x, "x")),
+              C.byref(_matrix(w_gate, "w_gate")), C.byref(_matrix(w_up, "w_up")),
+              C.byref(_matrix(w_down, "w_down")), _activation(activation),
+              C.byref(_matrix(gate, "gate")), C.byref(_matrix(up, "up")), _optional(dx, "dx"),
+              _optional(dw_gate, "dw_gate"), _optional(dw_up, "dw_up"),
+              _optional(dw_down, "dw_down"))
+    if st:
+        ctx.check(st)
 
 
 def abcd_dropout(ctx: Context, x, p, seed, offset, y, residual=None):
     """y = residual + dropout(x) with the mask of (seed, offset); y may be x or residual.  The next
     call's offset is past this one's: offset + ceil(rows * cols / 8)."""
-    mx, my, mr = _matrix(x, "x"), _matrix(y, "y"), _matrix(residual, "residual")
-    ctx.check(lib().abcd_dropout(ctx.h, C.byref(mx), float(p), int(seed), int(offset), _ref(mr),
-                                 C.byref(my)))
+    call = _call("abcd_dropout")
+    st = call(ctx.h, C.byref(_matrix(x, "x")), p, seed, offset, _optional(residual, "residual"),
+              C.byref(_matrix(y, "y")))
+    if st:
+        ctx.check(st)
 
 
 def abcd_dropout_backward(ctx: Context, dy, p, seed, offset, dx):
     """dx = dropout's gradient of dy under the mask of (seed, offset); dx may be dy."""
-    md, mx = _matrix(dy, "dy"), _matrix(dx, "dx")
-    ctx.check(lib().abcd_dropout_backward(ctx.h, C.byref(md), float(p), int(seed), int(offset),
-                                          C.byref(mx)))
+    call = _call("abcd_dropout_backward")
+    st = call(ctx.h, C.byref(_matrix(dy, "dy")), p, seed, offset, C.byref(_matrix(dx, "dx")))
+    if st:
+        ctx.check(st)
 
 
 class FeedForwardBlock:
