@@ -1,13 +1,14 @@
 // The gated feed-forward layer's forward pass for up to kFewRows tokens: two kernels without tensor
 // cores.
 //
-// What bounds it: the weights' bytes, each read once, and the calls' latency; with so few rows a
-// tile of the tensor cores' products is nearly empty, and its staging costs more than the sums.
-// Layout: a warp per hidden unit (both of its weight rows) and then per output column (one row); a
-// lane takes every 32nd piece of 16 bytes of a row, multiplies it with the tokens' elements from
-// shared memory into 32-bit sums, and the warp adds its lanes'.  The second kernel may start while
-// the first runs: it reads its weight row, which the first does not write, before it waits for the
-// hidden matrix.  Weight rows that do not start on 16-byte boundaries go element by element.
+// What bounds it: the weights' bytes, each read once, and latency; with so few rows a tile of the
+// tensor cores' products is nearly empty, and its staging costs more than the sums.  Layout: one, two,
+// four or eight warps per hidden unit (both of its weight rows) and then per output column (one row),
+// so that a lane has about four pieces of 16 bytes of a row in flight; it multiplies them with the
+// tokens' (from L1) into 32-bit sums, and the lanes' and warps' are added in a fixed order.  The second
+// kernel may start while the first runs: it asks for its weight row, which the first does not write,
+// before it waits for the hidden matrix.  Weight rows that are not whole pieces on 16-byte boundaries
+// go element by element.
 #include <algorithm>
 
 #include "ffproduct.cuh"
@@ -22,113 +23,100 @@ struct FewArgs {
   void* saved[2];                     // gate and up, or NULL
   int rows, k, n, act;
   int x_vec;                          // whether x's rows start on 16-byte boundaries
+  int share;                          // warps of a unit
   long long sx, sw[2], sy, ssaved[2];
 };
 
-constexpr int kFewThreads = 256;
-constexpr int kFewChunk = 8192;       // elements of the tokens in shared memory at a time
+constexpr int kFewWarps = 8;          // of a CTA
+constexpr int kFlight = 4;            // a lane's pieces of a weight row that are in flight at once
 
-// ROWS: tokens that the registers take (1, 2, 4 or 8).
+// ROWS: tokens that the registers take (1, 2, 4 or 8); VEC: pieces of 16 bytes, else of one element.
 template <typename T, int MATS, int ROWS, bool VEC>
-__global__ void __launch_bounds__(kFewThreads) few_kernel(const __grid_constant__ FewArgs a) {
+__global__ void __launch_bounds__(32 * kFewWarps) few_kernel(const __grid_constant__ FewArgs a) {
   constexpr int V = VEC ? 16 / sizeof(T) : 1;
   using P = Pack<T, V>;
-  __shared__ alignas(16) T xs[ROWS][kFewChunk / ROWS];
-  constexpr int CHUNK = kFewChunk / ROWS;
-  constexpr int kFlight = MATS == 2 ? 4 : 16;          // a lane's pieces of a weight row in flight at once
-  const int lane = threadIdx.x & 31;
-  const int unit = blockIdx.x * (kFewThreads / 32) + threadIdx.x / 32;
+  __shared__ float parts[kFewWarps][MATS][ROWS];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int unit = blockIdx.x * (kFewWarps / a.share) + warp / a.share, part = warp % a.share;
   const bool in = unit < a.n;
+  const int first = (part * 32 + lane) * V, step = 32 * V * a.share;
   const T* w[MATS];
 #pragma unroll
   for (int q = 0; q < MATS; ++q) w[q] = (const T*)a.w[q] + (long long)(in ? unit : 0) * a.sw[q];
+  const int end = in ? a.k : 0;
   float s[MATS][ROWS] = {};
   P piece[MATS][kFlight];
-  auto fetch = [&](int k0, int end) {                  // the lane's pieces from element k0 on
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int f = 0; f < kFlight; ++f)
+#pragma unroll
+      for (int q = 0; q < MATS; ++q)
+        if (k0 + f * step < end) piece[q][f] = *reinterpret_cast<const P*>(w[q] + k0 + f * step);
+  };
+  // up: the grids before this one may have written the weights, and down's grid may start from here on;
+  // down: its weights are not the grid before's, and that grid's own wait has seen the ones before end
+  if (MATS == 2) pdl_prologue();
+  fetch(first);
+  if (MATS == 1) pdl_wait();
+  for (int k0 = first; k0 < end; k0 += kFlight * step) {
+    if (k0 > first) fetch(k0);
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
-      const int k = k0 + (f * 32 + lane) * V;
-      if (!in || k >= end) continue;
+      const int k = k0 + f * step;
+      if (k >= end) break;
 #pragma unroll
-      for (int q = 0; q < MATS; ++q) {
-        if (k + V <= end) {
-          piece[q][f] = *reinterpret_cast<const P*>(w[q] + k);
+      for (int r = 0; r < ROWS; ++r) {
+        P x;
+        const T* from = (const T*)a.x + (r < a.rows ? r : 0) * a.sx + k;
+        if (a.x_vec) {
+          x = *reinterpret_cast<const P*>(from);
         } else {
 #pragma unroll
-          for (int e = 0; e < V; ++e) piece[q][f].v[e] = k + e < end ? w[q][k + e] : from_f32<T>(0.f);
+          for (int e = 0; e < V; ++e) x.v[e] = from[e];
         }
-      }
-    }
-  };
-  // up: the grids before this one wrote the weights, perhaps, and down's grid may start from here on;
-  // down: its weights are not the grid before's, whose own wait has seen the ones before that end
-  if (MATS == 2) pdl_prologue();
-  fetch(0, min(a.k, CHUNK));
-  if (MATS == 1) pdl_wait();
-  for (int c0 = 0; c0 < a.k; c0 += CHUNK) {
-    const int end = min(a.k, c0 + CHUNK);
-    __syncthreads();
-    const int n = min(CHUNK, (end - c0 + 32 * V - 1) / (32 * V) * 32 * V);     // whole turns of the warps
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-#pragma unroll 4
-      for (int k = threadIdx.x * V; k < n; k += kFewThreads * V) {
-        const T* x = (const T*)a.x + r * a.sx + c0 + k;
-        const int left = r < a.rows ? end - c0 - k : 0;
-        P xv;
-        if (VEC && a.x_vec && left >= V) {
-          xv = *reinterpret_cast<const P*>(x);
-        } else {
+        for (int q = 0; q < MATS; ++q)
 #pragma unroll
-          for (int e = 0; e < V; ++e) xv.v[e] = e < left ? x[e] : from_f32<T>(0.f);
-        }
-        *reinterpret_cast<P*>(&xs[r][k]) = xv;
-      }
-    __syncthreads();
-    for (int k0 = c0; k0 < end; k0 += 32 * V * kFlight) {
-      if (k0 > 0) fetch(k0, end);
-#pragma unroll
-      for (int f = 0; f < kFlight; ++f) {
-        const int k = k0 + (f * 32 + lane) * V;
-        if (!in || k >= end) continue;
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-          const P xv = *reinterpret_cast<const P*>(&xs[r][k - c0]);
-#pragma unroll
-          for (int q = 0; q < MATS; ++q)
-#pragma unroll
-            for (int e = 0; e < V; ++e) s[q][r] += to_f32(piece[q][f].v[e]) * to_f32(xv.v[e]);
-        }
+          for (int e = 0; e < V; ++e) s[q][r] += to_f32(piece[q][f].v[e]) * to_f32(x.v[e]);
       }
     }
   }
 #pragma unroll
   for (int q = 0; q < MATS; ++q)
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+    for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
       for (int o = 16; o; o >>= 1) s[q][r] += __shfl_xor_sync(~0u, s[q][r], o);
-  // lane r writes token r
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    if (lane != r || r >= a.rows || !in) continue;
-    float v[1] = {s[0][r]};
-    if (MATS == 2) {
-      const float u = s[MATS - 1][r];
-      if (a.saved[0]) {
-        ((T*)a.saved[0])[r * a.ssaved[0] + unit] = from_f32<T>(v[0]);
-        ((T*)a.saved[1])[r * a.ssaved[1] + unit] = from_f32<T>(u);
-      }
-      act_values(v, a.act);
-      v[0] *= u;
+      if (lane == 0) parts[warp][q][r] = s[q][r];
     }
-    ((T*)a.y)[r * a.sy + unit] = from_f32<T>(v[0]);
+  if (a.share > 1) __syncthreads();
+  else __syncwarp();
+  // lane r of a unit's first warp finishes token r
+  if (part || lane >= a.rows || !in) return;
+  float v[1] = {0.f}, u = 0.f;
+  for (int p = 0; p < a.share; ++p) {
+    v[0] += parts[warp + p][0][lane];
+    if (MATS == 2) u += parts[warp + p][MATS - 1][lane];
   }
+  if (MATS == 2) {
+    if (a.saved[0]) {
+      ((T*)a.saved[0])[lane * a.ssaved[0] + unit] = from_f32<T>(v[0]);
+      ((T*)a.saved[1])[lane * a.ssaved[1] + unit] = from_f32<T>(u);
+    }
+    act_values(v, a.act);
+    v[0] *= u;
+  }
+  ((T*)a.y)[lane * a.sy + unit] = from_f32<T>(v[0]);
 }
 
 template <typename T, int MATS>
-cudaError_t launch_few(abcd_ctx* ctx, const FewArgs& a, bool vec) {
-  const dim3 grid((unsigned)((a.n + kFewThreads / 32 - 1) / (kFewThreads / 32))), block(kFewThreads);
+cudaError_t launch_few(abcd_ctx* ctx, FewArgs a, bool aligned) {
+  constexpr int V = 16 / sizeof(T);
+  const bool vec = aligned && a.k % V == 0;
+  a.share = 1;
+  while (a.share < kFewWarps && a.k > 32 * (vec ? V : 1) * kFlight * a.share) a.share *= 2;
+  const int units = kFewWarps / a.share;
+  const dim3 grid((unsigned)((a.n + units - 1) / units)), block(32 * kFewWarps);
   auto go = [&](auto* kernel) { return launch_pdl(kernel, grid, block, 0, ctx->stream, a); };
   if (vec) {
     if (a.rows == 1) return go(few_kernel<T, MATS, 1, true>);
