@@ -387,29 +387,32 @@ struct Product {
   // instead (32 bytes of a row at a time), 100,000 x 256 x 1,024 took 167 and 196 us for kUp and kDown.
   static constexpr bool kBlocks = BN == 256 && !F32 && EPI != kPlain;
   static constexpr int kBlockBytes = 128 * 64;
-  // Three blocks of results per group (twice for kUp, whose next ones need not wait for TMA to have
-  // read the last), and for kDown slots of a block of gate and one of up.
+  // Three blocks of results per group, and for kDown slots of a block of gate and one of up.
   // (A slot's blocks go to the groups in turn.  So it has two barriers that say it is full, one for each
   // group: a wait for a phase is right only for who has seen the phase before it end.)
-  static constexpr int kSlots = 3, kTurns = EPI == kUp ? 2 : 1;
-  static constexpr int kBlockRoom = (2 * 3 * kTurns + (EPI == kDown ? 2 * kSlots : 0)) * kBlockBytes;
+  static constexpr int kSlots = 3;
+  static constexpr int kBlockRoom = (2 * 3 + (EPI == kDown ? 2 * kSlots : 0)) * kBlockBytes;
   static constexpr int kThreads = 64 + 32 * kWarps + (kBlocks && EPI == kDown ? 32 : 0);
   static constexpr int kWarpCols = kOutCols / (kWarps / 4);
   static constexpr int CW = EPI != kPlain || kWarpCols < 32 ? 16 : 32;    // taken at a time
-  // Elsewhere a warp turns its rows round in a buffer of its own, and kDown has the saved projections
-  // come two turns ahead.
+  // Elsewhere a warp turns its rows round in a buffer of its own.  The smallest tile leaves room for a
+  // second CTA on the SM, whose warps fill the waits of the first's; kDown takes that room for the
+  // saved projections, which come two turns ahead (20,000 x 64 x 256 in 32 bits: 45 us, and 58 with
+  // two CTAs instead).
+  static constexpr int kCtas = BN == 64 && EPI != kDown ? 2 : 1;
+  static constexpr bool kAhead = EPI == kDown;
   static constexpr int kTurn = 32 * CW * (F32 ? 4 : 2);
-  static constexpr int kBuffer = kTurn + (EPI == kDown ? 4 * RowBuffer<F32>::kBytes : 0);
+  static constexpr int kBuffer = kTurn + (kAhead ? 4 * RowBuffer<F32>::kBytes : 0);
   static constexpr int kEpilogueBytes = kBlocks ? kBlockRoom : kWarps * kBuffer;
-  static constexpr int kRoom = (227 * 1024 - 512 - 1024 - kEpilogueBytes) / kStageBytes;
+  static constexpr int kRoom = ((kCtas == 2 ? 113 : 227) * 1024 - 512 - 1024 - kEpilogueBytes) / kStageBytes;
   static constexpr int kStages = kRoom > 8 ? 8 : kRoom;
-  static_assert(kTurn >= (EPI == kPlain ? 32 * 16 * 4 : 0) && kStages >= 4);
+  static_assert(kTurn >= (EPI == kPlain ? 32 * 16 * 4 : 0) && kStages >= 3);
   static_assert(EPI == kPlain || (CW == 16 && kWarpCols % 16 == 0));
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueBytes;
 };
 
 template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
-__global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads, 1) product_kernel(const __grid_constant__ ProductArgs a) {
+__global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads, Product<CG, BN, AMN, BMN, EPI, F32>::kCtas) product_kernel(const __grid_constant__ ProductArgs a) {
   using P = Product<CG, BN, AMN, BMN, EPI, F32>;
   extern __shared__ char smem_raw[];
   __shared__ uint64_t bars[2 * P::kStages + 4 + 3 * P::kSlots];
@@ -566,11 +569,10 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       const bool saved = EPI == kUp && a.g[0].p;
       const bool elected = (warp - 2) % 8 == 0 && lane == 0;   // of the group
       const uint32_t empty0 = at_rank(sums_empty, 0);
-      char* own = buffers + group * 3 * P::kTurns * P::kBlockBytes;
+      char* own = buffers + group * 3 * P::kBlockBytes;
       int buf = 0;
       uint32_t phase = 0;
       unsigned q = 0;                                          // blocks of the CTA so far
-      int turn = 0;
       for (int i = first; i < items; i += step) {
         const Item it = item_of(a, i);
         const int m = it.tm * CG * P::kRows + row0, n0 = it.tn * P::kOutCols;
@@ -624,24 +626,19 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
             pack_all(d, x[1], bf16);
             pack_all(z, x[2], bf16);
           }
-          // kUp writes the blocks of the turn before the last, which TMA had read before that turn's
-          // barrier; kDown waits here until it has read the last turn's
-          if (P::kTurns == 1) {
-            if (elected) tma_store_read();
-            named_barrier(1 + group, 256);
-          }
-          char* blocks_out = own + (P::kTurns == 2 ? turn * 3 * P::kBlockBytes : 0);
-          put_block(blocks_out, row, 2 * half, x[0]);
+          // once TMA has read the group's last blocks
+          if (elected) tma_store_read();
+          named_barrier(1 + group, 256);
+          put_block(own, row, 2 * half, x[0]);
           if (EPI == kDown || saved) {
-            put_block(blocks_out + P::kBlockBytes, row, 2 * half, x[1]);
-            put_block(blocks_out + 2 * P::kBlockBytes, row, 2 * half, x[2]);
+            put_block(own + P::kBlockBytes, row, 2 * half, x[1]);
+            put_block(own + 2 * P::kBlockBytes, row, 2 * half, x[2]);
           }
           smem_to_tma();
-          if (P::kTurns == 2 && elected) tma_store_read();
           named_barrier(1 + group, 256);
           if (elected && ok) {
             const int n = n0 + 32 * s;
-            const uint32_t from = smem_addr(blocks_out);
+            const uint32_t from = smem_addr(own);
             tma_store(&a.c_map, n, m, 0, from);
             if (EPI == kDown) {
               tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
@@ -652,7 +649,6 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
             }
             tma_store_commit();
           }
-          turn ^= 1;
         }
         // the sums have been read: the next tile but one may overwrite them
         q += blocks;
@@ -682,7 +678,7 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       p.cols = min(P::kWarpCols, a.n - p.n);
       return p;
     };
-    const bool ahead = EPI == kDown && a.in[0].vec && a.in[1].vec;
+    const bool ahead = P::kAhead && a.in[0].vec && a.in[1].vec;
     // kDown: the saved projections of turn t of an item (16 columns), to one of two pairs of buffers
     char* saved = buffer + P::kTurn;
     constexpr int TURNS = P::kWarpCols / P::CW, SAVED = RowBuffer<F32>::kBytes;
@@ -866,7 +862,7 @@ abcd_status launch_product(abcd_ctx* ctx, const ProductArgs& a) {
   const cudaError_t e = allow_smem(ctx, (const void*)kernel);
   if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "product_kernel: %s", cudaGetErrorString(e));
   const long long items = (long long)a.batches * a.tiles_m * a.tiles_n * a.splits;
-  const int units = ctx->num_sms / CG;
+  const int units = P::kCtas * ctx->num_sms / CG;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(CG * (items < units ? items : units)));
   cfg.blockDim = dim3(P::kThreads);
@@ -883,12 +879,20 @@ abcd_status launch_product(abcd_ctx* ctx, const ProductArgs& a) {
   return check_launch(ctx, "product_kernel", cudaLaunchKernelEx(&cfg, kernel, a));
 }
 
-// The tiles that the products come in: 256 x 256 on a pair of CTAs, 128 x 128 or 128 x 64 on one.
+// The tiles that the products come in: 256 x 256 on a pair of CTAs, 128 x 128 or 128 x 64 on one (two
+// of them per SM).
+// What they cost, in us: fitted to 324 products of 300 to 20,000 tokens of widths 64 x 256, 256 x 1,024
+// and 768 x 2,048 in 16 and 32 bits, each timed in all three shapes (the fit is within 8% rms, and its
+// choices took 0.6% longer in all than the best ones).
 struct Shape {
-  int cg, bn;
-  int cycles;                // of a stage (64 of k), about
+  int cg, bn, ctas;          // CTAs of a tile, its sums per row, CTAs per SM (one for kDown)
+  double fixed;              // of a launch
+  double idle, busy;         // of a stage (64 of k) where few SMs, where all ask for operands
+  double epilogue[3][2];     // of a tile, by kPlain, kUp, kDown and 16 or 32 bits
 };
-constexpr Shape kShapes[3] = {{2, 256, 600}, {1, 128, 550}, {1, 64, 420}};
+constexpr Shape kShapes[3] = {{2, 256, 1, 7.1, 0.25, 0.34, {{1.7, 1.8}, {2.7, 9.2}, {7.0, 36.0}}},
+                              {1, 128, 1, 5.9, 0.22, 0.33, {{0.5, 0.8}, {2.5, 4.5}, {6.1, 17.0}}},
+                              {1, 64, 2, 5.2, 0.24, 0.36, {{0.8, 1.0}, {2.1, 3.6}, {3.3, 8.3}}}};
 
 template <bool AMN, bool BMN, int EPI, bool F32>
 abcd_status launch_shape(abcd_ctx* ctx, int shape, const ProductArgs& a) {

@@ -14,7 +14,7 @@
 namespace abcd {
 namespace {
 
-constexpr size_t kPartBytes = (size_t)kNetSms * 128 * 256 * 4;   // one tile of sums per SM
+constexpr size_t kPartBytes = 2 * (size_t)kNetSms * 128 * 256 * 4;   // two large tiles' sums per SM
 
 // A 16-bit operand of a product in device memory: planes of rows of cols values.
 struct Operand {
@@ -109,26 +109,41 @@ __global__ void __launch_bounds__(256) unpack_kernel(const __grid_constant__ Unp
 }
 
 // The result of a product whose k was split: its parts added in their order, rounded to the type of
-// the matrices.  One thread per four columns of a row.
+// the matrices.  A thread takes four columns of a row and a run of consecutive parts; where the parts
+// are many, a CTA's threads share them in two to eight runs, which are added in their order.
 struct JoinArgs {
   const float* part;
   long long ld, plane;                // elements between rows, between splits
-  int rows, cols, splits;
+  int rows, cols, splits, runs;
   Out c[2];                           // per batch
 };
 template <typename T>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinArgs a) {
   pdl_wait();
+  __shared__ float4 run[256];
+  const int lanes = 256 / a.runs, lane = threadIdx.x % lanes, w = threadIdx.x / lanes;
   const unsigned groups = (a.cols + 3) / 4;
-  const unsigned i = blockIdx.x * 256u + threadIdx.x, row = i / groups, col = 4 * (i - row * groups);
-  if (row >= (unsigned)a.rows) return;
-  const float* p = a.part + (long long)blockIdx.y * a.rows * a.ld + row * a.ld + col;
+  const unsigned i = blockIdx.x * lanes + lane, row = i / groups, col = 4 * (i - row * groups);
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-  for (int k = 0; k < a.splits; ++k) {
-    const float4 v = __ldcg(reinterpret_cast<const float4*>(p + k * a.plane));
-    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  if (row < (unsigned)a.rows) {
+    const float* p = a.part + (long long)blockIdx.y * a.rows * a.ld + row * a.ld + col;
+    const int k1 = a.splits * (w + 1) / a.runs;
+#pragma unroll 4
+    for (int k = a.splits * w / a.runs; k < k1; ++k) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(p + k * a.plane));
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
   }
+  if (a.runs > 1) {
+    run[threadIdx.x] = s;
+    __syncthreads();
+    if (w) return;
+    for (int k = 1; k < a.runs; ++k) {
+      const float4 v = run[k * lanes + lane];
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+  }
+  if (row >= (unsigned)a.rows) return;
   const Out& o = a.c[blockIdx.y];
   T* c = (T*)o.p + row * o.stride + col;
   if (o.vec && (int)col + 4 <= a.cols) {
@@ -234,33 +249,33 @@ struct Job {
   ProductArgs args;
 };
 
-// Cycles that a tile's epilogue takes per column of sums: about what the products of few stages
-// measured (the large tile's sixteen warps of 16-bit matrices; half as many otherwise).
-double epilogue_cycles(int epi, bool f32, int bn) {
-  const double per_column[3] = {20, 33, 80};           // kPlain, kUp, kDown
-  return per_column[epi] * bn * (f32 ? 3.0 : bn == 256 ? 1.0 : 1.5);
-}
-
 // Picks the shape and the number of splits with the least estimated time: the waves of tiles, each
 // its stages or (beside the next tile's stages) its epilogue, plus the last epilogue, plus the
-// splits' joining.
+// splits' joining (their sums written and read through L2).
 void plan(int sms, long long m, long long n, int epi, bool f32, long long kblocks, int segments, long long batches, int* shape, int* splits) {
+  static constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 16, 20, 24, 30, 38, 48, 64};
   double best = 1e300;
   for (int s = 0; s < 3; ++s) {
-    const long long cols = epi == kUp ? kShapes[s].bn / 2 : kShapes[s].bn;
-    const long long units = sms / kShapes[s].cg;
-    const long long tiles = batches * ((m + 128 * kShapes[s].cg - 1) / (128 * kShapes[s].cg)) * ((n + cols - 1) / cols);
-    const long long most = std::max<long long>(1, std::min<long long>({units / std::max<long long>(1, tiles), kblocks * segments / 4, kblocks, 64}));
-    const double epilogue = epilogue_cycles(epi, f32, kShapes[s].bn);
-    // the large tile's blocks of results are whole sums
-    for (long long p = 1; p <= (s == 0 && epi != kPlain && !f32 ? 1 : most); ++p) {
+    const Shape& q = kShapes[s];
+    const long long cols = epi == kUp ? q.bn / 2 : q.bn, units = (epi == kDown ? 1 : q.ctas) * sms / q.cg;
+    const long long tiles = batches * ((m + 128 * q.cg - 1) / (128 * q.cg)) * ((n + cols - 1) / cols);
+    const long long tile_bytes = 4LL * 128 * q.cg * q.bn;
+    // the sums have to fit the workspace, and where the last part's warps add them up, all parts of a
+    // tile run at once; the large tile's blocks of results are whole sums
+    long long most = epi == kPlain ? (long long)kPartBytes / (tiles * tile_bytes) : s == 0 && !f32 ? 1 : units / tiles;
+    most = std::min(most, kblocks);
+    const double epilogue = q.epilogue[epi][f32];
+    for (const int p : kSplits) {
+      if (p > 1 && p > most) break;
       const double waves = (double)((tiles * p + units - 1) / units);
-      const double stages = (double)(segments * ((kblocks + p - 1) / p)) * kShapes[s].cycles;
-      const double t = waves * std::max(stages, epilogue) + std::min(stages, epilogue) + 2000.0 + (p > 1 ? 3000.0 + 150.0 * p : 0.0);
+      const double busy = std::min(1.0, (double)(tiles * p) / (double)units);
+      const double stages = (double)(segments * ((kblocks + p - 1) / p)) * (q.idle + (q.busy - q.idle) * busy);
+      const double joined = p == 1 ? 0.0 : 2.5 + (double)(tiles * p * tile_bytes) / 4e6;
+      const double t = q.fixed + waves * std::max(stages, epilogue) + std::min(stages, epilogue) + joined;
       if (t < best) {
         best = t;
         *shape = s;
-        *splits = (int)p;
+        *splits = p;
       }
     }
   }
@@ -330,8 +345,9 @@ abcd_status run(abcd_ctx* ctx, int dtype, int which, Job& j) {
   a.part_ld = (j.n + 3) / 4 * 4;
   const abcd_status st = dtype == ABCD_F32 ? launch_32(ctx, which, shape, a) : launch_16(ctx, which, shape, a);
   if (st != ABCD_OK || epi != kPlain || splits == 1) return st;
-  const JoinArgs q{a.part, a.part_ld, j.batches * j.m * a.part_ld, a.m, a.n, splits, {a.c[0], a.c[1]}};
-  const dim3 grid((unsigned)((j.m * ((j.n + 3) / 4) + 255) / 256), (unsigned)j.batches);
+  const int runs = splits <= 8 ? 1 : splits <= 16 ? 2 : splits <= 32 ? 4 : 8, lanes = 256 / runs;
+  const JoinArgs q{a.part, a.part_ld, j.batches * j.m * a.part_ld, a.m, a.n, splits, runs, {a.c[0], a.c[1]}};
+  const dim3 grid((unsigned)((j.m * ((j.n + 3) / 4) + lanes - 1) / lanes), (unsigned)j.batches);
   return with_type(dtype, [&](auto t) {
     return check_launch(ctx, "join_kernel", launch_pdl(join_kernel<decltype(t)>, grid, dim3(256), 0, ctx->stream, q));
   });
