@@ -1,7 +1,9 @@
 // Dropout from a counter-based generator: y = residual + (kept ? x s : 0), s = 65536 / (65536 - t).
 // Element e (row * cols + column) is kept where the 16-bit number e % 8 of block offset + e / 8 of
 // Philox4x32-10 is at least t, so that the mask is never stored: the backward pass is the same
-// kernel on dy.  One thread takes a block of eight elements.
+// kernel on dy.
+// Bound by HBM, and not far from it by the generator's arithmetic (about 70 instructions a block of
+// eight elements).
 #include <algorithm>
 #include <cmath>
 
@@ -19,22 +21,20 @@ struct DropArgs {
   long long cols;
   long long sx, sr, sy;               // row strides
   unsigned long long offset;
-  unsigned key0, key1;
+  unsigned key[10][2];                // of the generator's rounds
   unsigned t;
   float scale;
 };
 
-// Ten rounds of Philox4x32 (Salmon et al., 2011): two 32 x 32 bit products a round, the key moved on
-// by the paper's two Weyl constants.
-__device__ __forceinline__ uint4 philox(unsigned long long block, unsigned k0, unsigned k1) {
+// Ten rounds of Philox4x32 (Salmon et al., 2011): two 32 x 32 bit products a round; the rounds' keys
+// come with the arguments.
+__device__ __forceinline__ uint4 philox(unsigned long long block, const DropArgs& a) {
   uint4 c = make_uint4((unsigned)block, (unsigned)(block >> 32), 0u, 0u);
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const unsigned long long p0 = (unsigned long long)c.x * 0xD2511F53u;
     const unsigned long long p1 = (unsigned long long)c.z * 0xCD9E8D57u;
-    c = make_uint4((unsigned)(p1 >> 32) ^ c.y ^ k0, (unsigned)p1, (unsigned)(p0 >> 32) ^ c.w ^ k1, (unsigned)p0);
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
+    c = make_uint4((unsigned)(p1 >> 32) ^ c.y ^ a.key[r][0], (unsigned)p1, (unsigned)(p0 >> 32) ^ c.w ^ a.key[r][1], (unsigned)p0);
   }
   return c;
 }
@@ -50,43 +50,52 @@ __device__ __forceinline__ void drop8(float (&v)[8], const uint4& w, unsigned t,
 }
 
 // Rows of a multiple of eight elements on 16-byte boundaries (or matrices without gaps, taken as one
-// row): a block is one 16-byte access of 16-bit elements, two of 32 bits.
-template <typename T>
+// row): a block is one 16-byte access of 16-bit elements, two of 32 bits.  The next block's are on
+// their way while the generator works on this one's.
+template <typename T, bool RES>
 __global__ void __launch_bounds__(256) dropout_vec_kernel(const __grid_constant__ DropArgs a) {
   pdl_wait();
   using P = Pack<T, 16 / sizeof(T)>;
-  constexpr int N = 8 / (16 / sizeof(T));
+  constexpr int N = sizeof(T) / 2;                      // accesses of a block
   const unsigned per_row = (unsigned)(a.cols / 8);
   const long long groups = a.n / 8, step = gridDim.x * 256LL;
-  for (long long g = blockIdx.x * 256LL + threadIdx.x; g < groups; g += step) {
+  struct Block { P x[N], res[N]; long long y; } now, next;
+  auto load = [&](long long g, Block& to) {
+    if (g >= groups) return;
     long long row = 0, col = 8 * g;
     if (a.rows > 1) {
       row = groups < (1LL << 32) ? (unsigned)g / per_row : g / per_row;
       col = 8 * (g - row * per_row);
     }
-    P px[N], pr[N];
+    to.y = row * a.sy + col;
 #pragma unroll
     for (int q = 0; q < N; ++q) {
-      px[q] = reinterpret_cast<const P*>((const T*)a.x + row * a.sx + col)[q];
-      if (a.res) pr[q] = reinterpret_cast<const P*>((const T*)a.res + row * a.sr + col)[q];
+      to.x[q] = reinterpret_cast<const P*>((const T*)a.x + row * a.sx + col)[q];
+      if (RES) to.res[q] = reinterpret_cast<const P*>((const T*)a.res + row * a.sr + col)[q];
     }
-    const uint4 w = philox(a.offset + (unsigned long long)g, a.key0, a.key1);
+  };
+  long long g = blockIdx.x * 256LL + threadIdx.x;
+  load(g, now);
+  for (; g < groups; g += step) {
+    load(g + step, next);
+    const uint4 w = philox(a.offset + (unsigned long long)g, a);
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = to_f32(px[j * N / 8].v[j % (8 / N)]);
+    for (int j = 0; j < 8; ++j) v[j] = to_f32(now.x[j * N / 8].v[j % (8 / N)]);
     drop8(v, w, a.t, a.scale);
-    if (a.res) {
+    if (RES) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += to_f32(pr[j * N / 8].v[j % (8 / N)]);
+      for (int j = 0; j < 8; ++j) v[j] += to_f32(now.res[j * N / 8].v[j % (8 / N)]);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) px[j * N / 8].v[j % (8 / N)] = from_f32<T>(v[j]);
+    for (int j = 0; j < 8; ++j) now.x[j * N / 8].v[j % (8 / N)] = from_f32<T>(v[j]);
 #pragma unroll
-    for (int q = 0; q < N; ++q) reinterpret_cast<P*>((T*)a.y + row * a.sy + col)[q] = px[q];
+    for (int q = 0; q < N; ++q) reinterpret_cast<P*>((T*)a.y + now.y)[q] = now.x[q];
+    now = next;
   }
   // matrices without gaps: the last, short block
   if (a.n & 7 && blockIdx.x == 0 && threadIdx.x == 0) {
-    const uint4 w = philox(a.offset + (unsigned long long)groups, a.key0, a.key1);
+    const uint4 w = philox(a.offset + (unsigned long long)groups, a);
     const int left = (int)(a.n & 7);
     float v[8] = {};
     for (int j = 0; j < left; ++j) v[j] = to_f32(((const T*)a.x)[8 * groups + j]);
@@ -98,39 +107,53 @@ __global__ void __launch_bounds__(256) dropout_vec_kernel(const __grid_constant_
   }
 }
 
-// Rows of any length and stride: element by element.
-template <typename T>
+// Rows of any other length: pieces of V consecutive elements of a row (16 bytes where the rows start
+// on such boundaries, else one element), which lie in one block or two of the generator.
+template <typename T, int V>
 __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropArgs a) {
   pdl_wait();
-  const long long groups = (a.n + 7) / 8, step = gridDim.x * 256LL;
-  for (long long g = blockIdx.x * 256LL + threadIdx.x; g < groups; g += step) {
-    const uint4 w = philox(a.offset + (unsigned long long)g, a.key0, a.key1);
-    const long long row0 = a.n < (1LL << 32) ? (unsigned)(8 * g) / (unsigned)a.cols : 8 * g / a.cols;
-    const int col0 = (int)(8 * g - row0 * a.cols), left = (int)min(8LL, a.n - 8 * g);
-    float v[8];
-    long long row = row0;
-    int col = col0;
+  using P = Pack<T, V>;
+  const unsigned per_row = (unsigned)((a.cols + V - 1) / V);
+  const long long pieces = per_row * a.rows, step = gridDim.x * 256LL;
+  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < pieces; i += step) {
+    const long long row = pieces < (1LL << 32) ? (unsigned)i / per_row : i / per_row;
+    const int col = V * (int)(i - row * per_row), left = (int)min((long long)V, a.cols - col);
+    const T* x = (const T*)a.x + row * a.sx + col;
+    const T* res = (const T*)a.res + row * a.sr + col;
+    T* y = (T*)a.y + row * a.sy + col;
+    P px, pr;
+    if (V > 1 && left == V) {
+      px = *reinterpret_cast<const P*>(x);
+      if (a.res) pr = *reinterpret_cast<const P*>(res);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[j] = j < left ? to_f32(((const T*)a.x)[row * a.sx + col]) : 0.f;
-      if (++col == (int)a.cols) { col = 0; ++row; }
-    }
-    drop8(v, w, a.t, a.scale);
-    if (a.res) {
-      row = row0;
-      col = col0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (j < left) v[j] += to_f32(((const T*)a.res)[row * a.sr + col]);
-        if (++col == (int)a.cols) { col = 0; ++row; }
+      for (int j = 0; j < V; ++j) {
+        px.v[j] = j < left ? x[j] : from_f32<T>(0.f);
+        if (a.res) pr.v[j] = j < left ? res[j] : from_f32<T>(0.f);
       }
     }
-    row = row0;
-    col = col0;
+    const unsigned long long e = (unsigned long long)(row * a.cols + col), block = a.offset + e / 8;
+    const int at = (int)(e % 8);
+    const uint4 w0 = philox(block, a);
+    const uint4 w1 = at + left > 8 ? philox(block + 1, a) : w0;
+    // the piece's numbers from bit 16 at of both blocks' 256 bits on
+    const unsigned word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (j < left) ((T*)a.y)[row * a.sy + col] = from_f32<T>(v[j]);
-      if (++col == (int)a.cols) { col = 0; ++row; }
+    for (int j = 0; j < V; ++j) {
+      unsigned pick = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) pick = (at + j) / 2 == k ? word[k] : pick;
+      const unsigned u = (at + j) & 1 ? pick >> 16 : pick & 0xffffu;
+      float v = u >= a.t ? to_f32(px.v[j]) * a.scale : 0.f;
+      if (a.res) v += to_f32(pr.v[j]);
+      px.v[j] = from_f32<T>(v);
+    }
+    if (V > 1 && left == V) {
+      *reinterpret_cast<P*>(y) = px;
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j < left) y[j] = px.v[j];
     }
   }
 }
@@ -156,8 +179,10 @@ abcd_status drop(abcd_ctx* ctx, const char* what, const abcd_matrix* x, double p
   a.sr = res ? res->stride : 0;
   a.sy = y->stride;
   a.offset = offset;
-  a.key0 = (unsigned)seed;
-  a.key1 = (unsigned)(seed >> 32);
+  for (int r = 0; r < 10; ++r) {        // moved on by the paper's two Weyl constants
+    a.key[r][0] = (unsigned)seed + (unsigned)r * 0x9E3779B9u;
+    a.key[r][1] = (unsigned)(seed >> 32) + (unsigned)r * 0xBB67AE85u;
+  }
   a.t = (unsigned)std::floor(p * 65536.0 + 0.5);
   a.scale = a.t < 65536u ? (float)(65536.0 / (double)(65536u - a.t)) : 0.f;
   // by vectors go rows in eights on 16-byte boundaries; without gaps the rows are one
@@ -170,12 +195,14 @@ abcd_status drop(abcd_ctx* ctx, const char* what, const abcd_matrix* x, double p
     a.rows = 1;
     a.cols = a.n;
   }
-  const long long blocks = std::min<long long>((a.n + 2047) / 2048, 8LL * ctx->num_sms);
+  const bool pieces = rows_aligned(x, 16) && rows_aligned(y, 16) && (!res || rows_aligned(res, 16));
   return with_type(x->dtype, [&](auto v) {
     using T = decltype(v);
-    return check_launch(ctx, "dropout_kernel",
-                        launch_pdl(vec ? dropout_vec_kernel<T> : dropout_kernel<T>, dim3((unsigned)blocks),
-                                   dim3(256), 0, ctx->stream, a));
+    constexpr int V = 16 / sizeof(T);
+    const long long work = vec ? (a.n + 7) / 8 : (pieces ? (a.cols + V - 1) / V : a.cols) * a.rows;
+    const long long blocks = std::min<long long>((work + 255) / 256, 8LL * ctx->num_sms);
+    auto* kernel = vec ? (res ? dropout_vec_kernel<T, true> : dropout_vec_kernel<T, false>) : pieces ? dropout_kernel<T, V> : dropout_kernel<T, 1>;
+    return check_launch(ctx, "dropout_kernel", launch_pdl(kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, a));
   });
 }
 

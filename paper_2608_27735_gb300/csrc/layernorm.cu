@@ -136,48 +136,71 @@ __device__ __forceinline__ void copy16(void* dst, const void* src, int bytes) {
 // The rows that a group of TPR threads takes one after another, their next ones on the way: each
 // thread copies its own bytes of the matrices to its own 16-byte slots [depth][matrix][NV][thread].
 template <typename T, typename R> struct RowRing {
-  char* slots;
-  const T* src[2];
-  long long stride[2];
-  long long rows, first, step, turns;
-  int cols, lane;
-
   static constexpr int kDepth = R::kDepth;
-  __device__ __forceinline__ char* slot(int d, int mat, int j) const {
-    return slots + ((((size_t)d * R::kMats + mat) * R::NV + j) * R::kThreads + threadIdx.x) * 16;
+  char* slots;                        // the thread's first slot
+  const T* src[R::kMats];             // where the thread's first vector of the next row to fetch lies
+  long long jump[R::kMats];           // elements from one of the group's rows to its next
+  int rows, turns;                    // the group's rows; turns of the CTA, alike in all its groups
+  int left;                           // elements of a row from the thread's first vector on
+
+  __device__ __forceinline__ RowRing(char* smem, const NormArgs& a) {
+    const int lane = threadIdx.x % R::TPR;
+    const long long first = (long long)blockIdx.x * R::kGroups + threadIdx.x / R::TPR, step = (long long)gridDim.x * R::kGroups;
+    slots = smem + threadIdx.x * 16;
+    left = a.cols - lane * R::V;
+    rows = first < a.rows ? (int)((a.rows - first + step - 1) / step) : 0;
+    turns = (int)((a.rows - (long long)blockIdx.x * R::kGroups + step - 1) / step);
+    const T* base[2] = {(const T*)a.x, (const T*)a.dy};
+    const long long stride[2] = {a.sx, a.sdy};
+#pragma unroll
+    for (int q = 0; q < R::kMats; ++q) {
+      src[q] = base[q] + first * stride[q] + lane * R::V;
+      jump[q] = step * stride[q];
+    }
   }
-  __device__ __forceinline__ void fetch(long long t) const {
+  __device__ __forceinline__ char* slot(int t, int mat, int j) const {
+    return slots + ((t % kDepth * R::kMats + mat) * R::NV + j) * R::kThreads * 16;
+  }
+  __device__ __forceinline__ void fetch(int t) {
     if constexpr (R::V > 1) {
-      if (t < turns) {
-        const long long r = first + t * step;
-        const int d = (int)(t % kDepth);
+      if (t < rows) {
 #pragma unroll
         for (int j = 0; j < R::NV; ++j) {
-          const int c = (j * R::TPR + lane) * R::V, bytes = r < rows ? (cols - c) * (int)sizeof(T) : 0;
-          if (bytes > 0) {
+          const int n = left - j * R::TPR * R::V;
+          if (n > 0) {
 #pragma unroll
-            for (int q = 0; q < R::kMats; ++q) copy16(slot(d, q, j), src[q] + r * stride[q] + c, bytes);
+            for (int q = 0; q < R::kMats; ++q) copy16(slot(t, q, j), src[q] + j * R::TPR * R::V, n < R::V ? n * (int)sizeof(T) : 16);
           }
         }
+#pragma unroll
+        for (int q = 0; q < R::kMats; ++q) src[q] += jump[q];
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
   }
-  __device__ __forceinline__ void start() const {
+  __device__ __forceinline__ void start() {
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) fetch(d);
   }
   // Asks for the row kDepth - 1 turns on and waits for the one of turn t.
-  __device__ __forceinline__ void turn(long long t) const {
+  __device__ __forceinline__ void turn(int t) {
     fetch(t + kDepth - 1);
     if constexpr (R::V > 1) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
   }
   // Vector j of the turn's row of a matrix; zeros past its end.
-  __device__ __forceinline__ void get(float (&v)[R::V], long long t, int mat, int j, int left) const {
+  __device__ __forceinline__ void get(float (&v)[R::V], int t, int mat, int j) const {
+    const int n = t < rows ? left - j * R::TPR * R::V : 0;
     if constexpr (R::V > 1) {
-      load_vec<T, R::V>(v, (const T*)slot((int)(t % kDepth), mat, j), left > 0 ? R::V : 0);
+      load_vec<T, R::V>(v, (const T*)slot(t, mat, j), n > 0 ? R::V : 0);
     } else {
-      load_vec<T, R::V>(v, src[mat] + (first + t * step) * stride[mat] + j * R::TPR + lane, left);
+      load_vec<T, R::V>(v, src[mat] + j * R::TPR * R::V, n);
+    }
+  }
+  // After a turn (rows that are not copied ahead are read where src stands).
+  __device__ __forceinline__ void next() {
+    if constexpr (R::V == 1) {
+#pragma unroll
+      for (int q = 0; q < R::kMats; ++q) src[q] += jump[q];
     }
   }
 };
@@ -189,10 +212,7 @@ __global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_cons
   __shared__ float2 red[2][32];
   pdl_wait();
   const int lane = threadIdx.x % TPR;
-  RowRing<T, R> ring{smem, {(const T*)a.x, nullptr}, {a.sx, 0}, a.rows,
-                        (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR, (long long)gridDim.x * R::kGroups,
-                        0, a.cols, lane};
-  ring.turns = (a.rows - (long long)blockIdx.x * R::kGroups + ring.step - 1) / ring.step;   // alike in the CTA
+  RowRing<T, R> ring(smem, a);
   ring.start();
   float w[NV][V], b[NV][V];
 #pragma unroll
@@ -202,22 +222,24 @@ __global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_cons
     load_weight<T, V>(b[j], a.b, a.wide_w, c, a.cols - c, 0.f);
   }
   const float inv = 1.f / (float)a.cols;
-  for (long long t = 0; t < ring.turns; ++t) {
+  const long long step = (long long)gridDim.x * R::kGroups;
+  long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR;
+  T* y = (T*)a.y + r * a.sy + lane * V;
+  for (int t = 0; t < ring.turns; ++t, r += step, y += step * a.sy) {
     ring.turn(t);
-    const long long r = ring.first + t * ring.step;
-    const bool in = r < a.rows;
     float v[NV][V], s = 0.f, q = 0.f, unused = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      ring.get(v[j], t, 0, j, in ? a.cols - (j * TPR + lane) * V : 0);
+      ring.get(v[j], t, 0, j);
 #pragma unroll
       for (int i = 0; i < V; ++i) s += v[j][i];
     }
+    ring.next();
     row_sum2<TPR>(s, unused, red, 0);
     const float mean = s * inv;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int left = a.cols - (j * TPR + lane) * V;
+      const int left = ring.left - j * TPR * V;
       if (left < V) {                                  // past the row's end nothing deviates
 #pragma unroll
         for (int i = 0; i < V; ++i) v[j][i] = i < left ? v[j][i] : mean;
@@ -230,15 +252,14 @@ __global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_cons
     }
     row_sum2<TPR>(q, unused, red, 1);
     const float rstd = rsqrtf(q * inv + a.eps);
-    if (!in) continue;
-    T* y = (T*)a.y + r * a.sy;
+    if (t >= ring.rows) continue;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + lane) * V, left = a.cols - c;
+      const int left = ring.left - j * TPR * V;
       if (left <= 0) break;
 #pragma unroll
       for (int i = 0; i < V; ++i) v[j][i] = v[j][i] * rstd * w[j][i] + b[j][i];
-      store_vec<T, V>(y + c, v[j], left);
+      store_vec<T, V>(y + j * TPR * V, v[j], left);
     }
     if (a.mean && lane == 0) {
       a.mean[r] = mean;
@@ -254,10 +275,7 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
   __shared__ float2 red[2][32];
   pdl_wait();
   const int lane = threadIdx.x % TPR;
-  RowRing<T, R> ring{smem, {(const T*)a.x, (const T*)a.dy}, {a.sx, a.sdy}, a.rows,
-                        (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR, (long long)gridDim.x * R::kGroups,
-                        0, a.cols, lane};
-  ring.turns = (a.rows - (long long)blockIdx.x * R::kGroups + ring.step - 1) / ring.step;
+  RowRing<T, R> ring(smem, a);
   ring.start();
   float w[NV][V], dw[NV][V] = {}, db[NV][V] = {};
 #pragma unroll
@@ -266,21 +284,30 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
     load_weight<T, V>(w[j], a.w, a.wide_w, c, a.cols - c, 1.f);
   }
   const float inv = 1.f / (float)a.cols;
-  for (long long t = 0; t < ring.turns; ++t) {
+  const long long step = (long long)gridDim.x * R::kGroups;
+  long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR;
+  T* dx = (T*)a.y + r * a.sy + lane * V;
+  const T* res = (const T*)a.res + r * a.sres + lane * V;
+  // mean and rstd of the rows come two turns ahead too
+  auto stat_of = [&](int t, long long row) {
+    return t < ring.rows ? make_float2(__ldg(a.mean + row), __ldg(a.rstd + row)) : make_float2(0.f, 0.f);
+  };
+  float2 stat[2] = {stat_of(0, r), stat_of(1, r + step)};
+  for (int t = 0; t < ring.turns; ++t, r += step, dx += step * a.sy, res += step * a.sres) {
     ring.turn(t);
-    const long long r = ring.first + t * ring.step;
-    const bool in = r < a.rows;
-    const float mean = in ? a.mean[r] : 0.f, rstd = in ? a.rstd[r] : 0.f;
+    const bool in = t < ring.rows;
+    const float rstd = stat[0].y, shift = -stat[0].x * rstd;
+    stat[0] = stat[1];
+    stat[1] = stat_of(t + 2, r + 2 * step);
     // past the row's end dy is zero, and so is what xh meets there
     float xh[NV][V], g[NV][V], s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int left = in ? a.cols - (j * TPR + lane) * V : 0;
-      ring.get(xh[j], t, 0, j, left);
-      ring.get(g[j], t, 1, j, left);
+      ring.get(xh[j], t, 0, j);
+      ring.get(g[j], t, 1, j);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        xh[j][i] = (xh[j][i] - mean) * rstd;
+        xh[j][i] = xh[j][i] * rstd + shift;
         dw[j][i] += g[j][i] * xh[j][i];
         db[j][i] += g[j][i];
         g[j][i] *= w[j][i];
@@ -288,25 +315,25 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
         s2 += g[j][i] * xh[j][i];
       }
     }
-    row_sum2<TPR>(s1, s2, red, (int)(t & 1));
-    s1 *= inv * rstd;
-    s2 *= inv * rstd;
+    ring.next();
+    row_sum2<TPR>(s1, s2, red, t & 1);
+    s1 *= -inv * rstd;
+    s2 *= -inv * rstd;
     if (a.y && in) {
-      T* dx = (T*)a.y + r * a.sy;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int c = (j * TPR + lane) * V, left = a.cols - c;
+        const int left = ring.left - j * TPR * V;
         if (left <= 0) break;
         float v[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = rstd * g[j][i] - s1 - xh[j][i] * s2;
+        for (int i = 0; i < V; ++i) v[i] = xh[j][i] * s2 + (rstd * g[j][i] + s1);
         if (a.res) {
-          float res[V];
-          load_vec<T, V>(res, (const T*)a.res + r * a.sres + c, left);
+          float add[V];
+          load_vec<T, V>(add, res + j * TPR * V, left);
 #pragma unroll
-          for (int i = 0; i < V; ++i) v[i] += res[i];
+          for (int i = 0; i < V; ++i) v[i] += add[i];
         }
-        store_vec<T, V>(dx + c, v, left);
+        store_vec<T, V>(dx + j * TPR * V, v, left);
       }
     }
   }
@@ -427,7 +454,7 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* part, int c
   float s = 0.f;
   if (c < 2 * cols) {
     const int k0 = ctas * k / 32, k1 = ctas * (k + 1) / 32;
-#pragma unroll 4
+#pragma unroll 10
     for (int q = k0; q < k1; ++q) s += part[(long long)q * 2 * cols + c];
   }
   run[k][lane] = s;
