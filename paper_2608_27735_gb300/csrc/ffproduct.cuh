@@ -18,6 +18,8 @@
 // not yet the result, by the warp that comes last.
 #pragma once
 
+#include <type_traits>
+
 #include "network.cuh"
 #include "tensor_core.cuh"
 
@@ -37,26 +39,37 @@ struct Out {
   int vec;                            // rows start on 16-byte boundaries
 };
 
-struct ProductArgs {
+// One of up to three products of a launch (kPlain; kUp and kDown have one).
+struct ProductJob {
   CUtensorMap a, b[2];
-  // the large tile of 16-bit matrices: kUp stores c, gate, up (g); kDown loads gate, up (in) and stores
-  // c, dG and dU (planes 0 and 1 of g[0])
-  CUtensorMap c_map, g_map[2], in_map[2];
+  // the operand lies with its own dimension contiguous instead of k: neither (kUp), B (kDown) or, of
+  // kPlain, none, B or both
+  int a_rows_last, b_rows_last;
   int m, n;                           // rows of A and B (kUp: of each B)
   int kblocks;                        // stages per segment
   int segments;
   unsigned char az[kMaxSegments], bsel[kMaxSegments], bz[kMaxSegments];
   int batch_az;                       // added to az for the second batch
   int tiles_m, tiles_n, batches, splits;
-  int dtype;
-  int act;
-  Out c[2];                           // kPlain: per batch; kUp, kDown: c[0] the hidden matrix
-  Out g[2];                           // kUp: gate and up (p NULL: not wanted); kDown: dG and dU
-  Out in[2];                          // kDown: the saved gate and up
-  // sums of the splits: kPlain [split][batch][m][part_ld], which a kernel of its own adds up;
-  // otherwise per warp of a tile, which the last warp to come adds up
+  int first;                          // the job's first item
+  Out c[2];                           // the result per batch (kUp, kDown: c[0] the hidden matrix)
+  // sums of the splits: kPlain [split][batch][m][part_ld], which a kernel of its own adds up; otherwise
+  // per warp of a tile, which the last warp to come adds up
   float* part;
   long long part_ld;
+};
+constexpr int kMaxJobs = 3;
+
+struct ProductArgs {
+  ProductJob job[kMaxJobs];
+  int jobs, items;
+  // the large tile of 16-bit matrices: kUp stores c, gate, up (g); kDown loads gate, up (in) and stores
+  // c, dG and dU (planes 0 and 1 of g[0])
+  CUtensorMap c_map, g_map[2], in_map[2];
+  int dtype;
+  int act;
+  Out g[2];                           // kUp: gate and up (p NULL: not wanted); kDown: dG and dU
+  Out in[2];                          // kDown: the saved gate and up
   unsigned* count;                    // finished splits per warp of a tile; zero between calls
   unsigned* status;
   unsigned limit;                     // polls of a wait
@@ -340,36 +353,38 @@ __device__ __forceinline__ void put_block(char* block, int row, int j, const uns
 
 // A work item of the persistent loop.
 struct Item {
-  int batch, split, tm, tn;
+  int job, batch, split, tm, tn;
   int tile;                           // number of (batch, tm, tn)
   int k0, k1;                         // stages [k0, k1) of every segment
 };
 
-// Items in order: the splits of a tile next to each other (they finish together), tiles in bands of
-// eight along m, so that the CTAs that run at once share operands in L2.
+// Items in order: the jobs one after another, the splits of a tile next to each other (they finish
+// together), tiles in bands of eight along m, so that the CTAs that run at once share operands in L2.
 __device__ __forceinline__ Item item_of(const ProductArgs& a, int i) {
   constexpr int BAND = 8;
   Item it;
-  it.split = i % a.splits;
-  int t = i / a.splits;
+  it.job = (a.jobs > 1 && i >= a.job[1].first) + (a.jobs > 2 && i >= a.job[2].first);
+  const ProductJob& q = a.job[it.job];
+  i -= q.first;
+  it.split = i % q.splits;
+  int t = i / q.splits;
   it.tile = t;
-  const int per_batch = a.tiles_m * a.tiles_n;
+  const int per_batch = q.tiles_m * q.tiles_n;
   it.batch = t / per_batch;
   t -= it.batch * per_batch;
-  const int band = t / (BAND * a.tiles_n);
-  t -= band * BAND * a.tiles_n;
-  const int height = min(BAND, a.tiles_m - band * BAND);
+  const int band = t / (BAND * q.tiles_n);
+  t -= band * BAND * q.tiles_n;
+  const int height = min(BAND, q.tiles_m - band * BAND);
   it.tn = t / height;
   it.tm = band * BAND + t % height;
-  it.k0 = (int)((long long)a.kblocks * it.split / a.splits);
-  it.k1 = (int)((long long)a.kblocks * (it.split + 1) / a.splits);
+  it.k0 = (int)((long long)q.kblocks * it.split / q.splits);
+  it.k1 = (int)((long long)q.kblocks * (it.split + 1) / q.splits);
   return it;
 }
 
-// CG: CTAs that share a tile (1 or 2) of 128 CG rows and BN sums per row; AMN, BMN: whether the
-// operand lies with its own dimension contiguous instead of k; EPI: what becomes of the sums; F32:
-// whether the call's matrices are in 32 bits.
-template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
+// CG: CTAs that share a tile (1 or 2) of 128 CG rows and BN sums per row; EPI: what becomes of the
+// sums; F32: whether the call's matrices are in 32 bits.
+template <int CG, int BN, int EPI, bool F32>
 struct Product {
   static constexpr int kRows = 128;                      // rows of A per CTA
   static constexpr int kBRows = BN / CG;                 // rows of B per CTA
@@ -411,9 +426,9 @@ struct Product {
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueBytes;
 };
 
-template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
-__global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads, Product<CG, BN, AMN, BMN, EPI, F32>::kCtas) product_kernel(const __grid_constant__ ProductArgs a) {
-  using P = Product<CG, BN, AMN, BMN, EPI, F32>;
+template <int CG, int BN, int EPI, bool F32>
+__global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<CG, BN, EPI, F32>::kCtas) product_kernel(const __grid_constant__ ProductArgs a) {
+  using P = Product<CG, BN, EPI, F32>;
   extern __shared__ char smem_raw[];
   __shared__ uint64_t bars[2 * P::kStages + 4 + 3 * P::kSlots];
   __shared__ uint32_t tmem_base;
@@ -441,9 +456,9 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       mbar_init(slot_empty + 8 * s, 8);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    prefetch_map(&a.a);
-    prefetch_map(&a.b[0]);
-    prefetch_map(&a.b[1]);
+    prefetch_map(&a.job[0].a);
+    prefetch_map(&a.job[0].b[0]);
+    prefetch_map(&a.job[0].b[1]);
   }
   if (warp == 1) tmem_alloc<CG>(smem_addr(&tmem_base), P::kTmemCols);
   tc_fence_before();
@@ -453,7 +468,7 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
   pdl_wait();
   const uint32_t tmem = tmem_base;
   const int first = blockIdx.x / CG, step = gridDim.x / CG;
-  const int items = a.batches * a.tiles_m * a.tiles_n * a.splits;
+  const int items = a.items;
 
   if (warp == 0) {
     if (lane == 0) {
@@ -463,50 +478,59 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       bool ok = true;
       for (int i = first; ok && i < items; i += step) {
         const Item it = item_of(a, i);
-        const int row_a = (it.tm * CG + (int)rank) * P::kRows;
-        for (int seg = 0, kb = it.k0; seg < a.segments; kb + 1 < it.k1 ? ++kb : (++seg, kb = it.k0)) {
-          if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, a.limit, &dead))) break;
-          const uint32_t bar = full0 + 8 * stage;
-          if (rank == 0) mbar_expect(full + 8 * stage, P::kStageBytes * CG);
-          const int k = kb * kBlockK;
-          const uint32_t sa = ring + stage * P::kStageBytes, sb = sa + P::kABytes;
-          const int az = a.az[seg] + it.batch * a.batch_az, bz = a.bz[seg];
-          if (AMN) {
+        // the job by a constant, so that its tensor maps have constant addresses (with addresses of run
+        // time, the loads kept the matrix instructions waiting: 16,384 x 2,048 x 8,192 in 16 bits, y in
+        // 355 us instead of 295)
+        auto feed = [&](auto number) {
+          const ProductJob& job = a.job[decltype(number)::value];
+          const bool a_last = job.a_rows_last, b_last = job.b_rows_last;
+          const int row_a = (it.tm * CG + (int)rank) * P::kRows;
+          const int row_b = EPI == kUp ? it.tn * P::kOutCols : it.tn * BN + (int)rank * P::kBRows;
+          for (int seg = 0, kb = it.k0; seg < job.segments; kb + 1 < it.k1 ? ++kb : (++seg, kb = it.k0)) {
+            if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, a.limit, &dead))) break;
+            const uint32_t bar = full0 + 8 * stage;
+            if (rank == 0) mbar_expect(full + 8 * stage, P::kStageBytes * CG);
+            const int k = kb * kBlockK;
+            const uint32_t sa = ring + stage * P::kStageBytes, sb = sa + P::kABytes;
+            const int az = job.az[seg] + it.batch * job.batch_az, bz = job.bz[seg];
+            if (EPI == kPlain && a_last) {
 #pragma unroll
-            for (int c = 0; c < P::kRows / 64; ++c) tma_load<CG>(sa + c * 8192, &a.a, row_a + c * 64, k, az, bar);
-          } else {
-            tma_load<CG>(sa, &a.a, k, row_a, az, bar);
-          }
-          if (EPI == kUp) {
-            // gate and up rows of the same hidden columns: sums [0, BN/2) and [BN/2, BN)
-            if (CG == 2) {
-              tma_load<CG>(sb, &a.b[rank], k, it.tn * P::kOutCols, bz, bar);
+              for (int c = 0; c < P::kRows / 64; ++c) tma_load<CG>(sa + c * 8192, &job.a, row_a + c * 64, k, az, bar);
             } else {
-              tma_load<CG>(sb, &a.b[0], k, it.tn * P::kOutCols, bz, bar);
-              tma_load<CG>(sb + P::kBBytes / 2, &a.b[1], k, it.tn * P::kOutCols, bz, bar);
+              tma_load<CG>(sa, &job.a, k, row_a, az, bar);
             }
-          } else {
-            const CUtensorMap* b = &a.b[a.bsel[seg]];
-            const int row_b = it.tn * BN + (int)rank * P::kBRows;
-            if (BMN) {
+            if (EPI == kUp) {
+              // gate and up rows of the same hidden columns: sums [0, BN/2) and [BN/2, BN)
+              if (CG == 2) {
+                tma_load<CG>(sb, &job.b[rank], k, row_b, bz, bar);
+              } else {
+                tma_load<CG>(sb, &job.b[0], k, row_b, bz, bar);
+                tma_load<CG>(sb + P::kBBytes / 2, &job.b[1], k, row_b, bz, bar);
+              }
+            } else {
+              const CUtensorMap* b = EPI == kDown ? &job.b[0] : &job.b[job.bsel[seg]];
+              if (EPI == kDown || b_last) {
 #pragma unroll
-              for (int c = 0; c < P::kBRows / 64; ++c) tma_load<CG>(sb + c * 8192, b, row_b + c * 64, k, bz, bar);
-            } else {
-              tma_load<CG>(sb, b, k, row_b, bz, bar);
+                for (int c = 0; c < P::kBRows / 64; ++c) tma_load<CG>(sb + c * 8192, b, row_b + c * 64, k, bz, bar);
+              } else {
+                tma_load<CG>(sb, b, k, row_b, bz, bar);
+              }
+            }
+            if (++stage == P::kStages) {
+              stage = 0;
+              phase ^= 1;
             }
           }
-          if (++stage == P::kStages) {
-            stage = 0;
-            phase ^= 1;
-          }
-        }
+        };
+        if (EPI != kPlain || it.job == 0) feed(std::integral_constant<int, 0>());
+        else if (it.job == 1) feed(std::integral_constant<int, 1>());
+        else feed(std::integral_constant<int, 2>());
       }
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      const uint32_t idesc = (1u << 4) | ((a.dtype == ABCD_F16 ? 0u : 1u) << 7) | ((a.dtype == ABCD_F16 ? 0u : 1u) << 10) |
-                             ((AMN ? 1u : 0u) << 15) | ((BMN ? 1u : 0u) << 16) | ((uint32_t)(BN / 8) << 17) |
-                             ((uint32_t)(128 * CG / 16) << 24);
+      const uint32_t type = a.dtype == ABCD_F16 ? 0u : 1u;
+      const uint32_t form = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)(BN / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
       int stage = 0;
       uint32_t phase = 0;
       int buf = 0;
@@ -516,20 +540,35 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
         const Item it = item_of(a, i);
         if (!(ok = mbar_wait(sums_empty + 8 * buf, sums_phase ^ 1, a.limit, &dead))) break;
         tc_fence_after();
-        const int stages = a.segments * (it.k1 - it.k0);
-        for (int kb = 0; kb < stages; ++kb) {
-          if (!(ok = mbar_wait(full + 8 * stage, phase, a.limit, &dead))) break;
-          tc_fence_after();
-          const uint32_t sa = ring + stage * P::kStageBytes, sb = sa + P::kABytes;
+        const ProductJob& job = a.job[it.job];
+        const int stages = job.segments * (it.k1 - it.k0);
+        // the operands' forms, and with them the descriptors' steps, are constants of the loop
+        auto multiply = [&](auto a_last, auto b_last) {
+          constexpr uint32_t A_STEP = decltype(a_last)::value ? 2048 : 32, B_STEP = decltype(b_last)::value ? 2048 : 32;   // bytes of 16 k
+          const uint32_t idesc = form | ((uint32_t)decltype(a_last)::value << 15) | ((uint32_t)decltype(b_last)::value << 16);
+          for (int kb = 0; kb < stages; ++kb) {
+            if (!(ok = mbar_wait(full + 8 * stage, phase, a.limit, &dead))) break;
+            tc_fence_after();
+            const uint32_t sa = ring + stage * P::kStageBytes, sb = sa + P::kABytes;
 #pragma unroll
-          for (int q = 0; q < kBlockK / 16; ++q)
-            mma16<CG>(tmem + buf * BN, tile_descriptor(sa + q * (AMN ? 2048 : 32), 8192),
-                      tile_descriptor(sb + q * (BMN ? 2048 : 32), 8192), idesc, kb > 0 || q > 0);
-          mma_commit<CG>(empty + 8 * stage);
-          if (++stage == P::kStages) {
-            stage = 0;
-            phase ^= 1;
+            for (int q = 0; q < kBlockK / 16; ++q)
+              mma16<CG>(tmem + buf * BN, tile_descriptor(sa + q * A_STEP, 8192), tile_descriptor(sb + q * B_STEP, 8192), idesc,
+                        kb > 0 || q > 0);
+            mma_commit<CG>(empty + 8 * stage);
+            if (++stage == P::kStages) {
+              stage = 0;
+              phase ^= 1;
+            }
           }
+        };
+        if constexpr (EPI == kUp) {
+          multiply(std::false_type(), std::false_type());
+        } else if constexpr (EPI == kDown) {
+          multiply(std::false_type(), std::true_type());
+        } else {
+          if (job.a_rows_last) multiply(std::true_type(), std::true_type());
+          else if (job.b_rows_last) multiply(std::false_type(), std::true_type());
+          else multiply(std::false_type(), std::false_type());
         }
         if (ok) mma_commit<CG>(sums_full + 8 * buf);
         buf ^= 1;
@@ -548,10 +587,10 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
         for (int i = first; ok && i < items; i += step) {
           const Item it = item_of(a, i);
           const int m = it.tm * CG * P::kRows + row0;
-          if (m >= a.m) continue;
+          if (m >= a.job[0].m) continue;
           for (int s = 0; s < BLOCKS; ++s) {
             const int n = it.tn * P::kOutCols + 32 * s;
-            if (n >= a.n) break;
+            if (n >= a.job[0].n) break;
             const int slot = q % P::kSlots;
             if (!(ok = mbar_wait(slot_empty + 8 * slot, (q / P::kSlots & 1) ^ 1, a.limit, &dead))) break;
             const uint32_t bar = slot_full + 8 * (q % (2 * P::kSlots)), at = smem_addr(buffers) + (6 + 2 * slot) * P::kBlockBytes;
@@ -580,7 +619,7 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
         __syncwarp();
         tc_fence_after();
         const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16);
-        const int blocks = m < a.m ? min(BLOCKS, (a.n - n0 + 31) / 32) : 0;
+        const int blocks = m < a.job[0].m ? min(BLOCKS, (a.job[0].n - n0 + 31) / 32) : 0;
 #pragma unroll 1
         for (int s = (q + group) & 1; s < blocks; s += 2) {
           const int c = 32 * s + 16 * half;
@@ -674,8 +713,8 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       Part p;
       p.m = (it.tm * CG + (int)rank) * P::kRows + quarter * 32;
       p.n = it.tn * P::kOutCols + share * P::kWarpCols;
-      p.rows = min(32, a.m - p.m);
-      p.cols = min(P::kWarpCols, a.n - p.n);
+      p.rows = min(32, a.job[it.job].m - p.m);
+      p.cols = min(P::kWarpCols, a.job[it.job].n - p.n);
       return p;
     };
     const bool ahead = P::kAhead && a.in[0].vec && a.in[1].vec;
@@ -703,6 +742,7 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       const Item next = item_of(a, min(i + step, items - 1));
       Part then = part_of(next);
       if (i + step >= items) then.rows = 0;
+      const ProductJob& job = a.job[it.job];
       const int m = p.m, n = p.n, rows = p.rows, cols = p.cols;
       if (!__all_sync(~0u, mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead))) break;
       tc_fence_after();
@@ -717,9 +757,9 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
       float* part = nullptr;
       constexpr int PARTS = EPI == kUp ? 2 : 1;
       constexpr long long PIECE = (long long)CG * P::kWarps * PARTS * P::kWarpCols * 32;
-      if (EPI != kPlain && a.splits > 1) {
+      if (EPI != kPlain && job.splits > 1) {
         // this part's sums to the workspace [column][row]; the last warp to have done so goes on
-        part = a.part + (long long)it.tile * a.splits * PIECE +
+        part = job.part + (long long)it.tile * job.splits * PIECE +
                ((long long)rank * P::kWarps + ewarp) * PARTS * P::kWarpCols * 32 + lane;
         if (mine) {
           float* mypart = part + it.split * PIECE;
@@ -739,21 +779,21 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
           unsigned* count = a.count + ((long long)it.tile * CG + rank) * P::kWarps + ewarp;
           if (lane == 0) {
             done = atomicAdd(count, 1u);
-            if (done == (unsigned)a.splits - 1) *count = 0;
+            if (done == (unsigned)job.splits - 1) *count = 0;
           }
           done = __shfl_sync(~0u, done, 0);
           __threadfence();
-          mine = done == (unsigned)a.splits - 1;
+          mine = done == (unsigned)job.splits - 1;
         }
       }
       auto sum_columns = [&](int c, int which, float (&v)[P::CW]) {
-        if (EPI == kPlain || a.splits == 1) {
+        if (EPI == kPlain || job.splits == 1) {
           tmem_load(sums + which * (BN / 2) + c, v);
         } else {
 #pragma unroll
           for (int q = 0; q < P::CW; ++q) v[q] = 0.f;
 #pragma unroll 2
-          for (int s = 0; s < a.splits; ++s) {
+          for (int s = 0; s < job.splits; ++s) {
             const float* from = part + s * PIECE + (which * P::kWarpCols + c) * 32;
 #pragma unroll
             for (int q = 0; q < P::CW; ++q) v[q] += __ldcg(from + q * 32);
@@ -787,7 +827,7 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
           act_values(v, a.act);
 #pragma unroll
           for (int q = 0; q < P::CW; ++q) v[q] *= u[q];
-          store_operand<F32, P::CW>(v, a.c[0], m, n + c, rows, w, bf16, buffer);
+          store_operand<F32, P::CW>(v, job.c[0], m, n + c, rows, w, bf16, buffer);
         } else if constexpr (EPI == kDown) {
           float z[P::CW], u[P::CW], s[P::CW];
           const char* zbuf = saved + (c / 16 & 1) * 2 * SAVED;
@@ -815,15 +855,15 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
           }
           store_operand<F32, P::CW>(s, a.g[0], m, n + c, rows, w, bf16, buffer);
           store_operand<F32, P::CW>(z, a.g[1], m, n + c, rows, w, bf16, buffer);
-          store_operand<F32, P::CW>(u, a.c[0], m, n + c, rows, w, bf16, buffer);
+          store_operand<F32, P::CW>(u, job.c[0], m, n + c, rows, w, bf16, buffer);
         } else {
           sum_columns(c, 0, v);
           tmem_load_wait(v);
           if (last) release();
-          if (a.splits == 1) {
-            store_matrix<F32, P::CW>(v, a.c[it.batch], m, n + c, rows, w, bf16, buffer);
+          if (job.splits == 1) {
+            store_matrix<F32, P::CW>(v, job.c[it.batch], m, n + c, rows, w, bf16, buffer);
           } else {
-            const Out o{a.part + ((long long)it.split * a.batches + it.batch) * a.m * a.part_ld, a.part_ld, 0, 1};
+            const Out o{job.part + ((long long)it.split * job.batches + it.batch) * job.m * job.part_ld, job.part_ld, 0, 1};
 #pragma unroll
             for (int e = 0; e < P::CW; e += 16) {      // sixteen of 32 bits take the buffer of 32 of 16
               float x[16];
@@ -855,13 +895,13 @@ __global__ void __launch_bounds__(Product<CG, BN, AMN, BMN, EPI, F32>::kThreads,
   if (threadIdx.x == 0 && dead) atomicOr(a.status, kStatusTimeout);
 }
 
-template <int CG, int BN, bool AMN, bool BMN, int EPI, bool F32>
+template <int CG, int BN, int EPI, bool F32>
 abcd_status launch_product(abcd_ctx* ctx, const ProductArgs& a) {
-  using P = Product<CG, BN, AMN, BMN, EPI, F32>;
-  auto* kernel = product_kernel<CG, BN, AMN, BMN, EPI, F32>;
+  using P = Product<CG, BN, EPI, F32>;
+  auto* kernel = product_kernel<CG, BN, EPI, F32>;
   const cudaError_t e = allow_smem(ctx, (const void*)kernel);
   if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "product_kernel: %s", cudaGetErrorString(e));
-  const long long items = (long long)a.batches * a.tiles_m * a.tiles_n * a.splits;
+  const int items = a.items;
   const int units = P::kCtas * ctx->num_sms / CG;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(CG * (items < units ? items : units)));
@@ -894,24 +934,18 @@ constexpr Shape kShapes[3] = {{2, 256, 1, 7.1, 0.25, 0.34, {{1.7, 1.8}, {2.7, 9.
                               {1, 128, 1, 5.9, 0.22, 0.33, {{0.5, 0.8}, {2.5, 4.5}, {6.1, 17.0}}},
                               {1, 64, 2, 5.2, 0.24, 0.36, {{0.8, 1.0}, {2.1, 3.6}, {3.3, 8.3}}}};
 
-template <bool AMN, bool BMN, int EPI, bool F32>
-abcd_status launch_shape(abcd_ctx* ctx, int shape, const ProductArgs& a) {
-  if (shape == 0) return launch_product<2, 256, AMN, BMN, EPI, F32>(ctx, a);
-  if (shape == 1) return launch_product<1, 128, AMN, BMN, EPI, F32>(ctx, a);
-  return launch_product<1, 64, AMN, BMN, EPI, F32>(ctx, a);
+template <int EPI, bool F32> abcd_status launch_shape(abcd_ctx* ctx, int shape, const ProductArgs& a) {
+  if (shape == 0) return launch_product<2, 256, EPI, F32>(ctx, a);
+  if (shape == 1) return launch_product<1, 128, EPI, F32>(ctx, a);
+  return launch_product<1, 64, EPI, F32>(ctx, a);
 }
-
-// The five products of the layer, by what they are of.
-enum { kProductUp, kProductOut, kProductDown, kProductDx, kProductDw };
-template <bool F32> abcd_status launch_any(abcd_ctx* ctx, int which, int shape, const ProductArgs& a) {
-  if (which == kProductUp) return launch_shape<false, false, kUp, F32>(ctx, shape, a);
-  if (which == kProductOut) return launch_shape<false, false, kPlain, F32>(ctx, shape, a);
-  if (which == kProductDown) return launch_shape<false, true, kDown, F32>(ctx, shape, a);
-  if (which == kProductDx) return launch_shape<false, true, kPlain, F32>(ctx, shape, a);
-  return launch_shape<true, true, kPlain, F32>(ctx, shape, a);
+template <bool F32> abcd_status launch_any(abcd_ctx* ctx, int epi, int shape, const ProductArgs& a) {
+  if (epi == kUp) return launch_shape<kUp, F32>(ctx, shape, a);
+  if (epi == kDown) return launch_shape<kDown, F32>(ctx, shape, a);
+  return launch_shape<kPlain, F32>(ctx, shape, a);
 }
 // One translation unit each.
-abcd_status launch_16(abcd_ctx* ctx, int which, int shape, const ProductArgs& a);
-abcd_status launch_32(abcd_ctx* ctx, int which, int shape, const ProductArgs& a);
+abcd_status launch_16(abcd_ctx* ctx, int epi, int shape, const ProductArgs& a);
+abcd_status launch_32(abcd_ctx* ctx, int epi, int shape, const ProductArgs& a);
 
 }  // namespace abcd

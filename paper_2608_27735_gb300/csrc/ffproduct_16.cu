@@ -3,8 +3,8 @@
 
 namespace abcd {
 
-abcd_status launch_16(abcd_ctx* ctx, int which, int shape, const ProductArgs& a) {
-  return launch_any<false>(ctx, which, shape, a);
+abcd_status launch_16(abcd_ctx* ctx, int epi, int shape, const ProductArgs& a) {
+  return launch_any<false>(ctx, epi, shape, a);
 }
 
 }  // namespace abcd

@@ -3,8 +3,8 @@
 
 namespace abcd {
 
-abcd_status launch_32(abcd_ctx* ctx, int which, int shape, const ProductArgs& a) {
-  return launch_any<true>(ctx, which, shape, a);
+abcd_status launch_32(abcd_ctx* ctx, int epi, int shape, const ProductArgs& a) {
+  return launch_any<true>(ctx, epi, shape, a);
 }
 
 }  // namespace abcd

@@ -2,12 +2,12 @@
 //   G = x Wg^T, U = x Wu^T, H = act(G) U, y = H Wd^T
 //   dH = dy Wd, dU = dH act(G), dG = dH U act'(G), dx = dG Wg + dU Wu,
 //   dWg = dG^T x, dWu = dU^T x, dWd = dy^T H.
-// Five products: both projections with the activation and H; y; dH with dG, dU and H again (from the
-// saved G and U, so that H need not be kept from the forward pass); dx as one sum over both weights;
-// dWg and dWu in one grid, and dWd.  The kernel is in ffproduct.cuh; this file is the host's side:
+// Four launches of products: both projections with the activation and H; y; dH with dG, dU and H again
+// (from the saved G and U, so that H need not be kept from the forward pass); dx (one sum over both
+// weights) with dWg, dWu and dWd.  The kernel is in ffproduct.cuh; this file is the host's side:
 // operands, tensor maps, the choice of tiles and splits, the workspace.
 #include <algorithm>
-#include <cstring>
+#include <cmath>
 
 #include "ffproduct.cuh"
 
@@ -108,53 +108,57 @@ __global__ void __launch_bounds__(256) unpack_kernel(const __grid_constant__ Unp
   }
 }
 
-// The result of a product whose k was split: its parts added in their order, rounded to the type of
-// the matrices.  A thread takes four columns of a row and a run of consecutive parts; where the parts
-// are many, a CTA's threads share them in two to eight runs, which are added in their order.
+// The results of products whose k was split: their parts added in their order, rounded to the type of
+// the matrices; up to four results a launch.  A thread takes four columns of a row and a run of
+// consecutive parts; where the parts are many, a CTA's threads share them in two to eight runs, which
+// are added in their order.
 struct JoinArgs {
-  const float* part;
-  long long ld, plane;                // elements between rows, between splits
-  int rows, cols, splits, runs;
-  Out c[2];                           // per batch
+  struct One {
+    const float* part;
+    long long ld, plane;              // elements between rows, between splits
+    int rows, cols, splits, runs;
+    Out c;
+  } r[4];
 };
 template <typename T>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinArgs a) {
   pdl_wait();
   __shared__ float4 run[256];
-  const int lanes = 256 / a.runs, lane = threadIdx.x % lanes, w = threadIdx.x / lanes;
-  const unsigned groups = (a.cols + 3) / 4;
+  const JoinArgs::One& q = a.r[blockIdx.y];
+  const int lanes = 256 / q.runs, lane = threadIdx.x % lanes, w = threadIdx.x / lanes;
+  const unsigned groups = (q.cols + 3) / 4;
+  if (blockIdx.x * lanes >= groups * q.rows) return;
   const unsigned i = blockIdx.x * lanes + lane, row = i / groups, col = 4 * (i - row * groups);
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (row < (unsigned)a.rows) {
-    const float* p = a.part + (long long)blockIdx.y * a.rows * a.ld + row * a.ld + col;
-    const int k1 = a.splits * (w + 1) / a.runs;
+  if (row < (unsigned)q.rows) {
+    const float* p = q.part + row * q.ld + col;
+    const int k1 = q.splits * (w + 1) / q.runs;
 #pragma unroll 4
-    for (int k = a.splits * w / a.runs; k < k1; ++k) {
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(p + k * a.plane));
+    for (int k = q.splits * w / q.runs; k < k1; ++k) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(p + k * q.plane));
       s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
   }
-  if (a.runs > 1) {
+  if (q.runs > 1) {
     run[threadIdx.x] = s;
     __syncthreads();
     if (w) return;
-    for (int k = 1; k < a.runs; ++k) {
+    for (int k = 1; k < q.runs; ++k) {
       const float4 v = run[k * lanes + lane];
       s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
   }
-  if (row >= (unsigned)a.rows) return;
-  const Out& o = a.c[blockIdx.y];
-  T* c = (T*)o.p + row * o.stride + col;
-  if (o.vec && (int)col + 4 <= a.cols) {
-    Pack<T, 4> q;
-    q.v[0] = from_f32<T>(s.x); q.v[1] = from_f32<T>(s.y); q.v[2] = from_f32<T>(s.z); q.v[3] = from_f32<T>(s.w);
-    *reinterpret_cast<Pack<T, 4>*>(c) = q;
+  if (row >= (unsigned)q.rows) return;
+  T* c = (T*)q.c.p + row * q.c.stride + col;
+  if (q.c.vec && (int)col + 4 <= q.cols) {
+    Pack<T, 4> v;
+    v.v[0] = from_f32<T>(s.x); v.v[1] = from_f32<T>(s.y); v.v[2] = from_f32<T>(s.z); v.v[3] = from_f32<T>(s.w);
+    *reinterpret_cast<Pack<T, 4>*>(c) = v;
   } else {
     const float v[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if ((int)col + e < a.cols) c[e] = from_f32<T>(v[e]);
+      if ((int)col + e < q.cols) c[e] = from_f32<T>(v[e]);
   }
 }
 
@@ -239,117 +243,178 @@ Out out_of(const Operand& o, int matrix, int dtype) {
   return Out{(unsigned short*)const_cast<void*>(o.p) + matrix * terms_of(dtype) * o.plane, o.pitch, o.plane, 1};
 }
 
-// One product: A and up to two B operands, whether each lies with its own dimension contiguous.
+// One product: A and up to two B operands (the sum of both products, or gate and up), and its results.
 struct Job {
   Operand a, b[2];
-  Operand c, g[2], in[2];    // kUp, kDown: the matrices of the epilogue (g[0].p NULL: no gate and up)
-  int nb;                    // B operands (kPlain with two: the sum of both products)
+  int nb;
+  bool a_rows_last, b_rows_last;   // the operand lies with its own dimension contiguous instead of k
   long long m, n, k;
   int batches;
-  ProductArgs args;
+  Out c[2];
+};
+// What the epilogues of kUp and kDown read and write besides.
+struct Hidden {
+  int act;
+  Operand c, g[2], in[2];
+  Out out[2], saved[2];            // the same as g and in
 };
 
-// Picks the shape and the number of splits with the least estimated time: the waves of tiles, each
-// its stages or (beside the next tile's stages) its epilogue, plus the last epilogue, plus the
-// splits' joining (their sums written and read through L2).
-void plan(int sms, long long m, long long n, int epi, bool f32, long long kblocks, int segments, long long batches, int* shape, int* splits) {
-  static constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 16, 20, 24, 30, 38, 48, 64};
+int segments_of(const Job& j, int epi, int dtype) {
+  return (epi == kUp ? 1 : j.nb) * (dtype == ABCD_F32 ? 6 : 1);
+}
+
+// Picks the shape and each product's splits with the least estimated time.  The items (tiles, or parts
+// of them) cost their stages or, beside the next item's stages, their epilogue; they are dealt out to
+// the CTAs in turn, so that the last wave is partly idle.  Splits bring the products' items near one
+// size, the whole work over one to three waves; their joining writes and reads the sums through L2.
+void plan(int sms, int dtype, int epi, const Job* jobs, int n, int* shape, int* splits) {
+  const bool f32 = dtype == ABCD_F32;
   double best = 1e300;
   for (int s = 0; s < 3; ++s) {
     const Shape& q = kShapes[s];
-    const long long cols = epi == kUp ? q.bn / 2 : q.bn, units = (epi == kDown ? 1 : q.ctas) * sms / q.cg;
-    const long long tiles = batches * ((m + 128 * q.cg - 1) / (128 * q.cg)) * ((n + cols - 1) / cols);
-    const long long tile_bytes = 4LL * 128 * q.cg * q.bn;
-    // the sums have to fit the workspace, and where the last part's warps add them up, all parts of a
-    // tile run at once; the large tile's blocks of results are whole sums
-    long long most = epi == kPlain ? (long long)kPartBytes / (tiles * tile_bytes) : s == 0 && !f32 ? 1 : units / tiles;
-    most = std::min(most, kblocks);
-    const double epilogue = q.epilogue[epi][f32];
-    for (const int p : kSplits) {
-      if (p > 1 && p > most) break;
-      const double waves = (double)((tiles * p + units - 1) / units);
-      const double busy = std::min(1.0, (double)(tiles * p) / (double)units);
-      const double stages = (double)(segments * ((kblocks + p - 1) / p)) * (q.idle + (q.busy - q.idle) * busy);
-      const double joined = p == 1 ? 0.0 : 2.5 + (double)(tiles * p * tile_bytes) / 4e6;
-      const double t = q.fixed + waves * std::max(stages, epilogue) + std::min(stages, epilogue) + joined;
+    const long long units = (epi == kDown ? 1 : q.ctas) * sms / q.cg, cols = epi == kUp ? q.bn / 2 : q.bn;
+    const double tile_bytes = 4.0 * 128 * q.cg * q.bn, epilogue = q.epilogue[epi][f32];
+    long long tiles[kMaxJobs], kblocks[kMaxJobs];
+    double work = 0;                                     // stages of all tiles
+    for (int k = 0; k < n; ++k) {
+      tiles[k] = jobs[k].batches * ((jobs[k].m + 128 * q.cg - 1) / (128 * q.cg)) * ((jobs[k].n + cols - 1) / cols);
+      kblocks[k] = (jobs[k].k + kBlockK - 1) / kBlockK;
+      work += (double)tiles[k] * (double)kblocks[k] * segments_of(jobs[k], epi, dtype);
+    }
+    for (int waves = 0; waves <= 6; ++waves) {           // 0: no splits
+      double room = (double)kPartBytes, joined = 0, total = 0, longest = 0, items = 0;
+      int p[kMaxJobs];
+      for (int k = 0; k < n; ++k) {
+        const double stages = (double)kblocks[k] * segments_of(jobs[k], epi, dtype);
+        double want = waves == 0 ? 1 : stages / std::max(1.0, work / (double)(units * waves));
+        // where the last part's warps add the parts up, all parts of a tile run at once; the large
+        // tile's blocks of results are whole sums
+        double most = epi == kPlain ? room / ((double)tiles[k] * tile_bytes) : s == 0 && !f32 ? 1 : (double)units / (double)tiles[k];
+        most = std::min({most, (double)kblocks[k], 64.0});
+        p[k] = std::max(1, (int)std::min(std::ceil(want - 0.05), std::floor(most)));
+        if (p[k] > 1) {
+          room -= (double)tiles[k] * p[k] * tile_bytes;
+          joined += (double)tiles[k] * p[k] * tile_bytes / 4e6;
+        }
+        items += (double)tiles[k] * p[k];
+      }
+      if (joined > 0) joined += 2.5;
+      const double busy = std::min(1.0, items / (double)units), stage = q.idle + (q.busy - q.idle) * busy;
+      double stages_last = 0;
+      for (int k = 0; k < n; ++k) {
+        const double stages = (double)((kblocks[k] + p[k] - 1) / p[k]) * segments_of(jobs[k], epi, dtype) * stage;
+        const double cost = std::max(stages, epilogue);
+        total += cost * (double)tiles[k] * p[k];
+        longest = std::max(longest, cost);
+        stages_last = std::max(stages_last, std::min(stages, epilogue));
+      }
+      // one product: whole waves; several: the last wave is filled to half on average
+      double t = n == 1 ? longest * std::ceil(items / (double)units) : std::max(longest, total / (double)units + 0.5 * longest);
+      t += q.fixed + stages_last + joined;
       if (t < best) {
         best = t;
         *shape = s;
-        *splits = p;
+        for (int k = 0; k < n; ++k) splits[k] = p[k];
       }
     }
   }
 }
 
-// Segments of a product: pairs of its operands' terms.
-int segments_of(int which, int dtype, int nb) {
-  return (which == kProductUp ? 1 : nb) * (dtype == ABCD_F32 ? 6 : 1);
-}
-int epilogue_of(int which) { return which == kProductUp ? kUp : which == kProductDown ? kDown : kPlain; }
-
-void plan_of(const abcd_ctx* ctx, int dtype, int which, int nb, long long m, long long n, long long k, long long batches, int* shape, int* splits) {
-  plan(std::min(ctx->num_sms, kNetSms), m, n, epilogue_of(which), dtype == ABCD_F32, (k + kBlockK - 1) / kBlockK,
-       segments_of(which, dtype, nb), batches, shape, splits);
-}
-// Whether the epilogue of kProductUp or kProductDown moves the saved projections by TMA.
-bool by_blocks(const abcd_ctx* ctx, int dtype, int which, long long m, long long n, long long k) {
-  int shape = 0, splits = 1;
+// Whether the epilogue of kUp or kDown moves the saved projections by TMA.
+bool by_blocks(const abcd_ctx* ctx, int dtype, int epi, long long m, long long n, long long k) {
   if (dtype == ABCD_F32) return false;
-  plan_of(ctx, dtype, which, 1, m, n, k, 1, &shape, &splits);
+  int shape = 0, splits[kMaxJobs];
+  Job j{};
+  j.nb = 1;
+  j.m = m;
+  j.n = n;
+  j.k = k;
+  j.batches = 1;
+  plan(std::min(ctx->num_sms, kNetSms), dtype, epi, &j, 1, &shape, splits);
   return shape == 0;
 }
 
-abcd_status run(abcd_ctx* ctx, int dtype, int which, Job& j) {
-  const int epi = epilogue_of(which);
-  const bool amn = which == kProductDw, bmn = amn || which == kProductDown || which == kProductDx;
-  ProductArgs& a = j.args;
+// Launches the products (and what joins their splits).
+abcd_status run(abcd_ctx* ctx, int dtype, int epi, const Job* jobs, int n, const Hidden* hidden = nullptr) {
+  ProductArgs a{};
   const int terms = terms_of(dtype);
-  a.m = (int)j.m;
-  a.n = (int)j.n;
-  a.kblocks = (int)((j.k + kBlockK - 1) / kBlockK);
-  a.segments = 0;
-  // pairs of terms, the smallest products first
-  const int pairs = epi == kUp ? 1 : j.nb;
-  for (int order = terms - 1; order >= 0; --order)
-    for (int b = 0; b < pairs; ++b)
-      for (int t = order; t >= 0; --t) {
-        a.az[a.segments] = (unsigned char)(b * terms + t);
-        a.bsel[a.segments] = (unsigned char)b;
-        a.bz[a.segments++] = (unsigned char)(order - t);
-      }
-  a.batches = j.batches;
-  a.batch_az = terms;
+  int shape = 0, splits[kMaxJobs];
+  plan(std::min(ctx->num_sms, kNetSms), dtype, epi, jobs, n, &shape, splits);
+  const int cg = kShapes[shape].cg, bn = kShapes[shape].bn, cols = epi == kUp ? bn / 2 : bn;
+  a.jobs = n;
   a.dtype = dtype;
-  int shape = 0, splits = 1;
-  plan_of(ctx, dtype, which, j.nb, j.m, j.n, j.k, j.batches, &shape, &splits);
-  const int cg = kShapes[shape].cg, bn = kShapes[shape].bn;
-  a.tiles_m = (int)((j.m + 128 * cg - 1) / (128 * cg));
-  const int cols = epi == kUp ? bn / 2 : bn;
-  a.tiles_n = (int)((j.n + cols - 1) / cols);
-  a.splits = splits;
   a.count = (unsigned*)(ctx->net_base + kNetCounters);
-  a.part = (float*)(ctx->net_base + kNetHeader);
   a.status = (unsigned*)ctx->net_base;
   a.limit = ctx->wait_limit;
-  bool ok = make_map(&a.a, j.a, dtype, amn ? 64 : 128);
-  for (int b = 0; ok && b < j.nb; ++b) ok = make_map(&a.b[b], j.b[b], dtype, bmn ? 64 : epi == kUp ? bn / 2 : bn / cg);
-  if (!ok) return fail(ctx, ABCD_ERR_CUDA, "tensor map of a product");
-  if (j.nb < 2) a.b[1] = a.b[0];
-  if (epi != kPlain && shape == 0 && dtype != ABCD_F32) {
-    ok = make_map(&a.c_map, j.c, dtype, 128, 32);
-    if (ok && j.g[0].p) ok = make_map(&a.g_map[0], j.g[0], dtype, 128, 32);
-    if (ok && j.g[1].p) ok = make_map(&a.g_map[1], j.g[1], dtype, 128, 32);
-    for (int b = 0; ok && epi == kDown && b < 2; ++b) ok = make_map(&a.in_map[b], j.in[b], dtype, 128, 32);
-    if (!ok) return fail(ctx, ABCD_ERR_CUDA, "tensor map of a product's results");
+  float* part = (float*)(ctx->net_base + kNetHeader);
+  JoinArgs join{};
+  int results = 0;
+  long long join_ctas = 0;
+  bool ok = true;
+  // the products of the longest items first: the short ones level the last wave
+  int order_of[kMaxJobs] = {0, 1, 2};
+  const auto length = [&](int k) { return (double)jobs[k].k * segments_of(jobs[k], epi, dtype) / splits[k]; };
+  std::sort(order_of, order_of + n, [&](int x, int y) { return length(x) != length(y) ? length(x) > length(y) : x < y; });
+  for (int slot = 0; slot < n; ++slot) {
+    const int q = order_of[slot];
+    const Job& j = jobs[q];
+    ProductJob& o = a.job[slot];
+    o.a_rows_last = j.a_rows_last;
+    o.b_rows_last = j.b_rows_last;
+    o.m = (int)j.m;
+    o.n = (int)j.n;
+    o.kblocks = (int)((j.k + kBlockK - 1) / kBlockK);
+    // pairs of terms, the smallest products first
+    for (int order = terms - 1; order >= 0; --order)
+      for (int b = 0; b < (epi == kUp ? 1 : j.nb); ++b)
+        for (int t = order; t >= 0; --t) {
+          o.az[o.segments] = (unsigned char)(b * terms + t);
+          o.bsel[o.segments] = (unsigned char)b;
+          o.bz[o.segments++] = (unsigned char)(order - t);
+        }
+    o.batch_az = terms;
+    o.batches = j.batches;
+    o.tiles_m = (int)((j.m + 128 * cg - 1) / (128 * cg));
+    o.tiles_n = (int)((j.n + cols - 1) / cols);
+    o.splits = splits[q];
+    o.first = a.items;
+    a.items += o.batches * o.tiles_m * o.tiles_n * o.splits;
+    o.c[0] = j.c[0];
+    o.c[1] = j.c[1];
+    o.part = part;
+    o.part_ld = (j.n + 3) / 4 * 4;
+    ok = ok && make_map(&o.a, j.a, dtype, j.a_rows_last ? 64 : 128);
+    for (int b = 0; ok && b < j.nb; ++b) ok = make_map(&o.b[b], j.b[b], dtype, j.b_rows_last ? 64 : epi == kUp ? bn / 2 : bn / cg);
+    if (j.nb < 2) o.b[1] = o.b[0];
+    if (epi != kPlain || splits[q] == 1) continue;
+    const long long plane = j.batches * j.m * o.part_ld;
+    for (int b = 0; b < j.batches; ++b) {
+      const int runs = splits[q] <= 8 ? 1 : splits[q] <= 16 ? 2 : splits[q] <= 32 ? 4 : 8, lanes = 256 / runs;
+      join.r[results++] = JoinArgs::One{part + b * j.m * o.part_ld, o.part_ld, plane, (int)j.m, (int)j.n, splits[q], runs, j.c[b]};
+      join_ctas = std::max(join_ctas, (j.m * ((j.n + 3) / 4) + lanes - 1) / lanes);
+    }
+    part += plane * splits[q];
   }
-  a.part_ld = (j.n + 3) / 4 * 4;
-  const abcd_status st = dtype == ABCD_F32 ? launch_32(ctx, which, shape, a) : launch_16(ctx, which, shape, a);
-  if (st != ABCD_OK || epi != kPlain || splits == 1) return st;
-  const int runs = splits <= 8 ? 1 : splits <= 16 ? 2 : splits <= 32 ? 4 : 8, lanes = 256 / runs;
-  const JoinArgs q{a.part, a.part_ld, j.batches * j.m * a.part_ld, a.m, a.n, splits, runs, {a.c[0], a.c[1]}};
-  const dim3 grid((unsigned)((j.m * ((j.n + 3) / 4) + lanes - 1) / lanes), (unsigned)j.batches);
+  if (hidden) {
+    a.act = hidden->act;
+    for (int k = 0; k < 2; ++k) {
+      a.g[k] = hidden->out[k];
+      a.in[k] = hidden->saved[k];
+    }
+    if (shape == 0 && dtype != ABCD_F32) {
+      ok = ok && make_map(&a.c_map, hidden->c, dtype, 128, 32);
+      for (int k = 0; k < 2; ++k) {
+        if (ok && hidden->g[k].p) ok = make_map(&a.g_map[k], hidden->g[k], dtype, 128, 32);
+        if (ok && hidden->in[k].p) ok = make_map(&a.in_map[k], hidden->in[k], dtype, 128, 32);
+      }
+    }
+  }
+  if (!ok) return fail(ctx, ABCD_ERR_CUDA, "tensor map of a product");
+  const abcd_status st = dtype == ABCD_F32 ? launch_32(ctx, epi, shape, a) : launch_16(ctx, epi, shape, a);
+  if (st != ABCD_OK || results == 0) return st;
   return with_type(dtype, [&](auto t) {
-    return check_launch(ctx, "join_kernel", launch_pdl(join_kernel<decltype(t)>, grid, dim3(256), 0, ctx->stream, q));
+    return check_launch(ctx, "join_kernel", launch_pdl(join_kernel<decltype(t)>, dim3((unsigned)join_ctas, (unsigned)results),
+                                                       dim3(256), 0, ctx->stream, join));
   });
 }
 
@@ -441,7 +506,7 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
   if (needs_pack(w_down)) need.operand(d, f, t);
   need.operand(m, f, t);
   // the saved projections by way of the workspace where TMA has to store them and cannot
-  const bool apart = gate && (needs_pack(gate) || needs_pack(up)) && by_blocks(ctx, t, kProductUp, m, f, d);
+  const bool apart = gate && (needs_pack(gate) || needs_pack(up)) && by_blocks(ctx, t, kUp, m, f, d);
   if (apart) need.operand(m, f, t, 2);
   abcd_status st = room(ctx, what, need.at);
   if (st != ABCD_OK) return st;
@@ -451,31 +516,31 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
   const Operand ox = in.add(x), og = in.add(w_gate), ou = in.add(w_up), od = in.add(w_down);
   if ((st = in.pack(ctx, t)) != ABCD_OK) return st;
   const Operand h = s.operand(m, f, t);
-  Job up_job{ox, {og, ou}, h, {}, {}, 2, m, f, d, 1, {}};
-  up_job.args.act = activation;
-  up_job.args.c[0] = out_of(h, 0, t);
+  const Job up_job{ox, {og, ou}, 2, false, false, m, f, d, 1, {out_of(h, 0, t)}};
+  Hidden hid{};
+  hid.act = activation;
+  hid.c = h;
   if (apart) {
     const Operand saved = s.operand(m, f, t, 2);
-    up_job.g[0] = Operand{saved.p, m, f, saved.pitch, 0, 1};
-    up_job.g[1] = Operand{(unsigned short*)saved.p + saved.plane, m, f, saved.pitch, 0, 1};
-    for (int k = 0; k < 2; ++k) up_job.args.g[k] = out_of(up_job.g[k], 0, t);
+    hid.g[0] = Operand{saved.p, m, f, saved.pitch, 0, 1};
+    hid.g[1] = Operand{(unsigned short*)saved.p + saved.plane, m, f, saved.pitch, 0, 1};
+    for (int k = 0; k < 2; ++k) hid.out[k] = out_of(hid.g[k], 0, t);
   } else if (gate) {
-    up_job.args.g[0] = out_of(gate);
-    up_job.args.g[1] = out_of(up);
-    up_job.g[0] = in_place(gate);
-    up_job.g[1] = in_place(up);
+    hid.g[0] = in_place(gate);
+    hid.g[1] = in_place(up);
+    hid.out[0] = out_of(gate);
+    hid.out[1] = out_of(up);
   }
-  if ((st = run(ctx, t, kProductUp, up_job)) != ABCD_OK) return st;
+  if ((st = run(ctx, t, kUp, &up_job, 1, &hid)) != ABCD_OK) return st;
   if (apart) {
-    const UnpackArgs u{{(const unsigned short*)up_job.g[0].p, (const unsigned short*)up_job.g[1].p},
+    const UnpackArgs u{{(const unsigned short*)hid.g[0].p, (const unsigned short*)hid.g[1].p},
                        {(unsigned short*)gate->data, (unsigned short*)up->data},
-                       m, f, up_job.g[0].pitch, {gate->stride, up->stride}};
+                       m, f, hid.g[0].pitch, {gate->stride, up->stride}};
     const dim3 grid((unsigned)std::min<long long>((m * ((f + 7) / 8) + 255) / 256, 8LL * ctx->num_sms), 2);
     if ((st = check_launch(ctx, "unpack_kernel", launch_pdl(unpack_kernel, grid, dim3(256), 0, ctx->stream, u))) != ABCD_OK) return st;
   }
-  Job y_job{h, {od, od}, {}, {}, {}, 1, m, d, f, 1, {}};
-  y_job.args.c[0] = out_of(y);
-  return run(ctx, t, kProductOut, y_job);
+  const Job y_job{h, {od}, 1, false, false, m, d, f, 1, {out_of(y)}};
+  return run(ctx, t, kPlain, &y_job, 1);
 }
 
 extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* dy,
@@ -538,33 +603,32 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
   }
   if ((st = in.pack(ctx, t)) != ABCD_OK) return st;
   const Operand h = s.operand(m, f, t), dgu = s.operand(m, f, t, 2);
-  Job down{ody, {od, od}, h, {dgu, {}}, {ogate, oup}, 1, m, f, d, 1, {}};
-  down.args.act = activation;
-  down.args.in[0] = apart ? out_of(ogate, 0, t) : out_of(gate);
-  down.args.in[1] = apart ? out_of(oup, 0, t) : out_of(up);
-  down.args.c[0] = out_of(h, 0, t);
-  down.args.g[0] = out_of(dgu, 0, t);
-  down.args.g[1] = out_of(dgu, 1, t);
-  if ((st = run(ctx, t, kProductDown, down)) != ABCD_OK) return st;
-  if (dx) {
-    Job j{dgu, {og, ou}, {}, {}, {}, 2, m, d, f, 1, {}};
-    j.args.c[0] = out_of(dx);
-    if ((st = run(ctx, t, kProductDx, j)) != ABCD_OK) return st;
-  }
+  const Job down{ody, {od}, 1, false, true, m, f, d, 1, {out_of(h, 0, t)}};
+  Hidden hid{};
+  hid.act = activation;
+  hid.c = h;
+  hid.g[0] = dgu;
+  hid.in[0] = ogate;
+  hid.in[1] = oup;
+  hid.out[0] = out_of(dgu, 0, t);
+  hid.out[1] = out_of(dgu, 1, t);
+  hid.saved[0] = apart ? out_of(ogate, 0, t) : out_of(gate);
+  hid.saved[1] = apart ? out_of(oup, 0, t) : out_of(up);
+  if ((st = run(ctx, t, kDown, &down, 1, &hid)) != ABCD_OK) return st;
+  // what is left does not depend on one another: one launch
+  Job jobs[kMaxJobs];
+  int n = 0;
+  if (dx) jobs[n++] = Job{dgu, {og, ou}, 2, false, true, m, d, f, 1, {out_of(dx)}};
   if (dw_gate || dw_up) {
     // dG^T x and dU^T x: the second starts at dU's planes
+    const bool both = dw_gate && dw_up;
     Operand left = dgu;
     if (!dw_gate) left.p = (const unsigned short*)dgu.p + (long long)terms_of(t) * dgu.plane;
-    left.planes = dw_gate && dw_up ? dgu.planes : terms_of(t);
-    Job j{left, {ox, ox}, {}, {}, {}, 1, f, d, m, dw_gate && dw_up ? 2 : 1, {}};
-    j.args.c[0] = out_of(dw_gate ? dw_gate : dw_up);
-    if (dw_gate && dw_up) j.args.c[1] = out_of(dw_up);
-    if ((st = run(ctx, t, kProductDw, j)) != ABCD_OK) return st;
+    left.planes = both ? dgu.planes : terms_of(t);
+    jobs[n] = Job{left, {ox}, 1, true, true, f, d, m, both ? 2 : 1, {out_of(dw_gate ? dw_gate : dw_up)}};
+    if (both) jobs[n].c[1] = out_of(dw_up);
+    ++n;
   }
-  if (dw_down) {
-    Job j{ody, {h, h}, {}, {}, {}, 1, d, f, m, 1, {}};
-    j.args.c[0] = out_of(dw_down);
-    if ((st = run(ctx, t, kProductDw, j)) != ABCD_OK) return st;
-  }
-  return ABCD_OK;
+  if (dw_down) jobs[n++] = Job{ody, {h}, 1, true, true, d, f, m, 1, {out_of(dw_down)}};
+  return n ? run(ctx, t, kPlain, jobs, n) : ABCD_OK;
 }
