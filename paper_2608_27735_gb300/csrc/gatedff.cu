@@ -266,7 +266,8 @@ int segments_of(const Job& j, int epi, int dtype) {
 // Picks the shape and each product's splits with the least estimated time.  The items (tiles, or parts
 // of them) cost their stages or, beside the next item's stages, their epilogue; they are dealt out to
 // the CTAs in turn, so that the last wave is partly idle.  Splits bring the products' items near one
-// size, the whole work over one to three waves; their joining writes and reads the sums through L2.
+// size: the whole work's share of a CTA, or a part of it.  Their joining writes and reads the sums
+// through L2.
 void plan(int sms, int dtype, int epi, const Job* jobs, int n, int* shape, int* splits) {
   const bool f32 = dtype == ABCD_F32;
   double best = 1e300;
@@ -281,7 +282,7 @@ void plan(int sms, int dtype, int epi, const Job* jobs, int n, int* shape, int* 
       kblocks[k] = (jobs[k].k + kBlockK - 1) / kBlockK;
       work += (double)tiles[k] * (double)kblocks[k] * segments_of(jobs[k], epi, dtype);
     }
-    for (int waves = 0; waves <= 6; ++waves) {           // 0: no splits
+    for (const int waves : {0, 1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {   // 0: no splits
       double room = (double)kPartBytes, joined = 0, total = 0, longest = 0, items = 0;
       int p[kMaxJobs];
       for (int k = 0; k < n; ++k) {
