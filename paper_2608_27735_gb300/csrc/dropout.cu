@@ -107,53 +107,46 @@ __global__ void __launch_bounds__(256) dropout_vec_kernel(const __grid_constant_
   }
 }
 
-// Rows of any other length: pieces of V consecutive elements of a row (16 bytes where the rows start
-// on such boundaries, else one element), which lie in one block or two of the generator.
-template <typename T, int V>
+// Rows of any other length and start: a warp takes 32 consecutive blocks, each lane makes one block's
+// eight bits of the mask, and the lanes then take consecutive elements, 32 at a time, and the bits from
+// the lanes that made them.
+template <typename T>
 __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropArgs a) {
   pdl_wait();
-  using P = Pack<T, V>;
-  const unsigned per_row = (unsigned)((a.cols + V - 1) / V);
-  const long long pieces = per_row * a.rows, step = gridDim.x * 256LL;
-  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < pieces; i += step) {
-    const long long row = pieces < (1LL << 32) ? (unsigned)i / per_row : i / per_row;
-    const int col = V * (int)(i - row * per_row), left = (int)min((long long)V, a.cols - col);
-    const T* x = (const T*)a.x + row * a.sx + col;
-    const T* res = (const T*)a.res + row * a.sr + col;
-    T* y = (T*)a.y + row * a.sy + col;
-    P px, pr;
-    if (V > 1 && left == V) {
-      px = *reinterpret_cast<const P*>(x);
-      if (a.res) pr = *reinterpret_cast<const P*>(res);
-    } else {
+  const int lane = threadIdx.x & 31;
+  const long long spans = (a.n + 255) / 256, step = gridDim.x * 8LL;
+  const unsigned cols = (unsigned)a.cols;
+  for (long long s = blockIdx.x * 8LL + threadIdx.x / 32; s < spans; s += step) {
+    const long long e0 = 256 * s;
+    // the span's first element; the lane's lie fewer than 256 columns on
+    const long long row0 = a.n < (1LL << 32) ? (unsigned)e0 / cols : e0 / cols;
+    const unsigned col0 = (unsigned)(e0 - row0 * cols);
+    long long row[8];
+    unsigned col[8];
+    T x[8], res[8];
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        px.v[j] = j < left ? x[j] : from_f32<T>(0.f);
-        if (a.res) pr.v[j] = j < left ? res[j] : from_f32<T>(0.f);
+    for (int k = 0; k < 8; ++k) {
+      const unsigned at = col0 + 32 * k + lane, over = at / cols;
+      row[k] = row0 + over;
+      col[k] = at - over * cols;
+      if (e0 + 32 * k + lane < a.n) {
+        x[k] = ((const T*)a.x)[row[k] * a.sx + col[k]];
+        if (a.res) res[k] = ((const T*)a.res)[row[k] * a.sr + col[k]];
       }
     }
-    const unsigned long long e = (unsigned long long)(row * a.cols + col), block = a.offset + e / 8;
-    const int at = (int)(e % 8);
-    const uint4 w0 = philox(block, a);
-    const uint4 w1 = at + left > 8 ? philox(block + 1, a) : w0;
-    // the piece's numbers from bit 16 at of both blocks' 256 bits on
-    const unsigned word[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+    const uint4 w = philox(a.offset + (unsigned long long)(32 * s + lane), a);
+    const unsigned word[4] = {w.x, w.y, w.z, w.w};
+    unsigned mask = 0;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      unsigned pick = 0;
+    for (int j = 0; j < 8; ++j) mask |= ((j & 1 ? word[j / 2] >> 16 : word[j / 2] & 0xffffu) >= a.t ? 1u : 0u) << j;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) pick = (at + j) / 2 == k ? word[k] : pick;
-      const unsigned u = (at + j) & 1 ? pick >> 16 : pick & 0xffffu;
-      float v = u >= a.t ? to_f32(px.v[j]) * a.scale : 0.f;
-      if (a.res) v += to_f32(pr.v[j]);
-      px.v[j] = from_f32<T>(v);
-    }
-    if (V > 1 && left == V) {
-      *reinterpret_cast<P*>(y) = px;
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (j < left) y[j] = px.v[j];
+    for (int k = 0; k < 8; ++k) {
+      const unsigned bits = __shfl_sync(~0u, mask, 4 * k + lane / 8);
+      if (e0 + 32 * k + lane < a.n) {
+        float v = bits >> (lane & 7) & 1 ? to_f32(x[k]) * a.scale : 0.f;
+        if (a.res) v += to_f32(res[k]);
+        ((T*)a.y)[row[k] * a.sy + col[k]] = from_f32<T>(v);
+      }
     }
   }
 }
@@ -195,13 +188,10 @@ abcd_status drop(abcd_ctx* ctx, const char* what, const abcd_matrix* x, double p
     a.rows = 1;
     a.cols = a.n;
   }
-  const bool pieces = rows_aligned(x, 16) && rows_aligned(y, 16) && (!res || rows_aligned(res, 16));
   return with_type(x->dtype, [&](auto v) {
     using T = decltype(v);
-    constexpr int V = 16 / sizeof(T);
-    const long long work = vec ? (a.n + 7) / 8 : (pieces ? (a.cols + V - 1) / V : a.cols) * a.rows;
-    const long long blocks = std::min<long long>((work + 255) / 256, 8LL * ctx->num_sms);
-    auto* kernel = vec ? (res ? dropout_vec_kernel<T, true> : dropout_vec_kernel<T, false>) : pieces ? dropout_kernel<T, V> : dropout_kernel<T, 1>;
+    const long long blocks = std::min<long long>((a.n + 2047) / 2048, 8LL * ctx->num_sms);
+    auto* kernel = vec ? (res ? dropout_vec_kernel<T, true> : dropout_vec_kernel<T, false>) : dropout_kernel<T>;
     return check_launch(ctx, "dropout_kernel", launch_pdl(kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, a));
   });
 }

@@ -63,7 +63,8 @@ constexpr int kMaxJobs = 3;
 struct ProductArgs {
   ProductJob job[kMaxJobs];
   int jobs, items;
-  // the large tile of 16-bit matrices: kUp stores c, gate, up (g); kDown loads gate, up (in) and stores
+  // the large tile of 16-bit matrices: kUp stores c and, where their rows allow it, gate and up (g);
+  // kDown loads gate, up (in) and stores
   // c, dG and dU (planes 0 and 1 of g[0])
   CUtensorMap c_map, g_map[2], in_map[2];
   int dtype;
@@ -170,48 +171,52 @@ __device__ __forceinline__ void pack_all(const float (&v)[CW], unsigned (&w)[CW 
   }
 }
 
-// 16 bytes of a row of which `bytes` are inside the matrix.
-static __device__ __noinline__ void store_edge(char* at, uint4 v, int bytes, int vec, int elem) {
-  if (bytes <= 0) return;
-  if (vec && bytes >= 16) {
-    *reinterpret_cast<uint4*>(at) = v;
-    return;
-  }
-  const unsigned e[4] = {v.x, v.y, v.z, v.w};
+// A warp's 32 rows in a buffer, as rows of PIECES 16-byte pieces swapped by row so that neither a lane
+// per row nor lanes along the rows meet bank conflicts.
+template <int PIECES> __device__ __forceinline__ int turned(int row, int j) {
+  constexpr int SPREAD = 8 / PIECES > 0 ? 8 / PIECES : 1;   // rows within 128 bytes of the buffer
+  return row * PIECES * 16 + ((j ^ ((row / SPREAD) % PIECES)) * 16);
+}
+// Such rows to a matrix whose rows start anywhere, or the part of them that is inside it: consecutive
+// lanes write consecutive elements.
+template <int PIECES, typename E>
+static __device__ __noinline__ void store_elements(const char* buf, char* base, long long stride_bytes, int rows, int cols) {
+  constexpr int WIDTH = PIECES * 16 / (int)sizeof(E);       // elements of a row
+  constexpr int ROWS = WIDTH < 32 ? 32 / WIDTH : 1;         // rows that the lanes take at a time
+  const int lane = threadIdx.x & 31, at = lane % WIDTH * (int)sizeof(E);
+  if (at >= cols * (int)sizeof(E)) return;
+  base += at;
+  for (int row0 = lane / WIDTH; row0 < rows; row0 += 8 * ROWS) {
+    E v[8];
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    if (2 * q >= bytes) break;
-    if (elem == 2) *reinterpret_cast<unsigned short*>(at + 2 * q) = (unsigned short)(e[q / 2] >> (16 * (q & 1)));
-    else if (!(q & 1)) *reinterpret_cast<unsigned*>(at + 2 * q) = e[q / 2];
+    for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const E*>(buf + turned<PIECES>((row0 + i * ROWS) & 31, at / 16) + at % 16);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (row0 + i * ROWS < rows) *reinterpret_cast<E*>(base + (row0 + i * ROWS) * stride_bytes) = v[i];
   }
 }
 
-// A warp's 32 rows x CW columns, lane l holding row l as words of 16-bit pairs (or 32-bit values):
-// turned round in the warp's buffer, so that consecutive lanes write consecutive 16 bytes of a row.
-// The buffer's 16-byte pieces are swapped by row so that neither side meets bank conflicts.
-template <int WORDS>
+// A warp's 32 rows x CW columns of elements E, lane l holding row l as words: turned round in the
+// warp's buffer, so that consecutive lanes write consecutive 16 bytes of a row.
+template <typename E, int WORDS>
 __device__ __forceinline__ void store_words(const unsigned (&w)[WORDS], char* buf, void* base,
-                                            long long stride_bytes, int rows, int bytes, bool vec, int elem) {
+                                            long long stride_bytes, int rows, int cols, bool vec) {
   constexpr int PIECES = WORDS / 4;                 // 16-byte pieces of a row
   constexpr int ROWS = 32 / PIECES;                 // rows that the lanes take at a time
-  constexpr int SPREAD = 8 / PIECES > 0 ? 8 / PIECES : 1;   // rows within 128 bytes of the buffer
   const int lane = threadIdx.x & 31;
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < PIECES; ++j)
-    *reinterpret_cast<uint4*>(buf + lane * PIECES * 16 + ((j ^ ((lane / SPREAD) % PIECES)) * 16)) =
-        make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    *reinterpret_cast<uint4*>(buf + turned<PIECES>(lane, j)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
   __syncwarp();
-  const int row0 = lane / PIECES, j = lane % PIECES;
-  char* at = (char*)base + row0 * stride_bytes + 16 * j;
-  const bool whole = vec && rows >= 32 && bytes >= PIECES * 16;
+  if (vec && rows >= 32 && cols * (int)sizeof(E) >= PIECES * 16) {
+    const int row0 = lane / PIECES, j = lane % PIECES;
+    char* at = (char*)base + row0 * stride_bytes + 16 * j;
 #pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int row = i * ROWS + row0;
-    const uint4 v = *reinterpret_cast<const uint4*>(buf + row * PIECES * 16 + ((j ^ ((row / SPREAD) % PIECES)) * 16));
-    if (whole) *reinterpret_cast<uint4*>(at) = v;
-    else if (row < rows) store_edge(at, v, bytes - 16 * j, vec, elem);
-    at += ROWS * stride_bytes;
+    for (int i = 0; i < PIECES; ++i, at += ROWS * stride_bytes)
+      *reinterpret_cast<uint4*>(at) = *reinterpret_cast<const uint4*>(buf + turned<PIECES>(i * ROWS + row0, j));
+  } else {
+    store_elements<PIECES, E>(buf, (char*)base, stride_bytes, rows, cols);
   }
 }
 
@@ -223,11 +228,11 @@ __device__ __forceinline__ void store_matrix(const float (&v)[CW], const Out& o,
     unsigned w[CW];
 #pragma unroll
     for (int i = 0; i < CW; ++i) w[i] = __float_as_uint(v[i]);
-    store_words<CW>(w, buf, (float*)o.p + m * o.stride + n, o.stride * 4, rows, cols * 4, o.vec, 4);
+    store_words<unsigned, CW>(w, buf, (float*)o.p + m * o.stride + n, o.stride * 4, rows, cols, o.vec);
   } else {
     unsigned w[CW / 2];
     pack_all(v, w, bf16);
-    store_words<CW / 2>(w, buf, (unsigned short*)o.p + m * o.stride + n, o.stride * 2, rows, cols * 2, o.vec, 2);
+    store_words<unsigned short, CW / 2>(w, buf, (unsigned short*)o.p + m * o.stride + n, o.stride * 2, rows, cols, o.vec);
   }
 }
 
@@ -249,8 +254,8 @@ __device__ __forceinline__ void store_operand(const float (&v)[CW], const Out& o
         const float a = take_term(rest[2 * i]), b = take_term(rest[2 * i + 1]);
         w[i] = pack2(a, b, true);
       }
-      store_words<CW / 2>(w, buf, (unsigned short*)o.p + t * o.plane + m * o.stride + n, o.stride * 2, rows,
-                          cols * 2, o.vec, 2);
+      store_words<unsigned short, CW / 2>(w, buf, (unsigned short*)o.p + t * o.plane + m * o.stride + n, o.stride * 2,
+                                          rows, cols, o.vec);
     }
   }
 }
@@ -303,17 +308,27 @@ template <bool F32> struct RowBuffer {
     return (row * kPieces + (j ^ (row * kPieces / 8 % kPieces))) * 16;
   }
 };
-// Rows m ... m + rows of sixteen columns from column n on, on their way to such a buffer.
+// Rows m ... m + rows of sixteen columns from column n on, on their way to such a buffer: by 16 bytes
+// or, of 32-bit values whose rows start anywhere, one by one.
 template <bool F32>
 __device__ __forceinline__ void rows_ahead(char* buf, const Out& o, long long m, int n, int rows, int cols) {
   using B = RowBuffer<F32>;
   constexpr int SIZE = F32 ? 4 : 2;
-  const int lane = threadIdx.x & 31, j = lane % B::kPieces;
+  const int lane = threadIdx.x & 31;
+  if (!F32 || o.vec) {
+    const int j = lane % B::kPieces;
 #pragma unroll
-  for (int i = 0; i < B::kPieces; ++i) {
-    const int row = i * (32 / B::kPieces) + lane / B::kPieces, bytes = row < rows ? SIZE * cols - 16 * j : 0;
-    const char* src = (const char*)o.p + ((m + row) * o.stride + n) * SIZE + 16 * j;
-    copy_piece(smem_addr(buf + B::at(row, j)), bytes > 0 ? src : (const char*)o.p, bytes);
+    for (int i = 0; i < B::kPieces; ++i) {
+      const int row = i * (32 / B::kPieces) + lane / B::kPieces, bytes = row < rows ? SIZE * cols - 16 * j : 0;
+      const char* src = (const char*)o.p + ((m + row) * o.stride + n) * SIZE + 16 * j;
+      copy_piece(smem_addr(buf + B::at(row, j)), bytes > 0 ? src : (const char*)o.p, bytes);
+    }
+  } else {
+    const int e = lane % 16;
+    for (int row = lane / 16; row < rows; row += 2)
+      if (e < cols)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(buf + B::at(row, e / 4) + e % 4 * 4)),
+                     "l"((const float*)o.p + (m + row) * o.stride + n + e) : "memory");
   }
 }
 // Eight 16-bit values of 16 bytes.
@@ -346,6 +361,22 @@ __device__ __forceinline__ void row_of(float (&v)[16], const char* buf, bool bf1
 
 // Where 16-byte piece j of a row lies in a block of 128 rows of 64 bytes under TMA's 64-byte swizzle.
 __device__ __forceinline__ int block_at(int row, int j) { return row * 64 + ((j ^ ((row / 2) % 4)) * 16); }
+// Sixteen columns, from piece j on, of a block's rows first ... first + 31 to a matrix whose rows start
+// anywhere: consecutive lanes write consecutive elements.
+static __device__ __noinline__ void block_elements(const char* block, int first, int j, const Out& o, long long m, int n, int rows, int cols) {
+  const int lane = threadIdx.x & 31, e = lane % 16;
+  if (e >= cols) return;
+  unsigned short* to = (unsigned short*)o.p + m * o.stride + n + e;
+  for (int row0 = lane / 16; row0 < rows; row0 += 16) {
+    unsigned short v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      v[i] = *reinterpret_cast<const unsigned short*>(block + block_at(first + ((row0 + 2 * i) & 31), j + e / 8) + e % 8 * 2);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (row0 + 2 * i < rows) to[(row0 + 2 * i) * o.stride] = v[i];
+  }
+}
 __device__ __forceinline__ void put_block(char* block, int row, int j, const unsigned (&w)[8]) {
   *reinterpret_cast<uint4*>(block + block_at(row, j)) = make_uint4(w[0], w[1], w[2], w[3]);
   *reinterpret_cast<uint4*>(block + block_at(row, j + 1)) = make_uint4(w[4], w[5], w[6], w[7]);
@@ -606,6 +637,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
       const int row = quarter * 32 + lane;
       const bool bf16 = a.dtype == ABCD_BF16;
       const bool saved = EPI == kUp && a.g[0].p;
+      const bool saved_by_tma = saved && a.g[0].vec && a.g[1].vec;
       const bool elected = (warp - 2) % 8 == 0 && lane == 0;   // of the group
       const uint32_t empty0 = at_rank(sums_empty, 0);
       char* own = buffers + group * 3 * P::kBlockBytes;
@@ -673,6 +705,12 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
             put_block(own + P::kBlockBytes, row, 2 * half, x[1]);
             put_block(own + 2 * P::kBlockBytes, row, 2 * half, x[2]);
           }
+          if (saved && !saved_by_tma && ok) {
+            __syncwarp();
+            for (int k = 0; k < 2; ++k)
+              block_elements(own + (k + 1) * P::kBlockBytes, quarter * 32, 2 * half, a.g[k], m + quarter * 32, n0 + c,
+                             min(32, a.job[0].m - m - quarter * 32), min(16, a.job[0].n - n0 - c));
+          }
           smem_to_tma();
           named_barrier(1 + group, 256);
           if (elected && ok) {
@@ -682,7 +720,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
             if (EPI == kDown) {
               tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
               tma_store(&a.g_map[0], n, m, 1, from + 2 * P::kBlockBytes);
-            } else if (saved) {
+            } else if (saved_by_tma) {
               tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
               tma_store(&a.g_map[1], n, m, 0, from + 2 * P::kBlockBytes);
             }
@@ -717,7 +755,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
       p.cols = min(P::kWarpCols, a.job[it.job].n - p.n);
       return p;
     };
-    const bool ahead = P::kAhead && a.in[0].vec && a.in[1].vec;
+    const bool ahead = P::kAhead && (F32 || (a.in[0].vec && a.in[1].vec));
     // kDown: the saved projections of turn t of an item (16 columns), to one of two pairs of buffers
     char* saved = buffer + P::kTurn;
     constexpr int TURNS = P::kWarpCols / P::CW, SAVED = RowBuffer<F32>::kBytes;

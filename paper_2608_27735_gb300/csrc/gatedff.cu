@@ -86,28 +86,6 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackA
   }
 }
 
-// Two 16-bit operands of rows of 16-byte boundaries to matrices whose rows start anywhere.
-struct UnpackArgs {
-  const unsigned short* src[2];
-  unsigned short* dst[2];
-  long long rows, cols, pitch, stride[2];
-};
-__global__ void __launch_bounds__(256) unpack_kernel(const __grid_constant__ UnpackArgs a) {
-  pdl_wait();
-  const long long groups = (a.cols + 7) / 8, total = groups * a.rows;
-  const int k = blockIdx.y;
-  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < total; i += gridDim.x * 256LL) {
-    const long long row = i < (1LL << 32) ? (unsigned)i / (unsigned)groups : i / groups;
-    const int col = (int)(8 * (i - row * groups)), left = (int)(a.cols - col);
-    const uint4 v = *reinterpret_cast<const uint4*>(a.src[k] + row * a.pitch + col);
-    const unsigned w[4] = {v.x, v.y, v.z, v.w};
-    unsigned short* to = a.dst[k] + row * a.stride[k] + col;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < left) to[j] = (unsigned short)(w[j / 2] >> (16 * (j & 1)));
-  }
-}
-
 // The results of products whose k was split: their parts added in their order, rounded to the type of
 // the matrices; up to four results a launch.  A thread takes four columns of a row and a run of
 // consecutive parts; where the parts are many, a CTA's threads share them in two to eight runs, which
@@ -255,7 +233,7 @@ struct Job {
 // What the epilogues of kUp and kDown read and write besides.
 struct Hidden {
   int act;
-  Operand c, g[2], in[2];
+  Operand c, g[2], in[2];          // as operands where TMA moves them
   Out out[2], saved[2];            // the same as g and in
 };
 
@@ -299,7 +277,7 @@ void plan(int sms, int dtype, int epi, const Job* jobs, int n, int* shape, int* 
         }
         items += (double)tiles[k] * p[k];
       }
-      if (joined > 0) joined += 2.5;
+      if (joined > 0) joined += 4.0;                     // a launch more
       const double busy = std::min(1.0, items / (double)units), stage = q.idle + (q.busy - q.idle) * busy;
       double stages_last = 0;
       for (int k = 0; k < n; ++k) {
@@ -319,20 +297,6 @@ void plan(int sms, int dtype, int epi, const Job* jobs, int n, int* shape, int* 
       }
     }
   }
-}
-
-// Whether the epilogue of kUp or kDown moves the saved projections by TMA.
-bool by_blocks(const abcd_ctx* ctx, int dtype, int epi, long long m, long long n, long long k) {
-  if (dtype == ABCD_F32) return false;
-  int shape = 0, splits[kMaxJobs];
-  Job j{};
-  j.nb = 1;
-  j.m = m;
-  j.n = n;
-  j.k = k;
-  j.batches = 1;
-  plan(std::min(ctx->num_sms, kNetSms), dtype, epi, &j, 1, &shape, splits);
-  return shape == 0;
 }
 
 // Launches the products (and what joins their splits).
@@ -434,7 +398,7 @@ size_t ff_scratch(long long rows, long long cols, long long ff, int dtype) {
   s.operand(cols, ff, dtype);             // w_down
   s.operand(rows, ff, dtype);             // hidden
   s.operand(rows, ff, dtype, 2);          // dG, dU
-  if (dtype != ABCD_F32) s.operand(rows, ff, dtype, 2);   // gate, up
+  if (dtype != ABCD_F32) s.operand(rows, ff, dtype, 2);   // gate, up (backward)
   return s.at;
 }
 
@@ -506,9 +470,6 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
   if (needs_pack(w_up)) need.operand(f, d, t);
   if (needs_pack(w_down)) need.operand(d, f, t);
   need.operand(m, f, t);
-  // the saved projections by way of the workspace where TMA has to store them and cannot
-  const bool apart = gate && (needs_pack(gate) || needs_pack(up)) && by_blocks(ctx, t, kUp, m, f, d);
-  if (apart) need.operand(m, f, t, 2);
   abcd_status st = room(ctx, what, need.at);
   if (st != ABCD_OK) return st;
   Scratch s{ctx->net_base};
@@ -521,25 +482,16 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
   Hidden hid{};
   hid.act = activation;
   hid.c = h;
-  if (apart) {
-    const Operand saved = s.operand(m, f, t, 2);
-    hid.g[0] = Operand{saved.p, m, f, saved.pitch, 0, 1};
-    hid.g[1] = Operand{(unsigned short*)saved.p + saved.plane, m, f, saved.pitch, 0, 1};
-    for (int k = 0; k < 2; ++k) hid.out[k] = out_of(hid.g[k], 0, t);
-  } else if (gate) {
-    hid.g[0] = in_place(gate);
-    hid.g[1] = in_place(up);
+  if (gate) {
+    // TMA stores them where their rows allow it
+    if (!needs_pack(gate) && !needs_pack(up)) {
+      hid.g[0] = in_place(gate);
+      hid.g[1] = in_place(up);
+    }
     hid.out[0] = out_of(gate);
     hid.out[1] = out_of(up);
   }
   if ((st = run(ctx, t, kUp, &up_job, 1, &hid)) != ABCD_OK) return st;
-  if (apart) {
-    const UnpackArgs u{{(const unsigned short*)hid.g[0].p, (const unsigned short*)hid.g[1].p},
-                       {(unsigned short*)gate->data, (unsigned short*)up->data},
-                       m, f, hid.g[0].pitch, {gate->stride, up->stride}};
-    const dim3 grid((unsigned)std::min<long long>((m * ((f + 7) / 8) + 255) / 256, 8LL * ctx->num_sms), 2);
-    if ((st = check_launch(ctx, "unpack_kernel", launch_pdl(unpack_kernel, grid, dim3(256), 0, ctx->stream, u))) != ABCD_OK) return st;
-  }
   const Job y_job{h, {od}, 1, false, false, m, d, f, 1, {out_of(y)}};
   return run(ctx, t, kPlain, &y_job, 1);
 }

@@ -6,12 +6,11 @@
 // from zero costs it no digits.
 //
 // Bound by HBM (forward x -> y, backward x, dy -> dx).  A row is read once: TPR lanes (part of a
-// warp, a warp, or a CTA) hold it in registers, NV accesses of V consecutive elements each, V = 16
-// bytes where the rows lie on 16-byte boundaries and one element where they do not; rows too long
-// for that are read again from L2.  A group of lanes takes many rows: the weights (and backward dw
+// warp, a warp, or a CTA) hold it in registers, NV vectors of V consecutive elements (16 bytes) each;
+// rows too long for that are read again from L2.  A group of lanes takes many rows: the weights (and backward dw
 // and db of its own columns) stay in registers, and the next rows are copied to shared memory
-// meanwhile (cp.async, each thread its own bytes, so no barrier is needed), which keeps the loads in
-// flight that the few warps of so many registers could not.  The CTAs' sums go to the workspace and a
+// meanwhile (cp.async), which keeps the loads in flight that the few warps of so many registers could
+// not.  The CTAs' sums go to the workspace and a
 // second kernel adds them in their order.
 #include <algorithm>
 #include <type_traits>
@@ -38,19 +37,22 @@ struct NormArgs {
   int wide_w;                         // weight and bias are fp32 whatever the matrices' type
 };
 
-// How a row lies over threads, forward (one matrix is read) and backward (two).
-template <int TPR_, int V_, int NV_, bool BWD> struct RowShape {
+// How a row lies over threads, forward (one matrix is read) and backward (two); SHIFT: rows that
+// start anywhere.
+template <int TPR_, int V_, int NV_, bool BWD, bool SHIFT> struct RowShape {
   static constexpr int TPR = TPR_, V = V_, NV = NV_;
+  static constexpr bool kShift = SHIFT;
   static constexpr int kThreads = TPR > 256 ? TPR : 256;
   static constexpr int kGroups = kThreads / TPR;          // rows of a CTA at a time
   static constexpr int kCapacity = TPR * V * NV;
   // Shared memory: four rows of each matrix per group (three where four leave no room for a second
-  // CTA; none are copied ahead element by element), and, backward, the sums of the CTA's columns at
-  // its end.
+  // CTA), a row as its vectors (and one more, which a row that starts between two reaches into), and,
+  // backward, the sums of the CTA's columns at its end.
   static constexpr int kMats = BWD ? 2 : 1;
-  static constexpr size_t kAhead = (size_t)kMats * NV * kThreads * 16;
+  static constexpr int kRowBytes = (TPR * NV + (SHIFT ? 1 : 0)) * 16;
+  static constexpr size_t kAhead = (size_t)kMats * kGroups * kRowBytes;
   static constexpr int kDepth = 4 * kAhead > 100 * 1024 ? 3 : 4;
-  static constexpr size_t kRing = V > 1 ? kDepth * kAhead : 0, kSums = BWD ? (size_t)2 * kCapacity * 4 : 0;
+  static constexpr size_t kRing = kDepth * kAhead, kSums = BWD ? (size_t)2 * kCapacity * 4 : 0;
   static constexpr size_t kSmem = kRing > kSums ? kRing : kSums;
   // CTAs per SM that the grid offers: as many as their registers (and rows) leave room for
   static constexpr int kCtas = kThreads > 256 || kSmem > 100 * 1024 ? 1 : V * NV > 8 ? 2 : 4;
@@ -133,20 +135,37 @@ __device__ __forceinline__ void copy16(void* dst, const void* src, int bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(bytes < 16 ? bytes : 16) : "memory");
 }
 
-// The rows that a group of TPR threads takes one after another, their next ones on the way: each
-// thread copies its own bytes of the matrices to its own 16-byte slots [depth][matrix][NV][thread].
+// The threads of a row meet.
+template <int TPR> __device__ __forceinline__ void row_sync() {
+  if constexpr (TPR <= 32) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / TPR), "n"(TPR) : "memory");
+}
+
+// The rows that a group of TPR threads takes one after another, their next ones on the way to shared
+// memory [depth][matrix][group][vectors of 16 bytes].
+//
+// Rows on 16-byte boundaries: each thread copies the vectors that it will use itself, so nobody waits
+// for another.  Rows that start anywhere (SHIFT): the 16-byte pieces that they reach into are copied,
+// the group meets, and each thread puts its vectors together from two pieces.  A piece then also holds
+// up to 14 bytes of what lies before or behind the row in its matrix; pieces that reach outside the
+// matrix (of its first and last row) are copied element by element.
 template <typename T, typename R> struct RowRing {
   static constexpr int kDepth = R::kDepth;
-  char* slots;                        // the thread's first slot
-  const T* src[R::kMats];             // where the thread's first vector of the next row to fetch lies
+  char* slots;                        // the group's first slot
+  const T* src[R::kMats];             // the start of the next row to fetch
+  const char* lowest[R::kMats];       // the matrices' first bytes, and the ones behind their last
+  const char* highest[R::kMats];
   long long jump[R::kMats];           // elements from one of the group's rows to its next
   int rows, turns;                    // the group's rows; turns of the CTA, alike in all its groups
+  int cols, lane;
   int left;                           // elements of a row from the thread's first vector on
 
   __device__ __forceinline__ RowRing(char* smem, const NormArgs& a) {
-    const int lane = threadIdx.x % R::TPR;
-    const long long first = (long long)blockIdx.x * R::kGroups + threadIdx.x / R::TPR, step = (long long)gridDim.x * R::kGroups;
-    slots = smem + threadIdx.x * 16;
+    const int group = threadIdx.x / R::TPR;
+    const long long first = (long long)blockIdx.x * R::kGroups + group, step = (long long)gridDim.x * R::kGroups;
+    lane = threadIdx.x % R::TPR;
+    cols = a.cols;
+    slots = smem + group * R::kRowBytes;
     left = a.cols - lane * R::V;
     rows = first < a.rows ? (int)((a.rows - first + step - 1) / step) : 0;
     turns = (int)((a.rows - (long long)blockIdx.x * R::kGroups + step - 1) / step);
@@ -154,29 +173,45 @@ template <typename T, typename R> struct RowRing {
     const long long stride[2] = {a.sx, a.sdy};
 #pragma unroll
     for (int q = 0; q < R::kMats; ++q) {
-      src[q] = base[q] + first * stride[q] + lane * R::V;
+      src[q] = base[q] + first * stride[q];
       jump[q] = step * stride[q];
+      lowest[q] = (const char*)base[q];
+      highest[q] = (const char*)(base[q] + (a.rows - 1) * stride[q] + a.cols);
     }
   }
-  __device__ __forceinline__ char* slot(int t, int mat, int j) const {
-    return slots + ((t % kDepth * R::kMats + mat) * R::NV + j) * R::kThreads * 16;
+  __device__ __forceinline__ char* slot(int t, int mat) const {
+    return slots + (t % kDepth * R::kMats + mat) * R::kGroups * R::kRowBytes;
+  }
+  // Piece i of a row that starts anywhere.
+  __device__ __forceinline__ void piece(int t, int q, int i) const {
+    const char* begin = (const char*)src[q];
+    const char* from = begin - ((uintptr_t)begin & 15) + 16 * i;
+    const char* end = (const char*)(src[q] + cols);
+    if (from >= end) return;
+    char* to = slot(t, q) + 16 * i;
+    if (from >= lowest[q] && from + 16 <= highest[q]) {
+      copy16(to, from, 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; e += (int)sizeof(T))
+        if (from + e >= begin && from + e < end) *reinterpret_cast<T*>(to + e) = *reinterpret_cast<const T*>(from + e);
+    }
   }
   __device__ __forceinline__ void fetch(int t) {
-    if constexpr (R::V > 1) {
-      if (t < rows) {
+    if (t < rows) {
+#pragma unroll
+      for (int q = 0; q < R::kMats; ++q) {
 #pragma unroll
         for (int j = 0; j < R::NV; ++j) {
           const int n = left - j * R::TPR * R::V;
-          if (n > 0) {
-#pragma unroll
-            for (int q = 0; q < R::kMats; ++q) copy16(slot(t, q, j), src[q] + j * R::TPR * R::V, n < R::V ? n * (int)sizeof(T) : 16);
-          }
+          if constexpr (R::kShift) piece(t, q, j * R::TPR + lane);
+          else if (n > 0) copy16(slot(t, q) + (j * R::TPR + lane) * 16, src[q] + lane * R::V + j * R::TPR * R::V, n < R::V ? n * (int)sizeof(T) : 16);
         }
-#pragma unroll
-        for (int q = 0; q < R::kMats; ++q) src[q] += jump[q];
+        if (R::kShift && lane == 0) piece(t, q, R::NV * R::TPR);
+        src[q] += jump[q];
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   }
   __device__ __forceinline__ void start() {
 #pragma unroll
@@ -184,23 +219,67 @@ template <typename T, typename R> struct RowRing {
   }
   // Asks for the row kDepth - 1 turns on and waits for the one of turn t.
   __device__ __forceinline__ void turn(int t) {
+    if constexpr (R::kShift) row_sync<R::TPR>();       // the last turn's row is done with
     fetch(t + kDepth - 1);
-    if constexpr (R::V > 1) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+    if constexpr (R::kShift) row_sync<R::TPR>();
   }
-  // Vector j of the turn's row of a matrix; zeros past its end.
-  __device__ __forceinline__ void get(float (&v)[R::V], int t, int mat, int j) const {
-    const int n = t < rows ? left - j * R::TPR * R::V : 0;
-    if constexpr (R::V > 1) {
-      load_vec<T, R::V>(v, (const T*)slot(t, mat, j), n > 0 ? R::V : 0);
+  // Vector j of the turn's row of a matrix (at: where the row starts); zeros past its end.
+  __device__ __forceinline__ void get(float (&v)[R::V], int t, int mat, int j, const T* at) const {
+    const int n = t < rows ? left - j * R::TPR * R::V : 0, c = (j * R::TPR + lane) * R::V;
+    if constexpr (!R::kShift) {
+      load_vec<T, R::V>(v, (const T*)(slot(t, mat) + c * sizeof(T)), n > 0 ? R::V : 0);
     } else {
-      load_vec<T, R::V>(v, src[mat] + j * R::TPR * R::V, n);
+      const int p = (int)((uintptr_t)at & 15) + c * (int)sizeof(T);
+      const unsigned* w = reinterpret_cast<const unsigned*>(slot(t, mat) + (p & ~3));
+      unsigned u[5];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) u[i] = n > 0 && (i < 4 || (p & 2)) ? w[i] : 0u;
+      if (p & 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = u[i] >> 16 | u[i + 1] << 16;
+      }
+      Pack<T, R::V> q;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) reinterpret_cast<unsigned*>(&q)[i] = u[i];
+#pragma unroll
+      for (int i = 0; i < R::V; ++i) v[i] = i < n ? to_f32(q.v[i]) : 0.f;
     }
   }
-  // After a turn (rows that are not copied ahead are read where src stands).
-  __device__ __forceinline__ void next() {
-    if constexpr (R::V == 1) {
+  // The turn's row of results to `to`: each thread puts its vectors' values, then all store pieces.
+  __device__ __forceinline__ void put(const float (&v)[R::V], int t, int j, T* to) const {
+    const int c = (j * R::TPR + lane) * R::V, n = t < rows ? left - j * R::TPR * R::V : 0;
+    if (n <= 0) return;
+    if constexpr (!R::kShift) {
+      store_vec<T, R::V>(to + c, v, n);
+    } else {
+      T* s = reinterpret_cast<T*>(slot(t, 0) + ((uintptr_t)to & 15)) + c;
 #pragma unroll
-      for (int q = 0; q < R::kMats; ++q) src[q] += jump[q];
+      for (int i = 0; i < R::V; ++i) s[i] = from_f32<T>(v[i]);     // the row's place has room for a vector more
+    }
+  }
+  __device__ __forceinline__ void flush(int t, T* to) const {
+    if constexpr (R::kShift) {
+      row_sync<R::TPR>();
+      if (t >= rows) return;
+      char* begin = (char*)to;
+      char* end = (char*)(to + cols);
+      char* base = begin - ((uintptr_t)begin & 15);
+      const char* s = slot(t, 0);
+#pragma unroll
+      for (int j = 0; j <= R::NV; ++j) {
+        const int i = j * R::TPR + lane;
+        if (j == R::NV && lane > 0) break;
+        char* at = base + 16 * i;
+        if (at >= end) break;
+        if (at >= begin && at + 16 <= end) {
+          *reinterpret_cast<uint4*>(at) = *reinterpret_cast<const uint4*>(s + 16 * i);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; e += (int)sizeof(T))
+            if (at + e >= begin && at + e < end) *reinterpret_cast<T*>(at + e) = *reinterpret_cast<const T*>(s + 16 * i + e);
+        }
+      }
     }
   }
 };
@@ -224,17 +303,17 @@ __global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_cons
   const float inv = 1.f / (float)a.cols;
   const long long step = (long long)gridDim.x * R::kGroups;
   long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR;
-  T* y = (T*)a.y + r * a.sy + lane * V;
-  for (int t = 0; t < ring.turns; ++t, r += step, y += step * a.sy) {
+  const T* x = (const T*)a.x + r * a.sx;
+  T* y = (T*)a.y + r * a.sy;
+  for (int t = 0; t < ring.turns; ++t, r += step, x += step * a.sx, y += step * a.sy) {
     ring.turn(t);
     float v[NV][V], s = 0.f, q = 0.f, unused = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      ring.get(v[j], t, 0, j);
+      ring.get(v[j], t, 0, j, x);
 #pragma unroll
       for (int i = 0; i < V; ++i) s += v[j][i];
     }
-    ring.next();
     row_sum2<TPR>(s, unused, red, 0);
     const float mean = s * inv;
 #pragma unroll
@@ -252,15 +331,14 @@ __global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_cons
     }
     row_sum2<TPR>(q, unused, red, 1);
     const float rstd = rsqrtf(q * inv + a.eps);
-    if (t >= ring.rows) continue;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int left = ring.left - j * TPR * V;
-      if (left <= 0) break;
 #pragma unroll
       for (int i = 0; i < V; ++i) v[j][i] = v[j][i] * rstd * w[j][i] + b[j][i];
-      store_vec<T, V>(y + j * TPR * V, v[j], left);
+      ring.put(v[j], t, j, y);
     }
+    ring.flush(t, y);
+    if (t >= ring.rows) continue;
     if (a.mean && lane == 0) {
       a.mean[r] = mean;
       a.rstd[r] = rstd;
@@ -286,14 +364,16 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
   const float inv = 1.f / (float)a.cols;
   const long long step = (long long)gridDim.x * R::kGroups;
   long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / TPR;
-  T* dx = (T*)a.y + r * a.sy + lane * V;
+  const T* x = (const T*)a.x + r * a.sx;
+  const T* dy = (const T*)a.dy + r * a.sdy;
+  T* dx = (T*)a.y + r * a.sy;
   const T* res = (const T*)a.res + r * a.sres + lane * V;
   // mean and rstd of the rows come two turns ahead too
   auto stat_of = [&](int t, long long row) {
     return t < ring.rows ? make_float2(__ldg(a.mean + row), __ldg(a.rstd + row)) : make_float2(0.f, 0.f);
   };
   float2 stat[2] = {stat_of(0, r), stat_of(1, r + step)};
-  for (int t = 0; t < ring.turns; ++t, r += step, dx += step * a.sy, res += step * a.sres) {
+  for (int t = 0; t < ring.turns; ++t, r += step, x += step * a.sx, dy += step * a.sdy, dx += step * a.sy, res += step * a.sres) {
     ring.turn(t);
     const bool in = t < ring.rows;
     const float rstd = stat[0].y, shift = -stat[0].x * rstd;
@@ -303,8 +383,8 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
     float xh[NV][V], g[NV][V], s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      ring.get(xh[j], t, 0, j);
-      ring.get(g[j], t, 1, j);
+      ring.get(xh[j], t, 0, j, x);
+      ring.get(g[j], t, 1, j, dy);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         xh[j][i] = xh[j][i] * rstd + shift;
@@ -315,26 +395,30 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
         s2 += g[j][i] * xh[j][i];
       }
     }
-    ring.next();
     row_sum2<TPR>(s1, s2, red, t & 1);
     s1 *= -inv * rstd;
     s2 *= -inv * rstd;
-    if (a.y && in) {
+    if (a.y) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int left = ring.left - j * TPR * V;
-        if (left <= 0) break;
+        const int left = in ? ring.left - j * TPR * V : 0;
         float v[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = xh[j][i] * s2 + (rstd * g[j][i] + s1);
-        if (a.res) {
+        if (a.res && left > 0) {
           float add[V];
-          load_vec<T, V>(add, res + j * TPR * V, left);
+          if constexpr (R::kShift) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) add[i] = i < left ? to_f32(res[j * TPR * V + i]) : 0.f;
+          } else {
+            load_vec<T, V>(add, res + j * TPR * V, left);
+          }
 #pragma unroll
           for (int i = 0; i < V; ++i) v[i] += add[i];
         }
-        store_vec<T, V>(dx + j * TPR * V, v, left);
+        ring.put(v, t, j, dx);
       }
+      ring.flush(t, dx);
     }
   }
   // the CTA's sums: rows that share a warp by shuffles, then the warps of a column one after another
@@ -473,24 +557,21 @@ constexpr int kNormCtasPerSm = 4;
 // 32 elements a thread forward (with as many weights and biases) and 16 backward (with as many
 // weights and sums); f of an int where none does.  Backward, 100,000 x 1,024 bf16 with 32 elements a
 // thread (eight warps per SM) took 164 us.
-template <typename T, bool BWD, typename F> abcd_status with_shape(long long cols, bool aligned, F&& f) {
-  if (aligned) {
-    constexpr int V = 16 / sizeof(T), N = (BWD ? 16 : 32) / V;   // accesses of 16 bytes per thread
-    if (cols <= 8 * V) return f(RowShape<8, V, 1, BWD>());
-    if (cols <= 16 * V) return f(RowShape<16, V, 1, BWD>());
-    if (cols <= 32 * V) return f(RowShape<32, V, 1, BWD>());
-    if (cols <= 64 * V) return f(RowShape<32, V, 2, BWD>());
-    if (cols <= 32 * V * N) return f(RowShape<32, V, N, BWD>());
-    if (cols <= 64 * V * N) return f(RowShape<64, V, N, BWD>());
-    if (cols <= 256 * V * N) return f(RowShape<256, V, N, BWD>());
-    if (cols <= 512 * V * N) return f(RowShape<512, V, N, BWD>());
-  } else {
-    if (cols <= 64) return f(RowShape<32, 1, 2, BWD>());
-    if (cols <= 256) return f(RowShape<32, 1, 8, BWD>());
-    if (cols <= 2048) return f(RowShape<256, 1, 8, BWD>());
-    if (cols <= 8192) return f(RowShape<1024, 1, 8, BWD>());
-  }
+template <typename T, bool BWD, bool SHIFT, typename F> abcd_status with_shape(long long cols, F&& f) {
+  constexpr int V = 16 / sizeof(T), N = (BWD ? 16 : 32) / V;   // vectors of 16 bytes per thread
+  if (cols <= 8 * V) return f(RowShape<8, V, 1, BWD, SHIFT>());
+  if (cols <= 16 * V) return f(RowShape<16, V, 1, BWD, SHIFT>());
+  if (cols <= 32 * V) return f(RowShape<32, V, 1, BWD, SHIFT>());
+  if (cols <= 64 * V) return f(RowShape<32, V, 2, BWD, SHIFT>());
+  if (cols <= 32 * V * N) return f(RowShape<32, V, N, BWD, SHIFT>());
+  if (cols <= 64 * V * N) return f(RowShape<64, V, N, BWD, SHIFT>());
+  if (cols <= 128 * V * N) return f(RowShape<128, V, N, BWD, SHIFT>());
+  if (cols <= 256 * V * N) return f(RowShape<256, V, N, BWD, SHIFT>());
+  if (cols <= 512 * V * N) return f(RowShape<512, V, N, BWD, SHIFT>());
   return f(0);
+}
+template <typename T, bool BWD, typename F> abcd_status with_shape(long long cols, bool aligned, F&& f) {
+  return aligned ? with_shape<T, BWD, false>(cols, f) : with_shape<T, BWD, true>(cols, f);
 }
 
 abcd_status room_for(abcd_ctx* ctx, const void* kernel, size_t smem) {
