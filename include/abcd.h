@@ -123,7 +123,8 @@ const char* abcd_last_error(const abcd_ctx* ctx);
 /* Number of kernels this context has launched since creation (instrumentation). */
 long long abcd_launch_count(const abcd_ctx* ctx);
 /* Bound on the polls of a device-side wait (the radix sort's decoupled look-back waits for the
- * tiles before its own, whose CTAs are already running) [2^20, about 40 ms]: a wait that
+ * tiles before its own, whose CTAs are already running; the gated feed-forward products' warps wait for
+ * one another's stages) [2^20, about 40 ms]: a wait that
  * reaches it gives up, the call's results are wrong and ABCD_ERR_TIMEOUT is set in the status
  * word (abcd_sync); nothing hangs, and later calls run normally once the status is cleared. */
 abcd_status abcd_set_wait_limit(abcd_ctx* ctx, unsigned polls);
@@ -499,7 +500,8 @@ abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix* dy, const
 /* Gated feed-forward layer: y = (act(x w_gate^T) * (x w_up^T)) w_down^T.  x, y [rows][d];
  * w_gate, w_up [ff][d]; w_down [d][ff]; all of one type.  gate, up [rows][ff], both NULL or both
  * given: x w_gate^T and x w_up^T, which the backward pass reads.  The hidden matrix
- * act(gate) * up is rounded to the matrices' type between the two products. */
+ * act(gate) * up is rounded to the matrices' type between the two products.  In 32 bits a factor is
+ * taken as three 16-bit terms (24 bits together), so one beyond 3.38e38 or infinite gives NaN. */
 abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const abcd_matrix* w_gate,
                           const abcd_matrix* w_up, const abcd_matrix* w_down, int activation,
                           const abcd_matrix* y, const abcd_matrix* gate, const abcd_matrix* up);

@@ -152,11 +152,14 @@ __device__ __forceinline__ unsigned pack2(float a, float b, bool bf16) {
 __device__ __forceinline__ float unpack(unsigned short v, bool bf16) {
   return bf16 ? __uint_as_float((unsigned)v << 16) : __half2float(__ushort_as_half(v));
 }
-// The next 16-bit term of v, which is left with the rest (nothing of an infinity or NaN).
-__device__ __forceinline__ float take_term(float& v) {
-  const float t = __bfloat162float(__float2bfloat16_rn(v));
-  v = fabsf(v) <= 3.4028234e38f && fabsf(t) <= 3.4028234e38f ? v - t : 0.f;
-  return t;
+// The next 16-bit terms of two 32-bit values as a pair, and the values with what they leave.  (Of an
+// infinity NaN is left, and NaN is what a product with it gives: with the exact rest, none, it would
+// be so too, wherever a lower term of the other factor is zero.)
+__device__ __forceinline__ unsigned take_terms(float& a, float& b) {
+  const unsigned w = pack2(a, b, true);
+  a -= __uint_as_float(w << 16);
+  b -= __uint_as_float(w & 0xffff0000u);
+  return w;
 }
 
 // Pairs of v as 16-bit values.
@@ -250,10 +253,7 @@ __device__ __forceinline__ void store_operand(const float (&v)[CW], const Out& o
     for (int t = 0; t < 3; ++t) {
       unsigned w[CW / 2];
 #pragma unroll
-      for (int i = 0; i < CW / 2; ++i) {
-        const float a = take_term(rest[2 * i]), b = take_term(rest[2 * i + 1]);
-        w[i] = pack2(a, b, true);
-      }
+      for (int i = 0; i < CW / 2; ++i) w[i] = take_terms(rest[2 * i], rest[2 * i + 1]);
       store_words<unsigned short, CW / 2>(w, buf, (unsigned short*)o.p + t * o.plane + m * o.stride + n, o.stride * 2,
                                           rows, cols, o.vec);
     }

@@ -67,10 +67,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackA
       for (int t = 0; t < 3; ++t) {
         unsigned w[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float lo = take_term(v[2 * j]), hi = take_term(v[2 * j + 1]);
-          w[j] = pack2(lo, hi, true);
-        }
+        for (int j = 0; j < 4; ++j) w[j] = take_terms(v[2 * j], v[2 * j + 1]);
         *reinterpret_cast<uint4*>(dst + t * o.plane) = make_uint4(w[0], w[1], w[2], w[3]);
       }
     } else {
@@ -246,7 +243,12 @@ int segments_of(const Job& j, int epi, int dtype) {
 // the CTAs in turn, so that the last wave is partly idle.  Splits bring the products' items near one
 // size: the whole work's share of a CTA, or a part of it.  Their joining writes and reads the sums
 // through L2.
-void plan(int sms, int dtype, int epi, const Job* jobs, int n, int* shape, int* splits) {
+struct Plan {
+  int shape, splits[kMaxJobs];
+};
+Plan plan(int sms, int dtype, int epi, const Job* jobs, int n) {
+  Plan found{0, {1, 1, 1}};
+  sms = std::min(sms, kNetSms);
   const bool f32 = dtype == ABCD_F32;
   double best = 1e300;
   for (int s = 0; s < 3; ++s) {
@@ -277,7 +279,8 @@ void plan(int sms, int dtype, int epi, const Job* jobs, int n, int* shape, int* 
         }
         items += (double)tiles[k] * p[k];
       }
-      if (joined > 0) joined += 4.0;                     // a launch more
+      // a launch more, or the last warps' reading of part after part
+      if (joined > 0) joined += epi == kPlain ? 4.0 : 1.5 + 0.4 * p[0];
       const double busy = std::min(1.0, items / (double)units), stage = q.idle + (q.busy - q.idle) * busy;
       double stages_last = 0;
       for (int k = 0; k < n; ++k) {
@@ -292,19 +295,20 @@ void plan(int sms, int dtype, int epi, const Job* jobs, int n, int* shape, int* 
       t += q.fixed + stages_last + joined;
       if (t < best) {
         best = t;
-        *shape = s;
-        for (int k = 0; k < n; ++k) splits[k] = p[k];
+        found.shape = s;
+        for (int k = 0; k < n; ++k) found.splits[k] = p[k];
       }
     }
   }
+  return found;
 }
 
 // Launches the products (and what joins their splits).
-abcd_status run(abcd_ctx* ctx, int dtype, int epi, const Job* jobs, int n, const Hidden* hidden = nullptr) {
+abcd_status run(abcd_ctx* ctx, int dtype, int epi, const Job* jobs, int n, const Plan& planned, const Hidden* hidden = nullptr) {
   ProductArgs a{};
   const int terms = terms_of(dtype);
-  int shape = 0, splits[kMaxJobs];
-  plan(std::min(ctx->num_sms, kNetSms), dtype, epi, jobs, n, &shape, splits);
+  const int shape = planned.shape;
+  const int* splits = planned.splits;
   const int cg = kShapes[shape].cg, bn = kShapes[shape].bn, cols = epi == kUp ? bn / 2 : bn;
   a.jobs = n;
   a.dtype = dtype;
@@ -398,7 +402,7 @@ size_t ff_scratch(long long rows, long long cols, long long ff, int dtype) {
   s.operand(cols, ff, dtype);             // w_down
   s.operand(rows, ff, dtype);             // hidden
   s.operand(rows, ff, dtype, 2);          // dG, dU
-  if (dtype != ABCD_F32) s.operand(rows, ff, dtype, 2);   // gate, up (backward)
+  for (int k = 0; k < 2 && dtype != ABCD_F32; ++k) s.operand(rows, ff, dtype);   // gate, up (backward)
   return s.at;
 }
 
@@ -491,9 +495,9 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
     hid.out[0] = out_of(gate);
     hid.out[1] = out_of(up);
   }
-  if ((st = run(ctx, t, kUp, &up_job, 1, &hid)) != ABCD_OK) return st;
+  if ((st = run(ctx, t, kUp, &up_job, 1, plan(ctx->num_sms, t, kUp, &up_job, 1), &hid)) != ABCD_OK) return st;
   const Job y_job{h, {od}, 1, false, false, m, d, f, 1, {out_of(y)}};
-  return run(ctx, t, kPlain, &y_job, 1);
+  return run(ctx, t, kPlain, &y_job, 1, plan(ctx->num_sms, t, kPlain, &y_job, 1));
 }
 
 extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* dy,
@@ -567,21 +571,33 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
   hid.out[1] = out_of(dgu, 1, t);
   hid.saved[0] = apart ? out_of(ogate, 0, t) : out_of(gate);
   hid.saved[1] = apart ? out_of(oup, 0, t) : out_of(up);
-  if ((st = run(ctx, t, kDown, &down, 1, &hid)) != ABCD_OK) return st;
-  // what is left does not depend on one another: one launch
+  if ((st = run(ctx, t, kDown, &down, 1, plan(ctx->num_sms, t, kDown, &down, 1), &hid)) != ABCD_OK) return st;
+  // what is left does not depend on one another: one launch, planned as for all of it, so that no
+  // gradient depends on which others are asked for
+  const Job all[kMaxJobs] = {Job{dgu, {og, ou}, 2, false, true, m, d, f, 1, {}},
+                             Job{dgu, {ox}, 1, true, true, f, d, m, 2, {}},      // dG^T x, dU^T x
+                             Job{ody, {h}, 1, true, true, d, f, m, 1, {}}};
+  const Plan whole = plan(ctx->num_sms, t, kPlain, all, kMaxJobs);
+  Plan part{whole.shape, {1, 1, 1}};
   Job jobs[kMaxJobs];
   int n = 0;
-  if (dx) jobs[n++] = Job{dgu, {og, ou}, 2, false, true, m, d, f, 1, {out_of(dx)}};
+  const auto take = [&](int k) -> Job& {
+    part.splits[n] = whole.splits[k];
+    jobs[n] = all[k];
+    return jobs[n++];
+  };
+  if (dx) take(0).c[0] = out_of(dx);
   if (dw_gate || dw_up) {
-    // dG^T x and dU^T x: the second starts at dU's planes
-    const bool both = dw_gate && dw_up;
-    Operand left = dgu;
-    if (!dw_gate) left.p = (const unsigned short*)dgu.p + (long long)terms_of(t) * dgu.plane;
-    left.planes = both ? dgu.planes : terms_of(t);
-    jobs[n] = Job{left, {ox}, 1, true, true, f, d, m, both ? 2 : 1, {out_of(dw_gate ? dw_gate : dw_up)}};
-    if (both) jobs[n].c[1] = out_of(dw_up);
-    ++n;
+    Job& j = take(1);
+    j.c[0] = out_of(dw_gate ? dw_gate : dw_up);
+    if (dw_gate && dw_up) {
+      j.c[1] = out_of(dw_up);
+    } else {                                       // one of them: dU's planes are the second half
+      if (!dw_gate) j.a.p = (const unsigned short*)dgu.p + (long long)terms_of(t) * dgu.plane;
+      j.a.planes = terms_of(t);
+      j.batches = 1;
+    }
   }
-  if (dw_down) jobs[n++] = Job{ody, {h}, 1, true, true, d, f, m, 1, {out_of(dw_down)}};
-  return n ? run(ctx, t, kPlain, jobs, n) : ABCD_OK;
+  if (dw_down) take(2).c[0] = out_of(dw_down);
+  return n ? run(ctx, t, kPlain, jobs, n, part) : ABCD_OK;
 }

@@ -390,6 +390,113 @@ def test_refusals(ctx):
     ab.abcd_gated_ff(fresh, x, wg, wg, wd, "silu", y)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,d,f", [(1, 1, 1), (9, 3, 5), (77, 59, 130), (130, 250, 999), (64, 520, 136)])
+def test_the_reserved_workspace_is_enough(kind, rows, d, f):
+    """A context that reserved for these very sizes takes them, whatever the rows' starts."""
+    c = ab.Context(0)
+    c.reserve_network(rows, d, f, TYPES[kind])
+    r = np.random.default_rng(1)
+    for pad, lead in ((0, 0), (3, 1)):
+        x = matrix(r.normal(size=(rows, d)), kind, pad, lead)
+        wg, wu, wd = ff_weights(r, d, f, kind, pad, lead)
+        gate, up = blank(rows, f, kind, pad, lead), blank(rows, f, kind, pad, lead)
+        ab.abcd_gated_ff(c, x, wg, wu, wd, "relu", x.clone(), gate, up)
+        ab.abcd_gated_ff_backward(c, x, x, wg, wu, wd, "relu", gate, up, x.clone(), wg.clone(), wu.clone(), wd.clone())
+        ab.abcd_layer_norm_backward(c, x, x, None, torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda"),
+                                    x.clone(), torch.zeros(d, dtype=x.dtype, device="cuda"))
+    c.sync()
+
+
+# ---- streams, graphs, waits
+
+def everything(ctx, x, dy, w, wg, wu, wd, out):
+    """Every call once, on the context's stream."""
+    y, gate, up, nx, dn, dx, mean, rstd, dw, db, g = out
+    ab.abcd_layer_norm(ctx, x, w, w, 1e-5, nx, mean, rstd)
+    ab.abcd_gated_ff(ctx, nx, wg, wu, wd, "silu", y, gate, up)
+    ab.abcd_dropout(ctx, y, 0.25, 9, 4, y, x)
+    ab.abcd_dropout_backward(ctx, dy, 0.25, 9, 4, dn)
+    ab.abcd_gated_ff_backward(ctx, dn, nx, wg, wu, wd, "silu", gate, up, dx, *g)
+    ab.abcd_layer_norm_backward(ctx, dx, x, w, mean, rstd, dx, dw, db, dy)
+
+
+def make_everything(n, d, f, kind, seed):
+    r = np.random.default_rng(seed)
+    x, dy = matrix(r.normal(size=(n, d)), kind), matrix(r.normal(size=(n, d)), kind)
+    w = torch.as_tensor(r.normal(1, 0.2, d)).to("cuda", TYPES[kind])
+    weights = ff_weights(r, d, f, kind, 0, 0)
+    out = (blank(n, d, kind), blank(n, f, kind), blank(n, f, kind), blank(n, d, kind), blank(n, d, kind),
+           blank(n, d, kind), torch.empty(n, device="cuda"), torch.empty(n, device="cuda"),
+           torch.empty_like(w), torch.empty_like(w), [blank(f, d, kind), blank(f, d, kind), blank(d, f, kind)])
+    return (x, dy, w, *weights), out
+
+
+def flat(out):
+    return [t.clone() for t in (*out[:-1], *out[-1])]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,d,f", [(1, 64, 128), (77, 59, 130), (700, 264, 520)])
+def test_other_streams_and_captured_graphs(ctx, kind, n, d, f):
+    """The same results on a stream of the context's own, and from a captured graph replayed on other
+    inputs."""
+    args, out = make_everything(n, d, f, kind, 20)
+    ctx.reserve_network(n, d, f, TYPES[kind])
+    everything(ctx, *args, out)
+    ctx.sync()
+    want = flat(out)
+    stream = torch.cuda.Stream()
+    side = ab.Context(0, stream)
+    side.reserve_network(n, d, f, TYPES[kind])
+    with torch.cuda.stream(stream):
+        stream.wait_stream(torch.cuda.default_stream())
+        for t in (*out[:-1], *out[-1]):
+            t.fill_(float("nan"))
+        everything(side, *args, out)
+    side.sync()
+    assert all(torch.equal(a, b) for a, b in zip(flat(out), want))
+    other, _ = make_everything(n, d, f, kind, 21)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        everything(side, *args, out)
+    everything(ctx, *other, out)
+    ctx.sync()
+    want = flat(out)
+    torch.cuda.synchronize()
+    for a, b in zip(args, other):
+        a.copy_(b)
+    for t in (*out[:-1], *out[-1]):
+        t.fill_(float("nan"))
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(flat(out), want))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,d,f", [(77, 64, 130), (3001, 72, 1032)])
+def test_a_wait_that_runs_out_is_reported(kind, n, d, f):
+    """With no polls allowed every wait of the products gives up at once: the calls end, the status
+    says so, and once it is cleared the calls are right again."""
+    args, out = make_everything(n, d, f, kind, 22)
+    c = ab.Context(0)
+    c.reserve_network(n, d, f, TYPES[kind])
+    everything(c, *args, out)
+    c.sync()
+    want = flat(out)
+    assert ab.lib().abcd_set_wait_limit(c.h, 0) == ab.ABCD_OK
+    x, dy, w, wg, wu, wd = args
+    ab.abcd_gated_ff(c, x, wg, wu, wd, "silu", out[0], out[1], out[2])
+    ab.abcd_gated_ff_backward(c, dy, x, wg, wu, wd, "silu", out[1], out[2], out[5], *out[-1])
+    assert status(c.sync) == ab.ABCD_ERR_TIMEOUT
+    assert ab.lib().abcd_set_wait_limit(c.h, 1 << 20) == ab.ABCD_OK
+    c.clear_status()
+    everything(c, *args, out)
+    c.sync()
+    assert all(torch.equal(a, b) for a, b in zip(flat(out), want))
+
+
 # ---- the block
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
