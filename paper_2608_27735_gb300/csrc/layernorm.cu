@@ -35,6 +35,8 @@ struct NormArgs {
   long long sx, sdy, sy, sres;
   float eps;
   int wide_w;                         // weight and bias are fp32 whatever the matrices' type
+  void* dw;                           // backward in one CTA: the sums' places, or NULL
+  void* db;
 };
 
 // How a row lies over threads, forward (one matrix is read) and backward (two); SHIFT: rows that
@@ -449,6 +451,19 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
       }
   }
   __syncthreads();
+  if (gridDim.x == 1) {                // nothing to add up
+    for (int c = threadIdx.x; c < a.cols; c += R::kThreads) {
+      const float s[2] = {sums[c], sums[R::kCapacity + c]};
+      void* const to[2] = {a.dw, a.db};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (!to[k]) continue;
+        if (a.wide_w) ((float*)to[k])[c] = s[k];
+        else ((T*)to[k])[c] = from_f32<T>(s[k]);
+      }
+    }
+    return;
+  }
   float* part = a.part + (long long)blockIdx.x * 2 * a.cols;
   for (int c = threadIdx.x; c < a.cols; c += R::kThreads) {
     part[c] = sums[c];
@@ -605,7 +620,7 @@ extern "C" abcd_status abcd_layer_norm(abcd_ctx* ctx, const abcd_matrix* x, cons
     return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_layer_norm: bad eps or statistics");
   if (x->rows == 0) return ABCD_OK;
   const NormArgs a{x->data, nullptr, weight, bias, y->data, nullptr, mean, rstd, nullptr, x->rows,
-                   (int)x->cols, x->stride, 0, y->stride, 0, eps, weight_dtype == ABCD_F32};
+                   (int)x->cols, x->stride, 0, y->stride, 0, eps, weight_dtype == ABCD_F32, nullptr, nullptr};
   return with_type(x->dtype, [&](auto t) {
     using T = decltype(t);
     return with_shape<T, false>(x->cols, rows_aligned(x, 16) && rows_aligned(y, 16), [&](auto shape) {
@@ -644,8 +659,9 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
                        (!d_residual || rows_aligned(d_residual, 16));
   NormArgs a{x->data, dy->data, weight, nullptr, dx ? dx->data : nullptr, d_residual ? d_residual->data : nullptr,
              (float*)mean, (float*)rstd, part, x->rows, (int)x->cols, x->stride, dy->stride, dx ? dx->stride : 0,
-             d_residual ? d_residual->stride : 0, 0.f, weight_dtype == ABCD_F32};
+             d_residual ? d_residual->stride : 0, 0.f, weight_dtype == ABCD_F32, dweight, dbias};
   int ctas = 0;
+  bool one = false;
   const abcd_status st = with_type(x->dtype, [&](auto t) {
     using T = decltype(t);
     return with_shape<T, true>(x->cols, aligned, [&](auto shape) {
@@ -657,6 +673,9 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
       } else {
         static_assert(R::kCtas <= kNormCtasPerSm);
         ctas = (int)std::min<long long>((x->rows + R::kGroups - 1) / R::kGroups, R::kCtas * sms);
+        // a few turns of one CTA take less than a launch to add up several CTAs' sums
+        one = ctas > 0 && ctas <= 4;
+        if (one) ctas = 1;
       }
       const size_t need = kNetHeader + (size_t)ctas * 2 * (size_t)x->cols * sizeof(float);
       if (need > ctx->net_bytes)
@@ -672,7 +691,7 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
       }
     });
   });
-  if (st != ABCD_OK || (!dweight && !dbias)) return st;
+  if (st != ABCD_OK || one || (!dweight && !dbias)) return st;
   const dim3 grid((unsigned)((2 * x->cols + 31) / 32));
   return with_type(weight_dtype, [&](auto w) {
     using W = decltype(w);
