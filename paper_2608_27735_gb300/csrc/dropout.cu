@@ -2,8 +2,9 @@
 // Element e (row * cols + column) is kept where the 16-bit number e % 8 of block offset + e / 8 of
 // Philox4x32-10 is at least t, so that the mask is never stored: the backward pass is the same
 // kernel on dy.
-// Bound by HBM, and not far from it by the generator's arithmetic (about 70 instructions a block of
-// eight elements).
+// Bound by HBM, and not far from it by the generator's arithmetic: 100,000 x 1,024 bf16 with a residual
+// 98 us (6.3 TB/s), without one 79 us (5.2 TB/s), half of whose instruction slots are taken.  Element by
+// element, with the rows' divisions for each, both took 264 us.
 #include <algorithm>
 #include <cmath>
 

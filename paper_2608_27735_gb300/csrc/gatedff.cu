@@ -257,6 +257,7 @@ Plan plan(int sms, int dtype, int epi, const Job* jobs, int n) {
     const double tile_bytes = 4.0 * 128 * q.cg * q.bn, epilogue = q.epilogue[epi][f32];
     long long tiles[kMaxJobs], kblocks[kMaxJobs];
     double work = 0;                                     // stages of all tiles
+    long long whole = 0;                                 // items without splits
     for (int k = 0; k < n; ++k) {
       tiles[k] = jobs[k].batches * ((jobs[k].m + 128 * q.cg - 1) / (128 * q.cg)) * ((jobs[k].n + cols - 1) / cols);
       kblocks[k] = (jobs[k].k + kBlockK - 1) / kBlockK;
@@ -279,8 +280,10 @@ Plan plan(int sms, int dtype, int epi, const Job* jobs, int n) {
         }
         items += (double)tiles[k] * p[k];
       }
+      if (waves > 0 && items == (double)whole) break;     // no splits again, nor with more waves
+      if (waves == 0) whole = (long long)items;
       // a launch more, or the last warps' reading of part after part
-      if (joined > 0) joined += epi == kPlain ? 4.0 : 1.5 + 0.4 * p[0];
+      if (joined > 0) joined += epi == kPlain ? 2.5 : 1.5 + 0.4 * p[0];
       const double busy = std::min(1.0, items / (double)units), stage = q.idle + (q.busy - q.idle) * busy;
       double stages_last = 0;
       for (int k = 0; k < n; ++k) {

@@ -10,7 +10,8 @@
 // rows too long for that are read again from L2.  A group of lanes takes many rows: the weights (and backward dw
 // and db of its own columns) stay in registers, and the next rows are copied to shared memory
 // meanwhile (cp.async), which keeps the loads in flight that the few warps of so many registers could
-// not.  The CTAs' sums go to the workspace and a
+// not.  100,000 x 1,024 bf16: forward 66 us and backward 100 (both 6.2 TB/s), and 4 us for the sums;
+// one CTA per row without any of this took 520 and 820.  The CTAs' sums go to the workspace and a
 // second kernel adds them in their order.
 #include <algorithm>
 #include <type_traits>
@@ -571,7 +572,7 @@ constexpr int kNormCtasPerSm = 4;
 // Calls f with the row shape for `cols` columns of T: the fewest threads whose registers hold a row,
 // 32 elements a thread forward (with as many weights and biases) and 16 backward (with as many
 // weights and sums); f of an int where none does.  Backward, 100,000 x 1,024 bf16 with 32 elements a
-// thread (eight warps per SM) took 164 us.
+// thread (eight warps per SM) took 164 us, with 16 it takes 100.
 template <typename T, bool BWD, bool SHIFT, typename F> abcd_status with_shape(long long cols, F&& f) {
   constexpr int V = 16 / sizeof(T), N = (BWD ? 16 : 32) / V;   // vectors of 16 bytes per thread
   if (cols <= 8 * V) return f(RowShape<8, V, 1, BWD, SHIFT>());
