@@ -264,41 +264,6 @@ __device__ __forceinline__ void store_operand(const float (&v)[CW], const Out& o
   }
 }
 
-// Row m's CW values from column n on (lanes past the matrix get zeros).
-template <bool F32, int CW>
-__device__ __forceinline__ void load_row(float (&v)[CW], const Out& o, long long m, int n, bool in,
-                                         int cols, bool bf16) {
-  if constexpr (F32) {
-    const float* p = (const float*)o.p + m * o.stride + n;
-#pragma unroll
-    for (int i = 0; i < CW; i += 4) {
-      if (in && o.vec && i + 4 <= cols) {
-        const float4 q = *reinterpret_cast<const float4*>(p + i);
-        v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[i + e] = in && i + e < cols ? p[i + e] : 0.f;
-      }
-    }
-  } else {
-    const unsigned short* p = (const unsigned short*)o.p + m * o.stride + n;
-#pragma unroll
-    for (int i = 0; i < CW; i += 8) {
-      unsigned w[4] = {0u, 0u, 0u, 0u};
-      if (in && o.vec && i + 8 <= cols) {
-        const uint4 q = *reinterpret_cast<const uint4*>(p + i);
-        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (in && i + e < cols) w[e / 2] |= (unsigned)p[i + e] << (16 * (e & 1));
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i + e] = unpack((unsigned short)(w[e / 2] >> (16 * (e & 1))), bf16);
-    }
-  }
-}
-
 // Asynchronous copy of `bytes` (16 at most) to 16 bytes of shared memory, zeros after them.
 __device__ __forceinline__ void copy_piece(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes < 0 ? 0 : bytes < 16 ? bytes : 16) : "memory");
@@ -313,7 +278,7 @@ template <bool F32> struct RowBuffer {
   }
 };
 // Rows m ... m + rows of sixteen columns from column n on, on their way to such a buffer: by 16 bytes
-// or, of 32-bit values whose rows start anywhere, one by one.
+// (16-bit matrices always lie so), or 32-bit values whose rows start anywhere one by one.
 template <bool F32>
 __device__ __forceinline__ void rows_ahead(char* buf, const Out& o, long long m, int n, int rows, int cols) {
   using B = RowBuffer<F32>;
@@ -760,7 +725,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
       p.cols = min(P::kWarpCols, a.job[it.job].n - p.n);
       return p;
     };
-    const bool ahead = P::kAhead && (F32 || (a.in[0].vec && a.in[1].vec));
+    constexpr bool ahead = P::kAhead;
     // kDown: the saved projections of turn t of an item (16 columns), to one of two pairs of buffers
     char* saved = buffer + P::kTurn;
     constexpr int TURNS = P::kWarpCols / P::CW, SAVED = RowBuffer<F32>::kBytes;
@@ -874,18 +839,13 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
         } else if constexpr (EPI == kDown) {
           float z[P::CW], u[P::CW], s[P::CW];
           const char* zbuf = saved + (c / 16 & 1) * 2 * SAVED;
-          if (ahead) {
-            asm volatile("cp.async.wait_group 1;" ::: "memory");
-            __syncwarp();
-            row_of<F32>(z, zbuf, bf16);
-            row_of<F32>(u, zbuf + SAVED, bf16);
-            __syncwarp();
-            if (c / 16 + 2 < TURNS) ask(p, c / 16 + 2);
-            else ask(then, c / 16 + 2 - TURNS);
-          } else {
-            load_row<F32, P::CW>(z, a.in[0], m + lane, n + c, lane < rows, w, bf16);
-            load_row<F32, P::CW>(u, a.in[1], m + lane, n + c, lane < rows, w, bf16);
-          }
+          asm volatile("cp.async.wait_group 1;" ::: "memory");
+          __syncwarp();
+          row_of<F32>(z, zbuf, bf16);
+          row_of<F32>(u, zbuf + SAVED, bf16);
+          __syncwarp();
+          if (c / 16 + 2 < TURNS) ask(p, c / 16 + 2);
+          else ask(then, c / 16 + 2 - TURNS);
           sum_columns(c, 0, v);
           act_slopes(z, s, a.act);
           tmem_load_wait(v);

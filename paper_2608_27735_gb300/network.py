@@ -178,8 +178,9 @@ class FeedForwardBlock:
         return (rows * self.cols + 7) // 8
 
     def forward(self, x, y, train=True):
-        """y = the block of x (both [rows'][cols], rows' <= rows; y may be x).  train: keep what the
-        backward pass needs, and drop with the next counters of the block's generator."""
+        """y = the block of x (both [rows'][cols], rows' <= rows).  train: keep what the backward pass
+        needs (x among it: y is another matrix), and drop with the next counters of the block's
+        generator; otherwise y may be x."""
         n, w = x.shape[0], self.w
         nx, out = self.normed[:n], self.out[:n]
         if not train:
