@@ -379,7 +379,7 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
   for (int t = 0; t < ring.turns; ++t, r += step, x += step * a.sx, dy += step * a.sdy, dx += step * a.sy, res += step * a.sres) {
     ring.turn(t);
     const bool in = t < ring.rows;
-    const float rstd = stat[0].y, shift = -stat[0].x * rstd;
+    const float mean = stat[0].x, rstd = stat[0].y;
     stat[0] = stat[1];
     stat[1] = stat_of(t + 2, r + 2 * step);
     // past the row's end dy is zero, and so is what xh meets there
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_cons
       ring.get(g[j], t, 1, j, dy);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        xh[j][i] = xh[j][i] * rstd + shift;
+        xh[j][i] = (xh[j][i] - mean) * rstd;           // the forward pass's value, bit for bit
         dw[j][i] += g[j][i] * xh[j][i];
         db[j][i] += g[j][i];
         g[j][i] *= w[j][i];

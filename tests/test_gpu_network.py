@@ -131,6 +131,19 @@ def test_norm_of_constant_rows_and_far_from_zero(ctx):
     close(y, N.norm(X, f64(w), f64(b), 1e-5)[0], N.norm_bound(X, f64(w), f64(b), 1e-5, "f32"))
 
 
+def test_norm_of_constant_rows_backward(ctx):
+    """Without spread xh is zero, whatever the rows' values: the weight gets no gradient."""
+    x = matrix(np.repeat([[1000.0], [-37.5], [0.0]], 64, 1), "f32")
+    dy = matrix(np.random.default_rng(15).normal(size=(3, 64)), "f32")
+    mean, rstd, y = torch.empty(3, device="cuda"), torch.empty(3, device="cuda"), blank(3, 64, "f32")
+    dw, dx = torch.full((64,), float("nan"), device="cuda"), blank(3, 64, "f32")
+    ctx.reserve_network(3, 64)
+    ab.abcd_layer_norm(ctx, x, None, None, 1e-5, y, mean, rstd)
+    ab.abcd_layer_norm_backward(ctx, dy, x, None, mean, rstd, dx, dw)
+    ctx.sync()
+    assert not y.any() and not dw.any()
+
+
 def test_norm_keeps_a_bad_row_to_itself(ctx):
     x = matrix(np.random.default_rng(6).normal(size=(6, 64)), "f32")
     want = blank(6, 64, "f32")
