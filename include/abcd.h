@@ -469,7 +469,7 @@ typedef struct {
 /* The gate's activation: z sigmoid(z), z Phi(z) with the normal distribution's Phi, max(z, 0). */
 enum { ABCD_SILU = 0, ABCD_GELU = 1, ABCD_RELU = 2 };
 
-/* Bytes of device scratch with which abcd_layer_norm_backward takes matrices of up to `cols`
+/* Bytes of device scratch with which abcd_layer_norm_backward takes up to `rows` rows of up to `cols`
  * columns and, with ff > 0, the gated feed-forward calls take up to `rows` tokens of up to `cols`
  * columns with up to `ff` hidden ones, all in type dtype.  It is separate from the renderer's
  * workspace; dropout and the layer norm's forward pass take none. */
@@ -501,14 +501,16 @@ abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix* dy, const
  * w_gate, w_up [ff][d]; w_down [d][ff]; all of one type.  gate, up [rows][ff], both NULL or both
  * given: x w_gate^T and x w_up^T, which the backward pass reads.  The hidden matrix
  * act(gate) * up is rounded to the matrices' type between the two products.  In 32 bits a factor is
- * taken as three 16-bit terms (24 bits together), so one beyond 3.38e38 or infinite gives NaN. */
+ * taken as three 16-bit terms (24 bits together), so one beyond 3.38e38 or infinite gives NaN.  y may
+ * be x; no other output may overlap an operand or an output. */
 abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const abcd_matrix* w_gate,
                           const abcd_matrix* w_up, const abcd_matrix* w_down, int activation,
                           const abcd_matrix* y, const abcd_matrix* gate, const abcd_matrix* up);
 /* Its backward pass.  With dh = dy w_down, du = dh act(gate), dg = dh up act'(gate):
  * dx = dg w_gate + du w_up, dw_gate = dg^T x, dw_up = du^T x, dw_down = dy^T (act(gate) * up); each
  * may be NULL, and the weights' gradients are zero without rows.  act'(0) of ABCD_RELU is 0.  dg,
- * du and the hidden matrix are rounded to the matrices' type between the products. */
+ * du and the hidden matrix are rounded to the matrices' type between the products.  No gradient may
+ * overlap an operand or another gradient: they are written side by side. */
 abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* dy, const abcd_matrix* x,
                                    const abcd_matrix* w_gate, const abcd_matrix* w_up,
                                    const abcd_matrix* w_down, int activation,

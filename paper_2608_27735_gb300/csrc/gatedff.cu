@@ -8,6 +8,7 @@
 // operands, tensor maps, the choice of tiles and splits, the workspace.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "ffproduct.cuh"
 
@@ -394,6 +395,16 @@ bool shape_is(const abcd_matrix* m, int dtype, long long rows, long long cols) {
   return matrix_ok(m) && m->dtype == dtype && m->rows == rows && m->cols == cols;
 }
 
+// Whether a result starts where an operand or another result does; one that is not given starts nowhere.
+bool same_place(std::initializer_list<const abcd_matrix*> results, std::initializer_list<const abcd_matrix*> operands) {
+  for (auto r = results.begin(); r != results.end(); ++r) {
+    if (!*r) continue;
+    const auto at = [&](const abcd_matrix* m) { return m && m->data == (*r)->data; };
+    if (std::any_of(operands.begin(), operands.end(), at) || std::any_of(results.begin(), r, at)) return true;
+  }
+  return false;
+}
+
 // The scratch of the calls when every matrix has to be copied: the most that they take.
 size_t ff_scratch(long long rows, long long cols, long long ff, int dtype) {
   Scratch s{nullptr};
@@ -432,7 +443,7 @@ extern "C" abcd_status abcd_network_workspace_size(long long rows, long long col
   if (!bytes || rows < 0 || rows > kMaxNetRows || cols < 1 || cols > kMaxNetCols || ff < 0 ||
       ff > kMaxNetCols || !dtype_ok(dtype))
     return ABCD_ERR_INVALID_ARG;
-  const size_t norm = kNetHeader + (size_t)norm_bwd_ctas(kNetSms) * 2 * (size_t)cols * sizeof(float);
+  const size_t norm = kNetHeader + (size_t)std::min<long long>(norm_bwd_ctas(kNetSms), rows) * 2 * (size_t)cols * sizeof(float);
   *bytes = ff > 0 ? std::max(norm, ff_scratch(rows, cols, ff, dtype)) : norm;
   return ABCD_OK;
 }
@@ -465,6 +476,8 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
   if (activation < ABCD_SILU || activation > ABCD_RELU)
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: unknown activation", what);
   if (m == 0) return ABCD_OK;
+  if (same_place({gate, up}, {x, w_gate, w_up, w_down, y}) || same_place({y}, {w_gate, w_up, w_down}))
+    return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: an output is an operand or another output", what);
   Scratch need{nullptr};
   if (m <= kFewRows) {
     need.operand(m, f, ABCD_F32);                  // room for the hidden matrix in any type
@@ -533,6 +546,8 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
     }
     return ABCD_OK;
   }
+  if (same_place({dx, dw_gate, dw_up, dw_down}, {dy, x, w_gate, w_up, w_down, gate, up}))
+    return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: a gradient is an operand or another gradient", what);
   Scratch need{nullptr};
   need.take(kPartBytes);
   if (needs_pack(dy)) need.operand(m, d, t);

@@ -232,6 +232,20 @@ def test_ff_backward_of_some(ctx, kind, want):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows", [5, 300])
+def test_ff_over_its_input(ctx, kind, rows):
+    r = np.random.default_rng(14)
+    x = matrix(r.normal(size=(rows, 64)), kind)
+    wg, wu, wd = ff_weights(r, 64, 130, kind, 0, 0)
+    ctx.reserve_network(rows, 64, 130, TYPES[kind])
+    y = blank(rows, 64, kind)
+    ab.abcd_gated_ff(ctx, x, wg, wu, wd, "silu", y)
+    ab.abcd_gated_ff(ctx, x, wg, wu, wd, "silu", x)
+    ctx.sync()
+    assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_without_rows(ctx, kind):
     e = torch.empty(0, 24, dtype=TYPES[kind], device="cuda")
     h = torch.empty(0, 40, dtype=TYPES[kind], device="cuda")
@@ -352,6 +366,129 @@ def test_dropout_of_consecutive_offsets_is_one_stream(ctx):
     assert torch.equal(whole, part)
 
 
+# ---- long matrices
+
+def far(rows, cols, kind, pad=0):
+    """A CUDA matrix of normal numbers."""
+    buf = torch.empty(rows, cols + pad, dtype=TYPES[kind], device="cuda")
+    return buf.normal_(0, 1)[:, :cols]
+
+
+def some_rows(rows, width):
+    """Rows at both ends and around the ones that start at elements 2^31 and 2^32 of rows `width` long."""
+    near = [0, 1, rows - 2, rows - 1] + [e // width + k for e in (2 ** 31, 2 ** 32) for k in (0, 1)]
+    return sorted({k for k in near if k < rows})
+
+
+def only(rows, cols, kind, chosen):
+    """Zeros but in the chosen rows."""
+    t = torch.zeros(rows, cols, dtype=TYPES[kind], device="cuda")
+    t[chosen] = torch.randn(len(chosen), cols, device="cuda").to(t.dtype)
+    return t
+
+
+@pytest.fixture
+def roomy():
+    """A context of its own, whose workspace is given back, and room for large matrices."""
+    torch.cuda.empty_cache()
+    torch.manual_seed(4)
+    c = ab.Context(0)
+    yield c
+    c.sync()
+    del c
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+def test_norm_past_32_bits(roomy, pad):
+    rows, cols, kind = 4_300_007, 1000, "f16"
+    chosen = some_rows(rows, cols + pad)
+    x, dy = far(rows, cols, kind, pad), only(rows, cols, kind, chosen)
+    w = torch.randn(cols, device="cuda")
+    y, dx = torch.full_like(dy, float("nan")), torch.full_like(dy, float("nan"))
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    dw, db = torch.empty_like(w), torch.empty_like(w)
+    roomy.reserve_network(rows, cols)
+    ab.abcd_layer_norm(roomy, x, w, None, 1e-5, y, mean, rstd)
+    ab.abcd_layer_norm_backward(roomy, dy, x, w, mean, rstd, dx, dw, db)
+    roomy.sync()
+    assert torch.isfinite(y.sum(1, dtype=torch.float32)).all()
+    X, DY, W = f64(x[chosen]), f64(dy[chosen]), f64(w)
+    close(y[chosen], N.norm(X, W, 0 * W, 1e-5)[0], N.norm_bound(X, W, 0 * W, 1e-5, kind))
+    m32, r32 = f64(mean[chosen])[:, None], f64(rstd[chosen])[:, None]
+    bounds = N.norm_grad_bounds(DY, X, W, m32, r32, kind, "f32")     # the other rows add zeros
+    for got, want, bound in zip((dx[chosen], dw, db), N.norm_grad(DY, X, W, m32, r32), bounds):
+        close(got, want, bound)
+    dx[chosen] = 0
+    assert not dx.any()
+
+
+@pytest.mark.parametrize("kind,rows,d,f", [("f16", 4_300_007, 64, 1000), ("f32", 2_200_003, 40, 1000)])
+def test_ff_past_32_bits(roomy, kind, rows, d, f):
+    chosen = some_rows(rows, f)
+    x, dy = far(rows, d, kind), only(rows, d, kind, chosen)
+    wg, wu, wd = ff_weights(np.random.default_rng(2), d, f, kind, 0, 0)
+    y, dx = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+    gate, up = (torch.empty(rows, f, dtype=x.dtype, device="cuda") for _ in range(2))
+    grads = [torch.full_like(t, float("nan")) for t in (wg, wu, wd)]
+    roomy.reserve_network(rows, d, f, TYPES[kind])
+    ab.abcd_gated_ff(roomy, x, wg, wu, wd, "silu", y, gate, up)
+    ab.abcd_gated_ff_backward(roomy, dy, x, wg, wu, wd, "silu", gate, up, dx, *grads)
+    roomy.sync()
+    assert torch.isfinite(y.sum(1, dtype=torch.float32)).all()
+    weights = [f64(t) for t in (wg, wu, wd)]
+    X, DY = f64(x[chosen]), f64(dy[chosen])
+    for got, want, bound in zip((y, gate, up), N.ff(X, *weights, "silu"), N.ff_bounds(X, *weights, "silu", kind)):
+        close(got[chosen], want, bound)
+    args = [DY, X, *weights, "silu", f64(gate[chosen]), f64(up[chosen])]
+    for got, want, bound in zip((dx[chosen], *grads), N.ff_grad(*args), N.ff_grad_bounds(*args, kind)):
+        close(got, want, bound)
+    dx[chosen] = 0
+    assert not dx.any()
+
+
+@pytest.mark.parametrize("kind", ["f16", "f32"])
+def test_ff_of_rows_far_apart(roomy, kind):
+    """Rows so far apart that a matrix reaches past 2^31 elements, all matrices in one buffer."""
+    rows, d, f = 300, 40, 72
+    stride = 2 ** 31 // 256
+    buf = torch.zeros(rows, stride, dtype=TYPES[kind], device="cuda")
+    place = iter(range(0, stride, 128))
+    matrices = lambda *shapes: [buf[:n, a:a + c] for (n, c), a in zip(shapes, place)]
+    x, dy, wg, wu, wd = matrices((rows, d), (rows, d), (f, d), (f, d), (d, f))
+    for t, s in zip((x, dy, wg, wu, wd), (1, 1, d ** -0.5, d ** -0.5, f ** -0.5)):
+        t.normal_(0, s)
+    y, gate, up, dx, *grads = matrices((rows, d), (rows, f), (rows, f), (rows, d), (f, d), (f, d), (d, f))
+    roomy.reserve_network(rows, d, f, TYPES[kind])
+    ab.abcd_gated_ff(roomy, x, wg, wu, wd, "gelu", y, gate, up)
+    ab.abcd_gated_ff_backward(roomy, dy, x, wg, wu, wd, "gelu", gate, up, dx, *grads)
+    roomy.sync()
+    A = [f64(t) for t in (x, wg, wu, wd)]
+    for got, want, bound in zip((y, gate, up), N.ff(*A, "gelu"), N.ff_bounds(*A, "gelu", kind)):
+        close(got, want, bound)
+    args = [f64(dy), *A, "gelu", f64(gate), f64(up)]
+    for got, want, bound in zip((dx, *grads), N.ff_grad(*args), N.ff_grad_bounds(*args, kind)):
+        close(got, want, bound)
+
+
+@pytest.mark.parametrize("cols,pad", [(1000, 0), (1000, 8), (999, 0), (1000, 3)])
+def test_dropout_past_32_bits(roomy, cols, pad):
+    rows, kind, offset = 4_300_008, "f16", 77
+    x = far(rows, cols, kind, pad)
+    y = torch.empty_like(x)
+    ab.abcd_dropout(roomy, x, 0.25, 5, offset, y, x)
+    roomy.sync()
+    chosen = sorted({8 * (k // 8) for k in some_rows(rows, cols + pad)})    # eight rows from each: whole blocks
+    for k in chosen:
+        keep, s = N.kept(8, cols, 0.25, 5, offset + k * cols // 8)
+        X = f64(x[k:k + 8])
+        want = keep * X * s + X
+        close(y[k:k + 8], want, 3 * N.EPS * (s + 1) * np.abs(X) + np.abs(want) * 2 * N.UNIT[kind] + N.TINY[kind])
+    ratio = (y / x).nan_to_num_(1.0)
+    share = float((ratio > 1.5).sum(1, dtype=torch.int32).double().mean() / cols)
+    assert abs(share - 0.75) < 1e-3                     # of 4e9 elements
+
+
 # ---- refusals
 
 def status(f, *a, **k):
@@ -384,6 +521,15 @@ def test_refusals(ctx):
     g = t(4, 6)
     assert status(ab.abcd_gated_ff_backward, ctx, y, x, wg, wg, wd, "silu", g, t(4, 5), t(4, 8)) == bad
     assert status(ab.abcd_gated_ff_backward, ctx, y, x, wg, wg, wd, "silu", g, g, t(4, 8), t(6, 9)) == bad
+    # outputs that are operands or other outputs; the forward pass's y may be x
+    up = t(4, 6)
+    assert status(ab.abcd_gated_ff, ctx, x, wg, wg, wd, "silu", y, g, g) == bad
+    assert status(ab.abcd_gated_ff, ctx, x, wg, wg, wd, "silu", wg[:4]) == bad
+    assert status(ab.abcd_gated_ff_backward, ctx, y, x, wg, wg, wd, "silu", g, up, y) == bad
+    assert status(ab.abcd_gated_ff_backward, ctx, y, x, wg, wg, wd, "silu", g, up, x) == bad
+    assert status(ab.abcd_gated_ff_backward, ctx, y, x, wg, wg, wd, "silu", g, up, None, t(6, 8), wg) == bad
+    same = t(6, 8)
+    assert status(ab.abcd_gated_ff_backward, ctx, y, x, wg, wg, wd, "silu", g, up, None, same, same) == bad
     with pytest.raises(ValueError):
         ab.abcd_gated_ff(ctx, x, wg, wg, wd, "tanh", y)
     with pytest.raises(ValueError):
