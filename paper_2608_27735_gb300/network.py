@@ -6,9 +6,9 @@ types float32, float16 or bfloat16.  The calls run on the context's stream: tens
 stream fills or frees need that stream's events, as everywhere in this package."""
 from __future__ import annotations
 
-import ctypes as C
+import struct
 
-from . import (ABCD_GELU, ABCD_RELU, ABCD_SILU, Context, _dtypes, _torch, abcd_matrix, lib)
+from . import ABCD_GELU, ABCD_RELU, ABCD_SILU, Context, _dtypes, _torch, lib
 
 ACTIVATIONS = {"silu": ABCD_SILU, "gelu": ABCD_GELU, "relu": ABCD_RELU}
 
@@ -29,12 +29,20 @@ def _call(name):
     return f
 
 
+# The bytes of an abcd_matrix.  ctypes hands on the address of a bytes object as it is, which takes a
+# quarter of the time that it takes to make a Structure and a reference to it (0.1 us instead of 0.4).
+_pack = struct.Struct("@Pqqqi0q").pack
+
+
 def _matrix(t, what):
-    """abcd_matrix of a 2-D CUDA tensor."""
-    if not t.is_cuda or t.dim() != 2:
+    """(abcd_matrix as bytes, rows, columns) of a 2-D CUDA tensor."""
+    try:
+        rows, cols = t.shape
+        stride, unit = t.stride()
+    except ValueError:
+        raise ValueError(f"{what} must be a 2-D CUDA tensor") from None
+    if not t.is_cuda:
         raise ValueError(f"{what} must be a 2-D CUDA tensor")
-    rows, cols = t.shape
-    stride, unit = t.stride()
     if unit != 1 and cols > 1:
         raise ValueError(f"{what} must have consecutive columns")
     kind = _KINDS.get(t.dtype)
@@ -42,11 +50,11 @@ def _matrix(t, what):
         raise ValueError(f"{what} has type {t.dtype}; float32, float16 and bfloat16 are taken")
     if rows <= 1 and stride < cols:
         stride = cols
-    return abcd_matrix(t.data_ptr(), rows, cols, stride, kind)
+    return _pack(t.data_ptr(), rows, cols, stride, kind), rows, cols
 
 
 def _optional(t, what):
-    return None if t is None else C.byref(_matrix(t, what))
+    return None if t is None else _matrix(t, what)[0]
 
 
 def _vector(t, n, what, dtype):
@@ -81,11 +89,11 @@ def abcd_layer_norm(ctx: Context, x, weight, bias, eps, y, mean=None, rstd=None)
     """y = layer norm of x's rows; weight, bias: [cols] or None; mean, rstd: float32 [rows] that the
     backward pass needs, or None."""
     call = _call("abcd_layer_norm")
-    mx, my = _matrix(x, "x"), _matrix(y, "y")
+    mx, rows, cols = _matrix(x, "x")
     wt = _weight_type(x, weight, bias)
-    st = call(ctx.h, C.byref(mx), _vector(weight, mx.cols, "weight", wt),
-              _vector(bias, mx.cols, "bias", wt), _KINDS[wt], eps, C.byref(my),
-              _vector(mean, mx.rows, "mean", _F32), _vector(rstd, mx.rows, "rstd", _F32))
+    st = call(ctx.h, mx, _vector(weight, cols, "weight", wt), _vector(bias, cols, "bias", wt),
+              _KINDS[wt], eps, _matrix(y, "y")[0], _vector(mean, rows, "mean", _F32),
+              _vector(rstd, rows, "rstd", _F32))
     if st:
         ctx.check(st)
 
@@ -95,12 +103,12 @@ def abcd_layer_norm_backward(ctx: Context, dy, x, weight, mean, rstd, dx=None, d
     """dx, dweight and dbias (each may be None) of abcd_layer_norm; d_residual is added to dx (which
     may be dy or d_residual).  Takes the network workspace (Context.reserve_network)."""
     call = _call("abcd_layer_norm_backward")
-    md, mx = _matrix(dy, "dy"), _matrix(x, "x")
+    mx, rows, cols = _matrix(x, "x")
     wt = _weight_type(x, weight, dweight, dbias)
-    st = call(ctx.h, C.byref(md), C.byref(mx), _vector(weight, mx.cols, "weight", wt), _KINDS[wt],
-              _vector(mean, mx.rows, "mean", _F32), _vector(rstd, mx.rows, "rstd", _F32),
+    st = call(ctx.h, _matrix(dy, "dy")[0], mx, _vector(weight, cols, "weight", wt), _KINDS[wt],
+              _vector(mean, rows, "mean", _F32), _vector(rstd, rows, "rstd", _F32),
               _optional(d_residual, "d_residual"), _optional(dx, "dx"),
-              _vector(dweight, mx.cols, "dweight", wt), _vector(dbias, mx.cols, "dbias", wt))
+              _vector(dweight, cols, "dweight", wt), _vector(dbias, cols, "dbias", wt))
     if st:
         ctx.check(st)
 
@@ -109,9 +117,9 @@ def abcd_gated_ff(ctx: Context, x, w_gate, w_up, w_down, activation, y, gate=Non
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T; gate, up: [rows][ff] that the backward pass
     needs, or None; activation: "silu", "gelu" or "relu".  Takes the network workspace."""
     call = _call("abcd_gated_ff")
-    st = call(ctx.h, C.byref(_matrix(x, "x")), C.byref(_matrix(w_gate, "w_gate")),
-              C.byref(_matrix(w_up, "w_up")), C.byref(_matrix(w_down, "w_down")),
-              _activation(activation), C.byref(_matrix(y, "y")), _optional(gate, "gate"),
+    st = call(ctx.h, _matrix(x, "x")[0], _matrix(w_gate, "w_gate")[0],
+              _matrix(w_up, "w_up")[0], _matrix(w_down, "w_down")[0],
+              _activation(activation), _matrix(y, "y")[0], _optional(gate, "gate"),
               _optional(up, "up"))
     if st:
         ctx.check(st)
@@ -122,10 +130,10 @@ def abcd_gated_ff_backward(ctx: Context, dy, x, w_gate, w_up, w_down, activation
     """dx and the weights' gradients (each may be None) of abcd_gated_ff, from what its forward call
     left in gate and up.  Takes the network workspace."""
     call = _call("abcd_gated_ff_backward")
-    st = call(ctx.h, C.byref(_matrix(dy, "dy")), C.byref(_matrix(x, "x")),
-              C.byref(_matrix(w_gate, "w_gate")), C.byref(_matrix(w_up, "w_up")),
-              C.byref(_matrix(w_down, "w_down")), _activation(activation),
-              C.byref(_matrix(gate, "gate")), C.byref(_matrix(up, "up")), _optional(dx, "dx"),
+    st = call(ctx.h, _matrix(dy, "dy")[0], _matrix(x, "x")[0],
+              _matrix(w_gate, "w_gate")[0], _matrix(w_up, "w_up")[0],
+              _matrix(w_down, "w_down")[0], _activation(activation),
+              _matrix(gate, "gate")[0], _matrix(up, "up")[0], _optional(dx, "dx"),
               _optional(dw_gate, "dw_gate"), _optional(dw_up, "dw_up"),
               _optional(dw_down, "dw_down"))
     if st:
@@ -136,8 +144,8 @@ def abcd_dropout(ctx: Context, x, p, seed, offset, y, residual=None):
     """y = residual + dropout(x) with the mask of (seed, offset); y may be x or residual.  The next
     call's offset is past this one's: offset + ceil(rows * cols / 8)."""
     call = _call("abcd_dropout")
-    st = call(ctx.h, C.byref(_matrix(x, "x")), p, seed, offset, _optional(residual, "residual"),
-              C.byref(_matrix(y, "y")))
+    st = call(ctx.h, _matrix(x, "x")[0], p, seed, offset, _optional(residual, "residual"),
+              _matrix(y, "y")[0])
     if st:
         ctx.check(st)
 
@@ -145,7 +153,7 @@ def abcd_dropout(ctx: Context, x, p, seed, offset, y, residual=None):
 def abcd_dropout_backward(ctx: Context, dy, p, seed, offset, dx):
     """dx = dropout's gradient of dy under the mask of (seed, offset); dx may be dy."""
     call = _call("abcd_dropout_backward")
-    st = call(ctx.h, C.byref(_matrix(dy, "dy")), p, seed, offset, C.byref(_matrix(dx, "dx")))
+    st = call(ctx.h, _matrix(dy, "dy")[0], p, seed, offset, _matrix(dx, "dx")[0])
     if st:
         ctx.check(st)
 

@@ -89,3 +89,13 @@ def test_struct_layout_matches_header(tmp_path):
     got = [int(v) for v in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
     assert got == [C.sizeof(ab.abcd_matrix)] + [getattr(ab.abcd_matrix, f).offset for f in fields] + \
         [ab.ABCD_BF16, ab.ABCD_SILU, ab.ABCD_GELU, ab.ABCD_RELU]
+
+
+def test_packed_matrix_is_the_struct():
+    from paper_2608_27735_gb300 import network
+    m = (0x123456789ABCDEF0, 7, 59, 64, ab.ABCD_BF16)
+    s = ab.abcd_matrix(*m)
+    raw = network._pack(*m)
+    assert len(raw) == C.sizeof(s)
+    got = ab.abcd_matrix.from_buffer_copy(raw)
+    assert [getattr(got, f) for f, _ in s._fields_] == list(m)
