@@ -10,7 +10,7 @@
 // rows too long for that are read again from L2.  A group of lanes takes many rows: the weights (and backward dw
 // and db of its own columns) stay in registers, and the next rows are copied to shared memory
 // meanwhile (cp.async), which keeps the loads in flight that the few warps of so many registers could
-// not.  100,000 x 1,024 bf16: forward 66 us and backward 100 (both 6.2 TB/s), and 4 us for the sums;
+// not.  100,000 x 1,024 bf16: forward 66 us and backward 101 (both 6.2 TB/s), and 2.4 us for the sums;
 // one CTA per row without any of this took 520 and 820.  The CTAs' sums go to the workspace and a
 // second kernel adds them in their order.
 #include <algorithm>
@@ -57,8 +57,13 @@ template <int TPR_, int V_, int NV_, bool BWD, bool SHIFT> struct RowShape {
   static constexpr int kDepth = 4 * kAhead > 100 * 1024 ? 3 : 4;
   static constexpr size_t kRing = kDepth * kAhead, kSums = BWD ? (size_t)2 * kCapacity * 4 : 0;
   static constexpr size_t kSmem = kRing > kSums ? kRing : kSums;
-  // CTAs per SM that the grid offers: as many as their registers (and rows) leave room for
-  static constexpr int kCtas = kThreads > 256 || kSmem > 100 * 1024 ? 1 : V * NV > 8 ? 2 : 4;
+  // CTAs per SM: as many as their registers (and rows) leave room for.  Short rows backward are held to
+  // the registers of three CTAs, or of four in 32 bits (1,000,000 x 64 bf16: 75 us, and 89 with two CTAs
+  // of as many registers as they like; rows that start anywhere of eight values a thread spill at three).
+  static constexpr bool kShort = V * NV <= 8;
+  static constexpr int kCtas = kThreads > 256 || kSmem > 100 * 1024 ? 1
+                               : !kShort || (BWD && SHIFT && V * NV == 8) ? 2
+                               : BWD && (SHIFT || V * NV == 8) ? 3 : 4;
 };
 
 template <typename T, int V>
@@ -350,7 +355,7 @@ __global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_cons
 }
 
 template <typename T, typename R>
-__global__ void __launch_bounds__(R::kThreads) norm_bwd_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(R::kThreads, R::kShort ? R::kCtas : 0) norm_bwd_kernel(const __grid_constant__ NormArgs a) {
   constexpr int V = R::V, NV = R::NV, TPR = R::TPR;
   extern __shared__ char smem[];
   __shared__ float2 red[2][32];
@@ -543,21 +548,25 @@ __global__ void __launch_bounds__(kLongThreads) norm_bwd_long_kernel(const __gri
   }
 }
 
-// dw and db from the CTAs' sums: 32 columns per CTA, 32 runs of consecutive CTAs added side by side
-// and then in their order.
-template <typename W>
+// dw and db from the CTAs' sums: COLS columns per CTA, 1024 / COLS runs of consecutive CTAs added side by
+// side and then in their order (the runs of a warp in pairs, the warps' one after another).  Of 32
+// columns, which are few CTAs and a long chain of loads, 59 columns take 4.6 us; of eight 2.2.
+template <typename W, int COLS>
 __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* part, int ctas, int cols, W* dw, W* db) {
   pdl_wait();
-  __shared__ float run[32][33];
-  const int lane = threadIdx.x & 31, k = threadIdx.x / 32;
-  const int c = blockIdx.x * 32 + lane;            // of [dw | db]
+  constexpr int RUNS = 1024 / COLS;
+  __shared__ float run[32][COLS + 1];
+  const int lane = threadIdx.x % COLS, k = threadIdx.x / COLS;
+  const int c = blockIdx.x * COLS + lane;          // of [dw | db]
   float s = 0.f;
   if (c < 2 * cols) {
-    const int k0 = ctas * k / 32, k1 = ctas * (k + 1) / 32;
-#pragma unroll 10
+    const int k0 = ctas * k / RUNS, k1 = ctas * (k + 1) / RUNS;
+#pragma unroll 5
     for (int q = k0; q < k1; ++q) s += part[(long long)q * 2 * cols + c];
   }
-  run[k][lane] = s;
+#pragma unroll
+  for (int o = COLS; o < 32; o *= 2) s += __shfl_xor_sync(~0u, s, o);
+  if ((threadIdx.x & 31) < COLS) run[threadIdx.x / 32][lane] = s;
   __syncthreads();
   if (k || c >= 2 * cols) return;
   s = 0.f;
@@ -673,7 +682,10 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
         ctas = (int)std::min<long long>(x->rows, 2LL * sms);
       } else {
         static_assert(R::kCtas <= kNormCtasPerSm);
-        ctas = (int)std::min<long long>((x->rows + R::kGroups - 1) / R::kGroups, R::kCtas * sms);
+        // with fewer than twelve turns a CTA, a third and fourth CTA per SM cost the kernel that adds up
+        // their sums more than they gain (100,000 x 64 bf16: 11.7 us with two, 12.1 with three)
+        const long long turns = (x->rows + R::kGroups - 1) / R::kGroups;
+        ctas = (int)std::min<long long>(turns, std::clamp<long long>(turns / (12 * sms), std::min(2, R::kCtas), R::kCtas) * sms);
         // a few turns of one CTA take less than a launch to add up several CTAs' sums
         one = ctas > 0 && ctas <= 4;
         if (one) ctas = 1;
@@ -693,10 +705,13 @@ extern "C" abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix
     });
   });
   if (st != ABCD_OK || one || (!dweight && !dbias)) return st;
-  const dim3 grid((unsigned)((2 * x->cols + 31) / 32));
+  // columns in eights until 32 a CTA give half the SMs one (3,000 x 4,096 bf16: both kernels 20.6 us by
+  // 32, 23.7 by eight)
+  const bool wide = 2 * x->cols >= 16LL * sms;
+  const dim3 grid((unsigned)((2 * x->cols + (wide ? 31 : 7)) / (wide ? 32 : 8)));
   return with_type(weight_dtype, [&](auto w) {
     using W = decltype(w);
-    return check_launch(ctx, "norm_sum_kernel", launch_pdl(norm_sum_kernel<W>, grid, dim3(1024), 0, ctx->stream,
-                                                           (const float*)part, ctas, (int)x->cols, (W*)dweight, (W*)dbias));
+    return check_launch(ctx, "norm_sum_kernel", launch_pdl(wide ? norm_sum_kernel<W, 32> : norm_sum_kernel<W, 8>, grid, dim3(1024), 0,
+                                                           ctx->stream, (const float*)part, ctas, (int)x->cols, (W*)dweight, (W*)dbias));
   });
 }
