@@ -3,7 +3,9 @@
 //   g = dy w, xh = (x - mean) rstd:  dx = rstd (g - mean(g) - xh mean(g xh)),
 //   dw = sum_rows dy xh,  db = sum_rows dy.
 // The variance is taken from the deviations, not from the difference of two moments, so a mean far
-// from zero costs it no digits.
+// from zero costs it no digits.  The deviations are from a mean whose sum and division have rounded, and
+// their own mean, what that one is off by, corrects it (rows of one value then have that value as their
+// mean: without this 1,000 columns of 1000.0 had one a unit higher, and xh of 0.019 instead of 0).
 //
 // Bound by HBM (forward x -> y, backward x, dy -> dx).  A row is read once: TPR lanes (part of a
 // warp, a warp, or a CTA) hold it in registers, NV vectors of V consecutive elements (16 bytes) each;
@@ -135,6 +137,12 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float2 (*red)[32], 
       b += red[turn][first + k].y;
     }
   }
+}
+
+// rstd from the mean of the squared deviations from a point that lies `off` below the mean.
+__device__ __forceinline__ float rstd_of(float squares, float off, float eps) {
+  const float var = squares - off * off;
+  return rsqrtf((var < 0.f ? 0.f : var) + eps);        // NaN stays NaN
 }
 
 // Asynchronous copy of min(16, bytes) bytes to 16 bytes of shared memory, zeros after them.
@@ -323,26 +331,28 @@ __global__ void __launch_bounds__(R::kThreads) norm_fwd_kernel(const __grid_cons
       for (int i = 0; i < V; ++i) s += v[j][i];
     }
     row_sum2<TPR>(s, unused, red, 0);
-    const float mean = s * inv;
+    const float about = s * inv;
+    float e = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int left = ring.left - j * TPR * V;
       if (left < V) {                                  // past the row's end nothing deviates
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[j][i] = i < left ? v[j][i] : mean;
+        for (int i = 0; i < V; ++i) v[j][i] = i < left ? v[j][i] : about;
       }
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        v[j][i] -= mean;
-        q += v[j][i] * v[j][i];
+        const float d = v[j][i] - about;
+        q += d * d;
+        e += d;
       }
     }
-    row_sum2<TPR>(q, unused, red, 1);
-    const float rstd = rsqrtf(q * inv + a.eps);
+    row_sum2<TPR>(q, e, red, 1);
+    const float mean = about + e * inv, rstd = rstd_of(q * inv, e * inv, a.eps);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[j][i] = v[j][i] * rstd * w[j][i] + b[j][i];
+      for (int i = 0; i < V; ++i) v[j][i] = (v[j][i] - mean) * rstd * w[j][i] + b[j][i];
       ring.put(v[j], t, j, y);
     }
     ring.flush(t, y);
@@ -490,13 +500,16 @@ __global__ void __launch_bounds__(kLongThreads) norm_fwd_long_kernel(const __gri
     float s = 0.f, q = 0.f, unused = 0.f;
     for (int c = threadIdx.x; c < a.cols; c += kLongThreads) s += to_f32(x[c]);
     row_sum2<kLongThreads>(s, unused, red, 0);
-    const float mean = s / (float)a.cols;
+    const float about = s / (float)a.cols;
+    float e = 0.f;
     for (int c = threadIdx.x; c < a.cols; c += kLongThreads) {
-      const float d = to_f32(x[c]) - mean;
+      const float d = to_f32(x[c]) - about;
       q += d * d;
+      e += d;
     }
-    row_sum2<kLongThreads>(q, unused, red, 1);
-    const float rstd = rsqrtf(q / (float)a.cols + a.eps);
+    row_sum2<kLongThreads>(q, e, red, 1);
+    e /= (float)a.cols;
+    const float mean = about + e, rstd = rstd_of(q / (float)a.cols, e, a.eps);
     for (int c = threadIdx.x; c < a.cols; c += kLongThreads) {
       float w[1], b[1];
       load_weight<T, 1>(w, a.w, a.wide_w, c, 1, 1.f);
