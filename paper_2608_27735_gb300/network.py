@@ -188,14 +188,16 @@ class FeedForwardBlock:
     def forward(self, x, y, train=True):
         """y = the block of x (both [rows'][cols], rows' <= rows).  train: keep what the backward pass
         needs (x among it: y is another matrix), and drop with the next counters of the block's
-        generator; otherwise y may be x."""
+        generator; otherwise y may be x, and what an earlier pass kept stays."""
         n, w = x.shape[0], self.w
-        nx, out = self.normed[:n], self.out[:n]
         if not train:
+            # in the backward pass's buffers: what the last training pass kept stays
+            nx, out = self.d_normed[:n], self.d_out[:n]
             abcd_layer_norm(self.ctx, x, w["norm_w"], w["norm_b"], self.eps, nx)
             abcd_gated_ff(self.ctx, nx, w["w_gate"], w["w_up"], w["w_down"], self.act, out)
             abcd_dropout(self.ctx, out, 0.0, self.seed, 0, y, x)
             return
+        nx, out = self.normed[:n], self.out[:n]
         self.drawn = self.offset
         self.offset += self._counters(n)
         abcd_layer_norm(self.ctx, x, w["norm_w"], w["norm_b"], self.eps, nx, self.mean[:n],

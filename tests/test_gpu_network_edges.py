@@ -46,3 +46,30 @@ def test_norm_of_constant_rows_at_any_width(ctx, kind, cols, pad, lead):
     want = f64(dy).sum(0)
     mag = np.abs(f64(dy)).sum(0)
     close(db, want, 22 * N.EPS * mag + (np.abs(want) + 22 * N.EPS * mag) * N.UNIT[kind] + N.TINY[kind])
+
+
+# ---- the block
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_block_evaluated_between_a_pass_and_its_backward_pass(ctx, kind):
+    """The gradients are those of the last training pass, whatever was evaluated since."""
+    r = np.random.default_rng(31)
+    n, d, f = 60, 28, 112
+    w = {"norm_w": torch.as_tensor(r.normal(1, 0.1, d)).to("cuda", TYPES[kind]),
+         "norm_b": torch.as_tensor(r.normal(0, 0.1, d)).to("cuda", TYPES[kind]),
+         "w_gate": matrix(r.normal(0, d ** -0.5, (f, d)), kind),
+         "w_up": matrix(r.normal(0, d ** -0.5, (f, d)), kind),
+         "w_down": matrix(r.normal(0, f ** -0.5, (d, f)), kind)}
+    x, other, dy = (matrix(r.normal(size=(n, d)), kind) for _ in range(3))
+    block = ab.FeedForwardBlock(ctx, w, n, p=0.2, seed=3)
+    found = []
+    for between in (False, True):
+        y, dx, seen = (blank(n, d, kind) for _ in range(3))
+        block.offset = 0                                # the same mask again
+        block.forward(x, y)
+        if between:
+            block.forward(other, seen, train=False)
+        block.backward(dy, x, dx)
+        ctx.sync()
+        found.append([t.clone() for t in (y, dx, *block.grads.values())])
+    assert all(torch.equal(a, b) for a, b in zip(*found))
