@@ -84,7 +84,8 @@ class Appearance:
 
     def forward(self, sh, ci, train=True):
         """The coefficients that camera ci sees of sh [n][D][3]: a new tensor of that shape."""
-        x = self.x
+        # without training in place, in the backward pass's buffer: what the last training pass kept stays
+        x = self.x if train else [self.dx] * len(self.x)
         x[0][:, :self.sh_cols] = sh.reshape(self.n, self.sh_cols)
         x[0][:, self.sh_cols:] = self.embed[ci]
         for k, block in enumerate(self.blocks):
@@ -92,8 +93,8 @@ class Appearance:
         return x[-1][:, :self.sh_cols].reshape(sh.shape).contiguous()
 
     def backward(self, d_sh, ci):
-        """The gradient of sh from that of forward(sh, ci)'s result; leaves the weights' and the
-        embeddings' gradients in Adam's buffer."""
+        """The gradient of sh from that of the last training forward(sh, ci)'s result; leaves the
+        weights' and the embeddings' gradients in Adam's buffer."""
         self.dx[:, :self.sh_cols] = d_sh.reshape(self.n, self.sh_cols)
         self.dx[:, self.sh_cols:] = 0.0
         for k in reversed(range(len(self.blocks))):

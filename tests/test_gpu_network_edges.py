@@ -73,3 +73,28 @@ def test_block_evaluated_between_a_pass_and_its_backward_pass(ctx, kind):
         ctx.sync()
         found.append([t.clone() for t in (y, dx, *block.grads.values())])
     assert all(torch.equal(a, b) for a, b in zip(*found))
+
+
+def test_appearance_evaluated_between_a_pass_and_its_backward_pass():
+    from paper_2608_27735_gb300.appearance import Appearance
+    ctx = ab.Context(0)
+    app = Appearance(ctx, 150, 1, 3, layers=2, embed=5, p=0.3, seed=4)
+    r = np.random.default_rng(1)
+    for b in app.blocks:
+        b.w["w_down"].copy_(torch.from_numpy(r.normal(0, 0.1, b.w["w_down"].shape).astype(np.float32)))
+    sh, other, d = (torch.from_numpy(r.normal(size=(150, 4, 3)).astype(np.float32)).cuda() for _ in range(3))
+    found = []
+    for between in (False, True):
+        for b in app.blocks:
+            b.offset = 0
+        seen = app.forward(sh, 1)
+        if between:
+            app.forward(other, 2, train=False)
+        d_sh = app.backward(d, 1)
+        ctx.sync()
+        found.append((seen.clone(), d_sh.clone(), app.adam.grads.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*found))
+    # and the evaluation is that of the layers: without dropout both are one
+    plain = Appearance(ctx, 150, 1, 3, layers=2, embed=5, p=0.0, seed=4)
+    plain.adam.values.copy_(app.adam.values)
+    assert torch.equal(plain.forward(sh, 2, train=False), plain.forward(sh, 2))
