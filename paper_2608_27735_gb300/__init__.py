@@ -339,6 +339,16 @@ class Context:
         if st != ABCD_OK:
             raise AbcdError(st, lib().abcd_last_error(self.h).decode(errors="replace"))
 
+    def hold(self, *tensors):
+        """Makes tensors that were allocated on the current stream the context's to use: its stream
+        waits for what the current one has queued (their memory may be what a kernel there still
+        writes), and their memory, once they are dropped, for the calls that use it."""
+        current = _torch().cuda.current_stream(self.device)
+        if current != self.stream:
+            self.stream.wait_stream(current)
+        for t in tensors:
+            t.record_stream(self.stream)
+
     def reserve(self, max_gaussians, max_pairs, max_pixels):
         """(Re)allocates the workspace if the limits grew."""
         torch = _torch()
@@ -369,9 +379,7 @@ class Context:
         if nbytes.value <= self.network_bytes:
             return
         ws = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=self.device)
-        ws.record_stream(self.stream)
-        if self.network_workspace is not None:       # calls in flight may still use it
-            self.network_workspace.record_stream(self.stream)
+        self.hold(ws)
         off = (-ws.data_ptr()) % 256
         self.check(lib().abcd_set_network_workspace(self.h, C.c_void_p(ws.data_ptr() + off),
                                                     nbytes.value))

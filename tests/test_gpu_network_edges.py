@@ -98,3 +98,41 @@ def test_appearance_evaluated_between_a_pass_and_its_backward_pass():
     plain = Appearance(ctx, 150, 1, 3, layers=2, embed=5, p=0.0, seed=4)
     plain.adam.values.copy_(app.adam.values)
     assert torch.equal(plain.forward(sh, 2, train=False), plain.forward(sh, 2))
+
+
+# ---- streams
+
+def pending(nbytes, value=255):
+    """Queues a wait of some ten milliseconds on the current stream and, behind it, a kernel that fills
+    nbytes with a value; gives the memory back at once.  Whoever gets it next has to wait for both."""
+    torch.cuda.empty_cache()
+    t = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    torch.cuda._sleep(40_000_000)
+    t.fill_(value)
+    return t.data_ptr()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_workspace_reserved_while_its_memory_is_written(kind):
+    """A context on a stream of its own, whose workspace the allocator takes from memory that the
+    current stream is still writing: the products' counters and sums are not written over."""
+    from .test_gpu_network import everything, flat, make_everything
+    n, d, f = 700, 264, 520
+    args, out = make_everything(n, d, f, kind, 23)
+    plain = ab.Context(0)
+    plain.reserve_network(n, d, f, TYPES[kind])
+    everything(plain, *args, out)
+    plain.sync()
+    want = flat(out)
+    nbytes = plain.network_bytes + 256
+    del plain
+    for t in (*out[:-1], *out[-1]):
+        t.fill_(float("nan"))
+    torch.cuda.synchronize()
+    side = ab.Context(0, torch.cuda.Stream())
+    at = pending(nbytes)
+    side.reserve_network(n, d, f, TYPES[kind])
+    assert side.network_workspace.data_ptr() == at
+    everything(side, *args, out)
+    side.sync()
+    assert all(torch.equal(a, b) for a, b in zip(flat(out), want))

@@ -1,0 +1,83 @@
+"""The host's side of the network calls without a GPU: streams of what the package allocates, calls on
+a null context, the library's tables."""
+import ctypes as C
+from types import SimpleNamespace
+
+import pytest
+
+import paper_2608_27735_gb300 as ab
+
+
+class Stream:
+    def __init__(self, name, log):
+        self.name, self.log = name, log
+
+    def wait_stream(self, other):
+        self.log.append(("wait", self.name, other.name))
+
+
+class Tensor:
+    def __init__(self, log):
+        self.log = log
+
+    def data_ptr(self):
+        return 0x1000
+
+    def record_stream(self, stream):
+        self.log.append(("record", stream.name))
+
+
+class Library:
+    """The library's calls that reserve a workspace, and what they were called after."""
+
+    def __init__(self, log):
+        self.log = log
+
+    def abcd_network_workspace_size(self, rows, cols, ff, dtype, out):
+        out._obj.value = 1024 * rows
+        return ab.ABCD_OK
+
+    def abcd_workspace_size(self, gaussians, pairs, pixels, out):
+        out._obj.value = 1024 * gaussians
+        return ab.ABCD_OK
+
+    def abcd_set_network_workspace(self, h, p, n):
+        self.log.append(("set",))
+        return ab.ABCD_OK
+
+    abcd_set_workspace = lambda self, *a: self.abcd_set_network_workspace(*a[:3])
+
+
+@pytest.fixture
+def context(monkeypatch):
+    """A context on a stream "own" while the current one is "current", and the log of both."""
+    log = []
+    current = Stream("current", log)
+    torch = SimpleNamespace(uint8=None, empty=lambda *a, **k: Tensor(log),
+                            cuda=SimpleNamespace(current_stream=lambda device: current))
+    library = Library(log)
+    monkeypatch.setattr(ab, "_torch", lambda: torch)
+    monkeypatch.setattr(ab, "lib", lambda: library)
+    c = ab.Context.__new__(ab.Context)
+    c.h, c.device, c.stream, c.workspace, c.limits = None, 0, Stream("own", log), None, (0, 0, 0)
+    c.network_workspace, c.network_bytes = None, 0
+    return c, current, log
+
+
+def test_network_workspace_waits_for_the_stream_it_was_allocated_on(context):
+    """The allocator hands out memory that kernels of the current stream may still write: the
+    context's stream waits for them before it clears the workspace, and the memory for the context's."""
+    c, current, log = context
+    c.reserve_network(4, 8, 8)
+    assert log == [("wait", "own", "current"), ("record", "own"), ("set",)]
+    c.reserve_network(2, 8, 8)                          # no more than it has
+    assert len(log) == 3
+    c.reserve_network(8, 8, 8)
+    assert log[3:] == log[:3]
+
+
+def test_network_workspace_on_the_current_stream_waits_for_nothing(context):
+    c, current, log = context
+    c.stream = current
+    c.reserve_network(4, 8, 8)
+    assert log == [("record", "current"), ("set",)]
