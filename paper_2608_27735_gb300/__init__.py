@@ -358,6 +358,7 @@ class Context:
         nbytes = C.c_size_t()
         self.check(lib().abcd_workspace_size(mg, mp, mx, C.byref(nbytes)))
         ws = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=self.device)
+        self.hold(ws)
         off = (-ws.data_ptr()) % 256
         self.workspace = ws
         self.check(lib().abcd_set_workspace(self.h, C.c_void_p(ws.data_ptr() + off), nbytes.value,

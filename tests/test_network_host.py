@@ -81,3 +81,14 @@ def test_network_workspace_on_the_current_stream_waits_for_nothing(context):
     c.stream = current
     c.reserve_network(4, 8, 8)
     assert log == [("record", "current"), ("set",)]
+
+
+def test_workspace_waits_for_the_stream_it_was_allocated_on(context):
+    """The renderer's workspace likewise; one that is replaced is kept for the calls that use it."""
+    c, current, log = context
+    c.reserve(4, 8, 8)
+    assert log == [("wait", "own", "current"), ("record", "own"), ("set",)]
+    c.reserve(4, 8, 8)                                  # no more than it has
+    assert len(log) == 3
+    c.reserve(8, 8, 8)
+    assert log[3:] == log[:3]
