@@ -180,6 +180,8 @@ class FeedForwardBlock:
         self.rstd = torch.empty_like(self.mean)
         self.grads = {k: torch.empty_like(t) for k, t in self.w.items()}
         self.offset = 0
+        ctx.hold(self.normed, self.out, self.gate, self.up, self.d_out, self.d_normed, self.mean, self.rstd,
+                 *self.grads.values())
         ctx.reserve_network(self.rows, self.cols, self.ff, dt)
 
     def _counters(self, rows):

@@ -136,3 +136,39 @@ def test_workspace_reserved_while_its_memory_is_written(kind):
     everything(side, *args, out)
     side.sync()
     assert all(torch.equal(a, b) for a, b in zip(flat(out), want))
+
+
+def test_block_made_and_dropped_while_its_memory_is_in_use():
+    """On a stream of the context's own: a block's buffers come from memory that the current stream
+    still writes, and go back while the block's calls still run."""
+    r = np.random.default_rng(33)
+    n, d, f = 4000, 64, 256
+    make = lambda: {"norm_w": torch.ones(d, device="cuda"), "norm_b": torch.zeros(d, device="cuda"),
+                    **{k: matrix(r.normal(0, 0.1, s), "f32") for k, s in
+                       (("w_gate", (f, d)), ("w_up", (f, d)), ("w_down", (d, f)))}}
+    w, x, dy = make(), matrix(r.normal(size=(n, d)), "f32"), matrix(r.normal(size=(n, d)), "f32")
+
+    def once(ctx, wait):
+        y, dx = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+        torch.cuda.synchronize()
+        if wait:
+            pending(8 * n * f * 4)                      # more than the block takes
+        block = ab.FeedForwardBlock(ctx, w, n, p=0.2, seed=3)
+        if wait:
+            with torch.cuda.stream(ctx.stream):
+                torch.cuda._sleep(40_000_000)           # the calls have yet to run when the block goes
+        block.forward(x, y)
+        block.backward(dy, x, dx)
+        del block
+        if wait:
+            others = [torch.full((n * d,), float("nan"), device="cuda") for _ in range(64)]
+            del others
+        ctx.sync()
+        torch.cuda.synchronize()
+        return y, dx
+
+    y, dx = once(ab.Context(0), False)
+    side = ab.Context(0, torch.cuda.Stream())
+    side.reserve_network(n, d, f)
+    y2, dx2 = once(side, True)
+    assert torch.equal(y, y2) and torch.equal(dx, dx2)

@@ -92,3 +92,27 @@ def test_workspace_waits_for_the_stream_it_was_allocated_on(context):
     assert len(log) == 3
     c.reserve(8, 8, 8)
     assert log[3:] == log[:3]
+
+
+def test_block_waits_for_the_stream_its_buffers_were_allocated_on(context, monkeypatch):
+    """Every buffer of a FeedForwardBlock is the context's stream's to use, and kept for its calls."""
+    from paper_2608_27735_gb300 import network
+    c, current, log = context
+    made = []
+
+    def allocate(*a, **k):
+        t = Tensor(log)
+        t.shape, t.dtype, t.device = (a[0] if isinstance(a[0], tuple) else a), None, None
+        made.append(t)
+        return t
+
+    torch = SimpleNamespace(uint8=None, float32=None, empty=allocate,
+                            empty_like=lambda t: allocate(t.shape), cuda=ab._torch().cuda)
+    for module in (ab, network):
+        monkeypatch.setattr(module, "_torch", lambda: torch)
+    held = []
+    monkeypatch.setattr(ab.Context, "hold", lambda self, *tensors: held.extend(tensors))
+    weights = {"norm_w": (8,), "norm_b": (8,), "w_gate": (16, 8), "w_up": (16, 8), "w_down": (8, 16)}
+    w = {k: SimpleNamespace(shape=s, dtype=None, device=None) for k, s in weights.items()}
+    network.FeedForwardBlock(c, w, 4)
+    assert {id(t) for t in made} == {id(t) for t in held}
