@@ -259,7 +259,7 @@ abcd_status abcd_set_workspace(abcd_ctx* ctx, void* ptr, size_t bytes, int max_g
 }
 
 abcd_status abcd_clear_status(abcd_ctx* ctx) {
-  if (!has_workspace(ctx) && !ctx->net_base) return ABCD_ERR_WORKSPACE;
+  if (!ctx || (!has_workspace(ctx) && !ctx->net_base)) return ABCD_ERR_WORKSPACE;
   cudaError_t e = has_workspace(ctx) ? cudaMemsetAsync(ctx->ws.status, 0, 8, ctx->stream) : cudaSuccess;
   // the products' status, and the counters that a product which gave up left in between
   if (e == cudaSuccess && ctx->net_base) e = cudaMemsetAsync(ctx->net_base, 0, kNetHeader, ctx->stream);

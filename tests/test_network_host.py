@@ -116,3 +116,15 @@ def test_block_waits_for_the_stream_its_buffers_were_allocated_on(context, monke
     w = {k: SimpleNamespace(shape=s, dtype=None, device=None) for k, s in weights.items()}
     network.FeedForwardBlock(c, w, 4)
     assert {id(t) for t in made} == {id(t) for t in held}
+
+
+def test_clear_status_rejects_a_null_context():
+    """In a process of its own, which a read through the null pointer would end."""
+    import os
+    import subprocess
+    import sys
+    ab.build()
+    code = "import paper_2608_27735_gb300 as ab; print(ab.lib().abcd_clear_status(None))"
+    run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True,
+                         cwd=os.path.dirname(os.path.dirname(ab.HEADER)))
+    assert (run.returncode, run.stdout.strip()) == (0, str(ab.ABCD_ERR_WORKSPACE))
