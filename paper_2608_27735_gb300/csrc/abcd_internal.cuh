@@ -25,7 +25,8 @@ constexpr int kVisSumCopies = 8;          // copies of the layer visibility sums
 // words of Workspace::os_ctr: [2 sorts][2] tile and finished-CTA counters of a radix pass, the run
 // placement's two, [2 calls in turn][2] the visible depth keys' range, the count kernel's finished CTAs
 constexpr int kCtrSorts = 0, kCtrPlace = 4, kCtrKeyRange = 8, kCtrTicket = 12;
-constexpr int kSmemKernels = 64;          // kernels with dynamic shared memory, at most
+// kernels with dynamic shared memory, at most: 62 of layer norm, 18 products, ten of the renderer
+constexpr int kSmemKernels = 128;
 
 // Device status bits (OR-ed into the status word; abcd_sync reports the lowest set code).
 constexpr unsigned kStatusCapacity = 1u << ABCD_ERR_CAPACITY;

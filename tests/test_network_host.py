@@ -128,3 +128,31 @@ def test_clear_status_rejects_a_null_context():
     run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True,
                          cwd=os.path.dirname(os.path.dirname(ab.HEADER)))
     assert (run.returncode, run.stdout.strip()) == (0, str(ab.ABCD_ERR_WORKSPACE))
+
+
+def test_every_kernel_with_much_shared_memory_has_a_place():
+    """A context remembers which kernels it has raised the shared memory limit of; one that finds no place
+    would be asked for again in every launch.  Counted from the sources: layer norm's row shapes (three
+    types, forward and backward, rows on 16-byte boundaries and not) whose rows ahead take more than
+    47 KB, the products' three shapes, three epilogues and two widths, and the renderer's kernels."""
+    import os
+    import re
+    csrc = os.path.join(os.path.dirname(ab.__file__), "csrc")
+    read = lambda name: open(os.path.join(csrc, name)).read()
+    shapes = re.findall(r"return f\(RowShape<(\d+), V, (\w+), BWD, SHIFT>", read("layernorm.cu"))
+    assert len(shapes) == 9
+    kernels = 0
+    for size in (4, 2, 2):
+        for backward in (False, True):
+            for shift in (False, True):
+                for lanes, vectors in shapes:
+                    lanes, nv = int(lanes), (16 if backward else 32) * size // 16 if vectors == "N" else int(vectors)
+                    ahead = (2 if backward else 1) * (max(lanes, 256) // lanes) * (lanes * nv + shift) * 16
+                    ring = (3 if 4 * ahead > 100 * 1024 else 4) * ahead
+                    sums = 2 * lanes * nv * 16 // size * 4 if backward else 0
+                    kernels += max(ring, sums) > 47 * 1024
+    products = len(re.findall(r"return launch_product<\d, \d+, EPI, F32>", read("ffproduct.cuh"))) * 3 * 2
+    assert products == 18
+    renderer = 4 + 2 + 1 + 1 + 2                        # visibility, tile rows, ranges, place, loss
+    table = int(re.search(r"kSmemKernels = (\d+)", read("abcd_internal.cuh"))[1])
+    assert kernels + products + renderer <= table, (kernels, products, renderer)
