@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_kernel(const __grid_consta
       ((T*)a.saved[0])[lane * a.ssaved[0] + unit] = from_f32<T>(v[0]);
       ((T*)a.saved[1])[lane * a.ssaved[1] + unit] = from_f32<T>(u);
     }
-    act_values(v, a.act);
+    act_values<sizeof(T) == 4>(v, a.act);
     v[0] *= u;
   }
   ((T*)a.y)[lane * a.sy + unit] = from_f32<T>(v[0]);

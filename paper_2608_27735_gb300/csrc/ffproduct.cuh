@@ -93,18 +93,25 @@ __device__ __forceinline__ float inverse_of(float x) {
   return r;
 }
 __device__ __forceinline__ float sigmoid_of(float z) { return inverse_of(1.f + exp2_of(-1.44269504f * z)); }
-// The normal distribution's Phi(z) and e = exp(-z^2 / 2): Abramowitz and Stegun, Handbook of
-// Mathematical Functions, 7.1.26 (erf within 1.5e-7), with x = |z| / sqrt(2).
-__device__ __forceinline__ float phi_of(float z, float& e) {
-  const float x = fabsf(z) * 0.70710678f;
-  const float t = inverse_of(1.f + 0.3275911f * x);
+// The normal distribution's Phi(z) and e = exp(-z^2 / 2).  Far below zero Phi is as small as e, and an
+// error that is small beside one is large beside it, so the tail is taken relative to itself: of 32-bit
+// matrices by the device's erfc (z^2 / 2 units of z's rounding, and a few of its own), of 16-bit ones as e
+// times a polynomial in t = 1 / (1 + 0.3 |z|), whose coefficients were fitted here to
+// exp(z^2 / 2) Phi(-|z|) by weighted minimax: in 32 bits Phi within 4.2e-7, and within 1.8e-5 of itself down
+// to z = -13, below half a unit of the 16-bit types.
+template <bool F32> __device__ __forceinline__ float phi_of(float z, float& e) {
   e = exp2_of(-0.72134752f * z * z);
-  const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-  return z < 0.f ? tail : 1.f - tail;
+  if constexpr (F32) {
+    return 0.5f * erfcf(-0.70710678f * z);
+  } else {
+    const float t = inverse_of(1.f + 0.3f * fabsf(z));
+    const float tail = e * t * (0.120121039f + t * (0.113127187f + t * (0.147127926f + t * (-0.0232996624f + t * (0.222333118f + t * -0.0794098675f)))));
+    return z < 0.f ? tail : 1.f - tail;
+  }
 }
 __device__ __forceinline__ float relu_of(float z) { return z > 0.f ? z : (z == z ? 0.f : z); }
 
-template <int N> __device__ __forceinline__ void act_values(float (&z)[N], int act) {
+template <bool F32, int N> __device__ __forceinline__ void act_values(float (&z)[N], int act) {
   if (act == ABCD_SILU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) z[i] *= sigmoid_of(z[i]);
@@ -112,7 +119,7 @@ template <int N> __device__ __forceinline__ void act_values(float (&z)[N], int a
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float e;
-      z[i] *= phi_of(z[i], e);
+      z[i] *= phi_of<F32>(z[i], e);
     }
   } else {
 #pragma unroll
@@ -120,7 +127,7 @@ template <int N> __device__ __forceinline__ void act_values(float (&z)[N], int a
   }
 }
 // z becomes act(z), s its slope.
-template <int N> __device__ __forceinline__ void act_slopes(float (&z)[N], float (&s)[N], int act) {
+template <bool F32, int N> __device__ __forceinline__ void act_slopes(float (&z)[N], float (&s)[N], int act) {
   if (act == ABCD_SILU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -132,7 +139,7 @@ template <int N> __device__ __forceinline__ void act_slopes(float (&z)[N], float
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float e;
-      const float c = phi_of(z[i], e);
+      const float c = phi_of<F32>(z[i], e);
       s[i] = c + z[i] * 0.39894228f * e;
       z[i] *= c;
     }
@@ -636,7 +643,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
               pack_all(v, x[1], bf16);
               pack_all(u, x[2], bf16);
             }
-            act_values(v, a.act);
+            act_values<F32>(v, a.act);
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] *= u[e];
             pack_all(v, x[0], bf16);
@@ -655,7 +662,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
             __syncwarp();
             if (lane == 0) mbar_arrive(slot_empty + 8 * slot);
             __syncwarp();
-            act_slopes(z, d, a.act);
+            act_slopes<F32>(z, d, a.act);
             tmem_load_wait(v);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -832,7 +839,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
             store_matrix<F32, P::CW>(v, a.g[0], m, n + c, rows, w, bf16, buffer);
             store_matrix<F32, P::CW>(u, a.g[1], m, n + c, rows, w, bf16, buffer);
           }
-          act_values(v, a.act);
+          act_values<F32>(v, a.act);
 #pragma unroll
           for (int q = 0; q < P::CW; ++q) v[q] *= u[q];
           store_operand<F32, P::CW>(v, job.c[0], m, n + c, rows, w, bf16, buffer);
@@ -847,7 +854,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
           if (c / 16 + 2 < TURNS) ask(p, c / 16 + 2);
           else ask(then, c / 16 + 2 - TURNS);
           sum_columns(c, 0, v);
-          act_slopes(z, s, a.act);
+          act_slopes<F32>(z, s, a.act);
           tmem_load_wait(v);
           if (last) release();
 #pragma unroll

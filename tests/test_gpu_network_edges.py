@@ -1,5 +1,7 @@
 """The network operators where they can go wrong: rows without spread, tails of the activations, calls
 between a pass and its backward pass, other streams, waits that run out."""
+import math
+
 import numpy as np
 import pytest
 
@@ -46,6 +48,62 @@ def test_norm_of_constant_rows_at_any_width(ctx, kind, cols, pad, lead):
     want = f64(dy).sum(0)
     mag = np.abs(f64(dy)).sum(0)
     close(db, want, 22 * N.EPS * mag + (np.abs(want) + 22 * N.EPS * mag) * N.UNIT[kind] + N.TINY[kind])
+
+
+# ---- gated feed-forward
+
+def gelu_parts(z):
+    """Phi(z), z phi(z) and what 32 bits may add to each, relative to itself.  z^2 / 2 is rounded three
+    times on its way into an exponential (or into erfc, whose logarithm falls like it): 2^-24 z^2 / 2 each
+    and so at most 0.7 z^2 EPS; the functions and products are good to 12 EPS."""
+    cdf = 0.5 * np.vectorize(math.erfc)(-z / math.sqrt(2.0))
+    return cdf, z * np.exp(-z * z / 2) / math.sqrt(2 * math.pi), (0.7 * z * z + 12) * N.EPS
+
+
+# 16-bit matrices: the tail's polynomial, 1.8e-5 of itself
+TAIL = {"f32": 0.0, "f16": 1.8e-5, "bf16": 1.8e-5}
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows", [5, 300, 3000])
+def test_gelu_far_below_zero(ctx, kind, rows):
+    """gelu of -8 ... -3 is as small as 1e-15, and as exact as elsewhere relative to itself: through
+    unit matrices, so that y is the hidden matrix, whose up projection is large."""
+    d = 64
+    r = np.random.default_rng(rows)
+    x = matrix(r.uniform(-8, -3, (rows, d)), kind)
+    one = matrix(np.eye(d), kind)
+    y = blank(rows, d, kind)
+    ctx.reserve_network(rows, d, d, TYPES[kind])
+    ab.abcd_gated_ff(ctx, x, one, matrix(1024 * np.eye(d), kind), one, "gelu", y)
+    ctx.sync()
+    z = f64(x)
+    cdf, _, rel = gelu_parts(z)
+    want = z * cdf * 1024 * z
+    wide = np.abs(want) * (rel + TAIL[kind])
+    # rounded to the type as the hidden matrix; as y it is a value of the type already
+    close(y, want, wide + (np.abs(want) + wide) * N.UNIT[kind] + N.TINY[kind])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_gelu_far_below_zero_backward(ctx, kind):
+    """The same for dG and dU, which unit matrices hand on as the weights' gradients."""
+    d = 64
+    r = np.random.default_rng(41)
+    gate, up = matrix(r.uniform(-8, -3, (d, d)), kind), matrix(np.full((d, d), 2048.0), kind)
+    one, dy = matrix(np.eye(d), kind), matrix(np.eye(d), kind)
+    down = matrix(np.ones((d, d)), kind)
+    dwg, dwu, dwd = (blank(d, d, kind) for _ in range(3))
+    ctx.reserve_network(d, d, d, TYPES[kind])
+    ab.abcd_gated_ff_backward(ctx, dy, one, one, one, down, "gelu", gate, up, None, dwg, dwu, dwd)
+    ctx.sync()
+    z = f64(gate)
+    cdf, zphi, rel = gelu_parts(z)
+    rel = rel + TAIL[kind]
+    for got, want, mag in ((dwg.T, 2048 * (cdf + zphi), 2048 * (cdf + np.abs(zphi))), (dwu.T, z * cdf, np.abs(z) * cdf),
+                           (dwd, 2048 * z * cdf, 2048 * np.abs(z) * cdf)):
+        wide = mag * rel
+        close(got, want, wide + (np.abs(want) + wide) * N.UNIT[kind] + N.TINY[kind])
 
 
 # ---- the block
