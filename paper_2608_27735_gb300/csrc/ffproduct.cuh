@@ -585,7 +585,8 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
     }
   } else if constexpr (P::kBlocks) {
     // Blocks of 32 result columns: the two groups take them in turn.  A wait that gave up skips the
-    // later waits and stores, not the groups' barriers.
+    // later waits and stores, not the groups' barriers; it gives up for the whole warp, whose lanes
+    // meet again below.
     constexpr int BLOCKS = P::kOutCols / 32;
     const int row0 = (int)rank * P::kRows;
     bool ok = true;
@@ -624,8 +625,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
       for (int i = first; i < items; i += step) {
         const Item it = item_of(a, i);
         const int m = it.tm * CG * P::kRows + row0, n0 = it.tn * P::kOutCols;
-        ok = ok && mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead);
-        __syncwarp();
+        ok = __all_sync(~0u, ok && mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead));
         tc_fence_after();
         const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16);
         const int blocks = m < a.job[0].m ? min(BLOCKS, (a.job[0].n - n0 + 31) / 32) : 0;
@@ -651,8 +651,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
             const unsigned at = q + s;
             const int slot = at % P::kSlots;
             const char* block = buffers + (6 + 2 * slot) * P::kBlockBytes;
-            ok = ok && mbar_wait(slot_full + 8 * (at % (2 * P::kSlots)), at / (2 * P::kSlots) & 1, a.limit, &dead);
-            __syncwarp();
+            ok = __all_sync(~0u, ok && mbar_wait(slot_full + 8 * (at % (2 * P::kSlots)), at / (2 * P::kSlots) & 1, a.limit, &dead));
             float z[16], d[16];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
