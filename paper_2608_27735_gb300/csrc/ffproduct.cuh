@@ -586,7 +586,8 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
   } else if constexpr (P::kBlocks) {
     // Blocks of 32 result columns: the two groups take them in turn.  A wait that gave up skips the
     // later waits and stores, not the groups' barriers; it gives up for the whole warp, whose lanes
-    // meet again below.
+    // meet again below.  Nor does it say that a slot or sums are free: the slots' loader would expect a
+    // slot's next block while the last one is still in flight, an arrival too many for its barrier.
     constexpr int BLOCKS = P::kOutCols / 32;
     const int row0 = (int)rank * P::kRows;
     bool ok = true;
@@ -659,7 +660,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
               unpack8(u + 8 * e, *reinterpret_cast<const uint4*>(block + P::kBlockBytes + block_at(row, 2 * half + e)), bf16);
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(slot_empty + 8 * slot);
+            if (ok && lane == 0) mbar_arrive(slot_empty + 8 * slot);
             __syncwarp();
             act_slopes<F32>(z, d, a.act);
             tmem_load_wait(v);
@@ -707,7 +708,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
         q += blocks;
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(empty0 + 8 * buf);
+        if (ok && lane == 0) mbar_arrive_cluster(empty0 + 8 * buf);
         buf ^= 1;
         if (buf == 0) phase ^= 1;
       }

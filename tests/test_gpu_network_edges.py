@@ -230,3 +230,34 @@ def test_block_made_and_dropped_while_its_memory_is_in_use():
     side.reserve_network(n, d, f)
     y2, dx2 = once(side, True)
     assert torch.equal(y, y2) and torch.equal(dx, dx2)
+
+
+# ---- waits
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,d,f", [(77, 64, 130), (3001, 72, 1032), (20000, 256, 1024)])
+def test_waits_that_run_out_in_part(kind, n, d, f):
+    """With few polls some waits of the products give up and others do not: the calls end, and once the
+    limit is back and the status cleared they are right again.  (Which waits give up is a matter of
+    chance, and so is whether the status says so.)"""
+    from .test_gpu_network import everything, flat, make_everything
+    args, out = make_everything(n, d, f, kind, 24)
+    c = ab.Context(0)
+    c.reserve_network(n, d, f, TYPES[kind])
+    everything(c, *args, out)
+    c.sync()
+    want = flat(out)
+    x, dy, w, wg, wu, wd = args
+    for polls in (1, 2, 3, 5, 10, 30, 100, 300):
+        assert ab.lib().abcd_set_wait_limit(c.h, polls) == ab.ABCD_OK
+        ab.abcd_gated_ff(c, x, wg, wu, wd, "silu", out[0], out[1], out[2])
+        ab.abcd_gated_ff_backward(c, dy, x, wg, wu, wd, "silu", out[1], out[2], out[5], *out[-1])
+        try:
+            c.sync()
+        except ab.AbcdError as e:
+            assert e.status == ab.ABCD_ERR_TIMEOUT
+        c.clear_status()
+    assert ab.lib().abcd_set_wait_limit(c.h, 1 << 20) == ab.ABCD_OK
+    everything(c, *args, out)
+    c.sync()
+    assert all(torch.equal(a, b) for a, b in zip(flat(out), want))
