@@ -502,15 +502,15 @@ abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix* dy, const
  * given: x w_gate^T and x w_up^T, which the backward pass reads.  The hidden matrix
  * act(gate) * up is rounded to the matrices' type between the two products.  In 32 bits a factor is
  * taken as three 16-bit terms (24 bits together), so one beyond 3.38e38 or infinite gives NaN.  y may
- * be x; no other output may overlap an operand or an output. */
+ * be x; any other output that overlaps an operand or an output is refused. */
 abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const abcd_matrix* w_gate,
                           const abcd_matrix* w_up, const abcd_matrix* w_down, int activation,
                           const abcd_matrix* y, const abcd_matrix* gate, const abcd_matrix* up);
 /* Its backward pass.  With dh = dy w_down, du = dh act(gate), dg = dh up act'(gate):
  * dx = dg w_gate + du w_up, dw_gate = dg^T x, dw_up = du^T x, dw_down = dy^T (act(gate) * up); each
  * may be NULL, and the weights' gradients are zero without rows.  act'(0) of ABCD_RELU is 0.  dg,
- * du and the hidden matrix are rounded to the matrices' type between the products.  No gradient may
- * overlap an operand or another gradient: they are written side by side. */
+ * du and the hidden matrix are rounded to the matrices' type between the products.  A gradient
+ * that overlaps an operand or another gradient is refused: they are written side by side. */
 abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* dy, const abcd_matrix* x,
                                    const abcd_matrix* w_gate, const abcd_matrix* w_up,
                                    const abcd_matrix* w_down, int activation,

@@ -395,11 +395,11 @@ bool shape_is(const abcd_matrix* m, int dtype, long long rows, long long cols) {
   return matrix_ok(m) && m->dtype == dtype && m->rows == rows && m->cols == cols;
 }
 
-// Whether a result starts where an operand or another result does; one that is not given starts nowhere.
+// Whether a result overlaps an operand or another result; one that is not given lies nowhere.
 bool same_place(std::initializer_list<const abcd_matrix*> results, std::initializer_list<const abcd_matrix*> operands) {
   for (auto r = results.begin(); r != results.end(); ++r) {
     if (!*r) continue;
-    const auto at = [&](const abcd_matrix* m) { return m && m->data == (*r)->data; };
+    const auto at = [&](const abcd_matrix* m) { return m && overlap(m, *r); };
     if (std::any_of(operands.begin(), operands.end(), at) || std::any_of(results.begin(), r, at)) return true;
   }
   return false;
@@ -477,7 +477,7 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: unknown activation", what);
   if (m == 0) return ABCD_OK;
   if (same_place({gate, up}, {x, w_gate, w_up, w_down, y}) || same_place({y}, {w_gate, w_up, w_down}))
-    return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: an output is an operand or another output", what);
+    return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: an output overlaps an operand or another output", what);
   Scratch need{nullptr};
   if (m <= kFewRows) {
     need.operand(m, f, ABCD_F32);                  // room for the hidden matrix in any type
@@ -547,7 +547,7 @@ extern "C" abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* 
     return ABCD_OK;
   }
   if (same_place({dx, dw_gate, dw_up, dw_down}, {dy, x, w_gate, w_up, w_down, gate, up}))
-    return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: a gradient is an operand or another gradient", what);
+    return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: a gradient overlaps an operand or another gradient", what);
   Scratch need{nullptr};
   need.take(kPartBytes);
   if (needs_pack(dy)) need.operand(m, d, t);

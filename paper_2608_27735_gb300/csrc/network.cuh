@@ -4,6 +4,9 @@
 
 #include <cuda_bf16.h>
 
+#include <algorithm>
+#include <utility>
+
 #include "abcd_internal.cuh"
 
 namespace abcd {
@@ -35,6 +38,41 @@ inline bool same_form(const abcd_matrix* a, const abcd_matrix* b) {
 inline bool rows_aligned(const abcd_matrix* m, size_t bytes) {
   return (((uintptr_t)m->data | (m->rows > 1 ? (size_t)m->stride * elem_size(m->dtype) : 0)) &
           (bytes - 1)) == 0;
+}
+
+// Whether an element of one matrix lies where one of the other does.  Both may be columns of one buffer,
+// their rows in turn: rows equally far apart are compared once, others row by row (of the matrix with
+// fewer), which only matrices that reach into one another come to.
+inline bool overlap(const abcd_matrix* a, const abcd_matrix* b) {
+  if (a->rows == 0 || b->rows == 0) return false;
+  struct Rows { uintptr_t first; long long n, width, step; };
+  const auto rows_of = [](const abcd_matrix* m) {
+    const long long e = (long long)elem_size(m->dtype);
+    Rows r{(uintptr_t)m->data, m->rows, m->cols * e, m->stride * e};
+    if (r.n == 1 || r.step == r.width) r = Rows{r.first, 1, r.n * r.width, r.n * r.width};   // one piece
+    return r;
+  };
+  Rows p = rows_of(a), q = rows_of(b);
+  if (p.n > q.n) std::swap(p, q);
+  const auto end = [](const Rows& r) { return r.first + (uintptr_t)(r.n - 1) * (uintptr_t)r.step + (uintptr_t)r.width; };
+  if (end(p) <= q.first || end(q) <= p.first) return false;
+  // whether the bytes [from, from + width), counted from q's first row, meet a row of q
+  const auto meets = [&](long long from, long long width) {
+    const long long row = from < 0 ? 0 : from / q.step;          // the last that starts at or before them
+    return (row < q.n && row * q.step < from + width && from < row * q.step + q.width) ||
+           (row + 1 < q.n && (row + 1) * q.step < from + width);
+  };
+  const long long from = (long long)(p.first - q.first);
+  if (p.step == q.step && p.n > 1) {
+    // row i of p against rows i + k of q: the two k whose rows may meet it
+    const long long k = from >= 0 ? from / q.step : -((-from + q.step - 1) / q.step);
+    const auto pair = [&](long long k) { return std::max(0LL, -k) < std::min(p.n, q.n - k); };
+    const long long at = from - k * q.step;                      // of p's row within that of q
+    return (pair(k) && at < q.width) || (pair(k + 1) && at + p.width > q.step);
+  }
+  for (long long i = 0; i < p.n; ++i)
+    if (meets(from + i * p.step, p.width)) return true;
+  return false;
 }
 
 __device__ __forceinline__ float to_f32(float v) { return v; }

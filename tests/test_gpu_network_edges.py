@@ -261,3 +261,39 @@ def test_waits_that_run_out_in_part(kind, n, d, f):
     everything(c, *args, out)
     c.sync()
     assert all(torch.equal(a, b) for a, b in zip(flat(out), want))
+
+
+# ---- refusals
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_ff_refuses_outputs_that_overlap_in_part(ctx, kind):
+    """An output that reaches into an operand or another output is refused wherever it starts; columns
+    of one buffer next to each other are taken."""
+    n, d, f = 20, 24, 40
+    buf = torch.zeros(300, 400, dtype=TYPES[kind], device="cuda")
+    at = lambda rows, cols, row, col: buf[row:row + rows, col:col + cols]
+    x, wg, wu, wd = at(n, d, 0, 0), at(f, d, 0, 24), at(f, d, 0, 48), at(d, f, 0, 72)
+    y, gate, up = at(n, d, 0, 112), at(n, f, 0, 136), at(n, f, 0, 176)
+    dy, dx = at(n, d, 0, 216), at(n, d, 0, 240)
+    dwg, dwu, dwd = at(f, d, 0, 264), at(f, d, 0, 288), at(d, f, 0, 312)
+    ctx.reserve_network(n, d, f, TYPES[kind])
+    forward = lambda y, gate, up: ab.abcd_gated_ff(ctx, x, wg, wu, wd, "silu", y, gate, up)
+    backward = lambda *g: ab.abcd_gated_ff_backward(ctx, dy, x, wg, wu, wd, "silu", gate, up, *g)
+    forward(y, gate, up)
+    forward(x, gate, up)
+    backward(dx, dwg, dwu, dwd)
+    ctx.sync()
+    x.zero_()
+    for call, args in ((forward, (at(n, d, 3, 25), gate, up)),          # y in w_gate
+                       (forward, (y, at(n, f, 19, 100), up)),           # gate's first row in w_down's
+                       (forward, (y, gate, at(n, f, 1, 137))),          # up in gate
+                       (forward, (y, at(n, f, 10, 111), up)),           # gate in y
+                       (backward, (at(n, d, 19, 216), dwg, dwu, dwd)),  # dx's first row in dy's last
+                       (backward, (at(n, d, 0, 239), dwg, dwu, dwd)),   # dx by one column
+                       (backward, (dx, at(f, d, 39, 288), dwu, dwd)),   # dw_gate in dw_up
+                       (backward, (dx, dwg, dwu, at(d, f, 0, 311)))):   # dw_down in dw_up by one column
+        with pytest.raises(ab.AbcdError) as e:
+            call(*args)
+        assert e.value.status == ab.ABCD_ERR_INVALID_ARG
+    backward(at(n, d, 20, 216), dwg, dwu, dwd)                          # right below dy
+    ctx.sync()

@@ -157,3 +157,51 @@ def test_every_kernel_with_much_shared_memory_has_a_place():
     renderer = 4 + 2 + 1 + 1 + 2                        # visibility, tile rows, ranges, place, loss
     table = int(re.search(r"kSmemKernels = (\d+)", read("abcd_internal.cuh"))[1])
     assert len(kernels) == 62 and len(kernels) + products + renderer <= table
+
+
+def test_overlap_of_matrices_is_that_of_their_elements(tmp_path):
+    """network.cuh's overlap() against every byte of both matrices: rows apart or not, in one buffer,
+    equally far apart or not."""
+    import os
+    import subprocess
+    from paper_2608_27735_gb300 import _build
+    src, exe = tmp_path / "overlap.cu", tmp_path / "overlap"
+    src.write_text(r"""
+#include <cstdio>
+#include <cstdlib>
+#include <vector>
+#include "network.cuh"
+using namespace abcd;
+static int draw(int n) { return rand() / 7 % n; }
+int main() {
+  long both[2] = {0, 0}, wrong = 0;
+  srand(5);
+  for (long k = 0; k < 400000; ++k) {
+    abcd_matrix m[2];
+    const int common = 1 + draw(12);
+    for (auto& q : m) {
+      q.dtype = draw(2) ? ABCD_F32 : ABCD_F16;
+      const int e = (int)elem_size(q.dtype);
+      q.rows = draw(7);
+      q.cols = 1 + draw(6);
+      q.stride = draw(2) ? q.cols + draw(8) : std::max<long long>(q.cols, common * 4 / e);
+      q.data = (void*)(uintptr_t)(4096 + e * draw(40));
+    }
+    std::vector<char> seen(8192, 0);
+    bool meet = false;
+    for (int w = 0; w < 2; ++w)
+      for (long long r = 0; r < m[w].rows; ++r)
+        for (long long b = 0; b < m[w].cols * (long long)elem_size(m[w].dtype); ++b) {
+          char& c = seen[(uintptr_t)m[w].data - 4096 + r * m[w].stride * elem_size(m[w].dtype) + b];
+          if (w && c) meet = true;
+          if (!w) c = 1;
+        }
+    ++both[meet];
+    wrong += overlap(&m[0], &m[1]) != meet || overlap(&m[1], &m[0]) != meet;
+  }
+  printf("%ld %ld %ld\n", both[0], both[1], wrong);
+}
+""")
+    subprocess.run([_build.nvcc(), *_build.ARCH, *_build.FLAGS, "-I", _build.CSRC, str(src), "-o", str(exe)], check=True)
+    apart, meeting, wrong = map(int, subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split())
+    assert apart > 50000 and meeting > 50000 and wrong == 0
