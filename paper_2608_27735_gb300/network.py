@@ -180,6 +180,7 @@ class FeedForwardBlock:
         self.rstd = torch.empty_like(self.mean)
         self.grads = {k: torch.empty_like(t) for k, t in self.w.items()}
         self.offset = 0
+        self.kept = None                                # rows of the last training pass
         ctx.hold(self.normed, self.out, self.gate, self.up, self.d_out, self.d_normed, self.mean, self.rstd,
                  *self.grads.values())
         ctx.reserve_network(self.rows, self.cols, self.ff, dt)
@@ -200,17 +201,20 @@ class FeedForwardBlock:
             abcd_dropout(self.ctx, out, 0.0, self.seed, 0, y, x)
             return
         nx, out = self.normed[:n], self.out[:n]
-        self.drawn = self.offset
+        self.kept, self.drawn = None, self.offset
         self.offset += self._counters(n)
         abcd_layer_norm(self.ctx, x, w["norm_w"], w["norm_b"], self.eps, nx, self.mean[:n],
                         self.rstd[:n])
         abcd_gated_ff(self.ctx, nx, w["w_gate"], w["w_up"], w["w_down"], self.act, out,
                       self.gate[:n], self.up[:n])
         abcd_dropout(self.ctx, out, self.p, self.seed, self.drawn, y, x)
+        self.kept = n
 
     def backward(self, dy, x, dx):
         """dx (may be dy) and `grads` of the last forward(x, ..., train=True); x as it was given."""
         n, w, g = x.shape[0], self.w, self.grads
+        if n != self.kept:
+            raise ValueError(f"x has {n} rows, the last training pass {self.kept}")
         d_out, d_nx = self.d_out[:n], self.d_normed[:n]
         abcd_dropout_backward(self.ctx, dy, self.p, self.seed, self.drawn, d_out)
         abcd_gated_ff_backward(self.ctx, d_out, self.normed[:n], w["w_gate"], w["w_up"],

@@ -297,3 +297,21 @@ def test_ff_refuses_outputs_that_overlap_in_part(ctx, kind):
         assert e.value.status == ab.ABCD_ERR_INVALID_ARG
     backward(at(n, d, 20, 216), dwg, dwu, dwd)                          # right below dy
     ctx.sync()
+
+
+def test_block_refuses_a_backward_pass_without_its_pass(ctx):
+    r = np.random.default_rng(35)
+    w = {"norm_w": torch.ones(24, device="cuda"), "norm_b": torch.zeros(24, device="cuda"),
+         **{k: matrix(r.normal(size=s), "f32") for k, s in (("w_gate", (40, 24)), ("w_up", (40, 24)), ("w_down", (24, 40)))}}
+    block = ab.FeedForwardBlock(ctx, w, 50)
+    x, y = matrix(r.normal(size=(20, 24)), "f32"), blank(20, 24, "f32")
+    with pytest.raises(ValueError):
+        block.backward(x, x, y)
+    block.forward(x, y, train=False)
+    with pytest.raises(ValueError):
+        block.backward(x, x, y)
+    block.forward(x, y)
+    with pytest.raises(ValueError):
+        block.backward(x[:10], x[:10], y[:10])
+    block.backward(x, x, y)
+    ctx.sync()
