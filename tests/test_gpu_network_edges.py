@@ -315,3 +315,32 @@ def test_block_refuses_a_backward_pass_without_its_pass(ctx):
         block.backward(x[:10], x[:10], y[:10])
     block.backward(x, x, y)
     ctx.sync()
+
+
+# ---- long and many rows
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,cols", [(900, 17003), (1000, 9001), (1500, 4097), (3000, 1100), (6000, 520), (20000, 59)])
+@pytest.mark.parametrize("pad,lead", [(0, 0), (5, 3), (16, 8)])
+def test_norm_of_many_rows(ctx, kind, rows, cols, pad, lead):
+    """Several rows per CTA at every row length (rows ahead, barriers and sums used again), and dx over the
+    residual's gradient."""
+    r = np.random.default_rng(rows + cols)
+    x = matrix(r.normal(0.5, 1, (rows, cols)), kind, pad, lead)
+    dy = matrix(r.normal(0, 0.3, (rows, cols)), kind, pad, lead)
+    res = matrix(r.normal(size=(rows, cols)), kind, pad, lead)
+    w = torch.as_tensor(r.normal(1, 0.3, cols)).to("cuda", TYPES[kind])
+    X, DY, R, W = f64(x), f64(dy), f64(res), f64(w)
+    y = blank(rows, cols, kind, pad, lead)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    dw, db = torch.full_like(w, float("nan")), torch.full_like(w, float("nan"))
+    ctx.reserve_network(rows, cols)
+    ab.abcd_layer_norm(ctx, x, w, None, 1e-5, y, mean, rstd)
+    ab.abcd_layer_norm_backward(ctx, dy, x, w, mean, rstd, res, dw, db, res)
+    ctx.sync()
+    close(y, N.norm(X, W, 0 * W, 1e-5)[0], N.norm_bound(X, W, 0 * W, 1e-5, kind))
+    m32, r32 = f64(mean)[:, None], f64(rstd)[:, None]
+    bounds = N.norm_grad_bounds(DY, X, W, m32, r32, kind, kind, R)
+    want = N.norm_grad(DY, X, W, m32, r32)
+    for got, exact, bound in zip((res, dw, db), (want[0] + R, *want[1:]), bounds):
+        close(got, exact, bound)
