@@ -124,7 +124,8 @@ const char* abcd_last_error(const abcd_ctx* ctx);
 long long abcd_launch_count(const abcd_ctx* ctx);
 /* Bound on the polls of a device-side wait (the radix sort's decoupled look-back waits for the
  * tiles before its own, whose CTAs are already running; the gated feed-forward products' warps wait for
- * one another's stages) [2^20, about 40 ms]: a wait that
+ * one another's stages) [2^20: about 40 ms of the look-back's, 1.5 s of the products', whose
+ * polls take 1.4 us each]: a wait that
  * reaches it gives up, the call's results are wrong and ABCD_ERR_TIMEOUT is set in the status
  * word (abcd_sync); nothing hangs, and later calls run normally once the status is cleared. */
 abcd_status abcd_set_wait_limit(abcd_ctx* ctx, unsigned polls);
@@ -500,16 +501,19 @@ abcd_status abcd_layer_norm_backward(abcd_ctx* ctx, const abcd_matrix* dy, const
 /* Gated feed-forward layer: y = (act(x w_gate^T) * (x w_up^T)) w_down^T.  x, y [rows][d];
  * w_gate, w_up [ff][d]; w_down [d][ff]; all of one type.  gate, up [rows][ff], both NULL or both
  * given: x w_gate^T and x w_up^T, which the backward pass reads.  The hidden matrix
- * act(gate) * up is rounded to the matrices' type between the two products.  In 32 bits a factor is
- * taken as three 16-bit terms (24 bits together), so one beyond 3.38e38 or infinite gives NaN.  y may
- * be x; any other output that overlaps an operand or an output is refused. */
+ * act(gate) * up is rounded to the matrices' type between the two products (in fp16 beyond 65,504 to
+ * infinity); who needs it wider hands over all matrices in 32 bits.  There a factor is taken as three
+ * 16-bit terms (24 bits together) when there are more than eight tokens, so one beyond 3.38e38 or
+ * infinite gives NaN; up to eight tokens are multiplied as they are.  y may be x; any other output that overlaps an operand or an output is refused. */
 abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const abcd_matrix* w_gate,
                           const abcd_matrix* w_up, const abcd_matrix* w_down, int activation,
                           const abcd_matrix* y, const abcd_matrix* gate, const abcd_matrix* up);
 /* Its backward pass.  With dh = dy w_down, du = dh act(gate), dg = dh up act'(gate):
  * dx = dg w_gate + du w_up, dw_gate = dg^T x, dw_up = du^T x, dw_down = dy^T (act(gate) * up); each
  * may be NULL, and the weights' gradients are zero without rows.  act'(0) of ABCD_RELU is 0.  dg,
- * du and the hidden matrix are rounded to the matrices' type between the products.  A gradient
+ * du and the hidden matrix are rounded to the matrices' type between the products (in fp16 below 6e-8
+ * to zero: scale the loss), and gate and up were when they were saved; in 32 bits a factor that is
+ * infinite or beyond 3.38e38 gives NaN, whatever the number of tokens.  A gradient
  * that overlaps an operand or another gradient is refused: they are written side by side. */
 abcd_status abcd_gated_ff_backward(abcd_ctx* ctx, const abcd_matrix* dy, const abcd_matrix* x,
                                    const abcd_matrix* w_gate, const abcd_matrix* w_up,

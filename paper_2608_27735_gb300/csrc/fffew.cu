@@ -8,9 +8,10 @@
 // tokens' (from L1) into 32-bit sums, and the lanes' and warps' are added in a fixed order.  The second
 // kernel may start while the first runs: it asks for its weight row, which the first does not write,
 // before it waits for the hidden matrix.  1 x 1,024 x 4,096 bf16 takes 6.1 and 4.4 us with its weights
-// in L2; the call is then the host's time.  Four tokens take 16 us, eight 23, as much as nine take on
-// the tensor cores (23, of which 3 join the splits).  Weight rows that are not whole pieces on 16-byte boundaries
-// go element by element.
+// in L2; the call is then the host's time.  Two tokens take 8.9 us, four
+// 13.8, eight 21.7: each lane converts and multiplies every weight once per token.  Nine take 25.7 on the
+// tensor cores, of which 3 join the splits.  Weight rows that are not whole pieces on 16-byte boundaries go
+// element by element: 1, 4 and 8 tokens of 1,025 x 4,097 bf16 take 15, 29 and 50 us.
 #include <algorithm>
 
 #include "ffproduct.cuh"

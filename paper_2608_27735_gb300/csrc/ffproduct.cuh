@@ -933,7 +933,11 @@ abcd_status launch_product(abcd_ctx* ctx, const ProductArgs& a) {
 // of them per SM).
 // What they cost, in us: fitted to 324 products of 300 to 20,000 tokens of widths 64 x 256, 256 x 1,024
 // and 768 x 2,048 in 16 and 32 bits, each timed in all three shapes (the fit is within 8% rms, and its
-// choices took 0.6% longer in all than the best ones).
+// choices took 0.6% longer in all than the best ones).  Outside of those, both passes of 1,500 x 28 x 112,
+// 8,000 x 1,024 x 4,096 and 1,000,000 x 64 x 256 in 32 bits and of 300 x 2,048 x 8,192, 5,430 x 1,713 x
+// 1,601, 40,000 x 1,024 x 1,024 and 16,384 x 2,048 x 8,192 in 16 take at most 4% more than with the best
+// one shape for all products of a call.  6,007 x 39 x 6,591 in 32 bits does not: its forward pass takes 363
+// us in the smallest tile, 237 in the large one.
 struct Shape {
   int cg, bn, ctas;          // CTAs of a tile, its sums per row, CTAs per SM (one for kDown)
   double fixed;              // of a launch
