@@ -3,9 +3,9 @@
 //   g = dy w, xh = (x - mean) rstd:  dx = rstd (g - mean(g) - xh mean(g xh)),
 //   dw = sum_rows dy xh,  db = sum_rows dy.
 // The variance is taken from the deviations, not from the difference of two moments, so a mean far
-// from zero costs it no digits.  The deviations are from a mean whose sum and division have rounded, and
-// their own mean, what that one is off by, corrects it (rows of one value then have that value as their
-// mean: without this 1,000 columns of 1000.0 had one a unit higher, and xh of 0.019 instead of 0).
+// from zero costs it no digits.  Rows of one value have that value as their mean: what the division rounds
+// is taken back, and where the sum may have rounded too, the deviations' own mean is.  (With a sum times a
+// rounded reciprocal alone, 1,000 columns of 1000.0 had a mean one unit higher, and xh of 0.019 instead of 0.)
 //
 // Bound by HBM (forward x -> y, backward x, dy -> dx).  A row is read once: TPR lanes (part of a
 // warp, a warp, or a CTA) hold it in registers, NV vectors of V consecutive elements (16 bytes) each;
@@ -66,6 +66,8 @@ template <int TPR_, int V_, int NV_, bool BWD, bool SHIFT> struct RowShape {
   // the registers of three CTAs, or of four in 32 bits (1,000,000 x 64 bf16: 75 us, and 89 with two CTAs
   // of as many registers as they like; rows that start anywhere of eight values a thread spill at three).
   static constexpr bool kShort = V * NV <= 8;
+  // Whether the sum of a row of one value may round: of up to 8,192 16-bit values (11 bits each) it is exact.
+  static constexpr bool kRounds = V == 4 || kCapacity > 8192;
   static constexpr int kCtas = kThreads > 256 || kSmem > 100 * 1024 ? 1
                                : !kShort || (BWD && SHIFT && V * NV == 8) ? 2
                                : BWD && (SHIFT || V * NV == 8) ? 3 : 4;
@@ -336,28 +338,39 @@ __global__ void __launch_bounds__(R::kThreads, R::V * R::NV == 32 ? R::kCtas : 0
       for (int i = 0; i < V; ++i) s += v[j][i];
     }
     row_sum2<TPR>(s, unused, red, 0);
-    const float about = s * inv;
+    // the division's rounding taken back, then, where the sum has rounded too, the sum's
+    float mean = s * inv;
+    mean = __fmaf_rn(__fmaf_rn(-mean, (float)a.cols, s), inv, mean);
     float e = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int left = ring.left - j * TPR * V;
       if (left < V) {                                  // past the row's end nothing deviates
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[j][i] = i < left ? v[j][i] : about;
+        for (int i = 0; i < V; ++i) v[j][i] = i < left ? v[j][i] : mean;
       }
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float d = v[j][i] - about;
+        const float d = v[j][i] - mean;
         q += d * d;
-        e += d;
+        if constexpr (R::kRounds) e += d;
+        else v[j][i] = d;
       }
     }
     row_sum2<TPR>(q, e, red, 1);
-    const float mean = about + e * inv, rstd = rstd_of(q * inv, e * inv, a.eps);
+    e *= inv;
+    if constexpr (R::kRounds) {
+      mean += e;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[j][i] -= mean;
+    }
+    const float rstd = rstd_of(q * inv, e, a.eps);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[j][i] = (v[j][i] - mean) * rstd * w[j][i] + b[j][i];
+      for (int i = 0; i < V; ++i) v[j][i] = v[j][i] * rstd * w[j][i] + b[j][i];
       ring.put(v[j], t, j, y);
     }
     ring.flush(t, y);
