@@ -17,7 +17,7 @@
 // second kernel adds them in their order.
 // Rows that start anywhere are bound by instructions (each vector is put together from two pieces, results
 // go to shared memory element by element, and the row's threads meet three times a turn): 1,000,000 x 59
-// without gaps 152 and 208 us in fp32, 128 and 189 in fp16; with rows 64 apart 117 and 138, 72 and 89.
+// without gaps 156 and 208 us in fp32, 124 and 190 in fp16; with rows 64 apart 120 and 138, 74 and 89.
 #include <algorithm>
 #include <type_traits>
 
@@ -306,7 +306,7 @@ template <typename T, typename R> struct RowRing {
 };
 
 // (Rows of 32 values a thread are held to the registers of the CTAs that the grid counts on: 10,000 x 1,500
-// fp32 27 us, and 29 with 141 registers.)
+// fp32 25 us, and 29 with 141 registers.)
 template <typename T, typename R>
 __global__ void __launch_bounds__(R::kThreads, R::V * R::NV == 32 ? R::kCtas : 0) norm_fwd_kernel(const __grid_constant__ NormArgs a) {
   constexpr int V = R::V, NV = R::NV, TPR = R::TPR;
