@@ -268,7 +268,7 @@ def _ready(s):
     elif c["op"] == "keep":
         s["packed"] = ab.Packed8(m, d)
     else:
-        _context.reserve_network(m, d, c["ff"], t)
+        _context.reserve_packed8(m, d, c["ff"], t)
         s["packed"] = ab.Packed8(m, d), ab.Packed8(m, c["ff"]), ab.Packed8(m, c["ff"])
     return _context
 
