@@ -538,6 +538,128 @@ abcd_status abcd_dropout_backward(abcd_ctx* ctx, const abcd_matrix* dy, double p
                                   unsigned long long seed, unsigned long long offset,
                                   const abcd_matrix* dx);
 
+/* ---- tokens of that network: lookups, products, the sums between blocks, what is kept ------- *
+ * The rules of the calls above hold here too: types, rows, 32-bit sums, one rounding, the same result
+ * in every run.  Each call that takes scratch names the function that says how much; the network
+ * workspace is one for all of them, as large as the largest needs. */
+
+/* Types of an index vector. */
+enum { ABCD_I32 = 3, ABCD_I64 = 4 };
+
+/* Bytes of network workspace that abcd_embedding_backward takes for up to `tokens` tokens of up to `cols`
+ * columns that name rows of a table of up to `table_rows` (the forward pass: its header, which any size
+ * has). */
+abcd_status abcd_embedding_workspace_size(long long tokens, long long table_rows, long long cols,
+                                          size_t* bytes);
+/* Embedding: y[t] = add[t] + scale table[index[t]] for each row t of y; add NULL for none.  index: y's
+ * rows many consecutive ABCD_I32 or ABCD_I64, aligned to their type.  A negative one names no row
+ * (y[t] = add[t], or 0).  One that is not below the table's rows names none either, and is reported:
+ * abcd_sync returns ABCD_ERR_INVALID_ARG until abcd_clear_status.  table, add and y are of one type;
+ * y may be add, and overlaps nothing else.  scale is finite. */
+abcd_status abcd_embedding(abcd_ctx* ctx, const abcd_matrix* table, const void* index, int index_dtype,
+                           float scale, const abcd_matrix* add, const abcd_matrix* y);
+/* Its backward pass: dtable[v] = scale times the sum of dy[t] over the tokens that name row v, zero for
+ * rows that none names; every row is written.  The sums are taken in the tokens' order, in parts.
+ * (add's gradient is dy.)  Indices as above.  dtable overlaps neither dy nor index. */
+abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix* dy, const void* index, int index_dtype,
+                                    float scale, const abcd_matrix* dtable);
+
+/* No activation, of abcd_linear alone. */
+enum { ABCD_NO_ACTIVATION = 3 };
+
+/* Bytes of network workspace that abcd_linear and abcd_linear_backward take for up to `rows` tokens of up
+ * to `cols` columns and results of up to `out`, in type dtype. */
+abcd_status abcd_linear_workspace_size(long long rows, long long cols, long long out, int dtype,
+                                       size_t* bytes);
+/* Linear layer: z = x weight^T + bias, y = residual + act(z).  x [rows][cols]; weight [out][cols]; bias
+ * [out] of type bias_dtype (the matrices' or ABCD_F32), NULL for none; residual, y and z [rows][out], all
+ * of one type.  residual NULL for none; z NULL when the backward pass is not wanted (or takes none).  y
+ * may be residual; other outputs that overlap an operand or each other are refused.  In 32 bits factors
+ * are three 16-bit terms as in abcd_gated_ff, with what is said there of values beyond 3.38e38. */
+abcd_status abcd_linear(abcd_ctx* ctx, const abcd_matrix* x, const abcd_matrix* weight, const void* bias,
+                        int bias_dtype, int activation, const abcd_matrix* residual, const abcd_matrix* y,
+                        const abcd_matrix* z);
+/* Its backward pass: dz = dy act'(z), dx = dz weight, dweight = dz^T x, dbias = the sum of dz's rows; each
+ * may be NULL, and dweight and dbias are zero without rows.  z as the forward pass left it (NULL for
+ * ABCD_NO_ACTIVATION, whose dz is dy).  dz is rounded to the matrices' type between the products (dbias is
+ * summed before).  (residual's gradient is dy.)  A gradient that overlaps an operand or another gradient
+ * is refused. */
+abcd_status abcd_linear_backward(abcd_ctx* ctx, const abcd_matrix* dy, const abcd_matrix* x,
+                                 const abcd_matrix* weight, int activation, const abcd_matrix* z,
+                                 const abcd_matrix* dx, const abcd_matrix* dweight, void* dbias,
+                                 int bias_dtype);
+
+/* A norm of rows of d columns: xh = (x - mean) rstd with rstd = 1 / sqrt(mean of (x - mean)^2 + eps),
+ * result xh weight + bias.  ABCD_RMS_NORM's mean is 0.  weight, bias: [d] of the call's weight_dtype,
+ * either may be NULL (1 and 0).  mean, rstd: [rows] fp32 for the backward pass, NULL when it is not
+ * wanted; ABCD_RMS_NORM takes no mean. */
+enum { ABCD_LAYER_NORM = 0, ABCD_RMS_NORM = 1 };
+typedef struct {
+  int kind;
+  const void* weight;
+  const void* bias;
+  float eps;
+  float* mean;
+  float* rstd;
+} abcd_norm;
+
+/* Bytes of network workspace that abcd_residual_norm_backward takes for up to `rows` rows of up to `cols`
+ * columns. */
+abcd_status abcd_residual_norm_workspace_size(long long rows, long long cols, size_t* bytes);
+/* The end of a block and the start of the next: y = x + scale gate after(f), n = before(y), where x is the
+ * residual stream, f the block's result, `after` the norm that closes the block and `before` the next
+ * block's.  after NULL: f as it is; before NULL: no n (which is then NULL too); gate [cols] of
+ * weight_dtype (the matrices' type or ABCD_F32), NULL for 1.  x, f, y, n are of one form.  n is taken from
+ * y before it is rounded.  y and n may each be x or f (the same rows); the backward pass needs both. */
+abcd_status abcd_residual_norm(abcd_ctx* ctx, const abcd_matrix* x, const abcd_matrix* f,
+                               const abcd_norm* after, const abcd_norm* before, const void* gate,
+                               int weight_dtype, float scale, const abcd_matrix* y, const abcd_matrix* n);
+/* Its backward pass, from x, f and the statistics that the forward pass left (y is made again in 32 bits).
+ * dy: the gradient that reaches y past the next block, NULL for none; dn: that of n, NULL without
+ * `before`, and only then.  With g = dy + before's gradient of dn: dx = g, df = after's gradient of
+ * scale gate g, dgate = the rows' sum of scale g after(f), and the norms' own gradients (NULL where the
+ * norm is).  Each may be NULL.  The vectors are [cols] of weight_dtype and zero without rows.  dx and df
+ * may be dy, dn, x or f. */
+abcd_status abcd_residual_norm_backward(abcd_ctx* ctx, const abcd_matrix* dy, const abcd_matrix* dn,
+                                        const abcd_matrix* x, const abcd_matrix* f, const abcd_norm* after,
+                                        const abcd_norm* before, const void* gate, int weight_dtype,
+                                        float scale, const abcd_matrix* dx, const abcd_matrix* df, void* dgate,
+                                        void* dafter_weight, void* dafter_bias, void* dbefore_weight,
+                                        void* dbefore_bias);
+
+/* A matrix in 8 bits, for what a backward pass needs and a forward pass only stores: each 32 consecutive
+ * columns of a row share a power of two 2^(p - 127), p their byte of `powers`, and an element is its code
+ * (-127 ... 127) times that.  p = max(1, e - 6 + 127) with e the exponent of the group's largest
+ * magnitude, so an element is off by at most a 128th of that magnitude (and 2^-127); a group that
+ * holds an infinity or NaN has p = 255 and reads as NaN. */
+typedef struct {
+  signed char* codes;     /* rows on 32-byte boundaries: aligned, stride a multiple of 32 */
+  unsigned char* powers;
+  long long rows;
+  long long cols;
+  long long stride;       /* bytes between rows of codes, >= cols */
+  long long power_stride; /* bytes between rows of powers, >= cols / 32 rounded up */
+} abcd_packed8;
+
+/* packed = x in 8 bits; the bytes between rows stay as they are.  packed does not overlap x. */
+abcd_status abcd_pack8(abcd_ctx* ctx, const abcd_matrix* x, const abcd_packed8* packed);
+/* y = what packed stands for, rounded to y's type (bf16 and fp32 hold it exactly, fp16 within its range).
+ * y does not overlap packed. */
+abcd_status abcd_unpack8(abcd_ctx* ctx, const abcd_packed8* packed, const abcd_matrix* y);
+
+/* Bytes of network workspace that abcd_gated_ff_backward_packed8 takes, as for
+ * abcd_network_workspace_size. */
+abcd_status abcd_packed8_workspace_size(long long rows, long long cols, long long ff, int dtype,
+                                        size_t* bytes);
+/* abcd_gated_ff_backward with x, gate and up as abcd_pack8 kept them: the same gradients, of what they
+ * stand for. */
+abcd_status abcd_gated_ff_backward_packed8(abcd_ctx* ctx, const abcd_matrix* dy, const abcd_packed8* x,
+                                           const abcd_matrix* w_gate, const abcd_matrix* w_up,
+                                           const abcd_matrix* w_down, int activation,
+                                           const abcd_packed8* gate, const abcd_packed8* up,
+                                           const abcd_matrix* dx, const abcd_matrix* dw_gate,
+                                           const abcd_matrix* dw_up, const abcd_matrix* dw_down);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,7 +21,9 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "abcd.h")
 ABCD_OK, ABCD_ERR_INVALID_ARG, ABCD_ERR_CUDA, ABCD_ERR_CAPACITY, ABCD_ERR_TIMEOUT, \
     ABCD_ERR_WORKSPACE = range(6)
 ABCD_F16, ABCD_F32, ABCD_BF16 = 0, 1, 2
-ABCD_SILU, ABCD_GELU, ABCD_RELU = 0, 1, 2
+ABCD_I32, ABCD_I64 = 3, 4
+ABCD_SILU, ABCD_GELU, ABCD_RELU, ABCD_NO_ACTIVATION = 0, 1, 2, 3
+ABCD_LAYER_NORM, ABCD_RMS_NORM = 0, 1
 ABCD_MAX_CACHE_SLOTS = 4096
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "CUDA", 3: "CAPACITY", 4: "TIMEOUT", 5: "WORKSPACE"}
 TILE = 16
@@ -69,6 +71,16 @@ class abcd_fwd_state(C.Structure):
 class abcd_matrix(C.Structure):
     _fields_ = [("data", C.c_void_p), ("rows", C.c_longlong), ("cols", C.c_longlong),
                 ("stride", C.c_longlong), ("dtype", C.c_int)]
+
+
+class abcd_norm(C.Structure):
+    _fields_ = [("kind", C.c_int), ("weight", C.c_void_p), ("bias", C.c_void_p), ("eps", C.c_float),
+                ("mean", C.c_void_p), ("rstd", C.c_void_p)]
+
+
+class abcd_packed8(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("powers", C.c_void_p), ("rows", C.c_longlong),
+                ("cols", C.c_longlong), ("stride", C.c_longlong), ("power_stride", C.c_longlong)]
 
 
 class abcd_alu_peaks(C.Structure):
@@ -140,6 +152,22 @@ _SIGS = {
                      C.c_void_p],
     "abcd_dropout_backward": [C.c_void_p, C.c_void_p, C.c_double, C.c_ulonglong, C.c_ulonglong,
                               C.c_void_p],
+    "abcd_embedding_workspace_size": [C.c_longlong, C.c_longlong, C.c_longlong,
+                                      C.POINTER(C.c_size_t)],
+    "abcd_embedding": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_float, C.c_void_p, C.c_void_p],
+    "abcd_embedding_backward": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_float, C.c_void_p],
+    "abcd_linear_workspace_size": [C.c_longlong, C.c_longlong, C.c_longlong, C.c_int,
+                                   C.POINTER(C.c_size_t)],
+    "abcd_linear": [C.c_void_p] * 4 + [C.c_int, C.c_int] + [C.c_void_p] * 3,
+    "abcd_linear_backward": [C.c_void_p] * 4 + [C.c_int] + [C.c_void_p] * 4 + [C.c_int],
+    "abcd_residual_norm_workspace_size": [C.c_longlong, C.c_longlong, C.POINTER(C.c_size_t)],
+    "abcd_residual_norm": [C.c_void_p] * 6 + [C.c_int, C.c_float] + [C.c_void_p] * 2,
+    "abcd_residual_norm_backward": [C.c_void_p] * 8 + [C.c_int, C.c_float] + [C.c_void_p] * 7,
+    "abcd_pack8": [C.c_void_p] * 3,
+    "abcd_unpack8": [C.c_void_p] * 3,
+    "abcd_packed8_workspace_size": [C.c_longlong, C.c_longlong, C.c_longlong, C.c_int,
+                                    C.POINTER(C.c_size_t)],
+    "abcd_gated_ff_backward_packed8": [C.c_void_p] * 6 + [C.c_int] + [C.c_void_p] * 6,
     "abcd_measure_alu_peaks": [C.c_int, C.c_void_p],
     "abcd_block_bounds": [C.c_void_p, C.c_void_p, C.c_void_p],
     "abcd_pair_visible": [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(C.c_int)],
@@ -370,13 +398,31 @@ class Context:
         columns, with `ff` hidden ones, of torch type dtype (float32 if None) need more than it
         has.  Call it before a CUDA graph is captured, not inside: a larger workspace replaces
         the one that captured calls use."""
+        self._reserve_network("abcd_network_workspace_size", int(rows), int(cols), int(ff), _dtype_id(dtype))
+
+    def reserve_embedding(self, tokens, table_rows, cols):
+        """As reserve_network, for the embedding calls of up to `tokens` tokens of `cols` columns that name
+        rows of tables of up to `table_rows`."""
+        self._reserve_network("abcd_embedding_workspace_size", int(tokens), int(table_rows), int(cols))
+
+    def reserve_linear(self, rows, cols, out, dtype=None):
+        """As reserve_network, for linear layers from `cols` to `out` columns."""
+        self._reserve_network("abcd_linear_workspace_size", int(rows), int(cols), int(out), _dtype_id(dtype))
+
+    def reserve_residual_norm(self, rows, cols):
+        """As reserve_network, for abcd_residual_norm_backward."""
+        self._reserve_network("abcd_residual_norm_workspace_size", int(rows), int(cols))
+
+    def reserve_packed8(self, rows, cols, ff, dtype=None):
+        """As reserve_network, for abcd_gated_ff_backward_packed8."""
+        self._reserve_network("abcd_packed8_workspace_size", int(rows), int(cols), int(ff), _dtype_id(dtype))
+
+    def _reserve_network(self, call, *sizes):
         torch = _torch()
         nbytes = C.c_size_t()
-        st = lib().abcd_network_workspace_size(int(rows), int(cols), int(ff),
-                                               _dtypes().get(dtype, -1) if dtype is not None else ABCD_F32,
-                                               C.byref(nbytes))
+        st = getattr(lib(), call)(*sizes, C.byref(nbytes))
         if st != ABCD_OK:
-            raise AbcdError(st, "abcd_network_workspace_size")
+            raise AbcdError(st, call)
         if nbytes.value <= self.network_bytes:
             return
         ws = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=self.device)
@@ -406,6 +452,11 @@ def _dtypes():
         _dtype_ids.update({torch.float16: ABCD_F16, torch.float32: ABCD_F32,
                            torch.bfloat16: ABCD_BF16})
     return _dtype_ids
+
+
+def _dtype_id(dtype):
+    """The ABCD_* type of a torch type (None: float32); -1, which every call refuses, of another."""
+    return ABCD_F32 if dtype is None else _dtypes().get(dtype, -1)
 
 
 # ---------------------------------------------------------------------------------------
@@ -727,6 +778,8 @@ def visible_pairs(ctx: Context, blocks, cameras, dims, origin, side, opts=None):
     return out
 
 
-from .network import (FeedForwardBlock, abcd_dropout, abcd_dropout_backward,  # noqa: E402,F401
-                      abcd_gated_ff, abcd_gated_ff_backward, abcd_layer_norm,
-                      abcd_layer_norm_backward)
+from .network import (FeedForwardBlock, Norm, Packed8, abcd_dropout, abcd_dropout_backward,  # noqa: E402,F401
+                      abcd_embedding, abcd_embedding_backward, abcd_gated_ff, abcd_gated_ff_backward,
+                      abcd_gated_ff_backward_packed8, abcd_layer_norm, abcd_layer_norm_backward,
+                      abcd_linear, abcd_linear_backward, abcd_pack8, abcd_residual_norm,
+                      abcd_residual_norm_backward, abcd_unpack8)

@@ -27,6 +27,11 @@ struct FewArgs {
   int rows, k, n, act;
   int x_vec;                          // whether x's rows start on 16-byte boundaries
   int share;                          // warps of a unit
+  // a linear layer: saved[0] its z
+  int linear, wide_bias;
+  const void* bias;                   // [n], or NULL
+  const void* res;                    // [rows][n], or NULL
+  long long sres;
   long long sx, sw[2], sy, ssaved[2];
 };
 
@@ -58,9 +63,11 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_kernel(const __grid_consta
   };
   // up: the grids before this one may have written the weights, and down's grid may start from here on;
   // down: its weights are not the grid before's, and that grid's own wait has seen the ones before end
+  const bool linear = MATS == 1 && a.linear;            // a layer by itself: waits as up does
   if (MATS == 2) pdl_prologue();
+  if (linear) pdl_wait();
   fetch(first);
-  if (MATS == 1) pdl_wait();
+  if (MATS == 1 && !linear) pdl_wait();
   for (int k0 = first; k0 < end; k0 += kFlight * step) {
     if (k0 > first) fetch(k0);
 #pragma unroll
@@ -108,6 +115,12 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_kernel(const __grid_consta
     }
     act_values<sizeof(T) == 4>(v, a.act);
     v[0] *= u;
+  }
+  if (linear) {
+    if (a.bias) v[0] += a.wide_bias ? ((const float*)a.bias)[unit] : to_f32(((const T*)a.bias)[unit]);
+    if (a.saved[0]) ((T*)a.saved[0])[lane * a.ssaved[0] + unit] = from_f32<T>(v[0]);
+    if (a.act != ABCD_NO_ACTIVATION) act_values<sizeof(T) == 4>(v, a.act);
+    if (a.res) v[0] += to_f32(((const T*)a.res)[lane * a.sres + unit]);
   }
   ((T*)a.y)[lane * a.sy + unit] = from_f32<T>(v[0]);
 }
@@ -177,6 +190,37 @@ abcd_status few_tokens(abcd_ctx* ctx, const abcd_matrix* x, const abcd_matrix* w
     const abcd_status st = check_launch(ctx, "few_kernel", launch_few<T, 2>(ctx, a, rows_aligned(w_gate, 16) && rows_aligned(w_up, 16)));
     if (st != ABCD_OK) return st;
     return check_launch(ctx, "few_kernel", launch_few<T, 1>(ctx, b, rows_aligned(w_down, 16)));
+  });
+}
+
+// A linear layer's forward pass for few tokens; the arguments have been checked.
+abcd_status few_linear(abcd_ctx* ctx, const abcd_matrix* x, const abcd_matrix* weight, const void* bias, int bias_dtype,
+                       int activation, const abcd_matrix* residual, const abcd_matrix* y, const abcd_matrix* z) {
+  FewArgs a{};
+  a.x = x->data;
+  a.w[0] = weight->data;
+  a.y = y->data;
+  a.rows = (int)x->rows;
+  a.k = (int)x->cols;
+  a.n = (int)weight->rows;
+  a.act = activation;
+  a.x_vec = rows_aligned(x, 16);
+  a.sx = x->stride;
+  a.sw[0] = weight->stride;
+  a.sy = y->stride;
+  a.linear = 1;
+  a.bias = bias;
+  a.wide_bias = bias_dtype == ABCD_F32;
+  if (residual) {
+    a.res = residual->data;
+    a.sres = residual->stride;
+  }
+  if (z) {
+    a.saved[0] = z->data;
+    a.ssaved[0] = z->stride;
+  }
+  return with_type(x->dtype, [&](auto t) {
+    return check_launch(ctx, "few_kernel", launch_few<decltype(t), 1>(ctx, a, rows_aligned(weight, 16)));
   });
 }
 

@@ -1,4 +1,5 @@
-// The matrix products of the gated feed-forward layer (gatedff.cu), one kernel template.
+// The matrix products of the gated feed-forward layer (gatedff.cu) and the linear layer (linear.cu), one
+// kernel template.
 //
 // C = sum over segments of A_s B_s^T with 16-bit operands and 32-bit sums, A_s [m][k], B_s [n][k].
 // Either operand may lie with k or with its other dimension contiguous.  Segments are how sums of
@@ -29,7 +30,7 @@
 
 namespace abcd {
 
-enum { kPlain, kUp, kDown };          // what becomes of the sums, see store()
+enum { kPlain, kUp, kDown, kLinear };   // what becomes of the sums
 
 constexpr int kMaxSegments = 12;
 constexpr int kBlockK = 64;           // elements of k per stage: 128 bytes, the swizzle's row
@@ -43,7 +44,7 @@ struct Out {
   int vec;                            // rows start on 16-byte boundaries
 };
 
-// One of up to three products of a launch (kPlain; kUp and kDown have one).
+// One of up to three products of a launch (kPlain; the others have one).
 struct ProductJob {
   CUtensorMap a, b[2];
   // the operand lies with its own dimension contiguous instead of k: neither (kUp), B (kDown) or, of
@@ -74,7 +75,9 @@ struct ProductArgs {
   int dtype;
   int act;
   Out g[2];                           // kUp: gate and up (p NULL: not wanted); kDown: dG and dU
-  Out in[2];                          // kDown: the saved gate and up
+  Out in[2];                          // kDown: the saved gate and up; kLinear: the residual (p NULL: none)
+  const void* bias;                   // kLinear, or NULL; z goes to g[0]
+  int wide_bias;                      // it is fp32 whatever the matrices' type
   unsigned* count;                    // finished splits per warp of a tile; zero between calls
   unsigned* status;
   unsigned limit;                     // polls of a wait
@@ -335,6 +338,41 @@ __device__ __forceinline__ void row_of(float (&v)[16], const char* buf, bool bf1
   }
 }
 
+// kLinear: the lane's row of sixteen columns of the residual, from column n of row m + lane on; zeros
+// outside of it.
+template <bool F32, int CW>
+__device__ __forceinline__ void residual_ahead(float (&v)[CW], const Out& o, long long m, int n, int rows, int cols, bool bf16) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int q = 0; q < CW; ++q) v[q] = 0.f;
+  if (!o.p || lane >= rows) return;
+  const long long at = (m + lane) * o.stride + n;
+  if constexpr (F32) {
+    const float* p = (const float*)o.p + at;
+    if (o.vec && cols >= CW) {
+#pragma unroll
+      for (int q = 0; q < CW; q += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(p + q);
+        v[q] = x.x; v[q + 1] = x.y; v[q + 2] = x.z; v[q + 3] = x.w;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < CW; ++q)
+        if (q < cols) v[q] = p[q];
+    }
+  } else {
+    const unsigned short* p = (const unsigned short*)o.p + at;
+    if (o.vec && cols >= CW) {
+#pragma unroll
+      for (int q = 0; q < CW; q += 8) unpack8(v + q, *reinterpret_cast<const uint4*>(p + q), bf16);
+    } else {
+#pragma unroll
+      for (int q = 0; q < CW; ++q)
+        if (q < cols) v[q] = unpack(p[q], bf16);
+    }
+  }
+}
+
 // Where 16-byte piece j of a row lies in a block of 128 rows of 64 bytes under TMA's 64-byte swizzle.
 __device__ __forceinline__ int block_at(int row, int j) { return row * 64 + ((j ^ ((row / 2) % 4)) * 16); }
 // Sixteen columns, from piece j on, of a block's rows first ... first + 31 to a matrix whose rows start
@@ -408,7 +446,7 @@ struct Product {
   // asks for the blocks of the saved projections up to three ahead.  With accesses of the warps' own
   // instead (32 bytes of a row at a time), 100,000 x 256 x 1,024 took 167 and 196 us for kUp and kDown;
   // with the blocks 119 and 171.
-  static constexpr bool kBlocks = BN == 256 && !F32 && EPI != kPlain;
+  static constexpr bool kBlocks = BN == 256 && !F32 && (EPI == kUp || EPI == kDown);
   static constexpr int kBlockBytes = 128 * 64;
   // Three blocks of results per group, and for kDown slots of a block of gate and one of up.
   // (A slot's blocks go to the groups in turn.  So it has two barriers that say it is full, one for each
@@ -569,7 +607,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
             }
           }
         };
-        if constexpr (EPI == kUp) {
+        if constexpr (EPI == kUp || EPI == kLinear) {
           multiply(std::false_type(), std::false_type());
         } else if constexpr (EPI == kDown) {
           multiply(std::false_type(), std::true_type());
@@ -866,6 +904,27 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
           store_operand<F32, P::CW>(s, a.g[0], m, n + c, rows, w, bf16, buffer);
           store_operand<F32, P::CW>(z, a.g[1], m, n + c, rows, w, bf16, buffer);
           store_operand<F32, P::CW>(u, job.c[0], m, n + c, rows, w, bf16, buffer);
+        } else if constexpr (EPI == kLinear) {
+          // the residual's and the bias's columns are on their way while the sums come
+          float add[P::CW];
+          residual_ahead<F32>(add, a.in[0], m, n + c, rows, w, bf16);
+          float b = 0.f;
+          if (a.bias && lane < w) {
+            if (F32 || a.wide_bias) b = __ldg((const float*)a.bias + n + c + lane);
+            else b = unpack(__ldg((const unsigned short*)a.bias + n + c + lane), bf16);
+          }
+          sum_columns(c, 0, v);
+          tmem_load_wait(v);
+          if (last) release();
+          if (a.bias) {
+#pragma unroll
+            for (int q = 0; q < P::CW; ++q) v[q] += __shfl_sync(~0u, b, q);
+          }
+          if (a.g[0].p) store_matrix<F32, P::CW>(v, a.g[0], m, n + c, rows, w, bf16, buffer);
+          if (a.act != ABCD_NO_ACTIVATION) act_values<F32>(v, a.act);
+#pragma unroll
+          for (int q = 0; q < P::CW; ++q) v[q] += add[q];
+          store_matrix<F32, P::CW>(v, job.c[0], m, n + c, rows, w, bf16, buffer);
         } else {
           sum_columns(c, 0, v);
           tmem_load_wait(v);
@@ -942,11 +1001,11 @@ struct Shape {
   int cg, bn, ctas;          // CTAs of a tile, its sums per row, CTAs per SM (one for kDown)
   double fixed;              // of a launch
   double idle, busy;         // of a stage (64 of k) where few SMs, where all ask for operands
-  double epilogue[3][2];     // of a tile, by kPlain, kUp, kDown and 16 or 32 bits
+  double epilogue[4][2];     // of a tile, by kPlain, kUp, kDown, kLinear and 16 or 32 bits
 };
-constexpr Shape kShapes[3] = {{2, 256, 1, 7.1, 0.25, 0.34, {{1.7, 1.8}, {2.7, 9.2}, {7.0, 36.0}}},
-                              {1, 128, 1, 5.9, 0.22, 0.33, {{0.5, 0.8}, {2.5, 4.5}, {6.1, 17.0}}},
-                              {1, 64, 2, 5.2, 0.24, 0.36, {{0.8, 1.0}, {2.1, 3.6}, {3.3, 8.3}}}};
+constexpr Shape kShapes[3] = {{2, 256, 1, 7.1, 0.25, 0.34, {{1.7, 1.8}, {2.7, 9.2}, {7.0, 36.0}, {2.4, 2.6}}},
+                              {1, 128, 1, 5.9, 0.22, 0.33, {{0.5, 0.8}, {2.5, 4.5}, {6.1, 17.0}, {0.8, 1.2}}},
+                              {1, 64, 2, 5.2, 0.24, 0.36, {{0.8, 1.0}, {2.1, 3.6}, {3.3, 8.3}, {1.1, 1.4}}}};
 
 template <int EPI, bool F32> abcd_status launch_shape(abcd_ctx* ctx, int shape, const ProductArgs& a) {
   if (shape == 0) return launch_product<2, 256, EPI, F32>(ctx, a);
@@ -956,6 +1015,7 @@ template <int EPI, bool F32> abcd_status launch_shape(abcd_ctx* ctx, int shape, 
 template <bool F32> abcd_status launch_any(abcd_ctx* ctx, int epi, int shape, const ProductArgs& a) {
   if (epi == kUp) return launch_shape<kUp, F32>(ctx, shape, a);
   if (epi == kDown) return launch_shape<kDown, F32>(ctx, shape, a);
+  if (epi == kLinear) return launch_shape<kLinear, F32>(ctx, shape, a);
   return launch_shape<kPlain, F32>(ctx, shape, a);
 }
 // One translation unit each.

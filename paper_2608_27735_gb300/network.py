@@ -1,5 +1,6 @@
-"""Operators of a network over a block's Gaussians (layer norm, gated feed-forward, dropout): the
-calls of ``include/abcd.h`` of the same names, and the residual block that they make up.
+"""Operators of a network over a block's Gaussians (layer norm, gated feed-forward, dropout; embedding,
+linear layer, the norms around a residual sum, matrices in 8 bits): the calls of ``include/abcd.h`` of the
+same names, and the residual blocks that they make up.
 
 Matrices are CUDA tensors [rows][cols] whose columns are consecutive (rows may be further apart);
 types float32, float16 or bfloat16.  The calls run on the context's stream: tensors that another
@@ -8,9 +9,14 @@ from __future__ import annotations
 
 import struct
 
-from . import ABCD_GELU, ABCD_RELU, ABCD_SILU, Context, _dtypes, _torch, lib
+from dataclasses import dataclass
+
+from . import (ABCD_GELU, ABCD_I32, ABCD_I64, ABCD_LAYER_NORM, ABCD_NO_ACTIVATION, ABCD_RELU,
+               ABCD_RMS_NORM, ABCD_SILU, Context, _dtypes, _torch, lib)
 
 ACTIVATIONS = {"silu": ABCD_SILU, "gelu": ABCD_GELU, "relu": ABCD_RELU}
+LINEAR_ACTIVATIONS = {**ACTIVATIONS, "none": ABCD_NO_ACTIVATION}
+NORMS = {"layer": ABCD_LAYER_NORM, "rms": ABCD_RMS_NORM}
 
 
 _F32 = None
@@ -154,6 +160,201 @@ def abcd_dropout_backward(ctx: Context, dy, p, seed, offset, dx):
     """dx = dropout's gradient of dy under the mask of (seed, offset); dx may be dy."""
     call = _call("abcd_dropout_backward")
     st = call(ctx.h, _matrix(dy, "dy")[0], p, seed, offset, _matrix(dx, "dx")[0])
+    if st:
+        ctx.check(st)
+
+
+def _index(t, n):
+    """(address, ABCD_* type) of a consecutive CUDA vector of n indices."""
+    if not t.is_cuda or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"index must be a consecutive CUDA vector of {n} elements")
+    torch = _torch()
+    if t.dtype is torch.int64:
+        return t.data_ptr(), ABCD_I64
+    if t.dtype is torch.int32:
+        return t.data_ptr(), ABCD_I32
+    raise ValueError(f"index has type {t.dtype}; int32 and int64 are taken")
+
+
+def abcd_embedding(ctx: Context, table, index, scale, y, add=None):
+    """y[t] = add[t] + scale table[index[t]]; index: int32 or int64, negative ones name no row.  One that is
+    past the table is reported by ctx.sync().  y may be add.  Takes the network workspace
+    (Context.reserve_embedding)."""
+    call = _call("abcd_embedding")
+    my, rows, _ = _matrix(y, "y")
+    at, kind = _index(index, rows)
+    st = call(ctx.h, _matrix(table, "table")[0], at, kind, scale, _optional(add, "add"), my)
+    if st:
+        ctx.check(st)
+
+
+def abcd_embedding_backward(ctx: Context, dy, index, scale, dtable):
+    """dtable[v] = scale times the sum of dy[t] over the tokens that name row v; every row is written.
+    Takes the network workspace (Context.reserve_embedding)."""
+    call = _call("abcd_embedding_backward")
+    my, rows, _ = _matrix(dy, "dy")
+    at, kind = _index(index, rows)
+    st = call(ctx.h, my, at, kind, scale, _matrix(dtable, "dtable")[0])
+    if st:
+        ctx.check(st)
+
+
+def _linear_activation(name):
+    act = LINEAR_ACTIVATIONS.get(name)
+    if act is None:
+        raise ValueError(f"unknown activation {name!r}; one of {sorted(LINEAR_ACTIVATIONS)}")
+    return act
+
+
+def abcd_linear(ctx: Context, x, weight, bias, activation, y, residual=None, z=None):
+    """y = residual + act(z), z = x weight^T + bias; weight [out][cols]; bias [out] or None; activation
+    "none", "silu", "gelu" or "relu"; z: kept for the backward pass, or None.  y may be residual.  Takes
+    the network workspace (Context.reserve_linear)."""
+    call = _call("abcd_linear")
+    mx = _matrix(x, "x")[0]
+    mw, out, _ = _matrix(weight, "weight")
+    bt = _weight_type(x, bias)
+    st = call(ctx.h, mx, mw, _vector(bias, out, "bias", bt), _KINDS[bt], _linear_activation(activation),
+              _optional(residual, "residual"), _matrix(y, "y")[0], _optional(z, "z"))
+    if st:
+        ctx.check(st)
+
+
+def abcd_linear_backward(ctx: Context, dy, x, weight, activation, z, dx=None, dweight=None, dbias=None):
+    """dx, dweight and dbias (each may be None) of abcd_linear from the z that it left (None for "none").
+    The residual's gradient is dy.  Takes the network workspace (Context.reserve_linear)."""
+    call = _call("abcd_linear_backward")
+    mw, out, _ = _matrix(weight, "weight")
+    bt = _weight_type(x, dbias)
+    st = call(ctx.h, _matrix(dy, "dy")[0], _matrix(x, "x")[0], mw, _linear_activation(activation),
+              _optional(z, "z"), _optional(dx, "dx"), _optional(dweight, "dweight"),
+              _vector(dbias, out, "dbias", bt), _KINDS[bt])
+    if st:
+        ctx.check(st)
+
+
+@dataclass
+class Norm:
+    """A norm of abcd_residual_norm: kind "layer" or "rms"; weight, bias: [cols] or None; mean, rstd:
+    float32 [rows] that the backward pass needs, or None (an rms norm has no mean; one that is given is
+    left as it is)."""
+    kind: str
+    weight: object = None
+    bias: object = None
+    eps: float = 1e-5
+    mean: object = None
+    rstd: object = None
+
+
+_pack_norm = struct.Struct("@iPPfPP").pack           # the bytes of an abcd_norm
+
+
+def _norm(q, rows, cols, dtype, what):
+    if q is None:
+        return None
+    kind = NORMS.get(q.kind)
+    if kind is None:
+        raise ValueError(f"unknown norm {q.kind!r}; one of {sorted(NORMS)}")
+    return _pack_norm(kind, _vector(q.weight, cols, what + ".weight", dtype) or 0,
+                      _vector(q.bias, cols, what + ".bias", dtype) or 0, q.eps,
+                      _vector(q.mean, rows, what + ".mean", _F32) or 0 if kind == ABCD_LAYER_NORM else 0,
+                      _vector(q.rstd, rows, what + ".rstd", _F32) or 0)
+
+
+def _norm_vectors(after, before):
+    for q in (after, before):
+        if q is not None:
+            yield q.weight
+            yield q.bias
+
+
+def abcd_residual_norm(ctx: Context, x, f, after, before, gate, scale, y, n=None):
+    """y = x + scale gate after(f), n = before(y): after and before Norms or None, gate [cols] or None;
+    n as before is.  All vectors are of one type (the matrices' or float32).  y and n may be x or f."""
+    call = _call("abcd_residual_norm")
+    mx, rows, cols = _matrix(x, "x")
+    wt = _weight_type(x, gate, *_norm_vectors(after, before))
+    st = call(ctx.h, mx, _matrix(f, "f")[0], _norm(after, rows, cols, wt, "after"),
+              _norm(before, rows, cols, wt, "before"), _vector(gate, cols, "gate", wt), _KINDS[wt], scale,
+              _matrix(y, "y")[0], _optional(n, "n"))
+    if st:
+        ctx.check(st)
+
+
+def abcd_residual_norm_backward(ctx: Context, dy, dn, x, f, after, before, gate, scale, dx=None, df=None,
+                                dgate=None, dafter_weight=None, dafter_bias=None, dbefore_weight=None,
+                                dbefore_bias=None):
+    """The gradients (each may be None) of abcd_residual_norm from x, f and the statistics that it left in
+    after and before; dy: the gradient that reaches y past n, or None; dn: n's, as before is.  dx and df
+    may be dy, dn, x or f.  Takes the network workspace (Context.reserve_residual_norm)."""
+    call = _call("abcd_residual_norm_backward")
+    mx, rows, cols = _matrix(x, "x")
+    wt = _weight_type(x, gate, dgate, dafter_weight, dafter_bias, dbefore_weight, dbefore_bias,
+                      *_norm_vectors(after, before))
+    v = lambda t, what: _vector(t, cols, what, wt)
+    st = call(ctx.h, _optional(dy, "dy"), _optional(dn, "dn"), mx, _matrix(f, "f")[0],
+              _norm(after, rows, cols, wt, "after"), _norm(before, rows, cols, wt, "before"),
+              v(gate, "gate"), _KINDS[wt], scale, _optional(dx, "dx"), _optional(df, "df"),
+              v(dgate, "dgate"), v(dafter_weight, "dafter_weight"), v(dafter_bias, "dafter_bias"),
+              v(dbefore_weight, "dbefore_weight"), v(dbefore_bias, "dbefore_bias"))
+    if st:
+        ctx.check(st)
+
+
+class Packed8:
+    """A matrix of rows x cols in 8 bits: `codes`, int8, its rows `stride` bytes apart, and `powers`, uint8,
+    one for each 32 columns of a row.  Allocated on the current stream (Context.hold for a context on
+    another one)."""
+
+    def __init__(self, rows, cols, device="cuda"):
+        torch = _torch()
+        rows, cols = int(rows), int(cols)
+        groups = -(-cols // 32)
+        self.rows, self.cols, self.stride = rows, cols, 32 * groups
+        self.codes = torch.empty(rows, self.stride, dtype=torch.int8, device=device)
+        self.powers = torch.empty(rows, groups, dtype=torch.uint8, device=device)
+        self._at(self.codes.data_ptr(), self.powers.data_ptr(), rows)
+
+    def _at(self, codes, powers, rows):
+        self.c = _pack_packed(codes, powers, rows, self.cols, self.stride, self.stride // 32)
+
+    def head(self, rows):
+        """Its first rows, as a packed matrix over the same memory."""
+        if not 0 <= rows <= self.rows:
+            raise ValueError(f"{rows} of {self.rows} rows")
+        part = Packed8.__new__(Packed8)
+        part.rows, part.cols, part.stride = int(rows), self.cols, self.stride
+        part.codes, part.powers = self.codes[:rows], self.powers[:rows]
+        part._at(part.codes.data_ptr(), part.powers.data_ptr(), part.rows)
+        return part
+
+
+_pack_packed = struct.Struct("@PPqqqq").pack         # the bytes of an abcd_packed8
+
+
+def abcd_pack8(ctx: Context, x, packed: Packed8):
+    """packed = x in 8 bits: an element is off by at most a 128th of the largest magnitude of the 32 columns
+    that share its power of two."""
+    st = _call("abcd_pack8")(ctx.h, _matrix(x, "x")[0], packed.c)
+    if st:
+        ctx.check(st)
+
+
+def abcd_unpack8(ctx: Context, packed: Packed8, y):
+    """y = what packed stands for."""
+    st = _call("abcd_unpack8")(ctx.h, packed.c, _matrix(y, "y")[0])
+    if st:
+        ctx.check(st)
+
+
+def abcd_gated_ff_backward_packed8(ctx: Context, dy, x, w_gate, w_up, w_down, activation, gate, up,
+                                   dx=None, dw_gate=None, dw_up=None, dw_down=None):
+    """abcd_gated_ff_backward with x, gate and up as Packed8.  Takes the network workspace
+    (Context.reserve_packed8)."""
+    call = _call("abcd_gated_ff_backward_packed8")
+    st = call(ctx.h, _matrix(dy, "dy")[0], x.c, _matrix(w_gate, "w_gate")[0], _matrix(w_up, "w_up")[0],
+              _matrix(w_down, "w_down")[0], _activation(activation), gate.c, up.c, _optional(dx, "dx"),
+              _optional(dw_gate, "dw_gate"), _optional(dw_up, "dw_up"), _optional(dw_down, "dw_down"))
     if st:
         ctx.check(st)
 
