@@ -9,6 +9,7 @@
 // Backward, y is made again from x and f: as many bytes as reading y, but in 32 bits, so that yh is the
 // forward pass's own.
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.cuh"
 
@@ -193,6 +194,320 @@ __global__ void __launch_bounds__(kLongThreads) close_bwd_long_kernel(const __gr
   }
 }
 
+// How a row lies over threads: eight values each, as vectors of 16 bytes, TPR threads a row.  VEC: rows on
+// 16-byte boundaries, copied ahead to shared memory by the threads that use them; else element by
+// element, TPR apart.
+template <typename T, int TPR_, bool BWD, bool VEC_> struct CloseRow {
+  static constexpr int TPR = TPR_;
+  static constexpr bool VEC = VEC_;
+  static constexpr int V = VEC ? 16 / (int)sizeof(T) : 1, NV = 8 / V;
+  static constexpr int kThreads = TPR > 256 ? TPR : 256, kGroups = kThreads / TPR;
+  static constexpr int kMats = BWD ? 4 : 2;
+  static constexpr int kDepth = VEC ? (BWD ? 3 : 4) : 0;   // rows of a thread that are there or on their way
+  static constexpr size_t kRing = (size_t)kDepth * kMats * (VEC ? NV : 0) * kThreads * 16;
+  static constexpr size_t kSums = BWD ? (size_t)4 * TPR * 8 * 4 : 0;
+  static constexpr size_t kSmem = kRing > kSums ? kRing : kSums;
+  static constexpr int kCtas = kThreads > 256 ? 1 : BWD ? 2 : 3;
+};
+
+template <typename T, typename R> struct CloseRows {
+  char* slots;                        // the thread's first slot
+  const T* src[R::kMats];             // the thread's first value of the next row to fetch (VEC) or use
+  long long jump[R::kMats];
+  bool there[R::kMats];
+  int rows, turns, lane, cols;        // rows of the group; turns of the CTA
+
+  __device__ __forceinline__ CloseRows(char* smem, const CloseArgs& a) {
+    const int group = threadIdx.x / R::TPR;
+    const long long first = (long long)blockIdx.x * R::kGroups + group, step = (long long)gridDim.x * R::kGroups;
+    lane = threadIdx.x % R::TPR;
+    cols = a.cols;
+    slots = smem + threadIdx.x * 16;
+    rows = first < a.rows ? (int)((a.rows - first + step - 1) / step) : 0;
+    turns = (int)((a.rows - (long long)blockIdx.x * R::kGroups + step - 1) / step);
+    const T* const base[4] = {(const T*)a.f, (const T*)a.x, (const T*)a.dy, (const T*)a.dn};
+    const long long stride[4] = {a.sf, a.sx, a.sdy, a.sdn};
+#pragma unroll
+    for (int q = 0; q < R::kMats; ++q) {
+      there[q] = base[q] != nullptr;
+      src[q] = base[q] + first * stride[q] + lane * R::V;
+      jump[q] = step * stride[q];
+    }
+  }
+  __device__ __forceinline__ int column(int j) const { return (j * R::TPR + lane) * R::V; }
+  __device__ __forceinline__ char* slot(int t, int mat, int j) const {
+    return slots + ((t % R::kDepth * R::kMats + mat) * R::NV + j) * R::kThreads * 16;
+  }
+  __device__ __forceinline__ void fetch(int t) {
+    if (t < rows) {
+#pragma unroll
+      for (int q = 0; q < R::kMats; ++q) {
+#pragma unroll
+        for (int j = 0; j < R::NV; ++j) {
+          const int left = cols - column(j);
+          if (there[q] && left > 0) copy16(slot(t, q, j), src[q] + j * R::TPR * R::V, left < R::V ? left * (int)sizeof(T) : 16);
+        }
+        src[q] += jump[q];
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  __device__ __forceinline__ void start() {
+    if constexpr (R::VEC) {
+#pragma unroll
+      for (int d = 0; d < R::kDepth - 1; ++d) fetch(d);
+    }
+  }
+  // Asks for a row to come and waits for turn t's.
+  __device__ __forceinline__ void turn(int t) {
+    if constexpr (R::VEC) {
+      fetch(t + R::kDepth - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
+    }
+  }
+  // Vector j of the turn's row of a matrix: zeros past its end, of no row and of a matrix that is not there.
+  __device__ __forceinline__ void get(float (&v)[8], int t, int mat) const {
+#pragma unroll
+    for (int j = 0; j < R::NV; ++j) {
+      const bool in = there[mat] && t < rows && column(j) < cols;
+      if constexpr (R::VEC) {
+        float w[R::V];
+        load_vec<T, R::V>(w, (const T*)slot(t, mat, j), in ? R::V : 0);
+#pragma unroll
+        for (int i = 0; i < R::V; ++i) v[j * R::V + i] = w[i];
+      } else {
+        v[j] = in ? to_f32(src[mat][j * R::TPR]) : 0.f;
+      }
+    }
+  }
+  // The next row (rows that are not copied ahead).
+  __device__ __forceinline__ void next() {
+    if constexpr (!R::VEC) {
+#pragma unroll
+      for (int q = 0; q < R::kMats; ++q) src[q] += jump[q];
+    }
+  }
+  __device__ __forceinline__ void put(T* to, const float (&v)[8], int t) const {
+    if (t >= rows) return;
+#pragma unroll
+    for (int j = 0; j < R::NV; ++j) {
+      float w[R::V];
+#pragma unroll
+      for (int i = 0; i < R::V; ++i) w[i] = v[j * R::V + i];
+      store_vec<T, R::V>(to + column(j), w, cols - column(j));
+    }
+  }
+  __device__ __forceinline__ void weights(float (&v)[8], const void* w, int wide, float none) const {
+#pragma unroll
+    for (int j = 0; j < R::NV; ++j) {
+      float u[R::V];
+      load_weight<T, R::V>(u, w, wide, column(j), cols - column(j), none);
+#pragma unroll
+      for (int i = 0; i < R::V; ++i) v[j * R::V + i] = u[i];
+    }
+  }
+  // Whether value e of the thread is one of the row's.
+  __device__ __forceinline__ bool inside(int e) const { return column(e / R::V) + e % R::V < cols; }
+};
+
+// A row's statistics from the threads' values; what lies past its end has no part in them.
+template <typename T, typename R>
+__device__ __forceinline__ Stat stat_of_row(const CloseRows<T, R>& rows, const float (&v)[8], int kind, float eps, float inv, float2 (*red)[32], int& turn) {
+  float s = 0.f, q = 0.f;
+  if (kind == ABCD_RMS_NORM) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q += v[e] * v[e];              // zero past the end
+    row_sum2<R::TPR>(q, s, red, turn);
+    turn ^= 1;
+    return Stat{0.f, rsqrtf(q * inv + eps)};
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s += v[e];
+  row_sum2<R::TPR>(s, q, red, turn);
+  // the division's rounding taken back, then what the sum has rounded
+  float mean = s * inv, off = 0.f;
+  mean = __fmaf_rn(__fmaf_rn(-mean, (float)rows.cols, s), inv, mean);
+  q = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float d = rows.inside(e) ? v[e] - mean : 0.f;
+    q += d * d;
+    off += d;
+  }
+  row_sum2<R::TPR>(q, off, red, turn ^ 1);
+  off *= inv;
+  return Stat{mean + off, rstd_of(q * inv, off, eps)};
+}
+
+// A and C of the thread's columns.
+template <typename T, typename R>
+__device__ __forceinline__ void factors(const CloseRows<T, R>& rows, const CloseArgs& a, float (&A)[8], float (&C)[8]) {
+  float g[8];
+  rows.weights(g, a.gate, a.wide_w, 1.f);
+  rows.weights(A, a.w[0], a.wide_w, 1.f);
+  rows.weights(C, a.b[0], a.wide_w, 0.f);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    A[e] *= a.scale * g[e];
+    C[e] *= a.scale * g[e];
+  }
+}
+
+template <typename T, typename R>
+__global__ void __launch_bounds__(R::kThreads, R::kCtas) close_fwd_kernel(const __grid_constant__ CloseArgs a) {
+  extern __shared__ __align__(16) char smem[];
+  __shared__ float2 red[2][32];
+  pdl_wait();
+  CloseRows<T, R> rows(smem, a);
+  rows.start();
+  float A[8], C[8], W[8], B[8];
+  factors(rows, a, A, C);
+  rows.weights(W, a.w[1], a.wide_w, 1.f);
+  rows.weights(B, a.b[1], a.wide_w, 0.f);
+  const float inv = 1.f / (float)a.cols;
+  const long long step = (long long)gridDim.x * R::kGroups;
+  long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / R::TPR;
+  T* y = (T*)a.y + r * a.sy;
+  T* n = (T*)a.n + r * a.sn;
+  int half = 0;
+  for (int t = 0; t < rows.turns; ++t, r += step, y += step * a.sy, n += step * a.sn) {
+    rows.turn(t);
+    float f[8], x[8];
+    rows.get(f, t, 0);
+    rows.get(x, t, 1);
+    Stat first{0.f, 1.f}, second{0.f, 1.f};
+    if (a.kind[0] != kNone) first = stat_of_row(rows, f, a.kind[0], a.eps[0], inv, red, half);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = rows.inside(e) ? close_value(x[e], (f[e] - first.mean) * first.rstd, A[e], C[e]) : 0.f;
+    if (a.kind[1] != kNone) {
+      second = stat_of_row(rows, x, a.kind[1], a.eps[1], inv, red, half);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = (x[e] - second.mean) * second.rstd * W[e] + B[e];
+      rows.put(n, f, t);
+    }
+    rows.put(y, x, t);
+    rows.next();
+    if (t < rows.rows && rows.lane == 0) {
+      const Stat s[2] = {first, second};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (a.mean[k]) a.mean[k][r] = s[k].mean;
+        if (a.rstd[k]) a.rstd[k][r] = s[k].rstd;
+      }
+    }
+  }
+}
+
+template <typename T, typename R>
+__global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const __grid_constant__ CloseArgs a) {
+  extern __shared__ __align__(16) char smem[];
+  __shared__ float2 red[2][32];
+  pdl_wait();
+  CloseRows<T, R> rows(smem, a);
+  rows.start();
+  float A[8], C[8], W[8], sums[4][8] = {};
+  factors(rows, a, A, C);
+  rows.weights(W, a.w[1], a.wide_w, 1.f);
+  const float inv = 1.f / (float)a.cols;
+  const float centre[2] = {a.kind[0] == ABCD_LAYER_NORM ? inv : 0.f, a.kind[1] == ABCD_LAYER_NORM ? inv : 0.f};
+  const long long step = (long long)gridDim.x * R::kGroups;
+  long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / R::TPR;
+  T* dx = (T*)a.y + r * a.sy;
+  T* df = (T*)a.n + r * a.sn;
+  Stat next[2] = {{0.f, 0.f}, {0.f, 0.f}};
+  if (rows.rows > 0) {
+    next[0] = stat_of(a, 0, r);
+    next[1] = stat_of(a, 1, r);
+  }
+  for (int t = 0; t < rows.turns; ++t, r += step, dx += step * a.sy, df += step * a.sn) {
+    rows.turn(t);
+    const Stat first = next[0], second = next[1];
+    if (t + 1 < rows.rows) {
+      next[0] = stat_of(a, 0, r + step);
+      next[1] = stat_of(a, 1, r + step);
+    }
+    float fh[8], yh[8], g[8], s1 = 0.f, s2 = 0.f;
+    rows.get(fh, t, 0);
+    rows.get(yh, t, 1);
+    rows.get(g, t, 2);
+    if (a.dn) {
+      float dn[8];
+      rows.get(dn, t, 3);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        fh[e] = (fh[e] - first.mean) * first.rstd;
+        yh[e] = (close_value(yh[e], fh[e], A[e], C[e]) - second.mean) * second.rstd;   // the forward pass's, bit for bit
+        sums[2][e] += dn[e];
+        sums[3][e] += dn[e] * yh[e];
+        dn[e] *= W[e];
+        s1 += dn[e];
+        s2 += dn[e] * yh[e];
+      }
+      row_sum2<R::TPR>(s1, s2, red, 0);
+      s1 *= centre[1];
+      s2 *= inv;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[e] = rows.inside(e) ? g[e] + second.rstd * (dn[e] - s1 - yh[e] * s2) : 0.f;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) fh[e] = (fh[e] - first.mean) * first.rstd;
+    }
+    const bool in = t < rows.rows;
+    if (a.y) rows.put(dx, g, t);
+    s1 = s2 = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (!in) g[e] = 0.f;
+      sums[0][e] += g[e];
+      sums[1][e] += g[e] * fh[e];
+      g[e] *= A[e];
+      s1 += g[e];
+      s2 += g[e] * fh[e];
+    }
+    if (a.n) {
+      if (a.kind[0] != kNone) {
+        row_sum2<R::TPR>(s1, s2, red, 1);
+        s1 *= centre[0];
+        s2 *= inv;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] = first.rstd * (g[e] - s1 - fh[e] * s2);
+      }
+      rows.put(df, g, t);
+    }
+    // a row's use of `red` ends before the next but one begins; where only one sum is taken, the row's
+    // threads meet here
+    if (R::TPR > 32 && (!a.dn || !a.n || a.kind[0] == kNone)) row_sync<R::TPR>();
+    rows.next();
+  }
+  // the CTA's sums: rows that share a warp by shuffles, then the warps of a column one after another
+  if constexpr (R::VEC) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  float* total = (float*)smem;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int o = 16; o >= R::TPR; o >>= 1) sums[k][e] += __shfl_xor_sync(~0u, sums[k][e], o);
+  constexpr int ROUNDS = R::TPR > 32 ? R::kGroups : R::kThreads / 32, CAPACITY = R::TPR * 8;
+  const int mine = R::TPR > 32 ? threadIdx.x / R::TPR : threadIdx.x / 32;
+  const bool one = R::TPR >= 32 || (threadIdx.x & 31) < R::TPR;
+  for (int q = 0; q < ROUNDS; ++q) {
+    __syncthreads();
+    if (mine != q || !one) continue;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float* to = total + k * CAPACITY + rows.column(e / R::V) + e % R::V;
+        *to = (q ? *to : 0.f) + sums[k][e];
+      }
+  }
+  __syncthreads();
+  float* part = a.part + (long long)blockIdx.x * 4 * a.cols;
+  for (int k = 0; k < 4; ++k)
+    for (int c = threadIdx.x; c < a.cols; c += R::kThreads) part[k * (long long)a.cols + c] = total[k * CAPACITY + c];
+}
+
 struct CloseSums {
   const float* part;
   int ctas, cols, wide_w;
@@ -239,6 +554,39 @@ __global__ void __launch_bounds__(1024) close_sum_kernel(const __grid_constant__
 }
 
 constexpr int kCloseCtasPerSm = 2;    // backward, with sums in the workspace
+
+// Calls f with the row shape for `cols` columns of T; f of an int where registers do not hold a row.
+template <typename T, bool BWD, typename F> abcd_status with_row(long long cols, bool aligned, F&& f) {
+  if (aligned) {
+    if (cols <= 64) return f(CloseRow<T, 8, BWD, true>());
+    if (cols <= 128) return f(CloseRow<T, 16, BWD, true>());
+    if (cols <= 256) return f(CloseRow<T, 32, BWD, true>());
+    if (cols <= 512) return f(CloseRow<T, 64, BWD, true>());
+    if (cols <= 1024) return f(CloseRow<T, 128, BWD, true>());
+    if (cols <= 2048) return f(CloseRow<T, 256, BWD, true>());
+    if (cols <= 4096) return f(CloseRow<T, 512, BWD, true>());
+  } else {
+    if (cols <= 256) return f(CloseRow<T, 32, BWD, false>());
+    if (cols <= 1024) return f(CloseRow<T, 128, BWD, false>());
+    if (cols <= 4096) return f(CloseRow<T, 512, BWD, false>());
+  }
+  return f(0);
+}
+
+template <typename K>
+abcd_status launch_rows(abcd_ctx* ctx, const char* what, K* kernel, int grid, int threads, size_t smem, const CloseArgs& a) {
+  if (smem > 47 * 1024) {
+    const cudaError_t e = allow_smem(ctx, (const void*)kernel);
+    if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+  }
+  return check_launch(ctx, what, launch_pdl(kernel, dim3((unsigned)grid), dim3((unsigned)threads), smem, ctx->stream, a));
+}
+
+// CTAs for rows of shape R: all of their rows at once, or as many as stay resident on `sms` SMs.
+template <typename R> int grid_of(long long rows, int sms) {
+  if constexpr (std::is_same_v<R, int>) return (int)std::min<long long>(rows, 2LL * sms);
+  else return (int)std::min<long long>((rows + R::kGroups - 1) / R::kGroups, (long long)R::kCtas * sms);
+}
 
 bool vector_ok(const void* p, int dtype) { return ((uintptr_t)p & (elem_size(dtype) - 1)) == 0; }
 
@@ -306,8 +654,13 @@ extern "C" abcd_status abcd_residual_norm(abcd_ctx* ctx, const abcd_matrix* x, c
   a.cols = (int)x->cols;
   return with_type(x->dtype, [&](auto t) {
     using T = decltype(t);
-    const unsigned grid = (unsigned)std::min<long long>(x->rows, 2LL * ctx->num_sms);
-    return check_launch(ctx, "close_fwd_long_kernel", launch_pdl(close_fwd_long_kernel<T>, dim3(grid), dim3(kLongThreads), 0, ctx->stream, a));
+    const bool aligned = rows_aligned(x, 16) && rows_aligned(f, 16) && rows_aligned(y, 16) && (!n || rows_aligned(n, 16));
+    return with_row<T, false>(x->cols, aligned, [&](auto shape) {
+      using R = decltype(shape);
+      const int grid = grid_of<R>(x->rows, ctx->num_sms);
+      if constexpr (std::is_same_v<R, int>) return launch_rows(ctx, "close_fwd_long_kernel", close_fwd_long_kernel<T>, grid, kLongThreads, 0, a);
+      else return launch_rows(ctx, "close_fwd_kernel", close_fwd_kernel<T, R>, grid, R::kThreads, R::kSmem, a);
+    });
   });
 }
 
@@ -349,16 +702,27 @@ extern "C" abcd_status abcd_residual_norm_backward(abcd_ctx* ctx, const abcd_mat
   a.rows = x->rows;
   a.cols = (int)x->cols;
   a.part = (float*)(ctx->net_base + kNetHeader);
-  const int ctas = (int)std::min<long long>(x->rows, (long long)kCloseCtasPerSm * std::min(ctx->num_sms, kNetSms));
-  const size_t need = kNetHeader + (size_t)ctas * 4 * (size_t)x->cols * sizeof(float);
-  if (need > ctx->net_bytes)
-    return fail(ctx, ABCD_ERR_WORKSPACE, "%s: the network workspace has %zu bytes, needs %zu", what, ctx->net_bytes, need);
+  const int sms = std::min(ctx->num_sms, kNetSms);
+  bool aligned = true;
+  for (const abcd_matrix* m : {dy, dn, x, f, dx, df}) aligned = aligned && (!m || rows_aligned(m, 16));
   return with_type(x->dtype, [&](auto t) {
     using T = decltype(t);
-    if (ctas > 0) {
-      const abcd_status st = check_launch(ctx, "close_bwd_long_kernel", launch_pdl(close_bwd_long_kernel<T>, dim3(ctas), dim3(kLongThreads), 0, ctx->stream, a));
-      if (st != ABCD_OK) return st;
-    }
+    int ctas = 0;
+    const abcd_status st = with_row<T, true>(x->cols, aligned, [&](auto shape) {
+      using R = decltype(shape);
+      ctas = grid_of<R>(x->rows, sms);
+      const size_t need = kNetHeader + (size_t)ctas * 4 * (size_t)x->cols * sizeof(float);
+      if (need > ctx->net_bytes)
+        return fail(ctx, ABCD_ERR_WORKSPACE, "%s: the network workspace has %zu bytes, needs %zu", what, ctx->net_bytes, need);
+      if (ctas == 0) return ABCD_OK;
+      if constexpr (std::is_same_v<R, int>) {
+        return launch_rows(ctx, "close_bwd_long_kernel", close_bwd_long_kernel<T>, ctas, kLongThreads, 0, a);
+      } else {
+        static_assert(R::kCtas <= kCloseCtasPerSm);
+        return launch_rows(ctx, "close_bwd_kernel", close_bwd_kernel<T, R>, ctas, R::kThreads, R::kSmem, a);
+      }
+    });
+    if (st != ABCD_OK) return st;
     if (std::all_of(to, to + 5, [](void* p) { return !p; })) return ABCD_OK;
     CloseSums s{a.part, ctas, a.cols, a.wide_w, scale, gate, a.w[0], a.b[0], {}};
     std::copy(to, to + 5, s.to);

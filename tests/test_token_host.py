@@ -200,6 +200,6 @@ def test_shared_memory_limits_have_a_place():
     table = int(re.search(r"kSmemKernels = (\d+)", read("abcd_internal.cuh"))[1])
     epilogues = re.search(r"enum \{ (kPlain[^}]*) \}", read("ffproduct.cuh"))[1].count(",") + 1
     shapes = len(re.findall(r"return launch_product<\d, \d+, EPI, F32>", read("ffproduct.cuh")))
-    rows = len(re.findall(r"return f\(CloseShape<", read("residualnorm.cu")))
+    rows = len(re.findall(r"return f\(CloseRow<", read("residualnorm.cu")))
     assert epilogues == 4 and shapes == 3
     assert 62 + 10 + epilogues * shapes * 2 + rows * 3 * 2 + 1 <= table
