@@ -1,12 +1,13 @@
 // Lookups in a table of learned rows, and the table's gradient.
 //   y[t] = add[t] + s table[i_t] (no row for i_t < 0),   dtable[v] = s sum of dy[t] over the t with i_t = v.
 // Forward: bound by HBM (y, add; the table's rows come from L2 when it fits there).
-// Backward: the tokens are sorted by the row that they name (a stable radix sort, 8 to 10 bits a pass), so
+// Backward: the tokens are sorted by the row that they name (a stable radix sort, up to 10 bits a pass), so
 // that a row's tokens lie next to each other in their own order; runs of equal rows are then summed in
 // registers, `kChunk` tokens at a time, and runs that pass the end of a chunk are joined from the chunks'
 // parts in order.  No atomic adds a gradient, so every run gives the same sums, whether all tokens name
 // one row or each its own.
 #include <algorithm>
+#include <type_traits>
 
 #include "network.cuh"
 
@@ -34,17 +35,61 @@ struct LookupArgs {
   unsigned* status;
 };
 
-template <typename T>
+// V consecutive elements a thread (16 bytes, or one where rows start anywhere), kFlight of them on their way
+// at once: first the tokens' indices, then the rows that they name.
+constexpr int kFlight = 4;
+template <typename T, int V>
 __global__ void __launch_bounds__(256) embed_kernel(const __grid_constant__ LookupArgs a) {
   pdl_wait();
-  const long long n = a.rows * a.cols;
-  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) {
-    const long long row = n < (1LL << 32) ? (unsigned)i / a.cols : i / a.cols;
-    const unsigned c = (unsigned)(i - row * a.cols);
-    const unsigned at = row_of_token(a.index, a.wide, row, a.table_rows, a.status);
-    float v = at < a.table_rows ? a.scale * to_f32(((const T*)a.table)[(long long)at * a.st + c]) : 0.f;
-    if (a.add) v += to_f32(((const T*)a.add)[row * a.sa + c]);
-    ((T*)a.y)[row * a.sy + c] = from_f32<T>(v);
+  using P = Pack<T, V>;
+  const unsigned per_row = (a.cols + V - 1) / V;
+  const long long n = a.rows * per_row, step = gridDim.x * 256LL;
+  for (long long i0 = blockIdx.x * 256LL + threadIdx.x; i0 < n; i0 += kFlight * step) {
+    long long row[kFlight];
+    unsigned col[kFlight], at[kFlight];
+    P v[kFlight], add[kFlight];
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      const long long i = min(i0 + k * step, n - 1);
+      row[k] = n < (1LL << 32) ? (unsigned)i / per_row : i / per_row;
+      col[k] = (unsigned)(i - row[k] * per_row) * V;
+      at[k] = row_of_token(a.index, a.wide, row[k], a.table_rows, a.status);
+    }
+    // (a row's last vector may pass its end: its elements one by one)
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      const bool whole = V == 1 || col[k] + V <= a.cols;
+      const T* t = (const T*)a.table + (long long)at[k] * a.st + col[k];
+      const T* p = (const T*)a.add + row[k] * a.sa + col[k];
+      if (whole) {
+        if (at[k] < a.table_rows) v[k] = *reinterpret_cast<const P*>(t);
+        if (a.add) add[k] = *reinterpret_cast<const P*>(p);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (at[k] < a.table_rows && col[k] + e < a.cols) v[k].v[e] = t[e];
+          if (a.add && col[k] + e < a.cols) add[k].v[e] = p[e];
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      if (i0 + k * step >= n) break;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float x = at[k] < a.table_rows ? a.scale * to_f32(v[k].v[e]) : 0.f;
+        if (a.add) x += to_f32(add[k].v[e]);
+        v[k].v[e] = from_f32<T>(x);
+      }
+      T* y = (T*)a.y + row[k] * a.sy + col[k];
+      if (V == 1 || col[k] + V <= a.cols) {
+        *reinterpret_cast<P*>(y) = v[k];
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (col[k] + e < a.cols) y[e] = v[k].v[e];
+      }
+    }
   }
 }
 
@@ -67,7 +112,25 @@ struct SortArgs {
   int wide;
   unsigned table_rows;
   unsigned* status;
+  // the first kernel of all clears the table's gradient with the CTAs behind its tiles' own
+  char* zero;
+  long long zero_rows, zero_bytes, zero_stride;       // of a row
 };
+
+// Clears the rows, a piece of E bytes at a time, with the CTAs from `first` on.
+template <typename E> __device__ __forceinline__ void clear_rows(const SortArgs& a, int first) {
+  const long long per_row = a.zero_bytes / (long long)sizeof(E), n = a.zero_rows * per_row;
+  for (long long i = (blockIdx.x - first) * (long long)kSortThreads + threadIdx.x; i < n; i += (gridDim.x - first) * (long long)kSortThreads) {
+    const long long row = a.zero_rows == 1 ? 0 : n < (1LL << 32) ? (unsigned)i / (unsigned)per_row : i / per_row;
+    *reinterpret_cast<E*>(a.zero + row * a.zero_stride + (i - row * per_row) * (long long)sizeof(E)) = E{};
+  }
+}
+__device__ __forceinline__ void clear_rows(const SortArgs& a, int first) {
+  const unsigned long long all = (uintptr_t)a.zero | (unsigned long long)a.zero_bytes | (unsigned long long)(a.zero_rows > 1 ? a.zero_stride : 0);
+  if (all % 16 == 0) clear_rows<uint4>(a, first);
+  else if (all % 4 == 0) clear_rows<unsigned>(a, first);
+  else clear_rows<unsigned short>(a, first);
+}
 
 __device__ __forceinline__ unsigned sort_key(const SortArgs& a, long long i) {
   return a.key ? a.key[i] : row_of_token(a.index, a.wide, i, a.table_rows, a.status);
@@ -76,6 +139,7 @@ __device__ __forceinline__ unsigned sort_key(const SortArgs& a, long long i) {
 // The tiles' tokens per digit.
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const __grid_constant__ SortArgs a) {
   pdl_wait();
+  if (blockIdx.x >= a.tiles) return clear_rows(a, a.tiles);
   __shared__ unsigned bins[kMaxDigits];
   const int digits = 1 << a.bits;
   for (int d = threadIdx.x; d < digits; d += kSortThreads) bins[d] = 0;
@@ -121,51 +185,57 @@ __device__ __forceinline__ unsigned warp_sums(unsigned v) {
 }
 
 // Tokens to their places, equal digits in their order: a warp takes consecutive tokens of the tile, 32 at a
-// time, and knows how many of a digit the warps before it have.
+// time, and knows how many of a digit the warps before it have.  One tile counts for itself.
 __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_constant__ SortArgs a) {
   pdl_wait();
-  extern __shared__ unsigned short before[];          // [warp][digit]: the warp's tokens, then those before it
+  if (blockIdx.x >= a.tiles) return clear_rows(a, a.tiles);
+  extern __shared__ unsigned keys[];                  // of the tile
   __shared__ unsigned place[kMaxDigits], sums[32];
   const int digits = 1 << a.bits, lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  for (int i = threadIdx.x; i < kSortWarps * digits; i += kSortThreads) before[i] = 0;
-  const unsigned mine = threadIdx.x < digits ? a.total[threadIdx.x] : 0u;
-  const unsigned up_to = warp_sums(mine);
-  if (lane == 31) sums[warp] = up_to;
-  __syncthreads();
-  if (warp == 0) sums[lane] = warp_sums(sums[lane]);
-  __syncthreads();
-  if (threadIdx.x < digits)
-    place[threadIdx.x] = (warp ? sums[warp - 1] : 0u) + up_to - mine + a.count[(long long)threadIdx.x * a.tiles + blockIdx.x];
   const int per_warp = a.per_tile / kSortWarps;
-  const long long first = (long long)blockIdx.x * a.per_tile + (long long)warp * per_warp;
+  const long long first = (long long)blockIdx.x * a.per_tile;
+  const int n = (int)min((long long)a.per_tile, a.n - first);
+  // [warp][digit]: the warp's tokens, then those of the warps before it
+  unsigned short* before = reinterpret_cast<unsigned short*>(keys + a.per_tile);
+  for (int i = threadIdx.x; i < kSortWarps * digits / 2; i += kSortThreads) reinterpret_cast<unsigned*>(before)[i] = 0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += kSortThreads) keys[i] = sort_key(a, first + i);
+  __syncthreads();
   unsigned short* own = before + warp * digits;
-  for (int k = 0; k < per_warp; k += 32) {
-    const long long i = first + k + lane;
-    const bool in = i < a.n;
-    const unsigned d = in ? sort_key(a, i) >> a.shift & (digits - 1) : ~0u;
+  const int start = warp * per_warp, end = min(start + per_warp, n);
+  for (int k = start; k < end; k += 32) {
+    const bool in = k + lane < end;
+    const unsigned d = in ? keys[k + lane] >> a.shift & (digits - 1) : ~0u;
     const unsigned same = __match_any_sync(~0u, d);
     if (in && lane == __ffs(same) - 1) own[d] += (unsigned short)__popc(same);
     __syncwarp();
   }
   __syncthreads();
+  unsigned total = 0;
   if (threadIdx.x < digits) {
-    unsigned s = 0;
     for (int w = 0; w < kSortWarps; ++w) {
       const unsigned v = before[w * digits + threadIdx.x];
-      before[w * digits + threadIdx.x] = (unsigned short)s;
-      s += v;
+      before[w * digits + threadIdx.x] = (unsigned short)total;
+      total += v;
     }
+    if (a.tiles > 1) total = a.total[threadIdx.x];
   }
+  const unsigned up_to = warp_sums(total);
+  if (lane == 31) sums[warp] = up_to;
   __syncthreads();
-  for (int k = 0; k < per_warp; k += 32) {
-    const long long i = first + k + lane;
-    const bool in = i < a.n;
-    const unsigned key = in ? sort_key(a, i) : 0u, d = in ? key >> a.shift & (digits - 1) : ~0u;
+  if (warp == 0) sums[lane] = warp_sums(sums[lane]);
+  __syncthreads();
+  if (threadIdx.x < digits)
+    place[threadIdx.x] = (warp ? sums[warp - 1] : 0u) + up_to - total + (a.tiles > 1 ? a.count[(long long)threadIdx.x * a.tiles + blockIdx.x] : 0u);
+  __syncthreads();
+  for (int k = start; k < end; k += 32) {
+    const bool in = k + lane < end;
+    const unsigned key = in ? keys[k + lane] : 0u, d = in ? key >> a.shift & (digits - 1) : ~0u;
     const unsigned same = __match_any_sync(~0u, d);
     if (in) {
       const unsigned at = place[d] + own[d] + __popc(same & ((1u << lane) - 1));
       a.to_key[at] = key;
-      a.to_id[at] = a.id ? a.id[i] : (unsigned)i;
+      a.to_id[at] = a.id ? a.id[first + k + lane] : (unsigned)(first + k + lane);
     }
     __syncwarp();
     if (in && lane == __ffs(same) - 1) own[d] += (unsigned short)__popc(same);
@@ -182,64 +252,176 @@ struct SumArgs {
   const unsigned* key;
   const unsigned* id;
   void* dtable;
-  float* part;                        // [chunk][2][cols]: a run that began before the chunk; one that goes on after it
+  float* part;                        // [chunk][2][ld]: a run that began before the chunk; one that goes on after it
   long long n, sdy, st;
-  unsigned table_rows, cols;
+  unsigned table_rows, cols, ld;
   float scale;
+  int lanes;                          // threads of a token's row (a power of two up to 256), V columns each
+  int slices;                         // of lanes x V columns
   long long chunks;
 };
 
-template <typename T> __device__ __forceinline__ void put_row(const SumArgs& a, unsigned row, unsigned c, float v) {
-  ((T*)a.dtable)[(long long)row * a.st + c] = from_f32<T>(a.scale * v);
+// V columns of a row of the table's gradient.
+template <typename T, int V> __device__ __forceinline__ void put_row(const SumArgs& a, unsigned row, unsigned c, const float (&s)[V]) {
+  T* to = (T*)a.dtable + (long long)row * a.st + c;
+  if (V > 1 && c + V <= a.cols) {
+    Pack<T, V> q;
+#pragma unroll
+    for (int e = 0; e < V; ++e) q.v[e] = from_f32<T>(a.scale * s[e]);
+    *reinterpret_cast<Pack<T, V>*>(to) = q;
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (c + e < a.cols) to[e] = from_f32<T>(a.scale * s[e]);
+  }
 }
 
-// One CTA per chunk and 256 columns: a thread walks the chunk's tokens with its column.
-template <typename T>
+// A chunk's tokens, in groups of threads that each walk a stretch of them, V columns a thread; eight tokens'
+// rows are on their way at once.  A run of equal rows inside a stretch is a row of the result.  One that
+// began before the stretch (its head) or goes on after it (its tail) is left in shared memory, and the
+// group that a run begins in adds up what the next ones have of it; what passes the chunk goes to the
+// workspace.
+template <typename T, int V>
 __global__ void __launch_bounds__(256) embed_sum_kernel(const __grid_constant__ SumArgs a) {
   pdl_wait();
   __shared__ unsigned key[kChunk + 2], id[kChunk];
-  const long long chunk = blockIdx.x, first = chunk * kChunk;
+  __shared__ float head[256 * V], tail[256 * V];
+  const long long chunk = blockIdx.x / a.slices, first = chunk * kChunk;
   const int n = (int)min((long long)kChunk, a.n - first);
-  for (int i = threadIdx.x; i < n; i += 256) {
-    key[i + 1] = a.key[first + i];
-    id[i] = a.id[first + i];
+  const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = 256 / a.lanes, stretch = kChunk / groups;
+  for (int i = threadIdx.x; i < kChunk + 1; i += 256) {
+    key[i + 1] = i < n || first + i < a.n ? a.key[first + i] : a.table_rows + 1;
+    if (i < n) id[i] = a.id[first + i];
   }
-  if (threadIdx.x == 0) {
-    key[0] = first > 0 ? a.key[first - 1] : a.table_rows;
-    key[n + 1] = first + n < a.n ? a.key[first + n] : a.table_rows;
+  if (threadIdx.x == 0) key[0] = first > 0 ? a.key[first - 1] : a.table_rows + 1;
+  __syncthreads();
+  // key[i + 1] is token i's; rows past the table's are no rows, sorted to the end
+  const unsigned c = ((unsigned)(blockIdx.x % a.slices) * a.lanes + lane) * V;
+  const bool in = c < a.cols;
+  const int g0 = group * stretch, g1 = min(g0 + stretch, n);
+  constexpr int U = 8;
+  float s[V] = {};
+  bool began = g0 < g1 && key[g0] == key[g0 + 1];       // the run at hand began before the stretch
+  bool has_tail = false;
+  for (int i0 = g0; i0 < g1 && key[i0 + 1] < a.table_rows; i0 += U) {
+    Pack<T, V> v[U];
+    if (in) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u;
+        if (i >= g1 || key[i + 1] >= a.table_rows) continue;
+        const T* p = (const T*)a.dy + (long long)id[i] * a.sdy + c;
+        if (V == 1 || c + V <= a.cols) {
+          v[u] = *reinterpret_cast<const Pack<T, V>*>(p);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[u].v[e] = c + e < a.cols ? p[e] : T(0.f);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u;
+      if (i >= g1 || key[i + 1] >= a.table_rows) break;
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] += to_f32(v[u].v[e]);
+      const bool ends = key[i + 2] != key[i + 1];
+      if (!ends && i + 1 < g1) continue;
+      if (began) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) head[threadIdx.x * V + e] = s[e];
+      } else if (!ends) {
+        has_tail = true;
+#pragma unroll
+        for (int e = 0; e < V; ++e) tail[threadIdx.x * V + e] = s[e];
+      } else if (in) {
+        put_row<T, V>(a, key[i + 1], c, s);
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] = 0.f;
+      began = false;
+    }
   }
   __syncthreads();
-  const unsigned c = blockIdx.y * 256 + threadIdx.x;
-  if (c >= a.cols) return;
-  float s = 0.f;
-  bool began = key[1] == key[0];      // the run began before the chunk
-  for (int i = 0; i < n && key[i + 1] < a.table_rows; ++i) {
-    s += to_f32(((const T*)a.dy)[(long long)id[i] * a.sdy + c]);
-    const bool last = key[i + 2] != key[i + 1];
-    if (!last && i + 1 < n) continue;
-    if (began) a.part[2 * chunk * a.cols + c] = s;
-    else if (!last) a.part[(2 * chunk + 1) * a.cols + c] = s;
-    else put_row<T>(a, key[i + 1], c, s);
-    s = 0.f;
-    began = false;
+  if (!in) return;
+  // what the groups from `from` on have of the run of `row`, added to s; whether it goes on after the chunk
+  auto follow = [&](unsigned row, int from) {
+    for (int g = from; g * stretch < n && key[g * stretch + 1] == row; ++g) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] += head[(g * a.lanes + lane) * V + e];
+    }
+    return key[n] == row && key[n + 1] == row;
+  };
+  auto leave = [&](int which) {
+    float* to = a.part + (2 * chunk + which) * a.ld + c;
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (c + e < a.cols) to[e] = s[e];
+  };
+  if (has_tail) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] = tail[threadIdx.x * V + e];
+    const unsigned row = key[g1];
+    if (follow(row, group + 1)) leave(1);
+    else put_row<T, V>(a, row, c, s);
+  }
+  if (group == 0 && key[0] == key[1] && key[1] < a.table_rows) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] = 0.f;
+    follow(key[1], 0);
+    leave(0);
   }
 }
 
-// Runs that pass a chunk's end: the CTA of the chunk that they begin in adds their parts in order.
-template <typename T>
-__global__ void __launch_bounds__(256) embed_join_kernel(const __grid_constant__ SumArgs a) {
+// Runs that pass a chunk's end: the CTA of the chunk that they begin in adds their parts, groups of threads
+// taking consecutive ones side by side, whose sums are then added in their order.
+constexpr int kJoinThreads = 512;
+template <typename T, int V>
+__global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_constant__ SumArgs a) {
   pdl_wait();
-  const long long chunk = blockIdx.x, end = (chunk + 1) * kChunk;
+  __shared__ float run[kJoinThreads * V];
+  const long long chunk = blockIdx.x / a.slices, end = (chunk + 1) * kChunk;
   if (end >= a.n) return;
   const unsigned row = a.key[end - 1];
   if (row >= a.table_rows || a.key[end] != row) return;
-  if (a.key[end - kChunk] == row && end > kChunk && a.key[end - kChunk - 1] == row) return;   // it began earlier
-  const unsigned c = blockIdx.y * 256 + threadIdx.x;
-  if (c >= a.cols) return;
-  float s = a.part[(2 * chunk + 1) * a.cols + c];
-  for (long long q = chunk + 1; q < a.chunks && a.key[q * kChunk] == row; ++q) s += a.part[2 * q * a.cols + c];
-  put_row<T>(a, row, c, s);
+  if (chunk > 0 && a.key[end - kChunk] == row && a.key[end - kChunk - 1] == row) return;   // it began earlier
+  // the last chunk that begins with the row: steps that double, then halve
+  long long last = chunk + 1, step = 1;
+  const auto has = [&](long long q) { return q < a.chunks && a.key[q * kChunk] == row; };
+  while (has(last + step)) {
+    last += step;
+    step *= 2;
+  }
+  for (; step; step /= 2)
+    if (has(last + step)) last += step;
+  const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = kJoinThreads / a.lanes;
+  const unsigned c = ((unsigned)(blockIdx.x % a.slices) * a.lanes + lane) * V;
+  const long long count = last - chunk;                 // the chunks after the first
+  const long long q0 = chunk + 1 + count * group / groups, q1 = chunk + 1 + count * (group + 1) / groups;
+  float s[V] = {};
+  if (c < a.cols) {
+#pragma unroll 4
+    for (long long q = q0; q < q1; ++q) {
+      const float* p = a.part + 2 * q * a.ld + c;
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] += c + e < a.cols ? __ldcg(p + e) : 0.f;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) run[threadIdx.x * V + e] = s[e];
+  __syncthreads();
+  if (group > 0 || c >= a.cols) return;
+  const float* p = a.part + (2 * chunk + 1) * a.ld + c;
+#pragma unroll
+  for (int e = 0; e < V; ++e) s[e] = c + e < a.cols ? __ldcg(p + e) : 0.f;
+  for (int g = 0; g < groups; ++g) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] += run[(g * a.lanes + lane) * V + e];
+  }
+  put_row<T, V>(a, row, c, s);
 }
+
+constexpr long long kOneTile = 24576;   // tokens of a tile at most: their keys lie in shared memory
 
 // How the tokens are sorted: passes of equal bits for the rows and one more (none).
 struct SortPlan {
@@ -251,15 +433,15 @@ SortPlan sort_plan(long long tokens, long long table_rows) {
   while ((1LL << need) <= table_rows) ++need;
   p.passes = (need + 9) / 10;
   p.bits = (need + p.passes - 1) / p.passes;
-  const long long least = 4096;
-  long long per = std::max(least, (tokens + kNetSms - 1) / kNetSms);
-  per = (per + kSortThreads - 1) / kSortThreads * kSortThreads;
-  // a warp counts its tokens of a digit in 16 bits
-  per = std::min<long long>(per, 32768 / 32 * kSortThreads);
+  // one tile needs no counts; more of them share the SMs, within what a CTA's shared memory holds
+  long long per = tokens <= kOneTile ? tokens : std::clamp<long long>((tokens + kNetSms - 1) / kNetSms, 4096, kOneTile);
+  per = std::max<long long>(1, (per + kSortThreads - 1) / kSortThreads) * kSortThreads;
   p.per_tile = (int)per;
   p.tiles = (int)((tokens + per - 1) / per);
   return p;
 }
+
+size_t part_ld(long long cols) { return (size_t)(cols + 3) / 4 * 4; }
 
 // The workspace behind its header.
 struct EmbedScratch {
@@ -278,7 +460,7 @@ EmbedScratch scratch_of(char* base, long long tokens, long long table_rows, long
   }
   s.count = (unsigned*)take((size_t)4 * kMaxDigits * (size_t)p.tiles);
   s.total = (unsigned*)take((size_t)4 * kMaxDigits);
-  s.part = (float*)take((size_t)8 * (size_t)cols * (size_t)((tokens + kChunk - 1) / kChunk));
+  s.part = (float*)take((size_t)8 * part_ld(cols) * (size_t)((tokens + kChunk - 1) / kChunk));
   s.bytes = at;
   return s;
 }
@@ -323,8 +505,10 @@ extern "C" abcd_status abcd_embedding(abcd_ctx* ctx, const abcd_matrix* table, c
                      (unsigned)table->rows, (unsigned)y->cols, index_dtype == ABCD_I64, scale, (unsigned*)ctx->net_base};
   return with_type(y->dtype, [&](auto t) {
     using T = decltype(t);
-    const long long grid = std::min<long long>((y->rows * y->cols + 255) / 256, 8LL * ctx->num_sms);
-    return check_launch(ctx, "embed_kernel", launch_pdl(embed_kernel<T>, dim3((unsigned)grid), dim3(256), 0, ctx->stream, a));
+    constexpr int V = 16 / sizeof(T);
+    const bool vec = rows_aligned(table, 16) && rows_aligned(y, 16) && (!add || rows_aligned(add, 16));
+    const long long units = y->rows * (vec ? (y->cols + V - 1) / V : y->cols), grid = std::min<long long>((units + 255) / 256, 8LL * ctx->num_sms);
+    return check_launch(ctx, "embed_kernel", launch_pdl(vec ? embed_kernel<T, V> : embed_kernel<T, 1>, dim3((unsigned)grid), dim3(256), 0, ctx->stream, a));
   });
 }
 
@@ -342,36 +526,50 @@ extern "C" abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix*
   const EmbedScratch s = scratch_of(ctx->net_base, n, dtable->rows, dy->cols);
   if (!ctx->net_base || s.bytes > ctx->net_bytes)
     return fail(ctx, ABCD_ERR_WORKSPACE, "%s: the network workspace has %zu bytes, needs %zu", what, ctx->net_bytes, s.bytes);
-  const size_t e = elem_size(dtable->dtype);
-  const cudaError_t z = cudaMemset2DAsync(dtable->data, (size_t)dtable->stride * e, 0, (size_t)dtable->cols * e, (size_t)dtable->rows, ctx->stream);
-  if (z != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(z));
-  if (n == 0) return ABCD_OK;
   const SortPlan p = sort_plan(n, dtable->rows);
-  const size_t smem = (size_t)kSortWarps * 2 * ((size_t)1 << p.bits);
+  const size_t smem = 4 * (size_t)p.per_tile + (size_t)kSortWarps * 2 * ((size_t)1 << p.bits);
   const cudaError_t room = allow_smem(ctx, (const void*)sort_place_kernel);
   if (room != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(room));
+  const long long e = (long long)elem_size(dtable->dtype);
+  const bool flat = dtable->stride == dtable->cols;
   SortArgs q{index, nullptr, nullptr, s.key[0], s.id[0], s.count, s.total, n, p.tiles, p.per_tile, 0, p.bits,
-             index_dtype == ABCD_I64, (unsigned)dtable->rows, (unsigned*)ctx->net_base};
+             index_dtype == ABCD_I64, (unsigned)dtable->rows, (unsigned*)ctx->net_base, (char*)dtable->data,
+             flat ? 1 : dtable->rows, (flat ? dtable->rows : 1) * dtable->cols * e, dtable->stride * e};
+  // CTAs that clear the gradient beside the first kernel's own
+  const long long clear = std::min<long long>((dtable->rows * dtable->cols * e + 65535) / 65536, 2LL * ctx->num_sms);
+  const auto sort = [&](const char* name, auto* kernel, long long grid, int threads, size_t bytes) {
+    return check_launch(ctx, name, launch_pdl(kernel, dim3((unsigned)grid), dim3((unsigned)threads), bytes, ctx->stream, q));
+  };
+  if (n == 0) return sort("sort_count_kernel", sort_count_kernel, clear, kSortThreads, 0);
   for (int pass = 0; pass < p.passes; ++pass) {
     q.shift = pass * p.bits;
-    abcd_status st = check_launch(ctx, "sort_count_kernel", launch_pdl(sort_count_kernel, dim3(p.tiles), dim3(kSortThreads), 0, ctx->stream, q));
-    if (st != ABCD_OK) return st;
-    st = check_launch(ctx, "sort_scan_kernel", launch_pdl(sort_scan_kernel, dim3(((1 << p.bits) + 7) / 8), dim3(256), 0, ctx->stream, q));
-    if (st != ABCD_OK) return st;
-    st = check_launch(ctx, "sort_place_kernel", launch_pdl(sort_place_kernel, dim3(p.tiles), dim3(kSortThreads), smem, ctx->stream, q));
+    const long long more = pass == 0 ? clear : 0;
+    abcd_status st = ABCD_OK;
+    if (p.tiles > 1) {
+      st = sort("sort_count_kernel", sort_count_kernel, p.tiles + more, kSortThreads, 0);
+      if (st == ABCD_OK) st = sort("sort_scan_kernel", sort_scan_kernel, ((1 << p.bits) + 7) / 8, 256, 0);
+    }
+    if (st == ABCD_OK) st = sort("sort_place_kernel", sort_place_kernel, p.tiles + (p.tiles > 1 ? 0 : more), kSortThreads, smem);
     if (st != ABCD_OK) return st;
     q.key = q.to_key;
     q.id = q.to_id;
     q.to_key = s.key[(pass + 1) & 1];
     q.to_id = s.id[(pass + 1) & 1];
   }
-  const SumArgs a{dy->data, q.key, q.id, dtable->data, s.part, n, dy->stride, dtable->stride, (unsigned)dtable->rows,
-                  (unsigned)dy->cols, scale, (n + kChunk - 1) / kChunk};
+  SumArgs a{dy->data, q.key, q.id, dtable->data, s.part, n, dy->stride, dtable->stride, (unsigned)dtable->rows,
+            (unsigned)dy->cols, (unsigned)part_ld(dy->cols), scale, 1, 1, (n + kChunk - 1) / kChunk};
+  const bool vec = rows_aligned(dy, 16) && rows_aligned(dtable, 16);
   return with_type(dy->dtype, [&](auto t) {
     using T = decltype(t);
-    const dim3 grid((unsigned)a.chunks, (a.cols + 255) / 256);
-    const abcd_status st = check_launch(ctx, "embed_sum_kernel", launch_pdl(embed_sum_kernel<T>, grid, dim3(256), 0, ctx->stream, a));
-    if (st != ABCD_OK) return st;
-    return check_launch(ctx, "embed_join_kernel", launch_pdl(embed_join_kernel<T>, grid, dim3(256), 0, ctx->stream, a));
+    const auto sum = [&](auto width) {
+      constexpr int V = decltype(width)::value;
+      while (a.lanes < 256 && a.lanes * V < (long long)a.cols) a.lanes *= 2;
+      a.slices = (int)((a.cols + a.lanes * V - 1) / (a.lanes * V));
+      const dim3 grid((unsigned)(a.chunks * a.slices));
+      const abcd_status st = check_launch(ctx, "embed_sum_kernel", launch_pdl(embed_sum_kernel<T, V>, grid, dim3(256), 0, ctx->stream, a));
+      if (st != ABCD_OK || a.chunks == 1) return st;
+      return check_launch(ctx, "embed_join_kernel", launch_pdl(embed_join_kernel<T, V>, grid, dim3(kJoinThreads), 0, ctx->stream, a));
+    };
+    return vec ? sum(std::integral_constant<int, 16 / sizeof(T)>()) : sum(std::integral_constant<int, 1>());
   });
 }

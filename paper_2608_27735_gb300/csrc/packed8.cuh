@@ -31,7 +31,7 @@ struct Unpacked {
   long long stride;
   int dtype;
 };
-// Up to three matrices unpacked by one launch.
+// Up to three matrices unpacked, by one launch for each type.
 abcd_status unpack(abcd_ctx* ctx, const Unpacked* list, int n);
 
 }  // namespace abcd
