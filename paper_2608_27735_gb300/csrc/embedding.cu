@@ -29,65 +29,73 @@ struct LookupArgs {
   const void* add;
   void* y;
   long long rows, st, sa, sy;
-  unsigned table_rows, cols;
+  unsigned table_rows, cols, lanes;   // lanes: threads of a token, up to 256
   int wide;                           // 64-bit indices
   float scale;
   unsigned* status;
 };
 
-// V consecutive elements a thread (16 bytes, or one where rows start anywhere), kFlight of them on their way
-// at once: first the tokens' indices, then the rows that they name.
+// V consecutive columns a thread (16 bytes, or one where rows start anywhere), `lanes` threads a token,
+// kFlight tokens of a thread on their way at once: first their indices, then the rows that they name.
 constexpr int kFlight = 4;
 template <typename T, int V>
-__global__ void __launch_bounds__(256) embed_kernel(const __grid_constant__ LookupArgs a) {
+__global__ void __launch_bounds__(256, V > 4 ? 3 : 4) embed_kernel(const __grid_constant__ LookupArgs a) {
   pdl_wait();
   using P = Pack<T, V>;
-  const unsigned per_row = (a.cols + V - 1) / V;
-  const long long n = a.rows * per_row, step = gridDim.x * 256LL;
-  for (long long i0 = blockIdx.x * 256LL + threadIdx.x; i0 < n; i0 += kFlight * step) {
-    long long row[kFlight];
-    unsigned col[kFlight], at[kFlight];
+  const unsigned groups = 256u / a.lanes, group = threadIdx.x / a.lanes;
+  const unsigned c = (blockIdx.x * a.lanes + threadIdx.x - group * a.lanes) * V;
+  if (group >= groups || c >= a.cols) return;
+  const bool whole = V == 1 || c + V <= a.cols;          // else the row's last vector passes its end
+  const T* table = (const T*)a.table + c;
+  const long long step = gridDim.y * (long long)(groups * kFlight);
+  unsigned at[kFlight];
+  auto rows_named = [&](long long r0) {
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k)
+      at[k] = r0 + k * groups < a.rows ? row_of_token(a.index, a.wide, r0 + k * groups, a.table_rows, a.status) : a.table_rows;
+  };
+  long long r0 = blockIdx.y * (long long)(groups * kFlight) + group;
+  rows_named(r0);
+  for (; r0 < a.rows; r0 += step) {
+    const int n = (int)min((long long)kFlight, (a.rows - r0 + groups - 1) / groups);
     P v[kFlight], add[kFlight];
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
-      const long long i = min(i0 + k * step, n - 1);
-      row[k] = n < (1LL << 32) ? (unsigned)i / per_row : i / per_row;
-      col[k] = (unsigned)(i - row[k] * per_row) * V;
-      at[k] = row_of_token(a.index, a.wide, row[k], a.table_rows, a.status);
+      if (at[k] >= a.table_rows) v[k] = P{};
+      else if (whole) v[k] = *reinterpret_cast<const P*>(table + at[k] * a.st);
+      else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[k].v[e] = c + e < a.cols ? table[at[k] * a.st + e] : T(0.f);
+      }
     }
-    // (a row's last vector may pass its end: its elements one by one)
+    rows_named(r0 + step);                                // the next ones' indices
+    if (a.add) {
+      const T* p = (const T*)a.add + r0 * a.sa + c;
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k) {
-      const bool whole = V == 1 || col[k] + V <= a.cols;
-      const T* t = (const T*)a.table + (long long)at[k] * a.st + col[k];
-      const T* p = (const T*)a.add + row[k] * a.sa + col[k];
-      if (whole) {
-        if (at[k] < a.table_rows) v[k] = *reinterpret_cast<const P*>(t);
-        if (a.add) add[k] = *reinterpret_cast<const P*>(p);
-      } else {
+      for (int k = 0; k < kFlight; ++k, p += groups * a.sa) {
+        if (k >= n) break;
+        if (whole) add[k] = *reinterpret_cast<const P*>(p);
+        else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          if (at[k] < a.table_rows && col[k] + e < a.cols) v[k].v[e] = t[e];
-          if (a.add && col[k] + e < a.cols) add[k].v[e] = p[e];
+          for (int e = 0; e < V; ++e) add[k].v[e] = c + e < a.cols ? p[e] : T(0.f);
         }
       }
     }
+    T* y = (T*)a.y + r0 * a.sy + c;
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k) {
-      if (i0 + k * step >= n) break;
+    for (int k = 0; k < kFlight; ++k, y += groups * a.sy) {
+      if (k >= n) break;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        float x = at[k] < a.table_rows ? a.scale * to_f32(v[k].v[e]) : 0.f;
+        float x = a.scale * to_f32(v[k].v[e]);
         if (a.add) x += to_f32(add[k].v[e]);
         v[k].v[e] = from_f32<T>(x);
       }
-      T* y = (T*)a.y + row[k] * a.sy + col[k];
-      if (V == 1 || col[k] + V <= a.cols) {
-        *reinterpret_cast<P*>(y) = v[k];
-      } else {
+      if (whole) *reinterpret_cast<P*>(y) = v[k];
+      else {
 #pragma unroll
         for (int e = 0; e < V; ++e)
-          if (col[k] + e < a.cols) y[e] = v[k].v[e];
+          if (c + e < a.cols) y[e] = v[k].v[e];
       }
     }
   }
@@ -145,8 +153,16 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const __grid_c
   for (int d = threadIdx.x; d < digits; d += kSortThreads) bins[d] = 0;
   __syncthreads();
   const long long first = (long long)blockIdx.x * a.per_tile, end = min(first + a.per_tile, a.n);
-  for (long long i = first + threadIdx.x; i < end; i += kSortThreads)
-    atomicAdd(&bins[sort_key(a, i) >> a.shift & (digits - 1)], 1u);
+  constexpr int U = 8;
+  for (long long i = first + threadIdx.x; i < end; i += U * kSortThreads) {
+    unsigned key[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u * kSortThreads < end) key[u] = sort_key(a, i + u * kSortThreads);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u * kSortThreads < end) atomicAdd(&bins[key[u] >> a.shift & (digits - 1)], 1u);
+  }
   __syncthreads();
   for (int d = threadIdx.x; d < digits; d += kSortThreads) a.count[(long long)d * a.tiles + blockIdx.x] = bins[d];
 }
@@ -190,7 +206,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
   pdl_wait();
   if (blockIdx.x >= a.tiles) return clear_rows(a, a.tiles);
   extern __shared__ unsigned keys[];                  // of the tile
-  __shared__ unsigned place[kMaxDigits], sums[32];
+  __shared__ unsigned place[kMaxDigits], local[kMaxDigits], sums[32];
   const int digits = 1 << a.bits, lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   const int per_warp = a.per_tile / kSortWarps;
   const long long first = (long long)blockIdx.x * a.per_tile;
@@ -201,6 +217,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
 #pragma unroll 4
   for (int i = threadIdx.x; i < n; i += kSortThreads) keys[i] = sort_key(a, first + i);
   __syncthreads();
+  unsigned short* sorted = before + kSortWarps * digits;     // the tile's tokens in the order of their digits
   unsigned short* own = before + warp * digits;
   const int start = warp * per_warp, end = min(start + per_warp, n);
   for (int k = start; k < end; k += 32) {
@@ -218,28 +235,45 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
       before[w * digits + threadIdx.x] = (unsigned short)total;
       total += v;
     }
-    if (a.tiles > 1) total = a.total[threadIdx.x];
   }
-  const unsigned up_to = warp_sums(total);
-  if (lane == 31) sums[warp] = up_to;
-  __syncthreads();
-  if (warp == 0) sums[lane] = warp_sums(sums[lane]);
-  __syncthreads();
-  if (threadIdx.x < digits)
-    place[threadIdx.x] = (warp ? sums[warp - 1] : 0u) + up_to - total + (a.tiles > 1 ? a.count[(long long)threadIdx.x * a.tiles + blockIdx.x] : 0u);
+  // a digit's first place, in all and in the tile
+  auto first_places = [&](unsigned count) {
+    const unsigned up_to = warp_sums(count);
+    __syncthreads();
+    if (lane == 31) sums[warp] = up_to;
+    __syncthreads();
+    if (warp == 0) sums[lane] = warp_sums(sums[lane]);
+    __syncthreads();
+    return (warp ? sums[warp - 1] : 0u) + up_to - count;
+  };
+  const unsigned inside = first_places(total);
+  unsigned outside = inside;
+  if (a.tiles > 1) {
+    outside = first_places(threadIdx.x < digits ? a.total[threadIdx.x] : 0u);
+    if (threadIdx.x < digits) outside += a.count[(long long)threadIdx.x * a.tiles + blockIdx.x];
+  }
+  if (threadIdx.x < digits) {
+    local[threadIdx.x] = inside;
+    place[threadIdx.x] = outside - inside;
+  }
   __syncthreads();
   for (int k = start; k < end; k += 32) {
     const bool in = k + lane < end;
-    const unsigned key = in ? keys[k + lane] : 0u, d = in ? key >> a.shift & (digits - 1) : ~0u;
+    const unsigned d = in ? keys[k + lane] >> a.shift & (digits - 1) : ~0u;
     const unsigned same = __match_any_sync(~0u, d);
-    if (in) {
-      const unsigned at = place[d] + own[d] + __popc(same & ((1u << lane) - 1));
-      a.to_key[at] = key;
-      a.to_id[at] = a.id ? a.id[first + k + lane] : (unsigned)(first + k + lane);
-    }
+    if (in) sorted[local[d] + own[d] + __popc(same & ((1u << lane) - 1))] = (unsigned short)(k + lane);
     __syncwarp();
     if (in && lane == __ffs(same) - 1) own[d] += (unsigned short)__popc(same);
     __syncwarp();
+  }
+  __syncthreads();
+  // consecutive lanes write consecutive places of a digit
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += kSortThreads) {
+    const int from = sorted[i];
+    const unsigned key = keys[from], at = place[key >> a.shift & (digits - 1)] + i;
+    a.to_key[at] = key;
+    a.to_id[at] = a.id ? a.id[first + from] : (unsigned)(first + from);
   }
 }
 
@@ -256,7 +290,7 @@ struct SumArgs {
   long long n, sdy, st;
   unsigned table_rows, cols, ld;
   float scale;
-  int lanes;                          // threads of a token's row (a power of two up to 256), V columns each
+  int lanes;                          // threads of a token's row, up to 256, V columns each
   int slices;                         // of lanes x V columns
   long long chunks;
 };
@@ -288,7 +322,7 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const __grid_constant__ 
   __shared__ float head[256 * V], tail[256 * V];
   const long long chunk = blockIdx.x / a.slices, first = chunk * kChunk;
   const int n = (int)min((long long)kChunk, a.n - first);
-  const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = 256 / a.lanes, stretch = kChunk / groups;
+  const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = 256 / a.lanes, stretch = (kChunk + groups - 1) / groups;
   for (int i = threadIdx.x; i < kChunk + 1; i += 256) {
     key[i + 1] = i < n || first + i < a.n ? a.key[first + i] : a.table_rows + 1;
     if (i < n) id[i] = a.id[first + i];
@@ -297,8 +331,8 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const __grid_constant__ 
   __syncthreads();
   // key[i + 1] is token i's; rows past the table's are no rows, sorted to the end
   const unsigned c = ((unsigned)(blockIdx.x % a.slices) * a.lanes + lane) * V;
-  const bool in = c < a.cols;
-  const int g0 = group * stretch, g1 = min(g0 + stretch, n);
+  const bool in = c < a.cols && group < groups;
+  const int g0 = group < groups ? group * stretch : n, g1 = min(g0 + stretch, n);
   constexpr int U = 8;
   float s[V] = {};
   bool began = g0 < g1 && key[g0] == key[g0 + 1];       // the run at hand began before the stretch
@@ -373,55 +407,80 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const __grid_constant__ 
   }
 }
 
-// Runs that pass a chunk's end: the CTA of the chunk that they begin in adds their parts, groups of threads
-// taking consecutive ones side by side, whose sums are then added in their order.
-constexpr int kJoinThreads = 512;
+// Runs that pass a chunk's end, by the chunk that they begin in.  A group of threads has a chunk; a run over
+// few chunks it adds up by itself, for longer ones all groups of the CTA take consecutive parts side by
+// side, whose sums are then added in their order.
+constexpr int kJoinThreads = 256, kJoinAlone = 8;
 template <typename T, int V>
 __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_constant__ SumArgs a) {
   pdl_wait();
   __shared__ float run[kJoinThreads * V];
-  const long long chunk = blockIdx.x / a.slices, end = (chunk + 1) * kChunk;
-  if (end >= a.n) return;
-  const unsigned row = a.key[end - 1];
-  if (row >= a.table_rows || a.key[end] != row) return;
-  if (chunk > 0 && a.key[end - kChunk] == row && a.key[end - kChunk - 1] == row) return;   // it began earlier
-  // the last chunk that begins with the row: steps that double, then halve
-  long long last = chunk + 1, step = 1;
-  const auto has = [&](long long q) { return q < a.chunks && a.key[q * kChunk] == row; };
-  while (has(last + step)) {
-    last += step;
-    step *= 2;
-  }
-  for (; step; step /= 2)
-    if (has(last + step)) last += step;
+  __shared__ long long last_of[kJoinThreads];
   const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = kJoinThreads / a.lanes;
+  const long long base = blockIdx.x / a.slices * (long long)groups;
   const unsigned c = ((unsigned)(blockIdx.x % a.slices) * a.lanes + lane) * V;
-  const long long count = last - chunk;                 // the chunks after the first
-  const long long q0 = chunk + 1 + count * group / groups, q1 = chunk + 1 + count * (group + 1) / groups;
-  float s[V] = {};
-  if (c < a.cols) {
-#pragma unroll 4
-    for (long long q = q0; q < q1; ++q) {
-      const float* p = a.part + 2 * q * a.ld + c;
+  const bool in = c < a.cols && group < groups;
+  const auto has = [&](long long q, unsigned row) { return q < a.chunks && a.key[q * kChunk] == row; };
+  auto add_part = [&](float (&s)[V], long long q, int which) {
+    const float* p = a.part + (2 * q + which) * a.ld + c;
 #pragma unroll
-      for (int e = 0; e < V; ++e) s[e] += c + e < a.cols ? __ldcg(p + e) : 0.f;
+    for (int e = 0; e < V; ++e) s[e] += c + e < a.cols ? __ldcg(p + e) : 0.f;
+  };
+  long long last = -1;                                  // of a run that is too long for the group
+  if (group < groups) {
+    const long long chunk = base + group, end = (chunk + 1) * kChunk;
+    if (end < a.n) {
+      const unsigned row = a.key[end - 1], then = a.key[end], first = a.key[end - kChunk], before = chunk > 0 ? a.key[end - kChunk - 1] : a.table_rows;
+      if (row < a.table_rows && then == row && !(first == row && before == row)) {
+        // the last chunk that begins with the row: steps that double, then halve
+        last = chunk + 1;
+        long long step = 1;
+        while (has(last + step, row)) {
+          last += step;
+          step *= 2;
+        }
+        for (; step; step /= 2)
+          if (has(last + step, row)) last += step;
+        if (last - chunk <= kJoinAlone) {
+          if (in) {
+            float s[V] = {};
+            add_part(s, chunk, 1);
+            for (long long q = chunk + 1; q <= last; ++q) add_part(s, q, 0);
+            put_row<T, V>(a, row, c, s);
+          }
+          last = -1;
+        }
+      }
     }
+    if (lane == 0) last_of[group] = last;
   }
-#pragma unroll
-  for (int e = 0; e < V; ++e) run[threadIdx.x * V + e] = s[e];
   __syncthreads();
-  if (group > 0 || c >= a.cols) return;
-  const float* p = a.part + (2 * chunk + 1) * a.ld + c;
-#pragma unroll
-  for (int e = 0; e < V; ++e) s[e] = c + e < a.cols ? __ldcg(p + e) : 0.f;
   for (int g = 0; g < groups; ++g) {
+    if (last_of[g] < 0) continue;
+    const long long chunk = base + g, count = last_of[g] - chunk;
+    float s[V] = {};
+    if (in) {
+      const long long q1 = chunk + 1 + count * (group + 1) / groups;
+#pragma unroll 4
+      for (long long q = chunk + 1 + count * group / groups; q < q1; ++q) add_part(s, q, 0);
+    }
+    __syncthreads();
 #pragma unroll
-    for (int e = 0; e < V; ++e) s[e] += run[(g * a.lanes + lane) * V + e];
+    for (int e = 0; e < V; ++e) run[threadIdx.x * V + e] = s[e];
+    __syncthreads();
+    if (group > 0 || !in) continue;
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] = 0.f;
+    add_part(s, chunk, 1);
+    for (int h = 0; h < groups; ++h) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] += run[(h * a.lanes + lane) * V + e];
+    }
+    put_row<T, V>(a, a.key[(chunk + 1) * kChunk], c, s);
   }
-  put_row<T, V>(a, row, c, s);
 }
 
-constexpr long long kOneTile = 24576;   // tokens of a tile at most: their keys lie in shared memory
+constexpr long long kOneTile = 16384;   // tokens of a tile at most: their keys lie in shared memory
 
 // How the tokens are sorted: passes of equal bits for the rows and one more (none).
 struct SortPlan {
@@ -501,14 +560,17 @@ extern "C" abcd_status abcd_embedding(abcd_ctx* ctx, const abcd_matrix* table, c
   const bool on_add = add && overlap(add, y) && !(add->data == y->data && (add->stride == y->stride || y->rows == 1));
   if (overlap(table, y) || on_add || on_index(y, index, index_dtype, y->rows))
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: y overlaps an operand", what);
-  const LookupArgs a{table->data, index, add ? add->data : nullptr, y->data, y->rows, table->stride, add ? add->stride : 0, y->stride,
-                     (unsigned)table->rows, (unsigned)y->cols, index_dtype == ABCD_I64, scale, (unsigned*)ctx->net_base};
+  LookupArgs a{table->data, index, add ? add->data : nullptr, y->data, y->rows, table->stride, add ? add->stride : 0, y->stride,
+                     (unsigned)table->rows, (unsigned)y->cols, 1, index_dtype == ABCD_I64, scale, (unsigned*)ctx->net_base};
   return with_type(y->dtype, [&](auto t) {
     using T = decltype(t);
     constexpr int V = 16 / sizeof(T);
     const bool vec = rows_aligned(table, 16) && rows_aligned(y, 16) && (!add || rows_aligned(add, 16));
-    const long long units = y->rows * (vec ? (y->cols + V - 1) / V : y->cols), grid = std::min<long long>((units + 255) / 256, 8LL * ctx->num_sms);
-    return check_launch(ctx, "embed_kernel", launch_pdl(vec ? embed_kernel<T, V> : embed_kernel<T, 1>, dim3((unsigned)grid), dim3(256), 0, ctx->stream, a));
+    const long long vectors = vec ? (y->cols + V - 1) / V : y->cols;
+    a.lanes = (unsigned)std::min(256LL, vectors);
+    const long long slices = (vectors + a.lanes - 1) / a.lanes, per_cta = 256 / a.lanes * kFlight;
+    const long long grid = std::min((y->rows + per_cta - 1) / per_cta, std::max(1LL, 12LL * ctx->num_sms / slices));
+    return check_launch(ctx, "embed_kernel", launch_pdl(vec ? embed_kernel<T, V> : embed_kernel<T, 1>, dim3((unsigned)slices, (unsigned)grid), dim3(256), 0, ctx->stream, a));
   });
 }
 
@@ -527,7 +589,7 @@ extern "C" abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix*
   if (!ctx->net_base || s.bytes > ctx->net_bytes)
     return fail(ctx, ABCD_ERR_WORKSPACE, "%s: the network workspace has %zu bytes, needs %zu", what, ctx->net_bytes, s.bytes);
   const SortPlan p = sort_plan(n, dtable->rows);
-  const size_t smem = 4 * (size_t)p.per_tile + (size_t)kSortWarps * 2 * ((size_t)1 << p.bits);
+  const size_t smem = 6 * (size_t)p.per_tile + (size_t)kSortWarps * 2 * ((size_t)1 << p.bits);
   const cudaError_t room = allow_smem(ctx, (const void*)sort_place_kernel);
   if (room != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(room));
   const long long e = (long long)elem_size(dtable->dtype);
@@ -563,12 +625,14 @@ extern "C" abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix*
     using T = decltype(t);
     const auto sum = [&](auto width) {
       constexpr int V = decltype(width)::value;
-      while (a.lanes < 256 && a.lanes * V < (long long)a.cols) a.lanes *= 2;
+      a.lanes = (int)std::min<long long>(256, (a.cols + V - 1) / V);
       a.slices = (int)((a.cols + a.lanes * V - 1) / (a.lanes * V));
       const dim3 grid((unsigned)(a.chunks * a.slices));
       const abcd_status st = check_launch(ctx, "embed_sum_kernel", launch_pdl(embed_sum_kernel<T, V>, grid, dim3(256), 0, ctx->stream, a));
       if (st != ABCD_OK || a.chunks == 1) return st;
-      return check_launch(ctx, "embed_join_kernel", launch_pdl(embed_join_kernel<T, V>, grid, dim3(kJoinThreads), 0, ctx->stream, a));
+      const long long groups = kJoinThreads / a.lanes;
+      return check_launch(ctx, "embed_join_kernel", launch_pdl(embed_join_kernel<T, V>, dim3((unsigned)((a.chunks + groups - 1) / groups * a.slices)),
+                                                              dim3(kJoinThreads), 0, ctx->stream, a));
     };
     return vec ? sum(std::integral_constant<int, 16 / sizeof(T)>()) : sum(std::integral_constant<int, 1>());
   });

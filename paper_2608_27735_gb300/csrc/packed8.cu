@@ -19,25 +19,29 @@ struct PackedArgs {
     signed char* codes;
     unsigned char* powers;
     long long rows, cols, sx, sc, sp;
-    long long first;                  // units before this matrix's
-    long long per_row;                // units of a row: eight columns each, four to a group
+    int lanes;                        // threads of a row, eight columns each, four to a group of columns
     int vec;                          // x's rows start on 16-byte boundaries
   } m[3];
-  int n;
-  long long units;
 };
 
-constexpr int kFlight = 4;            // units of a thread that are on their way at once
+constexpr int kFlight = 4;            // rows of a thread that are on their way at once
 
-// Where a unit lies.
-struct Place { long long row, col; int left; };
-__device__ __forceinline__ Place place_of(const PackedArgs::One& o, long long at) {
-  Place p;
-  p.row = o.rows == 1 ? 0 : at < (1LL << 32) ? (unsigned)at / (unsigned)o.per_row : at / o.per_row;
-  p.col = 8 * (at - p.row * o.per_row);
-  p.left = (int)min(8LL, o.cols - p.col);
-  return p;
-}
+// The rows that a CTA takes at a time, and the thread's place in them: the addresses of a thread's units then
+// differ by whole rows.
+struct Share {
+  long long row, step;                // the first row, rows from one turn to the next
+  int groups;                         // rows between a turn's units
+  long long col;
+  int left;                           // the thread's columns: none for a thread without a unit
+  __device__ __forceinline__ explicit Share(const PackedArgs::One& o) {
+    groups = 256 / o.lanes;
+    const int group = (int)threadIdx.x / o.lanes, lane = (int)threadIdx.x - group * o.lanes;
+    col = (blockIdx.x * (long long)o.lanes + lane) * 8;
+    left = group < groups ? (int)min(8LL, o.cols - col) : 0;
+    row = blockIdx.y * (long long)(groups * kFlight) + group;
+    step = gridDim.y * (long long)(groups * kFlight);
+  }
+};
 
 // Eight values of a unit as they lie in memory, zeros past the row's end.
 template <typename T> struct Eight {
@@ -101,36 +105,34 @@ __device__ __forceinline__ uint2 codes_of(Eight<T>& x, int power, unsigned top) 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) pack8_kernel(const __grid_constant__ PackedArgs a) {
+__global__ void __launch_bounds__(256, 4) pack8_kernel(const __grid_constant__ PackedArgs a) {
   pdl_wait();
   const PackedArgs::One& o = a.m[0];
-  const long long step = gridDim.x * 256LL;
-  // the four lanes of a group are in or out together
-  for (long long i0 = blockIdx.x * 256LL + threadIdx.x; i0 - (threadIdx.x & 31) < a.units; i0 += kFlight * step) {
-    Place p[kFlight];
-    Eight<T> x[kFlight];
+  const Share at(o);
+  const T* x = (const T*)o.x + at.row * o.sx + at.col;
+  signed char* to = o.codes + at.row * o.sc + at.col;
+  unsigned char* power_to = o.powers + at.row * o.sp + at.col / 32;
+  // (a warp's lanes take their turns together: the four lanes of a group share its largest magnitude)
+  for (long long r = at.row; r - (threadIdx.x / o.lanes) < o.rows; r += at.step, x += at.step * o.sx, to += at.step * o.sc, power_to += at.step * o.sp) {
+    Eight<T> v[kFlight];
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) v[k].load(x + k * at.groups * o.sx, r + k * at.groups < o.rows ? at.left : 0, o.vec);
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
-      const long long i = i0 + k * step;
-      p[k] = place_of(o, min(i, a.units - 1));
-      if (i >= a.units) p[k].left = 0;
-      x[k].load((const T*)o.x + p[k].row * o.sx + p[k].col, p[k].left, o.vec);
-    }
-#pragma unroll
-    for (int k = 0; k < kFlight; ++k) {
-      unsigned top = x[k].top();
+      unsigned top = v[k].top();
       top = max(top, __shfl_xor_sync(~0u, top, 1));
       top = max(top, __shfl_xor_sync(~0u, top, 2));
       const bool finite = top < 0x7f800000u;
       const int power = finite ? max((int)(top >> 23) - 6, 1) : 255;
-      const uint2 w = finite ? codes_of(x[k], power, top) : make_uint2(0u, 0u);
-      signed char* to = o.codes + p[k].row * o.sc + p[k].col;
-      if (p[k].left == 8) {
-        *reinterpret_cast<uint2*>(to) = w;
+      const uint2 w = finite ? codes_of(v[k], power, top) : make_uint2(0u, 0u);
+      if (r + k * at.groups >= o.rows) continue;
+      signed char* row = to + k * at.groups * o.sc;
+      if (at.left == 8) {
+        *reinterpret_cast<uint2*>(row) = w;
       } else {
-        for (int e = 0; e < p[k].left; ++e) to[e] = (signed char)((e < 4 ? w.x : w.y) >> 8 * (e & 3));
+        for (int e = 0; e < at.left; ++e) row[e] = (signed char)((e < 4 ? w.x : w.y) >> 8 * (e & 3));
       }
-      if ((threadIdx.x & 3) == 0 && p[k].left > 0) o.powers[p[k].row * o.sp + p[k].col / 32] = (unsigned char)power;
+      if ((threadIdx.x & 3) == 0 && at.left > 0) power_to[k * at.groups * o.sp] = (unsigned char)power;
     }
   }
 }
@@ -141,53 +143,51 @@ __device__ __forceinline__ float value_of(unsigned codes, int byte) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) unpack8_kernel(const __grid_constant__ PackedArgs a) {
+__global__ void __launch_bounds__(256, 4) unpack8_kernel(const __grid_constant__ PackedArgs a) {
   pdl_wait();
-  const long long step = gridDim.x * 256LL;
-  for (long long i0 = blockIdx.x * 256LL + threadIdx.x; i0 < a.units; i0 += kFlight * step) {
-    Place p[kFlight];
+  const PackedArgs::One& o = a.m[blockIdx.z];
+  const Share at(o);
+  if (at.left <= 0) return;
+  T* x = (T*)o.x + at.row * o.sx + at.col;
+  const signed char* from = o.codes + at.row * o.sc + at.col;
+  const unsigned char* power_from = o.powers + at.row * o.sp + at.col / 32;
+  for (long long r = at.row; r < o.rows; r += at.step, x += at.step * o.sx, from += at.step * o.sc, power_from += at.step * o.sp) {
     uint2 w[kFlight];
     unsigned power[kFlight];
-    int which[kFlight];
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
-      const long long i = min(i0 + k * step, a.units - 1);
-      which[k] = (a.n > 1 && i >= a.m[1].first) + (a.n > 2 && i >= a.m[2].first);
-      const PackedArgs::One& o = a.m[which[k]];
-      p[k] = place_of(o, i - o.first);
-      if (i0 + k * step >= a.units) p[k].left = 0;
-      if (p[k].left <= 0) continue;
-      // a row of codes has room for whole units
-      w[k] = *reinterpret_cast<const uint2*>(o.codes + p[k].row * o.sc + p[k].col);
-      power[k] = o.powers[p[k].row * o.sp + p[k].col / 32];
+      if (r + k * at.groups >= o.rows) break;
+      w[k] = *reinterpret_cast<const uint2*>(from + k * at.groups * o.sc);    // a row of codes has room for whole units
+      power[k] = power_from[k * at.groups * o.sp];
     }
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
-      if (p[k].left <= 0) continue;
-      const PackedArgs::One& o = a.m[which[k]];
+      if (r + k * at.groups >= o.rows) break;
       const float scale = __uint_as_float(power[k] << 23);     // 255: infinite, and NaN times the codes' zeros
-      Eight<T> x;
+      Eight<T> v;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x.at(e) = from_f32<T>(value_of((e < 4 ? w[k].x : w[k].y) ^ 0x80808080u, e & 3) * scale);
-      x.store((T*)o.x + p[k].row * o.sx + p[k].col, p[k].left, o.vec);
+      for (int e = 0; e < 8; ++e) v.at(e) = from_f32<T>(value_of((e < 4 ? w[k].x : w[k].y) ^ 0x80808080u, e & 3) * scale);
+      v.store(x + k * at.groups * o.sx, at.left, o.vec);
     }
   }
 }
 
-void add(PackedArgs& a, const abcd_packed8* q, void* x, long long stride, int dtype) {
+PackedArgs::One one_of(const abcd_packed8* q, void* x, long long stride, int dtype) {
   const bool vec = (((uintptr_t)x | (q->rows > 1 ? (size_t)stride * elem_size(dtype) : 0)) & 15) == 0;
-  PackedArgs::One o{x, q->codes, q->powers, q->rows, q->cols, stride, q->stride, q->power_stride, a.units, 4 * ((q->cols + 31) / 32), vec};
-  if (q->cols % 32 == 0 && stride == q->cols && q->stride == q->cols && q->power_stride == q->cols / 32) {   // without gaps: one row
-    o.cols *= o.rows;
-    o.per_row *= o.rows;
-    o.rows = 1;
-  }
-  a.m[a.n++] = o;
-  a.units += o.rows * o.per_row;
+  return PackedArgs::One{x, q->codes, q->powers, q->rows, q->cols, stride, q->stride, q->power_stride,
+                         (int)std::min<long long>(256, 4 * ((q->cols + 31) / 32)), vec};
 }
 
-unsigned grid_of(const abcd_ctx* ctx, long long units) {
-  return (unsigned)std::min<long long>((units + 255) / 256, 8LL * ctx->num_sms);
+// A grid for matrices of up to these: slices of columns, CTAs of rows, matrices.
+dim3 grid_of(const abcd_ctx* ctx, const PackedArgs& a, int n) {
+  long long slices = 1, rows = 1;
+  for (int k = 0; k < n; ++k) {
+    const PackedArgs::One& o = a.m[k];
+    const long long per_cta = 256 / o.lanes * kFlight, s = (o.cols + 8 * o.lanes - 1) / (8 * o.lanes);
+    slices = std::max(slices, s);
+    rows = std::max(rows, std::min((o.rows + per_cta - 1) / per_cta, std::max(1LL, 12LL * ctx->num_sms / (s * n))));
+  }
+  return dim3((unsigned)slices, (unsigned)rows, (unsigned)n);
 }
 
 }  // namespace
@@ -195,11 +195,12 @@ unsigned grid_of(const abcd_ctx* ctx, long long units) {
 abcd_status unpack(abcd_ctx* ctx, const Unpacked* list, int n) {
   for (const int dtype : {ABCD_BF16, ABCD_F16, ABCD_F32}) {          // a launch for each type there is
     PackedArgs a{};
+    int count = 0;
     for (int k = 0; k < n; ++k)
-      if (list[k].dtype == dtype) add(a, list[k].from, list[k].to, list[k].stride, dtype);
-    if (a.units == 0) continue;
+      if (list[k].dtype == dtype) a.m[count++] = one_of(list[k].from, list[k].to, list[k].stride, dtype);
+    if (count == 0) continue;
     const abcd_status st = with_type(dtype, [&](auto t) {
-      return check_launch(ctx, "unpack8_kernel", launch_pdl(unpack8_kernel<decltype(t)>, dim3(grid_of(ctx, a.units)), dim3(256), 0, ctx->stream, a));
+      return check_launch(ctx, "unpack8_kernel", launch_pdl(unpack8_kernel<decltype(t)>, grid_of(ctx, a, count), dim3(256), 0, ctx->stream, a));
     });
     if (st != ABCD_OK) return st;
   }
@@ -217,9 +218,9 @@ extern "C" abcd_status abcd_pack8(abcd_ctx* ctx, const abcd_matrix* x, const abc
   if (x->rows == 0) return ABCD_OK;
   if (touches(packed, x)) return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_pack8: the packed matrix overlaps x");
   PackedArgs a{};
-  add(a, packed, x->data, x->stride, x->dtype);
+  a.m[0] = one_of(packed, x->data, x->stride, x->dtype);
   return with_type(x->dtype, [&](auto t) {
-    return check_launch(ctx, "pack8_kernel", launch_pdl(pack8_kernel<decltype(t)>, dim3(grid_of(ctx, a.units)), dim3(256), 0, ctx->stream, a));
+    return check_launch(ctx, "pack8_kernel", launch_pdl(pack8_kernel<decltype(t)>, grid_of(ctx, a, 1), dim3(256), 0, ctx->stream, a));
   });
 }
 

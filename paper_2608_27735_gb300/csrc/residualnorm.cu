@@ -194,58 +194,96 @@ __global__ void __launch_bounds__(kLongThreads) close_bwd_long_kernel(const __gr
   }
 }
 
-// How a row lies over threads: eight values each, as vectors of 16 bytes, TPR threads a row.  VEC: rows on
-// 16-byte boundaries, copied ahead to shared memory by the threads that use them; else element by
-// element, TPR apart.
-template <typename T, int TPR_, bool BWD, bool VEC_> struct CloseRow {
-  static constexpr int TPR = TPR_;
+// How a row lies over threads: E values each, TPR threads a row.  VEC: rows on 16-byte boundaries, E values as
+// vectors of 16 bytes, which the threads that use them copy ahead to shared memory.  Else the 16-byte pieces
+// that a row reaches into are copied ahead by its threads together, and a thread takes every TPR-th
+// element.  Forward, 16-bit rows take 16 values a thread, which halves what a row's sums cost per value;
+// backward (with eight vectors of sums and factors in registers) and in 32 bits eight.
+template <typename T, int TPR_, int E_, bool BWD, bool VEC_> struct CloseRow {
+  static constexpr int TPR = TPR_, E = E_;
   static constexpr bool VEC = VEC_;
-  static constexpr int V = VEC ? 16 / (int)sizeof(T) : 1, NV = 8 / V;
+  static constexpr int V = VEC ? 16 / (int)sizeof(T) : 1, NV = E / V;
   static constexpr int kThreads = TPR > 256 ? TPR : 256, kGroups = kThreads / TPR;
   static constexpr int kMats = BWD ? 4 : 2;
-  static constexpr int kDepth = VEC ? (BWD ? 3 : 4) : 0;   // rows of a thread that are there or on their way
-  static constexpr size_t kRing = (size_t)kDepth * kMats * (VEC ? NV : 0) * kThreads * 16;
-  static constexpr size_t kSums = BWD ? (size_t)4 * TPR * 8 * 4 : 0;
+  static constexpr int kDepth = BWD ? 3 : 4;               // rows that are there or on their way
+  static constexpr int kRowBytes = TPR * E * (int)sizeof(T) + (VEC ? 0 : 32);
+  static constexpr int kMatBytes = kGroups * kRowBytes, kSlotBytes = kMats * kMatBytes;
+  static constexpr size_t kRing = (size_t)kDepth * kSlotBytes;
+  static constexpr size_t kSums = BWD ? (size_t)4 * TPR * E * 4 : 0;
   static constexpr size_t kSmem = kRing > kSums ? kRing : kSums;
-  static constexpr int kCtas = kThreads > 256 ? 1 : BWD ? 2 : 3;
+  static constexpr int kCtas = kThreads > 256 ? 1 : BWD || E > 8 ? 2 : 3;
 };
 
 template <typename T, typename R> struct CloseRows {
-  char* slots;                        // the thread's first slot
-  const T* src[R::kMats];             // the thread's first value of the next row to fetch (VEC) or use
+  char* slots;                        // the thread's first vector (VEC) or its row's first piece, of the first slot
+  const T* src[R::kMats];             // where the next row to fetch starts (VEC: the thread's first vector of it)
+  const char* lowest[R::kMats];       // else also: the matrices' first bytes, and the ones behind their last
+  const char* highest[R::kMats];
   long long jump[R::kMats];
-  bool there[R::kMats];
-  int rows, turns, lane, cols;        // rows of the group; turns of the CTA
+  int bytes[R::NV];                   // VEC: of the thread's vectors
+  int rows, turns, lane, cols;        // rows of the group; turns that its threads take together
+  int now;                            // the slot of the row at hand
 
   __device__ __forceinline__ CloseRows(char* smem, const CloseArgs& a) {
     const int group = threadIdx.x / R::TPR;
     const long long first = (long long)blockIdx.x * R::kGroups + group, step = (long long)gridDim.x * R::kGroups;
     lane = threadIdx.x % R::TPR;
     cols = a.cols;
-    slots = smem + threadIdx.x * 16;
     rows = first < a.rows ? (int)((a.rows - first + step - 1) / step) : 0;
-    turns = (int)((a.rows - (long long)blockIdx.x * R::kGroups + step - 1) / step);
+    // groups of whole warps go on by themselves; rows that share a warp take their turns together
+    turns = R::TPR >= 32 ? rows : (int)((a.rows - (long long)blockIdx.x * R::kGroups + step - 1) / step);
+    slots = smem + (R::VEC ? threadIdx.x * 16 : group * R::kRowBytes);
+    now = 0;
     const T* const base[4] = {(const T*)a.f, (const T*)a.x, (const T*)a.dy, (const T*)a.dn};
     const long long stride[4] = {a.sf, a.sx, a.sdy, a.sdn};
 #pragma unroll
     for (int q = 0; q < R::kMats; ++q) {
-      there[q] = base[q] != nullptr;
-      src[q] = base[q] + first * stride[q] + lane * R::V;
+      src[q] = base[q] ? base[q] + first * stride[q] + (R::VEC ? lane * R::V : 0) : nullptr;
       jump[q] = step * stride[q];
+      if (!R::VEC && base[q]) {
+        lowest[q] = (const char*)base[q];
+        highest[q] = (const char*)(base[q] + (a.rows - 1) * stride[q] + a.cols);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < R::NV; ++j) bytes[j] = R::VEC ? min(16, (cols - column(j)) * (int)sizeof(T)) : 0;
+    // what is never copied reads as zero
+    if constexpr (R::VEC) {
+#pragma unroll
+      for (int q = 0; q < R::kMats; ++q)
+#pragma unroll
+        for (int j = 0; j < R::NV; ++j)
+          if (!src[q] || bytes[j] <= 0)
+            for (int d = 0; d < R::kDepth; ++d) *reinterpret_cast<uint4*>(vector(d, q, j)) = make_uint4(0u, 0u, 0u, 0u);
     }
   }
   __device__ __forceinline__ int column(int j) const { return (j * R::TPR + lane) * R::V; }
-  __device__ __forceinline__ char* slot(int t, int mat, int j) const {
-    return slots + ((t % R::kDepth * R::kMats + mat) * R::NV + j) * R::kThreads * 16;
+  __device__ __forceinline__ char* vector(int slot, int mat, int j) const {
+    return slots + slot * R::kSlotBytes + mat * R::kMatBytes + j * R::kThreads * 16;
   }
-  __device__ __forceinline__ void fetch(int t) {
+  __device__ __forceinline__ char* pieces(int slot, int mat) const { return slots + slot * R::kSlotBytes + mat * R::kMatBytes; }
+  __device__ __forceinline__ void fetch(int t, int slot) {
     if (t < rows) {
 #pragma unroll
       for (int q = 0; q < R::kMats; ++q) {
+        if (!src[q]) continue;
+        if constexpr (R::VEC) {
 #pragma unroll
-        for (int j = 0; j < R::NV; ++j) {
-          const int left = cols - column(j);
-          if (there[q] && left > 0) copy16(slot(t, q, j), src[q] + j * R::TPR * R::V, left < R::V ? left * (int)sizeof(T) : 16);
+          for (int j = 0; j < R::NV; ++j)
+            if (bytes[j] > 0) copy16(vector(slot, q, j), src[q] + j * R::TPR * R::V, bytes[j]);
+        } else {
+          const char* begin = (const char*)src[q];
+          const char* end = begin + cols * (int)sizeof(T);
+          const char* from = begin - ((uintptr_t)begin & 15) + 16 * lane;
+          for (char* to = pieces(slot, q) + 16 * lane; from < end; from += 16 * R::TPR, to += 16 * R::TPR) {
+            if (from >= lowest[q] && from + 16 <= highest[q]) {
+              copy16(to, from, 16);
+            } else {                  // a piece that reaches out of the matrix
+#pragma unroll 1
+              for (int e = 0; e < 16; e += (int)sizeof(T))
+                if (from + e >= begin && from + e < end) *reinterpret_cast<T*>(to + e) = *reinterpret_cast<const T*>(from + e);
+            }
+          }
         }
         src[q] += jump[q];
       }
@@ -253,86 +291,98 @@ template <typename T, typename R> struct CloseRows {
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
   __device__ __forceinline__ void start() {
-    if constexpr (R::VEC) {
 #pragma unroll
-      for (int d = 0; d < R::kDepth - 1; ++d) fetch(d);
-    }
+    for (int d = 0; d < R::kDepth - 1; ++d) fetch(d, d);
   }
   // Asks for a row to come and waits for turn t's.
   __device__ __forceinline__ void turn(int t) {
+    if constexpr (!R::VEC) row_sync<R::TPR>();             // the last turn's row is done with
+    fetch(t + R::kDepth - 1, now == 0 ? R::kDepth - 1 : now - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
+    if constexpr (!R::VEC) row_sync<R::TPR>();
+  }
+  __device__ __forceinline__ void next() { now = now == R::kDepth - 1 ? 0 : now + 1; }
+  // The thread's values of the row at hand of a matrix (`at`: where the row starts): zeros past its end, of no
+  // row and of a matrix that is not there.
+  __device__ __forceinline__ void get(float (&v)[R::E], int t, int mat, const T* at) const {
     if constexpr (R::VEC) {
-      fetch(t + R::kDepth - 1);
-      asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
-    }
-  }
-  // Vector j of the turn's row of a matrix: zeros past its end, of no row and of a matrix that is not there.
-  __device__ __forceinline__ void get(float (&v)[8], int t, int mat) const {
 #pragma unroll
-    for (int j = 0; j < R::NV; ++j) {
-      const bool in = there[mat] && t < rows && column(j) < cols;
-      if constexpr (R::VEC) {
-        float w[R::V];
-        load_vec<T, R::V>(w, (const T*)slot(t, mat, j), in ? R::V : 0);
+      for (int j = 0; j < R::NV; ++j) {
+        const Pack<T, R::V> w = *reinterpret_cast<const Pack<T, R::V>*>(vector(now, mat, j));
 #pragma unroll
-        for (int i = 0; i < R::V; ++i) v[j * R::V + i] = w[i];
-      } else {
-        v[j] = in ? to_f32(src[mat][j * R::TPR]) : 0.f;
+        for (int i = 0; i < R::V; ++i) v[j * R::V + i] = R::TPR >= 32 || t < rows ? to_f32(w.v[i]) : 0.f;
       }
-    }
-  }
-  // The next row (rows that are not copied ahead).
-  __device__ __forceinline__ void next() {
-    if constexpr (!R::VEC) {
+    } else {
+      const T* p = (const T*)(pieces(now, mat) + ((uintptr_t)at & 15)) + lane;
 #pragma unroll
-      for (int q = 0; q < R::kMats; ++q) src[q] += jump[q];
+      for (int e = 0; e < R::E; ++e) v[e] = at && column(e) < cols ? to_f32(p[e * R::TPR]) : 0.f;
     }
   }
-  __device__ __forceinline__ void put(T* to, const float (&v)[8], int t) const {
-    if (t >= rows) return;
+  __device__ __forceinline__ void put(T* to, const float (&v)[R::E], int t) const {
+    if (R::TPR < 32 && t >= rows) return;
 #pragma unroll
     for (int j = 0; j < R::NV; ++j) {
       float w[R::V];
 #pragma unroll
       for (int i = 0; i < R::V; ++i) w[i] = v[j * R::V + i];
-      store_vec<T, R::V>(to + column(j), w, cols - column(j));
+      if constexpr (R::VEC) {
+        if (bytes[j] > 0) store_vec<T, R::V>(to + column(j), w, bytes[j] / (int)sizeof(T));
+      } else {
+        if (column(j) < cols) to[column(j)] = from_f32<T>(w[0]);
+      }
     }
   }
-  __device__ __forceinline__ void weights(float (&v)[8], const void* w, int wide, float none) const {
+  // A vector's values of the thread's columns; zero past their end.
+  __device__ __forceinline__ void weights(float (&v)[R::E], const void* w, int wide, float none) const {
 #pragma unroll
     for (int j = 0; j < R::NV; ++j) {
       float u[R::V];
-      load_weight<T, R::V>(u, w, wide, column(j), cols - column(j), none);
+      const int left = cols - column(j);
+      load_weight<T, R::V>(u, w, wide, column(j), left, none);
 #pragma unroll
-      for (int i = 0; i < R::V; ++i) v[j * R::V + i] = u[i];
+      for (int i = 0; i < R::V; ++i) v[j * R::V + i] = i < left ? u[i] : 0.f;
     }
   }
-  // Whether value e of the thread is one of the row's.
-  __device__ __forceinline__ bool inside(int e) const { return column(e / R::V) + e % R::V < cols; }
 };
 
-// A row's statistics from the threads' values; what lies past its end has no part in them.
+// The sum of a over the threads of a row, in each of them; as row_sum2.
+template <int TPR> __device__ __forceinline__ void row_sum(float& a, float2 (*red)[32], int turn) {
+  if constexpr (TPR > 32) {
+    float unused = 0.f;
+    row_sum2<TPR>(a, unused, red, turn);
+  } else {
+#pragma unroll
+    for (int o = TPR / 2; o; o >>= 1) a += __shfl_xor_sync(~0u, a, o);
+  }
+}
+
+// A row's statistics from the threads' values (which are zero past its end).
 template <typename T, typename R>
-__device__ __forceinline__ Stat stat_of_row(const CloseRows<T, R>& rows, const float (&v)[8], int kind, float eps, float inv, float2 (*red)[32], int& turn) {
+__device__ __forceinline__ Stat stat_of_row(const CloseRows<T, R>& rows, const float (&v)[R::E], int kind, float eps, float inv, float2 (*red)[32], int& turn) {
   float s = 0.f, q = 0.f;
   if (kind == ABCD_RMS_NORM) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q += v[e] * v[e];              // zero past the end
-    row_sum2<R::TPR>(q, s, red, turn);
+    for (int e = 0; e < R::E; ++e) q += v[e] * v[e];
+    row_sum<R::TPR>(q, red, turn);
     turn ^= 1;
     return Stat{0.f, rsqrtf(q * inv + eps)};
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s += v[e];
-  row_sum2<R::TPR>(s, q, red, turn);
+  for (int e = 0; e < R::E; ++e) s += v[e];
+  row_sum<R::TPR>(s, red, turn);
   // the division's rounding taken back, then what the sum has rounded
   float mean = s * inv, off = 0.f;
   mean = __fmaf_rn(__fmaf_rn(-mean, (float)rows.cols, s), inv, mean);
-  q = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float d = rows.inside(e) ? v[e] - mean : 0.f;
-    q += d * d;
-    off += d;
+  for (int j = 0; j < R::NV; ++j) {
+    const int left = rows.cols - rows.column(j);           // past the row's end nothing deviates
+#pragma unroll
+    for (int i = 0; i < R::V; ++i) {
+      float d = v[j * R::V + i] - mean;
+      if (left < R::V) d = i < left ? d : 0.f;
+      q += d * d;
+      off += d;
+    }
   }
   row_sum2<R::TPR>(q, off, red, turn ^ 1);
   off *= inv;
@@ -341,13 +391,13 @@ __device__ __forceinline__ Stat stat_of_row(const CloseRows<T, R>& rows, const f
 
 // A and C of the thread's columns.
 template <typename T, typename R>
-__device__ __forceinline__ void factors(const CloseRows<T, R>& rows, const CloseArgs& a, float (&A)[8], float (&C)[8]) {
-  float g[8];
+__device__ __forceinline__ void factors(const CloseRows<T, R>& rows, const CloseArgs& a, float (&A)[R::E], float (&C)[R::E]) {
+  float g[R::E];
   rows.weights(g, a.gate, a.wide_w, 1.f);
   rows.weights(A, a.w[0], a.wide_w, 1.f);
   rows.weights(C, a.b[0], a.wide_w, 0.f);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < R::E; ++e) {
     A[e] *= a.scale * g[e];
     C[e] *= a.scale * g[e];
   }
@@ -360,7 +410,7 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_fwd_kernel(const 
   pdl_wait();
   CloseRows<T, R> rows(smem, a);
   rows.start();
-  float A[8], C[8], W[8], B[8];
+  float A[R::E], C[R::E], W[R::E], B[R::E];
   factors(rows, a, A, C);
   rows.weights(W, a.w[1], a.wide_w, 1.f);
   rows.weights(B, a.b[1], a.wide_w, 0.f);
@@ -369,25 +419,27 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_fwd_kernel(const 
   long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / R::TPR;
   T* y = (T*)a.y + r * a.sy;
   T* n = (T*)a.n + r * a.sn;
+  const T* atf = (const T*)a.f + r * a.sf;               // (used where rows start anywhere)
+  const T* atx = (const T*)a.x + r * a.sx;
   int half = 0;
-  for (int t = 0; t < rows.turns; ++t, r += step, y += step * a.sy, n += step * a.sn) {
+  for (int t = 0; t < rows.turns; ++t, r += step, y += step * a.sy, n += step * a.sn, atf += step * a.sf, atx += step * a.sx) {
     rows.turn(t);
-    float f[8], x[8];
-    rows.get(f, t, 0);
-    rows.get(x, t, 1);
+    float f[R::E], x[R::E];
+    rows.get(f, t, 0, atf);
+    rows.get(x, t, 1, atx);
     Stat first{0.f, 1.f}, second{0.f, 1.f};
     if (a.kind[0] != kNone) first = stat_of_row(rows, f, a.kind[0], a.eps[0], inv, red, half);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = rows.inside(e) ? close_value(x[e], (f[e] - first.mean) * first.rstd, A[e], C[e]) : 0.f;
+    for (int e = 0; e < R::E; ++e) x[e] = close_value(x[e], (f[e] - first.mean) * first.rstd, A[e], C[e]);
     if (a.kind[1] != kNone) {
       second = stat_of_row(rows, x, a.kind[1], a.eps[1], inv, red, half);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = (x[e] - second.mean) * second.rstd * W[e] + B[e];
+      for (int e = 0; e < R::E; ++e) f[e] = (x[e] - second.mean) * second.rstd * W[e] + B[e];
       rows.put(n, f, t);
     }
     rows.put(y, x, t);
     rows.next();
-    if (t < rows.rows && rows.lane == 0) {
+    if ((R::TPR >= 32 || t < rows.rows) && rows.lane == 0) {
       const Stat s[2] = {first, second};
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -405,7 +457,7 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
   pdl_wait();
   CloseRows<T, R> rows(smem, a);
   rows.start();
-  float A[8], C[8], W[8], sums[4][8] = {};
+  float A[R::E], C[R::E], W[R::E], sums[4][R::E] = {};
   factors(rows, a, A, C);
   rows.weights(W, a.w[1], a.wide_w, 1.f);
   const float inv = 1.f / (float)a.cols;
@@ -414,6 +466,8 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
   long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / R::TPR;
   T* dx = (T*)a.y + r * a.sy;
   T* df = (T*)a.n + r * a.sn;
+  // (used where rows start anywhere)
+  const T* at[4] = {(const T*)a.f + r * a.sf, (const T*)a.x + r * a.sx, a.dy ? (const T*)a.dy + r * a.sdy : nullptr, a.dn ? (const T*)a.dn + r * a.sdn : nullptr};
   Stat next[2] = {{0.f, 0.f}, {0.f, 0.f}};
   if (rows.rows > 0) {
     next[0] = stat_of(a, 0, r);
@@ -426,15 +480,15 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
       next[0] = stat_of(a, 0, r + step);
       next[1] = stat_of(a, 1, r + step);
     }
-    float fh[8], yh[8], g[8], s1 = 0.f, s2 = 0.f;
-    rows.get(fh, t, 0);
-    rows.get(yh, t, 1);
-    rows.get(g, t, 2);
+    float fh[R::E], yh[R::E], g[R::E], s1 = 0.f, s2 = 0.f;
+    rows.get(fh, t, 0, at[0]);
+    rows.get(yh, t, 1, at[1]);
+    rows.get(g, t, 2, at[2]);
     if (a.dn) {
-      float dn[8];
-      rows.get(dn, t, 3);
+      float dn[R::E];
+      rows.get(dn, t, 3, at[3]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < R::E; ++e) {
         fh[e] = (fh[e] - first.mean) * first.rstd;
         yh[e] = (close_value(yh[e], fh[e], A[e], C[e]) - second.mean) * second.rstd;   // the forward pass's, bit for bit
         sums[2][e] += dn[e];
@@ -447,16 +501,16 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
       s1 *= centre[1];
       s2 *= inv;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] = rows.inside(e) ? g[e] + second.rstd * (dn[e] - s1 - yh[e] * s2) : 0.f;
+      for (int e = 0; e < R::E; ++e) g[e] += second.rstd * (dn[e] - s1 - yh[e] * s2);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) fh[e] = (fh[e] - first.mean) * first.rstd;
+      for (int e = 0; e < R::E; ++e) fh[e] = (fh[e] - first.mean) * first.rstd;
     }
-    const bool in = t < rows.rows;
+    const bool in = R::TPR >= 32 || t < rows.rows;
     if (a.y) rows.put(dx, g, t);
     s1 = s2 = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < R::E; ++e) {
       if (!in) g[e] = 0.f;
       sums[0][e] += g[e];
       sums[1][e] += g[e] * fh[e];
@@ -470,7 +524,7 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
         s1 *= centre[0];
         s2 *= inv;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = first.rstd * (g[e] - s1 - fh[e] * s2);
+        for (int e = 0; e < R::E; ++e) g[e] = first.rstd * (g[e] - s1 - fh[e] * s2);
       }
       rows.put(df, g, t);
     }
@@ -478,17 +532,23 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
     // threads meet here
     if (R::TPR > 32 && (!a.dn || !a.n || a.kind[0] == kNone)) row_sync<R::TPR>();
     rows.next();
+    if constexpr (!R::VEC) {
+      at[0] += step * a.sf;
+      at[1] += step * a.sx;
+      if (at[2]) at[2] += step * a.sdy;
+      if (at[3]) at[3] += step * a.sdn;
+    }
   }
   // the CTA's sums: rows that share a warp by shuffles, then the warps of a column one after another
-  if constexpr (R::VEC) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
   float* total = (float*)smem;
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < R::E; ++e)
 #pragma unroll
       for (int o = 16; o >= R::TPR; o >>= 1) sums[k][e] += __shfl_xor_sync(~0u, sums[k][e], o);
-  constexpr int ROUNDS = R::TPR > 32 ? R::kGroups : R::kThreads / 32, CAPACITY = R::TPR * 8;
+  constexpr int ROUNDS = R::TPR > 32 ? R::kGroups : R::kThreads / 32, CAPACITY = R::TPR * R::E;
   const int mine = R::TPR > 32 ? threadIdx.x / R::TPR : threadIdx.x / 32;
   const bool one = R::TPR >= 32 || (threadIdx.x & 31) < R::TPR;
   for (int q = 0; q < ROUNDS; ++q) {
@@ -497,7 +557,7 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < R::E; ++e) {
         float* to = total + k * CAPACITY + rows.column(e / R::V) + e % R::V;
         *to = (q ? *to : 0.f) + sums[k][e];
       }
@@ -558,17 +618,18 @@ constexpr int kCloseCtasPerSm = 2;    // backward, with sums in the workspace
 // Calls f with the row shape for `cols` columns of T; f of an int where registers do not hold a row.
 template <typename T, bool BWD, typename F> abcd_status with_row(long long cols, bool aligned, F&& f) {
   if (aligned) {
-    if (cols <= 64) return f(CloseRow<T, 8, BWD, true>());
-    if (cols <= 128) return f(CloseRow<T, 16, BWD, true>());
-    if (cols <= 256) return f(CloseRow<T, 32, BWD, true>());
-    if (cols <= 512) return f(CloseRow<T, 64, BWD, true>());
-    if (cols <= 1024) return f(CloseRow<T, 128, BWD, true>());
-    if (cols <= 2048) return f(CloseRow<T, 256, BWD, true>());
-    if (cols <= 4096) return f(CloseRow<T, 512, BWD, true>());
+    constexpr int N = !BWD && sizeof(T) == 2 ? 2 : 1, E = 8 * N;
+    if (cols <= 64) return f(CloseRow<T, 8 / N, E, BWD, true>());
+    if (cols <= 128) return f(CloseRow<T, 16 / N, E, BWD, true>());
+    if (cols <= 256) return f(CloseRow<T, 32 / N, E, BWD, true>());
+    if (cols <= 512) return f(CloseRow<T, 64 / N, E, BWD, true>());
+    if (cols <= 1024) return f(CloseRow<T, 128 / N, E, BWD, true>());
+    if (cols <= 2048) return f(CloseRow<T, 256 / N, E, BWD, true>());
+    if (cols <= 4096) return f(CloseRow<T, 512 / N, E, BWD, true>());
   } else {
-    if (cols <= 256) return f(CloseRow<T, 32, BWD, false>());
-    if (cols <= 1024) return f(CloseRow<T, 128, BWD, false>());
-    if (cols <= 4096) return f(CloseRow<T, 512, BWD, false>());
+    if (cols <= 256) return f(CloseRow<T, 32, 8, BWD, false>());
+    if (cols <= 1024) return f(CloseRow<T, 128, 8, BWD, false>());
+    if (cols <= 4096) return f(CloseRow<T, 512, 8, BWD, false>());
   }
   return f(0);
 }
