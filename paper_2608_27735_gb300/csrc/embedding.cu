@@ -37,7 +37,7 @@ struct LookupArgs {
 
 // V consecutive columns a thread (16 bytes, or one where rows start anywhere), `lanes` threads a token,
 // kFlight tokens of a thread on their way at once: first their indices, then the rows that they name.
-constexpr int kFlight = 4;
+constexpr int kFlight = 4, kEmbedWaves = 4;
 template <typename T, int V>
 __global__ void __launch_bounds__(256, V > 4 ? 3 : 4) embed_kernel(const __grid_constant__ LookupArgs a) {
   pdl_wait();
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
 
 // ---- the sums
 
-constexpr int kChunk = 256;           // sorted tokens of a CTA
+constexpr int kChunk = 256;           // sorted tokens of a CTA at most
 
 struct SumArgs {
   const void* dy;
@@ -292,6 +292,7 @@ struct SumArgs {
   float scale;
   int lanes;                          // threads of a token's row, up to 256, V columns each
   int slices;                         // of lanes x V columns
+  int chunk;                          // sorted tokens of a CTA
   long long chunks;
 };
 
@@ -320,10 +321,10 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const __grid_constant__ 
   pdl_wait();
   __shared__ unsigned key[kChunk + 2], id[kChunk];
   __shared__ float head[256 * V], tail[256 * V];
-  const long long chunk = blockIdx.x / a.slices, first = chunk * kChunk;
-  const int n = (int)min((long long)kChunk, a.n - first);
-  const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = 256 / a.lanes, stretch = (kChunk + groups - 1) / groups;
-  for (int i = threadIdx.x; i < kChunk + 1; i += 256) {
+  const long long chunk = blockIdx.x / a.slices, first = chunk * a.chunk;
+  const int n = (int)min((long long)a.chunk, a.n - first);
+  const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = 256 / a.lanes, stretch = (a.chunk + groups - 1) / groups;
+  for (int i = threadIdx.x; i < a.chunk + 1; i += 256) {
     key[i + 1] = i < n || first + i < a.n ? a.key[first + i] : a.table_rows + 1;
     if (i < n) id[i] = a.id[first + i];
   }
@@ -407,30 +408,40 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const __grid_constant__ 
   }
 }
 
-// Runs that pass a chunk's end, by the chunk that they begin in.  A group of threads has a chunk; a run over
-// few chunks it adds up by itself, for longer ones all groups of the CTA take consecutive parts side by
-// side, whose sums are then added in their order.
-constexpr int kJoinThreads = 256, kJoinAlone = 8;
+// Runs that pass a chunk's end, by the chunk that they begin in.  A group of up to sixteen threads, four columns
+// each, has a chunk; a run over few chunks it adds up by itself, for longer ones all groups of the CTA take
+// consecutive parts side by side, whose sums are then added in their order.
+constexpr int kJoinThreads = 1024, kJoinLanes = 16, kJoinAlone = 8;
 template <typename T, int V>
 __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_constant__ SumArgs a) {
   pdl_wait();
-  __shared__ float run[kJoinThreads * V];
+  __shared__ float4 run[kJoinThreads];
   __shared__ long long last_of[kJoinThreads];
   const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = kJoinThreads / a.lanes;
   const long long base = blockIdx.x / a.slices * (long long)groups;
-  const unsigned c = ((unsigned)(blockIdx.x % a.slices) * a.lanes + lane) * V;
+  const unsigned c = (blockIdx.x % a.slices * a.lanes + lane) * 4;
   const bool in = c < a.cols && group < groups;
-  const auto has = [&](long long q, unsigned row) { return q < a.chunks && a.key[q * kChunk] == row; };
-  auto add_part = [&](float (&s)[V], long long q, int which) {
-    const float* p = a.part + (2 * q + which) * a.ld + c;
+  const auto has = [&](long long q, unsigned row) { return q < a.chunks && a.key[q * a.chunk] == row; };
+  const auto part = [&](long long q, int which) { return __ldcg(reinterpret_cast<const float4*>(a.part + (2 * q + which) * a.ld + c)); };
+  const auto sum = [](float4& s, const float4& v) { s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w); };
+  const auto put = [&](unsigned row, const float4& s) {
+    if constexpr (V == 1) {
+      const float v[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
-    for (int e = 0; e < V; ++e) s[e] += c + e < a.cols ? __ldcg(p + e) : 0.f;
+      for (int e = 0; e < 4; ++e) {
+        const float one[1] = {v[e]};
+        if (c + e < a.cols) put_row<T, 1>(a, row, c + e, one);
+      }
+    } else {
+      const float v[4] = {s.x, s.y, s.z, s.w};
+      put_row<T, 4>(a, row, c, v);
+    }
   };
   long long last = -1;                                  // of a run that is too long for the group
   if (group < groups) {
-    const long long chunk = base + group, end = (chunk + 1) * kChunk;
+    const long long chunk = base + group, end = (chunk + 1) * a.chunk;
     if (end < a.n) {
-      const unsigned row = a.key[end - 1], then = a.key[end], first = a.key[end - kChunk], before = chunk > 0 ? a.key[end - kChunk - 1] : a.table_rows;
+      const unsigned row = a.key[end - 1], then = a.key[end], first = a.key[end - a.chunk], before = chunk > 0 ? a.key[end - a.chunk - 1] : a.table_rows;
       if (row < a.table_rows && then == row && !(first == row && before == row)) {
         // the last chunk that begins with the row: steps that double, then halve
         last = chunk + 1;
@@ -443,10 +454,9 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_c
           if (has(last + step, row)) last += step;
         if (last - chunk <= kJoinAlone) {
           if (in) {
-            float s[V] = {};
-            add_part(s, chunk, 1);
-            for (long long q = chunk + 1; q <= last; ++q) add_part(s, q, 0);
-            put_row<T, V>(a, row, c, s);
+            float4 s = part(chunk, 1);
+            for (long long q = chunk + 1; q <= last; ++q) sum(s, part(q, 0));
+            put(row, s);
           }
           last = -1;
         }
@@ -458,25 +468,19 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_c
   for (int g = 0; g < groups; ++g) {
     if (last_of[g] < 0) continue;
     const long long chunk = base + g, count = last_of[g] - chunk;
-    float s[V] = {};
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (in) {
       const long long q1 = chunk + 1 + count * (group + 1) / groups;
-#pragma unroll 4
-      for (long long q = chunk + 1 + count * group / groups; q < q1; ++q) add_part(s, q, 0);
+#pragma unroll 8
+      for (long long q = chunk + 1 + count * group / groups; q < q1; ++q) sum(s, part(q, 0));
     }
     __syncthreads();
-#pragma unroll
-    for (int e = 0; e < V; ++e) run[threadIdx.x * V + e] = s[e];
+    run[threadIdx.x] = s;
     __syncthreads();
     if (group > 0 || !in) continue;
-#pragma unroll
-    for (int e = 0; e < V; ++e) s[e] = 0.f;
-    add_part(s, chunk, 1);
-    for (int h = 0; h < groups; ++h) {
-#pragma unroll
-      for (int e = 0; e < V; ++e) s[e] += run[(h * a.lanes + lane) * V + e];
-    }
-    put_row<T, V>(a, a.key[(chunk + 1) * kChunk], c, s);
+    s = part(chunk, 1);
+    for (int h = 0; h < groups; ++h) sum(s, run[h * a.lanes + lane]);
+    put(a.key[(chunk + 1) * a.chunk], s);
   }
 }
 
@@ -500,6 +504,30 @@ SortPlan sort_plan(long long tokens, long long table_rows) {
   return p;
 }
 
+// How a chunk's threads lie over its tokens' columns: V of them each (16 bytes, or one where rows start
+// anywhere), and the tokens of a chunk.  A group of threads walks 32 tokens, fewer where the chunks would not
+// fill the SMs (of 4 tokens a group at least), and 64 at least go to a CTA of one or two groups, so that
+// the parts that the chunks leave stay few.  (100,000 x 1,024 bf16: 220 us with 256 tokens a CTA.)
+struct Chunks { int lanes, slices, tokens; };
+Chunks chunks_of(long long tokens, long long cols, int v) {
+  Chunks c;
+  c.lanes = (int)std::min<long long>(256, (cols + v - 1) / v);
+  c.slices = (int)((cols + (long long)c.lanes * v - 1) / ((long long)c.lanes * v));
+  const int groups = 256 / c.lanes;
+  const long long fill = (tokens * c.slices + 2 * kNetSms * groups - 1) / (2LL * kNetSms * groups);
+  const int stretch = (int)std::clamp<long long>(fill, 4, 32);
+  c.tokens = std::min(kChunk, std::max(stretch * groups, stretch == 32 ? 64 : 1));
+  return c;
+}
+
+// Chunks that up to `tokens` tokens of up to `cols` columns come in at most: of the tokens that a chunk has
+// at least where they fill the SMs, or as many as fill them.
+long long most_chunks(long long tokens, long long cols) {
+  const int groups = 256 / (int)std::min<long long>(256, cols);
+  const long long least = std::min(kChunk, std::max(32 * groups, 64));
+  return std::min(tokens, std::max((tokens + least - 1) / least, 2LL * kNetSms + 2));
+}
+
 size_t part_ld(long long cols) { return (size_t)(cols + 3) / 4 * 4; }
 
 // The workspace behind its header.
@@ -508,8 +536,7 @@ struct EmbedScratch {
   float* part;
   size_t bytes;
 };
-EmbedScratch scratch_of(char* base, long long tokens, long long table_rows, long long cols) {
-  const SortPlan p = sort_plan(tokens, table_rows);
+EmbedScratch scratch_of(char* base, long long tokens, long long cols) {
   size_t at = kNetHeader;
   const auto take = [&](size_t bytes) { char* q = base ? base + at : nullptr; at += net_align(bytes); return q; };
   EmbedScratch s;
@@ -517,9 +544,11 @@ EmbedScratch scratch_of(char* base, long long tokens, long long table_rows, long
     s.key[k] = (unsigned*)take(4 * (size_t)tokens);
     s.id[k] = (unsigned*)take(4 * (size_t)tokens);
   }
-  s.count = (unsigned*)take((size_t)4 * kMaxDigits * (size_t)p.tiles);
+  // (tiles of up to as many tokens)
+  const long long tiles = std::max(std::min<long long>((tokens + 4095) / 4096, kNetSms), (tokens + kOneTile - 1) / kOneTile);
+  s.count = (unsigned*)take((size_t)4 * kMaxDigits * (size_t)tiles);
   s.total = (unsigned*)take((size_t)4 * kMaxDigits);
-  s.part = (float*)take((size_t)8 * part_ld(cols) * (size_t)((tokens + kChunk - 1) / kChunk));
+  s.part = (float*)take((size_t)8 * part_ld(cols) * (size_t)most_chunks(tokens, cols));
   s.bytes = at;
   return s;
 }
@@ -542,7 +571,7 @@ using namespace abcd;
 extern "C" abcd_status abcd_embedding_workspace_size(long long tokens, long long table_rows, long long cols, size_t* bytes) {
   if (!bytes || tokens < 0 || tokens > kMaxNetRows || table_rows < 1 || table_rows > kMaxNetRows || cols < 1 || cols > kMaxNetCols)
     return ABCD_ERR_INVALID_ARG;
-  *bytes = scratch_of(nullptr, tokens, table_rows, cols).bytes;
+  *bytes = scratch_of(nullptr, tokens, cols).bytes;
   return ABCD_OK;
 }
 
@@ -569,7 +598,7 @@ extern "C" abcd_status abcd_embedding(abcd_ctx* ctx, const abcd_matrix* table, c
     const long long vectors = vec ? (y->cols + V - 1) / V : y->cols;
     a.lanes = (unsigned)std::min(256LL, vectors);
     const long long slices = (vectors + a.lanes - 1) / a.lanes, per_cta = 256 / a.lanes * kFlight;
-    const long long grid = std::min((y->rows + per_cta - 1) / per_cta, std::max(1LL, 12LL * ctx->num_sms / slices));
+    const long long grid = std::min((y->rows + per_cta - 1) / per_cta, std::max(1LL, (long long)kEmbedWaves * ctx->num_sms / slices));
     return check_launch(ctx, "embed_kernel", launch_pdl(vec ? embed_kernel<T, V> : embed_kernel<T, 1>, dim3((unsigned)slices, (unsigned)grid), dim3(256), 0, ctx->stream, a));
   });
 }
@@ -585,7 +614,7 @@ extern "C" abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix*
   if (overlap(dy, dtable) || on_index(dtable, index, index_dtype, dy->rows))
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: dtable overlaps an operand", what);
   const long long n = dy->rows;
-  const EmbedScratch s = scratch_of(ctx->net_base, n, dtable->rows, dy->cols);
+  const EmbedScratch s = scratch_of(ctx->net_base, n, dy->cols);
   if (!ctx->net_base || s.bytes > ctx->net_bytes)
     return fail(ctx, ABCD_ERR_WORKSPACE, "%s: the network workspace has %zu bytes, needs %zu", what, ctx->net_bytes, s.bytes);
   const SortPlan p = sort_plan(n, dtable->rows);
@@ -618,21 +647,21 @@ extern "C" abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix*
     q.to_key = s.key[(pass + 1) & 1];
     q.to_id = s.id[(pass + 1) & 1];
   }
-  SumArgs a{dy->data, q.key, q.id, dtable->data, s.part, n, dy->stride, dtable->stride, (unsigned)dtable->rows,
-            (unsigned)dy->cols, (unsigned)part_ld(dy->cols), scale, 1, 1, (n + kChunk - 1) / kChunk};
   const bool vec = rows_aligned(dy, 16) && rows_aligned(dtable, 16);
+  const Chunks c = chunks_of(n, dy->cols, vec ? 16 / (int)e : 1);
+  SumArgs a{dy->data, q.key, q.id, dtable->data, s.part, n, dy->stride, dtable->stride, (unsigned)dtable->rows,
+            (unsigned)dy->cols, (unsigned)part_ld(dy->cols), scale, c.lanes, c.slices, c.tokens, (n + c.tokens - 1) / c.tokens};
   return with_type(dy->dtype, [&](auto t) {
     using T = decltype(t);
     const auto sum = [&](auto width) {
       constexpr int V = decltype(width)::value;
-      a.lanes = (int)std::min<long long>(256, (a.cols + V - 1) / V);
-      a.slices = (int)((a.cols + a.lanes * V - 1) / (a.lanes * V));
-      const dim3 grid((unsigned)(a.chunks * a.slices));
-      const abcd_status st = check_launch(ctx, "embed_sum_kernel", launch_pdl(embed_sum_kernel<T, V>, grid, dim3(256), 0, ctx->stream, a));
+      const abcd_status st = check_launch(ctx, "embed_sum_kernel", launch_pdl(embed_sum_kernel<T, V>, dim3((unsigned)(a.chunks * a.slices)), dim3(256), 0, ctx->stream, a));
       if (st != ABCD_OK || a.chunks == 1) return st;
+      a.lanes = (int)std::min<unsigned>(kJoinLanes, a.ld / 4);
       const long long groups = kJoinThreads / a.lanes;
-      return check_launch(ctx, "embed_join_kernel", launch_pdl(embed_join_kernel<T, V>, dim3((unsigned)((a.chunks + groups - 1) / groups * a.slices)),
-                                                              dim3(kJoinThreads), 0, ctx->stream, a));
+      a.slices = (int)((a.ld / 4 + a.lanes - 1) / a.lanes);
+      const dim3 grid((unsigned)((a.chunks + groups - 1) / groups * a.slices));
+      return check_launch(ctx, "embed_join_kernel", launch_pdl(embed_join_kernel<T, V>, grid, dim3(kJoinThreads), 0, ctx->stream, a));
     };
     return vec ? sum(std::integral_constant<int, 16 / sizeof(T)>()) : sum(std::integral_constant<int, 1>());
   });

@@ -172,6 +172,69 @@ __global__ void __launch_bounds__(256, 4) unpack8_kernel(const __grid_constant__
   }
 }
 
+// Rows that start anywhere: a warp takes 256 columns of a row, a lane one of each group of 32, so that
+// consecutive lanes read and write consecutive elements.
+constexpr int kSpan = 8;              // groups of a warp
+template <typename T>
+__global__ void __launch_bounds__(256) pack8_any_kernel(const __grid_constant__ PackedArgs a) {
+  pdl_wait();
+  const PackedArgs::One& o = a.m[0];
+  const int lane = threadIdx.x & 31;
+  const long long col = blockIdx.x * 32LL * kSpan;
+  const int left = (int)min(32LL * kSpan, o.cols - col);
+  for (long long r = blockIdx.y * 8LL + threadIdx.x / 32; r < o.rows; r += gridDim.y * 8LL) {
+    const T* x = (const T*)o.x + r * o.sx + col + lane;
+    T v[kSpan];
+#pragma unroll
+    for (int g = 0; g < kSpan; ++g)
+      if (32 * g < left) v[g] = 32 * g + lane < left ? x[32 * g] : T(0.f);
+    signed char* to = o.codes + r * o.sc + col + lane;
+    unsigned powers = 0;
+#pragma unroll
+    for (int g = 0; g < kSpan; ++g) {
+      if (32 * g >= left) break;
+      const float f = to_f32(v[g]);
+      const unsigned top = __reduce_max_sync(~0u, __float_as_uint(f) & 0x7fffffffu);
+      const bool finite = top < 0x7f800000u;
+      const int power = finite ? max((int)(top >> 23) - 6, 1) : 255;
+      const float inverse = __uint_as_float((unsigned)(254 - power) << 23);
+      const int code = finite ? __float2int_rn(fminf(fmaxf(f * inverse, -127.f), 127.f)) : 0;
+      if (32 * g + lane < left) to[32 * g] = (signed char)code;
+      if (lane == g) powers = (unsigned)power;
+    }
+    if (32 * lane < left && lane < kSpan) o.powers[r * o.sp + col / 32 + lane] = (unsigned char)powers;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) unpack8_any_kernel(const __grid_constant__ PackedArgs a) {
+  pdl_wait();
+  const PackedArgs::One& o = a.m[0];
+  const int lane = threadIdx.x & 31;
+  const long long col = blockIdx.x * 32LL * kSpan;
+  const int left = (int)min(32LL * kSpan, o.cols - col);
+  for (long long r = blockIdx.y * 8LL + threadIdx.x / 32; r < o.rows; r += gridDim.y * 8LL) {
+    const signed char* from = o.codes + r * o.sc + col + lane;
+    const unsigned char* power = o.powers + r * o.sp + col / 32;
+    signed char code[kSpan];
+    unsigned char p[kSpan];
+#pragma unroll
+    for (int g = 0; g < kSpan; ++g)
+      if (32 * g + lane < left) {
+        code[g] = from[32 * g];
+        p[g] = power[g];
+      }
+    T* x = (T*)o.x + r * o.sx + col + lane;
+#pragma unroll
+    for (int g = 0; g < kSpan; ++g)
+      if (32 * g + lane < left) x[32 * g] = from_f32<T>((float)code[g] * __uint_as_float((unsigned)p[g] << 23));
+  }
+}
+dim3 any_grid(const abcd_ctx* ctx, const PackedArgs::One& o) {
+  const long long slices = (o.cols + 32 * kSpan - 1) / (32 * kSpan);
+  return dim3((unsigned)slices, (unsigned)std::min((o.rows + 7) / 8, std::max(1LL, 8LL * ctx->num_sms / slices)));
+}
+
 PackedArgs::One one_of(const abcd_packed8* q, void* x, long long stride, int dtype) {
   const bool vec = (((uintptr_t)x | (q->rows > 1 ? (size_t)stride * elem_size(dtype) : 0)) & 15) == 0;
   return PackedArgs::One{x, q->codes, q->powers, q->rows, q->cols, stride, q->stride, q->power_stride,
@@ -185,7 +248,7 @@ dim3 grid_of(const abcd_ctx* ctx, const PackedArgs& a, int n) {
     const PackedArgs::One& o = a.m[k];
     const long long per_cta = 256 / o.lanes * kFlight, s = (o.cols + 8 * o.lanes - 1) / (8 * o.lanes);
     slices = std::max(slices, s);
-    rows = std::max(rows, std::min((o.rows + per_cta - 1) / per_cta, std::max(1LL, 12LL * ctx->num_sms / (s * n))));
+    rows = std::max(rows, std::min((o.rows + per_cta - 1) / per_cta, std::max(1LL, 4LL * ctx->num_sms / (s * n))));
   }
   return dim3((unsigned)slices, (unsigned)rows, (unsigned)n);
 }
@@ -199,6 +262,13 @@ abcd_status unpack(abcd_ctx* ctx, const Unpacked* list, int n) {
     for (int k = 0; k < n; ++k)
       if (list[k].dtype == dtype) a.m[count++] = one_of(list[k].from, list[k].to, list[k].stride, dtype);
     if (count == 0) continue;
+    if (count == 1 && !a.m[0].vec) {
+      const abcd_status st = with_type(dtype, [&](auto t) {
+        return check_launch(ctx, "unpack8_any_kernel", launch_pdl(unpack8_any_kernel<decltype(t)>, any_grid(ctx, a.m[0]), dim3(256), 0, ctx->stream, a));
+      });
+      if (st != ABCD_OK) return st;
+      continue;
+    }
     const abcd_status st = with_type(dtype, [&](auto t) {
       return check_launch(ctx, "unpack8_kernel", launch_pdl(unpack8_kernel<decltype(t)>, grid_of(ctx, a, count), dim3(256), 0, ctx->stream, a));
     });
@@ -220,6 +290,8 @@ extern "C" abcd_status abcd_pack8(abcd_ctx* ctx, const abcd_matrix* x, const abc
   PackedArgs a{};
   a.m[0] = one_of(packed, x->data, x->stride, x->dtype);
   return with_type(x->dtype, [&](auto t) {
+    if (!a.m[0].vec)
+      return check_launch(ctx, "pack8_any_kernel", launch_pdl(pack8_any_kernel<decltype(t)>, any_grid(ctx, a.m[0]), dim3(256), 0, ctx->stream, a));
     return check_launch(ctx, "pack8_kernel", launch_pdl(pack8_kernel<decltype(t)>, grid_of(ctx, a, 1), dim3(256), 0, ctx->stream, a));
   });
 }

@@ -194,6 +194,16 @@ __global__ void __launch_bounds__(kLongThreads) close_bwd_long_kernel(const __gr
   }
 }
 
+// Pairs of values: one instruction does both (the kernels are bound by what they issue, not by the units).
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
+// a - b, rounded as the difference is
+__device__ __forceinline__ float2 sub2(float2 a, float b) { return __fadd2_rn(a, both(-b)); }
+// close_value of a pair
+__device__ __forceinline__ float2 close_pair(float2 x, float2 fh, float2 A, float2 C) { return add2(x, fma2(A, fh, C)); }
+
 // How a row lies over threads: E values each, TPR threads a row.  VEC: rows on 16-byte boundaries, E values as
 // vectors of 16 bytes, which the threads that use them copy ahead to shared memory.  Else the 16-byte pieces
 // that a row reaches into are copied ahead by its threads together, and a thread takes every TPR-th
@@ -223,6 +233,7 @@ template <typename T, typename R> struct CloseRows {
   int bytes[R::NV];                   // VEC: of the thread's vectors
   int rows, turns, lane, cols;        // rows of the group; turns that its threads take together
   int now;                            // the slot of the row at hand
+  bool partial;                       // the thread has columns past the row's end
 
   __device__ __forceinline__ CloseRows(char* smem, const CloseArgs& a) {
     const int group = threadIdx.x / R::TPR;
@@ -234,6 +245,7 @@ template <typename T, typename R> struct CloseRows {
     turns = R::TPR >= 32 ? rows : (int)((a.rows - (long long)blockIdx.x * R::kGroups + step - 1) / step);
     slots = smem + (R::VEC ? threadIdx.x * 16 : group * R::kRowBytes);
     now = 0;
+    partial = column(R::NV - 1) + R::V > cols;
     const T* const base[4] = {(const T*)a.f, (const T*)a.x, (const T*)a.dy, (const T*)a.dn};
     const long long stride[4] = {a.sf, a.sx, a.sdy, a.sdn};
 #pragma unroll
@@ -304,7 +316,8 @@ template <typename T, typename R> struct CloseRows {
   __device__ __forceinline__ void next() { now = now == R::kDepth - 1 ? 0 : now + 1; }
   // The thread's values of the row at hand of a matrix (`at`: where the row starts): zeros past its end, of no
   // row and of a matrix that is not there.
-  __device__ __forceinline__ void get(float (&v)[R::E], int t, int mat, const T* at) const {
+  __device__ __forceinline__ void get(float2 (&pairs)[R::E / 2], int t, int mat, const T* at) const {
+    float v[R::E];
     if constexpr (R::VEC) {
 #pragma unroll
       for (int j = 0; j < R::NV; ++j) {
@@ -317,14 +330,16 @@ template <typename T, typename R> struct CloseRows {
 #pragma unroll
       for (int e = 0; e < R::E; ++e) v[e] = at && column(e) < cols ? to_f32(p[e * R::TPR]) : 0.f;
     }
+#pragma unroll
+    for (int e = 0; e < R::E / 2; ++e) pairs[e] = make_float2(v[2 * e], v[2 * e + 1]);
   }
-  __device__ __forceinline__ void put(T* to, const float (&v)[R::E], int t) const {
+  __device__ __forceinline__ void put(T* to, const float2 (&v)[R::E / 2], int t) const {
     if (R::TPR < 32 && t >= rows) return;
 #pragma unroll
     for (int j = 0; j < R::NV; ++j) {
       float w[R::V];
 #pragma unroll
-      for (int i = 0; i < R::V; ++i) w[i] = v[j * R::V + i];
+      for (int i = 0; i < R::V; ++i) w[i] = (j * R::V + i) % 2 ? v[(j * R::V + i) / 2].y : v[(j * R::V + i) / 2].x;
       if constexpr (R::VEC) {
         if (bytes[j] > 0) store_vec<T, R::V>(to + column(j), w, bytes[j] / (int)sizeof(T));
       } else {
@@ -333,7 +348,8 @@ template <typename T, typename R> struct CloseRows {
     }
   }
   // A vector's values of the thread's columns; zero past their end.
-  __device__ __forceinline__ void weights(float (&v)[R::E], const void* w, int wide, float none) const {
+  __device__ __forceinline__ void weights(float2 (&pairs)[R::E / 2], const void* w, int wide, float none) const {
+    float v[R::E];
 #pragma unroll
     for (int j = 0; j < R::NV; ++j) {
       float u[R::V];
@@ -342,6 +358,8 @@ template <typename T, typename R> struct CloseRows {
 #pragma unroll
       for (int i = 0; i < R::V; ++i) v[j * R::V + i] = i < left ? u[i] : 0.f;
     }
+#pragma unroll
+    for (int e = 0; e < R::E / 2; ++e) pairs[e] = make_float2(v[2 * e], v[2 * e + 1]);
   }
 };
 
@@ -358,32 +376,38 @@ template <int TPR> __device__ __forceinline__ void row_sum(float& a, float2 (*re
 
 // A row's statistics from the threads' values (which are zero past its end).
 template <typename T, typename R>
-__device__ __forceinline__ Stat stat_of_row(const CloseRows<T, R>& rows, const float (&v)[R::E], int kind, float eps, float inv, float2 (*red)[32], int& turn) {
-  float s = 0.f, q = 0.f;
+__device__ __forceinline__ Stat stat_of_row(const CloseRows<T, R>& rows, const float2 (&v)[R::E / 2], int kind, float eps, float inv, float2 (*red)[32], int& turn) {
+  constexpr int P = R::E / 2;
+  float2 s2 = both(0.f), q2 = both(0.f);
   if (kind == ABCD_RMS_NORM) {
 #pragma unroll
-    for (int e = 0; e < R::E; ++e) q += v[e] * v[e];
+    for (int e = 0; e < P; ++e) q2 = fma2(v[e], v[e], q2);
+    float q = q2.x + q2.y;
     row_sum<R::TPR>(q, red, turn);
     turn ^= 1;
     return Stat{0.f, rsqrtf(q * inv + eps)};
   }
 #pragma unroll
-  for (int e = 0; e < R::E; ++e) s += v[e];
+  for (int e = 0; e < P; ++e) s2 = add2(s2, v[e]);
+  float s = s2.x + s2.y;
   row_sum<R::TPR>(s, red, turn);
   // the division's rounding taken back, then what the sum has rounded
-  float mean = s * inv, off = 0.f;
+  float mean = s * inv;
   mean = __fmaf_rn(__fmaf_rn(-mean, (float)rows.cols, s), inv, mean);
+  s2 = both(0.f);
 #pragma unroll
-  for (int j = 0; j < R::NV; ++j) {
-    const int left = rows.cols - rows.column(j);           // past the row's end nothing deviates
-#pragma unroll
-    for (int i = 0; i < R::V; ++i) {
-      float d = v[j * R::V + i] - mean;
-      if (left < R::V) d = i < left ? d : 0.f;
-      q += d * d;
-      off += d;
+  for (int e = 0; e < P; ++e) {
+    float2 d = sub2(v[e], mean);
+    // past the row's end nothing deviates
+    if (rows.partial) {
+      const int c = rows.column(2 * e / R::V) + 2 * e % R::V, next = R::V == 1 ? rows.column(2 * e + 1) : c + 1;
+      if (c >= rows.cols) d.x = 0.f;
+      if (next >= rows.cols) d.y = 0.f;
     }
+    q2 = fma2(d, d, q2);
+    s2 = add2(s2, d);
   }
+  float q = q2.x + q2.y, off = s2.x + s2.y;
   row_sum2<R::TPR>(q, off, red, turn ^ 1);
   off *= inv;
   return Stat{mean + off, rstd_of(q * inv, off, eps)};
@@ -391,15 +415,16 @@ __device__ __forceinline__ Stat stat_of_row(const CloseRows<T, R>& rows, const f
 
 // A and C of the thread's columns.
 template <typename T, typename R>
-__device__ __forceinline__ void factors(const CloseRows<T, R>& rows, const CloseArgs& a, float (&A)[R::E], float (&C)[R::E]) {
-  float g[R::E];
+__device__ __forceinline__ void factors(const CloseRows<T, R>& rows, const CloseArgs& a, float2 (&A)[R::E / 2], float2 (&C)[R::E / 2]) {
+  float2 g[R::E / 2];
   rows.weights(g, a.gate, a.wide_w, 1.f);
   rows.weights(A, a.w[0], a.wide_w, 1.f);
   rows.weights(C, a.b[0], a.wide_w, 0.f);
 #pragma unroll
-  for (int e = 0; e < R::E; ++e) {
-    A[e] *= a.scale * g[e];
-    C[e] *= a.scale * g[e];
+  for (int e = 0; e < R::E / 2; ++e) {
+    const float2 sg = mul2(g[e], both(a.scale));
+    A[e] = mul2(A[e], sg);
+    C[e] = mul2(C[e], sg);
   }
 }
 
@@ -407,10 +432,11 @@ template <typename T, typename R>
 __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_fwd_kernel(const __grid_constant__ CloseArgs a) {
   extern __shared__ __align__(16) char smem[];
   __shared__ float2 red[2][32];
+  constexpr int P = R::E / 2;
   pdl_wait();
   CloseRows<T, R> rows(smem, a);
   rows.start();
-  float A[R::E], C[R::E], W[R::E], B[R::E];
+  float2 A[P], C[P], W[P], B[P];
   factors(rows, a, A, C);
   rows.weights(W, a.w[1], a.wide_w, 1.f);
   rows.weights(B, a.b[1], a.wide_w, 0.f);
@@ -424,17 +450,17 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_fwd_kernel(const 
   int half = 0;
   for (int t = 0; t < rows.turns; ++t, r += step, y += step * a.sy, n += step * a.sn, atf += step * a.sf, atx += step * a.sx) {
     rows.turn(t);
-    float f[R::E], x[R::E];
+    float2 f[P], x[P];
     rows.get(f, t, 0, atf);
     rows.get(x, t, 1, atx);
     Stat first{0.f, 1.f}, second{0.f, 1.f};
     if (a.kind[0] != kNone) first = stat_of_row(rows, f, a.kind[0], a.eps[0], inv, red, half);
 #pragma unroll
-    for (int e = 0; e < R::E; ++e) x[e] = close_value(x[e], (f[e] - first.mean) * first.rstd, A[e], C[e]);
+    for (int e = 0; e < P; ++e) x[e] = close_pair(x[e], mul2(sub2(f[e], first.mean), both(first.rstd)), A[e], C[e]);
     if (a.kind[1] != kNone) {
       second = stat_of_row(rows, x, a.kind[1], a.eps[1], inv, red, half);
 #pragma unroll
-      for (int e = 0; e < R::E; ++e) f[e] = (x[e] - second.mean) * second.rstd * W[e] + B[e];
+      for (int e = 0; e < P; ++e) f[e] = fma2(mul2(sub2(x[e], second.mean), both(second.rstd)), W[e], B[e]);
       rows.put(n, f, t);
     }
     rows.put(y, x, t);
@@ -454,12 +480,17 @@ template <typename T, typename R>
 __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const __grid_constant__ CloseArgs a) {
   extern __shared__ __align__(16) char smem[];
   __shared__ float2 red[2][32];
+  constexpr int P = R::E / 2;
   pdl_wait();
   CloseRows<T, R> rows(smem, a);
   rows.start();
-  float A[R::E], C[R::E], W[R::E], sums[4][R::E] = {};
+  float2 A[P], C[P], W[P], sums[4][P];
   factors(rows, a, A, C);
   rows.weights(W, a.w[1], a.wide_w, 1.f);
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int e = 0; e < P; ++e) sums[k][e] = both(0.f);
   const float inv = 1.f / (float)a.cols;
   const float centre[2] = {a.kind[0] == ABCD_LAYER_NORM ? inv : 0.f, a.kind[1] == ABCD_LAYER_NORM ? inv : 0.f};
   const long long step = (long long)gridDim.x * R::kGroups;
@@ -480,51 +511,50 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
       next[0] = stat_of(a, 0, r + step);
       next[1] = stat_of(a, 1, r + step);
     }
-    float fh[R::E], yh[R::E], g[R::E], s1 = 0.f, s2 = 0.f;
+    float2 fh[P], yh[P], g[P], p1 = both(0.f), p2 = both(0.f);
     rows.get(fh, t, 0, at[0]);
     rows.get(yh, t, 1, at[1]);
     rows.get(g, t, 2, at[2]);
+#pragma unroll
+    for (int e = 0; e < P; ++e) fh[e] = mul2(sub2(fh[e], first.mean), both(first.rstd));
     if (a.dn) {
-      float dn[R::E];
+      float2 dn[P];
       rows.get(dn, t, 3, at[3]);
 #pragma unroll
-      for (int e = 0; e < R::E; ++e) {
-        fh[e] = (fh[e] - first.mean) * first.rstd;
-        yh[e] = (close_value(yh[e], fh[e], A[e], C[e]) - second.mean) * second.rstd;   // the forward pass's, bit for bit
-        sums[2][e] += dn[e];
-        sums[3][e] += dn[e] * yh[e];
-        dn[e] *= W[e];
-        s1 += dn[e];
-        s2 += dn[e] * yh[e];
+      for (int e = 0; e < P; ++e) {
+        yh[e] = mul2(sub2(close_pair(yh[e], fh[e], A[e], C[e]), second.mean), both(second.rstd));   // the forward pass's, bit for bit
+        sums[2][e] = add2(sums[2][e], dn[e]);
+        sums[3][e] = fma2(dn[e], yh[e], sums[3][e]);
+        dn[e] = mul2(dn[e], W[e]);
+        p1 = add2(p1, dn[e]);
+        p2 = fma2(dn[e], yh[e], p2);
       }
+      float s1 = p1.x + p1.y, s2 = p2.x + p2.y;
       row_sum2<R::TPR>(s1, s2, red, 0);
       s1 *= centre[1];
       s2 *= inv;
 #pragma unroll
-      for (int e = 0; e < R::E; ++e) g[e] += second.rstd * (dn[e] - s1 - yh[e] * s2);
-    } else {
-#pragma unroll
-      for (int e = 0; e < R::E; ++e) fh[e] = (fh[e] - first.mean) * first.rstd;
+      for (int e = 0; e < P; ++e) g[e] = fma2(fma2(yh[e], both(-s2), sub2(dn[e], s1)), both(second.rstd), g[e]);
     }
-    const bool in = R::TPR >= 32 || t < rows.rows;
     if (a.y) rows.put(dx, g, t);
-    s1 = s2 = 0.f;
+    p1 = p2 = both(0.f);
 #pragma unroll
-    for (int e = 0; e < R::E; ++e) {
-      if (!in) g[e] = 0.f;
-      sums[0][e] += g[e];
-      sums[1][e] += g[e] * fh[e];
-      g[e] *= A[e];
-      s1 += g[e];
-      s2 += g[e] * fh[e];
+    for (int e = 0; e < P; ++e) {
+      if (R::TPR < 32 && t >= rows.rows) g[e] = both(0.f);
+      sums[0][e] = add2(sums[0][e], g[e]);
+      sums[1][e] = fma2(g[e], fh[e], sums[1][e]);
+      g[e] = mul2(g[e], A[e]);
+      p1 = add2(p1, g[e]);
+      p2 = fma2(g[e], fh[e], p2);
     }
     if (a.n) {
       if (a.kind[0] != kNone) {
+        float s1 = p1.x + p1.y, s2 = p2.x + p2.y;
         row_sum2<R::TPR>(s1, s2, red, 1);
         s1 *= centre[0];
         s2 *= inv;
 #pragma unroll
-        for (int e = 0; e < R::E; ++e) g[e] = first.rstd * (g[e] - s1 - fh[e] * s2);
+        for (int e = 0; e < P; ++e) g[e] = mul2(fma2(fh[e], both(-s2), sub2(g[e], s1)), both(first.rstd));
       }
       rows.put(df, g, t);
     }
@@ -545,9 +575,10 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
-    for (int e = 0; e < R::E; ++e)
+    for (int e = 0; e < P; ++e)
 #pragma unroll
-      for (int o = 16; o >= R::TPR; o >>= 1) sums[k][e] += __shfl_xor_sync(~0u, sums[k][e], o);
+      for (int o = 16; o >= R::TPR; o >>= 1)
+        sums[k][e] = add2(sums[k][e], make_float2(__shfl_xor_sync(~0u, sums[k][e].x, o), __shfl_xor_sync(~0u, sums[k][e].y, o)));
   constexpr int ROUNDS = R::TPR > 32 ? R::kGroups : R::kThreads / 32, CAPACITY = R::TPR * R::E;
   const int mine = R::TPR > 32 ? threadIdx.x / R::TPR : threadIdx.x / 32;
   const bool one = R::TPR >= 32 || (threadIdx.x & 31) < R::TPR;
@@ -559,7 +590,7 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
 #pragma unroll
       for (int e = 0; e < R::E; ++e) {
         float* to = total + k * CAPACITY + rows.column(e / R::V) + e % R::V;
-        *to = (q ? *to : 0.f) + sums[k][e];
+        *to = (q ? *to : 0.f) + (e % 2 ? sums[k][e / 2].y : sums[k][e / 2].x);
       }
   }
   __syncthreads();
