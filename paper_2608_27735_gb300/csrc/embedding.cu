@@ -30,72 +30,75 @@ struct LookupArgs {
   void* y;
   long long rows, st, sa, sy;
   unsigned table_rows, cols, lanes;   // lanes: threads of a token, up to 256
+  int slices;                         // of lanes x V columns
   int wide;                           // 64-bit indices
   float scale;
   unsigned* status;
 };
 
-// V consecutive columns a thread (16 bytes, or one where rows start anywhere), `lanes` threads a token,
-// kFlight tokens of a thread on their way at once: first their indices, then the rows that they name.
-constexpr int kFlight = 4, kEmbedWaves = 4;
-template <typename T, int V>
-__global__ void __launch_bounds__(256, V > 4 ? 3 : 4) embed_kernel(const __grid_constant__ LookupArgs a) {
+// V elements at p; of a row's last vector, which may pass its end, those that `left` counts.
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_part(const T* p, bool whole, int left) {
+  Pack<T, V> v;
+  if (whole) {
+    v = *reinterpret_cast<const Pack<T, V>*>(p);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v.v[e] = e < left ? p[e] : T(0.f);
+  }
+  return v;
+}
+
+// V consecutive columns a thread (16 bytes, or one where rows start anywhere), `lanes` threads a token; a CTA
+// takes kLookup tokens of each group of threads.  Bound by latency, unless many rows are on their way at once:
+// the indices go to shared memory first, and a thread's loads are asked for U tokens at a time, without a
+// condition (with one, the compiler moved each load to its use: 1,000,000 x 64 fp32 90 us).
+constexpr int kLookup = 16;
+template <typename T, int V, bool ADD>
+__global__ void __launch_bounds__(256) embed_kernel(const __grid_constant__ LookupArgs a) {
   pdl_wait();
   using P = Pack<T, V>;
+  constexpr int U = ADD ? 4 : 8;
+  __shared__ unsigned at[256 * kLookup];
   const unsigned groups = 256u / a.lanes, group = threadIdx.x / a.lanes;
-  const unsigned c = (blockIdx.x * a.lanes + threadIdx.x - group * a.lanes) * V;
-  if (group >= groups || c >= a.cols) return;
-  const bool whole = V == 1 || c + V <= a.cols;          // else the row's last vector passes its end
+  const long long first = blockIdx.x / a.slices * (long long)(groups * kLookup);
+  const int n = (int)min((long long)(groups * kLookup), a.rows - first);
+  for (int i = threadIdx.x; i < n; i += 256) at[i] = row_of_token(a.index, a.wide, first + i, a.table_rows, a.status);
+  __syncthreads();
+  const unsigned c = (unsigned)(blockIdx.x % a.slices * a.lanes + threadIdx.x - group * a.lanes) * V;
+  if (group >= groups || c >= a.cols || (int)group >= n) return;
+  const bool whole = V == 1 || c + V <= a.cols;
+  const int left = (int)(a.cols - c);
   const T* table = (const T*)a.table + c;
-  const long long step = gridDim.y * (long long)(groups * kFlight);
-  unsigned at[kFlight];
-  auto rows_named = [&](long long r0) {
+  const T* add = ADD ? (const T*)a.add + first * a.sa + c : nullptr;
+  T* y = (T*)a.y + first * a.sy + c;
+  // the groups' tokens in turn
+  for (int i0 = group; i0 < n; i0 += U * groups) {
+    P v[U], w[ADD ? U : 1];
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k)
-      at[k] = r0 + k * groups < a.rows ? row_of_token(a.index, a.wide, r0 + k * groups, a.table_rows, a.status) : a.table_rows;
-  };
-  long long r0 = blockIdx.y * (long long)(groups * kFlight) + group;
-  rows_named(r0);
-  for (; r0 < a.rows; r0 += step) {
-    const int n = (int)min((long long)kFlight, (a.rows - r0 + groups - 1) / groups);
-    P v[kFlight], add[kFlight];
-#pragma unroll
-    for (int k = 0; k < kFlight; ++k) {
-      if (at[k] >= a.table_rows) v[k] = P{};
-      else if (whole) v[k] = *reinterpret_cast<const P*>(table + at[k] * a.st);
-      else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[k].v[e] = c + e < a.cols ? table[at[k] * a.st + e] : T(0.f);
-      }
+    for (int u = 0; u < U; ++u) {
+      const int i = min(i0 + u * (int)groups, n - 1);
+      const unsigned row = at[i] < a.table_rows ? at[i] : 0u;
+      v[u] = load_part<T, V>(table + row * a.st, whole, left);
+      if (ADD) w[u] = load_part<T, V>(add + i * a.sa, whole, left);
     }
-    rows_named(r0 + step);                                // the next ones' indices
-    if (a.add) {
-      const T* p = (const T*)a.add + r0 * a.sa + c;
 #pragma unroll
-      for (int k = 0; k < kFlight; ++k, p += groups * a.sa) {
-        if (k >= n) break;
-        if (whole) add[k] = *reinterpret_cast<const P*>(p);
-        else {
-#pragma unroll
-          for (int e = 0; e < V; ++e) add[k].v[e] = c + e < a.cols ? p[e] : T(0.f);
-        }
-      }
-    }
-    T* y = (T*)a.y + r0 * a.sy + c;
-#pragma unroll
-    for (int k = 0; k < kFlight; ++k, y += groups * a.sy) {
-      if (k >= n) break;
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * (int)groups;
+      if (i >= n) break;
+      const bool none = at[i] >= a.table_rows;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        float x = a.scale * to_f32(v[k].v[e]);
-        if (a.add) x += to_f32(add[k].v[e]);
-        v[k].v[e] = from_f32<T>(x);
+        float x = none ? 0.f : a.scale * to_f32(v[u].v[e]);
+        if (ADD) x += to_f32(w[u].v[e]);
+        v[u].v[e] = from_f32<T>(x);
       }
-      if (whole) *reinterpret_cast<P*>(y) = v[k];
-      else {
+      T* to = y + i * a.sy;
+      if (whole) {
+        *reinterpret_cast<P*>(to) = v[u];
+      } else {
 #pragma unroll
         for (int e = 0; e < V; ++e)
-          if (c + e < a.cols) y[e] = v[k].v[e];
+          if (e < left) to[e] = v[u].v[e];
       }
     }
   }
@@ -342,17 +345,8 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const __grid_constant__ 
     Pack<T, V> v[U];
     if (in) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + u;
-        if (i >= g1 || key[i + 1] >= a.table_rows) continue;
-        const T* p = (const T*)a.dy + (long long)id[i] * a.sdy + c;
-        if (V == 1 || c + V <= a.cols) {
-          v[u] = *reinterpret_cast<const Pack<T, V>*>(p);
-        } else {
-#pragma unroll
-          for (int e = 0; e < V; ++e) v[u].v[e] = c + e < a.cols ? p[e] : T(0.f);
-        }
-      }
+      for (int u = 0; u < U; ++u)     // without a condition, so that all are on their way before the first is used
+        v[u] = load_part<T, V>((const T*)a.dy + (long long)id[min(i0 + u, g1 - 1)] * a.sdy + c, V == 1 || c + V <= a.cols, (int)(a.cols - c));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -590,16 +584,17 @@ extern "C" abcd_status abcd_embedding(abcd_ctx* ctx, const abcd_matrix* table, c
   if (overlap(table, y) || on_add || on_index(y, index, index_dtype, y->rows))
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: y overlaps an operand", what);
   LookupArgs a{table->data, index, add ? add->data : nullptr, y->data, y->rows, table->stride, add ? add->stride : 0, y->stride,
-                     (unsigned)table->rows, (unsigned)y->cols, 1, index_dtype == ABCD_I64, scale, (unsigned*)ctx->net_base};
+                     (unsigned)table->rows, (unsigned)y->cols, 1, 1, index_dtype == ABCD_I64, scale, (unsigned*)ctx->net_base};
   return with_type(y->dtype, [&](auto t) {
     using T = decltype(t);
     constexpr int V = 16 / sizeof(T);
     const bool vec = rows_aligned(table, 16) && rows_aligned(y, 16) && (!add || rows_aligned(add, 16));
     const long long vectors = vec ? (y->cols + V - 1) / V : y->cols;
     a.lanes = (unsigned)std::min(256LL, vectors);
-    const long long slices = (vectors + a.lanes - 1) / a.lanes, per_cta = 256 / a.lanes * kFlight;
-    const long long grid = std::min((y->rows + per_cta - 1) / per_cta, std::max(1LL, (long long)kEmbedWaves * ctx->num_sms / slices));
-    return check_launch(ctx, "embed_kernel", launch_pdl(vec ? embed_kernel<T, V> : embed_kernel<T, 1>, dim3((unsigned)slices, (unsigned)grid), dim3(256), 0, ctx->stream, a));
+    a.slices = (int)((vectors + a.lanes - 1) / a.lanes);
+    const long long per_cta = 256 / a.lanes * kLookup, grid = (y->rows + per_cta - 1) / per_cta * a.slices;
+    auto* kernel = vec ? (add ? embed_kernel<T, V, true> : embed_kernel<T, V, false>) : (add ? embed_kernel<T, 1, true> : embed_kernel<T, 1, false>);
+    return check_launch(ctx, "embed_kernel", launch_pdl(kernel, dim3((unsigned)grid), dim3(256), 0, ctx->stream, a));
   });
 }
 

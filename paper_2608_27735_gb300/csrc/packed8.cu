@@ -116,7 +116,8 @@ __global__ void __launch_bounds__(256, 4) pack8_kernel(const __grid_constant__ P
   for (long long r = at.row; r - (threadIdx.x / o.lanes) < o.rows; r += at.step, x += at.step * o.sx, to += at.step * o.sc, power_to += at.step * o.sp) {
     Eight<T> v[kFlight];
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k) v[k].load(x + k * at.groups * o.sx, r + k * at.groups < o.rows ? at.left : 0, o.vec);
+    for (int k = 0; k < kFlight; ++k)      // without a condition: all are on their way before the first is used
+      v[k].load(x + (min(r + k * at.groups, o.rows - 1) - r) * o.sx, at.left, o.vec);
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
       unsigned top = v[k].top();
@@ -156,9 +157,9 @@ __global__ void __launch_bounds__(256, 4) unpack8_kernel(const __grid_constant__
     unsigned power[kFlight];
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
-      if (r + k * at.groups >= o.rows) break;
-      w[k] = *reinterpret_cast<const uint2*>(from + k * at.groups * o.sc);    // a row of codes has room for whole units
-      power[k] = power_from[k * at.groups * o.sp];
+      const long long row = min(r + k * at.groups, o.rows - 1) - r;
+      w[k] = *reinterpret_cast<const uint2*>(from + row * o.sc);              // a row of codes has room for whole units
+      power[k] = power_from[row * o.sp];
     }
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
