@@ -16,9 +16,11 @@ namespace {
 
 constexpr unsigned kBadIndex = 1u << ABCD_ERR_INVALID_ARG;    // the status bit of an index past the table
 
-// The row that token t names; `rows` for none.
-__device__ __forceinline__ unsigned row_of_token(const void* index, int wide, long long t, unsigned rows, unsigned* status) {
-  const long long i = wide ? ((const long long*)index)[t] : ((const int*)index)[t];
+// The row that token t names as it is given, and as it is taken: `rows` for none.
+__device__ __forceinline__ long long index_of(const void* index, int wide, long long t) {
+  return wide ? __ldg((const long long*)index + t) : (long long)__ldg((const int*)index + t);
+}
+__device__ __forceinline__ unsigned row_of(long long i, unsigned rows, unsigned* status) {
   if (i >= (long long)rows) atomicOr(status, kBadIndex);
   return i >= 0 && i < (long long)rows ? (unsigned)i : rows;
 }
@@ -31,6 +33,7 @@ struct LookupArgs {
   long long rows, st, sa, sy;
   unsigned table_rows, cols, lanes;   // lanes: threads of a token, up to 256
   int slices;                         // of lanes x V columns
+  int lookup;                         // tokens of a group of threads
   int wide;                           // 64-bit indices
   float scale;
   unsigned* status;
@@ -49,20 +52,27 @@ template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_part(con
 }
 
 // V consecutive columns a thread (16 bytes, or one where rows start anywhere), `lanes` threads a token; a CTA
-// takes kLookup tokens of each group of threads.  Bound by latency, unless many rows are on their way at once:
+// takes up to kLookup tokens of each group of threads.  Bound by latency, unless many rows are on their way at once:
 // the indices go to shared memory first, and a thread's loads are asked for U tokens at a time, without a
 // condition (with one, the compiler moved each load to its use: 1,000,000 x 64 fp32 90 us).
-constexpr int kLookup = 16;
+constexpr int kLookup = 16;           // at most: fewer where that leaves SMs idle
 template <typename T, int V, bool ADD>
 __global__ void __launch_bounds__(256) embed_kernel(const __grid_constant__ LookupArgs a) {
   pdl_wait();
   using P = Pack<T, V>;
-  constexpr int U = ADD ? 4 : 8;
+  constexpr int U = ADD || V > 4 ? 4 : 8;
   __shared__ unsigned at[256 * kLookup];
   const unsigned groups = 256u / a.lanes, group = threadIdx.x / a.lanes;
-  const long long first = blockIdx.x / a.slices * (long long)(groups * kLookup);
-  const int n = (int)min((long long)(groups * kLookup), a.rows - first);
-  for (int i = threadIdx.x; i < n; i += 256) at[i] = row_of_token(a.index, a.wide, first + i, a.table_rows, a.status);
+  const long long first = blockIdx.x / a.slices * (long long)(groups * a.lookup);
+  const int n = (int)min((long long)(groups * a.lookup), a.rows - first);
+  for (int i = threadIdx.x; i < n; i += 4 * 256) {
+    long long named[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) named[k] = index_of(a.index, a.wide, first + min(i + k * 256, n - 1));
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + k * 256 < n) at[i + k * 256] = row_of(named[k], a.table_rows, a.status);
+  }
   __syncthreads();
   const unsigned c = (unsigned)(blockIdx.x % a.slices * a.lanes + threadIdx.x - group * a.lanes) * V;
   if (group >= groups || c >= a.cols || (int)group >= n) return;
@@ -143,8 +153,19 @@ __device__ __forceinline__ void clear_rows(const SortArgs& a, int first) {
   else clear_rows<unsigned short>(a, first);
 }
 
-__device__ __forceinline__ unsigned sort_key(const SortArgs& a, long long i) {
-  return a.key ? a.key[i] : row_of_token(a.index, a.wide, i, a.table_rows, a.status);
+// The keys of N tokens, `step` apart from the first on: all are on their way before one is looked at.  (Past
+// `end`, that of the last one.)
+template <int N> __device__ __forceinline__ void sort_keys(const SortArgs& a, long long first, int step, long long end, unsigned (&key)[N]) {
+  if (a.key) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) key[k] = a.key[min(first + k * step, end - 1)];
+  } else {
+    long long named[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) named[k] = index_of(a.index, a.wide, min(first + k * step, end - 1));
+#pragma unroll
+    for (int k = 0; k < N; ++k) key[k] = row_of(named[k], a.table_rows, a.status);
+  }
 }
 
 // The tiles' tokens per digit.
@@ -156,12 +177,10 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const __grid_c
   for (int d = threadIdx.x; d < digits; d += kSortThreads) bins[d] = 0;
   __syncthreads();
   const long long first = (long long)blockIdx.x * a.per_tile, end = min(first + a.per_tile, a.n);
-  constexpr int U = 8;
+  constexpr int U = 4;
   for (long long i = first + threadIdx.x; i < end; i += U * kSortThreads) {
     unsigned key[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * kSortThreads < end) key[u] = sort_key(a, i + u * kSortThreads);
+    sort_keys(a, i, kSortThreads, end, key);
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (i + u * kSortThreads < end) atomicAdd(&bins[key[u] >> a.shift & (digits - 1)], 1u);
@@ -203,43 +222,51 @@ __device__ __forceinline__ unsigned warp_sums(unsigned v) {
   return v;
 }
 
-// Tokens to their places, equal digits in their order: a warp takes consecutive tokens of the tile, 32 at a
-// time, and knows how many of a digit the warps before it have.  One tile counts for itself.
+// Tokens to their places, equal digits in their order: a warp takes IT x 32 consecutive tokens of the tile, and
+// knows how many of a digit its lanes and the warps before it have.  They go to shared memory in the order of
+// their digits first, so that consecutive lanes write consecutive places.  One tile counts for itself.
+template <int IT>
 __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_constant__ SortArgs a) {
   pdl_wait();
   if (blockIdx.x >= a.tiles) return clear_rows(a, a.tiles);
-  extern __shared__ unsigned keys[];                  // of the tile
+  extern __shared__ uint2 sorted[];                   // key and id of the tile's tokens
   __shared__ unsigned place[kMaxDigits], local[kMaxDigits], sums[32];
   const int digits = 1 << a.bits, lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  const int per_warp = a.per_tile / kSortWarps;
-  const long long first = (long long)blockIdx.x * a.per_tile;
-  const int n = (int)min((long long)a.per_tile, a.n - first);
+  const long long first = (long long)blockIdx.x * (IT * kSortThreads);
+  const int n = (int)min((long long)(IT * kSortThreads), a.n - first), start = warp * 32 * IT + lane;
   // [warp][digit]: the warp's tokens, then those of the warps before it
-  unsigned short* before = reinterpret_cast<unsigned short*>(keys + a.per_tile);
-  for (int i = threadIdx.x; i < kSortWarps * digits / 2; i += kSortThreads) reinterpret_cast<unsigned*>(before)[i] = 0;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < n; i += kSortThreads) keys[i] = sort_key(a, first + i);
-  __syncthreads();
-  unsigned short* sorted = before + kSortWarps * digits;     // the tile's tokens in the order of their digits
+  unsigned short* before = reinterpret_cast<unsigned short*>(sorted + IT * kSortThreads);
   unsigned short* own = before + warp * digits;
-  const int start = warp * per_warp, end = min(start + per_warp, n);
-  for (int k = start; k < end; k += 32) {
-    const bool in = k + lane < end;
-    const unsigned d = in ? keys[k + lane] >> a.shift & (digits - 1) : ~0u;
+  unsigned key[IT];
+  sort_keys(a, first + start, 32, a.n, key);
+  for (int i = threadIdx.x; i < kSortWarps * digits / 2; i += kSortThreads) reinterpret_cast<unsigned*>(before)[i] = 0;
+  __syncthreads();
+  unsigned rank[IT];                                  // among the warp's tokens of the digit
+#pragma unroll
+  for (int k = 0; k < IT; ++k) {
+    const bool in = start + 32 * k < n;
+    const unsigned d = in ? key[k] >> a.shift & (digits - 1) : ~0u;
     const unsigned same = __match_any_sync(~0u, d);
-    if (in && lane == __ffs(same) - 1) own[d] += (unsigned short)__popc(same);
+    rank[k] = __popc(same & ((1u << lane) - 1));
+    unsigned had = in ? own[d] : 0u;
+    __syncwarp();
+    if (in && rank[k] == 0) own[d] = (unsigned short)(had + __popc(same));
+    rank[k] += had;
     __syncwarp();
   }
   __syncthreads();
   unsigned total = 0;
   if (threadIdx.x < digits) {
+    unsigned v[kSortWarps];
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) v[w] = before[w * digits + threadIdx.x];
+#pragma unroll
     for (int w = 0; w < kSortWarps; ++w) {
-      const unsigned v = before[w * digits + threadIdx.x];
       before[w * digits + threadIdx.x] = (unsigned short)total;
-      total += v;
+      total += v[w];
     }
   }
-  // a digit's first place, in all and in the tile
+  // a digit's first place, in the tile and in all
   auto first_places = [&](unsigned count) {
     const unsigned up_to = warp_sums(count);
     __syncthreads();
@@ -259,24 +286,28 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
     local[threadIdx.x] = inside;
     place[threadIdx.x] = outside - inside;
   }
-  __syncthreads();
-  for (int k = start; k < end; k += 32) {
-    const bool in = k + lane < end;
-    const unsigned d = in ? keys[k + lane] >> a.shift & (digits - 1) : ~0u;
-    const unsigned same = __match_any_sync(~0u, d);
-    if (in) sorted[local[d] + own[d] + __popc(same & ((1u << lane) - 1))] = (unsigned short)(k + lane);
-    __syncwarp();
-    if (in && lane == __ffs(same) - 1) own[d] += (unsigned short)__popc(same);
-    __syncwarp();
+  unsigned id[IT];
+#pragma unroll
+  for (int k = 0; k < IT; ++k) {
+    const long long i = min(first + start + 32 * k, a.n - 1);
+    id[k] = a.id ? a.id[i] : (unsigned)i;
   }
   __syncthreads();
-  // consecutive lanes write consecutive places of a digit
-#pragma unroll 4
-  for (int i = threadIdx.x; i < n; i += kSortThreads) {
-    const int from = sorted[i];
-    const unsigned key = keys[from], at = place[key >> a.shift & (digits - 1)] + i;
-    a.to_key[at] = key;
-    a.to_id[at] = a.id ? a.id[first + from] : (unsigned)(first + from);
+#pragma unroll
+  for (int k = 0; k < IT; ++k) {
+    if (start + 32 * k >= n) break;
+    const unsigned d = key[k] >> a.shift & (digits - 1);
+    sorted[local[d] + own[d] + rank[k]] = make_uint2(key[k], id[k]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < IT; ++k) {
+    const int i = threadIdx.x + k * kSortThreads;
+    if (i >= n) break;
+    const uint2 t = sorted[i];
+    const unsigned at = place[t.x >> a.shift & (digits - 1)] + i;
+    a.to_key[at] = t.x;
+    a.to_id[at] = t.y;
   }
 }
 
@@ -436,16 +467,19 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_c
     const long long chunk = base + group, end = (chunk + 1) * a.chunk;
     if (end < a.n) {
       const unsigned row = a.key[end - 1], then = a.key[end], first = a.key[end - a.chunk], before = chunk > 0 ? a.key[end - a.chunk - 1] : a.table_rows;
+      const unsigned beyond = end + a.chunk < a.n ? a.key[end + a.chunk] : a.table_rows;
       if (row < a.table_rows && then == row && !(first == row && before == row)) {
         // the last chunk that begins with the row: steps that double, then halve
         last = chunk + 1;
-        long long step = 1;
-        while (has(last + step, row)) {
-          last += step;
-          step *= 2;
+        if (beyond == row) {
+          long long step = 1;
+          while (has(last + step, row)) {
+            last += step;
+            step *= 2;
+          }
+          for (; step; step /= 2)
+            if (has(last + step, row)) last += step;
         }
-        for (; step; step /= 2)
-          if (has(last + step, row)) last += step;
         if (last - chunk <= kJoinAlone) {
           if (in) {
             float4 s = part(chunk, 1);
@@ -458,7 +492,7 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_c
     }
     if (lane == 0) last_of[group] = last;
   }
-  __syncthreads();
+  if (!__syncthreads_or(last >= 0)) return;
   for (int g = 0; g < groups; ++g) {
     if (last_of[g] < 0) continue;
     const long long chunk = base + g, count = last_of[g] - chunk;
@@ -491,8 +525,8 @@ SortPlan sort_plan(long long tokens, long long table_rows) {
   p.passes = (need + 9) / 10;
   p.bits = (need + p.passes - 1) / p.passes;
   // one tile needs no counts; more of them share the SMs, within what a CTA's shared memory holds
-  long long per = tokens <= kOneTile ? tokens : std::clamp<long long>((tokens + kNetSms - 1) / kNetSms, 4096, kOneTile);
-  per = std::max<long long>(1, (per + kSortThreads - 1) / kSortThreads) * kSortThreads;
+  long long per = 4096;
+  while (per < kOneTile && (tokens <= kOneTile ? tokens > per : tokens > per * kNetSms)) per *= 2;
   p.per_tile = (int)per;
   p.tiles = (int)((tokens + per - 1) / per);
   return p;
@@ -584,7 +618,7 @@ extern "C" abcd_status abcd_embedding(abcd_ctx* ctx, const abcd_matrix* table, c
   if (overlap(table, y) || on_add || on_index(y, index, index_dtype, y->rows))
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: y overlaps an operand", what);
   LookupArgs a{table->data, index, add ? add->data : nullptr, y->data, y->rows, table->stride, add ? add->stride : 0, y->stride,
-                     (unsigned)table->rows, (unsigned)y->cols, 1, 1, index_dtype == ABCD_I64, scale, (unsigned*)ctx->net_base};
+                     (unsigned)table->rows, (unsigned)y->cols, 1, 1, 1, index_dtype == ABCD_I64, scale, (unsigned*)ctx->net_base};
   return with_type(y->dtype, [&](auto t) {
     using T = decltype(t);
     constexpr int V = 16 / sizeof(T);
@@ -592,7 +626,9 @@ extern "C" abcd_status abcd_embedding(abcd_ctx* ctx, const abcd_matrix* table, c
     const long long vectors = vec ? (y->cols + V - 1) / V : y->cols;
     a.lanes = (unsigned)std::min(256LL, vectors);
     a.slices = (int)((vectors + a.lanes - 1) / a.lanes);
-    const long long per_cta = 256 / a.lanes * kLookup, grid = (y->rows + per_cta - 1) / per_cta * a.slices;
+    const long long groups = 256 / a.lanes;
+    a.lookup = (int)std::clamp<long long>(y->rows * a.slices / (4LL * ctx->num_sms * groups), 1, kLookup);
+    const long long per_cta = groups * a.lookup, grid = (y->rows + per_cta - 1) / per_cta * a.slices;
     auto* kernel = vec ? (add ? embed_kernel<T, V, true> : embed_kernel<T, V, false>) : (add ? embed_kernel<T, 1, true> : embed_kernel<T, 1, false>);
     return check_launch(ctx, "embed_kernel", launch_pdl(kernel, dim3((unsigned)grid), dim3(256), 0, ctx->stream, a));
   });
@@ -613,8 +649,9 @@ extern "C" abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix*
   if (!ctx->net_base || s.bytes > ctx->net_bytes)
     return fail(ctx, ABCD_ERR_WORKSPACE, "%s: the network workspace has %zu bytes, needs %zu", what, ctx->net_bytes, s.bytes);
   const SortPlan p = sort_plan(n, dtable->rows);
-  const size_t smem = 6 * (size_t)p.per_tile + (size_t)kSortWarps * 2 * ((size_t)1 << p.bits);
-  const cudaError_t room = allow_smem(ctx, (const void*)sort_place_kernel);
+  const size_t smem = 8 * (size_t)p.per_tile + (size_t)kSortWarps * 2 * ((size_t)1 << p.bits);
+  auto* place = p.per_tile == 4096 ? sort_place_kernel<4> : p.per_tile == 8192 ? sort_place_kernel<8> : sort_place_kernel<16>;
+  const cudaError_t room = allow_smem(ctx, (const void*)place);
   if (room != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(room));
   const long long e = (long long)elem_size(dtable->dtype);
   const bool flat = dtable->stride == dtable->cols;
@@ -635,7 +672,7 @@ extern "C" abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix*
       st = sort("sort_count_kernel", sort_count_kernel, p.tiles + more, kSortThreads, 0);
       if (st == ABCD_OK) st = sort("sort_scan_kernel", sort_scan_kernel, ((1 << p.bits) + 7) / 8, 256, 0);
     }
-    if (st == ABCD_OK) st = sort("sort_place_kernel", sort_place_kernel, p.tiles + (p.tiles > 1 ? 0 : more), kSortThreads, smem);
+    if (st == ABCD_OK) st = sort("sort_place_kernel", place, p.tiles + (p.tiles > 1 ? 0 : more), kSortThreads, smem);
     if (st != ABCD_OK) return st;
     q.key = q.to_key;
     q.id = q.to_id;
