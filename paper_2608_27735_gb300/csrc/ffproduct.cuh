@@ -30,7 +30,8 @@
 
 namespace abcd {
 
-enum { kPlain, kUp, kDown, kLinear };   // what becomes of the sums
+// What becomes of the sums.  kDown8 is kDown with the saved projections in 8 bits, of the large tile alone.
+enum { kPlain, kUp, kDown, kLinear, kDown8 };
 
 constexpr int kMaxSegments = 12;
 constexpr int kBlockK = 64;           // elements of k per stage: 128 bytes, the swizzle's row
@@ -68,13 +69,17 @@ constexpr int kMaxJobs = 3;
 struct ProductArgs {
   ProductJob job[kMaxJobs];
   int jobs, items;
-  // the large tile of 16-bit matrices: kUp stores c and, where their rows allow it, gate and up (g);
+  // the large tile of 16-bit matrices: kUp and kLinear store c and, where their rows allow it, gate and up, or z
+  // (g); kLinear loads the residual (in);
   // kDown loads gate, up (in) and stores
   // c, dG and dU (planes 0 and 1 of g[0])
   CUtensorMap c_map, g_map[2], in_map[2];
   int dtype;
   int act;
   Out g[2];                           // kUp: gate and up (p NULL: not wanted); kDown: dG and dU
+  // kDown8: the powers of gate's and up's groups of 32 columns
+  const unsigned char* power[2];
+  long long power_stride[2];
   Out in[2];                          // kDown: the saved gate and up; kLinear: the residual (p NULL: none)
   const void* bias;                   // kLinear, or NULL; z goes to g[0]
   int wide_bias;                      // it is fp32 whatever the matrices' type
@@ -396,6 +401,29 @@ __device__ __forceinline__ void put_block(char* block, int row, int j, const uns
   *reinterpret_cast<uint4*>(block + block_at(row, j + 1)) = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
+// kDown8: the powers of eight groups of 32 columns of a row, from group g on (a multiple of eight); 0, which
+// makes values nothing, outside of the matrix.
+__device__ __forceinline__ uint2 row_powers(const unsigned char* p, long long stride, int row, int rows, int g, int groups) {
+  uint2 v = make_uint2(0u, 0u);
+  if (row >= rows) return v;
+  p += row * stride + g;
+  if (((uintptr_t)p & 7) == 0 && g + 8 <= groups) return __ldg(reinterpret_cast<const uint2*>(p));
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (g + k < groups) (k < 4 ? v.x : v.y) |= (unsigned)__ldg(p + k) << (8 * (k & 3));
+  return v;
+}
+// 2^(p - 127) of group s.
+__device__ __forceinline__ float scale_at(const uint2& power, int s) {
+  return __uint_as_float(((s < 4 ? power.x : power.y) >> (8 * (s & 3)) & 255u) << 23);
+}
+// Sixteen codes' values.
+__device__ __forceinline__ void decode16(float (&v)[16], const uint4& x, float scale) {
+  const unsigned w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = code_value(w[e / 4] ^ 0x80808080u, e & 3) * scale;
+}
+
 // A work item of the persistent loop.
 struct Item {
   int job, batch, split, tm, tn;
@@ -446,16 +474,19 @@ struct Product {
   // asks for the blocks of the saved projections up to three ahead.  With accesses of the warps' own
   // instead (32 bytes of a row at a time), 100,000 x 256 x 1,024 took 167 and 196 us for kUp and kDown;
   // with the blocks 119 and 171.
-  static constexpr bool kBlocks = BN == 256 && !F32 && (EPI == kUp || EPI == kDown);
+  static constexpr bool kBlocks = BN == 256 && !F32 && EPI != kPlain;
   static constexpr int kBlockBytes = 128 * 64;
-  // Three blocks of results per group, and for kDown slots of a block of gate and one of up.
+  // Blocks of results per group (three, of kLinear two), and for kDown slots of a block of gate and one of up,
+  // for kLinear of one of the residual.
   // (A slot's blocks go to the groups in turn.  So it has two barriers that say it is full, one for each
   // group: a wait for a phase is right only for who has seen the phase before it end.)
   static constexpr int kSlots = 3;
-  static constexpr int kBlockRoom = (2 * 3 + (EPI == kDown ? 2 * kSlots : 0)) * kBlockBytes;
-  static constexpr int kThreads = 64 + 32 * kWarps + (kBlocks && EPI == kDown ? 32 : 0);
+  static constexpr bool kIsDown = EPI == kDown || EPI == kDown8;
+  static constexpr int kResults = EPI == kLinear ? 2 : 3, kAsked = kIsDown ? 2 : EPI == kLinear ? 1 : 0;
+  static constexpr int kBlockRoom = (2 * kResults + kAsked * kSlots) * kBlockBytes;
+  static constexpr int kThreads = 64 + 32 * kWarps + (kBlocks && kAsked ? 32 : 0);
   static constexpr int kWarpCols = kOutCols / (kWarps / 4);
-  static constexpr int CW = EPI != kPlain || kWarpCols < 32 ? 16 : 32;    // taken at a time
+  static constexpr int CW = EPI == kUp || EPI == kDown || EPI == kDown8 || kWarpCols < 32 ? 16 : 32;    // taken at a time
   // Elsewhere a warp turns its rows round in a buffer of its own.  The smallest tile leaves room for a
   // second CTA on the SM, whose warps fill the waits of the first's; kDown takes that room for the
   // saved projections, which come two turns ahead (20,000 x 64 x 256 in 32 bits: 45 us, and 58 with
@@ -468,7 +499,7 @@ struct Product {
   static constexpr int kRoom = ((kCtas == 2 ? 113 : 227) * 1024 - 512 - 1024 - kEpilogueBytes) / kStageBytes;
   static constexpr int kStages = kRoom > 8 ? 8 : kRoom;
   static_assert(kTurn >= (EPI == kPlain ? 32 * 16 * 4 : 0) && kStages >= 3);
-  static_assert(EPI == kPlain || (CW == 16 && kWarpCols % 16 == 0));
+  static_assert(kWarpCols % CW == 0 || EPI == kPlain);
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueBytes;
 };
 
@@ -554,8 +585,8 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
                 tma_load<CG>(sb + P::kBBytes / 2, &job.b[1], k, row_b, bz, bar);
               }
             } else {
-              const CUtensorMap* b = EPI == kDown ? &job.b[0] : &job.b[job.bsel[seg]];
-              if (EPI == kDown || b_last) {
+              const CUtensorMap* b = P::kIsDown ? &job.b[0] : &job.b[job.bsel[seg]];
+              if (P::kIsDown || b_last) {
 #pragma unroll
                 for (int c = 0; c < P::kBRows / 64; ++c) tma_load<CG>(sb + c * 8192, b, row_b + c * 64, k, bz, bar);
               } else {
@@ -609,7 +640,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
         };
         if constexpr (EPI == kUp || EPI == kLinear) {
           multiply(std::false_type(), std::false_type());
-        } else if constexpr (EPI == kDown) {
+        } else if constexpr (P::kIsDown) {
           multiply(std::false_type(), std::true_type());
         } else {
           if (job.a_rows_last) multiply(std::true_type(), std::true_type());
@@ -630,7 +661,7 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
     const int row0 = (int)rank * P::kRows;
     bool ok = true;
     if (warp == 2 + P::kWarps) {
-      if (lane == 0) {
+      if (lane == 0 && (EPI != kLinear || (a.in[0].p && a.in[0].vec))) {
         unsigned q = 0;
         for (int i = first; ok && i < items; i += step) {
           const Item it = item_of(a, i);
@@ -641,10 +672,10 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
             if (n >= a.job[0].n) break;
             const int slot = q % P::kSlots;
             if (!(ok = mbar_wait(slot_empty + 8 * slot, (q / P::kSlots & 1) ^ 1, a.limit, &dead))) break;
-            const uint32_t bar = slot_full + 8 * (q % (2 * P::kSlots)), at = smem_addr(buffers) + (6 + 2 * slot) * P::kBlockBytes;
-            mbar_expect(bar, 2 * P::kBlockBytes);
+            const uint32_t bar = slot_full + 8 * (q % (2 * P::kSlots)), at = smem_addr(buffers) + (2 * P::kResults + P::kAsked * slot) * P::kBlockBytes;
+            mbar_expect(bar, P::kAsked * (EPI == kDown8 ? 128 * 32 : P::kBlockBytes));
             tma_load<1>(at, &a.in_map[0], n, m, 0, bar);
-            tma_load<1>(at + P::kBlockBytes, &a.in_map[1], n, m, 0, bar);
+            if (P::kIsDown) tma_load<1>(at + P::kBlockBytes, &a.in_map[1], n, m, 0, bar);
             ++q;
           }
         }
@@ -653,17 +684,24 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
       const int quarter = warp & 3, share = (warp - 2) / 4, group = share / 2, half = share & 1;
       const int row = quarter * 32 + lane;
       const bool bf16 = a.dtype == ABCD_BF16;
-      const bool saved = EPI == kUp && a.g[0].p;
-      const bool saved_by_tma = saved && a.g[0].vec && a.g[1].vec;
+      // kUp's gate and up, kLinear's z
+      const bool saved = (EPI == kUp || EPI == kLinear) && a.g[0].p;
+      const bool saved_by_tma = saved && a.g[0].vec && (EPI == kLinear || a.g[1].vec);
+      const bool result_by_tma = EPI != kLinear || a.job[0].c[0].vec;
       const bool elected = (warp - 2) % 8 == 0 && lane == 0;   // of the group
       const uint32_t empty0 = at_rank(sums_empty, 0);
-      char* own = buffers + group * 3 * P::kBlockBytes;
+      char* own = buffers + group * P::kResults * P::kBlockBytes;
       int buf = 0;
       uint32_t phase = 0;
       unsigned q = 0;                                          // blocks of the CTA so far
       for (int i = first; i < items; i += step) {
         const Item it = item_of(a, i);
         const int m = it.tm * CG * P::kRows + row0, n0 = it.tn * P::kOutCols;
+        uint2 power[2];                                        // kDown8: of the row's eight groups of 32 columns
+        if constexpr (EPI == kDown8) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) power[k] = row_powers(a.power[k], a.power_stride[k], m + row, a.job[0].m, n0 / 32, (a.job[0].n + 31) / 32);
+        }
         ok = __all_sync(~0u, ok && mbar_wait(sums_full + 8 * buf, phase, a.limit, &dead));
         tc_fence_after();
         const uint32_t sums = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16);
@@ -686,16 +724,53 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] *= u[e];
             pack_all(v, x[0], bf16);
+          } else if constexpr (EPI == kLinear) {
+            const int rows = a.job[0].m - m - quarter * 32, cols = a.job[0].n - n0 - c;
+            float b = 0.f;
+            if (a.bias && lane < min(16, cols)) {
+              if (a.wide_bias) b = __ldg((const float*)a.bias + n0 + c + lane);
+              else b = unpack(__ldg((const unsigned short*)a.bias + n0 + c + lane), bf16);
+            }
+            if (a.in[0].p && a.in[0].vec) {
+              const unsigned at = q + s;
+              const int slot = at % P::kSlots;
+              const char* block = buffers + (2 * P::kResults + slot) * P::kBlockBytes;
+              ok = __all_sync(~0u, ok && mbar_wait(slot_full + 8 * (at % (2 * P::kSlots)), at / (2 * P::kSlots) & 1, a.limit, &dead));
+#pragma unroll
+              for (int e = 0; e < 2; ++e) unpack8(u + 8 * e, *reinterpret_cast<const uint4*>(block + block_at(row, 2 * half + e)), bf16);
+              __syncwarp();
+              if (ok && lane == 0) mbar_arrive(slot_empty + 8 * slot);
+              __syncwarp();
+            } else {
+              residual_ahead<F32>(u, a.in[0], m + quarter * 32, n0 + c, rows, cols, bf16);
+            }
+            tmem_load_wait(v);
+            if (a.bias) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] += __shfl_sync(~0u, b, e);
+            }
+            if (saved) pack_all(v, x[1], bf16);
+            if (a.act != ABCD_NO_ACTIVATION) act_values<F32>(v, a.act);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] += u[e];
+            pack_all(v, x[0], bf16);
           } else {
             const unsigned at = q + s;
             const int slot = at % P::kSlots;
             const char* block = buffers + (6 + 2 * slot) * P::kBlockBytes;
             ok = __all_sync(~0u, ok && mbar_wait(slot_full + 8 * (at % (2 * P::kSlots)), at / (2 * P::kSlots) & 1, a.limit, &dead));
             float z[16], d[16];
+            if constexpr (EPI == kDown8) {
+              // the codes' blocks: rows of 32 bytes under TMA's 32-byte swizzle
+              const int piece = row * 32 + ((half ^ (row / 4 & 1)) * 16);
+              decode16(z, *reinterpret_cast<const uint4*>(block + piece), scale_at(power[0], s));
+              decode16(u, *reinterpret_cast<const uint4*>(block + P::kBlockBytes + piece), scale_at(power[1], s));
+            } else {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              unpack8(z + 8 * e, *reinterpret_cast<const uint4*>(block + block_at(row, 2 * half + e)), bf16);
-              unpack8(u + 8 * e, *reinterpret_cast<const uint4*>(block + P::kBlockBytes + block_at(row, 2 * half + e)), bf16);
+              for (int e = 0; e < 2; ++e) {
+                unpack8(z + 8 * e, *reinterpret_cast<const uint4*>(block + block_at(row, 2 * half + e)), bf16);
+                unpack8(u + 8 * e, *reinterpret_cast<const uint4*>(block + P::kBlockBytes + block_at(row, 2 * half + e)), bf16);
+              }
             }
             __syncwarp();
             if (ok && lane == 0) mbar_arrive(slot_empty + 8 * slot);
@@ -716,13 +791,18 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
           if (elected) tma_store_read();
           named_barrier(1 + group, 256);
           put_block(own, row, 2 * half, x[0]);
-          if (EPI == kDown || saved) {
+          if (P::kIsDown || saved) {
             put_block(own + P::kBlockBytes, row, 2 * half, x[1]);
-            put_block(own + 2 * P::kBlockBytes, row, 2 * half, x[2]);
+            if (EPI != kLinear) put_block(own + 2 * P::kBlockBytes, row, 2 * half, x[2]);
+          }
+          if (!result_by_tma && ok) {
+            __syncwarp();
+            block_elements(own, quarter * 32, 2 * half, a.job[0].c[0], m + quarter * 32, n0 + c, min(32, a.job[0].m - m - quarter * 32),
+                           min(16, a.job[0].n - n0 - c));
           }
           if (saved && !saved_by_tma && ok) {
             __syncwarp();
-            for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < P::kResults - 1; ++k)
               block_elements(own + (k + 1) * P::kBlockBytes, quarter * 32, 2 * half, a.g[k], m + quarter * 32, n0 + c,
                              min(32, a.job[0].m - m - quarter * 32), min(16, a.job[0].n - n0 - c));
           }
@@ -731,8 +811,10 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
           if (elected && ok) {
             const int n = n0 + 32 * s;
             const uint32_t from = smem_addr(own);
-            tma_store(&a.c_map, n, m, 0, from);
-            if (EPI == kDown) {
+            if (result_by_tma) tma_store(&a.c_map, n, m, 0, from);
+            if (EPI == kLinear) {
+              if (saved_by_tma) tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
+            } else if (P::kIsDown) {
               tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
               tma_store(&a.g_map[0], n, m, 1, from + 2 * P::kBlockBytes);
             } else if (saved_by_tma) {
@@ -1003,9 +1085,9 @@ struct Shape {
   double idle, busy;         // of a stage (64 of k) where few SMs, where all ask for operands
   double epilogue[4][2];     // of a tile, by kPlain, kUp, kDown, kLinear and 16 or 32 bits
 };
-constexpr Shape kShapes[3] = {{2, 256, 1, 7.1, 0.25, 0.34, {{1.7, 1.8}, {2.7, 9.2}, {7.0, 36.0}, {2.4, 2.6}}},
-                              {1, 128, 1, 5.9, 0.22, 0.33, {{0.5, 0.8}, {2.5, 4.5}, {6.1, 17.0}, {0.8, 1.2}}},
-                              {1, 64, 2, 5.2, 0.24, 0.36, {{0.8, 1.0}, {2.1, 3.6}, {3.3, 8.3}, {1.1, 1.4}}}};
+constexpr Shape kShapes[3] = {{2, 256, 1, 7.1, 0.25, 0.34, {{1.7, 1.8}, {2.7, 9.2}, {7.0, 36.0}, {2.0, 2.6}}},
+                              {1, 128, 1, 5.9, 0.22, 0.33, {{0.5, 0.8}, {2.5, 4.5}, {6.1, 17.0}, {1.2, 1.4}}},
+                              {1, 64, 2, 5.2, 0.24, 0.36, {{0.8, 1.0}, {2.1, 3.6}, {3.3, 8.3}, {1.6, 1.6}}}};
 
 template <int EPI, bool F32> abcd_status launch_shape(abcd_ctx* ctx, int shape, const ProductArgs& a) {
   if (shape == 0) return launch_product<2, 256, EPI, F32>(ctx, a);

@@ -1,4 +1,4 @@
-// The gated feed-forward layer's products of 32-bit matrices.
+// The products of 32-bit matrices.
 #include "ffproduct.cuh"
 
 namespace abcd {

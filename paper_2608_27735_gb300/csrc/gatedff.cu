@@ -178,8 +178,12 @@ abcd_status ff_backward(abcd_ctx* ctx, const char* what, const abcd_matrix* dy, 
   if (needs_pack(w_up)) need.operand(f, d, t);
   if (needs_pack(w_down)) need.operand(d, f, t);
   const bool apart = t != ABCD_F32;                // gate and up are read as they are in 32 bits
-  if (apart && gate.moved()) need.operand(m, f, t);
-  if (apart && up.moved()) need.operand(m, f, t);
+  const Job shape_of{Operand{}, {Operand{}}, 1, false, true, m, f, d, 1, {}};
+  const Plan down_plan = plan(ctx->num_sms, t, kDown, &shape_of, 1);
+  // the large tile of 16-bit matrices takes 8-bit ones as they are
+  const bool direct = apart && gate.packed && up.packed && down_plan.shape == 0;
+  if (apart && !direct && gate.moved()) need.operand(m, f, t);
+  if (apart && !direct && up.moved()) need.operand(m, f, t);
   if (!apart && gate.packed) need.take(2 * net_align((size_t)m * (size_t)pitch_of(f) * 4));
   need.operand(m, f, t);
   need.operand(m, f, t, 2);
@@ -200,7 +204,11 @@ abcd_status ff_backward(abcd_ctx* ctx, const char* what, const abcd_matrix* dy, 
     return o;
   };
   Out wide[2]{};                                   // gate and up in 32 bits
-  if (apart) {
+  Hidden hid{};
+  if (direct) {
+    hid.packed[0] = gate.packed;
+    hid.packed[1] = up.packed;
+  } else if (apart) {
     ogate = operand(gate, t);
     oup = operand(up, t);
   } else {
@@ -223,7 +231,6 @@ abcd_status ff_backward(abcd_ctx* ctx, const char* what, const abcd_matrix* dy, 
   if (unpacked && (st = unpack(ctx, list, unpacked)) != ABCD_OK) return st;
   const Operand h = s.operand(m, f, t), dgu = s.operand(m, f, t, 2);
   const Job down{ody, {od}, 1, false, true, m, f, d, 1, {out_of(h, 0, t)}};
-  Hidden hid{};
   hid.act = activation;
   hid.c = h;
   hid.g[0] = dgu;
@@ -231,9 +238,9 @@ abcd_status ff_backward(abcd_ctx* ctx, const char* what, const abcd_matrix* dy, 
   hid.in[1] = oup;
   hid.out[0] = out_of(dgu, 0, t);
   hid.out[1] = out_of(dgu, 1, t);
-  hid.saved[0] = apart ? out_of(ogate, 0, t) : wide[0];
+  hid.saved[0] = apart ? out_of(ogate, 0, t) : wide[0];   // (of direct ones nothing: the codes' maps say it)
   hid.saved[1] = apart ? out_of(oup, 0, t) : wide[1];
-  if ((st = run(ctx, t, kDown, &down, 1, plan(ctx->num_sms, t, kDown, &down, 1), &hid)) != ABCD_OK) return st;
+  if ((st = run(ctx, t, direct ? kDown8 : kDown, &down, 1, down_plan, &hid)) != ABCD_OK) return st;
   // what is left does not depend on one another: one launch, planned as for all of it, so that no
   // gradient depends on which others are asked for
   const Job all[kMaxJobs] = {Job{dgu, {og, ou}, 2, false, true, m, d, f, 1, {}},

@@ -85,6 +85,11 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
   return __float2bfloat16_rn(v);
 }
 
+// The value of an 8-bit code (one of four, 128 added to each): its byte as the low bits of 2^23.
+__device__ __forceinline__ float code_value(unsigned codes, int byte) {
+  return __uint_as_float(__byte_perm(codes, 0x4b000000u, 0x7650 + byte)) - 8388736.f;
+}
+
 // V elements of T as one aligned access.
 template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
 

@@ -138,11 +138,6 @@ __global__ void __launch_bounds__(256, 4) pack8_kernel(const __grid_constant__ P
   }
 }
 
-// A code's value: its byte, 128 added, as the low bits of 2^23.
-__device__ __forceinline__ float value_of(unsigned codes, int byte) {
-  return __uint_as_float(__byte_perm(codes, 0x4b000000u, 0x7650 + byte)) - 8388736.f;
-}
-
 template <typename T>
 __global__ void __launch_bounds__(256, 4) unpack8_kernel(const __grid_constant__ PackedArgs a) {
   pdl_wait();
@@ -167,7 +162,7 @@ __global__ void __launch_bounds__(256, 4) unpack8_kernel(const __grid_constant__
       const float scale = __uint_as_float(power[k] << 23);     // 255: infinite, and NaN times the codes' zeros
       Eight<T> v;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v.at(e) = from_f32<T>(value_of((e < 4 ? w[k].x : w[k].y) ^ 0x80808080u, e & 3) * scale);
+      for (int e = 0; e < 8; ++e) v.at(e) = from_f32<T>(code_value((e < 4 ? w[k].x : w[k].y) ^ 0x80808080u, e & 3) * scale);
       v.store(x + k * at.groups * o.sx, at.left, o.vec);
     }
   }

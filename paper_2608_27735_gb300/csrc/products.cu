@@ -137,6 +137,16 @@ bool make_map(CUtensorMap* map, const Operand& o, int dtype, int box_rows, int b
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The tensor map of a packed matrix's codes, with boxes of 128 rows of a group's 32 bytes, swizzled.
+bool make_code_map(CUtensorMap* map, const abcd_packed8* q) {
+  const EncodeFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)q->cols, (cuuint64_t)q->rows, 1}, strides[2] = {(cuuint64_t)q->stride, (cuuint64_t)(q->rows * q->stride)};
+  const cuuint32_t box[3] = {32, 128, 1}, unit[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, q->codes, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int segments_of(const Job& j, int epi, int dtype) {
   return (epi == kUp ? 1 : j.nb) * (dtype != ABCD_F32 ? 1 : j.b_terms == 1 ? 3 : 6);
 }
@@ -284,11 +294,16 @@ abcd_status run(abcd_ctx* ctx, int dtype, int epi, const Job* jobs, int n, const
       a.g[k] = hidden->out[k];
       a.in[k] = hidden->saved[k];
     }
-    if (shape == 0 && dtype != ABCD_F32 && epi != kLinear) {
-      ok = ok && make_map(&a.c_map, hidden->c, dtype, 128, 32);
+    if (shape == 0 && dtype != ABCD_F32) {
+      if (hidden->c.p) ok = ok && make_map(&a.c_map, hidden->c, dtype, 128, 32);
       for (int k = 0; k < 2; ++k) {
         if (ok && hidden->g[k].p) ok = make_map(&a.g_map[k], hidden->g[k], dtype, 128, 32);
         if (ok && hidden->in[k].p) ok = make_map(&a.in_map[k], hidden->in[k], dtype, 128, 32);
+        if (ok && epi == kDown8) {
+          ok = make_code_map(&a.in_map[k], hidden->packed[k]);
+          a.power[k] = hidden->packed[k]->powers;
+          a.power_stride[k] = hidden->packed[k]->power_stride;
+        }
       }
     }
   }

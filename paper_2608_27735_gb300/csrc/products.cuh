@@ -95,6 +95,7 @@ struct Hidden {
   Out out[2], saved[2];            // the same as g and in; kLinear: z and the residual
   const void* bias;
   int wide_bias;
+  const abcd_packed8* packed[2];   // kDown8: gate and up
 };
 
 // The shape and the splits of a call's products.

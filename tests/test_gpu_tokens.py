@@ -221,7 +221,7 @@ def test_index_past_the_table_is_reported(ctx):
 # ---- linear layer
 
 LINEAR_SHAPES = [(1, 1, 1), (1, 64, 48), (7, 59, 33), (8, 1024, 96), (9, 64, 64), (130, 250, 257), (500, 64, 1000), (1000, 700, 16),
-                 (3000, 256, 256), (40, 2000, 300), (300, 8, 700)]
+                 (3000, 256, 256), (40, 2000, 300), (300, 8, 700), (5000, 300, 1100)]
 
 
 @pytest.mark.parametrize("kind", KINDS)
@@ -261,6 +261,29 @@ def test_linear(ctx, kind, rows, cols, out, name, pad, lead):
         one = torch.full_like(want, float("nan"))
         ab.abcd_linear_backward(ctx, dy, x, w, name, z, *[one if i == k else None for i in range(3)])
         assert torch.equal(one, want)
+
+
+@pytest.mark.parametrize("rows,cols,out", [(50, 64, 96), (5000, 256, 1024)])
+def test_linear_with_matrices_of_different_starts(ctx, rows, cols, out):
+    """Each of residual, y and z on 16-byte boundaries or not."""
+    r = np.random.default_rng(8)
+    x, w = matrix(r.normal(size=(rows, cols)), "bf16"), matrix(r.normal(size=(out, cols)) / cols ** 0.5, "bf16")
+    values = r.normal(size=(rows, out))
+    ctx.reserve_linear(rows, cols, out, torch.bfloat16)
+    want = None
+    for pads in np.ndindex(2, 2, 2):
+        res, y, z = matrix(values, "bf16", 3 * pads[0]), blank(rows, out, "bf16", 3 * pads[1]), blank(rows, out, "bf16", 3 * pads[2])
+        ab.abcd_linear(ctx, x, w, None, "gelu", y, res, z)
+        ctx.sync()
+        if want is None:
+            want = y.clone(), z.clone()
+            args = f64(x), f64(w), np.zeros(out), "gelu", f64(res)
+            for got, exact, bound in zip(want, K.linear(*args), K.linear_bounds(*args, "bf16")):
+                close(got, exact, bound)
+        assert torch.equal(y, want[0]) and torch.equal(z, want[1])
+        assert gaps_untouched(y) and gaps_untouched(z)
+        ab.abcd_linear(ctx, x, w, None, "gelu", res, res)
+        assert torch.equal(res, want[0]) and gaps_untouched(res)
 
 
 @pytest.mark.parametrize("kind", KINDS)
