@@ -7,6 +7,7 @@
 // fraction) a group's error is a quarter; a scale that is not a power of two would win half a bit more,
 // and make codes depend on how the division rounds.
 #include <algorithm>
+#include <type_traits>
 
 #include "packed8.cuh"
 
@@ -112,12 +113,15 @@ __global__ void __launch_bounds__(256, 4) pack8_kernel(const __grid_constant__ P
   const T* x = (const T*)o.x + at.row * o.sx + at.col;
   signed char* to = o.codes + at.row * o.sc + at.col;
   unsigned char* power_to = o.powers + at.row * o.sp + at.col / 32;
-  // (a warp's lanes take their turns together: the four lanes of a group share its largest magnitude)
-  for (long long r = at.row; r - (threadIdx.x / o.lanes) < o.rows; r += at.step, x += at.step * o.sx, to += at.step * o.sc, power_to += at.step * o.sp) {
+  const long long next_x = at.groups * o.sx, next_to = at.groups * o.sc, next_power = at.groups * o.sp;
+  // a turn's units; `full`: all of them are there.  (A warp's lanes take their turns together: the four lanes
+  // of a group share its largest magnitude.)
+  auto turn = [&](long long r, auto full) {
+    constexpr bool FULL = decltype(full)::value;
     Eight<T> v[kFlight];
 #pragma unroll
     for (int k = 0; k < kFlight; ++k)      // without a condition: all are on their way before the first is used
-      v[k].load(x + (min(r + k * at.groups, o.rows - 1) - r) * o.sx, at.left, o.vec);
+      v[k].load(FULL ? x + k * next_x : x + (min(r + k * at.groups, o.rows - 1) - r) * o.sx, at.left, o.vec);
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
       unsigned top = v[k].top();
@@ -126,15 +130,20 @@ __global__ void __launch_bounds__(256, 4) pack8_kernel(const __grid_constant__ P
       const bool finite = top < 0x7f800000u;
       const int power = finite ? max((int)(top >> 23) - 6, 1) : 255;
       const uint2 w = finite ? codes_of(v[k], power, top) : make_uint2(0u, 0u);
-      if (r + k * at.groups >= o.rows) continue;
-      signed char* row = to + k * at.groups * o.sc;
+      if (!FULL && r + k * at.groups >= o.rows) continue;
+      signed char* row = to + k * next_to;
       if (at.left == 8) {
         *reinterpret_cast<uint2*>(row) = w;
       } else {
         for (int e = 0; e < at.left; ++e) row[e] = (signed char)((e < 4 ? w.x : w.y) >> 8 * (e & 3));
       }
-      if ((threadIdx.x & 3) == 0 && at.left > 0) power_to[k * at.groups * o.sp] = (unsigned char)power;
+      if ((threadIdx.x & 3) == 0 && at.left > 0) power_to[k * next_power] = (unsigned char)power;
     }
+  };
+  const long long base = blockIdx.y * (long long)(at.groups * kFlight);
+  for (long long r = at.row, b = base; b < o.rows; r += at.step, b += at.step, x += at.step * o.sx, to += at.step * o.sc, power_to += at.step * o.sp) {
+    if (b + at.groups * kFlight <= o.rows) turn(r, std::true_type());
+    else turn(r, std::false_type());
   }
 }
 
@@ -147,24 +156,31 @@ __global__ void __launch_bounds__(256, 4) unpack8_kernel(const __grid_constant__
   T* x = (T*)o.x + at.row * o.sx + at.col;
   const signed char* from = o.codes + at.row * o.sc + at.col;
   const unsigned char* power_from = o.powers + at.row * o.sp + at.col / 32;
-  for (long long r = at.row; r < o.rows; r += at.step, x += at.step * o.sx, from += at.step * o.sc, power_from += at.step * o.sp) {
+  const long long next_x = at.groups * o.sx, next_from = at.groups * o.sc, next_power = at.groups * o.sp;
+  auto turn = [&](long long r, auto full) {
+    constexpr bool FULL = decltype(full)::value;
     uint2 w[kFlight];
     unsigned power[kFlight];
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
-      const long long row = min(r + k * at.groups, o.rows - 1) - r;
-      w[k] = *reinterpret_cast<const uint2*>(from + row * o.sc);              // a row of codes has room for whole units
-      power[k] = power_from[row * o.sp];
+      const long long back = FULL ? 0 : r + k * at.groups - min(r + k * at.groups, o.rows - 1);
+      w[k] = *reinterpret_cast<const uint2*>(from + k * next_from - back * o.sc);      // a row of codes has room for whole units
+      power[k] = power_from[k * next_power - back * o.sp];
     }
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
-      if (r + k * at.groups >= o.rows) break;
+      if (!FULL && r + k * at.groups >= o.rows) break;
       const float scale = __uint_as_float(power[k] << 23);     // 255: infinite, and NaN times the codes' zeros
       Eight<T> v;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v.at(e) = from_f32<T>(code_value((e < 4 ? w[k].x : w[k].y) ^ 0x80808080u, e & 3) * scale);
-      v.store(x + k * at.groups * o.sx, at.left, o.vec);
+      v.store(x + k * next_x, at.left, o.vec);
     }
+  };
+  const int per_turn = at.groups * kFlight;
+  for (long long r = at.row; r < o.rows; r += at.step, x += at.step * o.sx, from += at.step * o.sc, power_from += at.step * o.sp) {
+    if (r + per_turn <= o.rows) turn(r, std::true_type());
+    else turn(r, std::false_type());
   }
 }
 

@@ -215,48 +215,47 @@ template <typename T, int TPR_, int E_, bool BWD, bool VEC_> struct CloseRow {
   static constexpr int V = VEC ? 16 / (int)sizeof(T) : 1, NV = E / V;
   static constexpr int kThreads = TPR > 256 ? TPR : 256, kGroups = kThreads / TPR;
   static constexpr int kMats = BWD ? 4 : 2;
-  static constexpr int kDepth = BWD ? 3 : 4;               // rows that are there or on their way
   static constexpr int kRowBytes = TPR * E * (int)sizeof(T) + (VEC ? 0 : 32);
   static constexpr int kMatBytes = kGroups * kRowBytes, kSlotBytes = kMats * kMatBytes;
-  static constexpr size_t kRing = (size_t)kDepth * kSlotBytes;
-  static constexpr size_t kSums = BWD ? (size_t)4 * TPR * E * 4 : 0;
-  static constexpr size_t kSmem = kRing > kSums ? kRing : kSums;
-  static constexpr int kCtas = kThreads > 256 ? 1 : BWD || E > 8 ? 2 : 3;
+  // The factors of the columns (A, C, w_before and, forward, b_before), for all groups, behind the rows: in
+  // registers they would cost a third of the warps.
+  static constexpr int kFactors = BWD ? 3 : 4;
+  static constexpr size_t kFactorBytes = (size_t)kFactors * TPR * E * 4;
+  // rows that are there or on their way
+  static constexpr int kDepth = BWD ? (3 * (size_t)kSlotBytes + kFactorBytes > 224 * 1024 ? 2 : 3) : 4;
+  static constexpr size_t kRing = (size_t)kDepth * kSlotBytes, kSums = BWD ? (size_t)4 * TPR * E * 4 : 0;
+  static constexpr size_t kRows = kRing > kSums ? kRing : kSums;
+  static constexpr size_t kSmem = kRows + kFactorBytes;
+  // CTAs per SM, as many as registers and rows leave room for
+  static constexpr int kFit = (int)(227 * 1024 / (kSmem + 2048));
+  static_assert(kFit >= 1);
+  static constexpr int kMost = BWD ? 2 : 3;
+  static constexpr int kCtas = kThreads > 256 ? (kFit < 2 || BWD ? 1 : 2) : kFit < kMost ? kFit : kMost;
 };
 
 template <typename T, typename R> struct CloseRows {
+  const CloseArgs& a;
   char* slots;                        // the thread's first vector (VEC) or its row's first piece, of the first slot
-  const T* src[R::kMats];             // where the next row to fetch starts (VEC: the thread's first vector of it)
-  const char* lowest[R::kMats];       // else also: the matrices' first bytes, and the ones behind their last
-  const char* highest[R::kMats];
-  long long jump[R::kMats];
+  float4* factor;                     // the thread's first four factors of A
   int bytes[R::NV];                   // VEC: of the thread's vectors
   int rows, turns, lane, cols;        // rows of the group; turns that its threads take together
   int now;                            // the slot of the row at hand
   bool partial;                       // the thread has columns past the row's end
+  unsigned row, step;                 // the row at hand, from a turn to the next
 
-  __device__ __forceinline__ CloseRows(char* smem, const CloseArgs& a) {
+  __device__ __forceinline__ CloseRows(char* smem, const CloseArgs& args) : a(args) {
     const int group = threadIdx.x / R::TPR;
-    const long long first = (long long)blockIdx.x * R::kGroups + group, step = (long long)gridDim.x * R::kGroups;
+    row = blockIdx.x * R::kGroups + group;
+    step = gridDim.x * R::kGroups;
     lane = threadIdx.x % R::TPR;
     cols = a.cols;
-    rows = first < a.rows ? (int)((a.rows - first + step - 1) / step) : 0;
+    rows = row < a.rows ? (int)((a.rows - row + step - 1) / step) : 0;
     // groups of whole warps go on by themselves; rows that share a warp take their turns together
     turns = R::TPR >= 32 ? rows : (int)((a.rows - (long long)blockIdx.x * R::kGroups + step - 1) / step);
     slots = smem + (R::VEC ? threadIdx.x * 16 : group * R::kRowBytes);
+    factor = reinterpret_cast<float4*>(smem + R::kRows) + lane;
     now = 0;
     partial = column(R::NV - 1) + R::V > cols;
-    const T* const base[4] = {(const T*)a.f, (const T*)a.x, (const T*)a.dy, (const T*)a.dn};
-    const long long stride[4] = {a.sf, a.sx, a.sdy, a.sdn};
-#pragma unroll
-    for (int q = 0; q < R::kMats; ++q) {
-      src[q] = base[q] ? base[q] + first * stride[q] + (R::VEC ? lane * R::V : 0) : nullptr;
-      jump[q] = step * stride[q];
-      if (!R::VEC && base[q]) {
-        lowest[q] = (const char*)base[q];
-        highest[q] = (const char*)(base[q] + (a.rows - 1) * stride[q] + a.cols);
-      }
-    }
 #pragma unroll
     for (int j = 0; j < R::NV; ++j) bytes[j] = R::VEC ? min(16, (cols - column(j)) * (int)sizeof(T)) : 0;
     // what is never copied reads as zero
@@ -265,30 +264,37 @@ template <typename T, typename R> struct CloseRows {
       for (int q = 0; q < R::kMats; ++q)
 #pragma unroll
         for (int j = 0; j < R::NV; ++j)
-          if (!src[q] || bytes[j] <= 0)
+          if (!base(q) || bytes[j] <= 0)
             for (int d = 0; d < R::kDepth; ++d) *reinterpret_cast<uint4*>(vector(d, q, j)) = make_uint4(0u, 0u, 0u, 0u);
     }
   }
+  __device__ __forceinline__ const T* base(int q) const { return (const T*)(q == 0 ? a.f : q == 1 ? a.x : q == 2 ? a.dy : a.dn); }
+  __device__ __forceinline__ unsigned stride(int q) const { return (unsigned)(q == 0 ? a.sf : q == 1 ? a.sx : q == 2 ? a.sdy : a.sdn); }
+  // Where row r of a matrix starts (rows and strides have 32 bits, their product does not).
+  __device__ __forceinline__ const T* start_of(int q, unsigned r) const { return base(q) + (unsigned long long)r * stride(q); }
   __device__ __forceinline__ int column(int j) const { return (j * R::TPR + lane) * R::V; }
   __device__ __forceinline__ char* vector(int slot, int mat, int j) const {
     return slots + slot * R::kSlotBytes + mat * R::kMatBytes + j * R::kThreads * 16;
   }
   __device__ __forceinline__ char* pieces(int slot, int mat) const { return slots + slot * R::kSlotBytes + mat * R::kMatBytes; }
-  __device__ __forceinline__ void fetch(int t, int slot) {
+  __device__ __forceinline__ void fetch(int t, int slot, unsigned r) {
     if (t < rows) {
 #pragma unroll
       for (int q = 0; q < R::kMats; ++q) {
-        if (!src[q]) continue;
+        if (!base(q)) continue;
+        const T* src = start_of(q, r);
         if constexpr (R::VEC) {
 #pragma unroll
           for (int j = 0; j < R::NV; ++j)
-            if (bytes[j] > 0) copy16(vector(slot, q, j), src[q] + j * R::TPR * R::V, bytes[j]);
+            if (bytes[j] > 0) copy16(vector(slot, q, j), src + column(j), bytes[j]);
         } else {
-          const char* begin = (const char*)src[q];
+          const char* begin = (const char*)src;
           const char* end = begin + cols * (int)sizeof(T);
+          const char* lowest = (const char*)base(q);
+          const char* highest = (const char*)(start_of(q, (unsigned)a.rows - 1) + cols);
           const char* from = begin - ((uintptr_t)begin & 15) + 16 * lane;
           for (char* to = pieces(slot, q) + 16 * lane; from < end; from += 16 * R::TPR, to += 16 * R::TPR) {
-            if (from >= lowest[q] && from + 16 <= highest[q]) {
+            if (from >= lowest && from + 16 <= highest) {
               copy16(to, from, 16);
             } else {                  // a piece that reaches out of the matrix
 #pragma unroll 1
@@ -297,26 +303,28 @@ template <typename T, typename R> struct CloseRows {
             }
           }
         }
-        src[q] += jump[q];
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
   __device__ __forceinline__ void start() {
 #pragma unroll
-    for (int d = 0; d < R::kDepth - 1; ++d) fetch(d, d);
+    for (int d = 0; d < R::kDepth - 1; ++d) fetch(d, d, row + d * step);
   }
   // Asks for a row to come and waits for turn t's.
   __device__ __forceinline__ void turn(int t) {
     if constexpr (!R::VEC) row_sync<R::TPR>();             // the last turn's row is done with
-    fetch(t + R::kDepth - 1, now == 0 ? R::kDepth - 1 : now - 1);
+    fetch(t + R::kDepth - 1, now == 0 ? R::kDepth - 1 : now - 1, row + (R::kDepth - 1) * step);
     asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
     if constexpr (!R::VEC) row_sync<R::TPR>();
   }
-  __device__ __forceinline__ void next() { now = now == R::kDepth - 1 ? 0 : now + 1; }
-  // The thread's values of the row at hand of a matrix (`at`: where the row starts): zeros past its end, of no
-  // row and of a matrix that is not there.
-  __device__ __forceinline__ void get(float2 (&pairs)[R::E / 2], int t, int mat, const T* at) const {
+  __device__ __forceinline__ void next() {
+    now = now == R::kDepth - 1 ? 0 : now + 1;
+    row += step;
+  }
+  // The thread's values of the row at hand of a matrix: zeros past its end, of no row and of a matrix that is
+  // not there.
+  __device__ __forceinline__ void get(float2 (&pairs)[R::E / 2], int t, int mat) const {
     float v[R::E];
     if constexpr (R::VEC) {
 #pragma unroll
@@ -326,15 +334,18 @@ template <typename T, typename R> struct CloseRows {
         for (int i = 0; i < R::V; ++i) v[j * R::V + i] = R::TPR >= 32 || t < rows ? to_f32(w.v[i]) : 0.f;
       }
     } else {
-      const T* p = (const T*)(pieces(now, mat) + ((uintptr_t)at & 15)) + lane;
+      const bool there = base(mat) != nullptr;
+      const T* p = (const T*)(pieces(now, mat) + ((uintptr_t)start_of(mat, row) & 15)) + lane;
 #pragma unroll
-      for (int e = 0; e < R::E; ++e) v[e] = at && column(e) < cols ? to_f32(p[e * R::TPR]) : 0.f;
+      for (int e = 0; e < R::E; ++e) v[e] = there && column(e) < cols ? to_f32(p[e * R::TPR]) : 0.f;
     }
 #pragma unroll
     for (int e = 0; e < R::E / 2; ++e) pairs[e] = make_float2(v[2 * e], v[2 * e + 1]);
   }
-  __device__ __forceinline__ void put(T* to, const float2 (&v)[R::E / 2], int t) const {
+  // The row at hand of a result.
+  __device__ __forceinline__ void put(void* matrix, long long stride, const float2 (&v)[R::E / 2], int t) const {
     if (R::TPR < 32 && t >= rows) return;
+    T* to = (T*)matrix + (unsigned long long)row * (unsigned)stride;
 #pragma unroll
     for (int j = 0; j < R::NV; ++j) {
       float w[R::V];
@@ -413,20 +424,28 @@ __device__ __forceinline__ Stat stat_of_row(const CloseRows<T, R>& rows, const f
   return Stat{mean + off, rstd_of(q * inv, off, eps)};
 }
 
-// A and C of the thread's columns.
-template <typename T, typename R>
-__device__ __forceinline__ void factors(const CloseRows<T, R>& rows, const CloseArgs& a, float2 (&A)[R::E / 2], float2 (&C)[R::E / 2]) {
-  float2 g[R::E / 2];
-  rows.weights(g, a.gate, a.wide_w, 1.f);
-  rows.weights(A, a.w[0], a.wide_w, 1.f);
-  rows.weights(C, a.b[0], a.wide_w, 0.f);
+// The factors of the columns to shared memory, by the CTA's first group: [factor][four values][thread of a row].
+template <typename T, typename R> __device__ __forceinline__ void set_factors(const CloseRows<T, R>& rows, const CloseArgs& a) {
+  if (threadIdx.x < R::TPR) {
+    float2 g[R::E / 2], k[R::E / 2];
+    rows.weights(g, a.gate, a.wide_w, 1.f);
 #pragma unroll
-  for (int e = 0; e < R::E / 2; ++e) {
-    const float2 sg = mul2(g[e], both(a.scale));
-    A[e] = mul2(A[e], sg);
-    C[e] = mul2(C[e], sg);
+    for (int q = 0; q < R::kFactors; ++q) {
+      rows.weights(k, q == 0 ? a.w[0] : q == 1 ? a.b[0] : q == 2 ? a.w[1] : a.b[1], a.wide_w, q == 0 || q == 2 ? 1.f : 0.f);
+#pragma unroll
+      for (int e = 0; e < R::E / 2; ++e)
+        if (q < 2) k[e] = mul2(k[e], mul2(g[e], both(a.scale)));
+#pragma unroll
+      for (int e = 0; e < R::E / 4; ++e) rows.factor[(q * (R::E / 4) + e) * R::TPR] = make_float4(k[2 * e].x, k[2 * e].y, k[2 * e + 1].x, k[2 * e + 1].y);
+    }
   }
+  __syncthreads();
 }
+// Four of the thread's factors: pairs 2 e and 2 e + 1.
+template <typename T, typename R> __device__ __forceinline__ float4 factor_of(const CloseRows<T, R>& rows, int which, int e) {
+  return rows.factor[(which * (R::E / 4) + e) * R::TPR];
+}
+__device__ __forceinline__ float2 half_of(const float4& v, int h) { return h ? make_float2(v.z, v.w) : make_float2(v.x, v.y); }
 
 template <typename T, typename R>
 __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_fwd_kernel(const __grid_constant__ CloseArgs a) {
@@ -436,41 +455,39 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_fwd_kernel(const 
   pdl_wait();
   CloseRows<T, R> rows(smem, a);
   rows.start();
-  float2 A[P], C[P], W[P], B[P];
-  factors(rows, a, A, C);
-  rows.weights(W, a.w[1], a.wide_w, 1.f);
-  rows.weights(B, a.b[1], a.wide_w, 0.f);
+  set_factors(rows, a);
   const float inv = 1.f / (float)a.cols;
-  const long long step = (long long)gridDim.x * R::kGroups;
-  long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / R::TPR;
-  T* y = (T*)a.y + r * a.sy;
-  T* n = (T*)a.n + r * a.sn;
-  const T* atf = (const T*)a.f + r * a.sf;               // (used where rows start anywhere)
-  const T* atx = (const T*)a.x + r * a.sx;
   int half = 0;
-  for (int t = 0; t < rows.turns; ++t, r += step, y += step * a.sy, n += step * a.sn, atf += step * a.sf, atx += step * a.sx) {
+  for (int t = 0; t < rows.turns; ++t, rows.next()) {
     rows.turn(t);
     float2 f[P], x[P];
-    rows.get(f, t, 0, atf);
-    rows.get(x, t, 1, atx);
+    rows.get(f, t, 0);
+    rows.get(x, t, 1);
     Stat first{0.f, 1.f}, second{0.f, 1.f};
     if (a.kind[0] != kNone) first = stat_of_row(rows, f, a.kind[0], a.eps[0], inv, red, half);
 #pragma unroll
-    for (int e = 0; e < P; ++e) x[e] = close_pair(x[e], mul2(sub2(f[e], first.mean), both(first.rstd)), A[e], C[e]);
+    for (int e = 0; e < P; e += 2) {
+      const float4 A = factor_of(rows, 0, e / 2), C = factor_of(rows, 1, e / 2);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) x[e + h] = close_pair(x[e + h], mul2(sub2(f[e + h], first.mean), both(first.rstd)), half_of(A, h), half_of(C, h));
+    }
     if (a.kind[1] != kNone) {
       second = stat_of_row(rows, x, a.kind[1], a.eps[1], inv, red, half);
 #pragma unroll
-      for (int e = 0; e < P; ++e) f[e] = fma2(mul2(sub2(x[e], second.mean), both(second.rstd)), W[e], B[e]);
-      rows.put(n, f, t);
+      for (int e = 0; e < P; e += 2) {
+        const float4 W = factor_of(rows, 2, e / 2), B = factor_of(rows, 3, e / 2);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) f[e + h] = fma2(mul2(sub2(x[e + h], second.mean), both(second.rstd)), half_of(W, h), half_of(B, h));
+      }
+      rows.put(a.n, a.sn, f, t);
     }
-    rows.put(y, x, t);
-    rows.next();
+    rows.put(a.y, a.sy, x, t);
     if ((R::TPR >= 32 || t < rows.rows) && rows.lane == 0) {
       const Stat s[2] = {first, second};
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        if (a.mean[k]) a.mean[k][r] = s[k].mean;
-        if (a.rstd[k]) a.rstd[k][r] = s[k].rstd;
+        if (a.mean[k]) a.mean[k][rows.row] = s[k].mean;
+        if (a.rstd[k]) a.rstd[k][rows.row] = s[k].rstd;
       }
     }
   }
@@ -484,50 +501,49 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
   pdl_wait();
   CloseRows<T, R> rows(smem, a);
   rows.start();
-  float2 A[P], C[P], W[P], sums[4][P];
-  factors(rows, a, A, C);
-  rows.weights(W, a.w[1], a.wide_w, 1.f);
+  set_factors(rows, a);
+  float2 sums[4][P];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
     for (int e = 0; e < P; ++e) sums[k][e] = both(0.f);
   const float inv = 1.f / (float)a.cols;
   const float centre[2] = {a.kind[0] == ABCD_LAYER_NORM ? inv : 0.f, a.kind[1] == ABCD_LAYER_NORM ? inv : 0.f};
-  const long long step = (long long)gridDim.x * R::kGroups;
-  long long r = (long long)blockIdx.x * R::kGroups + threadIdx.x / R::TPR;
-  T* dx = (T*)a.y + r * a.sy;
-  T* df = (T*)a.n + r * a.sn;
-  // (used where rows start anywhere)
-  const T* at[4] = {(const T*)a.f + r * a.sf, (const T*)a.x + r * a.sx, a.dy ? (const T*)a.dy + r * a.sdy : nullptr, a.dn ? (const T*)a.dn + r * a.sdn : nullptr};
   Stat next[2] = {{0.f, 0.f}, {0.f, 0.f}};
   if (rows.rows > 0) {
-    next[0] = stat_of(a, 0, r);
-    next[1] = stat_of(a, 1, r);
+    next[0] = stat_of(a, 0, rows.row);
+    next[1] = stat_of(a, 1, rows.row);
   }
-  for (int t = 0; t < rows.turns; ++t, r += step, dx += step * a.sy, df += step * a.sn) {
+  for (int t = 0; t < rows.turns; ++t, rows.next()) {
     rows.turn(t);
     const Stat first = next[0], second = next[1];
     if (t + 1 < rows.rows) {
-      next[0] = stat_of(a, 0, r + step);
-      next[1] = stat_of(a, 1, r + step);
+      next[0] = stat_of(a, 0, rows.row + rows.step);
+      next[1] = stat_of(a, 1, rows.row + rows.step);
     }
-    float2 fh[P], yh[P], g[P], p1 = both(0.f), p2 = both(0.f);
-    rows.get(fh, t, 0, at[0]);
-    rows.get(yh, t, 1, at[1]);
-    rows.get(g, t, 2, at[2]);
+    float2 fh[P], g[P], p1 = both(0.f), p2 = both(0.f);
+    rows.get(fh, t, 0);
+    rows.get(g, t, 2);
 #pragma unroll
     for (int e = 0; e < P; ++e) fh[e] = mul2(sub2(fh[e], first.mean), both(first.rstd));
     if (a.dn) {
-      float2 dn[P];
-      rows.get(dn, t, 3, at[3]);
+      float2 yh[P], dn[P];
+      rows.get(yh, t, 1);
+      rows.get(dn, t, 3);
 #pragma unroll
-      for (int e = 0; e < P; ++e) {
-        yh[e] = mul2(sub2(close_pair(yh[e], fh[e], A[e], C[e]), second.mean), both(second.rstd));   // the forward pass's, bit for bit
-        sums[2][e] = add2(sums[2][e], dn[e]);
-        sums[3][e] = fma2(dn[e], yh[e], sums[3][e]);
-        dn[e] = mul2(dn[e], W[e]);
-        p1 = add2(p1, dn[e]);
-        p2 = fma2(dn[e], yh[e], p2);
+      for (int e = 0; e < P; e += 2) {
+        const float4 A = factor_of(rows, 0, e / 2), C = factor_of(rows, 1, e / 2), W = factor_of(rows, 2, e / 2);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int i = e + h;
+          // the forward pass's, bit for bit
+          yh[i] = mul2(sub2(close_pair(yh[i], fh[i], half_of(A, h), half_of(C, h)), second.mean), both(second.rstd));
+          sums[2][i] = add2(sums[2][i], dn[i]);
+          sums[3][i] = fma2(dn[i], yh[i], sums[3][i]);
+          dn[i] = mul2(dn[i], half_of(W, h));
+          p1 = add2(p1, dn[i]);
+          p2 = fma2(dn[i], yh[i], p2);
+        }
       }
       float s1 = p1.x + p1.y, s2 = p2.x + p2.y;
       row_sum2<R::TPR>(s1, s2, red, 0);
@@ -536,16 +552,21 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
 #pragma unroll
       for (int e = 0; e < P; ++e) g[e] = fma2(fma2(yh[e], both(-s2), sub2(dn[e], s1)), both(second.rstd), g[e]);
     }
-    if (a.y) rows.put(dx, g, t);
+    if (a.y) rows.put(a.y, a.sy, g, t);
     p1 = p2 = both(0.f);
 #pragma unroll
-    for (int e = 0; e < P; ++e) {
-      if (R::TPR < 32 && t >= rows.rows) g[e] = both(0.f);
-      sums[0][e] = add2(sums[0][e], g[e]);
-      sums[1][e] = fma2(g[e], fh[e], sums[1][e]);
-      g[e] = mul2(g[e], A[e]);
-      p1 = add2(p1, g[e]);
-      p2 = fma2(g[e], fh[e], p2);
+    for (int e = 0; e < P; e += 2) {
+      const float4 A = factor_of(rows, 0, e / 2);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int i = e + h;
+        if (R::TPR < 32 && t >= rows.rows) g[i] = both(0.f);
+        sums[0][i] = add2(sums[0][i], g[i]);
+        sums[1][i] = fma2(g[i], fh[i], sums[1][i]);
+        g[i] = mul2(g[i], half_of(A, h));
+        p1 = add2(p1, g[i]);
+        p2 = fma2(g[i], fh[i], p2);
+      }
     }
     if (a.n) {
       if (a.kind[0] != kNone) {
@@ -556,18 +577,11 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
 #pragma unroll
         for (int e = 0; e < P; ++e) g[e] = mul2(fma2(fh[e], both(-s2), sub2(g[e], s1)), both(first.rstd));
       }
-      rows.put(df, g, t);
+      rows.put(a.n, a.sn, g, t);
     }
     // a row's use of `red` ends before the next but one begins; where only one sum is taken, the row's
     // threads meet here
     if (R::TPR > 32 && (!a.dn || !a.n || a.kind[0] == kNone)) row_sync<R::TPR>();
-    rows.next();
-    if constexpr (!R::VEC) {
-      at[0] += step * a.sf;
-      at[1] += step * a.sx;
-      if (at[2]) at[2] += step * a.sdy;
-      if (at[3]) at[3] += step * a.sdn;
-    }
   }
   // the CTA's sums: rows that share a warp by shuffles, then the warps of a column one after another
   asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -644,7 +658,7 @@ __global__ void __launch_bounds__(1024) close_sum_kernel(const __grid_constant__
   if (which == 0) put(0, a.scale * (weight_at<T>(a.w, a.wide_w, c, 1.f) * s2 + weight_at<T>(a.b, a.wide_w, c, 0.f) * s1));
 }
 
-constexpr int kCloseCtasPerSm = 2;    // backward, with sums in the workspace
+constexpr int kCloseCtasPerSm = 2;    // backward at most, with sums in the workspace
 
 // Calls f with the row shape for `cols` columns of T; f of an int where registers do not hold a row.
 template <typename T, bool BWD, typename F> abcd_status with_row(long long cols, bool aligned, F&& f) {
@@ -656,7 +670,7 @@ template <typename T, bool BWD, typename F> abcd_status with_row(long long cols,
     if (cols <= 512) return f(CloseRow<T, 64 / N, E, BWD, true>());
     if (cols <= 1024) return f(CloseRow<T, 128 / N, E, BWD, true>());
     if (cols <= 2048) return f(CloseRow<T, 256 / N, E, BWD, true>());
-    if (cols <= 4096) return f(CloseRow<T, 512 / N, E, BWD, true>());
+    if (cols <= 4096) return f(CloseRow<T, 512, 8, BWD, true>());   // (rows of 256 threads leave room for one CTA of half the warps)
   } else {
     if (cols <= 256) return f(CloseRow<T, 32, 8, BWD, false>());
     if (cols <= 1024) return f(CloseRow<T, 128, 8, BWD, false>());
