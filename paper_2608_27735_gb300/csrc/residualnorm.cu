@@ -218,9 +218,11 @@ template <typename T, int TPR_, int E_, bool BWD, bool VEC_> struct CloseRow {
   static constexpr int kRowBytes = TPR * E * (int)sizeof(T) + (VEC ? 0 : 32);
   static constexpr int kMatBytes = kGroups * kRowBytes, kSlotBytes = kMats * kMatBytes;
   // The factors of the columns (A, C, w_before and, forward, b_before), for all groups, behind the rows: in
-  // registers they would cost a third of the warps.
+  // registers they would cost a third of the warps.  Wide rows forward hold them in registers all the same:
+  // there they would take the second CTA's shared memory (25,000 x 4,096 bf16: 266 us, and 163 so).
   static constexpr int kFactors = BWD ? 3 : 4;
-  static constexpr size_t kFactorBytes = (size_t)kFactors * TPR * E * 4;
+  static constexpr bool kHold = !BWD && TPR * E > 2048;
+  static constexpr size_t kFactorBytes = kHold ? 0 : (size_t)kFactors * TPR * E * 4;
   // rows that are there or on their way
   static constexpr int kDepth = BWD ? (3 * (size_t)kSlotBytes + kFactorBytes > 224 * 1024 ? 2 : 3) : 4;
   static constexpr size_t kRing = (size_t)kDepth * kSlotBytes, kSums = BWD ? (size_t)4 * TPR * E * 4 : 0;
@@ -229,7 +231,7 @@ template <typename T, int TPR_, int E_, bool BWD, bool VEC_> struct CloseRow {
   // CTAs per SM, as many as registers and rows leave room for
   static constexpr int kFit = (int)(227 * 1024 / (kSmem + 2048));
   static_assert(kFit >= 1);
-  static constexpr int kMost = BWD ? 2 : 3;
+  static constexpr int kMost = BWD || kHold ? 2 : 3;
   static constexpr int kCtas = kThreads > 256 ? (kFit < 2 || BWD ? 1 : 2) : kFit < kMost ? kFit : kMost;
 };
 
@@ -237,6 +239,7 @@ template <typename T, typename R> struct CloseRows {
   const CloseArgs& a;
   char* slots;                        // the thread's first vector (VEC) or its row's first piece, of the first slot
   float4* factor;                     // the thread's first four factors of A
+  float4 held[R::kHold ? R::kFactors * R::E / 4 : 1];
   int bytes[R::NV];                   // VEC: of the thread's vectors
   int rows, turns, lane, cols;        // rows of the group; turns that its threads take together
   int now;                            // the slot of the row at hand
@@ -425,8 +428,8 @@ __device__ __forceinline__ Stat stat_of_row(const CloseRows<T, R>& rows, const f
 }
 
 // The factors of the columns to shared memory, by the CTA's first group: [factor][four values][thread of a row].
-template <typename T, typename R> __device__ __forceinline__ void set_factors(const CloseRows<T, R>& rows, const CloseArgs& a) {
-  if (threadIdx.x < R::TPR) {
+template <typename T, typename R> __device__ __forceinline__ void set_factors(CloseRows<T, R>& rows, const CloseArgs& a) {
+  if (R::kHold || threadIdx.x < R::TPR) {
     float2 g[R::E / 2], k[R::E / 2];
     rows.weights(g, a.gate, a.wide_w, 1.f);
 #pragma unroll
@@ -436,14 +439,19 @@ template <typename T, typename R> __device__ __forceinline__ void set_factors(co
       for (int e = 0; e < R::E / 2; ++e)
         if (q < 2) k[e] = mul2(k[e], mul2(g[e], both(a.scale)));
 #pragma unroll
-      for (int e = 0; e < R::E / 4; ++e) rows.factor[(q * (R::E / 4) + e) * R::TPR] = make_float4(k[2 * e].x, k[2 * e].y, k[2 * e + 1].x, k[2 * e + 1].y);
+      for (int e = 0; e < R::E / 4; ++e) {
+        const float4 v = make_float4(k[2 * e].x, k[2 * e].y, k[2 * e + 1].x, k[2 * e + 1].y);
+        if constexpr (R::kHold) rows.held[q * (R::E / 4) + e] = v;
+        else rows.factor[(q * (R::E / 4) + e) * R::TPR] = v;
+      }
     }
   }
   __syncthreads();
 }
 // Four of the thread's factors: pairs 2 e and 2 e + 1.
 template <typename T, typename R> __device__ __forceinline__ float4 factor_of(const CloseRows<T, R>& rows, int which, int e) {
-  return rows.factor[(which * (R::E / 4) + e) * R::TPR];
+  if constexpr (R::kHold) return rows.held[which * (R::E / 4) + e];
+  else return rows.factor[(which * (R::E / 4) + e) * R::TPR];
 }
 __device__ __forceinline__ float2 half_of(const float4& v, int h) { return h ? make_float2(v.z, v.w) : make_float2(v.x, v.y); }
 
@@ -670,7 +678,7 @@ template <typename T, bool BWD, typename F> abcd_status with_row(long long cols,
     if (cols <= 512) return f(CloseRow<T, 64 / N, E, BWD, true>());
     if (cols <= 1024) return f(CloseRow<T, 128 / N, E, BWD, true>());
     if (cols <= 2048) return f(CloseRow<T, 256 / N, E, BWD, true>());
-    if (cols <= 4096) return f(CloseRow<T, 512, 8, BWD, true>());   // (rows of 256 threads leave room for one CTA of half the warps)
+    if (cols <= 4096) return f(CloseRow<T, 512 / N, E, BWD, true>());
   } else {
     if (cols <= 256) return f(CloseRow<T, 32, 8, BWD, false>());
     if (cols <= 1024) return f(CloseRow<T, 128, 8, BWD, false>());

@@ -262,10 +262,8 @@ def _norm(q, rows, cols, dtype, what):
 
 
 def _norm_vectors(after, before):
-    for q in (after, before):
-        if q is not None:
-            yield q.weight
-            yield q.bias
+    a = () if after is None else (after.weight, after.bias)
+    return a if before is None else (*a, before.weight, before.bias)
 
 
 def abcd_residual_norm(ctx: Context, x, f, after, before, gate, scale, y, n=None):
