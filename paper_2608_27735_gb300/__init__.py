@@ -778,7 +778,7 @@ def visible_pairs(ctx: Context, blocks, cameras, dims, origin, side, opts=None):
     return out
 
 
-from .network import (FeedForwardBlock, Norm, Packed8, abcd_dropout, abcd_dropout_backward,  # noqa: E402,F401
+from .network import (FeedForwardBlock, Norm, NormedStack, Packed8, abcd_dropout, abcd_dropout_backward,  # noqa: E402,F401
                       abcd_embedding, abcd_embedding_backward, abcd_gated_ff, abcd_gated_ff_backward,
                       abcd_gated_ff_backward_packed8, abcd_layer_norm, abcd_layer_norm_backward,
                       abcd_linear, abcd_linear_backward, abcd_pack8, abcd_residual_norm,

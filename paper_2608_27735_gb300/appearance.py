@@ -7,14 +7,20 @@ the coefficients that the camera sees.  They are rendered by the calls of a trai
 gradient that abcd_backward leaves for the coefficients goes back through the layers.  Everything is
 in 32 bits; all weights lie in one buffer, which abcd_adam_active updates.
 
-``appearance_experiment()`` runs it on a small seeded scene: the same block is fitted to photographs
-with and without the layers."""
+``TokenAppearance`` is the same with tokens of any width: a linear layer makes them from the
+coefficients, a row for the camera and one for the cell of the block that the Gaussian lies in are looked
+up and added, blocks with norms before and after follow, and a linear layer adds to the coefficients what
+comes out.  What the blocks keep for the backward pass may be held in 8 bits.
+
+``appearance_experiment()`` runs them on a small seeded scene: the same block is fitted to photographs
+with and without the layers, and with tokens."""
 from __future__ import annotations
 
 import numpy as np
 
-from . import (ABCD_F32, Context, FeedForwardBlock, FwdState, Gaussians, Projected, Tiles, _torch,
-               abcd_adam_active, abcd_backward, abcd_bin_sort, abcd_loss, abcd_project,
+from . import (ABCD_F32, Context, FeedForwardBlock, FwdState, Gaussians, NormedStack, Projected, Tiles,
+               _torch, abcd_adam_active, abcd_assign_cells, abcd_backward, abcd_bin_sort, abcd_embedding,
+               abcd_embedding_backward, abcd_linear, abcd_linear_backward, abcd_loss, abcd_project,
                abcd_render_composite_fwd, camera)
 
 
@@ -107,8 +113,100 @@ class Appearance:
         self.adam.step()
 
 
+class TokenAppearance:
+    """As Appearance, with tokens of width `width` for a block of Gaussians with the given means (numpy
+    [n][3]): a grid of `cells` cells per axis over the means' box gives each Gaussian the row of a learned
+    table.  packed: NormedStack's.  The layer behind the blocks starts at zero, so every camera first sees
+    the block's own coefficients."""
+
+    def __init__(self, ctx: Context, means, sh_degree, n_cameras, layers=2, width=64, widen=4, cells=4,
+                 packed=False, lr=2e-3, seed=0):
+        torch = _torch()
+        self.ctx, self.n, self.width = ctx, len(means), int(width)
+        self.sh_cols = 3 * (sh_degree + 1) ** 2
+        ff = int(widen) * self.width
+        low, high = means.min(0), means.max(0)
+        side = float(max(high - low)) / cells * (1 + 1e-6) or 1.0
+        cell = abcd_assign_cells(means, low.astype(np.float64), side, (cells,) * 3)
+        shapes = {"w_in": (self.width, self.sh_cols), "b_in": (self.width,), "cameras": (n_cameras, self.width),
+                  "cells": (cells ** 3, self.width), "w_out": (self.sh_cols, self.width), "b_out": (self.sh_cols,)}
+        block = {"before_w": (self.width,), "before_b": (self.width,), "after_w": (self.width,), "gate": (self.width,),
+                 "w_gate": (ff, self.width), "w_up": (ff, self.width), "w_down": (self.width, ff)}
+        size = lambda shape: (int(np.prod(shape)) + 3) // 4 * 4       # each on a 16-byte boundary
+        self.adam = Adam(ctx, sum(map(size, shapes.values())) + layers * sum(map(size, block.values())), lr)
+        rng = np.random.default_rng(seed)
+        at = 0
+
+        def take(shapes, start):
+            nonlocal at
+            w, g = {}, {}
+            for name, shape in shapes.items():
+                n = int(np.prod(shape))
+                w[name], g[name] = (t[at:at + n].view(shape) for t in (self.adam.values, self.adam.grads))
+                at += size(shape)
+                w[name].copy_(torch.from_numpy(np.broadcast_to(start(name, shape), shape).astype(np.float32)))
+            return w, g
+
+        def start(name, shape):
+            if name in ("w_out", "b_in", "b_out", "before_b"):
+                return 0.0
+            if name in ("before_w", "after_w"):
+                return 1.0
+            if name == "gate":
+                return 0.5
+            return rng.normal(0, 0.1 if name in ("cameras", "cells") else shape[1] ** -0.5, shape)
+
+        self.w, self.g = take(shapes, start)
+        blocks = [take(block, start) for _ in range(layers)]
+        self.stack = NormedStack(ctx, [w for w, _ in blocks], self.n, "silu", packed=packed)
+        self.stack.grads = [g for _, g in blocks]
+        self.cell = torch.from_numpy(cell.astype(np.int32)).cuda()
+        self.seen = torch.empty(self.n, dtype=torch.int32, device="cuda")          # the camera, for each token
+        new = lambda c: torch.empty(self.n, c, device="cuda")
+        self.tokens, self.result, self.d = new(self.width), new(self.width), new(self.width)
+        self.x, self.d_sh = new(self.sh_cols), new(self.sh_cols)
+        ctx.hold(self.cell, self.seen, self.tokens, self.result, self.d, self.x, self.d_sh)
+        for a, b in ((self.sh_cols, self.width), (self.width, self.sh_cols)):
+            ctx.reserve_linear(self.n, a, b)
+        ctx.reserve_embedding(self.n, max(n_cameras, cells ** 3), self.width)
+
+    def forward(self, sh, ci, train=True):
+        """The coefficients that camera ci sees of sh [n][D][3]: a new tensor of that shape."""
+        w, ctx = self.w, self.ctx
+        tokens = self.tokens if train else self.d
+        result = self.result if train else self.d
+        x = sh.reshape(self.n, self.sh_cols)
+        if train:
+            self.x.copy_(x)
+        self.seen.fill_(ci)
+        abcd_linear(ctx, x, w["w_in"], w["b_in"], "none", tokens)
+        abcd_embedding(ctx, w["cameras"], self.seen, 1.0, tokens, tokens)
+        abcd_embedding(ctx, w["cells"], self.cell, 1.0, tokens, tokens)
+        self.stack.forward(tokens, result, train)
+        out = _torch().empty_like(x)
+        abcd_linear(ctx, result, w["w_out"], w["b_out"], "none", out, x)
+        return out.reshape(sh.shape)
+
+    def backward(self, d_sh, ci):
+        """The gradient of sh from that of the last training forward(sh, ci)'s result; leaves the weights'
+        gradients in Adam's buffer."""
+        w, g, ctx = self.w, self.g, self.ctx
+        d = d_sh.reshape(self.n, self.sh_cols)
+        abcd_linear_backward(ctx, d, self.result, w["w_out"], "none", None, self.d, g["w_out"], g["b_out"])
+        self.stack.backward(self.d, self.d)
+        self.seen.fill_(ci)
+        abcd_embedding_backward(ctx, self.d, self.seen, 1.0, g["cameras"])
+        abcd_embedding_backward(ctx, self.d, self.cell, 1.0, g["cells"])
+        abcd_linear_backward(ctx, self.d, self.x, w["w_in"], "none", None, self.d_sh, g["w_in"], g["b_in"])
+        return (self.d_sh + d).reshape(d_sh.shape)
+
+    def step(self):
+        self.adam.step()
+
+
 class AppearanceStage:
-    """Fits a block's SH coefficients, and with `appearance` the layers, to photographs.
+    """Fits a block's SH coefficients, and with `appearance` the layers (True: Appearance, "tokens":
+    TokenAppearance), to photographs.
 
     gaussians: scenegen.Gaussians; cameras: objects as camera() takes; photos: float32
     [C][H][W][3]."""
@@ -129,8 +227,12 @@ class AppearanceStage:
         self.grads, self.m, self.v = (Gaussians.zeros_like(self.theta) for _ in range(3))
         self.loss = torch.zeros(1, device="cuda")
         self.lr = [0.0, 0.0, 0.0, 0.0, lr_sh, lr_sh / 20]         # the shapes stay
-        self.appearance = Appearance(self.ctx, n, gaussians.sh_degree, len(self.cams), seed=seed,
-                                     **layers) if appearance else None
+        if appearance == "tokens":
+            self.appearance = TokenAppearance(self.ctx, np.ascontiguousarray(gaussians.means, np.float32),
+                                              gaussians.sh_degree, len(self.cams), seed=seed, **layers)
+        else:
+            self.appearance = Appearance(self.ctx, n, gaussians.sh_degree, len(self.cams), seed=seed,
+                                         **layers) if appearance else None
         self.rng = np.random.default_rng(seed)
         self.t = 0
 
@@ -175,8 +277,8 @@ class AppearanceStage:
 
 def appearance_experiment(T=400, n=1500, n_cams=6, size=96, p=0.05, seed=7):
     """A block seen by cameras of different exposure and white balance (each scales the true colours
-    by a gain per channel), fitted for T steps with and without the layers, from the same SH
-    coefficients.  Returns {name: (loss before, loss after)}."""
+    by a gain per channel), fitted for T steps without layers, with them and with tokens, from the same
+    SH coefficients.  Returns {name: (loss before, loss after)}."""
     from . import scenegen as sg
     s = sg.grid_scene((1, 1, 1), 5.0, n, 1, seed=seed)
     cams = sg.ring_cameras(n_cams, 1.5 * sg.half_diagonal(s.grid), np.zeros(3), size, size, seed=seed,
@@ -189,9 +291,9 @@ def appearance_experiment(T=400, n=1500, n_cams=6, size=96, p=0.05, seed=7):
         truth.render(ci)
         photos.append(truth.out[..., :3].cpu().numpy() * gains[ci])
     out = {}
-    for name, layers in (("one_colour", False), ("appearance", True)):
-        run = AppearanceStage(s.gaussians, cams, np.stack(photos), appearance=layers, seed=seed,
-                              **({"p": p} if layers else {}))
+    for name, layers, more in (("one_colour", False, {}), ("appearance", True, {"p": p}),
+                               ("tokens", "tokens", {"packed": True})):
+        run = AppearanceStage(s.gaussians, cams, np.stack(photos), appearance=layers, seed=seed, **more)
         before = run.eval_loss()
         for _ in range(T):
             run.step()

@@ -34,6 +34,7 @@ struct LookupArgs {
   unsigned table_rows, cols, lanes;   // lanes: threads of a token, up to 256
   int slices;                         // of lanes x V columns
   int lookup;                         // tokens of a group of threads
+  int add_vec;                        // add's rows start on V elements' boundaries (the table's and y's do)
   int wide;                           // 64-bit indices
   float scale;
   unsigned* status;
@@ -76,7 +77,7 @@ __global__ void __launch_bounds__(256) embed_kernel(const __grid_constant__ Look
   __syncthreads();
   const unsigned c = (unsigned)(blockIdx.x % a.slices * a.lanes + threadIdx.x - group * a.lanes) * V;
   if (group >= groups || c >= a.cols || (int)group >= n) return;
-  const bool whole = V == 1 || c + V <= a.cols;
+  const bool whole = V == 1 || c + V <= a.cols, whole_add = whole && a.add_vec;
   const int left = (int)(a.cols - c);
   const T* table = (const T*)a.table + c;
   const T* add = ADD ? (const T*)a.add + first * a.sa + c : nullptr;
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(256) embed_kernel(const __grid_constant__ Look
       const int i = min(i0 + u * (int)groups, n - 1);
       const unsigned row = at[i] < a.table_rows ? at[i] : 0u;
       v[u] = load_part<T, V>(table + row * a.st, whole, left);
-      if (ADD) w[u] = load_part<T, V>(add + i * a.sa, whole, left);
+      if (ADD) w[u] = load_part<T, V>(add + i * a.sa, whole_add, left);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -327,13 +328,14 @@ struct SumArgs {
   int lanes;                          // threads of a token's row, up to 256, V columns each
   int slices;                         // of lanes x V columns
   int chunk;                          // sorted tokens of a CTA
+  int table_vec;                      // dtable's rows start on 16-byte boundaries
   long long chunks;
 };
 
 // V columns of a row of the table's gradient.
 template <typename T, int V> __device__ __forceinline__ void put_row(const SumArgs& a, unsigned row, unsigned c, const float (&s)[V]) {
   T* to = (T*)a.dtable + (long long)row * a.st + c;
-  if (V > 1 && c + V <= a.cols) {
+  if (V > 1 && a.table_vec && c + V <= a.cols) {
     Pack<T, V> q;
 #pragma unroll
     for (int e = 0; e < V; ++e) q.v[e] = from_f32<T>(a.scale * s[e]);
@@ -437,7 +439,7 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const __grid_constant__ 
 // each, has a chunk; a run over few chunks it adds up by itself, for longer ones all groups of the CTA take
 // consecutive parts side by side, whose sums are then added in their order.
 constexpr int kJoinThreads = 1024, kJoinLanes = 16, kJoinAlone = 8;
-template <typename T, int V>
+template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_constant__ SumArgs a) {
   pdl_wait();
   __shared__ float4 run[kJoinThreads];
@@ -450,17 +452,8 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_c
   const auto part = [&](long long q, int which) { return __ldcg(reinterpret_cast<const float4*>(a.part + (2 * q + which) * a.ld + c)); };
   const auto sum = [](float4& s, const float4& v) { s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w); };
   const auto put = [&](unsigned row, const float4& s) {
-    if constexpr (V == 1) {
-      const float v[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float one[1] = {v[e]};
-        if (c + e < a.cols) put_row<T, 1>(a, row, c + e, one);
-      }
-    } else {
-      const float v[4] = {s.x, s.y, s.z, s.w};
-      put_row<T, 4>(a, row, c, v);
-    }
+    const float v[4] = {s.x, s.y, s.z, s.w};
+    put_row<T, 4>(a, row, c, v);
   };
   long long last = -1;                                  // of a run that is too long for the group
   if (group < groups) {
@@ -618,11 +611,12 @@ extern "C" abcd_status abcd_embedding(abcd_ctx* ctx, const abcd_matrix* table, c
   if (overlap(table, y) || on_add || on_index(y, index, index_dtype, y->rows))
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: y overlaps an operand", what);
   LookupArgs a{table->data, index, add ? add->data : nullptr, y->data, y->rows, table->stride, add ? add->stride : 0, y->stride,
-                     (unsigned)table->rows, (unsigned)y->cols, 1, 1, 1, index_dtype == ABCD_I64, scale, (unsigned*)ctx->net_base};
+                     (unsigned)table->rows, (unsigned)y->cols, 1, 1, 1, add && rows_aligned(add, 16), index_dtype == ABCD_I64, scale, (unsigned*)ctx->net_base};
   return with_type(y->dtype, [&](auto t) {
     using T = decltype(t);
     constexpr int V = 16 / sizeof(T);
-    const bool vec = rows_aligned(table, 16) && rows_aligned(y, 16) && (!add || rows_aligned(add, 16));
+    const bool vec = rows_aligned(y, 16) && rows_aligned(table, 16);
+    if (!vec) a.add_vec = 1;                              // one element, wherever it lies
     const long long vectors = vec ? (y->cols + V - 1) / V : y->cols;
     a.lanes = (unsigned)std::min(256LL, vectors);
     a.slices = (int)((vectors + a.lanes - 1) / a.lanes);
@@ -679,10 +673,10 @@ extern "C" abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix*
     q.to_key = s.key[(pass + 1) & 1];
     q.to_id = s.id[(pass + 1) & 1];
   }
-  const bool vec = rows_aligned(dy, 16) && rows_aligned(dtable, 16);
+  const bool vec = rows_aligned(dy, 16);
   const Chunks c = chunks_of(n, dy->cols, vec ? 16 / (int)e : 1);
   SumArgs a{dy->data, q.key, q.id, dtable->data, s.part, n, dy->stride, dtable->stride, (unsigned)dtable->rows,
-            (unsigned)dy->cols, (unsigned)part_ld(dy->cols), scale, c.lanes, c.slices, c.tokens, (n + c.tokens - 1) / c.tokens};
+            (unsigned)dy->cols, (unsigned)part_ld(dy->cols), scale, c.lanes, c.slices, c.tokens, rows_aligned(dtable, 16), (n + c.tokens - 1) / c.tokens};
   return with_type(dy->dtype, [&](auto t) {
     using T = decltype(t);
     const auto sum = [&](auto width) {
@@ -693,7 +687,7 @@ extern "C" abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix*
       const long long groups = kJoinThreads / a.lanes;
       a.slices = (int)((a.ld / 4 + a.lanes - 1) / a.lanes);
       const dim3 grid((unsigned)((a.chunks + groups - 1) / groups * a.slices));
-      return check_launch(ctx, "embed_join_kernel", launch_pdl(embed_join_kernel<T, V>, grid, dim3(kJoinThreads), 0, ctx->stream, a));
+      return check_launch(ctx, "embed_join_kernel", launch_pdl(embed_join_kernel<T>, grid, dim3(kJoinThreads), 0, ctx->stream, a));
     };
     return vec ? sum(std::integral_constant<int, 16 / sizeof(T)>()) : sum(std::integral_constant<int, 1>());
   });

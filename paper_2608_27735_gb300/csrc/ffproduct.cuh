@@ -724,68 +724,63 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] *= u[e];
             pack_all(v, x[0], bf16);
-          } else if constexpr (EPI == kLinear) {
-            const int rows = a.job[0].m - m - quarter * 32, cols = a.job[0].n - n0 - c;
-            float b = 0.f;
-            if (a.bias && lane < min(16, cols)) {
-              if (a.wide_bias) b = __ldg((const float*)a.bias + n0 + c + lane);
-              else b = unpack(__ldg((const unsigned short*)a.bias + n0 + c + lane), bf16);
-            }
-            if (a.in[0].p && a.in[0].vec) {
-              const unsigned at = q + s;
-              const int slot = at % P::kSlots;
-              const char* block = buffers + (2 * P::kResults + slot) * P::kBlockBytes;
-              ok = __all_sync(~0u, ok && mbar_wait(slot_full + 8 * (at % (2 * P::kSlots)), at / (2 * P::kSlots) & 1, a.limit, &dead));
-#pragma unroll
-              for (int e = 0; e < 2; ++e) unpack8(u + 8 * e, *reinterpret_cast<const uint4*>(block + block_at(row, 2 * half + e)), bf16);
-              __syncwarp();
-              if (ok && lane == 0) mbar_arrive(slot_empty + 8 * slot);
-              __syncwarp();
-            } else {
-              residual_ahead<F32>(u, a.in[0], m + quarter * 32, n0 + c, rows, cols, bf16);
-            }
-            tmem_load_wait(v);
-            if (a.bias) {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) v[e] += __shfl_sync(~0u, b, e);
-            }
-            if (saved) pack_all(v, x[1], bf16);
-            if (a.act != ABCD_NO_ACTIVATION) act_values<F32>(v, a.act);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] += u[e];
-            pack_all(v, x[0], bf16);
           } else {
+            // the saved projections' (or the residual's) block of the slot
             const unsigned at = q + s;
             const int slot = at % P::kSlots;
-            const char* block = buffers + (6 + 2 * slot) * P::kBlockBytes;
-            ok = __all_sync(~0u, ok && mbar_wait(slot_full + 8 * (at % (2 * P::kSlots)), at / (2 * P::kSlots) & 1, a.limit, &dead));
+            const char* block = buffers + (2 * P::kResults + P::kAsked * slot) * P::kBlockBytes;
+            const bool asked = P::kIsDown || (a.in[0].p && a.in[0].vec);
+            if (asked)
+              ok = __all_sync(~0u, ok && mbar_wait(slot_full + 8 * (at % (2 * P::kSlots)), at / (2 * P::kSlots) & 1, a.limit, &dead));
             float z[16], d[16];
             if constexpr (EPI == kDown8) {
               // the codes' blocks: rows of 32 bytes under TMA's 32-byte swizzle
               const int piece = row * 32 + ((half ^ (row / 4 & 1)) * 16);
               decode16(z, *reinterpret_cast<const uint4*>(block + piece), scale_at(power[0], s));
               decode16(u, *reinterpret_cast<const uint4*>(block + P::kBlockBytes + piece), scale_at(power[1], s));
-            } else {
+            } else if (asked) {
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                unpack8(z + 8 * e, *reinterpret_cast<const uint4*>(block + block_at(row, 2 * half + e)), bf16);
-                unpack8(u + 8 * e, *reinterpret_cast<const uint4*>(block + P::kBlockBytes + block_at(row, 2 * half + e)), bf16);
+                if (EPI == kDown) unpack8(z + 8 * e, *reinterpret_cast<const uint4*>(block + block_at(row, 2 * half + e)), bf16);
+                unpack8(u + 8 * e, *reinterpret_cast<const uint4*>(block + (EPI == kDown ? P::kBlockBytes : 0) + block_at(row, 2 * half + e)), bf16);
               }
+            } else {
+              residual_ahead<F32>(u, a.in[0], m + quarter * 32, n0 + c, a.job[0].m - m - quarter * 32, a.job[0].n - n0 - c, bf16);
             }
-            __syncwarp();
-            if (ok && lane == 0) mbar_arrive(slot_empty + 8 * slot);
-            __syncwarp();
-            act_slopes<F32>(z, d, a.act);
-            tmem_load_wait(v);
+            if (asked) {
+              __syncwarp();
+              if (ok && lane == 0) mbar_arrive(slot_empty + 8 * slot);
+              __syncwarp();
+            }
+            if constexpr (EPI == kLinear) {
+              float b = 0.f;
+              if (a.bias && lane < min(16, a.job[0].n - n0 - c)) {
+                if (a.wide_bias) b = __ldg((const float*)a.bias + n0 + c + lane);
+                else b = unpack(__ldg((const unsigned short*)a.bias + n0 + c + lane), bf16);
+              }
+              tmem_load_wait(v);
+              if (a.bias) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              d[e] *= v[e] * u[e];
-              u[e] *= z[e];                                    // the hidden matrix
-              z[e] *= v[e];
+                for (int e = 0; e < 16; ++e) v[e] += __shfl_sync(~0u, b, e);
+              }
+              if (saved) pack_all(v, x[1], bf16);
+              if (a.act != ABCD_NO_ACTIVATION) act_values<F32>(v, a.act);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] += u[e];
+              pack_all(v, x[0], bf16);
+            } else {
+              act_slopes<F32>(z, d, a.act);
+              tmem_load_wait(v);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                d[e] *= v[e] * u[e];
+                u[e] *= z[e];                                  // the hidden matrix
+                z[e] *= v[e];
+              }
+              pack_all(u, x[0], bf16);
+              pack_all(d, x[1], bf16);
+              pack_all(z, x[2], bf16);
             }
-            pack_all(u, x[0], bf16);
-            pack_all(d, x[1], bf16);
-            pack_all(z, x[2], bf16);
           }
           // once TMA has read the group's last blocks
           if (elected) tma_store_read();

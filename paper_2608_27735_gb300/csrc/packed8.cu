@@ -20,7 +20,7 @@ struct PackedArgs {
     signed char* codes;
     unsigned char* powers;
     long long rows, cols, sx, sc, sp;
-    int lanes;                        // threads of a row, eight columns each, four to a group of columns
+    int lanes;                        // threads of a row, a unit of columns each, whole groups of 32 columns
     int vec;                          // x's rows start on 16-byte boundaries
   } m[3];
 };
@@ -34,13 +34,19 @@ struct Share {
   int groups;                         // rows between a turn's units
   long long col;
   int left;                           // the thread's columns: none for a thread without a unit
-  __device__ __forceinline__ explicit Share(const PackedArgs::One& o) {
+  // `width`: columns of a unit
+  __device__ __forceinline__ Share(const PackedArgs::One& o, int width) {
     groups = 256 / o.lanes;
     const int group = (int)threadIdx.x / o.lanes, lane = (int)threadIdx.x - group * o.lanes;
-    col = (blockIdx.x * (long long)o.lanes + lane) * 8;
-    left = group < groups ? (int)min(8LL, o.cols - col) : 0;
+    col = (blockIdx.x * (long long)o.lanes + lane) * width;
+    left = group < groups ? (int)min((long long)width, o.cols - col) : 0;
     row = blockIdx.y * (long long)(groups * kFlight) + group;
     step = gridDim.y * (long long)(groups * kFlight);
+    if (left <= 0) {                  // where it may read, it reads the CTA's first row
+      left = 0;
+      col = 0;
+      row -= group;
+    }
   }
 };
 
@@ -48,24 +54,14 @@ struct Share {
 template <typename T> struct Eight {
   Pack<T, 16 / sizeof(T)> q[sizeof(T) / 2];
   __device__ __forceinline__ T& at(int e) { return q[e / (16 / sizeof(T))].v[e % (16 / sizeof(T))]; }
-  __device__ __forceinline__ void load(const T* p, int left, bool vec) {
-    if (vec && left == 8) {
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-      for (int k = 0; k < (int)sizeof(T) / 2; ++k) q[k] = reinterpret_cast<const Pack<T, 16 / sizeof(T)>*>(p)[k];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) at(e) = e < left ? p[e] : T(0.f);
-    }
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) q[k] = reinterpret_cast<const Pack<T, 16 / sizeof(T)>*>(p)[k];
   }
-  __device__ __forceinline__ void store(T* p, int left, bool vec) {
-    if (vec && left == 8) {
+  __device__ __forceinline__ void load(const T* p, int left) {
+    if (left == 8) return load(p);
 #pragma unroll
-      for (int k = 0; k < (int)sizeof(T) / 2; ++k) reinterpret_cast<Pack<T, 16 / sizeof(T)>*>(p)[k] = q[k];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < left) p[e] = at(e);
-    }
+    for (int e = 0; e < 8; ++e) at(e) = e < left ? p[e] : T(0.f);
   }
   // The bits of the largest magnitude, as of a 32-bit value.
   __device__ __forceinline__ unsigned top() const {
@@ -105,11 +101,12 @@ __device__ __forceinline__ uint2 codes_of(Eight<T>& x, int power, unsigned top) 
   return w;
 }
 
-template <typename T>
+// Rows on 16-byte boundaries.  EIGHTS: of a multiple of eight columns, so that no unit is short.
+template <typename T, bool EIGHTS>
 __global__ void __launch_bounds__(256, 4) pack8_kernel(const __grid_constant__ PackedArgs a) {
   pdl_wait();
   const PackedArgs::One& o = a.m[0];
-  const Share at(o);
+  const Share at(o, 8);
   const T* x = (const T*)o.x + at.row * o.sx + at.col;
   signed char* to = o.codes + at.row * o.sc + at.col;
   unsigned char* power_to = o.powers + at.row * o.sp + at.col / 32;
@@ -120,11 +117,14 @@ __global__ void __launch_bounds__(256, 4) pack8_kernel(const __grid_constant__ P
     constexpr bool FULL = decltype(full)::value;
     Eight<T> v[kFlight];
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k)      // without a condition: all are on their way before the first is used
-      v[k].load(FULL ? x + k * next_x : x + (min(r + k * at.groups, o.rows - 1) - r) * o.sx, at.left, o.vec);
+    for (int k = 0; k < kFlight; ++k) {    // without a condition: all are on their way before the first is used
+      const T* from = FULL ? x + k * next_x : x + (min(r + k * at.groups, o.rows - 1) - r) * o.sx;
+      if (EIGHTS) v[k].load(from);
+      else v[k].load(from, at.left);
+    }
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
-      unsigned top = v[k].top();
+      unsigned top = at.left > 0 ? v[k].top() : 0u;     // (a group past the row's end may have threads without a unit)
       top = max(top, __shfl_xor_sync(~0u, top, 1));
       top = max(top, __shfl_xor_sync(~0u, top, 2));
       const bool finite = top < 0x7f800000u;
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(256, 4) pack8_kernel(const __grid_constant__ P
       signed char* row = to + k * next_to;
       if (at.left == 8) {
         *reinterpret_cast<uint2*>(row) = w;
-      } else {
+      } else if (!EIGHTS) {
         for (int e = 0; e < at.left; ++e) row[e] = (signed char)((e < 4 ? w.x : w.y) >> 8 * (e & 3));
       }
       if ((threadIdx.x & 3) == 0 && at.left > 0) power_to[k * next_power] = (unsigned char)power;
@@ -147,11 +147,15 @@ __global__ void __launch_bounds__(256, 4) pack8_kernel(const __grid_constant__ P
   }
 }
 
+// (32-bit results by four columns: eight, as two accesses of half the bytes each, took 59 us for 50,000 x 1,024
+// instead of 42.)
 template <typename T>
 __global__ void __launch_bounds__(256, 4) unpack8_kernel(const __grid_constant__ PackedArgs a) {
   pdl_wait();
   const PackedArgs::One& o = a.m[blockIdx.z];
-  const Share at(o);
+  constexpr int W = 16 / sizeof(T);                         // columns of a unit: 16 bytes of results
+  using Codes = std::conditional_t<W == 8, uint2, unsigned>;
+  const Share at(o, W);
   if (at.left <= 0) return;
   T* x = (T*)o.x + at.row * o.sx + at.col;
   const signed char* from = o.codes + at.row * o.sc + at.col;
@@ -159,22 +163,30 @@ __global__ void __launch_bounds__(256, 4) unpack8_kernel(const __grid_constant__
   const long long next_x = at.groups * o.sx, next_from = at.groups * o.sc, next_power = at.groups * o.sp;
   auto turn = [&](long long r, auto full) {
     constexpr bool FULL = decltype(full)::value;
-    uint2 w[kFlight];
+    Codes w[kFlight];
     unsigned power[kFlight];
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
       const long long back = FULL ? 0 : r + k * at.groups - min(r + k * at.groups, o.rows - 1);
-      w[k] = *reinterpret_cast<const uint2*>(from + k * next_from - back * o.sc);      // a row of codes has room for whole units
+      w[k] = *reinterpret_cast<const Codes*>(from + k * next_from - back * o.sc);      // a row of codes has room for whole units
       power[k] = power_from[k * next_power - back * o.sp];
     }
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
       if (!FULL && r + k * at.groups >= o.rows) break;
       const float scale = __uint_as_float(power[k] << 23);     // 255: infinite, and NaN times the codes' zeros
-      Eight<T> v;
+      Pack<T, W> v;
+      const unsigned* codes = reinterpret_cast<const unsigned*>(&w[k]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v.at(e) = from_f32<T>(code_value((e < 4 ? w[k].x : w[k].y) ^ 0x80808080u, e & 3) * scale);
-      v.store(x + k * next_x, at.left, o.vec);
+      for (int e = 0; e < W; ++e) v.v[e] = from_f32<T>(code_value(codes[e / 4] ^ 0x80808080u, e & 3) * scale);
+      T* to = x + k * next_x;
+      if (at.left == W) {
+        *reinterpret_cast<Pack<T, W>*>(to) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+          if (e < at.left) to[e] = v.v[e];
+      }
     }
   };
   const int per_turn = at.groups * kFlight;
@@ -247,18 +259,18 @@ dim3 any_grid(const abcd_ctx* ctx, const PackedArgs::One& o) {
   return dim3((unsigned)slices, (unsigned)std::min((o.rows + 7) / 8, std::max(1LL, 8LL * ctx->num_sms / slices)));
 }
 
-PackedArgs::One one_of(const abcd_packed8* q, void* x, long long stride, int dtype) {
+PackedArgs::One one_of(const abcd_packed8* q, void* x, long long stride, int dtype, int width) {
   const bool vec = (((uintptr_t)x | (q->rows > 1 ? (size_t)stride * elem_size(dtype) : 0)) & 15) == 0;
   return PackedArgs::One{x, q->codes, q->powers, q->rows, q->cols, stride, q->stride, q->power_stride,
-                         (int)std::min<long long>(256, 4 * ((q->cols + 31) / 32)), vec};
+                         (int)std::min<long long>(256, 32 / width * ((q->cols + 31) / 32)), vec};
 }
 
 // A grid for matrices of up to these: slices of columns, CTAs of rows, matrices.
-dim3 grid_of(const abcd_ctx* ctx, const PackedArgs& a, int n) {
+dim3 grid_of(const abcd_ctx* ctx, const PackedArgs& a, int n, int width) {
   long long slices = 1, rows = 1;
   for (int k = 0; k < n; ++k) {
     const PackedArgs::One& o = a.m[k];
-    const long long per_cta = 256 / o.lanes * kFlight, s = (o.cols + 8 * o.lanes - 1) / (8 * o.lanes);
+    const long long per_cta = 256 / o.lanes * kFlight, s = (o.cols + width * o.lanes - 1) / (width * o.lanes);
     slices = std::max(slices, s);
     rows = std::max(rows, std::min((o.rows + per_cta - 1) / per_cta, std::max(1LL, 4LL * ctx->num_sms / (s * n))));
   }
@@ -271,8 +283,9 @@ abcd_status unpack(abcd_ctx* ctx, const Unpacked* list, int n) {
   for (const int dtype : {ABCD_BF16, ABCD_F16, ABCD_F32}) {          // a launch for each type there is
     PackedArgs a{};
     int count = 0;
+    const int width = (int)(16 / elem_size(dtype));
     for (int k = 0; k < n; ++k)
-      if (list[k].dtype == dtype) a.m[count++] = one_of(list[k].from, list[k].to, list[k].stride, dtype);
+      if (list[k].dtype == dtype) a.m[count++] = one_of(list[k].from, list[k].to, list[k].stride, dtype, width);
     if (count == 0) continue;
     if (count == 1 && !a.m[0].vec) {
       const abcd_status st = with_type(dtype, [&](auto t) {
@@ -282,7 +295,7 @@ abcd_status unpack(abcd_ctx* ctx, const Unpacked* list, int n) {
       continue;
     }
     const abcd_status st = with_type(dtype, [&](auto t) {
-      return check_launch(ctx, "unpack8_kernel", launch_pdl(unpack8_kernel<decltype(t)>, grid_of(ctx, a, count), dim3(256), 0, ctx->stream, a));
+      return check_launch(ctx, "unpack8_kernel", launch_pdl(unpack8_kernel<decltype(t)>, grid_of(ctx, a, count, width), dim3(256), 0, ctx->stream, a));
     });
     if (st != ABCD_OK) return st;
   }
@@ -300,11 +313,12 @@ extern "C" abcd_status abcd_pack8(abcd_ctx* ctx, const abcd_matrix* x, const abc
   if (x->rows == 0) return ABCD_OK;
   if (touches(packed, x)) return fail(ctx, ABCD_ERR_INVALID_ARG, "abcd_pack8: the packed matrix overlaps x");
   PackedArgs a{};
-  a.m[0] = one_of(packed, x->data, x->stride, x->dtype);
+  a.m[0] = one_of(packed, x->data, x->stride, x->dtype, 8);
   return with_type(x->dtype, [&](auto t) {
     if (!a.m[0].vec)
       return check_launch(ctx, "pack8_any_kernel", launch_pdl(pack8_any_kernel<decltype(t)>, any_grid(ctx, a.m[0]), dim3(256), 0, ctx->stream, a));
-    return check_launch(ctx, "pack8_kernel", launch_pdl(pack8_kernel<decltype(t)>, grid_of(ctx, a, 1), dim3(256), 0, ctx->stream, a));
+    using T = decltype(t);
+    return check_launch(ctx, "pack8_kernel", launch_pdl(x->cols % 8 == 0 ? pack8_kernel<T, true> : pack8_kernel<T, false>, grid_of(ctx, a, 1, 8), dim3(256), 0, ctx->stream, a));
   });
 }
 

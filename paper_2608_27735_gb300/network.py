@@ -421,3 +421,106 @@ class FeedForwardBlock:
                                g["w_gate"], g["w_up"], g["w_down"])
         abcd_layer_norm_backward(self.ctx, d_nx, x, w["norm_w"], self.mean[:n], self.rstd[:n], dx,
                                  g["norm_w"], g["norm_b"], dy)
+
+
+class NormedStack:
+    """Residual blocks with a norm before and one after: block k takes n = before_k(x) to
+    x + scale gate_k after_k(gated_ff(n)), whose sum, gate and both norms around it (the next block's
+    `before` among them) are one call.  Up to `rows` tokens; `before` is a layer norm, `after` an rms norm.
+
+    weights: for each block {"before_w", "before_b", "after_w", "gate": [cols], "w_gate", "w_up": [ff][cols],
+    "w_down": [cols][ff]}, CUDA tensors of one type; `grads` holds their gradients under the same names
+    after backward().  packed: what a block keeps for its backward pass of its normed tokens and its
+    projections is in 8 bits (33/32 bytes an element instead of two or four); the gradients are then those
+    of what the packed matrices stand for."""
+
+    def __init__(self, ctx: Context, weights, rows, activation="silu", scale=1.0, eps=1e-5, packed=False):
+        torch = _torch()
+        self.ctx, self.w, self.rows = ctx, [dict(w) for w in weights], int(rows)
+        self.act, self.scale, self.eps, self.packed = activation, float(scale), float(eps), bool(packed)
+        self.ff, self.cols = self.w[0]["w_gate"].shape
+        dt, dev = self.w[0]["w_gate"].dtype, self.w[0]["w_gate"].device
+        new = lambda c: torch.empty(self.rows, c, dtype=dt, device=dev)
+        blocks = len(self.w)
+        self.x = [new(self.cols) for _ in range(blocks)]             # the blocks' inputs
+        self.f = [new(self.cols) for _ in range(blocks)]             # their feed-forward results
+        self.stats = torch.empty(blocks, 4, self.rows, dtype=torch.float32, device=dev)
+        # mean and rstd of a block's `before`, rstd of its `after`
+        full = 1 if packed else blocks
+        self.normed, self.gate, self.up = ([new(c) for _ in range(full)] for c in (self.cols, self.ff, self.ff))
+        self.d, self.df = [new(self.cols) for _ in range(2)], new(self.cols)
+        self.kept8 = [[Packed8(self.rows, c, dev) for c in (self.cols, self.ff, self.ff)] for _ in range(blocks)] if packed else []
+        self.grads = [{k: torch.empty_like(t) for k, t in w.items()} for w in self.w]
+        self.kept = None                                             # rows of the last training pass
+        ctx.hold(*self.x, *self.f, self.stats, *self.normed, *self.gate, *self.up, *self.d, self.df,
+                 *(t for g in self.grads for t in g.values()), *(t for q in self.kept8 for m in q for t in (m.codes, m.powers)))
+        (ctx.reserve_packed8 if packed else ctx.reserve_network)(self.rows, self.cols, self.ff, dt)
+        ctx.reserve_residual_norm(self.rows, self.cols)
+        ctx.reserve_network(self.rows, self.cols)                    # the first norm's backward pass
+
+    def _norms(self, k, n, train=True):
+        """`after` of block k and `before` of the next one (None after the last), over n rows."""
+        stat = lambda b, i: self.stats[b, i, :n] if train else None
+        after = Norm("rms", self.w[k]["after_w"], None, self.eps, None, stat(k, 2))
+        if k + 1 == len(self.w):
+            return after, None
+        nxt = self.w[k + 1]
+        return after, Norm("layer", nxt["before_w"], nxt["before_b"], self.eps, stat(k + 1, 0), stat(k + 1, 1))
+
+    def forward(self, x, y, train=True):
+        """y = the blocks of x (both [rows'][cols], rows' <= rows).  train: keep what the backward pass
+        needs; otherwise what an earlier pass kept stays, and y may be x."""
+        n, ctx, first = x.shape[0], self.ctx, self.w[0]
+        if not train:
+            # in the backward pass's buffers
+            at, normed, f = self.d[0][:n], self.d[1][:n], self.df[:n]
+            abcd_layer_norm(ctx, x, first["before_w"], first["before_b"], self.eps, normed)
+            for k, w in enumerate(self.w):
+                abcd_gated_ff(ctx, normed, w["w_gate"], w["w_up"], w["w_down"], self.act, f)
+                after, before = self._norms(k, n, False)
+                last = before is None
+                abcd_residual_norm(ctx, x, f, after, before, w["gate"], self.scale, y if last else at, None if last else normed)
+                x = at
+            return
+        self.kept = None
+        self.x[0][:n].copy_(x)
+        s = self.stats[0]
+        abcd_layer_norm(ctx, self.x[0][:n], first["before_w"], first["before_b"], self.eps, self.normed[0][:n], s[0, :n], s[1, :n])
+        for k, w in enumerate(self.w):
+            b = 0 if self.packed else k
+            normed, gate, up, f = self.normed[b][:n], self.gate[b][:n], self.up[b][:n], self.f[k][:n]
+            abcd_gated_ff(ctx, normed, w["w_gate"], w["w_up"], w["w_down"], self.act, f, gate, up)
+            if self.packed:
+                for t, q in zip((normed, gate, up), self.kept8[k]):
+                    abcd_pack8(ctx, t, q.head(n))
+            after, before = self._norms(k, n)
+            last = before is None
+            to = y if last else self.x[k + 1][:n]
+            abcd_residual_norm(ctx, self.x[k][:n], f, after, before, w["gate"], self.scale, to,
+                               None if last else self.normed[0 if self.packed else k + 1][:n])
+        self.kept = n
+
+    def backward(self, dy, dx):
+        """dx (may be dy) and `grads` of the last forward(..., train=True) from its result's gradient."""
+        n, ctx, blocks = dy.shape[0], self.ctx, len(self.w)
+        if n != self.kept:
+            raise ValueError(f"dy has {n} rows, the last training pass {self.kept}")
+        d, dn, df = dy, None, self.df[:n]
+        for k in reversed(range(blocks)):
+            w, g = self.w[k], self.grads[k]
+            after, before = self._norms(k, n)
+            nxt = {} if before is None else self.grads[k + 1]
+            to = self.d[0][:n]
+            abcd_residual_norm_backward(ctx, d, dn, self.x[k][:n], self.f[k][:n], after, before, w["gate"], self.scale,
+                                        to, df, g["gate"], g["after_w"], None, nxt.get("before_w"), nxt.get("before_b"))
+            d, dn = to, self.d[1][:n]
+            out = dn, g["w_gate"], g["w_up"], g["w_down"]
+            if self.packed:
+                q = [m.head(n) for m in self.kept8[k]]
+                abcd_gated_ff_backward_packed8(ctx, df, q[0], w["w_gate"], w["w_up"], w["w_down"], self.act, q[1], q[2], *out)
+            else:
+                abcd_gated_ff_backward(ctx, df, self.normed[k][:n], w["w_gate"], w["w_up"], w["w_down"], self.act,
+                                       self.gate[k][:n], self.up[k][:n], *out)
+        s, g = self.stats[0], self.grads[0]
+        abcd_layer_norm_backward(ctx, dn, self.x[0][:n], self.w[0]["before_w"], s[0, :n], s[1, :n], dx, g["before_w"],
+                                 g["before_b"], d)

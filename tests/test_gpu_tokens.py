@@ -92,7 +92,7 @@ def test_pack_of_part_of_the_rows(ctx):
         q.head(51)
 
 
-PACKED_FF = [(1, 8, 16), (9, 59, 40), (200, 64, 256), (300, 250, 129), (1100, 256, 512)]
+PACKED_FF = [(1, 8, 16), (9, 59, 40), (200, 64, 256), (300, 250, 129), (1100, 256, 512), (9000, 64, 700)]
 
 
 @pytest.mark.parametrize("kind", KINDS)
