@@ -118,6 +118,7 @@ __global__ void __launch_bounds__(256) embed_kernel(const __grid_constant__ Look
 // ---- the sort
 
 constexpr int kMaxDigits = 1024;      // bins of a pass
+constexpr int kScanned = 8;           // tiles up to which each adds up the counts for itself
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 
 struct SortArgs {
@@ -280,8 +281,24 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
   const unsigned inside = first_places(total);
   unsigned outside = inside;
   if (a.tiles > 1) {
-    outside = first_places(threadIdx.x < digits ? a.total[threadIdx.x] : 0u);
-    if (threadIdx.x < digits) outside += a.count[(long long)threadIdx.x * a.tiles + blockIdx.x];
+    unsigned all = 0, ahead = 0;                      // the digit's tokens, and those of the tiles before
+    if (threadIdx.x < digits) {
+      const unsigned* c = a.count + (long long)threadIdx.x * a.tiles;
+      if (a.tiles > kScanned) {
+        all = a.total[threadIdx.x];
+        ahead = c[blockIdx.x];
+      } else {
+        unsigned v[kScanned];
+#pragma unroll
+        for (int t = 0; t < kScanned; ++t) v[t] = c[min(t, a.tiles - 1)];
+#pragma unroll
+        for (int t = 0; t < kScanned; ++t) {
+          ahead += t < (int)blockIdx.x ? v[t] : 0u;
+          all += t < a.tiles ? v[t] : 0u;
+        }
+      }
+    }
+    outside = first_places(all) + ahead;
   }
   if (threadIdx.x < digits) {
     local[threadIdx.x] = inside;
@@ -664,7 +681,7 @@ extern "C" abcd_status abcd_embedding_backward(abcd_ctx* ctx, const abcd_matrix*
     abcd_status st = ABCD_OK;
     if (p.tiles > 1) {
       st = sort("sort_count_kernel", sort_count_kernel, p.tiles + more, kSortThreads, 0);
-      if (st == ABCD_OK) st = sort("sort_scan_kernel", sort_scan_kernel, ((1 << p.bits) + 7) / 8, 256, 0);
+      if (st == ABCD_OK && p.tiles > kScanned) st = sort("sort_scan_kernel", sort_scan_kernel, ((1 << p.bits) + 7) / 8, 256, 0);
     }
     if (st == ABCD_OK) st = sort("sort_place_kernel", place, p.tiles + (p.tiles > 1 ? 0 : more), kSortThreads, smem);
     if (st != ABCD_OK) return st;

@@ -631,28 +631,31 @@ struct CloseSums {
   void* to[5];                        // dgate, dafter_weight, dafter_bias, dbefore_weight, dbefore_bias
 };
 
-// The vectors' gradients from the CTAs' sums: eight columns a CTA, whose lanes are the four sums of each;
-// 32 runs of consecutive CTAs are added side by side and then in their order.
+// The vectors' gradients from the CTAs' sums: two columns a CTA, whose lanes are the four sums of each; 128
+// runs of consecutive CTAs are added side by side and then in their order (a warp's four in pairs, the
+// warps' one after another).  With eight columns and 32 runs 59 columns of 304 CTAs took 5.7 us.
 template <typename T>
 __global__ void __launch_bounds__(1024) close_sum_kernel(const __grid_constant__ CloseSums a) {
   pdl_wait();
-  __shared__ float run[32][33];
-  const int lane = threadIdx.x & 31, k = threadIdx.x / 32, which = lane / 8, c = blockIdx.x * 8 + lane % 8;
+  __shared__ float run[32][9];
+  const int lane = threadIdx.x & 7, k = threadIdx.x / 8, which = lane / 2, c = blockIdx.x * 2 + lane % 2;
   float s = 0.f;
   if (c < a.cols) {
     const float* p = a.part + (long long)which * a.cols + c;
-    const int q1 = (int)((long long)a.ctas * (k + 1) / 32);
-#pragma unroll 4
-    for (int q = (int)((long long)a.ctas * k / 32); q < q1; ++q) s += p[(long long)q * 4 * a.cols];
+    const int q1 = (int)((long long)a.ctas * (k + 1) / 128);
+#pragma unroll 3
+    for (int q = (int)((long long)a.ctas * k / 128); q < q1; ++q) s += p[(long long)q * 4 * a.cols];
   }
-  run[k][lane] = s;
+  s += __shfl_xor_sync(~0u, s, 8);
+  s += __shfl_xor_sync(~0u, s, 16);
+  if ((threadIdx.x & 31) < 8) run[threadIdx.x / 32][lane] = s;
   __syncthreads();
-  if (k) return;
+  if (threadIdx.x >= 32) return;
   s = 0.f;
 #pragma unroll
   for (int q = 0; q < 32; ++q) s += run[q][lane];
-  const float s1 = __shfl_sync(~0u, s, lane % 8), s2 = __shfl_sync(~0u, s, 8 + lane % 8);
-  if (c >= a.cols) return;
+  const float s1 = __shfl_sync(~0u, s, lane % 2), s2 = __shfl_sync(~0u, s, 2 + lane % 2);
+  if (threadIdx.x >= 8 || c >= a.cols) return;
   auto put = [&](int i, float v) {
     if (!a.to[i]) return;
     if (a.wide_w) ((float*)a.to[i])[c] = v;
@@ -840,6 +843,6 @@ extern "C" abcd_status abcd_residual_norm_backward(abcd_ctx* ctx, const abcd_mat
     if (std::all_of(to, to + 5, [](void* p) { return !p; })) return ABCD_OK;
     CloseSums s{a.part, ctas, a.cols, a.wide_w, scale, gate, a.w[0], a.b[0], {}};
     std::copy(to, to + 5, s.to);
-    return check_launch(ctx, "close_sum_kernel", launch_pdl(close_sum_kernel<T>, dim3((unsigned)((a.cols + 7) / 8)), dim3(1024), 0, ctx->stream, s));
+    return check_launch(ctx, "close_sum_kernel", launch_pdl(close_sum_kernel<T>, dim3((unsigned)((a.cols + 1) / 2)), dim3(1024), 0, ctx->stream, s));
   });
 }
