@@ -241,14 +241,37 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
   unsigned short* own = before + warp * digits;
   unsigned key[IT];
   sort_keys(a, first + start, 32, a.n, key);
-  for (int i = threadIdx.x; i < kSortWarps * digits / 2; i += kSortThreads) reinterpret_cast<unsigned*>(before)[i] = 0;
+      unsigned all = 0, ahead = 0;                      // the digit's tokens, and those of the tiles before
+      if (a.tiles > 1 && threadIdx.x < digits) {
+        const unsigned* c = a.count + (long long)threadIdx.x * a.tiles;
+        if (a.tiles > kScanned) {
+          all = a.total[threadIdx.x];
+          ahead = c[blockIdx.x];
+        } else {
+          unsigned v[kScanned];
+  #pragma unroll
+          for (int t = 0; t < kScanned; ++t) v[t] = c[min(t, a.tiles - 1)];
+  #pragma unroll
+          for (int t = 0; t < kScanned; ++t) {
+            ahead += t < (int)blockIdx.x ? v[t] : 0u;
+            all += t < a.tiles ? v[t] : 0u;
+          }
+        }
+      }
+  for (int i = threadIdx.x; i < kSortWarps * digits / 8; i += kSortThreads) reinterpret_cast<uint4*>(before)[i] = make_uint4(0u, 0u, 0u, 0u);
   __syncthreads();
   unsigned rank[IT];                                  // among the warp's tokens of the digit
 #pragma unroll
   for (int k = 0; k < IT; ++k) {
     const bool in = start + 32 * k < n;
-    const unsigned d = in ? key[k] >> a.shift & (digits - 1) : ~0u;
-    const unsigned same = __match_any_sync(~0u, d);
+    const unsigned d = key[k] >> a.shift & (digits - 1);
+    // the lanes with the same digit, bit by bit
+    unsigned same = __ballot_sync(~0u, in);
+    for (int b = 0; b < a.bits; ++b) {
+      const bool one = d >> b & 1;
+      const unsigned ones = __ballot_sync(~0u, one);
+      same &= one ? ones : ~ones;
+    }
     rank[k] = __popc(same & ((1u << lane) - 1));
     unsigned had = in ? own[d] : 0u;
     __syncwarp();
@@ -257,17 +280,22 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
     __syncwarp();
   }
   __syncthreads();
-  unsigned total = 0;
-  if (threadIdx.x < digits) {
-    unsigned v[kSortWarps];
+  // the warps' tokens of a digit become those of the warps before; a thread takes two digits, a word
+  if (threadIdx.x < digits / 2) {
+    unsigned* word = reinterpret_cast<unsigned*>(before) + threadIdx.x;
+    unsigned v[kSortWarps], sum = 0;
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) v[w] = before[w * digits + threadIdx.x];
+    for (int w = 0; w < kSortWarps; ++w) v[w] = word[w * (digits / 2)];
 #pragma unroll
     for (int w = 0; w < kSortWarps; ++w) {
-      before[w * digits + threadIdx.x] = (unsigned short)total;
-      total += v[w];
+      word[w * (digits / 2)] = sum;
+      sum += v[w];
     }
+    local[2 * threadIdx.x] = sum & 0xffffu;
+    local[2 * threadIdx.x + 1] = sum >> 16;
   }
+  __syncthreads();
+  const unsigned total = threadIdx.x < digits ? local[threadIdx.x] : 0u;
   // a digit's first place, in the tile and in all
   auto first_places = [&](unsigned count) {
     const unsigned up_to = warp_sums(count);
@@ -280,26 +308,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
   };
   const unsigned inside = first_places(total);
   unsigned outside = inside;
-  if (a.tiles > 1) {
-    unsigned all = 0, ahead = 0;                      // the digit's tokens, and those of the tiles before
-    if (threadIdx.x < digits) {
-      const unsigned* c = a.count + (long long)threadIdx.x * a.tiles;
-      if (a.tiles > kScanned) {
-        all = a.total[threadIdx.x];
-        ahead = c[blockIdx.x];
-      } else {
-        unsigned v[kScanned];
-#pragma unroll
-        for (int t = 0; t < kScanned; ++t) v[t] = c[min(t, a.tiles - 1)];
-#pragma unroll
-        for (int t = 0; t < kScanned; ++t) {
-          ahead += t < (int)blockIdx.x ? v[t] : 0u;
-          all += t < a.tiles ? v[t] : 0u;
-        }
-      }
-    }
-    outside = first_places(all) + ahead;
-  }
+  if (a.tiles > 1) outside = first_places(all) + ahead;
   if (threadIdx.x < digits) {
     local[threadIdx.x] = inside;
     place[threadIdx.x] = outside - inside;
@@ -364,8 +373,8 @@ template <typename T, int V> __device__ __forceinline__ void put_row(const SumAr
   }
 }
 
-// A chunk's tokens, in groups of threads that each walk a stretch of them, V columns a thread; eight tokens'
-// rows are on their way at once.  A run of equal rows inside a stretch is a row of the result.  One that
+// A chunk's tokens, in groups of threads that each walk a stretch of them, V columns a thread; eight (of
+// eight columns four) tokens' rows are on their way at once.  A run of equal rows inside a stretch is a row of the result.  One that
 // began before the stretch (its head) or goes on after it (its tail) is left in shared memory, and the
 // group that a run begins in adds up what the next ones have of it; what passes the chunk goes to the
 // workspace.
@@ -387,7 +396,7 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const __grid_constant__ 
   const unsigned c = ((unsigned)(blockIdx.x % a.slices) * a.lanes + lane) * V;
   const bool in = c < a.cols && group < groups;
   const int g0 = group < groups ? group * stretch : n, g1 = min(g0 + stretch, n);
-  constexpr int U = 8;
+  constexpr int U = V > 4 ? 4 : 8;
   float s[V] = {};
   bool began = g0 < g1 && key[g0] == key[g0 + 1];       // the run at hand began before the stretch
   bool has_tail = false;
@@ -460,7 +469,7 @@ template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_constant__ SumArgs a) {
   pdl_wait();
   __shared__ float4 run[kJoinThreads];
-  __shared__ long long last_of[kJoinThreads];
+  __shared__ bool long_of[kJoinThreads];
   const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = kJoinThreads / a.lanes;
   const long long base = blockIdx.x / a.slices * (long long)groups;
   const unsigned c = (blockIdx.x % a.slices * a.lanes + lane) * 4;
@@ -472,40 +481,38 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_c
     const float v[4] = {s.x, s.y, s.z, s.w};
     put_row<T, 4>(a, row, c, v);
   };
-  long long last = -1;                                  // of a run that is too long for the group
+  bool is_long = false;                                 // the group's run is too long for it
   if (group < groups) {
     const long long chunk = base + group, end = (chunk + 1) * a.chunk;
     if (end < a.n) {
-      const unsigned row = a.key[end - 1], then = a.key[end], first = a.key[end - a.chunk], before = chunk > 0 ? a.key[end - a.chunk - 1] : a.table_rows;
-      const unsigned beyond = end + a.chunk < a.n ? a.key[end + a.chunk] : a.table_rows;
-      if (row < a.table_rows && then == row && !(first == row && before == row)) {
-        // the last chunk that begins with the row: steps that double, then halve
-        last = chunk + 1;
-        if (beyond == row) {
-          long long step = 1;
-          while (has(last + step, row)) {
-            last += step;
-            step *= 2;
-          }
-          for (; step; step /= 2)
-            if (has(last + step, row)) last += step;
-        }
-        if (last - chunk <= kJoinAlone) {
-          if (in) {
-            float4 s = part(chunk, 1);
-            for (long long q = chunk + 1; q <= last; ++q) sum(s, part(q, 0));
-            put(row, s);
-          }
-          last = -1;
+      const unsigned row = a.key[end - 1], first = a.key[end - a.chunk], before = chunk > 0 ? a.key[end - a.chunk - 1] : a.table_rows;
+      unsigned then[kJoinAlone + 1];                    // the next chunks' first rows
+#pragma unroll
+      for (int k = 0; k <= kJoinAlone; ++k) then[k] = a.key[min(end + (long long)k * a.chunk, a.n - 1)];
+      if (row < a.table_rows && then[0] == row && !(first == row && before == row)) {
+        int more = 1;                                   // chunks that begin with the row
+#pragma unroll
+        for (int k = 1; k <= kJoinAlone; ++k) more += more == k && end + (long long)k * a.chunk < a.n && then[k] == row;
+        is_long = more > kJoinAlone;
+        if (!is_long && in) {
+          float4 s = part(chunk, 1);
+          for (int k = 1; k <= more; ++k) sum(s, part(chunk + k, 0));
+          put(row, s);
         }
       }
     }
-    if (lane == 0) last_of[group] = last;
+    if (lane == 0) long_of[group] = is_long;
   }
-  if (!__syncthreads_or(last >= 0)) return;
+  if (!__syncthreads_or(is_long)) return;
   for (int g = 0; g < groups; ++g) {
-    if (last_of[g] < 0) continue;
-    const long long chunk = base + g, count = last_of[g] - chunk;
+    if (!long_of[g]) continue;
+    const long long chunk = base + g, left = a.chunks - 1 - chunk;    // chunks after the first, some of the run
+    const unsigned row = a.key[(chunk + 1) * a.chunk];
+    // how many begin with the row: all threads look, first `wide` apart, then at what lies between
+    const long long wide = (left + kJoinThreads - 1) / kJoinThreads;
+    const long long coarse = chunk + 1 + (__syncthreads_count(has(chunk + 1 + threadIdx.x * wide, row)) - 1) * wide;
+    long long count = coarse - chunk - 1;
+    for (long long q = 0; q < wide; q += kJoinThreads) count += __syncthreads_count(q + threadIdx.x < wide && has(coarse + q + threadIdx.x, row));
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (in) {
       const long long q1 = chunk + 1 + count * (group + 1) / groups;
@@ -518,11 +525,11 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_c
     if (group > 0 || !in) continue;
     s = part(chunk, 1);
     for (int h = 0; h < groups; ++h) sum(s, run[h * a.lanes + lane]);
-    put(a.key[(chunk + 1) * a.chunk], s);
+    put(row, s);
   }
 }
 
-constexpr long long kOneTile = 16384;   // tokens of a tile at most: their keys lie in shared memory
+constexpr long long kMostTile = 16384;  // tokens of a tile at most: they lie in shared memory
 
 // How the tokens are sorted: passes of equal bits for the rows and one more (none).
 struct SortPlan {
@@ -534,9 +541,10 @@ SortPlan sort_plan(long long tokens, long long table_rows) {
   while ((1LL << need) <= table_rows) ++need;
   p.passes = (need + 9) / 10;
   p.bits = (need + p.passes - 1) / p.passes;
-  // one tile needs no counts; more of them share the SMs, within what a CTA's shared memory holds
+  // one tile needs no counts; more of them share the SMs, within what a CTA's shared memory holds.  (One tile
+  // of 16,384 took 25 us, four of 4,096 and their counts 15.)
   long long per = 4096;
-  while (per < kOneTile && (tokens <= kOneTile ? tokens > per : tokens > per * kNetSms)) per *= 2;
+  while (per < kMostTile && tokens > per * kNetSms) per *= 2;
   p.per_tile = (int)per;
   p.tiles = (int)((tokens + per - 1) / per);
   return p;
@@ -583,7 +591,7 @@ EmbedScratch scratch_of(char* base, long long tokens, long long cols) {
     s.id[k] = (unsigned*)take(4 * (size_t)tokens);
   }
   // (tiles of up to as many tokens)
-  const long long tiles = std::max(std::min<long long>((tokens + 4095) / 4096, kNetSms), (tokens + kOneTile - 1) / kOneTile);
+  const long long tiles = std::max(std::min<long long>((tokens + 4095) / 4096, kNetSms), (tokens + kMostTile - 1) / kMostTile);
   s.count = (unsigned*)take((size_t)4 * kMaxDigits * (size_t)tiles);
   s.total = (unsigned*)take((size_t)4 * kMaxDigits);
   s.part = (float*)take((size_t)8 * part_ld(cols) * (size_t)most_chunks(tokens, cols));
