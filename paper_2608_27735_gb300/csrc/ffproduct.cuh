@@ -401,6 +401,26 @@ __device__ __forceinline__ void put_block(char* block, int row, int j, const uns
   *reinterpret_cast<uint4*>(block + block_at(row, j + 1)) = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
+// kLinear: sixteen columns of the bias, in every lane (one address for the warp).
+__device__ __forceinline__ void bias_columns(float (&v)[16], const void* bias, int wide, int n, int cols, bool bf16) {
+  const char* p = (const char*)bias + (long long)n * (wide ? 4 : 2);
+  if (cols >= 16 && ((uintptr_t)p & 15) == 0) {
+    if (wide) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float4 x = __ldg(reinterpret_cast<const float4*>(p) + q);
+        v[4 * q] = x.x; v[4 * q + 1] = x.y; v[4 * q + 2] = x.z; v[4 * q + 3] = x.w;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) unpack8(v + 8 * q, __ldg(reinterpret_cast<const uint4*>(p) + q), bf16);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = e >= cols ? 0.f : wide ? __ldg((const float*)p + e) : unpack(__ldg((const unsigned short*)p + e), bf16);
+  }
+}
+
 // kDown8: the powers of eight groups of 32 columns of a row, from group g on (a multiple of eight); 0, which
 // makes values nothing, outside of the matrix.
 __device__ __forceinline__ uint2 row_powers(const unsigned char* p, long long stride, int row, int rows, int g, int groups) {
@@ -753,15 +773,11 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
               __syncwarp();
             }
             if constexpr (EPI == kLinear) {
-              float b = 0.f;
-              if (a.bias && lane < min(16, a.job[0].n - n0 - c)) {
-                if (a.wide_bias) b = __ldg((const float*)a.bias + n0 + c + lane);
-                else b = unpack(__ldg((const unsigned short*)a.bias + n0 + c + lane), bf16);
-              }
+              if (a.bias) bias_columns(z, a.bias, a.wide_bias, n0 + c, a.job[0].n - n0 - c, bf16);
               tmem_load_wait(v);
               if (a.bias) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] += __shfl_sync(~0u, b, e);
+                for (int e = 0; e < 16; ++e) v[e] += z[e];
               }
               if (saved) pack_all(v, x[1], bf16);
               if (a.act != ABCD_NO_ACTIVATION) act_values<F32>(v, a.act);
