@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const __grid_constant__ 
 // Runs that pass a chunk's end, by the chunk that they begin in.  A group of up to sixteen threads, four columns
 // each, has a chunk; a run over few chunks it adds up by itself, for longer ones all groups of the CTA take
 // consecutive parts side by side, whose sums are then added in their order.
-constexpr int kJoinThreads = 1024, kJoinLanes = 16, kJoinAlone = 8;
+constexpr int kJoinThreads = 1024, kJoinLanes = 16, kJoinAlone = 32;
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_constant__ SumArgs a) {
   pdl_wait();
@@ -486,18 +486,29 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_c
     const long long chunk = base + group, end = (chunk + 1) * a.chunk;
     if (end < a.n) {
       const unsigned row = a.key[end - 1], first = a.key[end - a.chunk], before = chunk > 0 ? a.key[end - a.chunk - 1] : a.table_rows;
-      unsigned then[kJoinAlone + 1];                    // the next chunks' first rows
+      // the first rows of the next chunk and of those 1, 2, 4 ... after it: all asked for at once
+      constexpr int LOOKS = 7;
+      static_assert(kJoinAlone == 1 << (LOOKS - 2));
+      unsigned then[LOOKS];
 #pragma unroll
-      for (int k = 0; k <= kJoinAlone; ++k) then[k] = a.key[min(end + (long long)k * a.chunk, a.n - 1)];
+      for (int k = 0; k < LOOKS; ++k) then[k] = a.key[min(end + (long long)(k ? 1 << (k - 1) : 0) * a.chunk, a.n - 1)];
       if (row < a.table_rows && then[0] == row && !(first == row && before == row)) {
-        int more = 1;                                   // chunks that begin with the row
+        int more = 0;                                   // chunks after the next one that begin with the row: as many as
 #pragma unroll
-        for (int k = 1; k <= kJoinAlone; ++k) more += more == k && end + (long long)k * a.chunk < a.n && then[k] == row;
-        is_long = more > kJoinAlone;
-        if (!is_long && in) {
-          float4 s = part(chunk, 1);
-          for (int k = 1; k <= more; ++k) sum(s, part(chunk + k, 0));
-          put(row, s);
+        for (int k = 1; k < LOOKS; ++k) {               // the last look that saw it, or up to twice that
+          const int q = 1 << (k - 1);
+          if (then[k] == row && end + (long long)q * a.chunk < a.n) more = q;
+        }
+        is_long = more == kJoinAlone;
+        if (!is_long) {
+          for (int half = more / 2; half; half /= 2)
+            if (has(chunk + 1 + more + half, row)) more += half;
+          if (in) {
+            float4 s = part(chunk, 1);
+#pragma unroll 8
+            for (int k = 0; k <= more; ++k) sum(s, part(chunk + 1 + k, 0));
+            put(row, s);
+          }
         }
       }
     }
@@ -557,7 +568,7 @@ SortPlan sort_plan(long long tokens, long long table_rows) {
 struct Chunks { int lanes, slices, tokens; };
 Chunks chunks_of(long long tokens, long long cols, int v) {
   Chunks c;
-  c.lanes = (int)std::min<long long>(256, (cols + v - 1) / v);
+  c.lanes = lanes_of((cols + v - 1) / v);
   c.slices = (int)((cols + (long long)c.lanes * v - 1) / ((long long)c.lanes * v));
   const int groups = 256 / c.lanes;
   const long long fill = (tokens * c.slices + 2 * kNetSms * groups - 1) / (2LL * kNetSms * groups);
@@ -643,7 +654,7 @@ extern "C" abcd_status abcd_embedding(abcd_ctx* ctx, const abcd_matrix* table, c
     const bool vec = rows_aligned(y, 16) && rows_aligned(table, 16);
     if (!vec) a.add_vec = 1;                              // one element, wherever it lies
     const long long vectors = vec ? (y->cols + V - 1) / V : y->cols;
-    a.lanes = (unsigned)std::min(256LL, vectors);
+    a.lanes = (unsigned)lanes_of(vectors);
     a.slices = (int)((vectors + a.lanes - 1) / a.lanes);
     const long long groups = 256 / a.lanes;
     a.lookup = (int)std::clamp<long long>(y->rows * a.slices / (4LL * ctx->num_sms * groups), 1, kLookup);

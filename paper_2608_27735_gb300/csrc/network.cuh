@@ -90,6 +90,24 @@ __device__ __forceinline__ float code_value(unsigned codes, int byte) {
   return __uint_as_float(__byte_perm(codes, 0x4b000000u, 0x7650 + byte)) - 8388736.f;
 }
 
+// Threads of a row where a CTA of 256 takes rows in groups of that many threads, a vector each: all of the row's
+// vectors up to 256, or an even share of them in up to four slices, where that leaves fewer threads idle
+// (160 vectors: one group of 160, or three of 80).  A multiple of `unit`.
+inline int lanes_of(long long vectors, int unit = 1) {
+  int best = 256 / unit * unit;
+  double used = 0;
+  for (int slices = 1; slices <= 4; ++slices) {
+    const long long lanes = ((vectors + slices - 1) / slices + unit - 1) / unit * unit;
+    if (lanes > 256) continue;
+    const double share = (double)(256 / lanes) * (double)vectors / (256.0 * slices);
+    if (share > used + 0.1) {
+      used = share;
+      best = (int)lanes;
+    }
+  }
+  return best;
+}
+
 // V elements of T as one aligned access.
 template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
 

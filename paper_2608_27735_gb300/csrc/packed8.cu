@@ -278,7 +278,7 @@ dim3 any_grid(const abcd_ctx* ctx, const PackedArgs::One& o) {
 PackedArgs::One one_of(const abcd_packed8* q, void* x, long long stride, int dtype, int width) {
   const bool vec = (((uintptr_t)x | (q->rows > 1 ? (size_t)stride * elem_size(dtype) : 0)) & 15) == 0;
   return PackedArgs::One{x, q->codes, q->powers, q->rows, q->cols, stride, q->stride, q->power_stride,
-                         (int)std::min<long long>(256, 32 / width * ((q->cols + 31) / 32)), vec};
+                         lanes_of(32 / width * ((q->cols + 31) / 32), 32 / width), vec};
 }
 
 // A grid for matrices of up to these: slices of columns, CTAs of rows, matrices.

@@ -146,8 +146,8 @@ __global__ void __launch_bounds__(kLongThreads) close_bwd_long_kernel(const __gr
     auto value = [&](int c) {
       Value v;
       v.k = factors_at<T>(a, c);
-      v.fh = (to_f32(f[c]) - first.mean) * first.rstd;
-      v.yh = (close_value(to_f32(x[c]), v.fh, v.k.x, v.k.y) - second.mean) * second.rstd;
+      v.fh = a.f ? (to_f32(f[c]) - first.mean) * first.rstd : 0.f;
+      v.yh = a.x ? (close_value(to_f32(x[c]), v.fh, v.k.x, v.k.y) - second.mean) * second.rstd : 0.f;
       v.dn = a.dn ? to_f32(dn[c]) : 0.f;
       v.g2 = v.dn * weight_at<T>(a.w[1], a.wide_w, c, 1.f);
       return v;
@@ -337,7 +337,7 @@ template <typename T, typename R> struct CloseRows {
         for (int i = 0; i < R::V; ++i) v[j * R::V + i] = R::TPR >= 32 || t < rows ? to_f32(w.v[i]) : 0.f;
       }
     } else {
-      const bool there = base(mat) != nullptr;
+      const bool there = base(mat) != nullptr && (R::TPR >= 32 || t < rows);
       const T* p = (const T*)(pieces(now, mat) + ((uintptr_t)start_of(mat, row) & 15)) + lane;
 #pragma unroll
       for (int e = 0; e < R::E; ++e) v[e] = there && column(e) < cols ? to_f32(p[e * R::TPR]) : 0.f;
@@ -631,31 +631,33 @@ struct CloseSums {
   void* to[5];                        // dgate, dafter_weight, dafter_bias, dbefore_weight, dbefore_bias
 };
 
-// The vectors' gradients from the CTAs' sums: two columns a CTA, whose lanes are the four sums of each; 128
-// runs of consecutive CTAs are added side by side and then in their order (a warp's four in pairs, the
-// warps' one after another).  With eight columns and 32 runs 59 columns of 304 CTAs took 5.7 us.
-template <typename T>
+// The vectors' gradients from the CTAs' sums: COLS columns a CTA, whose lanes are the four sums of each; 256 /
+// COLS runs of consecutive CTAs are added side by side and then in their order (a warp's in pairs, the
+// warps' one after another).  Few columns go by two (59 columns of 304 CTAs: 5.7 us by eight), many by
+// eight (3,584 columns: 17 us by two).
+template <typename T, int COLS>
 __global__ void __launch_bounds__(1024) close_sum_kernel(const __grid_constant__ CloseSums a) {
   pdl_wait();
-  __shared__ float run[32][9];
-  const int lane = threadIdx.x & 7, k = threadIdx.x / 8, which = lane / 2, c = blockIdx.x * 2 + lane % 2;
+  constexpr int LANES = 4 * COLS, RUNS = 1024 / LANES;
+  __shared__ float run[32][LANES + 1];
+  const int lane = threadIdx.x % LANES, k = threadIdx.x / LANES, which = lane / COLS, c = blockIdx.x * COLS + lane % COLS;
   float s = 0.f;
   if (c < a.cols) {
     const float* p = a.part + (long long)which * a.cols + c;
-    const int q1 = (int)((long long)a.ctas * (k + 1) / 128);
-#pragma unroll 3
-    for (int q = (int)((long long)a.ctas * k / 128); q < q1; ++q) s += p[(long long)q * 4 * a.cols];
+    const int q1 = (int)((long long)a.ctas * (k + 1) / RUNS);
+#pragma unroll 5
+    for (int q = (int)((long long)a.ctas * k / RUNS); q < q1; ++q) s += p[(long long)q * 4 * a.cols];
   }
-  s += __shfl_xor_sync(~0u, s, 8);
-  s += __shfl_xor_sync(~0u, s, 16);
-  if ((threadIdx.x & 31) < 8) run[threadIdx.x / 32][lane] = s;
+#pragma unroll
+  for (int o = LANES; o < 32; o *= 2) s += __shfl_xor_sync(~0u, s, o);
+  if ((threadIdx.x & 31) < LANES) run[threadIdx.x / 32][lane] = s;
   __syncthreads();
   if (threadIdx.x >= 32) return;
   s = 0.f;
 #pragma unroll
   for (int q = 0; q < 32; ++q) s += run[q][lane];
-  const float s1 = __shfl_sync(~0u, s, lane % 2), s2 = __shfl_sync(~0u, s, 2 + lane % 2);
-  if (threadIdx.x >= 8 || c >= a.cols) return;
+  const float s1 = __shfl_sync(~0u, s, lane % COLS), s2 = __shfl_sync(~0u, s, COLS + lane % COLS);
+  if (threadIdx.x >= LANES || c >= a.cols) return;
   auto put = [&](int i, float v) {
     if (!a.to[i]) return;
     if (a.wide_w) ((float*)a.to[i])[c] = v;
@@ -683,8 +685,12 @@ template <typename T, bool BWD, typename F> abcd_status with_row(long long cols,
     if (cols <= 2048) return f(CloseRow<T, 256 / N, E, BWD, true>());
     if (cols <= 4096) return f(CloseRow<T, 512 / N, E, BWD, true>());
   } else {
+    if (cols <= 64) return f(CloseRow<T, 8, 8, BWD, false>());
+    if (cols <= 128) return f(CloseRow<T, 16, 8, BWD, false>());
     if (cols <= 256) return f(CloseRow<T, 32, 8, BWD, false>());
+    if (cols <= 512) return f(CloseRow<T, 64, 8, BWD, false>());
     if (cols <= 1024) return f(CloseRow<T, 128, 8, BWD, false>());
+    if (cols <= 2048) return f(CloseRow<T, 256, 8, BWD, false>());
     if (cols <= 4096) return f(CloseRow<T, 512, 8, BWD, false>());
   }
   return f(0);
@@ -814,6 +820,9 @@ extern "C" abcd_status abcd_residual_norm_backward(abcd_ctx* ctx, const abcd_mat
   a.gate = gate;
   take_norm(a, 0, after);
   take_norm(a, 1, before);
+  // what the results do not depend on is not read: x without `before`, f without either norm and dgate
+  if (!before) a.x = nullptr;
+  if (!before && !after && !dgate) a.f = nullptr;
   a.scale = scale;
   a.wide_w = weight_dtype == ABCD_F32;
   a.rows = x->rows;
@@ -843,6 +852,7 @@ extern "C" abcd_status abcd_residual_norm_backward(abcd_ctx* ctx, const abcd_mat
     if (std::all_of(to, to + 5, [](void* p) { return !p; })) return ABCD_OK;
     CloseSums s{a.part, ctas, a.cols, a.wide_w, scale, gate, a.w[0], a.b[0], {}};
     std::copy(to, to + 5, s.to);
-    return check_launch(ctx, "close_sum_kernel", launch_pdl(close_sum_kernel<T>, dim3((unsigned)((a.cols + 1) / 2)), dim3(1024), 0, ctx->stream, s));
+    const bool wide = a.cols >= 8 * sms;                 // eight columns a CTA still give every SM one
+    return check_launch(ctx, "close_sum_kernel", launch_pdl(wide ? close_sum_kernel<T, 8> : close_sum_kernel<T, 2>, dim3((unsigned)((a.cols + (wide ? 7 : 1)) / (wide ? 8 : 2))), dim3(1024), 0, ctx->stream, s));
   });
 }
