@@ -633,7 +633,8 @@ abcd_status abcd_residual_norm_backward(abcd_ctx* ctx, const abcd_matrix* dy, co
  * magnitude, so an element is off by at most a 128th of that magnitude (and 2^-127); a group that
  * holds an infinity or NaN has p = 255 and reads as NaN. */
 typedef struct {
-  signed char* codes;     /* rows on 32-byte boundaries: aligned, stride a multiple of 32 */
+  signed char* codes;     /* [rows][stride] bytes, all of them there; rows on 32-byte boundaries: aligned, stride a
+                           * multiple of 32 */
   unsigned char* powers;
   long long rows;
   long long cols;
@@ -641,10 +642,11 @@ typedef struct {
   long long power_stride; /* bytes between rows of powers, >= cols / 32 rounded up */
 } abcd_packed8;
 
-/* packed = x in 8 bits; the bytes between rows stay as they are.  packed does not overlap x. */
+/* packed = x in 8 bits; the bytes between rows stay as they are.  packed does not overlap x (what lies between
+ * the rows of either counted in). */
 abcd_status abcd_pack8(abcd_ctx* ctx, const abcd_matrix* x, const abcd_packed8* packed);
 /* y = what packed stands for, rounded to y's type (bf16 and fp32 hold it exactly, fp16 within its range).
- * y does not overlap packed. */
+ * y does not overlap packed, as above. */
 abcd_status abcd_unpack8(abcd_ctx* ctx, const abcd_packed8* packed, const abcd_matrix* y);
 
 /* Bytes of network workspace that abcd_gated_ff_backward_packed8 takes, as for

@@ -3,9 +3,11 @@
 // Forward: bound by HBM (y, add; the table's rows come from L2 when it fits there).
 // Backward: the tokens are sorted by the row that they name (a stable radix sort, up to 10 bits a pass), so
 // that a row's tokens lie next to each other in their own order; runs of equal rows are then summed in
-// registers, `kChunk` tokens at a time, and runs that pass the end of a chunk are joined from the chunks'
+// registers, up to `kChunk` tokens a CTA, and runs that pass the end of a chunk are joined from the chunks'
 // parts in order.  No atomic adds a gradient, so every run gives the same sums, whether all tokens name
 // one row or each its own.
+// 1,000,000 tokens of 100,000 rows of 64 fp32: forward 53 us (5.4 TB/s), backward 105: the sums 60 (4.7 TB/s: a
+// token's row is 256 bytes somewhere), the sort 36 (two passes of nine bits: counts 6, places 12 each), joins 5.
 #include <algorithm>
 #include <type_traits>
 
@@ -55,7 +57,7 @@ template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_part(con
 // V consecutive columns a thread (16 bytes, or one where rows start anywhere), `lanes` threads a token; a CTA
 // takes up to kLookup tokens of each group of threads.  Bound by latency, unless many rows are on their way at once:
 // the indices go to shared memory first, and a thread's loads are asked for U tokens at a time, without a
-// condition (with one, the compiler moved each load to its use: 1,000,000 x 64 fp32 90 us).
+// condition (with one, the compiler moved each load to its use: 1,000,000 x 64 fp32 90 us instead of 53).
 constexpr int kLookup = 16;           // at most: fewer where that leaves SMs idle
 template <typename T, int V, bool ADD>
 __global__ void __launch_bounds__(256) embed_kernel(const __grid_constant__ LookupArgs a) {
@@ -226,7 +228,9 @@ __device__ __forceinline__ unsigned warp_sums(unsigned v) {
 
 // Tokens to their places, equal digits in their order: a warp takes IT x 32 consecutive tokens of the tile, and
 // knows how many of a digit its lanes and the warps before it have.  They go to shared memory in the order of
-// their digits first, so that consecutive lanes write consecutive places.  One tile counts for itself.
+// their digits first, so that consecutive lanes write consecutive places.  One tile counts for itself.  Bound
+// by latency: 1,000,000 tokens, nine bits, 12 us; with the match instruction instead of ballots 18, and with
+// scattered writes 27.
 template <int IT>
 __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_constant__ SortArgs a) {
   pdl_wait();
@@ -564,7 +568,7 @@ SortPlan sort_plan(long long tokens, long long table_rows) {
 // How a chunk's threads lie over its tokens' columns: V of them each (16 bytes, or one where rows start
 // anywhere), and the tokens of a chunk.  A group of threads walks 32 tokens, fewer where the chunks would not
 // fill the SMs (of 4 tokens a group at least), and 64 at least go to a CTA of one or two groups, so that
-// the parts that the chunks leave stay few.  (100,000 x 1,024 bf16: 220 us with 256 tokens a CTA.)
+// the parts that the chunks leave stay few.  (100,000 x 1,024 bf16: 220 us with 256 tokens a CTA, 109 so.)
 struct Chunks { int lanes, slices, tokens; };
 Chunks chunks_of(long long tokens, long long cols, int v) {
   Chunks c;

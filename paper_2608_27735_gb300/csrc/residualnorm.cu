@@ -8,6 +8,14 @@
 //   dw_after = s gate S2, db_after = s gate S1, dgate = s (w_after S2 + b_after S1).
 // Backward, y is made again from x and f: as many bytes as reading y, but in 32 bits, so that yh is the
 // forward pass's own.
+//
+// Bound by HBM in 32 bits (50,000 x 1,024: forward 127 us, 6.5 TB/s, backward 180, 6.8 TB/s), in 16 bits, with
+// twice the values for the bytes, also by instructions (100,000 x 1,024 bf16: 137 us, 6.0 TB/s, and 229, 5.4).
+// A row is read once: its threads hold it in registers, eight or sixteen values each, and the next rows are
+// copied to shared memory meanwhile.  Values go in pairs (one instruction for two), what lies past a row's
+// end is zero by the factors there and needs no tests, and the factors of the columns lie in shared memory
+// (in registers: 149 and 258 us).  One CTA per row that reads it again for each use took 6,615 us for both.
+// Rows that start anywhere are taken element by element from shared memory: 100,001 x 999 bf16 252 and 357.
 #include <algorithm>
 #include <type_traits>
 
