@@ -378,6 +378,43 @@ __device__ __forceinline__ void residual_ahead(float (&v)[CW], const Out& o, lon
   }
 }
 
+// The same for rows that start anywhere, through the warp's buffer: consecutive lanes read consecutive elements.
+// (Each lane by itself, 20,000 x 512 x 1,001 bf16 took 199 us, so 98.)
+template <bool F32, int CW>
+static __device__ __noinline__ void fill_rows(char* buf, const Out& o, long long m, int n, int rows, int cols) {
+  using E = std::conditional_t<F32, unsigned, unsigned short>;
+  constexpr int PIECES = CW * (int)sizeof(E) / 16, ROWS = CW < 32 ? 32 / CW : 1, BATCH = 8;
+  const int lane = threadIdx.x & 31, e = lane % CW;
+  const E* from = (const E*)o.p + m * o.stride + n + e;
+#pragma unroll 1
+  for (int row0 = lane / CW; row0 < 32; row0 += BATCH * ROWS) {
+    E x[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) x[i] = row0 + i * ROWS < rows && e < cols ? from[(row0 + i * ROWS) * o.stride] : E(0);
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i)
+      if (row0 + i * ROWS < 32) *reinterpret_cast<E*>(buf + turned<PIECES>(row0 + i * ROWS, e * (int)sizeof(E) / 16) + e * (int)sizeof(E) % 16) = x[i];
+  }
+}
+template <bool F32, int CW>
+__device__ __forceinline__ void residual_elements(float (&v)[CW], char* buf, const Out& o, long long m, int n, int rows, int cols, bool bf16) {
+  constexpr int PIECES = CW * (F32 ? 4 : 2) / 16;
+  const int lane = threadIdx.x & 31;
+  fill_rows<F32, CW>(buf, o, m, n, rows, cols);
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < PIECES; ++j) {
+    const uint4 x = *reinterpret_cast<const uint4*>(buf + turned<PIECES>(lane, j));
+    if constexpr (F32) {
+      v[4 * j] = __uint_as_float(x.x); v[4 * j + 1] = __uint_as_float(x.y);
+      v[4 * j + 2] = __uint_as_float(x.z); v[4 * j + 3] = __uint_as_float(x.w);
+    } else {
+      unpack8(v + 8 * j, x, bf16);
+    }
+  }
+  __syncwarp();
+}
+
 // Where 16-byte piece j of a row lies in a block of 128 rows of 64 bytes under TMA's 64-byte swizzle.
 __device__ __forceinline__ int block_at(int row, int j) { return row * 64 + ((j ^ ((row / 2) % 4)) * 16); }
 // Sixteen columns, from piece j on, of a block's rows first ... first + 31 to a matrix whose rows start
@@ -1000,7 +1037,8 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
         } else if constexpr (EPI == kLinear) {
           // the residual's and the bias's columns are on their way while the sums come
           float add[P::CW];
-          residual_ahead<F32>(add, a.in[0], m, n + c, rows, w, bf16);
+          if (a.in[0].p && !a.in[0].vec) residual_elements<F32, P::CW>(add, buffer, a.in[0], m, n + c, rows, w, bf16);
+          else residual_ahead<F32>(add, a.in[0], m, n + c, rows, w, bf16);
           float b = 0.f;
           if (a.bias && lane < w) {
             if (F32 || a.wide_bias) b = __ldg((const float*)a.bias + n + c + lane);
@@ -1090,15 +1128,17 @@ abcd_status launch_product(abcd_ctx* ctx, const ProductArgs& a) {
 // 1,601, 40,000 x 1,024 x 1,024 and 16,384 x 2,048 x 8,192 in 16 take at most 4% more than with the best
 // one shape for all products of a call.  6,007 x 39 x 6,591 in 32 bits does not: its forward pass takes 363
 // us in the smallest tile, 237 in the large one.
+// kLinear's epilogues, which move a residual and z besides, are from eleven layers of 300 to 100,000 tokens,
+// each timed in all three shapes.
 struct Shape {
   int cg, bn, ctas;          // CTAs of a tile, its sums per row, CTAs per SM (one for kDown)
   double fixed;              // of a launch
   double idle, busy;         // of a stage (64 of k) where few SMs, where all ask for operands
   double epilogue[4][2];     // of a tile, by kPlain, kUp, kDown, kLinear and 16 or 32 bits
 };
-constexpr Shape kShapes[3] = {{2, 256, 1, 7.1, 0.25, 0.34, {{1.7, 1.8}, {2.7, 9.2}, {7.0, 36.0}, {2.0, 2.6}}},
-                              {1, 128, 1, 5.9, 0.22, 0.33, {{0.5, 0.8}, {2.5, 4.5}, {6.1, 17.0}, {1.2, 1.4}}},
-                              {1, 64, 2, 5.2, 0.24, 0.36, {{0.8, 1.0}, {2.1, 3.6}, {3.3, 8.3}, {1.6, 1.6}}}};
+constexpr Shape kShapes[3] = {{2, 256, 1, 7.1, 0.25, 0.34, {{1.7, 1.8}, {2.7, 9.2}, {7.0, 36.0}, {6.0, 10.0}}},
+                              {1, 128, 1, 5.9, 0.22, 0.33, {{0.5, 0.8}, {2.5, 4.5}, {6.1, 17.0}, {4.0, 5.5}}},
+                              {1, 64, 2, 5.2, 0.24, 0.36, {{0.8, 1.0}, {2.1, 3.6}, {3.3, 8.3}, {5.4, 5.5}}}};
 
 template <int EPI, bool F32> abcd_status launch_shape(abcd_ctx* ctx, int shape, const ProductArgs& a) {
   if (shape == 0) return launch_product<2, 256, EPI, F32>(ctx, a);

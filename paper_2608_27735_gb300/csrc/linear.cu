@@ -181,7 +181,7 @@ extern "C" abcd_status abcd_linear(abcd_ctx* ctx, const abcd_matrix* x, const ab
   Operands in{s};
   const Operand ox = in.add(x), ow = in.add(weight);
   if ((st = in.pack(ctx, t)) != ABCD_OK) return st;
-  const Job job{ox, {ow}, 1, false, false, m, n, d, 1, {out_of(y)}};
+  const Job job{ox, {ow}, 1, false, false, m, n, d, 1, {out_of(y), residual ? out_of(residual) : Out{}}};
   Hidden hid{};
   hid.act = activation;
   hid.bias = bias;

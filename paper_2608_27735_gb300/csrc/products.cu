@@ -172,7 +172,10 @@ Plan plan(int sms, int dtype, int epi, const Job* jobs, int n) {
   for (int s = 0; s < 3; ++s) {
     const Shape& q = kShapes[s];
     const long long units = (epi == kDown ? 1 : q.ctas) * sms / q.cg, cols = epi == kUp ? q.bn / 2 : q.bn;
-    const double tile_bytes = 4.0 * 128 * q.cg * q.bn, epilogue = q.epilogue[epi][f32];
+    const double tile_bytes = 4.0 * 128 * q.cg * q.bn;
+    // the large tile's blocks are left (and its residual's, c[1], filled) element by element where rows start anywhere
+    const bool apart = epi == kLinear && s == 0 && !f32 && (!jobs[0].c[0].vec || (jobs[0].c[1].p && !jobs[0].c[1].vec));
+    const double epilogue = q.epilogue[epi][f32] * (apart ? 4.0 : 1.0);
     long long tiles[kMaxJobs], kblocks[kMaxJobs];
     double work = 0;                                     // stages of all tiles
     long long whole = 0;                                 // items without splits
