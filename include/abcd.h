@@ -541,7 +541,8 @@ abcd_status abcd_dropout_backward(abcd_ctx* ctx, const abcd_matrix* dy, double p
 /* ---- tokens of that network: lookups, products, the sums between blocks, what is kept ------- *
  * The rules of the calls above hold here too: types, rows, 32-bit sums, one rounding, the same result
  * in every run.  Each call that takes scratch names the function that says how much; the network
- * workspace is one for all of them, as large as the largest needs. */
+ * workspace is one for all of them, as large as the largest needs.  Graphs captured from one context share it, so
+ * their replays are ordered as its calls are; what is to run side by side takes a context each. */
 
 /* Types of an index vector. */
 enum { ABCD_I32 = 3, ABCD_I64 = 4 };

@@ -233,7 +233,7 @@ def abcd_linear_backward(ctx: Context, dy, x, weight, activation, z, dx=None, dw
         ctx.check(st)
 
 
-@dataclass
+@dataclass(slots=True)
 class Norm:
     """A norm of abcd_residual_norm: kind "layer" or "rms"; weight, bias: [cols] or None; mean, rstd:
     float32 [rows] that the backward pass needs, or None (an rms norm has no mean; one that is given is
@@ -249,16 +249,21 @@ class Norm:
 _pack_norm = struct.Struct("@iPPfPP").pack           # the bytes of an abcd_norm
 
 
-def _norm(q, rows, cols, dtype, what):
+_AFTER = "after.weight", "after.bias", "after.mean", "after.rstd"
+_BEFORE = "before.weight", "before.bias", "before.mean", "before.rstd"
+
+
+def _norm(q, rows, cols, dtype, names):
     if q is None:
         return None
     kind = NORMS.get(q.kind)
     if kind is None:
         raise ValueError(f"unknown norm {q.kind!r}; one of {sorted(NORMS)}")
-    return _pack_norm(kind, _vector(q.weight, cols, what + ".weight", dtype) or 0,
-                      _vector(q.bias, cols, what + ".bias", dtype) or 0, q.eps,
-                      _vector(q.mean, rows, what + ".mean", _F32) or 0 if kind == ABCD_LAYER_NORM else 0,
-                      _vector(q.rstd, rows, what + ".rstd", _F32) or 0)
+    w, b, m, r = q.weight, q.bias, q.mean, q.rstd
+    return _pack_norm(kind, 0 if w is None else _vector(w, cols, names[0], dtype),
+                      0 if b is None else _vector(b, cols, names[1], dtype), q.eps,
+                      0 if m is None or kind == ABCD_RMS_NORM else _vector(m, rows, names[2], _F32),
+                      0 if r is None else _vector(r, rows, names[3], _F32))
 
 
 def _norm_vectors(after, before):
@@ -272,8 +277,8 @@ def abcd_residual_norm(ctx: Context, x, f, after, before, gate, scale, y, n=None
     call = _call("abcd_residual_norm")
     mx, rows, cols = _matrix(x, "x")
     wt = _weight_type(x, gate, *_norm_vectors(after, before))
-    st = call(ctx.h, mx, _matrix(f, "f")[0], _norm(after, rows, cols, wt, "after"),
-              _norm(before, rows, cols, wt, "before"), _vector(gate, cols, "gate", wt), _KINDS[wt], scale,
+    st = call(ctx.h, mx, _matrix(f, "f")[0], _norm(after, rows, cols, wt, _AFTER),
+              _norm(before, rows, cols, wt, _BEFORE), _vector(gate, cols, "gate", wt), _KINDS[wt], scale,
               _matrix(y, "y")[0], _optional(n, "n"))
     if st:
         ctx.check(st)
@@ -291,7 +296,7 @@ def abcd_residual_norm_backward(ctx: Context, dy, dn, x, f, after, before, gate,
                       *_norm_vectors(after, before))
     v = lambda t, what: _vector(t, cols, what, wt)
     st = call(ctx.h, _optional(dy, "dy"), _optional(dn, "dn"), mx, _matrix(f, "f")[0],
-              _norm(after, rows, cols, wt, "after"), _norm(before, rows, cols, wt, "before"),
+              _norm(after, rows, cols, wt, _AFTER), _norm(before, rows, cols, wt, _BEFORE),
               v(gate, "gate"), _KINDS[wt], scale, _optional(dx, "dx"), _optional(df, "df"),
               v(dgate, "dgate"), v(dafter_weight, "dafter_weight"), v(dafter_bias, "dafter_bias"),
               v(dbefore_weight, "dbefore_weight"), v(dbefore_bias, "dbefore_bias"))
