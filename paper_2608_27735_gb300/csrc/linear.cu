@@ -5,8 +5,7 @@
 // the matrices' type, in 32 bits as three terms) and its columns' sums, and both products are one launch.
 // 16,384 x 4,096 x 4,096 bf16: forward with residual and z 332 us (1,660 TFLOP/s), the pass over dy and z 67 (6.0
 // TB/s), both products 600 (1,830).  100,000 x 256 x 256 bf16: 49 us (5.2 TB/s; six rounds of tiles for 5.1) and 72.
-// 20,000 x 59 x 256 fp32 with gelu: 28 us of the forward pass are two rounds of tiles whose epilogues take the
-// error function, 5 pack the operands.
+// 20,000 x 59 x 256 fp32 with gelu: 29 and 44 us, nine launches; the forward product is three rounds of tiles.
 #include "products.cuh"
 
 namespace abcd {
@@ -61,7 +60,7 @@ __global__ void __launch_bounds__(256) slope_kernel(const __grid_constant__ Slop
       if (a.z) {
         float z[8], s[8];
         load8(z, (const T*)a.z + r * a.sz + c, left, a.vec);
-        act_slopes<F32>(z, s, a.act);
+        act_slopes<F32, 8, true>(z, s, a.act);
 #pragma unroll
         for (int e = 0; e < 8; ++e) d[e] *= s[e];
       }

@@ -263,6 +263,32 @@ def test_linear(ctx, kind, rows, cols, out, name, pad, lead):
         assert torch.equal(one, want)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows", [5, 300])
+def test_linear_gelu_far_below_zero(ctx, kind, rows):
+    """gelu and its slope at -9 ... 3 are as exact as elsewhere relative to themselves, through unit matrices.
+    The exponential's argument z^2 / 2 is rounded twice and its factor once (0.7 z^2 EPS), the functions,
+    products and, of 16-bit matrices, the polynomial (1.8e-5) add what tests/test_gpu_network_edges.py says; the
+    products through unit matrices are sums of up to three terms that are not zero (less than that again), and
+    dz is rounded to its type before dx is."""
+    from .test_gpu_network_edges import TAIL, gelu_parts
+    d = 64
+    r = np.random.default_rng(rows)
+    x, one = matrix(r.uniform(-9, 3, (rows, d)), kind), matrix(np.eye(d), kind)
+    y, z, dx = (blank(rows, d, kind) for _ in range(3))
+    ctx.reserve_linear(rows, d, d, TYPES[kind])
+    ab.abcd_linear(ctx, x, one, None, "gelu", y, None, z)
+    ab.abcd_linear_backward(ctx, matrix(np.ones((rows, d)), kind), x, one, "gelu", z, dx)
+    ctx.sync()
+    v = f64(x)
+    assert (f64(z) == v).all()
+    cdf, zphi, rel = gelu_parts(v)
+    rel = rel + TAIL[kind]
+    for got, want, mag in ((y, v * cdf, np.abs(v) * cdf), (dx, cdf + zphi, cdf + np.abs(zphi))):
+        wide = mag * rel
+        close(got, want, 2 * wide + 2 * (np.abs(want) + wide) * N.UNIT[kind] + N.TINY[kind])
+
+
 @pytest.mark.parametrize("rows,cols,out", [(50, 64, 96), (5000, 256, 1024)])
 def test_linear_with_matrices_of_different_starts(ctx, rows, cols, out):
     """Each of residual, y and z on 16-byte boundaries or not."""
