@@ -10,7 +10,7 @@
 // forward pass's own.
 //
 // Bound by HBM in 32 bits (50,000 x 1,024: forward 127 us, 6.5 TB/s, backward 180, 6.8 TB/s), in 16 bits, with
-// twice the values for the bytes, also by instructions (100,000 x 1,024 bf16: 137 us, 6.0 TB/s, and 229, 5.4).
+// twice the values for the bytes, also by instructions (100,000 x 1,024 bf16: 139 us, 5.9 TB/s, and 235, 5.2).
 // A row is read once: its threads hold it in registers, eight or sixteen values each, and the next rows are
 // copied to shared memory meanwhile.  Values go in pairs (one instruction for two), what lies past a row's
 // end is zero by the factors there and needs no tests, and the factors of the columns lie in shared memory
@@ -334,8 +334,8 @@ template <typename T, typename R> struct CloseRows {
     row += step;
   }
   // The thread's values of the row at hand of a matrix: zeros past its end, of no row and of a matrix that is
-  // not there.
-  __device__ __forceinline__ void get(float2 (&pairs)[R::E / 2], int t, int mat) const {
+  // not there.  (Rows that start anywhere: `none`.)
+  __device__ __forceinline__ void get(float2 (&pairs)[R::E / 2], int t, int mat, float none = 0.f) const {
     float v[R::E];
     if constexpr (R::VEC) {
 #pragma unroll
@@ -348,7 +348,7 @@ template <typename T, typename R> struct CloseRows {
       const bool there = base(mat) != nullptr && (R::TPR >= 32 || t < rows);
       const T* p = (const T*)(pieces(now, mat) + ((uintptr_t)start_of(mat, row) & 15)) + lane;
 #pragma unroll
-      for (int e = 0; e < R::E; ++e) v[e] = there && column(e) < cols ? to_f32(p[e * R::TPR]) : 0.f;
+      for (int e = 0; e < R::E; ++e) v[e] = there && column(e) < cols ? to_f32(p[e * R::TPR]) : none;
     }
 #pragma unroll
     for (int e = 0; e < R::E / 2; ++e) pairs[e] = make_float2(v[2 * e], v[2 * e + 1]);
@@ -435,6 +435,15 @@ __device__ __forceinline__ Stat stat_of_row(const CloseRows<T, R>& rows, const f
   return Stat{mean + off, rstd_of(q * inv, off, eps)};
 }
 
+// What a row's deviations are multiplied by: rstd, or zero where the mean times it is infinite.  Such a row is of
+// one value (a single other one, a step of fp32 away, would leave rstd below 2^24 sqrt(cols) / mean), so
+// nothing deviates; but past the row's end zeros lie, and what they would be, an infinity, times the factors'
+// zeros is NaN.  (An infinite rstd stays.)
+__device__ __forceinline__ float factor_of_row(const Stat& s) {
+  constexpr float kMost = 3.402823466e38f;
+  return fabsf(s.mean) * s.rstd > kMost && s.rstd <= kMost ? 0.f : s.rstd;
+}
+
 // The factors of the columns to shared memory, by the CTA's first group: [factor][four values][thread of a row].
 template <typename T, typename R> __device__ __forceinline__ void set_factors(CloseRows<T, R>& rows, const CloseArgs& a) {
   if (R::kHold || threadIdx.x < R::TPR) {
@@ -481,11 +490,12 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_fwd_kernel(const 
     rows.get(x, t, 1);
     Stat first{0.f, 1.f}, second{0.f, 1.f};
     if (a.kind[0] != kNone) first = stat_of_row(rows, f, a.kind[0], a.eps[0], inv, red, half);
+    const float2 spread = both(factor_of_row(first));
 #pragma unroll
     for (int e = 0; e < P; e += 2) {
       const float4 A = factor_of(rows, 0, e / 2), C = factor_of(rows, 1, e / 2);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) x[e + h] = close_pair(x[e + h], mul2(sub2(f[e + h], first.mean), both(first.rstd)), half_of(A, h), half_of(C, h));
+      for (int h = 0; h < 2; ++h) x[e + h] = close_pair(x[e + h], mul2(sub2(f[e + h], first.mean), spread), half_of(A, h), half_of(C, h));
     }
     if (a.kind[1] != kNone) {
       second = stat_of_row(rows, x, a.kind[1], a.eps[1], inv, red, half);
@@ -538,14 +548,18 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
       next[1] = stat_of(a, 1, rows.row + rows.step);
     }
     float2 fh[P], g[P], p1 = both(0.f), p2 = both(0.f);
-    rows.get(fh, t, 0);
+    // past the end of a row that starts anywhere the mean, which costs no more than zero there (the other factor
+    // would: 100,001 x 999 bf16 377 us instead of 357)
+    rows.get(fh, t, 0, first.mean);
     rows.get(g, t, 2);
+    const float2 spread = both(R::VEC ? factor_of_row(first) : first.rstd);
 #pragma unroll
-    for (int e = 0; e < P; ++e) fh[e] = mul2(sub2(fh[e], first.mean), both(first.rstd));
+    for (int e = 0; e < P; ++e) fh[e] = mul2(sub2(fh[e], first.mean), spread);
     if (a.dn) {
       float2 yh[P], dn[P];
-      rows.get(yh, t, 1);
+      rows.get(yh, t, 1, second.mean);
       rows.get(dn, t, 3);
+      const float2 spread = both(R::VEC ? factor_of_row(second) : second.rstd);
 #pragma unroll
       for (int e = 0; e < P; e += 2) {
         const float4 A = factor_of(rows, 0, e / 2), C = factor_of(rows, 1, e / 2), W = factor_of(rows, 2, e / 2);
@@ -553,7 +567,7 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
         for (int h = 0; h < 2; ++h) {
           const int i = e + h;
           // the forward pass's, bit for bit
-          yh[i] = mul2(sub2(close_pair(yh[i], fh[i], half_of(A, h), half_of(C, h)), second.mean), both(second.rstd));
+          yh[i] = mul2(sub2(close_pair(yh[i], fh[i], half_of(A, h), half_of(C, h)), second.mean), spread);
           sums[2][i] = add2(sums[2][i], dn[i]);
           sums[3][i] = fma2(dn[i], yh[i], sums[3][i]);
           dn[i] = mul2(dn[i], half_of(W, h));

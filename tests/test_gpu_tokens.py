@@ -445,6 +445,39 @@ def test_residual_norm_of_rows_without_spread(ctx):
     ctx.sync()
 
 
+@pytest.mark.parametrize("cols", [59, 60, 200, 1000, 1001])
+@pytest.mark.parametrize("kind", KINDS)
+def test_residual_norm_of_rows_of_one_great_value(ctx, kind, cols):
+    """Such a row deviates by nothing, and its mean times rstd is beyond 32 bits: nothing of what a thread holds
+    past the row's end may come of that.  (Powers of two, so that the sums are exact; fp16 has no such values.)"""
+    level = 2.0 ** 9 if kind == "f16" else 2.0 ** 117
+    eps = 1e-30 if kind == "f16" else 1e-7
+    dtype = TYPES[kind]
+    m = 5
+    x, zero, y, n, dx, df = (torch.zeros(m, cols, device="cuda", dtype=dtype) for _ in range(6))
+    f = torch.full((m, cols), level, device="cuda", dtype=dtype)
+    x[:, ::2], x[:, 1::2] = 1.0, -1.0
+    one, b = torch.ones(cols, device="cuda"), torch.full((cols,), 0.25, device="cuda")
+    ctx.reserve_residual_norm(m, cols)
+    s = torch.empty(4, m, device="cuda")
+    # the norm that closes the block: its rows are its bias
+    after, before = ab.Norm("layer", one, b, eps, s[0], s[1]), ab.Norm("rms", one, None, 1e-5, None, s[3])
+    ab.abcd_residual_norm(ctx, x, f, after, before, None, 1.0, y, n)
+    assert torch.equal(y, x + 0.25)
+    want = (x + 0.25).double()
+    want = want / (want.square().mean(1, keepdim=True) + 1e-5).sqrt()
+    assert ((n.double() - want).abs() <= (N.UNIT[kind] + 16 * N.EPS) * want.abs()).all()     # the sums of squares are exact
+    ab.abcd_residual_norm_backward(ctx, zero, zero, x, f, after, before, None, 1.0, dx, df)
+    assert (dx == 0).all() and (df == 0).all()
+    # the next block's norm
+    after, before = None, ab.Norm("layer", one, b, eps, s[2], s[3])
+    ab.abcd_residual_norm(ctx, f, zero, after, before, None, 1.0, y, n)
+    assert torch.equal(y, f) and (n == 0.25).all()
+    w = [torch.empty(cols, device="cuda") for _ in range(2)]
+    ab.abcd_residual_norm_backward(ctx, x, zero, f, zero, after, before, None, 1.0, dx, df, None, None, None, *w)
+    assert torch.equal(dx, x) and torch.equal(df, x) and not any(v.any() for v in w)
+
+
 def test_residual_norm_without_rows(ctx):
     w, d = torch.ones(40, device="cuda"), [torch.ones(40, device="cuda") for _ in range(5)]
     e = torch.empty(0, 40, device="cuda")
