@@ -405,6 +405,7 @@ static __device__ __noinline__ void fill_rows(char* buf, const Out& o, long long
   constexpr int PIECES = CW * (int)sizeof(E) / 16, ROWS = CW < 32 ? 32 / CW : 1, BATCH = 8;
   const int lane = threadIdx.x & 31, e = lane % CW;
   const E* from = (const E*)o.p + m * o.stride + n + e;
+  __syncwarp();                                   // the turn before reads its results from the buffer
 #pragma unroll 1
   for (int row0 = lane / CW; row0 < 32; row0 += BATCH * ROWS) {
     E x[BATCH];

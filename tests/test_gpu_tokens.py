@@ -313,6 +313,25 @@ def test_linear_with_matrices_of_different_starts(ctx, rows, cols, out):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,out", [(300, 201), (5000, 131), (20001, 259), (40003, 515)])
+def test_linear_over_residuals_that_start_anywhere(ctx, kind, rows, out):
+    """In tiles of every width, whose warps take their columns in several turns: the residual's columns of a turn
+    and the results of the one before go through the same shared memory.  Whole numbers: exact."""
+    r = np.random.default_rng(rows)
+    whole = lambda shape, most, pad=0: matrix(r.integers(-most, most + 1, shape).astype(float), kind, pad)
+    x, w, res, b = whole((rows, 16), 1), whole((out, 16), 1), whole((rows, out), 9, 3), whole((1, out), 3)[0]
+    want = (x.float() @ w.float().T + b.float() + res.float()).to(TYPES[kind])          # up to 28
+    ctx.reserve_linear(rows, 16, out, TYPES[kind])
+    for pad in (0, 3):
+        y = blank(rows, out, kind, pad)
+        ab.abcd_linear(ctx, x, w, b, "none", y, res)
+        assert torch.equal(y, want) and gaps_untouched(y)
+    ab.abcd_linear(ctx, x, w, b, "none", res, res)
+    assert torch.equal(res, want) and gaps_untouched(res)
+    ctx.sync()
+
+
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("rows", [3, 300])
 def test_linear_over_its_residual_and_without_rows(ctx, kind, rows):
     r = np.random.default_rng(6)
