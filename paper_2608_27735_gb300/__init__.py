@@ -377,6 +377,10 @@ class Context:
         for t in tensors:
             t.record_stream(self.stream)
 
+    def on_stream(self):
+        """`with ctx.on_stream():` runs torch's operations on the context's stream, in order with its calls."""
+        return _torch().cuda.stream(self.stream)
+
     def reserve(self, max_gaussians, max_pairs, max_pixels):
         """(Re)allocates the workspace if the limits grew."""
         torch = _torch()

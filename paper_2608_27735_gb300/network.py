@@ -488,7 +488,8 @@ class NormedStack:
                 x = at
             return
         self.kept = None
-        self.x[0][:n].copy_(x)
+        with ctx.on_stream():
+            self.x[0][:n].copy_(x)
         s = self.stats[0]
         abcd_layer_norm(ctx, self.x[0][:n], first["before_w"], first["before_b"], self.eps, self.normed[0][:n], s[0, :n], s[1, :n])
         for k, w in enumerate(self.w):

@@ -166,6 +166,40 @@ def test_tokens_train_with_a_render(packed):
 
 # ---- streams, graphs, workspaces
 
+@pytest.mark.parametrize("packed", [False, True])
+def test_stack_on_a_stream_of_its_own(packed):
+    """Two training passes, called while the current stream is another one: each takes its input as the
+    context's stream leaves it, after the pass before has read its own."""
+    r = np.random.default_rng(12)
+    rows, cols, ff = 3000, 64, 128
+    w = block_weights(r, cols, ff)
+    inputs = [[matrix(r.normal(size=(rows, cols)), "f32") for _ in range(2)] for _ in range(2)]
+
+    def passes(ctx):
+        stack = ab.NormedStack(ctx, w, rows, packed=packed)
+        out = [[torch.full_like(inputs[0][0], float("nan")) for _ in range(2)] + [{k: torch.zeros_like(t) for k, t in g.items()} for g in stack.grads]
+               for _ in range(2)]
+        x = torch.full_like(inputs[0][0], float("nan"))
+        torch.cuda.synchronize()
+        for (given, dy), (y, dx, *grads) in zip(inputs, out):
+            with torch.cuda.stream(ctx.stream):
+                torch.cuda._sleep(10_000_000)
+                x.copy_(given)
+            stack.forward(x, y)
+            stack.backward(dy, dx)
+            with torch.cuda.stream(ctx.stream):
+                for a, b in zip(grads, stack.grads):
+                    for k in a:
+                        a[k].copy_(b[k])
+        ctx.sync()
+        torch.cuda.synchronize()
+        return [t for y, dx, *grads in out for t in (y, dx, *(v for g in grads for v in g.values()))]
+
+    want = passes(ab.Context(0))
+    assert torch.isfinite(want[0]).all() and not torch.equal(want[0], want[len(want) // 2])
+    assert all(torch.equal(a, b) for a, b in zip(passes(ab.Context(0, torch.cuda.Stream())), want))
+
+
 def every_call(ctx, t):
     """Each token operator once, over the tensors of operands()."""
     ab.abcd_embedding(ctx, t["table"], t["at"], 0.7, t["tokens"], t["x"])

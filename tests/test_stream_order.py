@@ -1,0 +1,78 @@
+"""Classes that mix the library's calls with torch's operations, on a context whose stream is not the current
+one: every operation that reads or writes a tensor is queued on the context's stream.  Without a GPU: the
+calls do nothing, the tensors lie in host memory, and the operations say where they would have run."""
+import contextlib
+
+import pytest
+
+from paper_2608_27735_gb300 import network
+
+torch = pytest.importorskip("torch")
+from torch.utils._python_dispatch import TorchDispatchMode  # noqa: E402
+
+# operations that neither read nor write elements
+STILL = {"slice", "select", "view", "_unsafe_view", "alias", "detach", "as_strided", "unsqueeze", "expand", "t", "transpose",
+         "empty", "empty_like", "new_empty", "empty_strided", "split", "split_with_sizes", "_reshape_alias"}
+
+
+class FakeContext:
+    """A context with a stream of its own."""
+
+    def __init__(self):
+        self.depth, self.held = 0, []
+
+    def hold(self, *tensors):
+        self.held += tensors
+
+    @contextlib.contextmanager
+    def on_stream(self):
+        self.depth += 1
+        yield
+        self.depth -= 1
+
+    def __getattr__(self, name):
+        if name.startswith("reserve"):
+            return lambda *sizes: None
+        raise AttributeError(name)
+
+
+class Watch(TorchDispatchMode):
+    """Collects the operations that ran elsewhere than on the context's stream, and counts those on it."""
+
+    def __init__(self, ctx):
+        super().__init__()
+        self.ctx, self.astray, self.there = ctx, [], 0
+
+    def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+        name = func._schema.name.split("::")[-1]
+        if name not in STILL:
+            if self.ctx.depth:
+                self.there += 1
+            else:
+                self.astray.append(name)
+        return func(*args, **(kwargs or {}))
+
+
+@pytest.fixture
+def ctx(monkeypatch):
+    for name in dir(network):
+        if name.startswith("abcd_"):
+            monkeypatch.setattr(network, name, lambda *a, **k: None)
+    return FakeContext()
+
+
+def block_weights(cols, ff):
+    return {**{k: torch.zeros(cols) for k in ("before_w", "before_b", "after_w", "gate")},
+            "w_gate": torch.zeros(ff, cols), "w_up": torch.zeros(ff, cols), "w_down": torch.zeros(cols, ff)}
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_stack(ctx, packed):
+    stack = network.NormedStack(ctx, [block_weights(8, 16) for _ in range(2)], 5, packed=packed)
+    x, y = torch.zeros(4, 8), torch.zeros(4, 8)
+    with Watch(ctx) as watch:
+        for _ in range(2):
+            stack.forward(x, y)
+            stack.forward(x, y, train=False)
+            stack.backward(x, y)
+    assert not watch.astray and watch.there == 2
