@@ -35,6 +35,7 @@ class Adam:
         n = (int(length) + 13) // 14
         self.values, self.grads = (torch.zeros(14 * n, device=device) for _ in range(2))
         m, v = (torch.zeros(14 * n, device=device) for _ in range(2))
+        ctx.hold(self.values, self.grads, m, v)
         self.parts = [self._parts(t, n) for t in (self.values, self.grads, m, v)]
 
     @staticmethod
@@ -175,30 +176,36 @@ class TokenAppearance:
         w, ctx = self.w, self.ctx
         tokens = self.tokens if train else self.d
         result = self.result if train else self.d
-        x = sh.reshape(self.n, self.sh_cols)
-        if train:
-            self.x.copy_(x)
-        self.seen.fill_(ci)
-        abcd_linear(ctx, x, w["w_in"], w["b_in"], "none", tokens)
-        abcd_embedding(ctx, w["cameras"], self.seen, 1.0, tokens, tokens)
-        abcd_embedding(ctx, w["cells"], self.cell, 1.0, tokens, tokens)
-        self.stack.forward(tokens, result, train)
-        out = _torch().empty_like(x)
-        abcd_linear(ctx, result, w["w_out"], w["b_out"], "none", out, x)
-        return out.reshape(sh.shape)
+        out = _torch().empty_like(self.x)
+        ctx.hold(out)
+        with ctx.on_stream():                           # (what reshape copies, too)
+            x = sh.reshape(self.n, self.sh_cols)
+            if train:
+                self.x.copy_(x)
+            self.seen.fill_(ci)
+            abcd_linear(ctx, x, w["w_in"], w["b_in"], "none", tokens)
+            abcd_embedding(ctx, w["cameras"], self.seen, 1.0, tokens, tokens)
+            abcd_embedding(ctx, w["cells"], self.cell, 1.0, tokens, tokens)
+            self.stack.forward(tokens, result, train)
+            abcd_linear(ctx, result, w["w_out"], w["b_out"], "none", out, x)
+        return out.view(sh.shape)
 
     def backward(self, d_sh, ci):
         """The gradient of sh from that of the last training forward(sh, ci)'s result; leaves the weights'
         gradients in Adam's buffer."""
         w, g, ctx = self.w, self.g, self.ctx
-        d = d_sh.reshape(self.n, self.sh_cols)
-        abcd_linear_backward(ctx, d, self.result, w["w_out"], "none", None, self.d, g["w_out"], g["b_out"])
-        self.stack.backward(self.d, self.d)
-        self.seen.fill_(ci)
-        abcd_embedding_backward(ctx, self.d, self.seen, 1.0, g["cameras"])
-        abcd_embedding_backward(ctx, self.d, self.cell, 1.0, g["cells"])
-        abcd_linear_backward(ctx, self.d, self.x, w["w_in"], "none", None, self.d_sh, g["w_in"], g["b_in"])
-        return (self.d_sh + d).reshape(d_sh.shape)
+        out = _torch().empty_like(self.x)
+        ctx.hold(out)
+        with ctx.on_stream():
+            d = d_sh.reshape(self.n, self.sh_cols)
+            abcd_linear_backward(ctx, d, self.result, w["w_out"], "none", None, self.d, g["w_out"], g["b_out"])
+            self.stack.backward(self.d, self.d)
+            self.seen.fill_(ci)
+            abcd_embedding_backward(ctx, self.d, self.seen, 1.0, g["cameras"])
+            abcd_embedding_backward(ctx, self.d, self.cell, 1.0, g["cells"])
+            abcd_linear_backward(ctx, self.d, self.x, w["w_in"], "none", None, self.d_sh, g["w_in"], g["b_in"])
+            _torch().add(self.d_sh, d, out=out)
+        return out.view(d_sh.shape)
 
     def step(self):
         self.adam.step()

@@ -240,6 +240,41 @@ def outputs(t):
     return [t[k] for k in OUTPUTS] + t["dv"] + t["g"] + [t["packed"].codes, t["packed"].powers]
 
 
+@pytest.mark.parametrize("packed", [False, True])
+def test_appearance_on_a_stream_of_its_own(packed):
+    """Training and other passes, called while the current stream is another one, whose memory they take."""
+    from paper_2608_27735_gb300.appearance import TokenAppearance
+    n, cams = 2000, 3
+    r = np.random.default_rng(13)
+    means = r.uniform(-2, 2, (n, 3)).astype(np.float32)
+    inputs = [[torch.from_numpy(r.normal(size=(n, 4, 4)).astype(np.float32)).cuda()[:, :, :3] for _ in range(2)] for _ in range(3)]
+
+    def passes(ctx):
+        app = TokenAppearance(ctx, means, 1, cams, width=24, packed=packed, seed=4)
+        given = torch.full_like(inputs[0][0], float("nan"))
+        kept = []
+        torch.cuda.synchronize()
+        for ci, (sh, d) in enumerate(inputs):
+            with torch.cuda.stream(ctx.stream):
+                torch.cuda._sleep(10_000_000)
+                given.copy_(sh)
+                app.w["w_out"].add_(0.01)
+            kept.append(app.forward(given, ci))
+            other = app.forward(given, 0, train=False)
+            del other                                   # its memory is the current stream's to use again
+            spoiled = [torch.full((n, 12), float("nan"), device="cuda") for _ in range(8)]
+            del spoiled
+            kept.append(app.backward(d, ci))
+            app.step()
+        ctx.sync()
+        torch.cuda.synchronize()
+        return [*kept, app.adam.values.clone()]
+
+    want = passes(ab.Context(0))
+    assert all(torch.isfinite(t).all() for t in want)
+    assert all(torch.equal(a, b) for a, b in zip(passes(ab.Context(0, torch.cuda.Stream())), want))
+
+
 def test_captured_and_replayed_with_other_inputs(ctx):
     """A graph of every call takes what its inputs hold when it runs."""
     stream = torch.cuda.Stream()

@@ -5,7 +5,7 @@ import contextlib
 
 import pytest
 
-from paper_2608_27735_gb300 import network
+from paper_2608_27735_gb300 import appearance, network
 
 torch = pytest.importorskip("torch")
 from torch.utils._python_dispatch import TorchDispatchMode  # noqa: E402
@@ -55,9 +55,10 @@ class Watch(TorchDispatchMode):
 
 @pytest.fixture
 def ctx(monkeypatch):
-    for name in dir(network):
-        if name.startswith("abcd_"):
-            monkeypatch.setattr(network, name, lambda *a, **k: None)
+    for module in (network, appearance):
+        for name in dir(module):
+            if name.startswith("abcd_"):
+                monkeypatch.setattr(module, name, lambda *a, **k: None)
     return FakeContext()
 
 
@@ -76,3 +77,30 @@ def test_stack(ctx, packed):
             stack.forward(x, y, train=False)
             stack.backward(x, y)
     assert not watch.astray and watch.there == 2
+
+
+def bare(cls, **fields):
+    """An instance without its constructor, which takes a GPU."""
+    self = cls.__new__(cls)
+    vars(self).update(fields)
+    return self
+
+
+def test_token_appearance(ctx):
+    """And what it returns is held: the library's calls write it on the context's stream."""
+    n, width, cols = 4, 8, 12
+    new = lambda c: torch.zeros(n, c)
+    weights = dict.fromkeys(("w_in", "b_in", "cameras", "cells", "w_out", "b_out"))
+    app = bare(appearance.TokenAppearance, ctx=ctx, n=n, width=width, sh_cols=cols, w=weights, g=weights, seen=torch.zeros(n, dtype=torch.int32),
+               cell=torch.zeros(n, dtype=torch.int32), tokens=new(width), result=new(width), d=new(width), x=new(cols), d_sh=new(cols),
+               stack=network.NormedStack(ctx, [block_weights(width, 16)], n))
+    for sh in (torch.zeros(n, 4, 3), torch.zeros(n, 4, 4)[:, :, :3]):      # the second is copied to be a matrix
+        with Watch(ctx) as watch:
+            out = app.forward(sh, 1), app.forward(sh, 0, train=False), app.backward(sh, 1)
+        assert not watch.astray and watch.there >= 6
+        assert all(t.shape == sh.shape and any(t.data_ptr() == h.data_ptr() for h in ctx.held) for t in out)
+
+
+def test_adam_holds_its_buffers(ctx):
+    adam = appearance.Adam(ctx, 20, 1e-3, "cpu")
+    assert {t.data_ptr() for t in ctx.held} == {p.means.data_ptr() for p in adam.parts}
