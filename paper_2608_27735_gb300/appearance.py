@@ -88,27 +88,36 @@ class Appearance:
         self.embed.copy_(torch.from_numpy(rng.normal(0, 1, (n_cameras, embed)).astype(np.float32)))
         self.x = [torch.empty(n, self.cols, device="cuda") for _ in range(layers + 1)]
         self.dx = torch.empty(n, self.cols, device="cuda")
+        ctx.hold(*self.x, self.dx)
 
     def forward(self, sh, ci, train=True):
         """The coefficients that camera ci sees of sh [n][D][3]: a new tensor of that shape."""
         # without training in place, in the backward pass's buffer: what the last training pass kept stays
         x = self.x if train else [self.dx] * len(self.x)
-        x[0][:, :self.sh_cols] = sh.reshape(self.n, self.sh_cols)
-        x[0][:, self.sh_cols:] = self.embed[ci]
-        for k, block in enumerate(self.blocks):
-            block.forward(x[k], x[k + 1], train)
-        return x[-1][:, :self.sh_cols].reshape(sh.shape).contiguous()
+        out = _torch().empty(self.n, self.sh_cols, device=self.dx.device)
+        self.ctx.hold(out)
+        with self.ctx.on_stream():
+            x[0][:, :self.sh_cols] = sh.reshape(self.n, self.sh_cols)
+            x[0][:, self.sh_cols:] = self.embed[ci]
+            for k, block in enumerate(self.blocks):
+                block.forward(x[k], x[k + 1], train)
+            out.copy_(x[-1][:, :self.sh_cols])
+        return out.view(sh.shape)
 
     def backward(self, d_sh, ci):
         """The gradient of sh from that of the last training forward(sh, ci)'s result; leaves the
         weights' and the embeddings' gradients in Adam's buffer."""
-        self.dx[:, :self.sh_cols] = d_sh.reshape(self.n, self.sh_cols)
-        self.dx[:, self.sh_cols:] = 0.0
-        for k in reversed(range(len(self.blocks))):
-            self.blocks[k].backward(self.dx, self.x[k], self.dx)
-        self.d_embed.zero_()
-        self.d_embed[ci] = self.dx[:, self.sh_cols:].sum(0)
-        return self.dx[:, :self.sh_cols].reshape(d_sh.shape).contiguous()
+        out = _torch().empty(self.n, self.sh_cols, device=self.dx.device)
+        self.ctx.hold(out)
+        with self.ctx.on_stream():
+            self.dx[:, :self.sh_cols] = d_sh.reshape(self.n, self.sh_cols)
+            self.dx[:, self.sh_cols:] = 0.0
+            for k in reversed(range(len(self.blocks))):
+                self.blocks[k].backward(self.dx, self.x[k], self.dx)
+            self.d_embed.zero_()
+            self.d_embed[ci] = self.dx[:, self.sh_cols:].sum(0)
+            out.copy_(self.dx[:, :self.sh_cols])
+        return out.view(d_sh.shape)
 
     def step(self):
         self.adam.step()
@@ -267,19 +276,22 @@ class AppearanceStage:
                       ABCD_F32, None, self.out, self.state, self.photos[ci], 0.2, self.loss, None,
                       self.grads)
         if self.appearance is not None:
-            self.grads.sh.copy_(self.appearance.backward(self.grads.sh, ci))
+            d_sh = self.appearance.backward(self.grads.sh, ci)
+            with self.ctx.on_stream():
+                self.grads.sh.copy_(d_sh)
             self.appearance.step()
         abcd_adam_active(self.ctx, self.theta, self.grads, self.m, self.v, self.lr, 0.9, 0.999,
                          1e-15, self.t)
 
     def eval_loss(self):
         """Mean loss over the photographs, without dropout."""
-        acc = _torch().zeros(len(self.cams), device="cuda")
-        for ci in range(len(self.cams)):
-            self.render(ci)
-            abcd_loss(self.ctx, self.out, self.photos[ci], self.W, self.H, 0.2, acc[ci:ci + 1], None)
-        self.ctx.sync()
-        return float(acc.mean().item())
+        with self.ctx.on_stream():
+            acc = _torch().zeros(len(self.cams), device=self.out.device)
+            for ci in range(len(self.cams)):
+                self.render(ci)
+                abcd_loss(self.ctx, self.out, self.photos[ci], self.W, self.H, 0.2, acc[ci:ci + 1], None)
+            self.ctx.sync()
+            return float(acc.mean().item())
 
 
 def appearance_experiment(T=400, n=1500, n_cams=6, size=96, p=0.05, seed=7):

@@ -240,17 +240,22 @@ def outputs(t):
     return [t[k] for k in OUTPUTS] + t["dv"] + t["g"] + [t["packed"].codes, t["packed"].powers]
 
 
-@pytest.mark.parametrize("packed", [False, True])
-def test_appearance_on_a_stream_of_its_own(packed):
+@pytest.mark.parametrize("layers", ["layers", "tokens", "packed tokens"])
+def test_appearance_on_a_stream_of_its_own(layers):
     """Training and other passes, called while the current stream is another one, whose memory they take."""
-    from paper_2608_27735_gb300.appearance import TokenAppearance
+    from paper_2608_27735_gb300.appearance import Appearance, TokenAppearance
     n, cams = 2000, 3
     r = np.random.default_rng(13)
     means = r.uniform(-2, 2, (n, 3)).astype(np.float32)
     inputs = [[torch.from_numpy(r.normal(size=(n, 4, 4)).astype(np.float32)).cuda()[:, :, :3] for _ in range(2)] for _ in range(3)]
 
     def passes(ctx):
-        app = TokenAppearance(ctx, means, 1, cams, width=24, packed=packed, seed=4)
+        if layers == "layers":
+            app = Appearance(ctx, n, 1, cams, p=0.1, seed=4)
+            last = app.blocks[-1].w["w_down"]
+        else:
+            app = TokenAppearance(ctx, means, 1, cams, width=24, packed=layers == "packed tokens", seed=4)
+            last = app.w["w_out"]
         given = torch.full_like(inputs[0][0], float("nan"))
         kept = []
         torch.cuda.synchronize()
@@ -258,7 +263,7 @@ def test_appearance_on_a_stream_of_its_own(packed):
             with torch.cuda.stream(ctx.stream):
                 torch.cuda._sleep(10_000_000)
                 given.copy_(sh)
-                app.w["w_out"].add_(0.01)
+                last.add_(0.01)
             kept.append(app.forward(given, ci))
             other = app.forward(given, 0, train=False)
             del other                                   # its memory is the current stream's to use again

@@ -3,9 +3,10 @@ one: every operation that reads or writes a tensor is queued on the context's st
 calls do nothing, the tensors lie in host memory, and the operations say where they would have run."""
 import contextlib
 
+import numpy as np
 import pytest
 
-from paper_2608_27735_gb300 import appearance, network
+from paper_2608_27735_gb300 import Gaussians, appearance, network
 
 torch = pytest.importorskip("torch")
 from torch.utils._python_dispatch import TorchDispatchMode  # noqa: E402
@@ -29,6 +30,9 @@ class FakeContext:
         self.depth += 1
         yield
         self.depth -= 1
+
+    def sync(self):
+        pass
 
     def __getattr__(self, name):
         if name.startswith("reserve"):
@@ -99,6 +103,36 @@ def test_token_appearance(ctx):
             out = app.forward(sh, 1), app.forward(sh, 0, train=False), app.backward(sh, 1)
         assert not watch.astray and watch.there >= 6
         assert all(t.shape == sh.shape and any(t.data_ptr() == h.data_ptr() for h in ctx.held) for t in out)
+
+
+def test_appearance(ctx):
+    n, cols = 4, 16
+    new = lambda c: torch.zeros(n, c)
+    weights = {"norm_w": torch.zeros(cols), "norm_b": torch.zeros(cols), "w_gate": torch.zeros(8, cols), "w_up": torch.zeros(8, cols),
+               "w_down": torch.zeros(cols, 8)}
+    app = bare(appearance.Appearance, ctx=ctx, n=n, sh_cols=12, cols=cols, embed=new(4), d_embed=new(4), x=[new(cols) for _ in range(2)],
+               dx=new(cols), blocks=[network.FeedForwardBlock(ctx, weights, n)])
+    sh = torch.zeros(n, 4, 4)[:, :, :3]
+    with Watch(ctx) as watch:
+        out = app.forward(sh, 1), app.forward(sh, 0, train=False), app.backward(sh, 1)
+    assert not watch.astray and watch.there >= 9
+    assert all(t.shape == sh.shape and any(t.data_ptr() == h.data_ptr() for h in ctx.held) for t in out)
+
+
+def test_appearance_stage(ctx):
+    class Layers:
+        forward = lambda self, sh, ci, train=True: sh
+        backward = lambda self, d_sh, ci: d_sh
+        step = lambda self: None
+
+    n = 3
+    new = lambda: Gaussians(torch.zeros(n, 3), torch.zeros(n, 3), torch.zeros(n, 4), torch.zeros(n), torch.zeros(n, 1, 3), 0)
+    stage = bare(appearance.AppearanceStage, ctx=ctx, theta=new(), grads=new(), m=None, v=None, cams=[None], photos=[None], W=8, H=8, proj=None,
+                 tiles=None, out=torch.zeros(8, 8, 4), state=None, loss=None, lr=None, appearance=Layers(), rng=np.random.default_rng(1), t=0)
+    with Watch(ctx) as watch:
+        stage.step()
+        stage.eval_loss()
+    assert not watch.astray and watch.there >= 3
 
 
 def test_adam_holds_its_buffers(ctx):
