@@ -546,6 +546,10 @@ __global__ void __launch_bounds__(R::kThreads, R::kCtas) close_bwd_kernel(const 
     if (t + 1 < rows.rows) {
       next[0] = stat_of(a, 0, rows.row + rows.step);
       next[1] = stat_of(a, 1, rows.row + rows.step);
+    } else if (R::TPR < 32) {
+      // a turn without a row: of an earlier row's statistics and the factors could come infinities, and NaN in
+      // the sums, where dn's zeros meet them
+      next[0] = next[1] = Stat{0.f, 0.f};
     }
     float2 fh[P], g[P], p1 = both(0.f), p2 = both(0.f);
     // past the end of a row that starts anywhere the mean, which costs no more than zero there (the other factor

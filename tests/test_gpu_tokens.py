@@ -497,6 +497,35 @@ def test_residual_norm_of_rows_of_one_great_value(ctx, kind, cols):
     assert torch.equal(dx, x) and torch.equal(df, x) and not any(v.any() for v in w)
 
 
+@pytest.mark.parametrize("cols", [12, 59, 60, 64, 100, 101])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [33, 9731, 20011])
+def test_residual_norm_of_great_values_and_groups_without_a_row(ctx, kind, cols, rows):
+    """Rows share a warp and are taken in several turns, the last of which some groups of threads have no row in:
+    what statistics of an earlier row would make of nothing, here infinities, is in no sum.  (fp16 has no such
+    values.)  Powers of two and whole numbers of rows: the sums are exact."""
+    dtype = TYPES[kind]
+    x, dy, dn, dx, df = (torch.zeros(rows, cols, device="cuda", dtype=dtype) for _ in range(5))
+    f = torch.full((rows, cols), 2.0 ** 117, device="cuda", dtype=dtype)
+    x[:, ::2], x[:, 1::2] = 1.0, -1.0
+    dy.fill_(1.0)
+    dn.fill_(0.5)
+    three, b, s = torch.full((cols,), 3.0, device="cuda"), torch.full((cols,), 0.25, device="cuda"), torch.empty(4, rows, device="cuda")
+    ctx.reserve_residual_norm(rows, cols)
+    after, before = ab.Norm("layer", three, b, 1e-6, s[0], s[1]), ab.Norm("rms", three, None, 0.0, None, s[3])
+    y, n = torch.empty_like(x), torch.empty_like(x)
+    ab.abcd_residual_norm(ctx, x, f, after, before, None, 1.0, y, n)
+    assert torch.equal(y, x + 0.25)
+    d = [torch.full((cols,), float("nan"), device="cuda") for _ in range(4)]
+    ab.abcd_residual_norm_backward(ctx, dy, dn, x, f, after, before, None, 1.0, dx, df, None, *d)
+    ctx.sync()
+    assert all(torch.isfinite(t).all() for t in (dx, df, *d))
+    assert (d[0] == 0).all() and (d[3] == 0.5 * rows).all()           # the rows normalise to zero
+    # dbefore_weight: rows of one value, (1.25 or -0.75) rstd; sums of `rows` equal terms in 32 bits
+    yh = (x[0].double() + 0.25) * s[3, 0].double()
+    assert ((d[2].double() - 0.5 * rows * yh).abs() <= (rows + 24) * N.EPS * 0.5 * rows * yh.abs()).all()
+
+
 def test_residual_norm_without_rows(ctx):
     w, d = torch.ones(40, device="cuda"), [torch.ones(40, device="cuda") for _ in range(5)]
     e = torch.empty(0, 40, device="cuda")
