@@ -119,7 +119,8 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_kernel(const __grid_consta
   if (linear) {
     if (a.bias) v[0] += a.wide_bias ? ((const float*)a.bias)[unit] : to_f32(((const T*)a.bias)[unit]);
     if (a.saved[0]) ((T*)a.saved[0])[lane * a.ssaved[0] + unit] = from_f32<T>(v[0]);
-    if (a.act != ABCD_NO_ACTIVATION) act_values<sizeof(T) == 4>(v, a.act);
+    // (gelu in the form that more tokens and the backward pass take)
+    if (a.act != ABCD_NO_ACTIVATION) act_values<sizeof(T) == 4, 1, true>(v, a.act);
     if (a.res) v[0] += to_f32(((const T*)a.res)[lane * a.sres + unit]);
   }
   ((T*)a.y)[lane * a.sy + unit] = from_f32<T>(v[0]);

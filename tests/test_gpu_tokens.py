@@ -289,6 +289,26 @@ def test_linear_gelu_far_below_zero(ctx, kind, rows):
         close(got, want, 2 * wide + 2 * (np.abs(want) + wide) * N.UNIT[kind] + N.TINY[kind])
 
 
+def test_linear_gelu_of_few_tokens_is_that_of_many(ctx):
+    """The activation of a value does not depend on how many rows lie beside it: in 32 bits one form of gelu, whatever
+    the product.  Through a unit matrix z is x; the exponentials are the same, and the polynomial, whose ten steps a
+    compiler may round once or twice each, is within 3.5 units of 2^-23 of itself in both kernels (as its coefficients
+    were fitted)."""
+    d = 64
+    x, one = matrix(np.random.default_rng(3).uniform(-12, 3, (300, d)), "f32"), matrix(np.eye(d), "f32")
+    ctx.reserve_linear(300, d, d)
+    y = torch.empty_like(x)
+    ab.abcd_linear(ctx, x, one, None, "gelu", y)
+    for rows in (1, 3, 8, 9):
+        few, z = torch.empty(rows, d, device="cuda"), torch.empty(rows, d, device="cuda")
+        for at in range(0, 300 - rows, 8):
+            ab.abcd_linear(ctx, x[at:at + rows], one, None, "gelu", few, None, z)
+            assert torch.equal(z, x[at:at + rows])
+            want = y[at:at + rows].double()
+            assert ((few.double() - want).abs() <= 7 * 2.0 ** -23 * want.abs()).all()
+    ctx.sync()
+
+
 @pytest.mark.parametrize("rows,cols,out", [(50, 64, 96), (5000, 256, 1024)])
 def test_linear_with_matrices_of_different_starts(ctx, rows, cols, out):
     """Each of residual, y and z on 16-byte boundaries or not."""
