@@ -620,7 +620,8 @@ abcd_status abcd_residual_norm(abcd_ctx* ctx, const abcd_matrix* x, const abcd_m
  * `before`, and only then.  With g = dy + before's gradient of dn: dx = g, df = after's gradient of
  * scale gate g, dgate = the rows' sum of scale g after(f), and the norms' own gradients (NULL where the
  * norm is).  Each may be NULL.  The vectors are [cols] of weight_dtype and zero without rows; like the forward
- * pass's statistics they lie apart from all else that the call is given.  dx and df may be dy, dn, x or f. */
+ * pass's statistics they lie apart from all else that the call is given, which is refused otherwise.  dx and df
+ * may be dy, dn, x or f. */
 abcd_status abcd_residual_norm_backward(abcd_ctx* ctx, const abcd_matrix* dy, const abcd_matrix* dn,
                                         const abcd_matrix* x, const abcd_matrix* f, const abcd_norm* after,
                                         const abcd_norm* before, const void* gate, int weight_dtype,

@@ -755,6 +755,61 @@ bool same_or_apart(const abcd_matrix* result, const abcd_matrix* operand) {
   return result->data == operand->data && (result->stride == operand->stride || result->rows == 1);
 }
 
+// What a call is given, and whether a vector that it writes overlaps any of that, or a matrix that it writes a vector
+// (matrices among themselves: same_or_apart).  Most bounds lie apart, which is all that is looked at then.
+class Places {
+  struct Range { uintptr_t first, end; };
+  Range matrix_[6];                   // x, f, dy, dn and two results
+  Range vector_[9], written_[5];      // two norms' four vectors and the gate; the gradients, or (of vector_) the statistics
+  const abcd_matrix* of_[6];
+  unsigned results_ = 0;              // of the matrices, a bit each
+  int matrices_ = 0, vectors_ = 0, writtens_ = 0;
+  static bool meet(const Range& p, const Range& q) { return p.first < q.end && q.first < p.end; }
+  bool in_matrix(const Range& v, int k) const {
+    if (!meet(v, matrix_[k])) return false;
+    const long long halves = (long long)(v.end - v.first) / 2;          // as 16-bit elements
+    const abcd_matrix row{(void*)v.first, 1, halves, halves, ABCD_F16};
+    return overlap(&row, of_[k]);
+  }
+
+ public:
+  void matrix(const abcd_matrix* m, bool result) {
+    if (!m || m->rows == 0) return;
+    const uintptr_t first = (uintptr_t)m->data, elements = (uintptr_t)((m->rows - 1) * m->stride + m->cols);
+    matrix_[matrices_] = Range{first, first + elements * elem_size(m->dtype)};
+    of_[matrices_] = m;
+    results_ |= (result ? 1u : 0u) << matrices_++;
+  }
+  void vector(const void* p, long long n, int dtype, bool written) {
+    if (!p || n == 0) return;
+    const Range r{(uintptr_t)p, (uintptr_t)p + (uintptr_t)n * elem_size(dtype)};
+    if (written) written_[writtens_++] = r;
+    else vector_[vectors_++] = r;
+  }
+  void norm(const abcd_norm* q, long long rows, long long cols, int dtype, bool written) {
+    if (!q) return;
+    vector(q->weight, cols, dtype, false);
+    vector(q->bias, cols, dtype, false);
+    vector(q->mean, rows, ABCD_F32, written);
+    vector(q->rstd, rows, ABCD_F32, written);
+  }
+  bool clash() const {
+    for (int i = 0; i < writtens_; ++i) {
+      for (int k = 0; k < matrices_; ++k)
+        if (in_matrix(written_[i], k)) return true;
+      for (int k = 0; k < vectors_; ++k)
+        if (meet(written_[i], vector_[k])) return true;
+      for (int k = 0; k < i; ++k)
+        if (meet(written_[i], written_[k])) return true;
+    }
+    for (int k = 0; k < matrices_; ++k)
+      if (results_ >> k & 1)
+        for (int i = 0; i < vectors_; ++i)
+          if (in_matrix(vector_[i], k)) return true;
+    return false;
+  }
+};
+
 void take_norm(CloseArgs& a, int k, const abcd_norm* q) {
   a.kind[k] = q ? q->kind : kNone;
   if (!q) return;
@@ -791,6 +846,15 @@ extern "C" abcd_status abcd_residual_norm(abcd_ctx* ctx, const abcd_matrix* x, c
   if (!same_or_apart(y, x) || !same_or_apart(y, f) || !same_or_apart(n, x) || !same_or_apart(n, f) || (n && overlap(y, n)))
     return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: an output overlaps an operand or the other output", what);
   if (x->rows == 0) return ABCD_OK;
+  Places all;
+  all.matrix(x, false);
+  all.matrix(f, false);
+  all.matrix(y, true);
+  all.matrix(n, true);
+  all.norm(after, x->rows, x->cols, weight_dtype, true);
+  all.norm(before, x->rows, x->cols, weight_dtype, true);
+  all.vector(gate, x->cols, weight_dtype, false);
+  if (all.clash()) return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: the statistics or an output overlap a vector or a matrix", what);
   CloseArgs a{};
   a.x = x->data; a.f = f->data; a.y = y->data; a.n = n ? n->data : nullptr;
   a.sx = x->stride; a.sf = f->stride; a.sy = y->stride; a.sn = n ? n->stride : 0;
@@ -838,6 +902,14 @@ extern "C" abcd_status abcd_residual_norm_backward(abcd_ctx* ctx, const abcd_mat
   for (const abcd_matrix* out : {dx, df})
     for (const abcd_matrix* in : {dy, dn, x, f}) apart = apart && same_or_apart(out, in);
   if (!apart) return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: a gradient overlaps an operand or the other gradient", what);
+  Places all;
+  for (const abcd_matrix* m : {dy, dn, x, f}) all.matrix(m, false);
+  for (const abcd_matrix* m : {dx, df}) all.matrix(m, true);
+  all.norm(after, x->rows, x->cols, weight_dtype, false);
+  all.norm(before, x->rows, x->cols, weight_dtype, false);
+  all.vector(gate, x->cols, weight_dtype, false);
+  for (const void* p : to) all.vector(p, x->cols, weight_dtype, true);
+  if (all.clash()) return fail(ctx, ABCD_ERR_INVALID_ARG, "%s: a vector's gradient overlaps what the call is given, or a gradient a vector", what);
   CloseArgs a{};
   a.x = x->data; a.f = f->data; a.dy = dy ? dy->data : nullptr; a.dn = dn ? dn->data : nullptr;
   a.y = dx ? dx->data : nullptr; a.n = df ? df->data : nullptr;

@@ -170,6 +170,38 @@ def test_residual_norm_refusals(lib, ctx):
     assert lib.abcd_residual_norm(None, ref(x), ref(f), None, None, None, BF16, 1.0, ref(one), None) == BAD
 
 
+def test_residual_norm_refuses_vectors_that_overlap(lib, ctx):
+    """What a call writes of vectors lies apart from all else that it is given, and its matrices from the vectors."""
+    x, f, y, n = (matrix(8, 64, k) for k in range(4))
+    first = dict(weight=address(20), bias=address(21), mean=address(22), rstd=address(23))
+    second = dict(weight=address(24), bias=address(25), mean=address(26), rstd=address(27))
+    call = Call(lib.abcd_residual_norm, x=x, f=f, after=norm(**first), before=norm(**second), gate=address(28), kind=BF16, scale=1.0, y=y, n=n)
+    assert call(ctx) == ab.ABCD_ERR_CUDA              # all that is missing: a GPU
+    shared = dict(after=norm(**{**first, "weight": address(28)}), before=norm(**{**second, "weight": address(28), "bias": address(21)}))
+    assert call(ctx, **shared) == ab.ABCD_ERR_CUDA    # what is only read
+    close_by = address(22) + 8 * 4
+    assert call(ctx, after=norm(**{**first, "rstd": close_by})) == ab.ABCD_ERR_CUDA
+    for change in (dict(after=norm(**{**first, "rstd": close_by - 4})), dict(after=norm(**{**first, "mean": address(20) + 64 * 2 - 4})),
+                   dict(before=norm(**{**second, "mean": address(22)})), dict(before=norm(**{**second, "rstd": address(0) + 8 * 64 * 2 - 4})),
+                   dict(before=norm(**{**second, "mean": address(1)})), dict(before=norm(**{**second, "rstd": address(2)})),
+                   dict(after=norm(**{**first, "mean": address(28)})), dict(y=matrix(8, 64, 24)), dict(n=matrix(8, 64, 28)), dict(n=matrix(8, 64, 21))):
+        assert call(ctx, **change) == BAD, change
+    # between a matrix's rows
+    wide = dict(x=matrix(8, 64, 0, stride=256), y=matrix(8, 64, 2, stride=256))
+    assert call(ctx, **wide, gate=address(2) + 64 * 2) == ab.ABCD_ERR_CUDA
+    assert call(ctx, **wide, gate=address(2) + 64 * 2 - 2) == BAD
+    back = Call(lib.abcd_residual_norm_backward, dy=matrix(8, 64, 4), dn=matrix(8, 64, 5), x=x, f=f, after=norm(**first), before=norm(**second),
+                gate=address(28), kind=F32, scale=1.0, dx=matrix(8, 64, 6), df=matrix(8, 64, 7), dgate=address(30), aw=address(31), ab=address(32),
+                bw=address(33), bb=address(34))
+    assert back(ctx) == WORKSPACE
+    assert back(ctx, **shared) == WORKSPACE
+    assert back(ctx, dgate=address(30) + 64 * 4, aw=address(30)) == WORKSPACE
+    for change in (dict(dgate=address(28)), dict(aw=address(30) + 64 * 4 - 4), dict(ab=address(33)), dict(bw=address(23)), dict(bb=address(0)),
+                   dict(bb=address(4) + 8 * 64 * 2 - 4), dict(aw=address(6)), dict(dgate=address(7)), dict(dx=matrix(8, 64, 22)),
+                   dict(df=matrix(8, 64, 24)), dict(bw=address(5)), dict(dx=matrix(8, 64, 28))):
+        assert back(ctx, **change) == BAD, change
+
+
 def packed(rows, cols, at, stride=None, powers=None, power_stride=None):
     groups = -(-cols // 32)
     return ab.abcd_packed8(address(at), address(at + 0.5) if powers is None else powers, rows, cols, stride or 32 * groups, power_stride or groups)
