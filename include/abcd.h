@@ -642,7 +642,8 @@ typedef struct {
   long long cols;
   long long stride;       /* bytes between rows of codes, >= cols */
   long long power_stride; /* bytes between rows of powers, >= cols / 32 rounded up */
-} abcd_packed8;
+} abcd_packed8;           /* powers may lie between the rows of codes; where they share a byte with codes, the matrix
+                           * is refused */
 
 /* packed = x in 8 bits; the bytes between rows stay as they are.  packed does not overlap x (what lies between
  * the rows of either counted in). */

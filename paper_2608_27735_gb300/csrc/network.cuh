@@ -40,21 +40,17 @@ inline bool rows_aligned(const abcd_matrix* m, size_t bytes) {
           (bytes - 1)) == 0;
 }
 
-// Whether an element of one matrix lies where one of the other does.  Both may be columns of one buffer,
+// The bytes of a matrix: n rows of `width`, `step` apart.
+struct ByteRows { uintptr_t first; long long n, width, step; };
+// Whether a byte of one matrix lies where one of the other does.  Both may be columns of one buffer,
 // their rows in turn: rows equally far apart are compared once, others row by row (of the matrix with
 // fewer), which only matrices that reach into one another come to.
-inline bool overlap(const abcd_matrix* a, const abcd_matrix* b) {
-  if (a->rows == 0 || b->rows == 0) return false;
-  struct Rows { uintptr_t first; long long n, width, step; };
-  const auto rows_of = [](const abcd_matrix* m) {
-    const long long e = (long long)elem_size(m->dtype);
-    Rows r{(uintptr_t)m->data, m->rows, m->cols * e, m->stride * e};
-    if (r.n == 1 || r.step == r.width) r = Rows{r.first, 1, r.n * r.width, r.n * r.width};   // one piece
-    return r;
-  };
-  Rows p = rows_of(a), q = rows_of(b);
+inline bool overlap(ByteRows p, ByteRows q) {
+  if (p.n == 0 || q.n == 0) return false;
+  for (ByteRows* r : {&p, &q})
+    if (r->n == 1 || r->step == r->width) *r = ByteRows{r->first, 1, r->n * r->width, r->n * r->width};   // one piece
   if (p.n > q.n) std::swap(p, q);
-  const auto end = [](const Rows& r) { return r.first + (uintptr_t)(r.n - 1) * (uintptr_t)r.step + (uintptr_t)r.width; };
+  const auto end = [](const ByteRows& r) { return r.first + (uintptr_t)(r.n - 1) * (uintptr_t)r.step + (uintptr_t)r.width; };
   if (end(p) <= q.first || end(q) <= p.first) return false;
   // whether the bytes [from, from + width), counted from q's first row, meet a row of q
   const auto meets = [&](long long from, long long width) {
@@ -73,6 +69,13 @@ inline bool overlap(const abcd_matrix* a, const abcd_matrix* b) {
   for (long long i = 0; i < p.n; ++i)
     if (meets(from + i * p.step, p.width)) return true;
   return false;
+}
+inline bool overlap(const abcd_matrix* a, const abcd_matrix* b) {
+  const auto rows_of = [](const abcd_matrix* m) {
+    const long long e = (long long)elem_size(m->dtype);
+    return ByteRows{(uintptr_t)m->data, m->rows, m->cols * e, m->stride * e};
+  };
+  return overlap(rows_of(a), rows_of(b));
 }
 
 __device__ __forceinline__ float to_f32(float v) { return v; }

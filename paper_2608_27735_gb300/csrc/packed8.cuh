@@ -5,12 +5,15 @@
 
 namespace abcd {
 
-// A packed matrix that a call may read or write.
+// A packed matrix that a call may read or write: its shape within the limits, its codes on 32-byte boundaries and
+// apart from its powers (which may lie between the rows of codes).
 inline bool packed_ok(const abcd_packed8* q) {
   return q && q->rows >= 0 && q->rows <= kMaxNetRows && q->cols >= 1 && q->cols <= kMaxNetCols &&
          q->stride >= q->cols && q->stride <= (1LL << 31) && q->stride % 32 == 0 &&
          q->power_stride >= (q->cols + 31) / 32 && q->power_stride <= (1LL << 31) &&
-         (q->rows == 0 || (q->codes && q->powers)) && ((uintptr_t)q->codes & 31) == 0;
+         (q->rows == 0 || (q->codes && q->powers)) && ((uintptr_t)q->codes & 31) == 0 &&
+         !overlap(ByteRows{(uintptr_t)q->codes, q->rows, q->cols, q->stride},
+                  ByteRows{(uintptr_t)q->powers, q->rows, (q->cols + 31) / 32, q->power_stride});
 }
 
 // Whether a packed matrix and another may share a byte: the codes, or the powers, lie within the other's reach

@@ -92,6 +92,22 @@ def test_pack_of_part_of_the_rows(ctx):
         q.head(51)
 
 
+@pytest.mark.parametrize("kind,pad", [("f32", 0), ("bf16", 0), ("f16", 3)])
+def test_pack_with_powers_between_the_rows_of_codes(ctx, kind, pad):
+    from paper_2608_27735_gb300 import network
+    rows, cols = 130, 70
+    x = matrix(values_to_pack(np.random.default_rng(4), rows, cols), kind, pad)
+    apart, together, buf = ab.Packed8(rows, cols), ab.Packed8(rows, cols), torch.full((rows, 128), 55, dtype=torch.int8, device="cuda")
+    together.c = network._pack_packed(buf.data_ptr(), buf.data_ptr() + 100, rows, cols, 128, 128)
+    back = [blank(rows, cols, kind, pad) for _ in range(2)]
+    for q, y in zip((apart, together), back):
+        ab.abcd_pack8(ctx, x, q)
+        ab.abcd_unpack8(ctx, q, y)
+    ctx.sync()
+    assert torch.equal(buf[:, :cols], apart.codes[:, :cols]) and torch.equal(buf[:, 100:103], apart.powers.view(torch.int8))
+    assert (buf[:, cols:100] == 55).all() and (buf[:, 103:] == 55).all() and torch.equal(*back)
+
+
 PACKED_FF = [(1, 8, 16), (9, 59, 40), (200, 64, 256), (300, 250, 129), (1100, 256, 512), (9000, 64, 700)]
 
 
