@@ -335,17 +335,24 @@ class Packed8:
 _pack_packed = struct.Struct("@PPqqqq").pack         # the bytes of an abcd_packed8
 
 
+def _packed(q, what):
+    """The abcd_packed8 as bytes of a Packed8 in device memory."""
+    if not isinstance(q, Packed8) or not q.codes.is_cuda:
+        raise ValueError(f"{what} must be a Packed8 of CUDA memory")
+    return q.c
+
+
 def abcd_pack8(ctx: Context, x, packed: Packed8):
     """packed = x in 8 bits: an element is off by at most a 128th of the largest magnitude of the 32 columns
     that share its power of two."""
-    st = _call("abcd_pack8")(ctx.h, _matrix(x, "x")[0], packed.c)
+    st = _call("abcd_pack8")(ctx.h, _matrix(x, "x")[0], _packed(packed, "packed"))
     if st:
         ctx.check(st)
 
 
 def abcd_unpack8(ctx: Context, packed: Packed8, y):
     """y = what packed stands for."""
-    st = _call("abcd_unpack8")(ctx.h, packed.c, _matrix(y, "y")[0])
+    st = _call("abcd_unpack8")(ctx.h, _packed(packed, "packed"), _matrix(y, "y")[0])
     if st:
         ctx.check(st)
 
@@ -355,8 +362,8 @@ def abcd_gated_ff_backward_packed8(ctx: Context, dy, x, w_gate, w_up, w_down, ac
     """abcd_gated_ff_backward with x, gate and up as Packed8.  Takes the network workspace
     (Context.reserve_packed8)."""
     call = _call("abcd_gated_ff_backward_packed8")
-    st = call(ctx.h, _matrix(dy, "dy")[0], x.c, _matrix(w_gate, "w_gate")[0], _matrix(w_up, "w_up")[0],
-              _matrix(w_down, "w_down")[0], _activation(activation), gate.c, up.c, _optional(dx, "dx"),
+    st = call(ctx.h, _matrix(dy, "dy")[0], _packed(x, "x"), _matrix(w_gate, "w_gate")[0], _matrix(w_up, "w_up")[0],
+              _matrix(w_down, "w_down")[0], _activation(activation), _packed(gate, "gate"), _packed(up, "up"), _optional(dx, "dx"),
               _optional(dw_gate, "dw_gate"), _optional(dw_up, "dw_up"), _optional(dw_down, "dw_down"))
     if st:
         ctx.check(st)

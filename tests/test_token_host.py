@@ -231,6 +231,24 @@ def test_packed_refusals(lib, ctx):
         assert call(ctx, **change) == BAD, change
 
 
+def test_matrices_in_8_bits_of_host_memory_are_refused(monkeypatch):
+    """Before the library sees an address, as the other tensors are."""
+    torch = pytest.importorskip("torch")
+    from paper_2608_27735_gb300 import network
+    class Context:
+        h = None
+    def never(*args):
+        raise AssertionError("the library was called")
+    monkeypatch.setattr(network, "_call", lambda name: never)
+    monkeypatch.setattr(network, "_matrix", lambda t, what: (b"", 4, 40))
+    q = ab.Packed8(4, 40, "cpu")
+    for call in (lambda q: network.abcd_pack8(Context, None, q), lambda q: network.abcd_unpack8(Context, q, None),
+                 lambda q: network.abcd_gated_ff_backward_packed8(Context, None, q, None, None, None, "silu", q, q)):
+        for bad in (q, None, torch.zeros(4, 40)):
+            with pytest.raises(ValueError):
+                call(bad)
+
+
 def test_shared_memory_limits_have_a_place():
     """As the sources' own count in tests/test_network_host.py, with the kernels of the token operators."""
     csrc = os.path.join(os.path.dirname(ab.__file__), "csrc")
