@@ -8,6 +8,7 @@ library is missing or no GPU is present, every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import re
@@ -372,14 +373,17 @@ class Context:
         waits for what the current one has queued (their memory may be what a kernel there still
         writes), and their memory, once they are dropped, for the calls that use it."""
         current = _torch().cuda.current_stream(self.device)
-        if current != self.stream:
-            self.stream.wait_stream(current)
+        if current == self.stream:
+            return
+        self.stream.wait_stream(current)
         for t in tensors:
             t.record_stream(self.stream)
 
     def on_stream(self):
         """`with ctx.on_stream():` runs torch's operations on the context's stream, in order with its calls."""
-        return _torch().cuda.stream(self.stream)
+        cuda = _torch().cuda
+        # where it is the current one anyway, setting it again would take 6 us instead of 1.5
+        return contextlib.nullcontext() if cuda.current_stream(self.device) == self.stream else cuda.stream(self.stream)
 
     def reserve(self, max_gaussians, max_pairs, max_pixels):
         """(Re)allocates the workspace if the limits grew."""
