@@ -657,7 +657,7 @@ abcd_status abcd_unpack8(abcd_ctx* ctx, const abcd_packed8* packed, const abcd_m
 abcd_status abcd_packed8_workspace_size(long long rows, long long cols, long long ff, int dtype,
                                         size_t* bytes);
 /* abcd_gated_ff_backward with x, gate and up as abcd_pack8 kept them: the same gradients, of what they
- * stand for. */
+ * stand for (in fp16 within its range: a value that it does not hold may be taken as infinite). */
 abcd_status abcd_gated_ff_backward_packed8(abcd_ctx* ctx, const abcd_matrix* dy, const abcd_packed8* x,
                                            const abcd_matrix* w_gate, const abcd_matrix* w_up,
                                            const abcd_matrix* w_down, int activation,

@@ -230,7 +230,8 @@ __device__ __forceinline__ unsigned warp_sums(unsigned v) {
 // knows how many of a digit its lanes and the warps before it have.  They go to shared memory in the order of
 // their digits first, so that consecutive lanes write consecutive places.  One tile counts for itself.  Bound
 // by latency: 1,000,000 tokens, nine bits, 12 us; with the match instruction instead of ballots 18, and with
-// scattered writes 27.
+// scattered writes 27.  (The 1,024 threads leave 64 registers each, and 88 to 172 bytes, by the tile's size, spill:
+// the warps' counts of two digits are 32 registers.)
 template <int IT>
 __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_constant__ SortArgs a) {
   pdl_wait();
@@ -245,23 +246,23 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
   unsigned short* own = before + warp * digits;
   unsigned key[IT];
   sort_keys(a, first + start, 32, a.n, key);
-      unsigned all = 0, ahead = 0;                      // the digit's tokens, and those of the tiles before
-      if (a.tiles > 1 && threadIdx.x < digits) {
-        const unsigned* c = a.count + (long long)threadIdx.x * a.tiles;
-        if (a.tiles > kScanned) {
-          all = a.total[threadIdx.x];
-          ahead = c[blockIdx.x];
-        } else {
-          unsigned v[kScanned];
-  #pragma unroll
-          for (int t = 0; t < kScanned; ++t) v[t] = c[min(t, a.tiles - 1)];
-  #pragma unroll
-          for (int t = 0; t < kScanned; ++t) {
-            ahead += t < (int)blockIdx.x ? v[t] : 0u;
-            all += t < a.tiles ? v[t] : 0u;
-          }
-        }
+  unsigned all = 0, ahead = 0;                      // the digit's tokens, and those of the tiles before
+  if (a.tiles > 1 && threadIdx.x < digits) {
+    const unsigned* c = a.count + (long long)threadIdx.x * a.tiles;
+    if (a.tiles > kScanned) {
+      all = a.total[threadIdx.x];
+      ahead = c[blockIdx.x];
+    } else {
+      unsigned v[kScanned];
+#pragma unroll
+      for (int t = 0; t < kScanned; ++t) v[t] = c[min(t, a.tiles - 1)];
+#pragma unroll
+      for (int t = 0; t < kScanned; ++t) {
+        ahead += t < (int)blockIdx.x ? v[t] : 0u;
+        all += t < a.tiles ? v[t] : 0u;
       }
+    }
+  }
   for (int i = threadIdx.x; i < kSortWarps * digits / 8; i += kSortThreads) reinterpret_cast<uint4*>(before)[i] = make_uint4(0u, 0u, 0u, 0u);
   __syncthreads();
   unsigned rank[IT];                                  // among the warp's tokens of the digit

@@ -5,7 +5,9 @@
 // the matrices' type, in 32 bits as three terms) and its columns' sums, and both products are one launch.
 // 16,384 x 4,096 x 4,096 bf16: forward with residual and z 332 us (1,660 TFLOP/s), the pass over dy and z 67 (6.0
 // TB/s), both products 600 (1,830).  100,000 x 256 x 256 bf16: 49 us (5.2 TB/s; six rounds of tiles for 5.1) and 72.
-// 20,000 x 59 x 256 fp32 with gelu: 29 and 44 us, nine launches; the forward product is three rounds of tiles.
+// 20,000 x 59 x 256 fp32 with gelu: 29 and 44 us, two launches (operands, product) and five (operands, dz, dbias, products,
+// their parts); the forward product is three rounds of the smallest tile, whose epilogue spills (104 bytes at the 96
+// registers that two CTAs an SM leave).
 #include "products.cuh"
 
 namespace abcd {
