@@ -373,9 +373,8 @@ class Context:
         waits for what the current one has queued (their memory may be what a kernel there still
         writes), and their memory, once they are dropped, for the calls that use it."""
         current = _torch().cuda.current_stream(self.device)
-        if current == self.stream:
-            return
-        self.stream.wait_stream(current)
+        if current != self.stream:
+            self.stream.wait_stream(current)
         for t in tensors:
             t.record_stream(self.stream)
 
