@@ -25,7 +25,7 @@ constexpr int kVisSumCopies = 8;          // copies of the layer visibility sums
 // words of Workspace::os_ctr: [2 sorts][2] tile and finished-CTA counters of a radix pass, the run
 // placement's two, [2 calls in turn][2] the visible depth keys' range, the count kernel's finished CTAs
 constexpr int kCtrSorts = 0, kCtrPlace = 4, kCtrKeyRange = 8, kCtrTicket = 12;
-// kernels with dynamic shared memory, at most: 62 of layer norm, 84 of the residual norm, 25 products, three of
+// kernels with dynamic shared memory, at most: 62 of layer norm, 84 of the residual norm, 27 products, three of
 // the tokens' sort, ten of the renderer
 constexpr int kSmemKernels = 192;
 

@@ -457,6 +457,11 @@ static __device__ __noinline__ void block_elements(const char* block, int first,
       if (row0 + 2 * i < rows) to[(row0 + 2 * i) * o.stride] = v[i];
   }
 }
+// What TMA leaves of such columns: those from column `whole` of the matrix on, behind a row's last whole piece.
+static __device__ __noinline__ void block_tail(const char* block, int first, int j, const Out& o, long long m, int n, int rows, int cols, int whole) {
+  const int skip = whole - n;
+  if (skip >= 0 && skip < 16 && skip < cols) block_elements(block, first, j + skip / 8, o, m, whole, rows, cols - skip);
+}
 __device__ __forceinline__ void put_block(char* block, int row, int j, const unsigned (&w)[8]) {
   *reinterpret_cast<uint4*>(block + block_at(row, j)) = make_uint4(w[0], w[1], w[2], w[3]);
   *reinterpret_cast<uint4*>(block + block_at(row, j + 1)) = make_uint4(w[4], w[5], w[6], w[7]);
@@ -584,7 +589,9 @@ struct Product {
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpilogueBytes;
 };
 
-template <int CG, int BN, int EPI, bool F32>
+// ODD, of the large tile of 16-bit matrices: the rows of the caller's results end inside a piece of 16 bytes.  (A kernel
+// of its own: the test for it in the loop cost kUp 2 to 14 us of the 172 of 100,000 x 256 x 1,024.)
+template <int CG, int BN, int EPI, bool F32, bool ODD>
 __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<CG, BN, EPI, F32>::kCtas) product_kernel(const __grid_constant__ ProductArgs a) {
   using P = Product<CG, BN, EPI, F32>;
   extern __shared__ char smem_raw[];
@@ -867,6 +874,15 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
             put_block(own + P::kBlockBytes, row, 2 * half, x[1]);
             if (EPI != kLinear) put_block(own + 2 * P::kBlockBytes, row, 2 * half, x[2]);
           }
+          const int whole = a.job[0].n & ~7;                   // ODD: columns of the caller's matrices that TMA stores
+          if (ODD && ok) {
+            __syncwarp();
+            const int rows = min(32, a.job[0].m - m - quarter * 32), cols = min(16, a.job[0].n - n0 - c);
+            if (EPI == kLinear && result_by_tma) block_tail(own, quarter * 32, 2 * half, a.job[0].c[0], m + quarter * 32, n0 + c, rows, cols, whole);
+            if (saved_by_tma)
+              for (int k = 0; k < P::kResults - 1; ++k)
+                block_tail(own + (k + 1) * P::kBlockBytes, quarter * 32, 2 * half, a.g[k], m + quarter * 32, n0 + c, rows, cols, whole);
+          }
           if (!result_by_tma && ok) {
             __syncwarp();
             block_elements(own, quarter * 32, 2 * half, a.job[0].c[0], m + quarter * 32, n0 + c, min(32, a.job[0].m - m - quarter * 32),
@@ -883,13 +899,14 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
           if (elected && ok) {
             const int n = n0 + 32 * s;
             const uint32_t from = smem_addr(own);
-            if (result_by_tma) tma_store(&a.c_map, n, m, 0, from);
+            const bool pieces = !ODD || n < whole;
+            if (result_by_tma && (EPI != kLinear || pieces)) tma_store(&a.c_map, n, m, 0, from);
             if (EPI == kLinear) {
-              if (saved_by_tma) tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
+              if (saved_by_tma && pieces) tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
             } else if (P::kIsDown) {
               tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
               tma_store(&a.g_map[0], n, m, 1, from + 2 * P::kBlockBytes);
-            } else if (saved_by_tma) {
+            } else if (saved_by_tma && pieces) {
               tma_store(&a.g_map[0], n, m, 0, from + P::kBlockBytes);
               tma_store(&a.g_map[1], n, m, 0, from + 2 * P::kBlockBytes);
             }
@@ -1119,10 +1136,10 @@ __global__ void __launch_bounds__(Product<CG, BN, EPI, F32>::kThreads, Product<C
   if (threadIdx.x == 0 && dead) atomicOr(a.status, kStatusTimeout);
 }
 
-template <int CG, int BN, int EPI, bool F32>
+template <int CG, int BN, int EPI, bool F32, bool ODD = false>
 abcd_status launch_product(abcd_ctx* ctx, const ProductArgs& a) {
   using P = Product<CG, BN, EPI, F32>;
-  auto* kernel = product_kernel<CG, BN, EPI, F32>;
+  auto* kernel = product_kernel<CG, BN, EPI, F32, ODD>;
   const cudaError_t e = allow_smem(ctx, (const void*)kernel);
   if (e != cudaSuccess) return fail(ctx, ABCD_ERR_CUDA, "product_kernel: %s", cudaGetErrorString(e));
   const int items = a.items;

@@ -112,8 +112,8 @@ extern "C" abcd_status abcd_gated_ff(abcd_ctx* ctx, const abcd_matrix* x, const 
   if (gate) {
     // TMA stores them where their rows allow it
     if (!needs_pack(gate) && !needs_pack(up)) {
-      hid.g[0] = in_place(gate);
-      hid.g[1] = in_place(up);
+      hid.g[0] = stored_in_place(gate);
+      hid.g[1] = stored_in_place(up);
     }
     hid.out[0] = out_of(gate);
     hid.out[1] = out_of(up);

@@ -190,8 +190,8 @@ extern "C" abcd_status abcd_linear(abcd_ctx* ctx, const abcd_matrix* x, const ab
   if (z) hid.out[0] = out_of(z);
   if (residual) hid.saved[0] = out_of(residual);
   // what TMA moves, where rows allow it
-  if (!needs_pack(y)) hid.c = in_place(y);
-  if (z && !needs_pack(z)) hid.g[0] = in_place(z);
+  if (!needs_pack(y)) hid.c = stored_in_place(y);
+  if (z && !needs_pack(z)) hid.g[0] = stored_in_place(z);
   if (residual && !needs_pack(residual)) hid.in[0] = in_place(residual);
   return run(ctx, t, kLinear, &job, 1, plan(ctx->num_sms, t, kLinear, &job, 1), &hid);
 }

@@ -56,6 +56,14 @@ inline Operand in_place(const abcd_matrix* m) {
   return Operand{m->data, m->rows, m->cols, (m->stride + 7) / 8 * 8, 0, 1};
 }
 
+// A result that TMA stores: the whole 16-byte pieces of its rows.  (It writes the piece that a row ends in to that
+// piece's end, over what lies behind the row, so what remains of a row goes by elements.)
+inline Operand stored_in_place(const abcd_matrix* m) {
+  Operand o = in_place(m);
+  o.cols &= ~7LL;
+  return o.cols ? o : Operand{};
+}
+
 // The matrices of a call as operands: in place where TMA can read them, else as copies in the
 // workspace, which one launch makes.
 struct Operands {

@@ -280,6 +280,56 @@ def test_linear(ctx, kind, rows, cols, out, name, pad, lead):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,cols,out", [(300, 59, 67), (5000, 64, 515), (9000, 59, 1067), (50000, 8, 515), (9000, 64, 1065), (20000, 16, 1022)])
+@pytest.mark.parametrize("more", [0, 8])
+def test_linear_writes_nothing_behind_its_rows(ctx, kind, rows, cols, out, more):
+    """Rows on 16-byte boundaries whose last 16 bytes reach past them, in tiles of every size: what lies there is
+    someone else's (the next columns of a wider matrix)."""
+    r = np.random.default_rng(out)
+    pad = -out % 8 + more
+    x, w = matrix(r.normal(size=(rows, cols)), kind, -cols % 8), matrix(r.normal(size=(out, cols)) / cols ** 0.5, kind, -cols % 8)
+    b = vector(r.normal(size=out), "f32")
+    ctx.reserve_linear(rows, cols, out, TYPES[kind])
+    res = matrix(r.normal(size=(rows, out)), kind, pad)
+    args = f64(x), f64(w), f64(b), "silu", f64(res)
+    want, bounds = K.linear(*args), K.linear_bounds(*args, kind)
+    for pads in ((pad, pad), (pad, pad + 1), (pad + 1, pad)):
+        y, z = (blank(rows, out, kind, p) for p in pads)
+        ab.abcd_linear(ctx, x, w, b, "silu", y, res, z)
+        ctx.sync()
+        for got, exact, bound in zip((y, z), want, bounds):
+            close(got, exact, bound)
+            assert gaps_untouched(got)
+    ab.abcd_linear(ctx, x, w, b, "silu", res, res)
+    ctx.sync()
+    close(res, want[0], bounds[0])
+    assert gaps_untouched(res)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,cols,ff", [(300, 59, 67), (5000, 16, 1067), (7536, 64, 515), (9000, 35, 1001)])
+@pytest.mark.parametrize("more", [0, 8])
+def test_feed_forward_writes_nothing_behind_its_rows(ctx, kind, rows, cols, ff, more):
+    """The same of the result, gate and up of the gated feed-forward layer and its gradients."""
+    r = np.random.default_rng(ff)
+    new = lambda rows, cols, scale=1.0: matrix(scale * r.normal(size=(rows, cols)), kind, -cols % 8 + more)
+    out = lambda rows, cols: blank(rows, cols, kind, -cols % 8 + more)
+    x, dy, wg, wu, wd = new(rows, cols), new(rows, cols, 0.1), new(ff, cols, cols ** -0.5), new(ff, cols, cols ** -0.5), new(cols, ff, ff ** -0.5)
+    y, gate, up, grads = out(rows, cols), out(rows, ff), out(rows, ff), [out(rows, cols), out(ff, cols), out(ff, cols), out(cols, ff)]
+    ctx.reserve_network(rows, cols, ff, TYPES[kind])
+    ab.abcd_gated_ff(ctx, x, wg, wu, wd, "silu", y, gate, up)
+    ab.abcd_gated_ff_backward(ctx, dy, x, wg, wu, wd, "silu", gate, up, *grads)
+    ctx.sync()
+    args = f64(x), f64(wg), f64(wu), f64(wd), "silu"
+    for got, exact, bound in zip((y, gate, up), N.ff(*args), N.ff_bounds(*args, kind)):
+        close(got, exact, bound)
+    args = f64(dy), *args, f64(gate), f64(up)
+    for got, exact, bound in zip(grads, N.ff_grad(*args), N.ff_grad_bounds(*args, kind)):
+        close(got, exact, bound)
+    assert all(gaps_untouched(t) for t in (y, gate, up, *grads))
+
+
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("rows", [5, 300])
 def test_linear_gelu_far_below_zero(ctx, kind, rows):
     """gelu and its slope at -9 ... 3 are as exact as elsewhere relative to themselves, through unit matrices.
