@@ -216,12 +216,6 @@ def test_packed_refusals(lib, ctx):
                      (m, packed(8, 70, 2.0 + 16 / (1 << 20))), (m, packed(8, 70, 2, power_stride=2)), (matrix(8, 70, 2), q), (matrix(8, 70, 2.5), q),
                      (m, packed(8, 70, 0))):
             assert call(a, b) == BAD, (name, a, b)
-        # powers in the codes; between their rows
-        at = address(2)
-        for powers, apart in ((at, 3), (at + 69, 3), (at - 8 * 3 + 1, 3), (at + 7 * 256 + 60, 3), (at + 69, 256), (at + 256 - 2, 256), (at + 62, 512)):
-            assert call(m, packed(8, 70, 2, stride=256, powers=powers, power_stride=apart)) == BAD, (name, powers - at, apart)
-        for powers, apart in ((at + 70, 256), (at + 253, 256), (at - 8 * 3, 3), (at + 7 * 256 + 70, 3)):
-            assert call(m, packed(8, 70, 2, stride=256, powers=powers, power_stride=apart)) == ab.ABCD_ERR_CUDA      # all that is missing: a GPU
         assert call(matrix(0, 70), packed(0, 70, 2)) == OK
     call = Call(lib.abcd_gated_ff_backward_packed8, dy=matrix(20, 64), x=packed(20, 64, 1), wg=matrix(96, 64, 2), wu=matrix(96, 64, 3), wd=matrix(64, 96, 4),
                 act=ab.ABCD_SILU, gate=packed(20, 96, 5), up=packed(20, 96, 6), dx=matrix(20, 64, 7), dg=matrix(96, 64, 8), du=matrix(96, 64, 9), dd=matrix(64, 96, 10))
@@ -229,6 +223,19 @@ def test_packed_refusals(lib, ctx):
     for change in (dict(x=packed(20, 63, 1)), dict(gate=packed(19, 96, 5)), dict(up=None), dict(x=None), dict(act=3), dict(dx=matrix(20, 64, 1)),
                    dict(dd=matrix(64, 96, 5.5)), dict(dg=matrix(96, 64, 6)), dict(dy=None), dict(wd=matrix(64, 95, 4))):
         assert call(ctx, **change) == BAD, change
+
+
+def test_powers_in_the_codes_are_refused(lib, ctx):
+    """Those between the rows of codes are not."""
+    at, m = address(2), matrix(8, 70)
+    for name in ("abcd_pack8", "abcd_unpack8"):
+        def call(powers, apart):
+            q = packed(8, 70, 2, stride=256, powers=powers, power_stride=apart)
+            return getattr(lib, name)(ctx, *((ref(m), ref(q)) if name == "abcd_pack8" else (ref(q), ref(m))))
+        for powers, apart in ((at, 3), (at + 69, 3), (at - 8 * 3 + 1, 3), (at + 7 * 256 + 60, 3), (at + 69, 256), (at + 256 - 2, 256), (at + 62, 512)):
+            assert call(powers, apart) == BAD, (name, powers - at, apart)
+        for powers, apart in ((at + 70, 256), (at + 253, 256), (at - 8 * 3, 3), (at + 7 * 256 + 70, 3)):
+            assert call(powers, apart) == ab.ABCD_ERR_CUDA      # all that is missing: a GPU
 
 
 def test_matrices_in_8_bits_of_host_memory_are_refused(monkeypatch):
