@@ -454,7 +454,8 @@ abcd_status abcd_partition_split(const int dims[3], const double origin[3], doub
  * layers' operators, forward and backward.
  *
  * A matrix is row-major with consecutive columns and `stride` elements from row to row, aligned to
- * its element type; rows may be 0 and the data of a matrix without rows NULL.  All sums (products,
+ * its element type; rows may be 0 and the data of a matrix without rows NULL; what lies between the rows
+ * of a result stays as it is.  All sums (products,
  * statistics, reductions over the rows) are held in 32 bits, results are rounded once to the type of
  * their matrix, and every result is the same in every run (no atomic sums).  An output may not
  * overlap an input unless a call says so.  Like every call these are asynchronous on the context's
